@@ -15,7 +15,10 @@
  *   - a batched sweep of all of the above over many traces and settings,
  *   - and, beside the paper's signal: the time-averaged occupancy variant of
  *     Eq. 1's demand term, per-(model, SLO class) scoring through pair ids,
- *     and a scoring entry point that needs no workspace.
+ *     and a scoring entry point that needs no workspace,
+ *   - and what a replica of a served model runs on this GPU for each batch of new
+ *     tokens: norms and rotation of heads, a paged cache (quantised or not) and
+ *     attention over it.
  *
  * Conventions (every entry point):
  *   - Array arguments are DEVICE pointers owned by the caller, unless a field
@@ -59,7 +62,11 @@ typedef enum {
   TRE_ETIMEOUT = 5   /* reserved: a bounded device wait gave up (reported in diag.err) */
 } tre_status;
 
-typedef enum { TRE_F32 = 0, TRE_F64 = 1 } tre_dtype;
+/* Scoring is in TRE_F32 or TRE_F64; the other types are those of a served
+ * model's heads and of its cache (see tre_kv_cache). */
+typedef enum {
+  TRE_F32 = 0, TRE_F64 = 1, TRE_BF16 = 2, TRE_F16 = 3, TRE_E4M3 = 4, TRE_I8 = 5
+} tre_dtype;
 
 /* Region of a model in a window (Sec. III-B): Z < tau_crit critical, Z > tau_surplus
  * surplus, otherwise nominal. A window with no tokens and no running or waiting
@@ -488,6 +495,127 @@ tre_status tre_replay(const tre_grid* grid, const tre_latent* lat, const tre_pro
                       const tre_ctrl* ctrl, const int32_t* r0, const tre_replay_spec* spec,
                       const int32_t* slo_ttft_ms, const tre_replay_out* out, void* ws,
                       size_t* ws_bytes, tre_diag* diag, tre_stream stream);
+
+/* ---------------------------------------------------------------------------
+ * A replica's step. The telemetry that the entry points above score comes from
+ * replicas that serve models: what a prompt token costs them against a decode
+ * token (Eq. 1's w_p), and the service times that tre_replay takes, are set by
+ * the passes below on this GPU. A step norms and rotates the new tokens' queries
+ * and keys, writes keys and values into a paged cache, and attends over it:
+ *     tre_kv_append (or tre_qk_norm_rope without a cache), tre_chunk_attention;
+ * tre_kv_read takes tokens out of a cache (to move a request to another replica).
+ * No counterpart in the paper, whose replicas run an unmodified serving engine
+ * (Sec. V). Sums, softmax statistics and norms are held in 32 bits; every result
+ * is the same bit for bit when the same call is made again.
+ * diag may be NULL in these calls.
+ * ------------------------------------------------------------------------- */
+
+/* A paged cache: n_pages pages of `page` tokens of `heads` keys and values of
+ * `dim` elements (64 or 128). Keys and values have the same strides (in elements
+ * of dtype; the last axis is dense); base addresses and strides are multiples of
+ * 16 bytes. dtype: TRE_BF16 or TRE_F16 (the model's own type), or TRE_E4M3 or
+ * TRE_I8 with a float scale for each token and head: an element is code * scale.
+ * Scale strides are in floats, the same for keys and values. */
+typedef struct {
+  tre_dtype dtype;
+  int32_t n_pages, page, heads, dim;
+  void *k, *v;
+  int64_t page_stride, token_stride, head_stride;
+  float *k_scale, *v_scale;
+  int64_t scale_page_stride, scale_token_stride, scale_head_stride;
+} tre_kv_cache;
+
+/* The new tokens of a batch of sequences (device arrays): rows q_start[i] to
+ * q_start[i+1]-1 of n_rows are sequence i's newest tokens (q_start: n_seq + 1
+ * entries, not decreasing), and ctx_len[i] is its length with them, so that its
+ * row r stands at position ctx_len[i] - (q_start[i+1] - r). Position p lies in
+ * slot p % page of page pages[i * pages_row + p / page] of the cache. Entries
+ * outside [0, n_pages) hold nothing: such positions are not written (counted in
+ * diag.dropped_range), read as zeros (counted too) and seen by no row; the same
+ * goes for positions below zero or past max_pages pages. Rows of no sequence
+ * (before q_start[0], from q_start[n_seq] on) give zeros and are not counted.
+ * max_new, max_ctx: the longest sequence's new tokens and length, as far as the
+ * host knows them, 0 where it does not; they set how work is split, not what is
+ * computed. */
+typedef struct {
+  int32_t n_seq, n_rows, max_new, max_ctx, max_pages;
+  const int32_t* pages;
+  int64_t pages_row;
+  const int32_t *ctx_len, *q_start;
+} tre_kv_batch;
+
+/* Queries and keys of n_rows tokens: q [n_rows][q_heads][dim] and
+ * k [n_rows][k_heads][dim] of dtype (TRE_BF16, TRE_F16, or TRE_F32 without a
+ * cache), strides in elements, base addresses and strides multiples of 16 bytes,
+ * dim 64 or 128; either may have no heads. Each head is divided by
+ * sqrt(mean of squares + eps) and multiplied by its weight (dim elements of
+ * weight_dtype: TRE_F32 or dtype; NULL: neither), then its first `rot` elements
+ * (a multiple of 16) are turned by the row's position: cos_sin is
+ * [n_pos][cos_sin_row] floats, rot/2 cosines then rot/2 sines (NULL: not
+ * turned). Pairs are (i, i + rot/2), or (2i, 2i + 1) when interleaved. Rows at a
+ * position outside [0, n_pos) give zeros and are counted in diag.dropped_range.
+ * Outputs may be the inputs themselves (with the same strides). */
+typedef struct {
+  tre_dtype dtype;
+  int32_t n_rows, q_heads, k_heads, dim;
+  const void *q, *k;
+  int64_t q_row, q_head, k_row, k_head;
+  void *q_out, *k_out;
+  int64_t q_out_row, q_out_head, k_out_row, k_out_head;
+  tre_dtype weight_dtype;
+  const void *q_weight, *k_weight;
+  float eps;
+  const float* cos_sin;
+  int64_t cos_sin_row;
+  int32_t n_pos, rot, interleaved;
+} tre_heads;
+
+/* tre_qk_norm_rope -- norms and rotation of queries and keys in one pass, without
+ * a cache. positions: device int32[n_rows] (may be NULL without cos_sin). */
+tre_status tre_qk_norm_rope(const tre_heads* heads, const int32_t* positions, tre_diag* diag,
+                            tre_stream stream);
+
+/* tre_kv_append -- the new tokens' keys and values into the cache, keys (and the
+ * queries, to q_out) normed and rotated at their own positions on the way; k_out
+ * is not used. v: [n_rows][cache heads][dim], strides in elements. A cache of
+ * codes gets scale = max|x| / 448 (e4m3) or / 127 (int8) of the 32-bit values of
+ * each token and head, and x / scale rounded to nearest even; a row with a value
+ * that is infinite or no number reads back as NaN. */
+tre_status tre_kv_append(const tre_kv_cache* cache, const tre_kv_batch* batch,
+                         const tre_heads* heads, const void* v, int64_t v_row, int64_t v_head,
+                         tre_diag* diag, tre_stream stream);
+
+/* tre_kv_read -- the batch's rows (for whole contexts: q_start the sums of
+ * ctx_len) out of the cache as [n_rows][heads][dim] of out_dtype (TRE_F32,
+ * TRE_BF16, TRE_F16); strides in elements, the same for both outputs. */
+tre_status tre_kv_read(const tre_kv_cache* cache, const tre_kv_batch* batch, tre_dtype out_dtype,
+                       void* k_out, void* v_out, int64_t out_row, int64_t out_head,
+                       tre_diag* diag, tre_stream stream);
+
+/* Queries of tre_chunk_attention: [n_rows][heads][dim] of dtype (TRE_BF16 or
+ * TRE_F16; the cache is of the same type or of codes), heads a multiple of the
+ * cache's: query head h reads cache head h / (heads / cache heads). Strides in
+ * elements, multiples of 8; addresses multiples of 16 bytes. scale > 0. window:
+ * a row sees its last `window` positions only (0: all). lse: NULL, or float
+ * [n_rows][heads], the logarithm of each row's sum of exp(scale * q.k). */
+typedef struct {
+  tre_dtype dtype;
+  int32_t heads, window;
+  float scale;
+  const void* q;
+  int64_t q_row, q_head;
+  void* out;
+  int64_t out_row, out_head;
+  float* lse;
+} tre_attend;
+
+/* tre_chunk_attention -- each new token's attention over its sequence up to and
+ * including itself; the batch's rows are in the cache already. A row that sees no
+ * position gives zeros and lse = -inf. Values at positions that a row does not
+ * see do not reach it, whatever they hold. */
+tre_status tre_chunk_attention(const tre_kv_cache* cache, const tre_kv_batch* batch,
+                               const tre_attend* at, void* ws, size_t* ws_bytes,
+                               tre_stream stream);
 
 /* Kernel-phase tracing (host side, not thread safe). While enabled, every
  * kernel phase an entry point enqueues is bracketed by a pair of CUDA events

@@ -153,6 +153,7 @@ def load(build_if_missing: bool = True):
                                C.POINTER(Ctrl), P, C.POINTER(ReplaySpec), P,
                                C.POINTER(ReplayOut), P, C.POINTER(C.c_size_t), P, P]
     lib.tre_replay.restype = C.c_int
+    replica.declare(lib)
     lib.tre_status_str.argtypes = [C.c_int]
     lib.tre_status_str.restype = C.c_char_p
     _lib = lib
@@ -828,3 +829,8 @@ def tre_replay(latent, M, window_ms, K, profile, budget, r0, r_min, footprint, *
     plan = ReplayPlan(latent, M, window_ms, K, profile, budget, r0, r_min, footprint, **kw)
     out = plan.run()
     return out, plan.moves(), plan.diag
+
+
+from . import replica  # noqa: E402  (it uses the helpers above)
+from .replica import (KvBatch, KvCache, tre_chunk_attention, tre_kv_append,  # noqa: E402,F401
+                      tre_kv_read, tre_qk_norm_rope)

@@ -1,0 +1,594 @@
+// Attention of new tokens over a paged cache.
+//
+//   out_r = sum_j softmax_j(scale * q_r . k_j) v_j  over the positions j <= pos(r)
+//   (j > pos(r) - window with a window) whose page is mapped
+//
+// in one pass over the keys and values: a running maximum m, the sum l of
+// exp2(s - m), and the weighted sum of values, all in 32 bits.
+//
+// k_attend takes 16 rows at a time (tokens x query heads of one cache head: the
+// heads that share a key read it once) against a part of the context. Its four
+// warps each run their own stream of 16-token tiles through a ring of asynchronous
+// 16-byte copies of their own, so no warp waits for another before the end, when
+// their four (m, l, O) are joined. Products are m16n8k16 matrix instructions: with
+// one or a few new tokens the call is bound by the cache's bytes, at which rate 16
+// rows keep those units under a third busy. Positions within a row of keys and
+// columns of values are taken in the order in which a lane's 16-byte reads deliver
+// them, which a sum over positions does not see.
+#include <algorithm>
+
+#include "attend.cuh"
+#include "internal.h"
+
+namespace tre {
+namespace {
+
+constexpr int kWarps = 4, kTile = 16;
+
+template <class T> struct Mma;
+template <> struct Mma<__nv_bfloat16> {
+  static __device__ __forceinline__ void run(float* d, const uint32_t* a, uint32_t b0,
+                                             uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+        "{%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  }
+};
+template <> struct Mma<__half> {
+  static __device__ __forceinline__ void run(float* d, const uint32_t* a, uint32_t b0,
+                                             uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+        "{%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  }
+};
+
+// Two 8-bit codes (the low 16 bits of w) as a pair of T. Both kinds of code are
+// exact in either type.
+template <class T, Code CODE> __device__ __forceinline__ uint32_t pair_of(uint32_t w) {
+  if constexpr (CODE == Code::kE4m3) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)w, __NV_E4M3);
+    const __half2 v = *reinterpret_cast<const __half2*>(&h);
+    if constexpr (sizeof(T) == 2 && std::is_same<T, __half>::value)
+      return *reinterpret_cast<const uint32_t*>(&v);
+    const float2 f = __half22float2(v);
+    return pack<T>(f.x, f.y);
+  } else {
+    const float lo = (float)(int8_t)w, hi = (float)(int8_t)(w >> 8);
+    return pack<T>(lo, hi);
+  }
+}
+
+template <int N> __device__ __forceinline__ void wait_copies() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+template <Code CODE, int DIM> struct Shape {
+  static constexpr int CB = CODE == Code::kHalf ? 2 : 1;
+  static constexpr int ROW = DIM * CB;                  // bytes of one key
+  static constexpr int CPR = ROW / 16;                  // 16-byte pieces of one key
+  static constexpr int SCALES = CODE == Code::kHalf ? 0 : 2 * kTile * 4;
+  static constexpr int STAGE = 2 * kTile * ROW + SCALES + 128;
+  static constexpr int STAGES = ROW == 256 ? 3 : ROW == 128 ? 6 : 8;
+  static constexpr int SMEM_RING = kWarps * STAGES * STAGE;
+  static constexpr int SMEM_JOIN = kWarps * kTile * (DIM + 4) * 4;
+  static constexpr int SMEM = SMEM_RING > SMEM_JOIN ? SMEM_RING : SMEM_JOIN;
+  // Place of 16-byte piece u = token * CPR + piece: eight neighbours of a read
+  // (two tokens x four pieces of keys, four even or odd tokens x two pieces of
+  // values) fall on different banks.
+  static __device__ __forceinline__ int place(int tok, int piece) {
+    const int u = tok * CPR + piece;
+    if constexpr (CPR == 4) return u ^ (((tok >> 1) & 3) << 1);
+    return u ^ ((((tok >> 1) & 3) << 1) ^ ((tok & 1) << 2));
+  }
+};
+
+template <class T, Code CODE, int DIM>
+__global__ void __launch_bounds__(kWarps * 32, 2)
+k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
+  using S = Shape<CODE, DIM>;
+  using PV = typename std::conditional<CODE == Code::kHalf, T, __nv_bfloat16>::type;
+  constexpr int EPT = 16 / S::CB, SPB = EPT / 4, BLOCKS = DIM / (4 * EPT);
+  extern __shared__ __align__(128) uint8_t sm[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int g = lane >> 2, cc = lane & 3;
+  const int kvh = blockIdx.x % c.heads;
+  int rest = blockIdx.x / c.heads;
+  const int sp = rest % a.n_split;
+  rest /= a.n_split;
+  const int rt0 = rest % a.row_tiles, i = rest / a.row_tiles;
+  if (blockIdx.x == 0) loose_rows<T, DIM>(a, b);
+  const Seq sq = seq_of(b, i);
+  const int rows = sq.n * a.group, base = sq.ctx - sq.n;
+
+  for (int rt = rt0; rt * kTile < rows; rt += a.row_tiles) {
+    const int r_first = rt * kTile, r_last = min(r_first + kTile, rows) - 1;
+    const int t_first = a.by_group.div(r_first);
+    int lo, hi;
+    range_of(sq, c, b, a.window, t_first, a.by_group.div(r_last), lo, hi);
+    part_of<kTile * kWarps>(a, sp, lo, hi);
+    const int n_tiles = hi > lo ? (hi - lo + kTile - 1) / kTile : 0;
+    const int mine = n_tiles > warp ? (n_tiles - warp + kWarps - 1) / kWarps : 0;
+
+    // this lane's two rows
+    int pos[2];
+    const T* qp[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int r = r_first + g + 8 * x;
+      const int t = a.by_group.div(r);
+      pos[x] = base + t;
+      qp[x] = r < rows ? reinterpret_cast<const T*>(a.q) + (int64_t)(sq.start + t) * a.q_row +
+                             (int64_t)(kvh * a.group + (r - t * a.group)) * a.q_head
+                       : nullptr;
+    }
+
+    uint8_t* ring = sm + warp * (S::STAGES * S::STAGE);
+    const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
+    // the page of token (lane & 15) of the next tile to copy
+    int next_tile = 0, page = -1, slot = 0;
+    auto look = [&]() {
+      const int j = lo + (warp + next_tile * kWarps) * kTile + (lane & 15);
+      page = next_tile < mine && j < hi ? page_of(c, b, i, j, slot) : -1;
+    };
+    auto issue = [&]() {
+      if (next_tile < mine) {
+        const int st = next_tile % S::STAGES;
+        const uint32_t dst = ring_s + st * S::STAGE;
+        const bool there = page >= 0;
+        const int64_t off =
+            there ? (page * c.s_page + slot * c.s_token + kvh * c.s_head) * S::CB : 0;
+        const unsigned held = __ballot_sync(0xffffffffu, there);
+#pragma unroll
+        for (int it = 0; it < S::CPR / 2; ++it) {
+          const int u = it * 32 + lane, tok = u / S::CPR, piece = u % S::CPR;
+          const int64_t o = __shfl_sync(0xffffffffu, off, tok) + piece * 16;
+          const int n = held >> tok & 1 ? 16 : 0;
+          const uint32_t at = dst + S::place(tok, piece) * 16;
+          const uint8_t *pk = n ? c.k + o : c.k, *pv = n ? c.v + o : c.v;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(pk), "r"(n)
+                       : "memory");
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + kTile * S::ROW),
+                       "l"(pv), "r"(n)
+                       : "memory");
+        }
+        if (S::SCALES) {
+          const float* sc = lane < 16 ? c.k_scale : c.v_scale;
+          const float* p = there ? sc + page * c.c_page + slot * c.c_token + kvh * c.c_head : sc;
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst + 2 * kTile * S::ROW +
+                                                                            lane * 4),
+                       "l"(p), "r"(there ? 4 : 0)
+                       : "memory");
+        }
+        if (lane == 0)
+          *reinterpret_cast<uint32_t*>(ring + st * S::STAGE + 2 * kTile * S::ROW + S::SCALES) = held;
+        ++next_tile;
+        look();
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+
+    look();
+#pragma unroll 1
+    for (int k = 0; k < S::STAGES - 1; ++k) issue();
+
+    uint32_t qf[DIM / 16][4];
+#pragma unroll
+    for (int s = 0; s < DIM / 16; ++s) {
+      const int e = (s / SPB * 4 + cc) * EPT + (s % SPB) * 4;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        uint2 v = make_uint2(0, 0);
+        if (qp[x]) v = *reinterpret_cast<const uint2*>(qp[x] + e);
+        qf[s][x] = v.x;
+        qf[s][x + 2] = v.y;
+      }
+    }
+
+    float o[DIM / 8][4];
+#pragma unroll
+    for (int n = 0; n < DIM / 8; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+
+#pragma unroll 1
+    for (int k = 0; k < mine; ++k) {
+      wait_copies<S::STAGES - 2>();
+      __syncwarp();
+      const uint8_t* st = ring + (k % S::STAGES) * S::STAGE;
+      const uint4* kt = reinterpret_cast<const uint4*>(st);
+      const uint4* vt = reinterpret_cast<const uint4*>(st + kTile * S::ROW);
+      const float* sc = reinterpret_cast<const float*>(st + 2 * kTile * S::ROW);
+      const uint32_t held =
+          *reinterpret_cast<const uint32_t*>(st + 2 * kTile * S::ROW + S::SCALES) & 0xffffu;
+
+      float s[2][4];
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
+#pragma unroll
+      for (int bl = 0; bl < BLOCKS; ++bl)
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+          const uint4 v = kt[S::place(g + 8 * nt, 4 * bl + cc)];
+          if constexpr (CODE == Code::kHalf) {
+            Mma<T>::run(s[nt], qf[2 * bl], v.x, v.y);
+            Mma<T>::run(s[nt], qf[2 * bl + 1], v.z, v.w);
+          } else {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              Mma<T>::run(s[nt], qf[4 * bl + x], pair_of<T, CODE>(w[x]),
+                          pair_of<T, CODE>(w[x] >> 16));
+          }
+        }
+
+      const int j0 = lo + (warp + k * kWarps) * kTile;
+      float vs[2][2];
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int tok = nt * 8 + 2 * cc + x;
+          const float ks = S::SCALES ? mul_rn(sc[tok], a.scale2) : a.scale2;
+          vs[nt][x] = S::SCALES ? sc[kTile + tok] : 1.f;
+          s[nt][x] = mul_rn(s[nt][x], ks);
+          s[nt][x + 2] = mul_rn(s[nt][x + 2], ks);
+        }
+      const int p_first = base + t_first;
+      const bool whole = held == 0xffffu && j0 + kTile - 1 <= p_first &&
+                         (a.window == 0 || j0 > base + a.by_group.div(r_last) - a.window);
+      if (!whole) {
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int tok = nt * 8 + 2 * cc + (e & 1), j = j0 + tok, p = pos[e >> 1];
+            const bool vis = (held >> tok & 1) && j <= p && (a.window == 0 || j > p - a.window);
+            if (!vis) s[nt][e] = -INFINITY;
+          }
+      }
+
+      float corr[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        float t = fmaxf(fmaxf(s[0][2 * x], s[0][2 * x + 1]), fmaxf(s[1][2 * x], s[1][2 * x + 1]));
+        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
+        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
+        const float mn = fmaxf(m[x], t), use = mn == -INFINITY ? 0.f : mn;
+        corr[x] = exp2_fast(m[x] - use);
+        m[x] = mn;
+        float sum = 0.f;
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float p = exp2_fast(s[nt][2 * x + e] - use);
+            sum += p;
+            s[nt][2 * x + e] = p;
+          }
+        l[x] = __fmaf_rn(l[x], corr[x], sum);
+      }
+      if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
+#pragma unroll
+        for (int n = 0; n < DIM / 8; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[n][e] *= corr[e >> 1];
+      }
+      uint32_t pf[4];
+      if constexpr (CODE == Code::kHalf) {
+        pf[0] = pack<PV>(s[0][0], s[0][1]);
+        pf[1] = pack<PV>(s[0][2], s[0][3]);
+        pf[2] = pack<PV>(s[1][0], s[1][1]);
+        pf[3] = pack<PV>(s[1][2], s[1][3]);
+      } else {
+        // a masked position's scale may be anything: its weight stays zero
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const float u = s[nt][2 * x], w = s[nt][2 * x + 1];
+            pf[2 * nt + x] = pack<PV>(u == 0.f ? 0.f : u * vs[nt][0], w == 0.f ? 0.f : w * vs[nt][1]);
+          }
+      }
+      // values: columns of n-tile jj stand 8 (16) elements apart, as a lane's read
+      // of neighbouring elements delivers them
+      if constexpr (CODE == Code::kHalf) {
+#pragma unroll
+        for (int set = 0; set < DIM / 64; ++set) {
+          uint4 v[4];
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            v[x] = vt[S::place(2 * cc + (x & 1) + (x >> 1) * 8, 8 * set + g)];
+          const uint32_t w[4][4] = {{v[0].x, v[0].y, v[0].z, v[0].w},
+                                    {v[1].x, v[1].y, v[1].z, v[1].w},
+                                    {v[2].x, v[2].y, v[2].z, v[2].w},
+                                    {v[3].x, v[3].y, v[3].z, v[3].w}};
+#pragma unroll
+          for (int jj = 0; jj < 8; ++jj) {
+            const uint32_t sel = jj & 1 ? 0x7632 : 0x5410;
+            Mma<PV>::run(o[set * 8 + jj], pf, __byte_perm(w[0][jj >> 1], w[1][jj >> 1], sel),
+                         __byte_perm(w[2][jj >> 1], w[3][jj >> 1], sel));
+          }
+        }
+      } else {
+        constexpr int W = DIM / 32;       // words of codes a lane reads of a token
+        uint32_t w[4][W];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int tok = 2 * cc + (x & 1) + (x >> 1) * 8;
+          if constexpr (W == 4) {
+            const uint4 v = vt[S::place(tok, g)];
+            w[x][0] = v.x;
+            w[x][1] = v.y;
+            w[x][2] = v.z;
+            w[x][3] = v.w;
+          } else {
+            const uint2 v = reinterpret_cast<const uint2*>(vt + S::place(tok, g >> 1))[g & 1];
+            w[x][0] = v.x;
+            w[x][1] = v.y;
+          }
+        }
+#pragma unroll
+        for (int y = 0; y < W; ++y)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            const uint32_t sel = hf ? 0x7362 : 0x5140;
+            const uint32_t u = __byte_perm(w[0][y], w[1][y], sel);
+            const uint32_t z = __byte_perm(w[2][y], w[3][y], sel);
+            Mma<PV>::run(o[4 * y + 2 * hf], pf, pair_of<PV, CODE>(u), pair_of<PV, CODE>(z));
+            Mma<PV>::run(o[4 * y + 2 * hf + 1], pf, pair_of<PV, CODE>(u >> 16),
+                         pair_of<PV, CODE>(z >> 16));
+          }
+      }
+      __syncwarp();
+      issue();
+    }
+    wait_copies<0>();
+
+    // join the four warps
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      l[x] += __shfl_xor_sync(0xffffffffu, l[x], 1);
+      l[x] += __shfl_xor_sync(0xffffffffu, l[x], 2);
+    }
+    __shared__ float w_m[kWarps][kTile], w_l[kWarps][kTile];
+    __shared__ unsigned again;
+    if (cc == 0) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        w_m[warp][g + 8 * x] = m[x];
+        w_l[warp][g + 8 * x] = l[x];
+      }
+    }
+    if (threadIdx.x == 0) again = 0;
+    __syncthreads();
+    constexpr int PITCH = DIM + 4;
+    float* os = reinterpret_cast<float*>(sm);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int r = g + 8 * x;
+      float top = w_m[0][r];
+#pragma unroll
+      for (int w = 1; w < kWarps; ++w) top = fmaxf(top, w_m[w][r]);
+      const float f = m[x] == -INFINITY ? 0.f : exp2_fast(m[x] - top);
+      float* dst = os + (warp * kTile + r) * PITCH;
+#pragma unroll
+      for (int n = 0; n < DIM / 8; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          // column of n-tile n that this lane holds: see the reads above
+          int d;
+          if constexpr (CODE == Code::kHalf) d = (n / 8) * 64 + 8 * (2 * cc + e) + n % 8;
+          else d = (DIM / 8) * (2 * cc + e) + n;
+          // a warp that saw nothing has nothing to add, whatever it multiplied
+          dst[d] = f == 0.f ? 0.f : o[n][2 * x + e] * f;
+        }
+    }
+    __syncthreads();
+    constexpr int LPR = 32, EL = DIM / LPR;
+    for (int r = warp; r < kTile; r += kWarps) {
+      const int rr = r_first + r;
+      if (rr >= rows) break;
+      float top = w_m[0][r];
+#pragma unroll
+      for (int w = 1; w < kWarps; ++w) top = fmaxf(top, w_m[w][r]);
+      float sum = 0.f, x[EL];
+#pragma unroll
+      for (int e = 0; e < EL; ++e) x[e] = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = w_m[w][r] == -INFINITY ? 0.f : exp2_fast(w_m[w][r] - top);
+        sum = __fmaf_rn(w_l[w][r], f, sum);
+#pragma unroll
+        for (int e = 0; e < EL; ++e) x[e] += os[(w * kTile + r) * PITCH + lane * EL + e];
+      }
+      bool odd = false;
+#pragma unroll
+      for (int e = 0; e < EL; ++e) odd |= !(fabsf(x[e]) < INFINITY);
+      const int t = a.by_group.div(rr), h = kvh * a.group + (rr - t * a.group);
+      const int64_t row = (int64_t)(sq.start + t);
+      if (__any_sync(0xffffffffu, odd) && top > -INFINITY)
+        row_again<T, CODE, DIM>(a, b, c, i, kvh,
+                                reinterpret_cast<const T*>(a.q) + row * a.q_row + h * a.q_head,
+                                base + t, lo, hi, top, x);
+      if (a.n_split > 1) {
+        const int64_t at = ((int64_t)sp * b.n_rows + row) * a.heads + h;
+        if (lane == 0) {
+          a.part_ml[2 * at] = top;
+          a.part_ml[2 * at + 1] = sum;
+        }
+        float* p = a.part_o + at * DIM + lane * EL;
+        if (sum > 0.f || sum != sum) {
+          if constexpr (EL == 4) *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+          else *reinterpret_cast<float2*>(p) = make_float2(x[0], x[1]);
+        }
+      } else {
+        const float by = top == -INFINITY ? 0.f : div_rn(1.f, sum);
+        T* p = reinterpret_cast<T*>(a.out) + row * a.o_row + h * a.o_head + lane * EL;
+#pragma unroll
+        for (int e = 0; e < EL; e += 2)
+          *reinterpret_cast<uint32_t*>(p + e) = pack<T>(x[e] * by, x[e + 1] * by);
+        if (a.lse && lane == 0)
+          a.lse[row * a.heads + h] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * kLn2;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Joins the parts of each row: one warp a (row, head).
+template <class T, int DIM>
+__global__ void __launch_bounds__(128) k_join(AttendArgs a, int64_t rows_heads) {
+  const int lane = threadIdx.x & 31;
+  const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (w >= rows_heads) return;
+  constexpr int EL = DIM / 32;
+  float top = -INFINITY;
+  for (int sp = lane; sp < a.n_split; sp += 32)
+    top = fmaxf(top, a.part_ml[2 * (sp * rows_heads + w)]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  float sum = 0.f, x[EL];
+#pragma unroll
+  for (int e = 0; e < EL; ++e) x[e] = 0.f;
+  if (top > -INFINITY) {
+#pragma unroll 4
+    for (int sp = 0; sp < a.n_split; ++sp) {
+      const int64_t at = sp * rows_heads + w;
+      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * at);
+      if (ml.x == -INFINITY) continue;
+      const float f = exp2_fast(ml.x - top);
+      sum = __fmaf_rn(ml.y, f, sum);
+      const float* p = a.part_o + at * DIM + lane * EL;
+      float y[EL];
+      if constexpr (EL == 4) {
+        const float4 v = *reinterpret_cast<const float4*>(p);
+        y[0] = v.x; y[1] = v.y; y[2] = v.z; y[3] = v.w;
+      } else {
+        const float2 v = *reinterpret_cast<const float2*>(p);
+        y[0] = v.x; y[1] = v.y;
+      }
+#pragma unroll
+      for (int e = 0; e < EL; ++e) x[e] = __fmaf_rn(y[e], f, x[e]);
+    }
+  }
+  const int64_t t = w / a.heads, h = w - t * a.heads;
+  const float by = top == -INFINITY ? 0.f : div_rn(1.f, sum);
+  T* p = reinterpret_cast<T*>(a.out) + t * a.o_row + h * a.o_head + lane * EL;
+#pragma unroll
+  for (int e = 0; e < EL; e += 2)
+    *reinterpret_cast<uint32_t*>(p + e) = pack<T>(x[e] * by, x[e + 1] * by);
+  if (a.lse && lane == 0)
+    a.lse[w] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * kLn2;
+}
+
+template <class T, Code CODE, int DIM>
+cudaError_t launch_typed(const AttendArgs& a, const BatchArgs& b, const CacheArgs& c,
+                         cudaStream_t s) {
+  using S = Shape<CODE, DIM>;
+  const void* fn = (const void*)k_attend<T, CODE, DIM>;
+  cudaError_t e = func_smem_once(fn, S::SMEM, true);
+  if (e) return e;
+  const int64_t blocks = (int64_t)c.heads * a.n_split * a.row_tiles * b.n_seq;
+  if (blocks > 2147483647) return cudaErrorInvalidValue;
+  k_attend<T, CODE, DIM><<<(unsigned)blocks, kWarps * 32, S::SMEM, s>>>(a, b, c);
+  if (a.n_split > 1) {
+    const int64_t rh = (int64_t)b.n_rows * a.heads;
+    k_join<T, DIM><<<(unsigned)((rh + 3) / 4), 128, 0, s>>>(a, rh);
+  }
+  return cudaGetLastError();
+}
+
+template <class T, Code CODE>
+cudaError_t launch_dim(int dim, const AttendArgs& a, const BatchArgs& b, const CacheArgs& c,
+                       cudaStream_t s) {
+  return dim == 64 ? launch_typed<T, CODE, 64>(a, b, c, s) : launch_typed<T, CODE, 128>(a, b, c, s);
+}
+
+template <class T>
+cudaError_t launch_code(int code, int dim, const AttendArgs& a, const BatchArgs& b,
+                        const CacheArgs& c, cudaStream_t s) {
+  if (code == TRE_E4M3) return launch_dim<T, Code::kE4m3>(dim, a, b, c, s);
+  if (code == TRE_I8) return launch_dim<T, Code::kI8>(dim, a, b, c, s);
+  return launch_dim<T, Code::kHalf>(dim, a, b, c, s);
+}
+
+// Parts of a context: enough blocks to fill the GPU a few times over, none
+// shorter than 256 tokens (a part costs a block's start and its share of the
+// join, about what 256 tokens of keys and values cost to read).
+void choose_parts(AttendArgs& a, const tre_kv_batch* b, int heads, int page) {
+  const int max_new = b->max_new > 0 ? b->max_new : b->n_rows;
+  const int64_t rows = (int64_t)std::max(max_new, 1) * a.group;
+  a.row_tiles = (int)std::min<int64_t>((rows + kTile - 1) / kTile, 1 << 20);
+  int64_t len = b->max_ctx > 0 ? b->max_ctx : (int64_t)b->max_pages * page;
+  if (a.window > 0) len = std::min<int64_t>(len, (int64_t)a.window + max_new + 15);
+  const int64_t units = std::max<int64_t>(1, (int64_t)b->n_seq * heads * a.row_tiles);
+  const int64_t want = std::max<int64_t>(1, ((int64_t)device_sm_count() * 2 * 4 + units - 1) / units);
+  const int64_t most = std::max<int64_t>(1, len / 256);
+  a.n_split = (int)std::min<int64_t>({want, most, 256});
+  const int64_t part = (len + a.n_split - 1) / a.n_split;
+  a.split = (int)std::max<int64_t>(kTile * kWarps, part);
+}
+
+}  // namespace
+}  // namespace tre
+
+using namespace tre;
+
+extern "C" tre_status tre_chunk_attention(const tre_kv_cache* cache, const tre_kv_batch* batch,
+                                          const tre_attend* at, void* ws, size_t* ws_bytes,
+                                          tre_stream stream) {
+  AttendArgs a{};
+  BatchArgs b;
+  CacheArgs c;
+  if (!at || !ws_bytes || !batch_args(batch, b) || !cache_args(cache, c)) return TRE_EINVAL;
+  if (at->dtype != TRE_BF16 && at->dtype != TRE_F16) return TRE_EINVAL;
+  if (cache->dtype != at->dtype && cache->dtype != TRE_E4M3 && cache->dtype != TRE_I8)
+    return TRE_EINVAL;
+  if (at->heads < 1 || at->heads % cache->heads || at->heads > 65536 || at->window < 0)
+    return TRE_EINVAL;
+  if (!(at->scale > 0.f) || !(at->scale < 3e38f)) return TRE_EINVAL;
+  const int64_t strides[4] = {at->q_row, at->q_head, at->out_row, at->out_head};
+  for (int64_t x : strides)
+    if (x % 8) return TRE_EINVAL;
+  if (((uintptr_t)at->q & 15) || ((uintptr_t)at->out & 15)) return TRE_EINVAL;
+  a.heads = at->heads;
+  a.group = at->heads / cache->heads;
+  if (b.n_rows > 0 && (int64_t)b.n_rows * a.group > 2147483647ll / 2) return TRE_EINVAL;
+  a.by_group = FastDiv31((uint32_t)a.group);
+  a.window = at->window;
+  if (b.n_seq > 0) choose_parts(a, batch, c.heads, c.page);
+  Arena arena(ws);
+  if (a.n_split > 1) {
+    const size_t rh = (size_t)b.n_rows * a.heads;
+    a.part_ml = arena.take<float>(2 * rh * a.n_split);
+    a.part_o = arena.take<float>(rh * a.n_split * cache->dim);
+  }
+  if (!ws) {
+    *ws_bytes = arena.off;
+    return TRE_OK;
+  }
+  if (*ws_bytes < arena.off) return TRE_ENOMEM;
+  if (b.n_rows == 0) return TRE_OK;
+  if (b.n_seq == 0 || !at->q || !at->out) return TRE_EINVAL;
+  a.q = static_cast<const uint8_t*>(at->q);
+  a.out = static_cast<uint8_t*>(at->out);
+  a.lse = at->lse;
+  a.q_row = at->q_row;
+  a.q_head = at->q_head;
+  a.o_row = at->out_row;
+  a.o_head = at->out_head;
+  a.scale2 = (float)((double)at->scale * 1.4426950408889634);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const cudaError_t e = at->dtype == TRE_BF16
+                            ? launch_code<__nv_bfloat16>(cache->dtype, cache->dim, a, b, c, s)
+                            : launch_code<__half>(cache->dtype, cache->dim, a, b, c, s);
+  return e == cudaSuccess ? TRE_OK : TRE_ECUDA;
+}

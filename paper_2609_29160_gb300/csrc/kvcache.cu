@@ -1,0 +1,545 @@
+// Rows of heads on their way into a paged cache and out of it.
+//
+// k_heads: y = x * w / sqrt(mean x^2 + eps), then the rotation of the row's
+// position, then either a rounding to the input's type or a cache code: scale
+// amax|y| / Q (Q = 448 for e4m3, 127 for int8), code = round(y / scale). A row of
+// 64 or 128 elements is read once, 16 bytes a lane, stays in registers, and its
+// sums and maxima are shuffles among its lanes; everything is 32-bit until the one
+// rounding at the end, and the division is the exact one, so codes do not depend on
+// how a row is reached. Bound by HBM when there are many rows, by the chain
+// q_start -> lengths -> page -> store when there are few.
+//
+// k_read: codes (and scales) of whole tokens back to rows of a model's type.
+#include <algorithm>
+
+#include "internal.h"
+#include "kvcache.cuh"
+
+namespace tre {
+namespace {
+
+constexpr int kThreads = 256;
+
+struct HeadsArgs {
+  const uint8_t* in[3];           // q, k, v
+  int64_t row[3], head[3];        // bytes
+  uint8_t* out[2];
+  int64_t orow[2], ohead[2];      // bytes
+  const void* weight[2];
+  const float* cos_sin;
+  int64_t cs_row;
+  const int32_t* positions;       // without a cache
+  int32_t heads[3];
+  int32_t n_rows, n_pos, rot;
+  float eps;
+  bool interleaved, weight_f32;
+};
+
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+template <int W> __device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int o = W / 2; o > 0; o >>= 1) v = add_rn(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+template <int W> __device__ __forceinline__ float group_max(float v) {
+#pragma unroll
+  for (int o = W / 2; o > 0; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+
+// One warp takes NIT iterations of 32 / LPR rows of one token: the token's place
+// and its cosines and sines are fetched once for all of them.
+template <class T, Code CODE, int D, int NIT>
+__global__ void __launch_bounds__(kThreads)
+k_heads(HeadsArgs a, BatchArgs b, CacheArgs c, int groups, tre_diag* diag) {
+  constexpr int N = Vec<T>::N, LPR = D / N, RPW = 32 / LPR;
+  const int lane = threadIdx.x & 31, sub = lane / LPR, e0 = (lane % LPR) * N;
+  const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+  const int64_t t64 = w / groups;
+  if (t64 >= a.n_rows) return;
+  const int t = (int)t64, grp = (int)(w - t64 * groups);
+  const int n_heads = a.heads[0] + a.heads[1] + a.heads[2];
+
+  // the rows first: they depend on nothing
+  uint4 raw[NIT];
+  int kind[NIT], head[NIT];
+#pragma unroll
+  for (int it = 0; it < NIT; ++it) {
+    int h = (grp * NIT + it) * RPW + sub;
+    kind[it] = -1;
+    raw[it] = make_uint4(0, 0, 0, 0);
+    if (h < n_heads) {
+      int s = 0;
+      if (h >= a.heads[0]) { h -= a.heads[0]; s = 1; }
+      if (s == 1 && h >= a.heads[1]) { h -= a.heads[1]; s = 2; }
+      kind[it] = s;
+      head[it] = h;
+      raw[it] = *reinterpret_cast<const uint4*>(a.in[s] + t * a.row[s] + h * a.head[s] +
+                                                e0 * (int)sizeof(T));
+    }
+  }
+
+  // where the token stands
+  int pos, page = 0, slot = 0;
+  bool ok = true, counted = true;
+  if (CODE == Code::kNone) {
+    pos = a.positions ? a.positions[t] : 0;
+  } else {
+    const int i = find_seq(b, t);
+    if (i < 0) {
+      ok = counted = false;
+      pos = 0;
+    } else {
+      const int end = b.q_start[i + 1];
+      if (t >= end) {
+        ok = counted = false;
+        pos = 0;
+      } else {
+        pos = b.ctx_len[i] - (end - t);
+        page = page_of(c, b, i, pos, slot);
+        ok = page >= 0;
+      }
+    }
+  }
+  if (a.cos_sin && (pos < 0 || pos >= a.n_pos)) ok = false;
+  if (!ok && counted && diag && grp == 0 && lane == 0)
+    atomicAdd((unsigned long long*)&diag->dropped_range, 1ull);
+
+  float cs[N], sn[N];
+  const int half = a.rot >> 1;
+  const bool turned = a.cos_sin && e0 < a.rot;
+  const int mate = a.interleaved || !turned ? lane : lane + (e0 < half ? half : -half) / N;
+  if (turned && ok) {
+    const float* p = a.cos_sin + pos * a.cs_row;
+    if (a.interleaved) {
+#pragma unroll
+      for (int e = 0; e < N; e += 2) {
+        cs[e] = cs[e + 1] = p[(e0 + e) >> 1];
+        sn[e + 1] = p[half + ((e0 + e) >> 1)];
+        sn[e] = -sn[e + 1];
+      }
+    } else {
+      const int i0 = e0 < half ? e0 : e0 - half;
+#pragma unroll
+      for (int e = 0; e < N; e += 4) {
+        const float4 u = *reinterpret_cast<const float4*>(p + i0 + e);
+        const float4 z = *reinterpret_cast<const float4*>(p + half + i0 + e);
+        cs[e] = u.x; cs[e + 1] = u.y; cs[e + 2] = u.z; cs[e + 3] = u.w;
+        sn[e] = z.x; sn[e + 1] = z.y; sn[e + 2] = z.z; sn[e + 3] = z.w;
+      }
+      if (e0 < half) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) sn[e] = -sn[e];
+      }
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) { cs[e] = 1.f; sn[e] = 0.f; }
+  }
+
+#pragma unroll
+  for (int it = 0; it < NIT; ++it) {
+    const int s = kind[it];
+    float x[N];
+    Vec<T>::get(raw[it], x);
+    const void* wt = s == 0 ? a.weight[0] : s == 1 ? a.weight[1] : nullptr;
+    if (a.weight[0] || a.weight[1]) {
+      float ss = 0.f;
+#pragma unroll
+      for (int e = 0; e < N; ++e) ss = __fmaf_rn(x[e], x[e], ss);
+      ss = group_sum<LPR>(ss);
+      if (wt) {
+        const float r = div_rn(1.f, __fsqrt_rn(add_rn(div_rn(ss, (float)D), a.eps)));
+        float g[N];
+        if (a.weight_f32) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) g[e] = static_cast<const float*>(wt)[e0 + e];
+        } else {
+          Vec<T>::get(*reinterpret_cast<const uint4*>(static_cast<const T*>(wt) + e0), g);
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = mul_rn(mul_rn(x[e], r), g[e]);
+      }
+    }
+    if (a.cos_sin) {
+      float y[N];
+      if (a.interleaved) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] = x[e ^ 1];
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] = __shfl_sync(0xffffffffu, x[e], mate);
+      }
+      if (turned && s < 2) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = add_rn(mul_rn(x[e], cs[e]), mul_rn(y[e], sn[e]));
+      }
+    }
+    const bool stored = CODE != Code::kNone && s >= 1;
+    if (s >= 0 && !stored) {
+      if (!ok) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = 0.f;
+      }
+      *reinterpret_cast<uint4*>(a.out[s] + t * a.orow[s] + head[it] * a.ohead[s] +
+                                e0 * (int)sizeof(T)) = Vec<T>::put(x);
+    }
+    if (CODE == Code::kHalf && stored && ok) {
+      uint8_t* base = s == 1 ? c.k : c.v;
+      *reinterpret_cast<uint4*>(base + (page * c.s_page + slot * c.s_token + head[it] * c.s_head +
+                                        e0) * (int)sizeof(T)) = Vec<T>::put(x);
+    }
+    if (CODE == Code::kE4m3 || CODE == Code::kI8) {
+      float m = fabsf(x[0]);
+#pragma unroll
+      for (int e = 1; e < N; ++e) m = max_nan(m, fabsf(x[e]));
+      m = group_max<LPR>(m);
+      if (stored && ok) {
+        const float sc = div_rn(m, CODE == Code::kE4m3 ? 448.f : 127.f);
+        const float by = sc == 0.f ? 1.f : sc;
+        uint32_t code[N / 4 > 0 ? N / 4 : 1];
+#pragma unroll
+        for (int e = 0; e < N; e += 4) {
+          float y[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[j] = div_rn(x[e + j], by);
+          if (CODE == Code::kE4m3) {
+            const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(y[0], y[1]), __NV_SATFINITE,
+                                                         __NV_E4M3);
+            const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(y[2], y[3]), __NV_SATFINITE,
+                                                         __NV_E4M3);
+            code[e / 4] = lo | hi << 16;
+          } else {
+            uint32_t v = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              v |= (uint32_t)(uint8_t)(int8_t)max(-127, min(127, __float2int_rn(y[j]))) << (8 * j);
+            code[e / 4] = v;
+          }
+        }
+        uint8_t* base = (s == 1 ? c.k : c.v) + page * c.s_page + slot * c.s_token +
+                        head[it] * c.s_head + e0;
+        *reinterpret_cast<uint2*>(base) = make_uint2(code[0], code[N / 4 - 1]);
+        if (e0 == 0)
+          (s == 1 ? c.k_scale : c.v_scale)[page * c.c_page + slot * c.c_token +
+                                           head[it] * c.c_head] = sc;
+      }
+    }
+  }
+}
+
+struct ReadOut {
+  uint8_t *k, *v;
+  int64_t row, head;             // elements
+};
+
+// One warp takes one token's keys and values, 16 bytes of the cache a lane, the
+// token's place once.
+template <class T, class OUT, Code CODE, int D>
+__global__ void __launch_bounds__(kThreads)
+k_read(BatchArgs b, CacheArgs c, ReadOut o, tre_diag* diag) {
+  constexpr int CB = CODE == Code::kHalf ? 2 : 1;       // bytes of an element in the cache
+  constexpr int N = 16 / CB, LPR = D / N, RPW = 32 / LPR, OV = Vec<OUT>::N;
+  const int lane = threadIdx.x & 31, sub = lane / LPR, e0 = (lane % LPR) * N;
+  const int64_t t64 = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+  if (t64 >= b.n_rows) return;
+  const int t = (int)t64, i = find_seq(b, t);
+  int page = -1, slot = 0;
+  if (i >= 0) {
+    const int end = b.q_start[i + 1];
+    if (t < end) {
+      page = page_of(c, b, i, b.ctx_len[i] - (end - t), slot);
+      if (page < 0 && diag && lane == 0)
+        atomicAdd((unsigned long long*)&diag->dropped_range, 1ull);
+    }
+  }
+  const int64_t at = page * c.s_page + slot * c.s_token, sat = page * c.c_page + slot * c.c_token;
+  const int rows = 2 * c.heads;
+  constexpr int U = 4;
+  for (int r0 = sub; r0 < rows; r0 += U * RPW) {
+    uint4 raw[U];
+    float sc[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + u * RPW;
+      raw[u] = make_uint4(0, 0, 0, 0);
+      sc[u] = 0.f;
+      if (r < rows && page >= 0) {
+        const bool val = r >= c.heads;
+        const int h = val ? r - c.heads : r;
+        raw[u] = *reinterpret_cast<const uint4*>((val ? c.v : c.k) + (at + h * c.s_head + e0) * CB);
+        if (CB == 1) sc[u] = (val ? c.v_scale : c.k_scale)[sat + h * c.c_head];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + u * RPW;
+      if (r >= rows) continue;
+      const bool val = r >= c.heads;
+      const int h = val ? r - c.heads : r;
+      float x[N];
+      if constexpr (CB == 2) {
+        Vec<T>::get(raw[u], x);
+      } else {
+        const uint32_t q[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) codes4(q[j], x + 4 * j, CODE == Code::kI8);
+        if (page >= 0) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) x[e] = mul_rn(x[e], sc[u]);
+        }
+      }
+      OUT* dst = reinterpret_cast<OUT*>(val ? o.v : o.k) + t * o.row + h * o.head + e0;
+#pragma unroll
+      for (int e = 0; e < N; e += OV) *reinterpret_cast<uint4*>(dst + e) = Vec<OUT>::put(x + e);
+    }
+  }
+}
+
+bool mult16(int64_t elements, int size) { return elements * size % 16 == 0; }
+bool at16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+int type_size(int d) {
+  switch (d) {
+    case TRE_F32: return 4;
+    case TRE_BF16: case TRE_F16: return 2;
+    case TRE_E4M3: case TRE_I8: return 1;
+  }
+  return 0;
+}
+
+// Fills `a` from the caller's struct; false for what no kernel takes.
+bool heads_args(const tre_heads* h, bool keys_out, HeadsArgs& a) {
+  if (!h || (h->dim != 64 && h->dim != 128) || h->n_rows < 0 || h->q_heads < 0 || h->k_heads < 0)
+    return false;
+  const int el = type_size(h->dtype);
+  if (el < 2 || h->q_heads > 65536 || h->k_heads > 65536) return false;
+  if (!(h->eps >= 0.f) || h->eps > 3e38f) return false;
+  if ((h->q_weight || h->k_weight) &&
+      (h->weight_dtype != h->dtype && h->weight_dtype != TRE_F32))
+    return false;
+  if ((h->q_weight && !at16(h->q_weight)) || (h->k_weight && !at16(h->k_weight))) return false;
+  if (h->cos_sin) {
+    if (h->rot < 16 || h->rot > h->dim || h->rot % 16 || h->n_pos < 1 || !at16(h->cos_sin) ||
+        !mult16(h->cos_sin_row, 4))
+      return false;
+  }
+  const void* in[2] = {h->q, h->k};
+  void* out[2] = {h->q_out, h->k_out};
+  const int64_t row[2] = {h->q_row, h->k_row}, head[2] = {h->q_head, h->k_head};
+  const int64_t orow[2] = {h->q_out_row, h->k_out_row}, ohead[2] = {h->q_out_head, h->k_out_head};
+  for (int s = 0; s < 2; ++s) {
+    const int n = s ? h->k_heads : h->q_heads;
+    a.heads[s] = n;
+    a.in[s] = static_cast<const uint8_t*>(in[s]);
+    a.out[s] = static_cast<uint8_t*>(out[s]);
+    a.row[s] = row[s] * el;
+    a.head[s] = head[s] * el;
+    a.orow[s] = orow[s] * el;
+    a.ohead[s] = ohead[s] * el;
+    if (n == 0 || h->n_rows == 0) continue;
+    if (!in[s] || !at16(in[s]) || !mult16(row[s], el) || !mult16(head[s], el)) return false;
+    if (s == 1 && !keys_out) continue;
+    if (!out[s] || !at16(out[s]) || !mult16(orow[s], el) || !mult16(ohead[s], el)) return false;
+  }
+  a.heads[2] = 0;
+  a.in[2] = nullptr;
+  a.row[2] = a.head[2] = 0;
+  a.weight[0] = h->q_weight;
+  a.weight[1] = h->k_weight;
+  a.weight_f32 = h->weight_dtype == TRE_F32;
+  a.cos_sin = h->cos_sin;
+  a.cs_row = h->cos_sin_row;
+  a.positions = nullptr;
+  a.n_rows = h->n_rows;
+  a.n_pos = h->n_pos;
+  a.rot = h->cos_sin ? h->rot : 0;
+  a.eps = h->eps;
+  a.interleaved = h->interleaved != 0;
+  return true;
+}
+
+// Four rows a lane when that still leaves every SM 32 warps (one load of the
+// token's place and of its rotation for four times the rows), one otherwise.
+template <class T, Code CODE, int D>
+cudaError_t launch_heads(const HeadsArgs& a, const BatchArgs& b, const CacheArgs& c,
+                         tre_diag* diag, cudaStream_t s) {
+  constexpr int RPW = 32 / (D / Vec<T>::N);
+  const int n = a.heads[0] + a.heads[1] + a.heads[2];
+  if (n == 0 || a.n_rows == 0) return cudaSuccess;
+  const int g4 = (n + 4 * RPW - 1) / (4 * RPW), g1 = (n + RPW - 1) / RPW;
+  constexpr int64_t per = kThreads / 32;
+  if ((int64_t)a.n_rows * g4 >= (int64_t)device_sm_count() * 32) {
+    const int64_t blocks = ((int64_t)a.n_rows * g4 + per - 1) / per;
+    if (blocks > 2147483647) return cudaErrorInvalidValue;
+    k_heads<T, CODE, D, 4><<<(unsigned)blocks, kThreads, 0, s>>>(a, b, c, g4, diag);
+  } else {
+    const int64_t blocks = ((int64_t)a.n_rows * g1 + per - 1) / per;
+    k_heads<T, CODE, D, 1><<<(unsigned)blocks, kThreads, 0, s>>>(a, b, c, g1, diag);
+  }
+  return cudaGetLastError();
+}
+
+template <class T, Code CODE>
+cudaError_t heads_by_dim(int dim, const HeadsArgs& a, const BatchArgs& b, const CacheArgs& c,
+                         tre_diag* diag, cudaStream_t s) {
+  return dim == 64 ? launch_heads<T, CODE, 64>(a, b, c, diag, s)
+                   : launch_heads<T, CODE, 128>(a, b, c, diag, s);
+}
+
+template <class T>
+cudaError_t append_by_code(int code, int dim, const HeadsArgs& a, const BatchArgs& b,
+                           const CacheArgs& c, tre_diag* diag, cudaStream_t s) {
+  if (code == TRE_E4M3) return heads_by_dim<T, Code::kE4m3>(dim, a, b, c, diag, s);
+  if (code == TRE_I8) return heads_by_dim<T, Code::kI8>(dim, a, b, c, diag, s);
+  return heads_by_dim<T, Code::kHalf>(dim, a, b, c, diag, s);
+}
+
+template <class T, class OUT, Code CODE>
+cudaError_t launch_read(int dim, const BatchArgs& b, const CacheArgs& c, const ReadOut& o,
+                        tre_diag* diag, cudaStream_t s) {
+  constexpr int64_t per = kThreads / 32;
+  const unsigned blocks = (unsigned)(((int64_t)b.n_rows + per - 1) / per);
+  if (dim == 64) k_read<T, OUT, CODE, 64><<<blocks, kThreads, 0, s>>>(b, c, o, diag);
+  else k_read<T, OUT, CODE, 128><<<blocks, kThreads, 0, s>>>(b, c, o, diag);
+  return cudaGetLastError();
+}
+
+template <class OUT>
+cudaError_t read_by_code(int code, int dim, const BatchArgs& b, const CacheArgs& c,
+                         const ReadOut& o, tre_diag* diag, cudaStream_t s) {
+  switch (code) {
+    case TRE_BF16: return launch_read<__nv_bfloat16, OUT, Code::kHalf>(dim, b, c, o, diag, s);
+    case TRE_F16: return launch_read<__half, OUT, Code::kHalf>(dim, b, c, o, diag, s);
+    case TRE_E4M3: return launch_read<__half, OUT, Code::kE4m3>(dim, b, c, o, diag, s);
+    default: return launch_read<__half, OUT, Code::kI8>(dim, b, c, o, diag, s);
+  }
+}
+
+}  // namespace
+
+bool cache_args(const tre_kv_cache* c, CacheArgs& a) {
+  if (!c || (c->dim != 64 && c->dim != 128) || c->page < 1 || c->heads < 1 || c->heads > 65535 ||
+      c->n_pages < 0)
+    return false;
+  const bool coded = c->dtype == TRE_E4M3 || c->dtype == TRE_I8;
+  if (!coded && c->dtype != TRE_BF16 && c->dtype != TRE_F16) return false;
+  const int el = type_size(c->dtype);
+  if (c->n_pages > 0) {
+    if (!c->k || !c->v || !at16(c->k) || !at16(c->v)) return false;
+    if (coded && (!c->k_scale || !c->v_scale)) return false;
+  }
+  if (!mult16(c->page_stride, el) || !mult16(c->token_stride, el) || !mult16(c->head_stride, el))
+    return false;
+  a.k = static_cast<uint8_t*>(c->k);
+  a.v = static_cast<uint8_t*>(c->v);
+  a.k_scale = coded ? c->k_scale : nullptr;
+  a.v_scale = coded ? c->v_scale : nullptr;
+  a.s_page = c->page_stride;
+  a.s_token = c->token_stride;
+  a.s_head = c->head_stride;
+  a.c_page = c->scale_page_stride;
+  a.c_token = c->scale_token_stride;
+  a.c_head = c->scale_head_stride;
+  a.n_pages = c->n_pages;
+  a.page = c->page;
+  a.heads = c->heads;
+  a.by_page = FastDiv31((uint32_t)c->page);
+  return true;
+}
+
+bool batch_args(const tre_kv_batch* b, BatchArgs& a) {
+  if (!b || b->n_seq < 0 || b->n_rows < 0 || b->max_pages < 0 || b->max_new < 0 || b->max_ctx < 0)
+    return false;
+  if (b->n_seq > 0 && (!b->ctx_len || !b->q_start)) return false;
+  if (b->n_seq > 0 && b->max_pages > 0 && !b->pages) return false;
+  a.pages = b->pages;
+  a.ctx_len = b->ctx_len;
+  a.q_start = b->q_start;
+  a.pages_row = b->pages_row;
+  a.n_seq = b->n_seq;
+  a.n_rows = b->n_rows;
+  a.max_pages = b->max_pages;
+  return true;
+}
+
+}  // namespace tre
+
+using namespace tre;
+
+extern "C" {
+
+tre_status tre_qk_norm_rope(const tre_heads* heads, const int32_t* positions, tre_diag* diag,
+                            tre_stream stream) {
+  HeadsArgs a;
+  if (!heads_args(heads, true, a) || (heads->cos_sin && heads->n_rows > 0 && !positions))
+    return TRE_EINVAL;
+  a.positions = positions;
+  BatchArgs b{};
+  CacheArgs c{};
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  if (heads->dtype == TRE_F32) e = heads_by_dim<float, Code::kNone>(heads->dim, a, b, c, diag, s);
+  else if (heads->dtype == TRE_BF16)
+    e = heads_by_dim<__nv_bfloat16, Code::kNone>(heads->dim, a, b, c, diag, s);
+  else e = heads_by_dim<__half, Code::kNone>(heads->dim, a, b, c, diag, s);
+  return e == cudaSuccess ? TRE_OK : TRE_ECUDA;
+}
+
+tre_status tre_kv_append(const tre_kv_cache* cache, const tre_kv_batch* batch,
+                         const tre_heads* heads, const void* v, int64_t v_row, int64_t v_head,
+                         tre_diag* diag, tre_stream stream) {
+  HeadsArgs a;
+  BatchArgs b;
+  CacheArgs c;
+  if (!heads_args(heads, false, a) || !batch_args(batch, b) || !cache_args(cache, c))
+    return TRE_EINVAL;
+  if (heads->dtype != TRE_BF16 && heads->dtype != TRE_F16) return TRE_EINVAL;
+  if (cache->dtype != heads->dtype && cache->dtype != TRE_E4M3 && cache->dtype != TRE_I8)
+    return TRE_EINVAL;
+  if (heads->k_heads != cache->heads || heads->dim != cache->dim || heads->n_rows != batch->n_rows)
+    return TRE_EINVAL;
+  if (heads->n_rows == 0) return TRE_OK;
+  if (!v || !at16(v) || !mult16(v_row, 2) || !mult16(v_head, 2)) return TRE_EINVAL;
+  if (batch->n_seq == 0) return TRE_EINVAL;
+  a.heads[2] = cache->heads;
+  a.in[2] = static_cast<const uint8_t*>(v);
+  a.row[2] = v_row * 2;
+  a.head[2] = v_head * 2;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const cudaError_t e =
+      heads->dtype == TRE_BF16
+          ? append_by_code<__nv_bfloat16>(cache->dtype, heads->dim, a, b, c, diag, s)
+          : append_by_code<__half>(cache->dtype, heads->dim, a, b, c, diag, s);
+  return e == cudaSuccess ? TRE_OK : TRE_ECUDA;
+}
+
+tre_status tre_kv_read(const tre_kv_cache* cache, const tre_kv_batch* batch, tre_dtype out_dtype,
+                       void* k_out, void* v_out, int64_t out_row, int64_t out_head,
+                       tre_diag* diag, tre_stream stream) {
+  BatchArgs b;
+  CacheArgs c;
+  if (!batch_args(batch, b) || !cache_args(cache, c)) return TRE_EINVAL;
+  const int el = type_size(out_dtype);
+  if (el < 2) return TRE_EINVAL;
+  if (batch->n_rows == 0) return TRE_OK;
+  if (batch->n_seq == 0) return TRE_EINVAL;
+  if (!k_out || !v_out || !at16(k_out) || !at16(v_out) || !mult16(out_row, el) ||
+      !mult16(out_head, el))
+    return TRE_EINVAL;
+  ReadOut o{static_cast<uint8_t*>(k_out), static_cast<uint8_t*>(v_out), out_row, out_head};
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  if (out_dtype == TRE_F32) e = read_by_code<float>(cache->dtype, cache->dim, b, c, o, diag, s);
+  else if (out_dtype == TRE_BF16)
+    e = read_by_code<__nv_bfloat16>(cache->dtype, cache->dim, b, c, o, diag, s);
+  else e = read_by_code<__half>(cache->dtype, cache->dim, b, c, o, diag, s);
+  return e == cudaSuccess ? TRE_OK : TRE_ECUDA;
+}
+
+}  // extern "C"
