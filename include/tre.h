@@ -59,7 +59,7 @@ typedef enum {
   TRE_ENOMEM = 2,    /* workspace smaller than the queried size */
   TRE_ECUDA = 3,     /* a CUDA launch or runtime call failed */
   TRE_EOVERFLOW = 4, /* move list longer than its capacity (reported in diag.err) */
-  TRE_ETIMEOUT = 5   /* reserved: a bounded device wait gave up (reported in diag.err) */
+  TRE_ETIMEOUT = 5   /* a bounded device wait gave up (reported in diag.err) */
 } tre_status;
 
 /* Scoring is in TRE_F32 or TRE_F64; the other types are those of a served
@@ -612,10 +612,11 @@ typedef struct {
 /* tre_chunk_attention -- each new token's attention over its sequence up to and
  * including itself; the batch's rows are in the cache already. A row that sees no
  * position gives zeros and lse = -inf. Values at positions that a row does not
- * see do not reach it, whatever they hold. */
+ * see do not reach it, whatever they hold. A wait on the device that does not end
+ * in about two seconds gives up (diag.err = TRE_ETIMEOUT, outputs undefined). */
 tre_status tre_chunk_attention(const tre_kv_cache* cache, const tre_kv_batch* batch,
                                const tre_attend* at, void* ws, size_t* ws_bytes,
-                               tre_stream stream);
+                               tre_diag* diag, tre_stream stream);
 
 /* Kernel-phase tracing (host side, not thread safe). While enabled, every
  * kernel phase an entry point enqueues is bracketed by a pair of CUDA events

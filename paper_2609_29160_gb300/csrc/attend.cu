@@ -18,6 +18,7 @@
 #include <algorithm>
 
 #include "attend.cuh"
+#include "attend_tc.h"
 #include "internal.h"
 
 namespace tre {
@@ -91,19 +92,20 @@ template <class T, Code CODE, int DIM>
 __global__ void __launch_bounds__(kWarps * 32, 2)
 k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
   using S = Shape<CODE, DIM>;
-  using PV = typename std::conditional<CODE == Code::kHalf, T, __nv_bfloat16>::type;
+  using CT = typename std::conditional<CODE == Code::kHalf, T, __half>::type;
   constexpr int EPT = 16 / S::CB, SPB = EPT / 4, BLOCKS = DIM / (4 * EPT);
   extern __shared__ __align__(128) uint8_t sm[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, cc = lane & 3;
   const int kvh = blockIdx.x % c.heads;
   int rest = blockIdx.x / c.heads;
-  const int sp = rest % a.n_split;
-  rest /= a.n_split;
+  const int sp = rest % a.parts;
+  rest /= a.parts;
   const int rt0 = rest % a.row_tiles, i = rest / a.row_tiles;
   if (blockIdx.x == 0) loose_rows<T, DIM>(a, b);
   const Seq sq = seq_of(b, i);
   const int rows = sq.n * a.group, base = sq.ctx - sq.n;
+  if (rows > a.few) return;
 
   for (int rt = rt0; rt * kTile < rows; rt += a.row_tiles) {
     const int r_first = rt * kTile, r_last = min(r_first + kTile, rows) - 1;
@@ -188,6 +190,38 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
         qf[s][x + 2] = v.y;
       }
     }
+    // Codes are multiplied as halves, which both kinds turn into in a step or two;
+    // bfloat16 queries then go as halves too, each row divided by a power of two
+    // (its largest element's) that its scores get back: nothing within 2^-24 of the
+    // row's largest element is lost.
+    float back[2] = {1.f, 1.f};
+    if constexpr (!std::is_same<T, CT>::value) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        float top = 0.f;
+#pragma unroll
+        for (int s = 0; s < DIM / 16; ++s)
+#pragma unroll
+          for (int y = x; y < 4; y += 2) {
+            float u, v;
+            unpack(qf[s][y], u, v, T());
+            top = fmaxf(top, fmaxf(fabsf(u), fabsf(v)));
+          }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int ex = min(max((int)(__float_as_uint(top) >> 23), 1), 253);
+        back[x] = __uint_as_float((uint32_t)ex << 23);
+        const float by = __uint_as_float((uint32_t)(254 - ex) << 23);
+#pragma unroll
+        for (int s = 0; s < DIM / 16; ++s)
+#pragma unroll
+          for (int y = x; y < 4; y += 2) {
+            float u, v;
+            unpack(qf[s][y], u, v, T());
+            qf[s][y] = pack<CT>(u * by, v * by);
+          }
+      }
+    }
 
     float o[DIM / 8][4];
 #pragma unroll
@@ -218,19 +252,19 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
         for (int nt = 0; nt < 2; ++nt) {
           const uint4 v = kt[S::place(g + 8 * nt, 4 * bl + cc)];
           if constexpr (CODE == Code::kHalf) {
-            Mma<T>::run(s[nt], qf[2 * bl], v.x, v.y);
-            Mma<T>::run(s[nt], qf[2 * bl + 1], v.z, v.w);
+            Mma<CT>::run(s[nt], qf[2 * bl], v.x, v.y);
+            Mma<CT>::run(s[nt], qf[2 * bl + 1], v.z, v.w);
           } else {
             const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
             for (int x = 0; x < 4; ++x)
-              Mma<T>::run(s[nt], qf[4 * bl + x], pair_of<T, CODE>(w[x]),
-                          pair_of<T, CODE>(w[x] >> 16));
+              Mma<CT>::run(s[nt], qf[4 * bl + x], pair_of<CT, CODE>(w[x]),
+                          pair_of<CT, CODE>(w[x] >> 16));
           }
         }
 
       const int j0 = lo + (warp + k * kWarps) * kTile;
-      float vs[2][2];
+      float vs[2][2], ex[2][2];
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
@@ -238,8 +272,9 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
           const int tok = nt * 8 + 2 * cc + x;
           const float ks = S::SCALES ? mul_rn(sc[tok], a.scale2) : a.scale2;
           vs[nt][x] = S::SCALES ? sc[kTile + tok] : 1.f;
-          s[nt][x] = mul_rn(s[nt][x], ks);
-          s[nt][x + 2] = mul_rn(s[nt][x + 2], ks);
+          ex[nt][x] = S::SCALES ? weight_exponent(vs[nt][x]) : 0.f;
+          s[nt][x] = mul_rn(mul_rn(s[nt][x], back[0]), ks);
+          s[nt][x + 2] = mul_rn(mul_rn(s[nt][x + 2], back[1]), ks);
         }
       const int p_first = base + t_first;
       const bool whole = held == 0xffffu && j0 + kTile - 1 <= p_first &&
@@ -258,7 +293,8 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
       float corr[2];
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        float t = fmaxf(fmaxf(s[0][2 * x], s[0][2 * x + 1]), fmaxf(s[1][2 * x], s[1][2 * x + 1]));
+        float t = fmaxf(fmaxf(s[0][2 * x] + ex[0][0], s[0][2 * x + 1] + ex[0][1]),
+                        fmaxf(s[1][2 * x] + ex[1][0], s[1][2 * x + 1] + ex[1][1]));
         t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
         t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
         const float mn = fmaxf(m[x], t), use = mn == -INFINITY ? 0.f : mn;
@@ -283,10 +319,10 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
       }
       uint32_t pf[4];
       if constexpr (CODE == Code::kHalf) {
-        pf[0] = pack<PV>(s[0][0], s[0][1]);
-        pf[1] = pack<PV>(s[0][2], s[0][3]);
-        pf[2] = pack<PV>(s[1][0], s[1][1]);
-        pf[3] = pack<PV>(s[1][2], s[1][3]);
+        pf[0] = pack<CT>(s[0][0], s[0][1]);
+        pf[1] = pack<CT>(s[0][2], s[0][3]);
+        pf[2] = pack<CT>(s[1][0], s[1][1]);
+        pf[3] = pack<CT>(s[1][2], s[1][3]);
       } else {
         // a masked position's scale may be anything: its weight stays zero
 #pragma unroll
@@ -294,7 +330,7 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             const float u = s[nt][2 * x], w = s[nt][2 * x + 1];
-            pf[2 * nt + x] = pack<PV>(u == 0.f ? 0.f : u * vs[nt][0], w == 0.f ? 0.f : w * vs[nt][1]);
+            pf[2 * nt + x] = pack<CT>(u == 0.f ? 0.f : u * vs[nt][0], w == 0.f ? 0.f : w * vs[nt][1]);
           }
       }
       // values: columns of n-tile jj stand 8 (16) elements apart, as a lane's read
@@ -313,7 +349,7 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
 #pragma unroll
           for (int jj = 0; jj < 8; ++jj) {
             const uint32_t sel = jj & 1 ? 0x7632 : 0x5410;
-            Mma<PV>::run(o[set * 8 + jj], pf, __byte_perm(w[0][jj >> 1], w[1][jj >> 1], sel),
+            Mma<CT>::run(o[set * 8 + jj], pf, __byte_perm(w[0][jj >> 1], w[1][jj >> 1], sel),
                          __byte_perm(w[2][jj >> 1], w[3][jj >> 1], sel));
           }
         }
@@ -342,9 +378,9 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
             const uint32_t sel = hf ? 0x7362 : 0x5140;
             const uint32_t u = __byte_perm(w[0][y], w[1][y], sel);
             const uint32_t z = __byte_perm(w[2][y], w[3][y], sel);
-            Mma<PV>::run(o[4 * y + 2 * hf], pf, pair_of<PV, CODE>(u), pair_of<PV, CODE>(z));
-            Mma<PV>::run(o[4 * y + 2 * hf + 1], pf, pair_of<PV, CODE>(u >> 16),
-                         pair_of<PV, CODE>(z >> 16));
+            Mma<CT>::run(o[4 * y + 2 * hf], pf, pair_of<CT, CODE>(u), pair_of<CT, CODE>(z));
+            Mma<CT>::run(o[4 * y + 2 * hf + 1], pf, pair_of<CT, CODE>(u >> 16),
+                         pair_of<CT, CODE>(z >> 16));
           }
       }
       __syncwarp();
@@ -418,12 +454,9 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
         row_again<T, CODE, DIM>(a, b, c, i, kvh,
                                 reinterpret_cast<const T*>(a.q) + row * a.q_row + h * a.q_head,
                                 base + t, lo, hi, top, x);
-      if (a.n_split > 1) {
+      if (lane == 0) row_state(a, b, sp, row, h, top, sum);
+      if (a.parts > 1) {
         const int64_t at = ((int64_t)sp * b.n_rows + row) * a.heads + h;
-        if (lane == 0) {
-          a.part_ml[2 * at] = top;
-          a.part_ml[2 * at + 1] = sum;
-        }
         float* p = a.part_o + at * DIM + lane * EL;
         if (sum > 0.f || sum != sum) {
           if constexpr (EL == 4) *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
@@ -435,8 +468,6 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
 #pragma unroll
         for (int e = 0; e < EL; e += 2)
           *reinterpret_cast<uint32_t*>(p + e) = pack<T>(x[e] * by, x[e + 1] * by);
-        if (a.lse && lane == 0)
-          a.lse[row * a.heads + h] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * kLn2;
       }
     }
     __syncthreads();
@@ -450,6 +481,7 @@ __global__ void __launch_bounds__(128) k_join(AttendArgs a, int64_t rows_heads) 
   const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
   if (w >= rows_heads) return;
   constexpr int EL = DIM / 32;
+  if (a.part_ml[2 * w + 1] < 0.f) return;       // written already
   float top = -INFINITY;
   for (int sp = lane; sp < a.n_split; sp += 32)
     top = fmaxf(top, a.part_ml[2 * (sp * rows_heads + w)]);
@@ -496,45 +528,100 @@ cudaError_t launch_typed(const AttendArgs& a, const BatchArgs& b, const CacheArg
   const void* fn = (const void*)k_attend<T, CODE, DIM>;
   cudaError_t e = func_smem_once(fn, S::SMEM, true);
   if (e) return e;
-  const int64_t blocks = (int64_t)c.heads * a.n_split * a.row_tiles * b.n_seq;
+  const int64_t blocks = (int64_t)c.heads * a.parts * a.row_tiles * b.n_seq;
   if (blocks > 2147483647) return cudaErrorInvalidValue;
   k_attend<T, CODE, DIM><<<(unsigned)blocks, kWarps * 32, S::SMEM, s>>>(a, b, c);
-  if (a.n_split > 1) {
-    const int64_t rh = (int64_t)b.n_rows * a.heads;
-    k_join<T, DIM><<<(unsigned)((rh + 3) / 4), 128, 0, s>>>(a, rh);
-  }
   return cudaGetLastError();
-}
-
-template <class T, Code CODE>
-cudaError_t launch_dim(int dim, const AttendArgs& a, const BatchArgs& b, const CacheArgs& c,
-                       cudaStream_t s) {
-  return dim == 64 ? launch_typed<T, CODE, 64>(a, b, c, s) : launch_typed<T, CODE, 128>(a, b, c, s);
 }
 
 template <class T>
 cudaError_t launch_code(int code, int dim, const AttendArgs& a, const BatchArgs& b,
                         const CacheArgs& c, cudaStream_t s) {
-  if (code == TRE_E4M3) return launch_dim<T, Code::kE4m3>(dim, a, b, c, s);
-  if (code == TRE_I8) return launch_dim<T, Code::kI8>(dim, a, b, c, s);
-  return launch_dim<T, Code::kHalf>(dim, a, b, c, s);
+  if (code == TRE_E4M3)
+    return dim == 64 ? launch_typed<T, Code::kE4m3, 64>(a, b, c, s)
+                     : launch_typed<T, Code::kE4m3, 128>(a, b, c, s);
+  if (code == TRE_I8)
+    return dim == 64 ? launch_typed<T, Code::kI8, 64>(a, b, c, s)
+                     : launch_typed<T, Code::kI8, 128>(a, b, c, s);
+  return dim == 64 ? launch_typed<T, Code::kHalf, 64>(a, b, c, s)
+                   : launch_typed<T, Code::kHalf, 128>(a, b, c, s);
 }
 
-// Parts of a context: enough blocks to fill the GPU a few times over, none
-// shorter than 256 tokens (a part costs a block's start and its share of the
-// join, about what 256 tokens of keys and values cost to read).
-void choose_parts(AttendArgs& a, const tre_kv_batch* b, int heads, int page) {
-  const int max_new = b->max_new > 0 ? b->max_new : b->n_rows;
-  const int64_t rows = (int64_t)std::max(max_new, 1) * a.group;
-  a.row_tiles = (int)std::min<int64_t>((rows + kTile - 1) / kTile, 1 << 20);
+template <class T>
+cudaError_t launch_join(int dim, const AttendArgs& a, const BatchArgs& b, cudaStream_t s) {
+  const int64_t rh = (int64_t)b.n_rows * a.heads;
+  const unsigned blocks = (unsigned)((rh + 3) / 4);
+  if (dim == 64) k_join<T, 64><<<blocks, 128, 0, s>>>(a, rh);
+  else k_join<T, 128><<<blocks, 128, 0, s>>>(a, rh);
+  return cudaGetLastError();
+}
+
+// How a call is split, from what the host knows of it.
+struct Plan {
+  bool tc;                        // some sequence may have more than `few` rows
+  int32_t few, n_split;
+  int32_t parts[2], split[2], row_tiles[2];     // k_attend, k_attend_tc
+};
+
+// Up to 64 rows of a sequence go to k_attend, whose 16-row tiles then read each key
+// up to four times (from L2) where k_attend_tc would multiply mostly empty rows.
+constexpr int kFew = 64;
+
+Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page) {
+  Plan p{};
+  const int64_t max_new = std::max(1, b->max_new > 0 ? b->max_new : b->n_rows);
+  const int64_t rows = max_new * a.group;
   int64_t len = b->max_ctx > 0 ? b->max_ctx : (int64_t)b->max_pages * page;
   if (a.window > 0) len = std::min<int64_t>(len, (int64_t)a.window + max_new + 15);
-  const int64_t units = std::max<int64_t>(1, (int64_t)b->n_seq * heads * a.row_tiles);
-  const int64_t want = std::max<int64_t>(1, ((int64_t)device_sm_count() * 2 * 4 + units - 1) / units);
-  const int64_t most = std::max<int64_t>(1, len / 256);
-  a.n_split = (int)std::min<int64_t>({want, most, 256});
-  const int64_t part = (len + a.n_split - 1) / a.n_split;
-  a.split = (int)std::max<int64_t>(kTile * kWarps, part);
+  len = std::max<int64_t>(len, 1);
+  const int64_t sms = device_sm_count();
+  p.tc = rows > kFew;
+  p.few = p.tc ? kFew : 2147483647;
+  {
+    // Parts of a context: enough blocks to fill the GPU a few times over, none
+    // shorter than 256 tokens (a part costs a block's start and its share of the
+    // join, about what 256 tokens of keys and values cost to read).
+    const int64_t r = p.tc ? kFew : rows;
+    p.row_tiles[0] = (int)std::min<int64_t>((r + kTile - 1) / kTile, 1 << 20);
+    const int64_t units = std::max<int64_t>(1, (int64_t)b->n_seq * heads * (p.tc ? 1 : p.row_tiles[0]));
+    const int64_t want = std::max<int64_t>(1, (sms * 8 + units - 1) / units);
+    p.parts[0] = (int)std::min<int64_t>({want, std::max<int64_t>(1, len / 256), 256});
+    p.split[0] = (int)std::max<int64_t>(kTile * kWarps, (len + p.parts[0] - 1) / p.parts[0]);
+  }
+  p.n_split = p.parts[0];
+  if (p.tc) {
+    p.row_tiles[1] = (int)std::min<int64_t>((rows + kTcRows - 1) / kTcRows, 1 << 20);
+    const int64_t tiles = std::min<int64_t>((int64_t)b->n_seq * p.row_tiles[1],
+                                            (int64_t)b->n_rows * a.group / kTcRows + b->n_seq);
+    const int64_t units = std::max<int64_t>(1, tiles * heads);
+    const int64_t want = std::max<int64_t>(1, sms / units);
+    p.parts[1] = (int)std::min<int64_t>({want, std::max<int64_t>(1, len / 512), 64});
+    p.split[1] = (int)std::max<int64_t>(kTcTokens, (len + p.parts[1] - 1) / p.parts[1]);
+    p.n_split = std::max(p.n_split, p.parts[1]);
+  }
+  return p;
+}
+
+cudaError_t launch_all(int dtype, int code, int dim, AttendArgs a, const Plan& p,
+                       const BatchArgs& b, const CacheArgs& c, tre_diag* diag, cudaStream_t s) {
+  a.few = p.few;
+  a.n_split = p.n_split;
+  cudaError_t e = cudaSuccess;
+  if (p.tc) {
+    a.parts = p.parts[1];
+    a.split = p.split[1];
+    a.row_tiles = p.row_tiles[1];
+    e = launch_attend_tc(dtype, code, dim, a, b, c, diag, s);
+    if (e) return e;
+  }
+  a.parts = p.parts[0];
+  a.split = p.split[0];
+  a.row_tiles = p.row_tiles[0];
+  const bool bf = dtype == TRE_BF16;
+  e = bf ? launch_code<__nv_bfloat16>(code, dim, a, b, c, s)
+         : launch_code<__half>(code, dim, a, b, c, s);
+  if (e || p.n_split == 1) return e;
+  return bf ? launch_join<__nv_bfloat16>(dim, a, b, s) : launch_join<__half>(dim, a, b, s);
 }
 
 }  // namespace
@@ -544,7 +631,7 @@ using namespace tre;
 
 extern "C" tre_status tre_chunk_attention(const tre_kv_cache* cache, const tre_kv_batch* batch,
                                           const tre_attend* at, void* ws, size_t* ws_bytes,
-                                          tre_stream stream) {
+                                          tre_diag* diag, tre_stream stream) {
   AttendArgs a{};
   BatchArgs b;
   CacheArgs c;
@@ -564,12 +651,13 @@ extern "C" tre_status tre_chunk_attention(const tre_kv_cache* cache, const tre_k
   if (b.n_rows > 0 && (int64_t)b.n_rows * a.group > 2147483647ll / 2) return TRE_EINVAL;
   a.by_group = FastDiv31((uint32_t)a.group);
   a.window = at->window;
-  if (b.n_seq > 0) choose_parts(a, batch, c.heads, c.page);
+  Plan plan{};
+  if (b.n_seq > 0) plan = plan_of(batch, a, c.heads, c.page);
   Arena arena(ws);
-  if (a.n_split > 1) {
+  if (plan.n_split > 1) {
     const size_t rh = (size_t)b.n_rows * a.heads;
-    a.part_ml = arena.take<float>(2 * rh * a.n_split);
-    a.part_o = arena.take<float>(rh * a.n_split * cache->dim);
+    a.part_ml = arena.take<float>(2 * rh * plan.n_split);
+    a.part_o = arena.take<float>(rh * plan.n_split * cache->dim);
   }
   if (!ws) {
     *ws_bytes = arena.off;
@@ -587,8 +675,7 @@ extern "C" tre_status tre_chunk_attention(const tre_kv_cache* cache, const tre_k
   a.o_head = at->out_head;
   a.scale2 = (float)((double)at->scale * 1.4426950408889634);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const cudaError_t e = at->dtype == TRE_BF16
-                            ? launch_code<__nv_bfloat16>(cache->dtype, cache->dim, a, b, c, s)
-                            : launch_code<__half>(cache->dtype, cache->dim, a, b, c, s);
+  const cudaError_t e =
+      launch_all(at->dtype, cache->dtype, cache->dim, a, plan, b, c, diag, s);
   return e == cudaSuccess ? TRE_OK : TRE_ECUDA;
 }

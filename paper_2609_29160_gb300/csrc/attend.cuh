@@ -17,9 +17,13 @@ struct AttendArgs {
   FastDiv31 by_group;
   float scale2;                   // scale * log2(e): scores are kept in powers of two
   int32_t window;                 // 0: none
-  int32_t n_split, split;         // parts of a context, and the shortest part
-  float *part_o, *part_ml;        // [n_split][n_rows * heads][dim], [..][2]
-  int32_t row_tiles;
+  int32_t parts, split;           // parts of a context, and the shortest part
+  int32_t row_tiles;              // blocks along a sequence's rows
+  int32_t few;                    // rows of a sequence that k_attend takes
+  // parts of either kernel at most; with more than one, [n_split][n_rows * heads][dim]
+  // sums and [..][2] maxima and weights of theirs
+  int32_t n_split;
+  float *part_o, *part_ml;
 };
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -59,12 +63,34 @@ template <int STEP>
 __device__ __forceinline__ void part_of(const AttendArgs& a, int sp, int& lo, int& hi) {
   const int len = hi - lo;
   if (len <= 0) return;
-  int chunk = max(a.split, (len + a.n_split - 1) / a.n_split);
+  int chunk = max(a.split, (len + a.parts - 1) / a.parts);
   chunk = (chunk + STEP - 1) / STEP * STEP;
   const int64_t from = (int64_t)lo + (int64_t)sp * chunk;
   const int to = (int)min64(hi, from + chunk);
   lo = (int)min64(from, hi);
   hi = to;
+}
+
+// What a block leaves beside a row's sum: for its part of the join, or (one part)
+// the row's logarithm, and for the join that the row is done (a weight below zero).
+__device__ __forceinline__ void row_state(const AttendArgs& a, const BatchArgs& b, int sp,
+                                          int64_t row, int head, float m, float l) {
+  const int64_t at = row * a.heads + head, all = (int64_t)b.n_rows * a.heads;
+  if (a.n_split > 1) {
+    float2* ml = reinterpret_cast<float2*>(a.part_ml) + at;
+    ml[sp * all] = a.parts > 1 ? make_float2(m, l) : make_float2(0.f, -1.f);
+    if (sp == 0 && a.parts > 1)
+      for (int s = a.parts; s < a.n_split; ++s) ml[s * all] = make_float2(-INFINITY, 0.f);
+  }
+  if (a.parts == 1 && a.lse)
+    a.lse[at] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+// The power of two of a value's scale, which counts in its weight: with m the
+// largest s + exponent, a weight exp2(s - m) * scale stays below two whatever the
+// scales are. (Bounded, so that a scale of zero leaves m finite.)
+__device__ __forceinline__ float weight_exponent(float scale) {
+  return fminf(fmaxf(__log2f(fabsf(scale)), -100.f), 100.f);
 }
 
 // DIM/32 elements of one cached row, as floats (without the scale).
@@ -117,7 +143,7 @@ __device__ void row_again(const AttendArgs& a, const BatchArgs& b, const CacheAr
     s *= a.scale2;
     if (CODE != Code::kHalf) s *= c.k_scale[soff];
     float p = exp2_fast(s - m);
-    if (CODE != Code::kHalf) p *= c.v_scale[soff];
+    if (CODE != Code::kHalf) p = mul_rn(p, c.v_scale[soff]);
     cached<T, CODE, DIM>(c.v, off, lane, y);
 #pragma unroll
     for (int e = 0; e < N; ++e) acc[e] = __fmaf_rn(p, y[e], acc[e]);

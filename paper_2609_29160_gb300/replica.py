@@ -30,7 +30,7 @@ def declare(lib):
     lib.tre_qk_norm_rope.argtypes = [P, P, P, P]
     lib.tre_kv_append.argtypes = [P, P, P, P, L, L, P, P]
     lib.tre_kv_read.argtypes = [P, P, C.c_int, P, P, L, L, P, P]
-    lib.tre_chunk_attention.argtypes = [P, P, P, P, C.POINTER(C.c_size_t), P]
+    lib.tre_chunk_attention.argtypes = [P, P, P, P, C.POINTER(C.c_size_t), P, P]
     for f in ("tre_qk_norm_rope", "tre_kv_append", "tre_kv_read", "tre_chunk_attention"):
         getattr(lib, f).restype = C.c_int
 
@@ -315,7 +315,8 @@ def tre_kv_read(cache, batch, dtype="bf16", k_out=None, v_out=None, diag=None, s
     return k_out, v_out
 
 
-def tre_chunk_attention(q, cache, batch, scale=None, window=0, lse=False, out=None, stream=None):
+def tre_chunk_attention(q, cache, batch, scale=None, window=0, lse=False, out=None, diag=None,
+                        stream=None):
     """Attention of the batch's rows q [rows][heads][dim] over the cache, each row up
     to its own position (its last `window` positions only, with a window). Returns
     out [rows][heads][dim]; with lse also float32 [rows][heads]."""
@@ -338,11 +339,12 @@ def tre_chunk_attention(q, cache, batch, scale=None, window=0, lse=False, out=No
                      q.data_ptr(), qr, qh, out.data_ptr(), o_row, oh,
                      0 if ls is None else ls.data_ptr())
     size, s = C.c_size_t(0), _current(stream)
-    code = lib.tre_chunk_attention(cache.packed, batch.packed, at, None, size, s)
+    dg = None if diag is None else diag.data_ptr()
+    code = lib.tre_chunk_attention(cache.packed, batch.packed, at, None, size, dg, s)
     if code:
         tre._check("tre_chunk_attention", code)
     ws = q.new_empty(max(size.value, 256), dtype=_torch.uint8)
-    code = lib.tre_chunk_attention(cache.packed, batch.packed, at, ws.data_ptr(), size, s)
+    code = lib.tre_chunk_attention(cache.packed, batch.packed, at, ws.data_ptr(), size, dg, s)
     if code:
         tre._check("tre_chunk_attention", code)
     if stream is not None:

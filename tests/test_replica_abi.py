@@ -65,7 +65,7 @@ def test_caches_are_checked(bad):
     n = C.c_size_t(0)
     assert lib.tre_kv_append(c, batch(), heads(), A, 128, 64, None, None) == 1
     assert lib.tre_kv_read(c, batch(), R.BF16, A, A, 128, 64, None, None) == 1
-    assert lib.tre_chunk_attention(c, batch(), attend(), None, C.byref(n), None) == 1
+    assert lib.tre_chunk_attention(c, batch(), attend(), None, C.byref(n), None, None) == 1
 
 
 @pytest.mark.parametrize("bad", BAD_BATCHES)
@@ -74,7 +74,7 @@ def test_batches_are_checked(bad):
     n = C.c_size_t(1 << 40)
     assert lib.tre_kv_append(cache(), b, heads(), A, 128, 64, None, None) == 1
     assert lib.tre_kv_read(cache(), b, R.BF16, A, A, 128, 64, None, None) == 1
-    assert lib.tre_chunk_attention(cache(), b, attend(), A, C.byref(n), None) == 1
+    assert lib.tre_chunk_attention(cache(), b, attend(), A, C.byref(n), None, None) == 1
 
 
 def test_append_and_read_arguments():
@@ -97,17 +97,17 @@ def test_append_and_read_arguments():
 def test_attention_arguments(bad):
     n = C.c_size_t(0)
     assert tre.load().tre_chunk_attention(cache(), batch(), attend(**bad), None, C.byref(n),
-                                          None) == 1
+                                          None, None) == 1
 
 
 def test_attention_workspace():
     lib = tre.load()
     n = C.c_size_t(0)
     b = batch(max_new=3, max_ctx=100_000, max_pages=7000, row=7000)
-    assert lib.tre_chunk_attention(cache(), b, attend(), None, C.byref(n), None) == 0
+    assert lib.tre_chunk_attention(cache(), b, attend(), None, C.byref(n), None, None) == 0
     assert n.value > 0
     small = C.c_size_t(n.value - 1)
-    assert lib.tre_chunk_attention(cache(), b, attend(), A, C.byref(small), None) == 2
-    assert lib.tre_chunk_attention(cache(), b, attend(), None, None, None) == 1
+    assert lib.tre_chunk_attention(cache(), b, attend(), A, C.byref(small), None, None) == 2
+    assert lib.tre_chunk_attention(cache(), b, attend(), None, None, None, None) == 1
     assert lib.tre_chunk_attention(cache(), batch(rows=0), attend(q=0, out=0), A, C.byref(n),
-                                   None) == 0
+                                   None, None) == 0
