@@ -111,7 +111,7 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
     const int r_first = rt * kTile, r_last = min(r_first + kTile, rows) - 1;
     const int t_first = a.by_group.div(r_first);
     int lo, hi;
-    range_of(sq, c, b, a.window, t_first, a.by_group.div(r_last), lo, hi);
+    range_of<kTile>(sq, c, b, a.window, t_first, a.by_group.div(r_last), lo, hi);
     part_of<kTile * kWarps>(a, sp, lo, hi);
     const int n_tiles = hi > lo ? (hi - lo + kTile - 1) / kTile : 0;
     const int mine = n_tiles > warp ? (n_tiles - warp + kWarps - 1) / kWarps : 0;

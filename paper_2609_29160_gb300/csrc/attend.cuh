@@ -46,7 +46,8 @@ __device__ __forceinline__ Seq seq_of(const BatchArgs& b, int i) {
 }
 
 // Positions [lo, hi) that rows of tokens t0..t1 of a sequence may see; lo is a
-// multiple of 16.
+// multiple of STEP.
+template <int STEP>
 __device__ __forceinline__ void range_of(const Seq& s, const CacheArgs& c, const BatchArgs& b,
                                          int window, int t0, int t1, int& lo, int& hi) {
   const int base = s.ctx - s.n;
@@ -54,7 +55,7 @@ __device__ __forceinline__ void range_of(const Seq& s, const CacheArgs& c, const
   const int64_t h = min64((int64_t)base + t1 + 1, cap);
   hi = (int)(h > 0 ? h : 0);
   int64_t l = window > 0 ? (int64_t)base + t0 - window + 1 : 0;
-  lo = (int)(l > 0 ? l : 0) & ~15;
+  lo = (int)(l > 0 ? l : 0) / STEP * STEP;
 }
 
 // Part sp of a range: contexts longer than the host expected get longer parts.

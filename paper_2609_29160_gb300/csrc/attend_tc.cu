@@ -7,7 +7,7 @@
 // tiles of 128 rows against a part of the context, 128 positions at a time:
 //
 //   S = Q K^T       both operands in shared memory, S (128 x 128, float) in TMEM
-//   P = exp2(S - m) a thread a row: S out of TMEM, P back over it in 16 bits
+//   P = exp2(S - m) S out of TMEM, P back over it in 16 bits
 //   O += P V        P from TMEM, V from shared memory, O (128 x dim, float) in TMEM
 //
 // While one tile's warps take exponentials the tensor cores multiply for the other.
@@ -15,11 +15,19 @@
 // time (weights then reach 256, far inside either 16-bit type's range; m and l are
 // exact in any case), so the pass over O is rare.
 //
-// Warps 0-3, 4-7: a tile's rows. Warps 8-11: copies, through pages, of keys and
-// values into a ring of 128-token tiles (codes are converted on the way: both kinds
-// are exact in 16 bits; the scales go into the scores and weights instead). Warp 12
-// issues the products. Registers go to the row warps.
+// Whole tiles of 16-bit elements come by tensor copies, a box a page; the last tile of a
+// range, and every tile of pages that 8 does not divide, by 16-byte pieces, which leave
+// zeros past the range's end.
+//
+// Warps 0-3, 4-7: a tile's rows, a thread a row with its 128 scores in registers. Warps
+// 8-10: copies, through pages, of keys and values into a ring of 128-token tiles (codes
+// are converted on the way: both kinds are exact in 16 bits; the scales go into the
+// scores and weights instead). Warp 11 issues the products.
+#include <cuda.h>
+
 #include <algorithm>
+#include <cstring>
+#include <numeric>
 
 #include "attend.cuh"
 #include "attend_tc.h"
@@ -28,7 +36,10 @@
 namespace tre {
 namespace {
 
-constexpr int kThreads = 512, kRows = 128, kTok = 128;
+constexpr int kRows = 128, kTok = 128;
+constexpr int kRowWarps = 8, kCopyWarp = kRowWarps, kCopyWarps = 3;
+constexpr int kMmaWarp = kCopyWarp + kCopyWarps;
+constexpr int kThreads = (kMmaWarp + 1) * 32;
 constexpr long long kWaitClocks = 4000000000ll;
 
 __device__ __forceinline__ uint32_t smem_of(const void* p) {
@@ -39,6 +50,11 @@ __device__ __forceinline__ void bar_init(uint64_t* b, uint32_t n) {
 }
 __device__ __forceinline__ void bar_arrive(uint64_t* b) {
   asm volatile("mbarrier.arrive.shared.b64 _, [%0];" ::"r"(smem_of(b)) : "memory");
+}
+// One arrival for a warp whose lanes are all done.
+__device__ __forceinline__ void bar_arrive_warp(uint64_t* b) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) bar_arrive(b);
 }
 __device__ __forceinline__ bool bar_poll(uint64_t* b, uint32_t parity) {
   uint32_t ok;
@@ -90,8 +106,45 @@ __device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t* r) {
       "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
-__device__ __forceinline__ void tmem_wait_ld() {
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
+      "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t at, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15])
+      : "r"(at)
+      : "memory");
+}
+// (names the registers, so that nothing reads them before)
+__device__ __forceinline__ void tmem_wait_ld(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
+                 "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :
+               : "memory");
+  asm volatile(""
+               : "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]),
+                 "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]),
+                 "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               :
+               : "memory");
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 __device__ __forceinline__ void tmem_wait_st() {
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
@@ -107,30 +160,82 @@ __device__ __forceinline__ void commit(uint64_t* b) {
                    smem_of(b))
                : "memory");
 }
-// D (TMEM) = or += A * B, both operands in shared memory / A in TMEM
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
-                                       uint32_t add) {
+// One lane of a warp, in a way that lets the compiler keep what it computes in the
+// warp's shared registers: the operands of a product come from those, and moving
+// them there one by one takes longer than the product.
+__device__ __forceinline__ bool one_lane() {
+  uint32_t r;
+  asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.b32 %0, 1, 0, p; }" : "=r"(r));
+  return r != 0;
+}
+// D (TMEM) = or += A * B, both operands in shared memory / A in TMEM. Operands of
+// shared memory by the low half of their description (see operand).
+constexpr uint32_t kOperandHigh = (1024 >> 4) | 1u << 14 | 2u << 29;
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
+                                       bool add) {
   asm volatile(
-      "{ .reg .pred p; setp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(add)
+      "{ .reg .pred p; .reg .b64 x, y; setp.ne.b32 p, %4, 0; mov.b64 x, {%1, %5}; "
+      "mov.b64 y, {%2, %5};\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p; }" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "n"(kOperandHigh)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
-                                       uint32_t add) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
+                                       bool add) {
   asm volatile(
-      "{ .reg .pred p; setp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(add)
+      "{ .reg .pred p; .reg .b64 y; setp.ne.b32 p, %4, 0; mov.b64 y, {%2, %5};\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p; }" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "n"(kOperandHigh)
       : "memory");
 }
 
-// Shared-memory operand in rows of 128 bytes, 16-byte pieces of row r at piece ^ (r & 7).
-// lead: bytes to the next 64 elements along the dense axis (where that axis is not
-// the one summed over), 1024 bytes to the next eight rows.
-__device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t lead) {
-  return (uint64_t)((at >> 4) & 0x3fff) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 |
-         1ull << 46 | 2ull << 61;
+// Two floats at a time
+__device__ __forceinline__ uint64_t two(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void split(uint64_t v, uint32_t* x) {
+  asm("mov.b64 {%0, %1}, %2;" : "=r"(x[0]), "=r"(x[1]) : "l"(v));
+}
+__device__ __forceinline__ uint64_t two(const uint32_t* x) {
+  return two(__uint_as_float(x[0]), __uint_as_float(x[1]));
+}
+__device__ __forceinline__ void fma2(uint32_t* x, float f, float plus) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(two(x)), "l"(two(f, f)), "l"(two(plus, plus)));
+  split(r, x);
+}
+__device__ __forceinline__ void mul2(uint32_t* x, float f, float g) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(two(x)), "l"(two(f, g)));
+  split(r, x);
+}
+__device__ __forceinline__ void add2(uint32_t* x, float f, float g) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(two(x)), "l"(two(f, g)));
+  split(r, x);
+}
+__device__ __forceinline__ uint64_t sum2(uint64_t s, float a, float b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(s), "l"(two(a, b)));
+  return r;
+}
+__device__ __forceinline__ float halves_sum(uint64_t a, uint64_t b) {
+  uint32_t x[2], y[2];
+  split(a, x);
+  split(b, y);
+  return (__uint_as_float(x[0]) + __uint_as_float(y[0])) +
+         (__uint_as_float(x[1]) + __uint_as_float(y[1]));
+}
+
+// Low half of the description of an operand in shared memory, in rows of 128 bytes with
+// the 16-byte pieces of row r at piece ^ (r & 7): its address and `lead`, the bytes to
+// the next 64 elements along the dense axis (where that axis is not the one summed
+// over). The high half (kOperandHigh) says 1024 bytes to the next eight rows and that
+// order of pieces.
+__device__ __forceinline__ uint32_t operand(uint32_t at, uint32_t lead) {
+  return ((at >> 4) & 0x3fff) | (lead >> 4) << 16;
 }
 template <class T> __host__ __device__ constexpr uint32_t idesc_of(int n, bool b_turned) {
   const uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
@@ -138,15 +243,47 @@ template <class T> __host__ __device__ constexpr uint32_t idesc_of(int n, bool b
          (uint32_t)(kRows >> 4) << 24;
 }
 
+// Keys and values as tensors of (element, slot, head, page), read in boxes of `box`
+// slots and 64 elements; box 0: not to be read that way.
+struct Maps {
+  CUtensorMap k, v;
+  int32_t box;
+};
+__device__ __forceinline__ void box_load(uint32_t dst, const CUtensorMap* map, int x, int slot,
+                                         int head, int page, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(slot), "r"(head), "r"(page), "r"(smem_of(bar))
+      : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(smem_of(b)), "r"(bytes)
+               : "memory");
+}
+
+// A position's page, asked for now and looked at later.
+struct Ask {
+  int id = -1, slot = 0;
+  __device__ __forceinline__ void at(const CacheArgs& c, const BatchArgs& b, int i, int j,
+                                     int end) {
+    const int q = (int)c.by_page.div((uint32_t)j);
+    slot = j - q * c.page;
+    id = j < end && q < b.max_pages ? b.pages[(int64_t)i * b.pages_row + q] : -1;
+  }
+  __device__ __forceinline__ int page(const CacheArgs& c) const {
+    return id >= 0 && id < c.n_pages ? id : -1;
+  }
+};
+
 template <Code CODE, int DIM> struct Tc {
   static constexpr bool CODED = CODE != Code::kHalf;
   static constexpr int BUF = kTok * DIM * 2;            // a tile of keys or values
   static constexpr int RING = DIM == 128 ? (CODED ? 4 : 5) : (CODED ? 8 : 8);
-  static constexpr int META = 8;                        // tiles whose scales and masks are kept
+  static constexpr int META = DIM == 128 ? 4 : 8;                        // tiles whose scales and masks are kept
   static constexpr int Q = 2 * kRows * DIM * 2;
   static constexpr int AT_RING = Q;
-  static constexpr int AT_OFF = AT_RING + RING * BUF;   // int64 [2][kTok]
-  static constexpr int AT_MASK = AT_OFF + 2 * kTok * 8; // uint32 [META][4]
+  static constexpr int AT_MASK = AT_RING + RING * BUF;  // uint32 [META][4]
   static constexpr int AT_SCALE = AT_MASK + META * 16;  // float [META][3][kTok]
   static constexpr int AT_BAR = AT_SCALE + (CODED ? META * 3 * kTok * 4 : 0);
   static constexpr int BARS = 2 * RING + META + 7;
@@ -171,10 +308,12 @@ __device__ __forceinline__ void widen(const uint4& v, uint4& lo, uint4& hi) {
 
 template <class T, Code CODE, int DIM>
 __global__ void __launch_bounds__(kThreads, 1)
-k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, tre_diag* diag) {
+k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps maps,
+            tre_diag* diag) {
   using L = Tc<CODE, DIM>;
   extern __shared__ __align__(1024) uint8_t sm[];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int kvh = blockIdx.x % c.heads;
   int rest = blockIdx.x / c.heads;
   const int sp = rest % a.parts;
@@ -190,11 +329,10 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, tre_diag* diag) {
            *p_full = s_full + 2, *o_done = p_full + 2, *q_full = o_done + 2;
   uint32_t* tmem_at = reinterpret_cast<uint32_t*>(bars + L::BARS);
   volatile int* dead = reinterpret_cast<volatile int*>(tmem_at + 1);
-  int64_t* off_s = reinterpret_cast<int64_t*>(sm + L::AT_OFF);
   uint32_t* mask_s = reinterpret_cast<uint32_t*>(sm + L::AT_MASK);
   float* scale_s = reinterpret_cast<float*>(sm + L::AT_SCALE);
 
-  if (warp == 12) {
+  if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(
                      smem_of(tmem_at))
                  : "memory");
@@ -209,13 +347,13 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, tre_diag* diag) {
   auto turn = [&](int rt) {
     r0 = rt * 2 * kRows;
     const int end = min(r0 + 2 * kRows, rows) - 1;
-    range_of(sq, c, b, a.window, a.by_group.div(r0), a.by_group.div(end), lo, hi);
+    range_of<kTok>(sq, c, b, a.window, a.by_group.div(r0), a.by_group.div(end), lo, hi);
     part_of<kTok>(a, sp, lo, hi);
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const int f = r0 + x * kRows, l = min(f + kRows, rows) - 1;
       int l2 = 0, h2 = 0;
-      if (f < rows) range_of(sq, c, b, a.window, a.by_group.div(f), a.by_group.div(l), l2, h2);
+      if (f < rows) range_of<kTok>(sq, c, b, a.window, a.by_group.div(f), a.by_group.div(l), l2, h2);
       h2 = min(h2, hi);
       n_x[x] = h2 > lo ? (h2 - lo + kTok - 1) / kTok : 0;
     }
@@ -227,32 +365,42 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, tre_diag* diag) {
         for (int k = 0; k < L::BARS; ++k)
           asm volatile("mbarrier.inval.shared.b64 [%0];" ::"r"(smem_of(bars + k)) : "memory");
       for (int k = 0; k < L::RING; ++k) {
-        bar_init(full + k, 128);
+        bar_init(full + k, kCopyWarps);
         bar_init(empty + k, 1);
       }
-      for (int k = 0; k < L::META; ++k) bar_init(meta + k, 128);
+      for (int k = 0; k < L::META; ++k) bar_init(meta + k, 4);
       for (int x = 0; x < 2; ++x) {
         bar_init(s_full + x, 1);
-        bar_init(p_full + x, 128);
+        bar_init(p_full + x, kRowWarps / 2);
         bar_init(o_done + x, 1);
       }
-      bar_init(q_full, 256);
+      bar_init(q_full, kRowWarps);
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     tmem_before();
     __syncthreads();
     tmem_after();
-    tmem = *tmem_at;
+    tmem = __shfl_sync(0xffffffffu, *tmem_at, 0);
   };
 
-  // Registers move once: 184 for the row warps, 96 for the copies, 48 for the rest,
-  // together the launch's 4 x 128 (in groups of four warps).
-  if (warp < 8) {
+  auto finish = [&]() {
+    __syncthreads();
+    if (warp == kMmaWarp) {
+      tmem_after();
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(*tmem_at));
+    }
+    if (tid == 0 && *dead && diag) diag->err = TRE_ETIMEOUT;
+  };
+
+  // Registers move once, from the launch's 3 x 168 (in groups of four warps) to twice
+  // 208 for the rows and 88 for copies and products.
+  if (warp < kRowWarps) {
     // ---- rows --------------------------------------------------------------
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     for (int rt = rt0; rt * 2 * kRows < rows; rt += a.row_tiles) {
       turn(rt);
-      const int x = warp >> 2, row = (warp & 3) * 32 + lane, r = r0 + x * kRows + row;
+      const int x = warp >> 2, row = (warp & 3) * 32 + lane;
+      const int r = r0 + x * kRows + row;
       const int n_mine = n_x[x];
       // queries: 16-byte pieces, neighbouring lanes along a row
       {
@@ -273,10 +421,9 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, tre_diag* diag) {
           *reinterpret_cast<uint4*>(q_s + hf * (kRows * 128) + rr * 128 + ((pc ^ (rr & 7)) << 4)) = v;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        bar_arrive(q_full);
+        bar_arrive_warp(q_full);
       }
-      const int tok = a.by_group.div(min(r, rows - 1));
-      const int pos = base + tok;
+      const int pos = base + a.by_group.div(min(r, rows - 1));
       const int first = base + a.by_group.div(r0 + x * kRows < rows ? r0 + x * kRows : 0);
       const int last = base + a.by_group.div(min(r0 + x * kRows + kRows, rows) - 1);
       const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -291,59 +438,57 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, tre_diag* diag) {
           break;
         }
         tmem_after();
-        uint32_t s[kTok];
+        uint32_t v[kTok];
 #pragma unroll
-        for (int h = 0; h < 4; ++h) tmem_ld32(s_at + 32 * h, s + 32 * h);
-        tmem_wait_ld();
+        for (int h = 0; h < 4; ++h) tmem_ld32(s_at + 32 * h, v + 32 * h);
         const int j0 = lo + k * kTok;
         const uint4 held = *reinterpret_cast<const uint4*>(mask_s + ms * 4);
         const bool whole = (held.x & held.y & held.z & held.w) == 0xffffffffu &&
                            j0 + kTok - 1 <= first && (a.window == 0 || j0 > last - a.window);
-        const float4* ks4 = reinterpret_cast<const float4*>(scale_s + ms * 3 * kTok);
-        const float4* vs4 = ks4 + kTok / 4;
-        const float4* lv4 = vs4 + kTok / 4;
+        const float* meta_s = scale_s + ms * 3 * kTok;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) tmem_wait_ld(v + 32 * h);
         if constexpr (L::CODED) {
 #pragma unroll
-          for (int e = 0; e < kTok / 4; ++e) {
-            const float4 f = ks4[e];
-            s[4 * e] = __float_as_uint(__uint_as_float(s[4 * e]) * f.x);
-            s[4 * e + 1] = __float_as_uint(__uint_as_float(s[4 * e + 1]) * f.y);
-            s[4 * e + 2] = __float_as_uint(__uint_as_float(s[4 * e + 2]) * f.z);
-            s[4 * e + 3] = __float_as_uint(__uint_as_float(s[4 * e + 3]) * f.w);
+          for (int e = 0; e < kTok; e += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(meta_s + e);
+            mul2(v + e, f.x, f.y);
+            mul2(v + e + 2, f.z, f.w);
           }
         }
         if (!whole) {
           const uint32_t hw[4] = {held.x, held.y, held.z, held.w};
-          const int top = pos - j0, bottom = a.window ? pos - a.window + 1 - j0 : 0;
 #pragma unroll
           for (int h = 0; h < 4; ++h) {
-            const int t = min(max(top - 32 * h + 1, 0), 32), u = min(max(bottom - 32 * h, 0), 32);
-            const uint32_t below = t == 32 ? 0xffffffffu : (1u << t) - 1;
-            const uint32_t above = u == 32 ? 0u : 0xffffffffu << u;
-            const uint32_t see = hw[h] & below & above;
+            const int to = min(max(pos - j0 - 32 * h + 1, 0), 32);
+            const int from = a.window ? min(max(pos - a.window + 1 - j0 - 32 * h, 0), 32) : 0;
+            const uint32_t see = hw[h] & (to == 32 ? 0xffffffffu : (1u << to) - 1) &
+                                 (from == 32 ? 0u : 0xffffffffu << from);
 #pragma unroll
             for (int e = 0; e < 32; ++e)
-              if (!(see >> e & 1)) s[32 * h + e] = 0xff800000u;
+              if (!(see >> e & 1)) v[32 * h + e] = 0xff800000u;
           }
         }
         float t0 = -INFINITY, t1 = -INFINITY, t2 = -INFINITY, t3 = -INFINITY;
-        if constexpr (L::CODED) {
-          // a value's scale counts in its weight: the largest weight is below one
 #pragma unroll
-          for (int e = 0; e < kTok / 4; ++e) {
-            const float4 f = lv4[e];
-            t0 = fmaxf(t0, __uint_as_float(s[4 * e]) + f.x);
-            t1 = fmaxf(t1, __uint_as_float(s[4 * e + 1]) + f.y);
-            t2 = fmaxf(t2, __uint_as_float(s[4 * e + 2]) + f.z);
-            t3 = fmaxf(t3, __uint_as_float(s[4 * e + 3]) + f.w);
-          }
-        } else {
+        for (int e = 0; e < kTok; e += 8) {
+          if constexpr (L::CODED) {
+            // a value's scale counts in its weight: the largest weight is below one by
+            // the scale's power of two
 #pragma unroll
-          for (int e = 0; e < kTok; e += 4) {
-            t0 = fmaxf(t0, __uint_as_float(s[e]));
-            t1 = fmaxf(t1, __uint_as_float(s[e + 1]));
-            t2 = fmaxf(t2, __uint_as_float(s[e + 2]));
-            t3 = fmaxf(t3, __uint_as_float(s[e + 3]));
+            for (int y = 0; y < 8; y += 4) {
+              const float4 f = *reinterpret_cast<const float4*>(meta_s + 2 * kTok + e + y);
+              uint32_t z[4] = {v[e + y], v[e + y + 1], v[e + y + 2], v[e + y + 3]};
+              add2(z, f.x, f.y);
+              add2(z + 2, f.z, f.w);
+              t0 = max3(t0, __uint_as_float(z[0]), __uint_as_float(z[1]));
+              t1 = max3(t1, __uint_as_float(z[2]), __uint_as_float(z[3]));
+            }
+          } else {
+            t0 = max3(t0, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
+            t1 = max3(t1, __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3]));
+            t2 = max3(t2, __uint_as_float(v[e + 4]), __uint_as_float(v[e + 5]));
+            t3 = max3(t3, __uint_as_float(v[e + 6]), __uint_as_float(v[e + 7]));
           }
         }
         float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3));
@@ -354,51 +499,51 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, tre_diag* diag) {
           m = mn;
           l *= f;
           if (k > 0) {
+#pragma unroll 1
+            for (int h = 0; h < DIM / 16; ++h) {
+              uint32_t o[16];
+              tmem_ld16(o_at + 16 * h, o);
 #pragma unroll
-            for (int h = 0; h < DIM / 32; ++h) {
-              uint32_t o[32];
-              tmem_ld32(o_at + 32 * h, o);
-              tmem_wait_ld();
-#pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-              tmem_st32(o_at + 32 * h, o);
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+              tmem_st16(o_at + 16 * h, o);
             }
           }
         }
         const float use = m == -INFINITY ? 0.f : m;
-        float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
+        uint64_t l0 = 0, l1 = 0;                 // pairs of sums
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t p[32];
+        for (int h = 0; h < 4; ++h) {
+          uint32_t p[16];
 #pragma unroll
-          for (int e = 0; e < 64; e += 4) {
-            const int at = 64 * h + e;
+          for (int e = 32 * h; e < 32 * h + 32; e += 4) {
+            if constexpr (L::CODED) {
+              add2(v + e, -use, -use);
+              add2(v + e + 2, -use, -use);
+            } else {
+              fma2(v + e, a.scale2, -use);
+              fma2(v + e + 2, a.scale2, -use);
+            }
             float y[4];
 #pragma unroll
-            for (int z = 0; z < 4; ++z) {
-              const float v = __uint_as_float(s[at + z]);
-              y[z] = exp2_fast(L::CODED ? v - use : __fmaf_rn(v, a.scale2, -use));
-            }
-            l0 += y[0];
-            l1 += y[1];
-            l2 += y[2];
-            l3 += y[3];
+            for (int z = 0; z < 4; ++z) y[z] = exp2_fast(__uint_as_float(v[e + z]));
+            l0 = sum2(l0, y[0], y[1]);
+            l1 = sum2(l1, y[2], y[3]);
             if constexpr (L::CODED) {
-              const float4 f = vs4[at / 4];
+              const float4 f = *reinterpret_cast<const float4*>(meta_s + kTok + e);
               const float w[4] = {f.x, f.y, f.z, f.w};
+              // (a masked position's scale may be anything: its weight stays zero)
 #pragma unroll
-              for (int z = 0; z < 4; ++z)
-                y[z] = !whole && s[at + z] == 0xff800000u ? 0.f : y[z] * w[z];
+              for (int z = 0; z < 4; ++z) y[z] = !whole && y[z] == 0.f ? 0.f : y[z] * w[z];
             }
-            p[e / 2] = pack<T>(y[0], y[1]);
-            p[e / 2 + 1] = pack<T>(y[2], y[3]);
+            p[(e - 32 * h) / 2] = pack<T>(y[0], y[1]);
+            p[(e - 32 * h) / 2 + 1] = pack<T>(y[2], y[3]);
           }
-          tmem_st32(s_at + 32 * h, p);
+          tmem_st16(s_at + 16 * h, p);
         }
-        l += (l0 + l1) + (l2 + l3);
+        l += halves_sum(l0, l1);
         tmem_wait_st();
         tmem_before();
-        bar_arrive(p_full + x);
+        bar_arrive_warp(p_full + x);
       }
       if (alive && n_mine > 0 && !bar_wait(o_done + x, 0, dead)) alive = false;
       tmem_after();
@@ -406,6 +551,7 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, tre_diag* diag) {
       // ---- a thread writes its row ------------------------------------------
       // (a row without weight gives zeros, whatever was multiplied for it)
       const bool mine = r < rows && alive;
+      const int tok = a.by_group.div(min(r, rows - 1));
       const int h_q = kvh * a.group + (min(r, rows - 1) - tok * a.group);
       const int64_t t_row = (int64_t)(sq.start + tok);
       const float by = m == -INFINITY ? 0.f : a.parts > 1 ? 1.f : div_rn(1.f, l);
@@ -416,7 +562,7 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, tre_diag* diag) {
         uint32_t o[32];
         if (n_mine > 0) {
           tmem_ld32(o_at + 32 * h, o);
-          tmem_wait_ld();
+          tmem_wait_ld(o);
         }
         float y[32];
 #pragma unroll
@@ -426,15 +572,15 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, tre_diag* diag) {
         }
         if (mine) {
           if (a.parts > 1) {
-            float4* p = reinterpret_cast<float4*>(a.part_o + at * DIM + 32 * h);
+            float4* q = reinterpret_cast<float4*>(a.part_o + at * DIM + 32 * h);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              p[e] = make_float4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
+              q[e] = make_float4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
           } else {
-            uint4* p = reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.out) + t_row * a.o_row +
+            uint4* q = reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.out) + t_row * a.o_row +
                                                 h_q * a.o_head + 32 * h);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) p[e] = Vec<T>::put(y + 8 * e);
+            for (int e = 0; e < 4; ++e) q[e] = Vec<T>::put(y + 8 * e);
           }
         }
       }
@@ -463,133 +609,199 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, tre_diag* diag) {
       }
       tmem_before();
     }
-  } else if (warp < 12) {
+    return finish();
+  }
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+  if (warp < kMmaWarp) {
     // ---- copies --------------------------------------------------------------
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
     for (int rt = rt0; rt * 2 * kRows < rows; rt += a.row_tiles) {
       turn(rt);
-      const int t = tid - 256;                 // the token whose place this thread finds
+      const int cw = warp - kCopyWarp;
       constexpr int CB = L::CODED ? 1 : 2, PPT = DIM * CB / 16;    // 16-byte pieces of a token
-      const int piece = t % PPT, tok0 = t / PPT;
-      constexpr int TPI = 128 / PPT, ITS = kTok / TPI;
-      int page = -1, slot = 0;
-      auto look = [&](int k) {
-        const int j = lo + k * kTok + t;
-        page = k < n && j < hi ? page_of(c, b, i, j, slot) : -1;
-      };
-      auto note = [&](int k) {                 // its place, mask bit and scales, for tile k
-        const bool there = page >= 0;
-        off_s[(k & 1) * kTok + t] =
-            there ? (page * c.s_page + slot * c.s_token + kvh * c.s_head) * CB : -1;
-        const unsigned held = __ballot_sync(0xffffffffu, there);
-        const int ms = k % L::META;
-        if (lane == 0) mask_s[ms * 4 + (t >> 5)] = held;
-        if constexpr (L::CODED) {
-          float ks = 0.f, vs = 0.f;
-          if (there) {
-            const int64_t o = page * c.c_page + slot * c.c_token + kvh * c.c_head;
-            ks = c.k_scale[o] * a.scale2;
-            vs = c.v_scale[o];
+      constexpr int STEPS = kTok * PPT / 32, TPS = 32 / PPT;       // 32 pieces a step of a warp
+      const int piece = lane % PPT, tok0 = lane / PPT;
+      // A warp copies the tokens of steps cw, cw + 3, ..; its lanes find their places,
+      // and those of the mask and scales: groups of 32 tokens, warp cw group cw and the
+      // first warp group 3 too.
+      // (What the tables say is looked at a tile later: nothing waits for it.)
+      int64_t off[2] = {-1, -1};
+      Ask list[2], group[2];
+      auto look = [&](int k, bool pieces) {
+        const int j0 = lo + k * kTok, end = k < n ? hi : 0;
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          if (pieces) {
+            const int q = g * 32 + lane, st = cw + kCopyWarps * (q / TPS);
+            list[g].at(c, b, i, j0 + st * TPS + q % TPS, st < STEPS ? end : 0);
           }
-          scale_s[ms * 3 * kTok + t] = ks;
-          scale_s[ms * 3 * kTok + kTok + t] = vs;
-          scale_s[ms * 3 * kTok + 2 * kTok + t] = weight_exponent(vs);
+          if (g == 0 || cw == 0) group[g].at(c, b, i, j0 + (g ? 96 : cw * 32) + lane, end);
         }
-        bar_arrive(meta + ms);
       };
-      look(0);
+      auto take = [&]() {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const int pg = list[g].page(c);
+          off[g] = pg < 0 ? -1
+                          : (pg * c.s_page + list[g].slot * c.s_token + kvh * c.s_head) * CB;
+        }
+      };
+      auto place = [&](int i_step) {           // of this lane's piece in the warp's step
+        const int q = i_step * TPS + tok0;
+        const int64_t x = __shfl_sync(0xffffffffu, off[0], q & 31);
+        const int64_t y = __shfl_sync(0xffffffffu, off[1], q & 31);
+        return q < 32 ? x : y;
+      };
+      auto note = [&](int k) {                 // mask bits and scales, for tile k
+        const int ms = k % L::META;
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          if (g == 1 && cw != 0) break;
+          const int t = (g ? 96 : cw * 32) + lane;
+          const int pg = group[g].page(c);
+          const bool there = pg >= 0;
+          const unsigned held = __ballot_sync(0xffffffffu, there);
+          if (lane == 0) mask_s[ms * 4 + (t >> 5)] = held;
+          if constexpr (L::CODED) {
+            float ks = 0.f, vs = 0.f;
+            if (there) {
+              const int64_t o = pg * c.c_page + group[g].slot * c.c_token + kvh * c.c_head;
+              ks = c.k_scale[o] * a.scale2;
+              vs = c.v_scale[o];
+            }
+            scale_s[ms * 3 * kTok + t] = ks;
+            scale_s[ms * 3 * kTok + kTok + t] = vs;
+            scale_s[ms * 3 * kTok + 2 * kTok + t] = weight_exponent(vs);
+          }
+          bar_arrive_warp(meta + ms);
+        }
+      };
+      // Boxes of whole tiles: a lane of the first warp knows each box's page (one that
+      // the cache does not have where the table names none: its rows come as zeros).
+      const int box = L::CODED ? 0 : maps.box, boxes = box ? kTok / box : 0;
+      auto whole_box = [&](int k) { return box > 0 && lo + (k + 1) * kTok <= hi; };
+      Ask boxed;
+      int box_page = 0, box_slot = 0;
+      look(0, !whole_box(0));
+      if (lane < boxes) boxed.at(c, b, i, lo + lane * box, hi);
+      int pending = -1;                        // a tile copied by pieces, not yet announced
       bool alive = true;
 #pragma unroll 1
-      for (int k = 0; k < n; ++k) {
+      for (int k = 0; k < n && alive; ++k) {
+        const bool by_box = !L::CODED && whole_box(k);
         note(k);
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        look(k + 1);
-        const int64_t* off = off_s + (k & 1) * kTok;
+        if (!by_box) take();
+        box_page = boxed.page(c);
+        if (box_page < 0) box_page = c.n_pages;
+        box_slot = boxed.slot;
+        look(k + 1, !whole_box(k + 1));
+        if (lane < boxes) boxed.at(c, b, i, lo + (k + 1) * kTok + lane * box, k + 1 < n ? hi : 0);
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
           const int seq = 2 * k + kv, buf = seq % L::RING;
-          const uint8_t* src = kv ? c.v : c.k;
+          const uint8_t* src = (kv ? c.v : c.k) + piece * 16;
           uint8_t* dst = sm + L::AT_RING + buf * L::BUF;
-          if constexpr (!L::CODED) {
-            alive = alive && bar_wait(empty + buf, ((seq / L::RING) & 1) ^ 1, dead);
-            if (!alive) break;           // (not out of the loop over k: its barrier is shared)
-            const uint32_t to = smem_of(dst) + (piece >> 3) * (kTok * 128);
+          alive = alive && bar_wait(empty + buf, ((seq / L::RING) & 1) ^ 1, dead);
+          if (!alive) break;
+          if (by_box) {
+            if (cw == 0) {
+              if (one_lane()) bar_expect(full + buf, L::BUF);
+              for (int x = 0; x < boxes; ++x) {
+                const int pg = __shfl_sync(0xffffffffu, box_page, x);
+                const int sl = __shfl_sync(0xffffffffu, box_slot, x);
+                if (one_lane()) {
+                  const uint32_t to = smem_of(dst) + x * box * 128;
 #pragma unroll
-            for (int it = 0; it < ITS; ++it) {
-              const int tk = tok0 + it * TPI;
-              const int64_t o = off[tk];
-              const uint8_t* p = src + (o < 0 ? 0 : o + piece * 16);
+                  for (int h = 0; h < DIM / 64; ++h)
+                    box_load(to + h * (kTok * 128), kv ? &maps.v : &maps.k, h * 64, sl, kvh, pg,
+                             full + buf);
+                }
+              }
+            } else if (lane == 0) {
+              bar_arrive(full + buf);
+            }
+          } else if constexpr (!L::CODED) {
+            const uint32_t to = smem_of(dst) + (piece >> 3) * (kTok * 128);
+#pragma unroll 4
+            for (int is = 0; is < (STEPS + 2) / kCopyWarps; ++is) {
+              const int64_t o = place(is);
+              const int st = cw + is * kCopyWarps, tk = tok0 + st * TPS;
+              if (st >= STEPS) break;
               asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
                                to + tk * 128 + (((piece & 7) ^ (tk & 7)) << 4)),
-                           "l"(p), "r"(o < 0 ? 0 : 16)
+                           "l"(src + (o < 0 ? 0 : o)), "r"(o < 0 ? 0 : 16)
                            : "memory");
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
-            if (seq > 0) {
+            if (pending >= 0) {
               asm volatile("cp.async.wait_group 1;" ::: "memory");
               asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-              bar_arrive(full + (seq - 1) % L::RING);
+              bar_arrive_warp(full + pending);
             }
+            pending = buf;
           } else {
-            uint4 v[ITS];
-#pragma unroll
-            for (int it = 0; it < ITS; ++it) {
-              const int64_t o = off[tok0 + it * TPI];
-              v[it] = make_uint4(0, 0, 0, 0);
-              if (o >= 0) v[it] = *reinterpret_cast<const uint4*>(src + o + piece * 16);
-            }
-            alive = alive && bar_wait(empty + buf, ((seq / L::RING) & 1) ^ 1, dead);
-            if (!alive) break;
             // 16 codes are two 16-byte pieces of a row
             uint8_t* to = dst + (piece >> 2) * (kTok * 128);
             const int pc = (piece & 3) * 2;
+            constexpr int U = 4;
+#pragma unroll 1
+            for (int is = 0; is * kCopyWarps + cw < STEPS; is += U) {
+              const int st = cw + is * kCopyWarps;
+              uint4 v[U];
 #pragma unroll
-            for (int it = 0; it < ITS; ++it) {
-              const int tk = tok0 + it * TPI;
-              uint4 w0, w1;
-              widen<T, CODE>(v[it], w0, w1);
-              *reinterpret_cast<uint4*>(to + tk * 128 + ((pc ^ (tk & 7)) << 4)) = w0;
-              *reinterpret_cast<uint4*>(to + tk * 128 + (((pc + 1) ^ (tk & 7)) << 4)) = w1;
+              for (int u = 0; u < U; ++u) {
+                const int64_t o = place(is + u);       // (-1 past the last step)
+                v[u] = make_uint4(0, 0, 0, 0);
+                if (o >= 0) v[u] = *reinterpret_cast<const uint4*>(src + o);
+              }
+#pragma unroll
+              for (int u = 0; u < U; ++u) {
+                const int s = st + u * kCopyWarps, tk = tok0 + s * TPS;
+                if (s >= STEPS) break;
+                uint4 w0, w1;
+                widen<T, CODE>(v[u], w0, w1);
+                *reinterpret_cast<uint4*>(to + tk * 128 + ((pc ^ (tk & 7)) << 4)) = w0;
+                *reinterpret_cast<uint4*>(to + tk * 128 + (((pc + 1) ^ (tk & 7)) << 4)) = w1;
+              }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            bar_arrive(full + buf);
+            bar_arrive_warp(full + buf);
           }
         }
       }
       if constexpr (!L::CODED) {
         asm volatile("cp.async.wait_group 0;" ::: "memory");
-        if (alive && n > 0) {
+        if (alive && pending >= 0) {
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          bar_arrive(full + (2 * n - 1) % L::RING);
+          bar_arrive_warp(full + pending);
         }
       }
     }
   } else {
     // ---- products --------------------------------------------------------------
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     for (int rt = rt0; rt * 2 * kRows < rows; rt += a.row_tiles) {
       turn(rt);
-      if (warp == 12) {
+      {
         constexpr uint32_t id_s = idesc_of<T>(kTok, false), id_o = idesc_of<T>(DIM, true);
-        const uint32_t q_at = smem_of(sm), ring_at = smem_of(sm + L::AT_RING);
+        const uint32_t q_op = operand(smem_of(sm), 16);
+        const uint32_t k_op = operand(smem_of(sm + L::AT_RING), 16);
+        const uint32_t v_op = operand(smem_of(sm + L::AT_RING), kTok * 128);
         auto scores = [&](int x, int buf) {
-          if (lane == 0) {
+          const uint32_t qa = q_op + x * (kRows * DIM * 2 >> 4), ka = k_op + buf * (L::BUF >> 4);
+          const uint32_t d = tmem + x * kTok;
 #pragma unroll
-            for (int k = 0; k < DIM / 16; ++k) {
-              const uint32_t step = (k / 4) * (kTok * 128) + (k % 4) * 32;
-              mma_ss(tmem + x * kTok, operand(q_at + x * kRows * DIM * 2 + step, 16),
-                     operand(ring_at + buf * L::BUF + step, 16), id_s, k > 0);
-            }
-            commit(s_full + x);
+          for (int k = 0; k < DIM / 16; ++k) {
+            const uint32_t step = ((k / 4) * (kTok * 128) + (k % 4) * 32) >> 4;
+            mma_ss(d, qa + step, ka + step, id_s, k > 0);
           }
+          commit(s_full + x);
         };
         bool alive = n > 0 && bar_wait(q_full, 0, dead) && bar_wait(full, 0, dead);
         if (alive) {
           tmem_after();
 #pragma unroll
           for (int x = 0; x < 2; ++x)
-            if (n_x[x] > 0) scores(x, 0);
-          if (lane == 0 && L::RING < 2 * n) commit(empty);
+            if (n_x[x] > 0 && one_lane()) scores(x, 0);
+          if (L::RING < 2 * n && one_lane()) commit(empty);
         }
 #pragma unroll 1
         for (int k = 0; k < n && alive; ++k) {
@@ -604,12 +816,12 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, tre_diag* diag) {
                 break;
               }
               tmem_after();
-              if (lane == 0) {
+              if (one_lane()) {
+                const uint32_t va = v_op + vb * (L::BUF >> 4), d = tmem + 256 + x * 128;
+                const uint32_t pa = tmem + x * kTok;
 #pragma unroll
                 for (int s = 0; s < kTok / 16; ++s)
-                  mma_ts(tmem + 256 + x * 128, tmem + x * kTok + s * 8,
-                         operand(ring_at + vb * L::BUF + s * 2048, kTok * 128), id_o,
-                         k > 0 || s > 0);
+                  mma_ts(d, pa + s * 8, va + s * (2048 >> 4), id_o, k > 0 || s > 0);
                 if (k == n_x[x] - 1) commit(o_done + x);
               }
             }
@@ -620,10 +832,10 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, tre_diag* diag) {
               }
               have = true;
               tmem_after();
-              scores(x, kb);
+              if (one_lane()) scores(x, kb);
             }
           }
-          if (alive && lane == 0) {
+          if (alive && one_lane()) {
             // only where the copies go round once more, so that no arrival is left over
             if (2 * k + 1 + L::RING < 2 * n) commit(empty + vb);
             if (2 * k + 2 + L::RING < 2 * n) commit(empty + kb);
@@ -633,12 +845,54 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, tre_diag* diag) {
       }
     }
   }
-  __syncthreads();
-  if (warp == 12) {
-    tmem_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(*tmem_at));
+  finish();
+}
+
+// The driver's encoder of tensor maps, looked up once (it is not part of the runtime).
+using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
+                            const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                            const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                            CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+Encode encoder() {
+  static const Encode fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
+                                         &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      p = nullptr;
+    }
+    return reinterpret_cast<Encode>(p);
+  }();
+  return fn;
+}
+
+// Maps of a cache of 16-bit elements. Tiles start at multiples of 128, so a box of the
+// greatest common divisor of 128 and the page lies in one page; below 8 slots (or where
+// the encoder refuses the strides) tiles are copied by pieces.
+void make_maps(Maps& m, const CacheArgs& c, int dtype, int dim) {
+  m.box = 0;
+  const int box = std::gcd(c.page, kTok);
+  const Encode enc = box >= 8 && c.n_pages > 0 ? encoder() : nullptr;
+  if (!enc) return;
+  const int64_t st[3] = {c.s_token * 2, c.s_head * 2, c.s_page * 2};
+  cuuint64_t strides[3];
+  for (int x = 0; x < 3; ++x) {
+    if (st[x] <= 0 || st[x] >= (1ll << 40)) return;
+    strides[x] = (cuuint64_t)st[x];
   }
-  if (tid == 0 && *dead && diag) diag->err = TRE_ETIMEOUT;
+  const cuuint64_t dims[4] = {(cuuint64_t)dim, (cuuint64_t)c.page, (cuuint64_t)c.heads,
+                              (cuuint64_t)c.n_pages};
+  const cuuint32_t size[4] = {64, (cuuint32_t)box, 1, 1}, one[4] = {1, 1, 1, 1};
+  const CUtensorMapDataType type =
+      dtype == TRE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  for (int x = 0; x < 2; ++x)
+    if (enc(x ? &m.v : &m.k, type, 4, x ? c.v : c.k, dims, strides, size, one,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return;
+  m.box = box;
 }
 
 template <class T, Code CODE, int DIM>
@@ -650,7 +904,11 @@ cudaError_t launch_typed(const AttendArgs& a, const BatchArgs& b, const CacheArg
   if (e) return e;
   const int64_t blocks = (int64_t)c.heads * a.parts * b.n_seq * a.row_tiles;
   if (blocks > 2147483647) return cudaErrorInvalidValue;
-  k_attend_tc<T, CODE, DIM><<<(unsigned)blocks, kThreads, L::SMEM, s>>>(a, b, c, diag);
+  Maps maps;
+  memset(&maps, 0, sizeof(maps));
+  if (CODE == Code::kHalf)
+    make_maps(maps, c, std::is_same<T, __nv_bfloat16>::value ? TRE_BF16 : TRE_F16, DIM);
+  k_attend_tc<T, CODE, DIM><<<(unsigned)blocks, kThreads, L::SMEM, s>>>(a, b, c, maps, diag);
   return cudaGetLastError();
 }
 
