@@ -454,9 +454,10 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
         row_again<T, CODE, DIM>(a, b, c, i, kvh,
                                 reinterpret_cast<const T*>(a.q) + row * a.q_row + h * a.q_head,
                                 base + t, lo, hi, top, x);
-      if (lane == 0) row_state(a, b, sp, row, h, top, sum);
+      const int64_t part_row = a.tokens > 0 ? (int64_t)i * a.tokens + t : row;
+      if (lane == 0) row_state(a, sp, row, part_row, h, top, sum);
       if (a.parts > 1) {
-        const int64_t at = ((int64_t)sp * b.n_rows + row) * a.heads + h;
+        const int64_t at = (sp * a.part_rows + part_row) * a.heads + h;
         float* p = a.part_o + at * DIM + lane * EL;
         if (sum > 0.f || sum != sum) {
           if constexpr (EL == 4) *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
@@ -474,17 +475,30 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
   }
 }
 
-// Joins the parts of each row: one warp a (row, head).
+// Joins the parts of each row: a block a part row, a warp a (row, head).
+constexpr int kJoinWarps = 8;
 template <class T, int DIM>
-__global__ void __launch_bounds__(128) k_join(AttendArgs a, int64_t rows_heads) {
-  const int lane = threadIdx.x & 31;
-  const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-  if (w >= rows_heads) return;
+__global__ void __launch_bounds__(kJoinWarps * 32)
+k_join(AttendArgs a, BatchArgs b) {
+  const int lane = threadIdx.x & 31, h = blockIdx.y * kJoinWarps + (threadIdx.x >> 5);
+  if (h >= a.heads) return;
+  int64_t t = blockIdx.x;
+  if (a.tokens > 0) {
+    const int i = blockIdx.x / a.tokens, r = blockIdx.x - i * a.tokens;
+    const Seq s = seq_of(b, i);
+    if (r >= s.n || s.n * a.group > a.few) return;
+    t = s.start + r;
+  }
+  const int64_t w = (int64_t)blockIdx.x * a.heads + h, rows_heads = a.part_rows * a.heads;
   constexpr int EL = DIM / 32;
-  if (a.part_ml[2 * w + 1] < 0.f) return;       // written already
-  float top = -INFINITY;
-  for (int sp = lane; sp < a.n_split; sp += 32)
-    top = fmaxf(top, a.part_ml[2 * (sp * rows_heads + w)]);
+  const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
+  float top = -INFINITY, first = 0.f;
+  for (int sp = lane; sp < a.parts; sp += 32) {
+    const float2 v = ml[sp * rows_heads + w];
+    if (sp == 0) first = v.y;
+    top = fmaxf(top, v.x);
+  }
+  if (__shfl_sync(0xffffffffu, first, 0) < 0.f) return;         // not this join's
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
   float sum = 0.f, x[EL];
@@ -492,33 +506,32 @@ __global__ void __launch_bounds__(128) k_join(AttendArgs a, int64_t rows_heads) 
   for (int e = 0; e < EL; ++e) x[e] = 0.f;
   if (top > -INFINITY) {
 #pragma unroll 4
-    for (int sp = 0; sp < a.n_split; ++sp) {
+    for (int sp = 0; sp < a.parts; ++sp) {
       const int64_t at = sp * rows_heads + w;
-      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * at);
-      if (ml.x == -INFINITY) continue;
-      const float f = exp2_fast(ml.x - top);
-      sum = __fmaf_rn(ml.y, f, sum);
+      const float2 v = ml[at];
+      if (v.x == -INFINITY) continue;
+      const float f = exp2_fast(v.x - top);
+      sum = __fmaf_rn(v.y, f, sum);
       const float* p = a.part_o + at * DIM + lane * EL;
       float y[EL];
       if constexpr (EL == 4) {
-        const float4 v = *reinterpret_cast<const float4*>(p);
-        y[0] = v.x; y[1] = v.y; y[2] = v.z; y[3] = v.w;
+        const float4 u = *reinterpret_cast<const float4*>(p);
+        y[0] = u.x; y[1] = u.y; y[2] = u.z; y[3] = u.w;
       } else {
-        const float2 v = *reinterpret_cast<const float2*>(p);
-        y[0] = v.x; y[1] = v.y;
+        const float2 u = *reinterpret_cast<const float2*>(p);
+        y[0] = u.x; y[1] = u.y;
       }
 #pragma unroll
       for (int e = 0; e < EL; ++e) x[e] = __fmaf_rn(y[e], f, x[e]);
     }
   }
-  const int64_t t = w / a.heads, h = w - t * a.heads;
   const float by = top == -INFINITY ? 0.f : div_rn(1.f, sum);
   T* p = reinterpret_cast<T*>(a.out) + t * a.o_row + h * a.o_head + lane * EL;
 #pragma unroll
   for (int e = 0; e < EL; e += 2)
     *reinterpret_cast<uint32_t*>(p + e) = pack<T>(x[e] * by, x[e + 1] * by);
   if (a.lse && lane == 0)
-    a.lse[w] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * kLn2;
+    a.lse[t * a.heads + h] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
 template <class T, Code CODE, int DIM>
@@ -549,18 +562,21 @@ cudaError_t launch_code(int code, int dim, const AttendArgs& a, const BatchArgs&
 
 template <class T>
 cudaError_t launch_join(int dim, const AttendArgs& a, const BatchArgs& b, cudaStream_t s) {
-  const int64_t rh = (int64_t)b.n_rows * a.heads;
-  const unsigned blocks = (unsigned)((rh + 3) / 4);
-  if (dim == 64) k_join<T, 64><<<blocks, 128, 0, s>>>(a, rh);
-  else k_join<T, 128><<<blocks, 128, 0, s>>>(a, rh);
+  if (a.part_rows > 2147483647) return cudaErrorInvalidValue;
+  const dim3 grid((unsigned)a.part_rows, (a.heads + kJoinWarps - 1) / kJoinWarps);
+  if (dim == 64) k_join<T, 64><<<grid, kJoinWarps * 32, 0, s>>>(a, b);
+  else k_join<T, 128><<<grid, kJoinWarps * 32, 0, s>>>(a, b);
   return cudaGetLastError();
 }
 
 // How a call is split, from what the host knows of it.
 struct Plan {
   bool tc;                        // some sequence may have more than `few` rows
-  int32_t few, n_split;
-  int32_t parts[2], split[2], row_tiles[2];     // k_attend, k_attend_tc
+  int32_t few, tokens;            // (see AttendArgs)
+  int32_t parts[2], split[2];     // k_attend, k_attend_tc
+  int64_t part_rows[2];
+  int32_t row_tiles;
+  int64_t units;                  // of k_attend_tc, at most
 };
 
 // Up to 64 rows of a sequence go to k_attend, whose 16-row tiles then read each key
@@ -581,47 +597,69 @@ Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page) {
     // Parts of a context: enough blocks to fill the GPU a few times over, none
     // shorter than 256 tokens (a part costs a block's start and its share of the
     // join, about what 256 tokens of keys and values cost to read).
-    const int64_t r = p.tc ? kFew : rows;
-    p.row_tiles[0] = (int)std::min<int64_t>((r + kTile - 1) / kTile, 1 << 20);
-    const int64_t units = std::max<int64_t>(1, (int64_t)b->n_seq * heads * (p.tc ? 1 : p.row_tiles[0]));
+    p.row_tiles = p.tc ? 1 : (int)std::min<int64_t>((rows + kTile - 1) / kTile, 1 << 20);
+    const int64_t units = std::max<int64_t>(1, (int64_t)b->n_seq * heads * p.row_tiles);
     const int64_t want = std::max<int64_t>(1, (sms * 8 + units - 1) / units);
     p.parts[0] = (int)std::min<int64_t>({want, std::max<int64_t>(1, len / 256), 256});
     p.split[0] = (int)std::max<int64_t>(kTile * kWarps, (len + p.parts[0] - 1) / p.parts[0]);
   }
-  p.n_split = p.parts[0];
+  p.tokens = p.tc ? std::max(1, kFew / a.group) : 0;
+  p.part_rows[0] = p.tc ? (int64_t)b->n_seq * p.tokens : b->n_rows;
+  p.part_rows[1] = b->n_rows;
+  p.parts[1] = 1;
   if (p.tc) {
-    p.row_tiles[1] = (int)std::min<int64_t>((rows + kTcRows - 1) / kTcRows, 1 << 20);
-    const int64_t tiles = std::min<int64_t>((int64_t)b->n_seq * p.row_tiles[1],
-                                            (int64_t)b->n_rows * a.group / kTcRows + b->n_seq);
+    // Whole rounds of one block an SM: the number of parts with the least rounds' worth
+    // of context. A part costs what a row's partial sum costs to write and read, about
+    // 400 positions' products, spread over all SMs; none is shorter than 512.
+    const int64_t tiles = std::min<int64_t>(
+        (int64_t)b->n_seq * ((rows + kTcRows - 1) / kTcRows),
+        (int64_t)b->n_rows * a.group / kTcRows + b->n_seq);
     const int64_t units = std::max<int64_t>(1, tiles * heads);
-    const int64_t want = std::max<int64_t>(1, sms / units);
-    p.parts[1] = (int)std::min<int64_t>({want, std::max<int64_t>(1, len / 512), 64});
+    double least = 0;
+    for (int n = 1; n <= 64 && (n == 1 || len / n >= 512); ++n) {
+      const double rounds = (double)((units * n + sms - 1) / sms);
+      const double cost = rounds / n * len + (n > 1 ? 400.0 * n * units / sms + 2000 : 0);
+      if (n == 1 || cost < least) {
+        least = cost;
+        p.parts[1] = n;
+      }
+    }
     p.split[1] = (int)std::max<int64_t>(kTcTokens, (len + p.parts[1] - 1) / p.parts[1]);
-    p.n_split = std::max(p.n_split, p.parts[1]);
+    p.units = units * p.parts[1];
   }
   return p;
 }
 
 cudaError_t launch_all(int dtype, int code, int dim, AttendArgs a, const Plan& p,
-                       const BatchArgs& b, const CacheArgs& c, tre_diag* diag, cudaStream_t s) {
+                       float* const* part_o, float* const* part_ml, const BatchArgs& b,
+                       const CacheArgs& c, tre_diag* diag, cudaStream_t s) {
+  const bool bf = dtype == TRE_BF16;
   a.few = p.few;
-  a.n_split = p.n_split;
+  auto of = [&](int k) {
+    AttendArgs x = a;
+    x.parts = p.parts[k];
+    x.split = p.split[k];
+    x.part_o = part_o[k];
+    x.part_ml = part_ml[k];
+    x.part_rows = p.part_rows[k];
+    return x;
+  };
   cudaError_t e = cudaSuccess;
   if (p.tc) {
-    a.parts = p.parts[1];
-    a.split = p.split[1];
-    a.row_tiles = p.row_tiles[1];
-    e = launch_attend_tc(dtype, code, dim, a, b, c, diag, s);
+    e = launch_attend_tc(dtype, code, dim, of(1), b, c, p.units, diag, s);
     if (e) return e;
   }
-  a.parts = p.parts[0];
-  a.split = p.split[0];
-  a.row_tiles = p.row_tiles[0];
-  const bool bf = dtype == TRE_BF16;
-  e = bf ? launch_code<__nv_bfloat16>(code, dim, a, b, c, s)
-         : launch_code<__half>(code, dim, a, b, c, s);
-  if (e || p.n_split == 1) return e;
-  return bf ? launch_join<__nv_bfloat16>(dim, a, b, s) : launch_join<__half>(dim, a, b, s);
+  AttendArgs x = of(0);
+  x.row_tiles = p.row_tiles;
+  x.tokens = p.tokens;
+  if (p.parts[1] > 1) x.done = reinterpret_cast<float2*>(part_ml[1]);
+  e = bf ? launch_code<__nv_bfloat16>(code, dim, x, b, c, s)
+         : launch_code<__half>(code, dim, x, b, c, s);
+  if (!e && p.parts[0] > 1)
+    e = bf ? launch_join<__nv_bfloat16>(dim, x, b, s) : launch_join<__half>(dim, x, b, s);
+  if (!e && p.parts[1] > 1)
+    e = bf ? launch_join<__nv_bfloat16>(dim, of(1), b, s) : launch_join<__half>(dim, of(1), b, s);
+  return e;
 }
 
 }  // namespace
@@ -654,10 +692,12 @@ extern "C" tre_status tre_chunk_attention(const tre_kv_cache* cache, const tre_k
   Plan plan{};
   if (b.n_seq > 0) plan = plan_of(batch, a, c.heads, c.page);
   Arena arena(ws);
-  if (plan.n_split > 1) {
-    const size_t rh = (size_t)b.n_rows * a.heads;
-    a.part_ml = arena.take<float>(2 * rh * plan.n_split);
-    a.part_o = arena.take<float>(rh * plan.n_split * cache->dim);
+  float *part_o[2] = {}, *part_ml[2] = {};
+  for (int k = 0; k < 2; ++k) {
+    if (plan.parts[k] < 2) continue;
+    const size_t rh = (size_t)plan.part_rows[k] * a.heads * plan.parts[k];
+    part_ml[k] = arena.take<float>(2 * rh);
+    part_o[k] = arena.take<float>(rh * cache->dim);
   }
   if (!ws) {
     *ws_bytes = arena.off;
@@ -676,6 +716,6 @@ extern "C" tre_status tre_chunk_attention(const tre_kv_cache* cache, const tre_k
   a.scale2 = (float)((double)at->scale * 1.4426950408889634);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const cudaError_t e =
-      launch_all(at->dtype, cache->dtype, cache->dim, a, plan, b, c, diag, s);
+      launch_all(at->dtype, cache->dtype, cache->dim, a, plan, part_o, part_ml, b, c, diag, s);
   return e == cudaSuccess ? TRE_OK : TRE_ECUDA;
 }

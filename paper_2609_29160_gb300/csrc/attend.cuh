@@ -18,12 +18,15 @@ struct AttendArgs {
   float scale2;                   // scale * log2(e): scores are kept in powers of two
   int32_t window;                 // 0: none
   int32_t parts, split;           // parts of a context, and the shortest part
-  int32_t row_tiles;              // blocks along a sequence's rows
+  int32_t row_tiles;              // k_attend: blocks along a sequence's rows
   int32_t few;                    // rows of a sequence that k_attend takes
-  // parts of either kernel at most; with more than one, [n_split][n_rows * heads][dim]
-  // sums and [..][2] maxima and weights of theirs
-  int32_t n_split;
+  // Sums, maxima and weights of parts, for the join: [parts][part_rows * heads][dim], [..][2].
+  // tokens > 0: row r of sequence i stands at part row i * tokens + r (only sequences
+  // of few rows have any), else at its own.
   float *part_o, *part_ml;
+  int64_t part_rows;
+  int32_t tokens;
+  float2* done;                   // the other kernel's part_ml: rows that are not its
 };
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -73,18 +76,16 @@ __device__ __forceinline__ void part_of(const AttendArgs& a, int sp, int& lo, in
 }
 
 // What a block leaves beside a row's sum: for its part of the join, or (one part)
-// the row's logarithm, and for the join that the row is done (a weight below zero).
-__device__ __forceinline__ void row_state(const AttendArgs& a, const BatchArgs& b, int sp,
-                                          int64_t row, int head, float m, float l) {
-  const int64_t at = row * a.heads + head, all = (int64_t)b.n_rows * a.heads;
-  if (a.n_split > 1) {
-    float2* ml = reinterpret_cast<float2*>(a.part_ml) + at;
-    ml[sp * all] = a.parts > 1 ? make_float2(m, l) : make_float2(0.f, -1.f);
-    if (sp == 0 && a.parts > 1)
-      for (int s = a.parts; s < a.n_split; ++s) ml[s * all] = make_float2(-INFINITY, 0.f);
-  }
-  if (a.parts == 1 && a.lse)
-    a.lse[at] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * kLn2;
+// the row's logarithm, and for the other kernel's join that the row is not its (a weight
+// below zero).
+__device__ __forceinline__ void row_state(const AttendArgs& a, int sp, int64_t row,
+                                          int64_t part_row, int head, float m, float l) {
+  if (a.parts > 1)
+    reinterpret_cast<float2*>(a.part_ml)[(sp * a.part_rows + part_row) * a.heads + head] =
+        make_float2(m, l);
+  else if (a.lse)
+    a.lse[row * a.heads + head] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * kLn2;
+  if (a.done && sp == 0) a.done[row * a.heads + head] = make_float2(0.f, -1.f);
 }
 
 // The power of two of a value's scale, which counts in its weight: with m the
@@ -161,17 +162,12 @@ __device__ void loose_rows(const AttendArgs& a, const BatchArgs& b) {
   for (int64_t r = threadIdx.x; r < (int64_t)loose * a.heads; r += blockDim.x) {
     const int k = (int)(r / a.heads), h = (int)(r - (int64_t)k * a.heads);
     const int64_t t = k < first ? k : last + (k - first);
-    if (a.n_split > 1) {
-      for (int sp = 0; sp < a.n_split; ++sp) {
-        float* ml = a.part_ml + 2 * (((int64_t)sp * b.n_rows + t) * a.heads + h);
-        ml[0] = -INFINITY;
-        ml[1] = 0.f;
-      }
-    } else {
-      T* o = reinterpret_cast<T*>(a.out) + t * a.o_row + h * a.o_head;
-      for (int e = 0; e < DIM; ++e) o[e] = T(0.f);
-      if (a.lse) a.lse[t * a.heads + h] = -INFINITY;
-    }
+    T* o = reinterpret_cast<T*>(a.out) + t * a.o_row + h * a.o_head;
+    for (int e = 0; e < DIM; ++e) o[e] = T(0.f);
+    if (a.lse) a.lse[t * a.heads + h] = -INFINITY;
+    if (a.done) a.done[t * a.heads + h] = make_float2(0.f, -1.f);
+    if (a.parts > 1 && a.tokens == 0)
+      reinterpret_cast<float2*>(a.part_ml)[t * a.heads + h] = make_float2(0.f, -1.f);
   }
 }
 

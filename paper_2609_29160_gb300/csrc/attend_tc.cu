@@ -286,8 +286,69 @@ template <Code CODE, int DIM> struct Tc {
   static constexpr int AT_MASK = AT_RING + RING * BUF;  // uint32 [META][4]
   static constexpr int AT_SCALE = AT_MASK + META * 16;  // float [META][3][kTok]
   static constexpr int AT_BAR = AT_SCALE + (CODED ? META * 3 * kTok * 4 : 0);
-  static constexpr int BARS = 2 * RING + META + 7;
-  static constexpr int SMEM = AT_BAR + BARS * 8 + 16;
+  static constexpr int BARS = 2 * RING + META + 8;
+  static constexpr int AT_UNIT = AT_BAR + BARS * 8 + 16;       // Unit [kRowWarps]
+  static constexpr int SMEM = AT_UNIT + kRowWarps * 64;
+};
+
+// A block's piece of work: up to 256 rows of a sequence against one part of its context
+// for one cache head. Units go through the sequences' row tiles (of those that are not
+// k_attend's), each sequence's longest ranges first, heads fastest: heads of a tile read
+// neighbouring memory, rows of a head the same.
+struct Unit {
+  int i, kvh, sp, r0, rows, start, base, lo, hi;
+  int n_x[2];                     // 128-token tiles that each half of the rows sees
+  // The whole warp looks; false past the last unit.
+  __device__ __forceinline__ bool find(const AttendArgs& a, const BatchArgs& b,
+                                       const CacheArgs& c, uint32_t u) {
+    const int lane = threadIdx.x & 31;
+    kvh = (int)(u % c.heads);
+    u /= c.heads;
+    sp = (int)(u % a.parts);
+    int t = (int)(u / a.parts);
+    i = -1;
+    int tiles = 0, rt = 0;
+    for (int from = 0; from < b.n_seq; from += 32) {
+      int mine = 0;
+      if (from + lane < b.n_seq) {
+        const int r = seq_of(b, from + lane).n * a.group;
+        mine = r > a.few ? (r + 2 * kRows - 1) / (2 * kRows) : 0;
+      }
+      int upto = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += y;
+      }
+      const unsigned past = __ballot_sync(0xffffffffu, t < upto);
+      if (past) {
+        const int who = __ffs(past) - 1;
+        i = from + who;
+        tiles = __shfl_sync(0xffffffffu, mine, who);
+        rt = tiles - 1 - (int)(t - (__shfl_sync(0xffffffffu, upto, who) - tiles));
+        break;
+      }
+      t -= __shfl_sync(0xffffffffu, upto, 31);
+    }
+    if (i < 0) return false;
+    const Seq s = seq_of(b, i);
+    start = s.start;
+    rows = s.n * a.group;
+    base = s.ctx - s.n;
+    r0 = rt * 2 * kRows;
+    const int end = min(r0 + 2 * kRows, rows) - 1;
+    range_of<kTok>(s, c, b, a.window, a.by_group.div(r0), a.by_group.div(end), lo, hi);
+    part_of<kTok>(a, sp, lo, hi);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int f = r0 + x * kRows, l = min(f + kRows, rows) - 1;
+      int l2 = 0, h2 = 0;
+      if (f < rows) range_of<kTok>(s, c, b, a.window, a.by_group.div(f), a.by_group.div(l), l2, h2);
+      h2 = min(h2, hi);
+      n_x[x] = h2 > lo ? (h2 - lo + kTok - 1) / kTok : 0;
+    }
+    return true;
+  }
 };
 
 // 16 bytes of codes as 16 elements of T
@@ -314,15 +375,10 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
   extern __shared__ __align__(1024) uint8_t sm[];
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
-  const int kvh = blockIdx.x % c.heads;
-  int rest = blockIdx.x / c.heads;
-  const int sp = rest % a.parts;
-  rest /= a.parts;
-  const int i = rest % b.n_seq;
-  const int rt0 = a.row_tiles - 1 - rest / b.n_seq;     // the longest ranges first
-  const Seq sq = seq_of(b, i);
-  const int rows = sq.n * a.group, base = sq.ctx - sq.n;
-  if (rows <= a.few || rt0 * 2 * kRows >= rows) return;
+  {
+    Unit w;
+    if (!w.find(a, b, c, blockIdx.x)) return;
+  }
 
   uint64_t* bars = reinterpret_cast<uint64_t*>(sm + L::AT_BAR);
   uint64_t *full = bars, *empty = bars + L::RING, *meta = empty + L::RING, *s_full = meta + L::META,
@@ -338,51 +394,25 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
-  if (tid == 0) *dead = 0;
-
-  // Rows r0.. of the block's turn: the two tiles' positions, and how many 128-token
-  // tiles each sees. (One turn, unless a sequence has more rows than the host said.)
-  int r0, lo, hi, n_x[2], n;
-  uint32_t tmem;
-  auto turn = [&](int rt) {
-    r0 = rt * 2 * kRows;
-    const int end = min(r0 + 2 * kRows, rows) - 1;
-    range_of<kTok>(sq, c, b, a.window, a.by_group.div(r0), a.by_group.div(end), lo, hi);
-    part_of<kTok>(a, sp, lo, hi);
-#pragma unroll
+  if (tid == 0) {
+    *dead = 0;
+    for (int k = 0; k < L::RING; ++k) {
+      bar_init(full + k, kCopyWarps);
+      bar_init(empty + k, 1);
+    }
+    for (int k = 0; k < L::META; ++k) bar_init(meta + k, 4);
     for (int x = 0; x < 2; ++x) {
-      const int f = r0 + x * kRows, l = min(f + kRows, rows) - 1;
-      int l2 = 0, h2 = 0;
-      if (f < rows) range_of<kTok>(sq, c, b, a.window, a.by_group.div(f), a.by_group.div(l), l2, h2);
-      h2 = min(h2, hi);
-      n_x[x] = h2 > lo ? (h2 - lo + kTok - 1) / kTok : 0;
+      bar_init(s_full + x, 1);
+      bar_init(p_full + x, kRowWarps / 2);
+      bar_init(o_done + x, 1);
+      bar_init(q_full + x, kRowWarps / 2);
     }
-    n = max(n_x[0], n_x[1]);
-    __syncthreads();
-    if (tid == 0) {
-      // (every arrival of an earlier turn has been waited for)
-      if (rt != rt0)
-        for (int k = 0; k < L::BARS; ++k)
-          asm volatile("mbarrier.inval.shared.b64 [%0];" ::"r"(smem_of(bars + k)) : "memory");
-      for (int k = 0; k < L::RING; ++k) {
-        bar_init(full + k, kCopyWarps);
-        bar_init(empty + k, 1);
-      }
-      for (int k = 0; k < L::META; ++k) bar_init(meta + k, 4);
-      for (int x = 0; x < 2; ++x) {
-        bar_init(s_full + x, 1);
-        bar_init(p_full + x, kRowWarps / 2);
-        bar_init(o_done + x, 1);
-      }
-      bar_init(q_full, kRowWarps);
-      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    tmem_before();
-    __syncthreads();
-    tmem_after();
-    tmem = __shfl_sync(0xffffffffu, *tmem_at, 0);
-  };
-
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  tmem_before();
+  __syncthreads();
+  tmem_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_at, 0);
   auto finish = [&]() {
     __syncthreads();
     if (warp == kMmaWarp) {
@@ -397,13 +427,29 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
   if (warp < kRowWarps) {
     // ---- rows --------------------------------------------------------------
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-    for (int rt = rt0; rt * 2 * kRows < rows; rt += a.row_tiles) {
-      turn(rt);
-      const int x = warp >> 2, row = (warp & 3) * 32 + lane;
-      const int r = r0 + x * kRows + row;
-      const int n_mine = n_x[x];
-      // queries: 16-byte pieces, neighbouring lanes along a row
+    // (counted over the block's units: the barriers' phases)
+    uint32_t n_tile = 0, n_own = 0, n_unit = 0;
+    const int x = warp >> 2, row = (warp & 3) * 32 + lane;
+    bool alive = true;
+    Unit w;
+    for (uint32_t u = blockIdx.x; alive && w.find(a, b, c, u); u += gridDim.x) {
+      // (kept aside: the registers of the tile loop are all taken)
+      volatile Unit* kept = reinterpret_cast<volatile Unit*>(sm + L::AT_UNIT + warp * 64);
+      const int n_mine = x ? w.n_x[1] : w.n_x[0], lo = w.lo;
+      int pos, first, last;
+      // queries: 16-byte pieces, neighbouring lanes along a row (the last unit's products
+      // have been waited for)
       {
+        const int rows = w.rows, r0 = w.r0;
+        __syncwarp();
+        if (lane == 0) *reinterpret_cast<Unit*>(sm + L::AT_UNIT + warp * 64) = w;
+        __syncwarp();
+        pos = w.base + a.by_group.div(min(r0 + x * kRows + row, rows - 1));
+        first = w.base + a.by_group.div(r0 + x * kRows < rows ? r0 + x * kRows : 0);
+        last = w.base + a.by_group.div(min(r0 + x * kRows + kRows, rows) - 1);
+      }
+      if (n_mine > 0) {
+        const int rows = w.rows, r0 = w.r0, kvh = w.kvh, start = w.start;
         constexpr int PPR = DIM / 8, RPW = 32 / PPR;
         uint8_t* q_s = sm + x * kRows * DIM * 2;
         const int piece = lane % PPR;
@@ -413,7 +459,7 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
           uint4 v = make_uint4(0, 0, 0, 0);
           if (rg < rows) {
             const int t = a.by_group.div(rg);
-            const T* p = reinterpret_cast<const T*>(a.q) + (int64_t)(sq.start + t) * a.q_row +
+            const T* p = reinterpret_cast<const T*>(a.q) + (int64_t)(start + t) * a.q_row +
                          (int64_t)(kvh * a.group + (rg - t * a.group)) * a.q_head;
             v = reinterpret_cast<const uint4*>(p)[piece];
           }
@@ -421,19 +467,16 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
           *reinterpret_cast<uint4*>(q_s + hf * (kRows * 128) + rr * 128 + ((pc ^ (rr & 7)) << 4)) = v;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        bar_arrive_warp(q_full);
+        bar_arrive_warp(q_full + x);
       }
-      const int pos = base + a.by_group.div(min(r, rows - 1));
-      const int first = base + a.by_group.div(r0 + x * kRows < rows ? r0 + x * kRows : 0);
-      const int last = base + a.by_group.div(min(r0 + x * kRows + kRows, rows) - 1);
       const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
       const uint32_t s_at = tmem + lanes + x * kTok, o_at = tmem + lanes + 256 + x * 128;
       float m = -INFINITY, l = 0.f;
-      bool alive = true;
 #pragma unroll 1
       for (int k = 0; k < n_mine; ++k) {
-        const int ms = k % L::META;
-        if (!bar_wait(meta + ms, (k / L::META) & 1, dead) || !bar_wait(s_full + x, k & 1, dead)) {
+        const int ms = (n_tile + k) % L::META;
+        if (!bar_wait(meta + ms, ((n_tile + k) / L::META) & 1, dead) ||
+            !bar_wait(s_full + x, (n_own + k) & 1, dead)) {
           alive = false;
           break;
         }
@@ -545,17 +588,22 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
         tmem_before();
         bar_arrive_warp(p_full + x);
       }
-      if (alive && n_mine > 0 && !bar_wait(o_done + x, 0, dead)) alive = false;
+      if (alive && n_mine > 0) alive = bar_wait(o_done + x, n_unit & 1, dead);
+      n_tile += max(kept->n_x[0], kept->n_x[1]);
+      n_own += n_mine;
+      n_unit += n_mine > 0;
       tmem_after();
 
       // ---- a thread writes its row ------------------------------------------
+      const int i = kept->i, kvh = kept->kvh, sp = kept->sp, hi = kept->hi, rows = kept->rows;
+      const int start = kept->start, r = kept->r0 + x * kRows + row;
       // (a row without weight gives zeros, whatever was multiplied for it)
       const bool mine = r < rows && alive;
       const int tok = a.by_group.div(min(r, rows - 1));
       const int h_q = kvh * a.group + (min(r, rows - 1) - tok * a.group);
-      const int64_t t_row = (int64_t)(sq.start + tok);
+      const int64_t t_row = (int64_t)(start + tok);
       const float by = m == -INFINITY ? 0.f : a.parts > 1 ? 1.f : div_rn(1.f, l);
-      const int64_t at = ((int64_t)sp * b.n_rows + t_row) * a.heads + h_q;
+      const int64_t at = ((int64_t)sp * a.part_rows + t_row) * a.heads + h_q;
       bool odd = false;
 #pragma unroll 1
       for (int h = 0; h < DIM / 32; ++h) {
@@ -584,7 +632,7 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
           }
         }
       }
-      if (mine) row_state(a, b, sp, t_row, h_q, m, l);
+      if (mine) row_state(a, sp, t_row, t_row, h_q, m, l);
       // rows with values that are no number, one at a time by the whole warp
       unsigned redo = __ballot_sync(0xffffffffu, mine && odd && m > -INFINITY);
       while (redo) {
@@ -601,7 +649,7 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
 #pragma unroll
         for (int e = 0; e < EL; ++e) {
           if (a.parts > 1)
-            a.part_o[(((int64_t)sp * b.n_rows + tr) * a.heads + hq) * DIM + lane * EL + e] = acc[e];
+            a.part_o[(((int64_t)sp * a.part_rows + tr) * a.heads + hq) * DIM + lane * EL + e] = acc[e];
           else
             (reinterpret_cast<T*>(a.out) + tr * a.o_row + hq * a.o_head)[lane * EL + e] =
                 T(acc[e] * bb);
@@ -614,8 +662,11 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
   asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
   if (warp < kMmaWarp) {
     // ---- copies --------------------------------------------------------------
-    for (int rt = rt0; rt * 2 * kRows < rows; rt += a.row_tiles) {
-      turn(rt);
+    uint32_t n_tile = 0;
+    bool alive = true;
+    Unit w;
+    for (uint32_t u = blockIdx.x; alive && w.find(a, b, c, u); u += gridDim.x) {
+      const int i = w.i, kvh = w.kvh, lo = w.lo, hi = w.hi, n = max(w.n_x[0], w.n_x[1]);
       const int cw = warp - kCopyWarp;
       constexpr int CB = L::CODED ? 1 : 2, PPT = DIM * CB / 16;    // 16-byte pieces of a token
       constexpr int STEPS = kTok * PPT / 32, TPS = 32 / PPT;       // 32 pieces a step of a warp
@@ -652,7 +703,7 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
         return q < 32 ? x : y;
       };
       auto note = [&](int k) {                 // mask bits and scales, for tile k
-        const int ms = k % L::META;
+        const int ms = (n_tile + k) % L::META;
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
           if (g == 1 && cw != 0) break;
@@ -684,7 +735,6 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
       look(0, !whole_box(0));
       if (lane < boxes) boxed.at(c, b, i, lo + lane * box, hi);
       int pending = -1;                        // a tile copied by pieces, not yet announced
-      bool alive = true;
 #pragma unroll 1
       for (int k = 0; k < n && alive; ++k) {
         const bool by_box = !L::CODED && whole_box(k);
@@ -697,7 +747,7 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
         if (lane < boxes) boxed.at(c, b, i, lo + (k + 1) * kTok + lane * box, k + 1 < n ? hi : 0);
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
-          const int seq = 2 * k + kv, buf = seq % L::RING;
+          const uint32_t seq = 2 * (n_tile + k) + kv, buf = seq % L::RING;
           const uint8_t* src = (kv ? c.v : c.k) + piece * 16;
           uint8_t* dst = sm + L::AT_RING + buf * L::BUF;
           alive = alive && bar_wait(empty + buf, ((seq / L::RING) & 1) ^ 1, dead);
@@ -775,11 +825,16 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
           bar_arrive_warp(full + pending);
         }
       }
+      n_tile += n;
     }
   } else {
     // ---- products --------------------------------------------------------------
-    for (int rt = rt0; rt * 2 * kRows < rows; rt += a.row_tiles) {
-      turn(rt);
+    uint32_t n_tile = 0, n_own[2] = {0, 0}, n_unit[2] = {0, 0};
+    bool alive = true;
+    Unit w;
+    for (uint32_t u = blockIdx.x; alive && w.find(a, b, c, u); u += gridDim.x) {
+      const int n = max(w.n_x[0], w.n_x[1]);
+      const int n_x[2] = {w.n_x[0], w.n_x[1]};
       {
         constexpr uint32_t id_s = idesc_of<T>(kTok, false), id_o = idesc_of<T>(DIM, true);
         const uint32_t q_op = operand(smem_of(sm), 16);
@@ -795,28 +850,30 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
           }
           commit(s_full + x);
         };
-        bool alive = n > 0 && bar_wait(q_full, 0, dead) && bar_wait(full, 0, dead);
+        if (n == 0) continue;
+        const uint32_t at = 2 * n_tile;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          if (n_x[x] > 0) alive = alive && bar_wait(q_full + x, n_unit[x] & 1, dead);
+        alive = alive && bar_wait(full + at % L::RING, (at / L::RING) & 1, dead);
         if (alive) {
           tmem_after();
 #pragma unroll
           for (int x = 0; x < 2; ++x)
-            if (n_x[x] > 0 && one_lane()) scores(x, 0);
-          if (L::RING < 2 * n && one_lane()) commit(empty);
+            if (n_x[x] > 0 && one_lane()) scores(x, at % L::RING);
+          if (one_lane()) commit(empty + at % L::RING);
         }
 #pragma unroll 1
         for (int k = 0; k < n && alive; ++k) {
-          const int vb = (2 * k + 1) % L::RING, kb = (2 * k + 2) % L::RING;
-          if (!bar_wait(full + vb, ((2 * k + 1) / L::RING) & 1, dead)) break;
+          const uint32_t vs = at + 2 * k + 1, vb = vs % L::RING, kb = (vs + 1) % L::RING;
+          alive = bar_wait(full + vb, (vs / L::RING) & 1, dead);
           bool have = false;
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             if (k < n_x[x]) {
-              if (!bar_wait(p_full + x, k & 1, dead)) {
-                alive = false;
-                break;
-              }
+              alive = alive && bar_wait(p_full + x, (n_own[x] + k) & 1, dead);
               tmem_after();
-              if (one_lane()) {
+              if (alive && one_lane()) {
                 const uint32_t va = v_op + vb * (L::BUF >> 4), d = tmem + 256 + x * 128;
                 const uint32_t pa = tmem + x * kTok;
 #pragma unroll
@@ -826,23 +883,30 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
               }
             }
             if (k + 1 < n_x[x]) {
-              if (!have && !bar_wait(full + kb, ((2 * k + 2) / L::RING) & 1, dead)) {
-                alive = false;
-                break;
-              }
+              if (!have) alive = alive && bar_wait(full + kb, ((vs + 1) / L::RING) & 1, dead);
               have = true;
               tmem_after();
-              if (one_lane()) scores(x, kb);
+              if (alive && one_lane()) scores(x, kb);
             }
           }
           if (alive && one_lane()) {
-            // only where the copies go round once more, so that no arrival is left over
-            if (2 * k + 1 + L::RING < 2 * n) commit(empty + vb);
-            if (2 * k + 2 + L::RING < 2 * n) commit(empty + kb);
+            commit(empty + vb);
+            if (k + 1 < n) commit(empty + kb);
           }
+        }
+        n_tile += n;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          n_own[x] += n_x[x];
+          n_unit[x] += n_x[x] > 0;
         }
         __syncwarp();
       }
+    }
+    // the arrivals that no copy waits for any more
+    for (uint32_t s = 2 * n_tile; alive && s > 0 && s + 2 > 2 * n_tile;) {
+      --s;
+      alive = bar_wait(empty + s % L::RING, (s / L::RING) & 1, dead);
     }
   }
   finish();
@@ -897,13 +961,13 @@ void make_maps(Maps& m, const CacheArgs& c, int dtype, int dim) {
 
 template <class T, Code CODE, int DIM>
 cudaError_t launch_typed(const AttendArgs& a, const BatchArgs& b, const CacheArgs& c,
-                         tre_diag* diag, cudaStream_t s) {
+                         int64_t units, tre_diag* diag, cudaStream_t s) {
   using L = Tc<CODE, DIM>;
   const void* fn = (const void*)k_attend_tc<T, CODE, DIM>;
   cudaError_t e = func_smem_once(fn, L::SMEM, true);
   if (e) return e;
-  const int64_t blocks = (int64_t)c.heads * a.parts * b.n_seq * a.row_tiles;
-  if (blocks > 2147483647) return cudaErrorInvalidValue;
+  if (units > 2000000000) return cudaErrorInvalidValue;
+  const int64_t blocks = std::min<int64_t>(units, device_sm_count());
   Maps maps;
   memset(&maps, 0, sizeof(maps));
   if (CODE == Code::kHalf)
@@ -914,24 +978,25 @@ cudaError_t launch_typed(const AttendArgs& a, const BatchArgs& b, const CacheArg
 
 template <class T>
 cudaError_t launch_code(int code, int dim, const AttendArgs& a, const BatchArgs& b,
-                        const CacheArgs& c, tre_diag* diag, cudaStream_t s) {
+                        const CacheArgs& c, int64_t units, tre_diag* diag,
+                        cudaStream_t s) {
   if (code == TRE_E4M3)
-    return dim == 64 ? launch_typed<T, Code::kE4m3, 64>(a, b, c, diag, s)
-                     : launch_typed<T, Code::kE4m3, 128>(a, b, c, diag, s);
+    return dim == 64 ? launch_typed<T, Code::kE4m3, 64>(a, b, c, units, diag, s)
+                     : launch_typed<T, Code::kE4m3, 128>(a, b, c, units, diag, s);
   if (code == TRE_I8)
-    return dim == 64 ? launch_typed<T, Code::kI8, 64>(a, b, c, diag, s)
-                     : launch_typed<T, Code::kI8, 128>(a, b, c, diag, s);
-  return dim == 64 ? launch_typed<T, Code::kHalf, 64>(a, b, c, diag, s)
-                   : launch_typed<T, Code::kHalf, 128>(a, b, c, diag, s);
+    return dim == 64 ? launch_typed<T, Code::kI8, 64>(a, b, c, units, diag, s)
+                     : launch_typed<T, Code::kI8, 128>(a, b, c, units, diag, s);
+  return dim == 64 ? launch_typed<T, Code::kHalf, 64>(a, b, c, units, diag, s)
+                   : launch_typed<T, Code::kHalf, 128>(a, b, c, units, diag, s);
 }
 
 }  // namespace
 
 cudaError_t launch_attend_tc(int dtype, int code, int dim, const AttendArgs& a,
-                             const BatchArgs& b, const CacheArgs& c, tre_diag* diag,
-                             cudaStream_t s) {
-  return dtype == TRE_BF16 ? launch_code<__nv_bfloat16>(code, dim, a, b, c, diag, s)
-                           : launch_code<__half>(code, dim, a, b, c, diag, s);
+                             const BatchArgs& b, const CacheArgs& c, int64_t units,
+                             tre_diag* diag, cudaStream_t s) {
+  return dtype == TRE_BF16 ? launch_code<__nv_bfloat16>(code, dim, a, b, c, units, diag, s)
+                           : launch_code<__half>(code, dim, a, b, c, units, diag, s);
 }
 
 }  // namespace tre
