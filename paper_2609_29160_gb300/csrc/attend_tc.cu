@@ -40,6 +40,7 @@ constexpr int kRows = 128, kTok = 128;
 constexpr int kRowWarps = 8, kCopyWarp = kRowWarps, kCopyWarps = 3;
 constexpr int kMmaWarp = kCopyWarp + kCopyWarps;
 constexpr int kThreads = (kMmaWarp + 1) * 32;
+constexpr int kUnits = 4;          // units that the copies may be ahead
 constexpr long long kWaitClocks = 4000000000ll;
 
 __device__ __forceinline__ uint32_t smem_of(const void* p) {
@@ -280,22 +281,22 @@ template <Code CODE, int DIM> struct Tc {
   static constexpr bool CODED = CODE != Code::kHalf;
   static constexpr int BUF = kTok * DIM * 2;            // a tile of keys or values
   static constexpr int RING = DIM == 128 ? (CODED ? 4 : 5) : (CODED ? 8 : 8);
-  static constexpr int META = DIM == 128 ? 4 : 8;                        // tiles whose scales and masks are kept
+  static constexpr int META = DIM == 128 ? 4 : 8;       // tiles whose scales and masks are kept
   static constexpr int Q = 2 * kRows * DIM * 2;
   static constexpr int AT_RING = Q;
   static constexpr int AT_MASK = AT_RING + RING * BUF;  // uint32 [META][4]
   static constexpr int AT_SCALE = AT_MASK + META * 16;  // float [META][3][kTok]
   static constexpr int AT_BAR = AT_SCALE + (CODED ? META * 3 * kTok * 4 : 0);
-  static constexpr int BARS = 2 * RING + META + 8;
-  static constexpr int AT_UNIT = AT_BAR + BARS * 8 + 16;       // Unit [kRowWarps]
-  static constexpr int SMEM = AT_UNIT + kRowWarps * 64;
+  static constexpr int BARS = 2 * RING + META + 8 + 2 * kUnits;
+  static constexpr int AT_UNIT = (AT_BAR + BARS * 8 + 16 + 63) / 64 * 64;    // Unit [kUnits]
+  static constexpr int SMEM = AT_UNIT + kUnits * 64;
 };
 
 // A block's piece of work: up to 256 rows of a sequence against one part of its context
 // for one cache head. Units go through the sequences' row tiles (of those that are not
 // k_attend's), each sequence's longest ranges first, heads fastest: heads of a tile read
 // neighbouring memory, rows of a head the same.
-struct Unit {
+struct alignas(64) Unit {
   int i, kvh, sp, r0, rows, start, base, lo, hi;
   int n_x[2];                     // 128-token tiles that each half of the rows sees
   // The whole warp looks; false past the last unit.
@@ -382,11 +383,13 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
 
   uint64_t* bars = reinterpret_cast<uint64_t*>(sm + L::AT_BAR);
   uint64_t *full = bars, *empty = bars + L::RING, *meta = empty + L::RING, *s_full = meta + L::META,
-           *p_full = s_full + 2, *o_done = p_full + 2, *q_full = o_done + 2;
+           *p_full = s_full + 2, *o_done = p_full + 2, *q_full = o_done + 2,
+           *u_full = q_full + 2, *u_empty = u_full + kUnits;
   uint32_t* tmem_at = reinterpret_cast<uint32_t*>(bars + L::BARS);
   volatile int* dead = reinterpret_cast<volatile int*>(tmem_at + 1);
   uint32_t* mask_s = reinterpret_cast<uint32_t*>(sm + L::AT_MASK);
   float* scale_s = reinterpret_cast<float*>(sm + L::AT_SCALE);
+  const volatile Unit* units = reinterpret_cast<const volatile Unit*>(sm + L::AT_UNIT);
 
   if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(
@@ -406,6 +409,10 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
       bar_init(p_full + x, kRowWarps / 2);
       bar_init(o_done + x, 1);
       bar_init(q_full + x, kRowWarps / 2);
+    }
+    for (int k = 0; k < kUnits; ++k) {
+      bar_init(u_full + k, 1);
+      bar_init(u_empty + k, kRowWarps + 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -431,43 +438,51 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
     uint32_t n_tile = 0, n_own = 0, n_unit = 0;
     const int x = warp >> 2, row = (warp & 3) * 32 + lane;
     bool alive = true;
-    Unit w;
-    for (uint32_t u = blockIdx.x; alive && w.find(a, b, c, u); u += gridDim.x) {
-      // (kept aside: the registers of the tile loop are all taken)
-      volatile Unit* kept = reinterpret_cast<volatile Unit*>(sm + L::AT_UNIT + warp * 64);
-      const int n_mine = x ? w.n_x[1] : w.n_x[0], lo = w.lo;
-      int pos, first, last;
-      // queries: 16-byte pieces, neighbouring lanes along a row (the last unit's products
-      // have been waited for)
-      {
-        const int rows = w.rows, r0 = w.r0;
-        __syncwarp();
-        if (lane == 0) *reinterpret_cast<Unit*>(sm + L::AT_UNIT + warp * 64) = w;
-        __syncwarp();
-        pos = w.base + a.by_group.div(min(r0 + x * kRows + row, rows - 1));
-        first = w.base + a.by_group.div(r0 + x * kRows < rows ? r0 + x * kRows : 0);
-        last = w.base + a.by_group.div(min(r0 + x * kRows + kRows, rows) - 1);
-      }
-      if (n_mine > 0) {
-        const int rows = w.rows, r0 = w.r0, kvh = w.kvh, start = w.start;
-        constexpr int PPR = DIM / 8, RPW = 32 / PPR;
-        uint8_t* q_s = sm + x * kRows * DIM * 2;
-        const int piece = lane % PPR;
-#pragma unroll 4
-        for (int k = 0; k < 32 / RPW; ++k) {
-          const int rr = (warp & 3) * 32 + k * RPW + lane / PPR, rg = r0 + x * kRows + rr;
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (rg < rows) {
-            const int t = a.by_group.div(rg);
-            const T* p = reinterpret_cast<const T*>(a.q) + (int64_t)(start + t) * a.q_row +
-                         (int64_t)(kvh * a.group + (rg - t * a.group)) * a.q_head;
-            v = reinterpret_cast<const uint4*>(p)[piece];
-          }
-          const int hf = piece >> 3, pc = piece & 7;
-          *reinterpret_cast<uint4*>(q_s + hf * (kRows * 128) + rr * 128 + ((pc ^ (rr & 7)) << 4)) = v;
+    // Queries of a unit: 16-byte pieces, neighbouring lanes along a row
+    constexpr int PPR = DIM / 8, RPW = 32 / PPR, QS = 32 / RPW;
+    const int q_row0 = (warp & 3) * 32 + lane / PPR, q_piece = lane % PPR;
+    auto q_load = [&](const volatile Unit* w, uint4* v) {
+      const int rows = w->rows, r0 = w->r0 + x * kRows, kvh = w->kvh, start = w->start;
+#pragma unroll
+      for (int k = 0; k < QS; ++k) {
+        const int rg = r0 + q_row0 + k * RPW;
+        v[k] = make_uint4(0, 0, 0, 0);
+        if (rg < rows) {
+          const int t = a.by_group.div(rg);
+          const T* p = reinterpret_cast<const T*>(a.q) + (int64_t)(start + t) * a.q_row +
+                       (int64_t)(kvh * a.group + (rg - t * a.group)) * a.q_head;
+          v[k] = reinterpret_cast<const uint4*>(p)[q_piece];
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        bar_arrive_warp(q_full + x);
+      }
+    };
+    auto q_store = [&](const uint4* v) {
+      uint8_t* q_s = sm + x * kRows * DIM * 2 + (q_piece >> 3) * (kRows * 128);
+#pragma unroll
+      for (int k = 0; k < QS; ++k) {
+        const int rr = q_row0 + k * RPW;
+        *reinterpret_cast<uint4*>(q_s + rr * 128 + (((q_piece & 7) ^ (rr & 7)) << 4)) = v[k];
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      bar_arrive_warp(q_full + x);
+    };
+    uint32_t nu = 0;
+    alive = bar_wait(u_full, 0, dead);
+    if (alive && units[0].i >= 0 && units[0].n_x[x] > 0) {
+      uint4 v[QS];
+      q_load(units, v);
+      q_store(v);
+    }
+    while (alive) {
+      // (what the tile loop does not need stays in shared memory)
+      const volatile Unit* w = units + nu % kUnits;
+      if (w->i < 0) break;
+      const int n_mine = w->n_x[x], lo = w->lo;
+      int pos, first, last;
+      {
+        const int rows = w->rows, r0 = w->r0 + x * kRows, base = w->base;
+        pos = base + a.by_group.div(min(r0 + row, rows - 1));
+        first = base + a.by_group.div(r0 < rows ? r0 : 0);
+        last = base + a.by_group.div(min(r0 + kRows, rows) - 1);
       }
       const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
       const uint32_t s_at = tmem + lanes + x * kTok, o_at = tmem + lanes + 256 + x * 128;
@@ -588,15 +603,26 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
         tmem_before();
         bar_arrive_warp(p_full + x);
       }
-      if (alive && n_mine > 0) alive = bar_wait(o_done + x, n_unit & 1, dead);
-      n_tile += max(kept->n_x[0], kept->n_x[1]);
+      // the next unit's queries are on their way while the last products run, and its
+      // first products run while this one's rows are written
+      const uint32_t nn = nu + 1;
+      const volatile Unit* wn = units + nn % kUnits;
+      alive = alive && bar_wait(u_full + nn % kUnits, (nn / kUnits) & 1, dead);
+      {
+        const bool more = alive && wn->i >= 0 && wn->n_x[x] > 0;
+        uint4 v[QS];
+        if (more) q_load(wn, v);
+        if (n_mine > 0) alive = alive && bar_wait(o_done + x, n_unit & 1, dead);
+        if (more && alive) q_store(v);
+      }
+      n_tile += max(w->n_x[0], w->n_x[1]);
       n_own += n_mine;
       n_unit += n_mine > 0;
       tmem_after();
 
       // ---- a thread writes its row ------------------------------------------
-      const int i = kept->i, kvh = kept->kvh, sp = kept->sp, hi = kept->hi, rows = kept->rows;
-      const int start = kept->start, r = kept->r0 + x * kRows + row;
+      const int i = w->i, kvh = w->kvh, sp = w->sp, hi = w->hi, rows = w->rows;
+      const int start = w->start, r = w->r0 + x * kRows + row;
       // (a row without weight gives zeros, whatever was multiplied for it)
       const bool mine = r < rows && alive;
       const int tok = a.by_group.div(min(r, rows - 1));
@@ -656,16 +682,28 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
         }
       }
       tmem_before();
+      bar_arrive_warp(u_empty + nu % kUnits);
+      ++nu;
     }
     return finish();
   }
   asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
   if (warp < kMmaWarp) {
     // ---- copies --------------------------------------------------------------
-    uint32_t n_tile = 0;
+    uint32_t n_tile = 0, nu = 0;
     bool alive = true;
-    Unit w;
-    for (uint32_t u = blockIdx.x; alive && w.find(a, b, c, u); u += gridDim.x) {
+    for (uint32_t u = blockIdx.x; alive; u += gridDim.x, ++nu) {
+      // units are found here, ahead of those who need them
+      Unit w;
+      const bool some = w.find(a, b, c, u);
+      if (!some) w.i = -1;
+      if (warp == kCopyWarp) {
+        alive = bar_wait(u_empty + nu % kUnits, ((nu / kUnits) & 1) ^ 1, dead);
+        if (!alive) break;
+        if (lane == 0) *reinterpret_cast<Unit*>(sm + L::AT_UNIT + nu % kUnits * 64) = w;
+        bar_arrive_warp(u_full + nu % kUnits);
+      }
+      if (!some) break;
       const int i = w.i, kvh = w.kvh, lo = w.lo, hi = w.hi, n = max(w.n_x[0], w.n_x[1]);
       const int cw = warp - kCopyWarp;
       constexpr int CB = L::CODED ? 1 : 2, PPT = DIM * CB / 16;    // 16-byte pieces of a token
@@ -726,25 +764,25 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
           bar_arrive_warp(meta + ms);
         }
       };
-      // Boxes of whole tiles: a lane of the first warp knows each box's page (one that
-      // the cache does not have where the table names none: its rows come as zeros).
+      // Boxes of whole tiles, every third a warp, one a lane: its page (one that the cache
+      // does not have where the table names none: its rows come as zeros).
       const int box = L::CODED ? 0 : maps.box, boxes = box ? kTok / box : 0;
+      const int my_box = cw + kCopyWarps * lane, my_boxes = (boxes + 2 - cw) / kCopyWarps;
       auto whole_box = [&](int k) { return box > 0 && lo + (k + 1) * kTok <= hi; };
       Ask boxed;
-      int box_page = 0, box_slot = 0;
       look(0, !whole_box(0));
-      if (lane < boxes) boxed.at(c, b, i, lo + lane * box, hi);
+      if (my_box < boxes) boxed.at(c, b, i, lo + my_box * box, hi);
       int pending = -1;                        // a tile copied by pieces, not yet announced
 #pragma unroll 1
       for (int k = 0; k < n && alive; ++k) {
         const bool by_box = !L::CODED && whole_box(k);
         note(k);
         if (!by_box) take();
-        box_page = boxed.page(c);
+        int box_page = boxed.page(c);
+        const int box_slot = boxed.slot;
         if (box_page < 0) box_page = c.n_pages;
-        box_slot = boxed.slot;
         look(k + 1, !whole_box(k + 1));
-        if (lane < boxes) boxed.at(c, b, i, lo + (k + 1) * kTok + lane * box, k + 1 < n ? hi : 0);
+        if (my_box < boxes) boxed.at(c, b, i, lo + (k + 1) * kTok + my_box * box, k + 1 < n ? hi : 0);
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
           const uint32_t seq = 2 * (n_tile + k) + kv, buf = seq % L::RING;
@@ -753,22 +791,16 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
           alive = alive && bar_wait(empty + buf, ((seq / L::RING) & 1) ^ 1, dead);
           if (!alive) break;
           if (by_box) {
-            if (cw == 0) {
-              if (one_lane()) bar_expect(full + buf, L::BUF);
-              for (int x = 0; x < boxes; ++x) {
-                const int pg = __shfl_sync(0xffffffffu, box_page, x);
-                const int sl = __shfl_sync(0xffffffffu, box_slot, x);
-                if (one_lane()) {
-                  const uint32_t to = smem_of(dst) + x * box * 128;
+            if (lane == 0) bar_expect(full + buf, my_boxes * box * DIM * 2);
+            __syncwarp();
+            if (my_box < boxes) {
+              const uint32_t to = smem_of(dst) + my_box * box * 128;
 #pragma unroll
-                  for (int h = 0; h < DIM / 64; ++h)
-                    box_load(to + h * (kTok * 128), kv ? &maps.v : &maps.k, h * 64, sl, kvh, pg,
-                             full + buf);
-                }
-              }
-            } else if (lane == 0) {
-              bar_arrive(full + buf);
+              for (int h = 0; h < DIM / 64; ++h)
+                box_load(to + h * (kTok * 128), kv ? &maps.v : &maps.k, h * 64, box_slot, kvh,
+                         box_page, full + buf);
             }
+            __syncwarp();
           } else if constexpr (!L::CODED) {
             const uint32_t to = smem_of(dst) + (piece >> 3) * (kTok * 128);
 #pragma unroll 4
@@ -831,10 +863,15 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
     // ---- products --------------------------------------------------------------
     uint32_t n_tile = 0, n_own[2] = {0, 0}, n_unit[2] = {0, 0};
     bool alive = true;
-    Unit w;
-    for (uint32_t u = blockIdx.x; alive && w.find(a, b, c, u); u += gridDim.x) {
-      const int n = max(w.n_x[0], w.n_x[1]);
-      const int n_x[2] = {w.n_x[0], w.n_x[1]};
+    for (uint32_t nu = 0; alive; ++nu) {
+      alive = bar_wait(u_full + nu % kUnits, (nu / kUnits) & 1, dead);
+      if (!alive) break;
+      const volatile Unit* w = units + nu % kUnits;
+      if (__shfl_sync(0xffffffffu, w->i, 0) < 0) break;
+      const int n_x[2] = {__shfl_sync(0xffffffffu, w->n_x[0], 0),
+                          __shfl_sync(0xffffffffu, w->n_x[1], 0)};
+      const int n = max(n_x[0], n_x[1]);
+      bar_arrive_warp(u_empty + nu % kUnits);
       {
         constexpr uint32_t id_s = idesc_of<T>(kTok, false), id_o = idesc_of<T>(DIM, true);
         const uint32_t q_op = operand(smem_of(sm), 16);
