@@ -74,7 +74,8 @@ template <Code CODE, int DIM> struct Shape {
   static constexpr int CPR = ROW / 16;                  // 16-byte pieces of one key
   static constexpr int SCALES = CODE == Code::kHalf ? 0 : 2 * kTile * 4;
   static constexpr int STAGE = 2 * kTile * ROW + SCALES + 128;
-  static constexpr int STAGES = ROW == 256 ? 3 : ROW == 128 ? 6 : 8;
+  static constexpr int STAGES = ROW == 256 ? 3 : ROW == 128 ? 4 : 8;
+  static constexpr int BLOCKS_AN_SM = ROW == 256 ? 2 : 3;
   static constexpr int SMEM_RING = kWarps * STAGES * STAGE;
   static constexpr int SMEM_JOIN = kWarps * kTile * (DIM + 4) * 4;
   static constexpr int SMEM = SMEM_RING > SMEM_JOIN ? SMEM_RING : SMEM_JOIN;
@@ -89,7 +90,7 @@ template <Code CODE, int DIM> struct Shape {
 };
 
 template <class T, Code CODE, int DIM>
-__global__ void __launch_bounds__(kWarps * 32, 2)
+__global__ void __launch_bounds__(kWarps * 32, Shape<CODE, DIM>::BLOCKS_AN_SM)
 k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
   using S = Shape<CODE, DIM>;
   using CT = typename std::conditional<CODE == Code::kHalf, T, __half>::type;
@@ -194,7 +195,7 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
     // bfloat16 queries then go as halves too, each row divided by a power of two
     // (its largest element's) that its scores get back: nothing within 2^-24 of the
     // row's largest element is lost.
-    float back[2] = {1.f, 1.f};
+    float back[2] = {a.scale2, a.scale2};
     if constexpr (!std::is_same<T, CT>::value) {
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
@@ -210,7 +211,7 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const int ex = min(max((int)(__float_as_uint(top) >> 23), 1), 253);
-        back[x] = __uint_as_float((uint32_t)ex << 23);
+        back[x] = __uint_as_float((uint32_t)ex << 23) * a.scale2;
         const float by = __uint_as_float((uint32_t)(254 - ex) << 23);
 #pragma unroll
         for (int s = 0; s < DIM / 16; ++s)
@@ -270,11 +271,10 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           const int tok = nt * 8 + 2 * cc + x;
-          const float ks = S::SCALES ? mul_rn(sc[tok], a.scale2) : a.scale2;
           vs[nt][x] = S::SCALES ? sc[kTile + tok] : 1.f;
           ex[nt][x] = S::SCALES ? weight_exponent(vs[nt][x]) : 0.f;
-          s[nt][x] = mul_rn(mul_rn(s[nt][x], back[0]), ks);
-          s[nt][x + 2] = mul_rn(mul_rn(s[nt][x + 2], back[1]), ks);
+          s[nt][x] *= S::SCALES ? back[0] * sc[tok] : back[0];
+          s[nt][x + 2] *= S::SCALES ? back[1] * sc[tok] : back[1];
         }
       const int p_first = base + t_first;
       const bool whole = held == 0xffffu && j0 + kTile - 1 <= p_first &&

@@ -63,6 +63,11 @@ def _code(dtype, allowed, what):
     return c
 
 
+def _like(t):
+    """A dense tensor of t's shape (torch's quickest way to one)."""
+    return _torch.empty_like(t, memory_format=_torch.contiguous_format)
+
+
 def _gpu(t, what):
     if not t.is_cuda:
         raise ValueError(f"{what}: must be a CUDA tensor")
@@ -95,11 +100,6 @@ def _index(t, what, n):
         tre._need(t, "int32", n, what)
         _gpu(t, what)
     return t.data_ptr()
-
-
-def _current(stream):
-    """Address of the launch stream (the current torch stream's when None)."""
-    return tre._stream(stream)
 
 
 def _kept(stream, *tensors):
@@ -203,7 +203,7 @@ def _heads(q, k, q_weight, k_weight, eps, cos_sin, interleaved, q_out, k_out, ke
         shape, qr, qh = _rows(q, "q", dtype)
         rows, hq, dim = shape
         if q_out is None:
-            q_out = q.new_empty(shape)
+            q_out = _like(q)
             oor, oh = hq * dim, dim
         else:
             _, oor, oh = _rows(q_out, "q_out", dtype, *shape)
@@ -215,7 +215,7 @@ def _heads(q, k, q_weight, k_weight, eps, cos_sin, interleaved, q_out, k_out, ke
         kp = k.data_ptr()
         if keys_out:
             if k_out is None:
-                k_out = k.new_empty(shape)
+                k_out = _like(k)
                 ur, uh = hk * dim, dim
             else:
                 _, ur, uh = _rows(k_out, "k_out", dtype, *shape)
@@ -255,7 +255,7 @@ def tre_qk_norm_rope(q, k, positions=None, q_weight=None, k_weight=None, eps=1e-
     if positions is not None:
         at = _index(positions, "positions", (q if q is not None else k).shape[0])
     code = lib.tre_qk_norm_rope(packed, at, None if diag is None else diag.data_ptr(),
-                                _current(stream))
+                                tre._stream(stream))
     if code:
         tre._check("tre_qk_norm_rope", code)
     if stream is not None:
@@ -281,7 +281,7 @@ def tre_kv_append(cache, batch, k, v, q=None, q_weight=None, k_weight=None, eps=
     if cache.dtype is not dtype and cache.code not in _CODES:
         raise ValueError(f"k: a cache of {cache.dtype} takes no type {dtype}")
     code = lib.tre_kv_append(cache.packed, batch.packed, packed, v.data_ptr(), vr, vh,
-                             None if diag is None else diag.data_ptr(), _current(stream))
+                             None if diag is None else diag.data_ptr(), tre._stream(stream))
     if code:
         tre._check("tre_kv_append", code)
     if stream is not None:
@@ -299,7 +299,8 @@ def tre_kv_read(cache, batch, dtype="bf16", k_out=None, v_out=None, diag=None, s
     row, head = shape[1] * shape[2], shape[2]
     if k_out is None:
         tt = _torch_type(code)
-        k_out, v_out = cache.k.new_empty(shape, dtype=tt), cache.k.new_empty(shape, dtype=tt)
+        k_out = _torch.empty(shape, dtype=tt, device=cache.k.device)
+        v_out = _like(k_out)
     else:
         tt = _torch_type(code)
         _, row, head = _rows(k_out, "k_out", tt, *shape)
@@ -307,7 +308,7 @@ def tre_kv_read(cache, batch, dtype="bf16", k_out=None, v_out=None, diag=None, s
             raise ValueError("k_out, v_out: expected the same strides")
     code = lib.tre_kv_read(cache.packed, batch.packed, code, k_out.data_ptr(), v_out.data_ptr(),
                            row, head, None if diag is None else diag.data_ptr(),
-                           _current(stream))
+                           tre._stream(stream))
     if code:
         tre._check("tre_kv_read", code)
     if stream is not None:
@@ -330,21 +331,22 @@ def tre_chunk_attention(q, cache, batch, scale=None, window=0, lse=False, out=No
     if heads == 0 or heads % cache.heads:
         raise ValueError(f"q: expected a multiple of {cache.heads} heads, got {heads}")
     if out is None:
-        out = q.new_empty(shape)
+        out = _like(q)
         o_row, oh = heads * cache.dim, cache.dim
     else:
         _, o_row, oh = _rows(out, "out", dtype, *shape)
-    ls = q.new_empty(shape[:2], dtype=_torch.float32) if lse else None
+    ls = _torch.empty(shape[:2], dtype=_torch.float32, device=q.device) if lse else None
     at = ATTEND.pack(code, heads, window, 1.0 / math.sqrt(cache.dim) if scale is None else scale,
                      q.data_ptr(), qr, qh, out.data_ptr(), o_row, oh,
                      0 if ls is None else ls.data_ptr())
-    size, s = C.c_size_t(0), _current(stream)
+    size, s = C.c_size_t(0), tre._stream(stream)
     dg = None if diag is None else diag.data_ptr()
     code = lib.tre_chunk_attention(cache.packed, batch.packed, at, None, size, dg, s)
     if code:
         tre._check("tre_chunk_attention", code)
-    ws = q.new_empty(max(size.value, 256), dtype=_torch.uint8)
-    code = lib.tre_chunk_attention(cache.packed, batch.packed, at, ws.data_ptr(), size, dg, s)
+    # (a call that needs none still wants an address: it then only hands it back)
+    ws = _torch.empty(size.value, dtype=_torch.uint8, device=q.device) if size.value else out
+    code = lib.tre_chunk_attention(cache.packed, batch.packed, at, ws.data_ptr() or 256, size, dg, s)
     if code:
         tre._check("tre_chunk_attention", code)
     if stream is not None:
