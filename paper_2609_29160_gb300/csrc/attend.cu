@@ -6,15 +6,15 @@
 // in one pass over the keys and values: a running maximum m, the sum l of
 // exp2(s - m), and the weighted sum of values, all in 32 bits.
 //
-// k_attend takes 16 rows at a time (tokens x query heads of one cache head: the
+// k_attend takes 8 * NT rows at a time (tokens x query heads of one cache head: the
 // heads that share a key read it once) against a part of the context. Its four
 // warps each run their own stream of 16-token tiles through a ring of asynchronous
 // 16-byte copies of their own, so no warp waits for another before the end, when
-// their four (m, l, O) are joined. Products are m16n8k16 matrix instructions: with
-// one or a few new tokens the call is bound by the cache's bytes, at which rate 16
-// rows keep those units under a third busy. Positions within a row of keys and
-// columns of values are taken in the order in which a lane's 16-byte reads deliver
-// them, which a sum over positions does not see.
+// their four (m, l, O) are joined. Products are m16n8k16 matrix instructions with
+// positions (then elements) along m and rows along n, S^T = K Q^T and O^T = V^T P^T:
+// eight rows, the query heads of one token, fill a tile that way, and a lane holds two
+// rows' weights of two positions. Elements of a key and columns of values are taken in
+// the order in which a lane's 16-byte reads deliver them, which a sum does not see.
 #include <algorithm>
 
 #include "attend.cuh"
@@ -68,16 +68,18 @@ template <int N> __device__ __forceinline__ void wait_copies() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-template <Code CODE, int DIM> struct Shape {
+template <Code CODE, int DIM, int NT> struct Shape {
   static constexpr int CB = CODE == Code::kHalf ? 2 : 1;
   static constexpr int ROW = DIM * CB;                  // bytes of one key
   static constexpr int CPR = ROW / 16;                  // 16-byte pieces of one key
   static constexpr int SCALES = CODE == Code::kHalf ? 0 : 2 * kTile * 4;
   static constexpr int STAGE = 2 * kTile * ROW + SCALES + 128;
-  static constexpr int STAGES = ROW == 256 ? 3 : ROW == 128 ? 4 : 8;
-  static constexpr int BLOCKS_AN_SM = ROW == 256 ? 2 : 3;
+  static constexpr int ROWS = 8 * NT;
+  // about 200 KB of copies in flight an SM, four blocks where registers allow
+  static constexpr int BLOCKS_AN_SM = ROW == 256 ? 2 : NT == 1 ? 4 : 3;
+  static constexpr int STAGES = ROW == 256 ? 3 : ROW == 128 ? (NT == 1 ? 3 : 4) : (NT == 1 ? 5 : 7);
   static constexpr int SMEM_RING = kWarps * STAGES * STAGE;
-  static constexpr int SMEM_JOIN = kWarps * kTile * (DIM + 4) * 4;
+  static constexpr int SMEM_JOIN = kWarps * ROWS * (DIM + 4) * 4;
   static constexpr int SMEM = SMEM_RING > SMEM_JOIN ? SMEM_RING : SMEM_JOIN;
   // Place of 16-byte piece u = token * CPR + piece: eight neighbours of a read
   // (two tokens x four pieces of keys, four even or odd tokens x two pieces of
@@ -89,10 +91,17 @@ template <Code CODE, int DIM> struct Shape {
   }
 };
 
-template <class T, Code CODE, int DIM>
-__global__ void __launch_bounds__(kWarps * 32, Shape<CODE, DIM>::BLOCKS_AN_SM)
+// An 8 x 8 tile of 16-bit elements turned within the warp.
+__device__ __forceinline__ uint32_t turned(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+template <class T, Code CODE, int DIM, int NT>
+__global__ void __launch_bounds__(kWarps * 32, Shape<CODE, DIM, NT>::BLOCKS_AN_SM)
 k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
-  using S = Shape<CODE, DIM>;
+  using S = Shape<CODE, DIM, NT>;
   using CT = typename std::conditional<CODE == Code::kHalf, T, __half>::type;
   constexpr int EPT = 16 / S::CB, SPB = EPT / 4, BLOCKS = DIM / (4 * EPT);
   extern __shared__ __align__(128) uint8_t sm[];
@@ -108,27 +117,14 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
   const int rows = sq.n * a.group, base = sq.ctx - sq.n;
   if (rows > a.few) return;
 
-  for (int rt = rt0; rt * kTile < rows; rt += a.row_tiles) {
-    const int r_first = rt * kTile, r_last = min(r_first + kTile, rows) - 1;
-    const int t_first = a.by_group.div(r_first);
+  for (int rt = rt0; rt * S::ROWS < rows; rt += a.row_tiles) {
+    const int r_first = rt * S::ROWS, r_last = min(r_first + S::ROWS, rows) - 1;
+    const int t_first = a.by_group.div(r_first), t_last = a.by_group.div(r_last);
     int lo, hi;
-    range_of<kTile>(sq, c, b, a.window, t_first, a.by_group.div(r_last), lo, hi);
+    range_of<kTile>(sq, c, b, a.window, t_first, t_last, lo, hi);
     part_of<kTile * kWarps>(a, sp, lo, hi);
     const int n_tiles = hi > lo ? (hi - lo + kTile - 1) / kTile : 0;
     const int mine = n_tiles > warp ? (n_tiles - warp + kWarps - 1) / kWarps : 0;
-
-    // this lane's two rows
-    int pos[2];
-    const T* qp[2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int r = r_first + g + 8 * x;
-      const int t = a.by_group.div(r);
-      pos[x] = base + t;
-      qp[x] = r < rows ? reinterpret_cast<const T*>(a.q) + (int64_t)(sq.start + t) * a.q_row +
-                             (int64_t)(kvh * a.group + (r - t * a.group)) * a.q_head
-                       : nullptr;
-    }
 
     uint8_t* ring = sm + warp * (S::STAGES * S::STAGE);
     const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
@@ -179,57 +175,79 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
 #pragma unroll 1
     for (int k = 0; k < S::STAGES - 1; ++k) issue();
 
-    uint32_t qf[DIM / 16][4];
+    // queries: row g of each eight, in the order of a key's reads
+    uint32_t qf[NT][DIM / 16][2];
 #pragma unroll
-    for (int s = 0; s < DIM / 16; ++s) {
-      const int e = (s / SPB * 4 + cc) * EPT + (s % SPB) * 4;
+    for (int nt = 0; nt < NT; ++nt) {
+      const int r = r_first + 8 * nt + g, t = a.by_group.div(r);
+      const T* qp = reinterpret_cast<const T*>(a.q) + (int64_t)(sq.start + t) * a.q_row +
+                    (int64_t)(kvh * a.group + (r - t * a.group)) * a.q_head;
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
+      for (int s = 0; s < DIM / 16; ++s) {
         uint2 v = make_uint2(0, 0);
-        if (qp[x]) v = *reinterpret_cast<const uint2*>(qp[x] + e);
-        qf[s][x] = v.x;
-        qf[s][x + 2] = v.y;
+        if (r < rows) v = *reinterpret_cast<const uint2*>(qp + (s / SPB * 4 + cc) * EPT + (s % SPB) * 4);
+        qf[nt][s][0] = v.x;
+        qf[nt][s][1] = v.y;
       }
     }
+    // The rows whose weights this lane holds: 2 cc and 2 cc + 1 of each eight.
     // Codes are multiplied as halves, which both kinds turn into in a step or two;
     // bfloat16 queries then go as halves too, each row divided by a power of two
     // (its largest element's) that its scores get back: nothing within 2^-24 of the
     // row's largest element is lost.
-    float back[2] = {a.scale2, a.scale2};
-    if constexpr (!std::is_same<T, CT>::value) {
+    int pos[NT][2];
+    float back[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
+        pos[nt][x] = base + a.by_group.div(min(r_first + 8 * nt + 2 * cc + x, rows - 1));
+        back[nt][x] = a.scale2;
+      }
+      if constexpr (!std::is_same<T, CT>::value) {
         float top = 0.f;
 #pragma unroll
         for (int s = 0; s < DIM / 16; ++s)
 #pragma unroll
-          for (int y = x; y < 4; y += 2) {
+          for (int y = 0; y < 2; ++y) {
             float u, v;
-            unpack(qf[s][y], u, v, T());
+            unpack(qf[nt][s][y], u, v, T());
             top = fmaxf(top, fmaxf(fabsf(u), fabsf(v)));
           }
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const int ex = min(max((int)(__float_as_uint(top) >> 23), 1), 253);
-        back[x] = __uint_as_float((uint32_t)ex << 23) * a.scale2;
+        const float f = __uint_as_float((uint32_t)ex << 23) * a.scale2;
         const float by = __uint_as_float((uint32_t)(254 - ex) << 23);
 #pragma unroll
         for (int s = 0; s < DIM / 16; ++s)
 #pragma unroll
-          for (int y = x; y < 4; y += 2) {
+          for (int y = 0; y < 2; ++y) {
             float u, v;
-            unpack(qf[s][y], u, v, T());
-            qf[s][y] = pack<CT>(u * by, v * by);
+            unpack(qf[nt][s][y], u, v, T());
+            qf[nt][s][y] = pack<CT>(u * by, v * by);
           }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)          // (row r's factor is in lanes 4 r ..)
+          back[nt][x] = __shfl_sync(0xffffffffu, f, 4 * (2 * cc + x));
       }
     }
 
-    float o[DIM / 8][4];
+    float o[NT][DIM / 16][4];
 #pragma unroll
-    for (int n = 0; n < DIM / 8; ++n)
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+      for (int n = 0; n < DIM / 16; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[nt][n][e] = 0.f;
+    float m[NT][2], l[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        m[nt][x] = -INFINITY;
+        l[nt][x] = 0.f;
+      }
 
 #pragma unroll 1
     for (int k = 0; k < mine; ++k) {
@@ -242,99 +260,112 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
       const uint32_t held =
           *reinterpret_cast<const uint32_t*>(st + 2 * kTile * S::ROW + S::SCALES) & 0xffffu;
 
-      float s[2][4];
+      float s[NT][4];                // positions g, g + 8 by rows 2 cc, 2 cc + 1
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
 #pragma unroll
-      for (int bl = 0; bl < BLOCKS; ++bl)
+      for (int bl = 0; bl < BLOCKS; ++bl) {
+        const uint4 u = kt[S::place(g, 4 * bl + cc)], v = kt[S::place(g + 8, 4 * bl + cc)];
+        if constexpr (CODE == Code::kHalf) {
+          const uint32_t f0[4] = {u.x, v.x, u.y, v.y}, f1[4] = {u.z, v.z, u.w, v.w};
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
-          const uint4 v = kt[S::place(g + 8 * nt, 4 * bl + cc)];
-          if constexpr (CODE == Code::kHalf) {
-            Mma<CT>::run(s[nt], qf[2 * bl], v.x, v.y);
-            Mma<CT>::run(s[nt], qf[2 * bl + 1], v.z, v.w);
-          } else {
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+          for (int nt = 0; nt < NT; ++nt) {
+            Mma<CT>::run(s[nt], f0, qf[nt][2 * bl][0], qf[nt][2 * bl][1]);
+            Mma<CT>::run(s[nt], f1, qf[nt][2 * bl + 1][0], qf[nt][2 * bl + 1][1]);
+          }
+        } else {
+          const uint32_t wu[4] = {u.x, u.y, u.z, u.w}, wv[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
-              Mma<CT>::run(s[nt], qf[4 * bl + x], pair_of<CT, CODE>(w[x]),
-                          pair_of<CT, CODE>(w[x] >> 16));
+          for (int x = 0; x < 4; ++x) {
+            const uint32_t f[4] = {pair_of<CT, CODE>(wu[x]), pair_of<CT, CODE>(wv[x]),
+                                   pair_of<CT, CODE>(wu[x] >> 16), pair_of<CT, CODE>(wv[x] >> 16)};
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+              Mma<CT>::run(s[nt], f, qf[nt][4 * bl + x][0], qf[nt][4 * bl + x][1]);
           }
         }
+      }
 
       const int j0 = lo + (warp + k * kWarps) * kTile;
-      float vs[2][2], ex[2][2];
+      float vs[2] = {1.f, 1.f}, ex[2] = {0.f, 0.f}, ks[2] = {1.f, 1.f};
+      if constexpr (S::SCALES > 0) {
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int tok = nt * 8 + 2 * cc + x;
-          vs[nt][x] = S::SCALES ? sc[kTile + tok] : 1.f;
-          ex[nt][x] = S::SCALES ? weight_exponent(vs[nt][x]) : 0.f;
-          s[nt][x] *= S::SCALES ? back[0] * sc[tok] : back[0];
-          s[nt][x + 2] *= S::SCALES ? back[1] * sc[tok] : back[1];
+        for (int y = 0; y < 2; ++y) {
+          ks[y] = sc[g + 8 * y];
+          vs[y] = sc[kTile + g + 8 * y];
+          ex[y] = weight_exponent(vs[y]);
         }
-      const int p_first = base + t_first;
-      const bool whole = held == 0xffffu && j0 + kTile - 1 <= p_first &&
-                         (a.window == 0 || j0 > base + a.by_group.div(r_last) - a.window);
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[nt][e] *= back[nt][e & 1];
+          if (S::SCALES) s[nt][e] *= ks[e >> 1];
+        }
+      const bool whole = held == 0xffffu && j0 + kTile - 1 <= base + t_first &&
+                         (a.window == 0 || j0 > base + t_last - a.window);
       if (!whole) {
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
+        for (int e = 0; e < 4; ++e) {
+          const int tok = g + 8 * (e >> 1), j = j0 + tok;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int tok = nt * 8 + 2 * cc + (e & 1), j = j0 + tok, p = pos[e >> 1];
+          for (int nt = 0; nt < NT; ++nt) {
+            const int p = pos[nt][e & 1];
             const bool vis = (held >> tok & 1) && j <= p && (a.window == 0 || j > p - a.window);
             if (!vis) s[nt][e] = -INFINITY;
           }
+        }
       }
-
-      float corr[2];
+      // The maximum moves when some weight would pass 2^8 (first of all from nothing);
+      // until then no lane needs another's scores.
+      bool past = false;
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        float t = fmaxf(fmaxf(s[0][2 * x] + ex[0][0], s[0][2 * x + 1] + ex[0][1]),
-                        fmaxf(s[1][2 * x] + ex[1][0], s[1][2 * x + 1] + ex[1][1]));
-        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
-        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
-        const float mn = fmaxf(m[x], t), use = mn == -INFINITY ? 0.f : mn;
-        corr[x] = exp2_fast(m[x] - use);
-        m[x] = mn;
-        float sum = 0.f;
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
+        for (int e = 0; e < 4; ++e) {
+          const float t = s[nt][e] + ex[e >> 1];
+          past |= t > m[nt][e & 1] + 8.f;
+        }
+      if (__any_sync(0xffffffffu, past)) {
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float p = exp2_fast(s[nt][2 * x + e] - use);
-            sum += p;
-            s[nt][2 * x + e] = p;
-          }
-        l[x] = __fmaf_rn(l[x], corr[x], sum);
-      }
-      if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
-#pragma unroll
-        for (int n = 0; n < DIM / 8; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[n][e] *= corr[e >> 1];
-      }
-      uint32_t pf[4];
-      if constexpr (CODE == Code::kHalf) {
-        pf[0] = pack<CT>(s[0][0], s[0][1]);
-        pf[1] = pack<CT>(s[0][2], s[0][3]);
-        pf[2] = pack<CT>(s[1][0], s[1][1]);
-        pf[3] = pack<CT>(s[1][2], s[1][3]);
-      } else {
-        // a masked position's scale may be anything: its weight stays zero
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            const float u = s[nt][2 * x], w = s[nt][2 * x + 1];
-            pf[2 * nt + x] = pack<CT>(u == 0.f ? 0.f : u * vs[nt][0], w == 0.f ? 0.f : w * vs[nt][1]);
+            float t = fmaxf(s[nt][x] + ex[0], s[nt][x + 2] + ex[1]);
+            t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
+            t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
+            t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
+            const float mn = fmaxf(m[nt][x], t);
+            const float f = m[nt][x] == -INFINITY ? 0.f : exp2_fast(m[nt][x] - mn);
+            m[nt][x] = mn;
+            l[nt][x] *= f;
+#pragma unroll
+            for (int n = 0; n < DIM / 16; ++n) {
+              o[nt][n][x] *= f;
+              o[nt][n][x + 2] *= f;
+            }
           }
       }
-      // values: columns of n-tile jj stand 8 (16) elements apart, as a lane's read
-      // of neighbouring elements delivers them
+      uint32_t pf[NT][2];            // rows g by positions 2 cc, 2 cc + 1 (+ 8)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float use = m[nt][e & 1] == -INFINITY ? 0.f : m[nt][e & 1];
+          p[e] = exp2_fast(s[nt][e] - use);
+          l[nt][e & 1] += p[e];
+          // (a masked position's scale may be anything: its weight stays zero)
+          if (S::SCALES) p[e] = p[e] == 0.f ? 0.f : p[e] * vs[e >> 1];
+        }
+        pf[nt][0] = turned(pack<CT>(p[0], p[1]));
+        pf[nt][1] = turned(pack<CT>(p[2], p[3]));
+      }
+      // values: an m-tile's rows g and g + 8 are neighbouring elements, as a lane's
+      // read delivers them
       if constexpr (CODE == Code::kHalf) {
 #pragma unroll
         for (int set = 0; set < DIM / 64; ++set) {
@@ -347,10 +378,13 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
                                     {v[2].x, v[2].y, v[2].z, v[2].w},
                                     {v[3].x, v[3].y, v[3].z, v[3].w}};
 #pragma unroll
-          for (int jj = 0; jj < 8; ++jj) {
-            const uint32_t sel = jj & 1 ? 0x7632 : 0x5410;
-            Mma<CT>::run(o[set * 8 + jj], pf, __byte_perm(w[0][jj >> 1], w[1][jj >> 1], sel),
-                         __byte_perm(w[2][jj >> 1], w[3][jj >> 1], sel));
+          for (int y = 0; y < 4; ++y) {
+            const uint32_t f[4] = {__byte_perm(w[0][y], w[1][y], 0x5410),
+                                   __byte_perm(w[0][y], w[1][y], 0x7632),
+                                   __byte_perm(w[2][y], w[3][y], 0x5410),
+                                   __byte_perm(w[2][y], w[3][y], 0x7632)};
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) Mma<CT>::run(o[nt][set * 4 + y], f, pf[nt][0], pf[nt][1]);
           }
         }
       } else {
@@ -378,9 +412,10 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
             const uint32_t sel = hf ? 0x7362 : 0x5140;
             const uint32_t u = __byte_perm(w[0][y], w[1][y], sel);
             const uint32_t z = __byte_perm(w[2][y], w[3][y], sel);
-            Mma<CT>::run(o[4 * y + 2 * hf], pf, pair_of<CT, CODE>(u), pair_of<CT, CODE>(z));
-            Mma<CT>::run(o[4 * y + 2 * hf + 1], pf, pair_of<CT, CODE>(u >> 16),
-                         pair_of<CT, CODE>(z >> 16));
+            const uint32_t f[4] = {pair_of<CT, CODE>(u), pair_of<CT, CODE>(u >> 16),
+                                   pair_of<CT, CODE>(z), pair_of<CT, CODE>(z >> 16)};
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) Mma<CT>::run(o[nt][2 * y + hf], f, pf[nt][0], pf[nt][1]);
           }
       }
       __syncwarp();
@@ -389,47 +424,48 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
     wait_copies<0>();
 
     // join the four warps
+    __shared__ float w_m[kWarps][S::ROWS], w_l[kWarps][S::ROWS];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      l[x] += __shfl_xor_sync(0xffffffffu, l[x], 1);
-      l[x] += __shfl_xor_sync(0xffffffffu, l[x], 2);
-    }
-    __shared__ float w_m[kWarps][kTile], w_l[kWarps][kTile];
-    __shared__ unsigned again;
-    if (cc == 0) {
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        w_m[warp][g + 8 * x] = m[x];
-        w_l[warp][g + 8 * x] = l[x];
+        float sum = l[nt][x];
+        sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+        if (g == 0) {
+          w_m[warp][8 * nt + 2 * cc + x] = m[nt][x];
+          w_l[warp][8 * nt + 2 * cc + x] = sum;
+        }
       }
-    }
-    if (threadIdx.x == 0) again = 0;
     __syncthreads();
     constexpr int PITCH = DIM + 4;
     float* os = reinterpret_cast<float*>(sm);
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int r = g + 8 * x;
-      float top = w_m[0][r];
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int w = 1; w < kWarps; ++w) top = fmaxf(top, w_m[w][r]);
-      const float f = m[x] == -INFINITY ? 0.f : exp2_fast(m[x] - top);
-      float* dst = os + (warp * kTile + r) * PITCH;
+      for (int x = 0; x < 2; ++x) {
+        const int r = 8 * nt + 2 * cc + x;
+        float top = w_m[0][r];
 #pragma unroll
-      for (int n = 0; n < DIM / 8; ++n)
+        for (int w = 1; w < kWarps; ++w) top = fmaxf(top, w_m[w][r]);
+        const float f = m[nt][x] == -INFINITY ? 0.f : exp2_fast(m[nt][x] - top);
+        float* dst = os + (warp * S::ROWS + r) * PITCH;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          // column of n-tile n that this lane holds: see the reads above
+        for (int n = 0; n < DIM / 16; ++n) {
+          // elements of m-tile n that this lane holds: see the reads above
           int d;
-          if constexpr (CODE == Code::kHalf) d = (n / 8) * 64 + 8 * (2 * cc + e) + n % 8;
-          else d = (DIM / 8) * (2 * cc + e) + n;
+          if constexpr (CODE == Code::kHalf) d = (n / 4) * 64 + 8 * g + 2 * (n % 4);
+          else d = (DIM / 8) * g + 2 * n;
           // a warp that saw nothing has nothing to add, whatever it multiplied
-          dst[d] = f == 0.f ? 0.f : o[n][2 * x + e] * f;
+          *reinterpret_cast<float2*>(dst + d) =
+              f == 0.f ? make_float2(0.f, 0.f)
+                       : make_float2(o[nt][n][x] * f, o[nt][n][x + 2] * f);
         }
-    }
+      }
     __syncthreads();
     constexpr int LPR = 32, EL = DIM / LPR;
-    for (int r = warp; r < kTile; r += kWarps) {
+    for (int r = warp; r < S::ROWS; r += kWarps) {
       const int rr = r_first + r;
       if (rr >= rows) break;
       float top = w_m[0][r];
@@ -443,7 +479,7 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
         const float f = w_m[w][r] == -INFINITY ? 0.f : exp2_fast(w_m[w][r] - top);
         sum = __fmaf_rn(w_l[w][r], f, sum);
 #pragma unroll
-        for (int e = 0; e < EL; ++e) x[e] += os[(w * kTile + r) * PITCH + lane * EL + e];
+        for (int e = 0; e < EL; ++e) x[e] += os[(w * S::ROWS + r) * PITCH + lane * EL + e];
       }
       bool odd = false;
 #pragma unroll
@@ -464,7 +500,7 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
           else *reinterpret_cast<float2*>(p) = make_float2(x[0], x[1]);
         }
       } else {
-        const float by = top == -INFINITY ? 0.f : div_rn(1.f, sum);
+        const float by = saw_nothing(top, sum) ? 0.f : div_rn(1.f, sum);
         T* p = reinterpret_cast<T*>(a.out) + row * a.o_row + h * a.o_head + lane * EL;
 #pragma unroll
         for (int e = 0; e < EL; e += 2)
@@ -504,14 +540,14 @@ k_join(AttendArgs a, BatchArgs b) {
   float sum = 0.f, x[EL];
 #pragma unroll
   for (int e = 0; e < EL; ++e) x[e] = 0.f;
-  if (top > -INFINITY) {
+  {
 #pragma unroll 4
     for (int sp = 0; sp < a.parts; ++sp) {
       const int64_t at = sp * rows_heads + w;
       const float2 v = ml[at];
-      if (v.x == -INFINITY) continue;
-      const float f = exp2_fast(v.x - top);
+      const float f = v.x == -INFINITY ? 0.f : exp2_fast(v.x - top);
       sum = __fmaf_rn(v.y, f, sum);
+      if (f == 0.f) continue;              // (nothing was left there)
       const float* p = a.part_o + at * DIM + lane * EL;
       float y[EL];
       if constexpr (EL == 4) {
@@ -525,39 +561,45 @@ k_join(AttendArgs a, BatchArgs b) {
       for (int e = 0; e < EL; ++e) x[e] = __fmaf_rn(y[e], f, x[e]);
     }
   }
-  const float by = top == -INFINITY ? 0.f : div_rn(1.f, sum);
+  const float by = saw_nothing(top, sum) ? 0.f : div_rn(1.f, sum);
   T* p = reinterpret_cast<T*>(a.out) + t * a.o_row + h * a.o_head + lane * EL;
 #pragma unroll
   for (int e = 0; e < EL; e += 2)
     *reinterpret_cast<uint32_t*>(p + e) = pack<T>(x[e] * by, x[e + 1] * by);
   if (a.lse && lane == 0)
-    a.lse[t * a.heads + h] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * kLn2;
+    a.lse[t * a.heads + h] = saw_nothing(top, sum) ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
-template <class T, Code CODE, int DIM>
+template <class T, Code CODE, int DIM, int NT>
 cudaError_t launch_typed(const AttendArgs& a, const BatchArgs& b, const CacheArgs& c,
                          cudaStream_t s) {
-  using S = Shape<CODE, DIM>;
-  const void* fn = (const void*)k_attend<T, CODE, DIM>;
+  using S = Shape<CODE, DIM, NT>;
+  const void* fn = (const void*)k_attend<T, CODE, DIM, NT>;
   cudaError_t e = func_smem_once(fn, S::SMEM, true);
   if (e) return e;
   const int64_t blocks = (int64_t)c.heads * a.parts * a.row_tiles * b.n_seq;
   if (blocks > 2147483647) return cudaErrorInvalidValue;
-  k_attend<T, CODE, DIM><<<(unsigned)blocks, kWarps * 32, S::SMEM, s>>>(a, b, c);
+  k_attend<T, CODE, DIM, NT><<<(unsigned)blocks, kWarps * 32, S::SMEM, s>>>(a, b, c);
   return cudaGetLastError();
 }
 
+template <class T, Code CODE, int DIM>
+cudaError_t launch_rows(int nt, const AttendArgs& a, const BatchArgs& b, const CacheArgs& c,
+                        cudaStream_t s) {
+  return nt == 1 ? launch_typed<T, CODE, DIM, 1>(a, b, c, s) : launch_typed<T, CODE, DIM, 2>(a, b, c, s);
+}
+
 template <class T>
-cudaError_t launch_code(int code, int dim, const AttendArgs& a, const BatchArgs& b,
+cudaError_t launch_code(int code, int dim, int nt, const AttendArgs& a, const BatchArgs& b,
                         const CacheArgs& c, cudaStream_t s) {
   if (code == TRE_E4M3)
-    return dim == 64 ? launch_typed<T, Code::kE4m3, 64>(a, b, c, s)
-                     : launch_typed<T, Code::kE4m3, 128>(a, b, c, s);
+    return dim == 64 ? launch_rows<T, Code::kE4m3, 64>(nt, a, b, c, s)
+                     : launch_rows<T, Code::kE4m3, 128>(nt, a, b, c, s);
   if (code == TRE_I8)
-    return dim == 64 ? launch_typed<T, Code::kI8, 64>(a, b, c, s)
-                     : launch_typed<T, Code::kI8, 128>(a, b, c, s);
-  return dim == 64 ? launch_typed<T, Code::kHalf, 64>(a, b, c, s)
-                   : launch_typed<T, Code::kHalf, 128>(a, b, c, s);
+    return dim == 64 ? launch_rows<T, Code::kI8, 64>(nt, a, b, c, s)
+                     : launch_rows<T, Code::kI8, 128>(nt, a, b, c, s);
+  return dim == 64 ? launch_rows<T, Code::kHalf, 64>(nt, a, b, c, s)
+                   : launch_rows<T, Code::kHalf, 128>(nt, a, b, c, s);
 }
 
 template <class T>
@@ -575,7 +617,7 @@ struct Plan {
   int32_t few, tokens;            // (see AttendArgs)
   int32_t parts[2], split[2];     // k_attend, k_attend_tc
   int64_t part_rows[2];
-  int32_t row_tiles;
+  int32_t row_tiles, nt;          // of k_attend: tiles of 8 * nt rows
   int64_t units;                  // of k_attend_tc, at most
 };
 
@@ -597,7 +639,10 @@ Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page) {
     // Parts of a context: enough blocks to fill the GPU a few times over, none
     // shorter than 256 tokens (a part costs a block's start and its share of the
     // join, about what 256 tokens of keys and values cost to read).
-    p.row_tiles = p.tc ? 1 : (int)std::min<int64_t>((rows + kTile - 1) / kTile, 1 << 20);
+    // Tiles of 8 rows where one new token's heads (or all rows there are) fit in one,
+    // else of 16, which read keys and values once for twice the rows.
+    p.nt = (p.tc ? a.group : rows) <= 8 ? 1 : 2;
+    p.row_tiles = p.tc ? 1 : (int)std::min<int64_t>((rows + 8 * p.nt - 1) / (8 * p.nt), 1 << 20);
     const int64_t units = std::max<int64_t>(1, (int64_t)b->n_seq * heads * p.row_tiles);
     const int64_t want = std::max<int64_t>(1, (sms * 8 + units - 1) / units);
     p.parts[0] = (int)std::min<int64_t>({want, std::max<int64_t>(1, len / 256), 256});
@@ -653,8 +698,8 @@ cudaError_t launch_all(int dtype, int code, int dim, AttendArgs a, const Plan& p
   x.row_tiles = p.row_tiles;
   x.tokens = p.tokens;
   if (p.parts[1] > 1) x.done = reinterpret_cast<float2*>(part_ml[1]);
-  e = bf ? launch_code<__nv_bfloat16>(code, dim, x, b, c, s)
-         : launch_code<__half>(code, dim, x, b, c, s);
+  e = bf ? launch_code<__nv_bfloat16>(code, dim, p.nt, x, b, c, s)
+         : launch_code<__half>(code, dim, p.nt, x, b, c, s);
   if (!e && p.parts[0] > 1)
     e = bf ? launch_join<__nv_bfloat16>(dim, x, b, s) : launch_join<__half>(dim, x, b, s);
   if (!e && p.parts[1] > 1)

@@ -75,6 +75,9 @@ __device__ __forceinline__ void part_of(const AttendArgs& a, int sp, int& lo, in
   hi = to;
 }
 
+// Whether a row saw no position (scores that are no number leave m alone, not l).
+__device__ __forceinline__ bool saw_nothing(float m, float l) { return m == -INFINITY && l == l; }
+
 // What a block leaves beside a row's sum: for its part of the join, or (one part)
 // the row's logarithm, and for the other kernel's join that the row is not its (a weight
 // below zero).
@@ -84,7 +87,7 @@ __device__ __forceinline__ void row_state(const AttendArgs& a, int sp, int64_t r
     reinterpret_cast<float2*>(a.part_ml)[(sp * a.part_rows + part_row) * a.heads + head] =
         make_float2(m, l);
   else if (a.lse)
-    a.lse[row * a.heads + head] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * kLn2;
+    a.lse[row * a.heads + head] = saw_nothing(m, l) ? -INFINITY : (m + log2f(l)) * kLn2;
   if (a.done && sp == 0) a.done[row * a.heads + head] = make_float2(0.f, -1.f);
 }
 

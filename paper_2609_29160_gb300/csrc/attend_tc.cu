@@ -628,7 +628,7 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
       const int tok = a.by_group.div(min(r, rows - 1));
       const int h_q = kvh * a.group + (min(r, rows - 1) - tok * a.group);
       const int64_t t_row = (int64_t)(start + tok);
-      const float by = m == -INFINITY ? 0.f : a.parts > 1 ? 1.f : div_rn(1.f, l);
+      const float by = saw_nothing(m, l) ? 0.f : a.parts > 1 ? 1.f : div_rn(1.f, l);
       const int64_t at = ((int64_t)sp * a.part_rows + t_row) * a.heads + h_q;
       bool odd = false;
 #pragma unroll 1

@@ -141,6 +141,15 @@ def test_values_ahead_do_not_reach_earlier_rows(pool, lens):
     assert not torch.isfinite(out[-1].double()).any()
 
 
+@pytest.mark.parametrize("lens", [[(40, 1)], [(4000, 1)], [(30, 200)]])
+def test_keys_that_are_no_number(lens):
+    bt = ref.Batch(lens, 16, 1, 64, torch.bfloat16, seed=20)
+    bt.k[:] = math.nan
+    q = torch.randn(bt.rows, 4, 64, device="cuda").bfloat16()
+    out, lse = tre.tre_chunk_attention(q, bt.cache(tre), bt.batch(tre), lse=True)
+    assert torch.isnan(out).all() and torch.isnan(lse).all()
+
+
 @pytest.mark.parametrize("scale", [1e-6, 3.0])
 def test_scales(scale):
     bt = ref.Batch([(400, 1), (100, 150)], 16, 2, 64, torch.bfloat16, seed=15)
