@@ -511,14 +511,15 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
   }
 }
 
-// Joins the parts of each row: a block a part row, a warp a (row, head).
+// Joins the parts of each row, W warps a (row, head), the parts dealt out among them.
 constexpr int kJoinWarps = 8;
-template <class T, int DIM>
+template <class T, int DIM, int W>
 __global__ void __launch_bounds__(kJoinWarps * 32)
 k_join(AttendArgs a, BatchArgs b) {
-  const int lane = threadIdx.x & 31, h = blockIdx.y * kJoinWarps + (threadIdx.x >> 5);
-  if (h >= a.heads) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int h = blockIdx.y * (kJoinWarps / W) + warp / W, mine = warp % W;
   int64_t t = blockIdx.x;
+  bool go = h < a.heads;
   if (a.tokens > 0) {
     const int i = blockIdx.x / a.tokens, r = blockIdx.x - i * a.tokens;
     const Seq s = seq_of(b, i);
@@ -529,20 +530,22 @@ k_join(AttendArgs a, BatchArgs b) {
   constexpr int EL = DIM / 32;
   const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
   float top = -INFINITY, first = 0.f;
-  for (int sp = lane; sp < a.parts; sp += 32) {
-    const float2 v = ml[sp * rows_heads + w];
-    if (sp == 0) first = v.y;
-    top = fmaxf(top, v.x);
+  if (go) {
+    for (int sp = lane; sp < a.parts; sp += 32) {
+      const float2 v = ml[sp * rows_heads + w];
+      if (sp == 0) first = v.y;
+      top = fmaxf(top, v.x);
+    }
   }
-  if (__shfl_sync(0xffffffffu, first, 0) < 0.f) return;         // not this join's
+  go = go && !(__shfl_sync(0xffffffffu, first, 0) < 0.f);       // not this join's
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
   float sum = 0.f, x[EL];
 #pragma unroll
   for (int e = 0; e < EL; ++e) x[e] = 0.f;
-  {
+  if (go) {
 #pragma unroll 4
-    for (int sp = 0; sp < a.parts; ++sp) {
+    for (int sp = mine; sp < a.parts; sp += W) {
       const int64_t at = sp * rows_heads + w;
       const float2 v = ml[at];
       const float f = v.x == -INFINITY ? 0.f : exp2_fast(v.x - top);
@@ -561,6 +564,21 @@ k_join(AttendArgs a, BatchArgs b) {
       for (int e = 0; e < EL; ++e) x[e] = __fmaf_rn(y[e], f, x[e]);
     }
   }
+  if constexpr (W > 1) {
+    __shared__ float part[kJoinWarps][DIM + 1];
+#pragma unroll
+    for (int e = 0; e < EL; ++e) part[warp][lane * EL + e] = x[e];
+    if (lane == 0) part[warp][DIM] = sum;
+    __syncthreads();
+    if (mine != 0) return;
+#pragma unroll
+    for (int k = 1; k < W; ++k) {
+      sum += part[warp + k][DIM];
+#pragma unroll
+      for (int e = 0; e < EL; ++e) x[e] += part[warp + k][lane * EL + e];
+    }
+  }
+  if (!go) return;
   const float by = saw_nothing(top, sum) ? 0.f : div_rn(1.f, sum);
   T* p = reinterpret_cast<T*>(a.out) + t * a.o_row + h * a.o_head + lane * EL;
 #pragma unroll
@@ -602,13 +620,26 @@ cudaError_t launch_code(int code, int dim, int nt, const AttendArgs& a, const Ba
                    : launch_rows<T, Code::kHalf, 128>(nt, a, b, c, s);
 }
 
-template <class T>
-cudaError_t launch_join(int dim, const AttendArgs& a, const BatchArgs& b, cudaStream_t s) {
+// From 16 parts on a block's eight warps share a row: a warp alone reads them one after
+// another.
+template <class T, int DIM>
+cudaError_t launch_join(const AttendArgs& a, const BatchArgs& b, cudaStream_t s) {
   if (a.part_rows > 2147483647) return cudaErrorInvalidValue;
-  const dim3 grid((unsigned)a.part_rows, (a.heads + kJoinWarps - 1) / kJoinWarps);
-  if (dim == 64) k_join<T, 64><<<grid, kJoinWarps * 32, 0, s>>>(a, b);
-  else k_join<T, 128><<<grid, kJoinWarps * 32, 0, s>>>(a, b);
+  if (a.parts >= 16) {
+    const dim3 grid((unsigned)a.part_rows, a.heads);
+    k_join<T, DIM, kJoinWarps><<<grid, kJoinWarps * 32, 0, s>>>(a, b);
+  } else {
+    const dim3 grid((unsigned)a.part_rows, (a.heads + kJoinWarps - 1) / kJoinWarps);
+    k_join<T, DIM, 1><<<grid, kJoinWarps * 32, 0, s>>>(a, b);
+  }
   return cudaGetLastError();
+}
+
+cudaError_t join(int dtype, int dim, const AttendArgs& a, const BatchArgs& b, cudaStream_t s) {
+  if (a.parts < 2) return cudaSuccess;
+  if (dtype == TRE_BF16)
+    return dim == 64 ? launch_join<__nv_bfloat16, 64>(a, b, s) : launch_join<__nv_bfloat16, 128>(a, b, s);
+  return dim == 64 ? launch_join<__half, 64>(a, b, s) : launch_join<__half, 128>(a, b, s);
 }
 
 // How a call is split, from what the host knows of it.
@@ -636,16 +667,18 @@ Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page) {
   p.tc = rows > kFew;
   p.few = p.tc ? kFew : 2147483647;
   {
-    // Parts of a context: enough blocks to fill the GPU a few times over, none
-    // shorter than 256 tokens (a part costs a block's start and its share of the
-    // join, about what 256 tokens of keys and values cost to read).
+    // Parts of a context: about 16 blocks an SM, so that sequences of unequal length
+    // even out (8 blocks an SM took 3 to 14% longer on ragged batches, 48 up to 9%), of
+    // 1,024 tokens at least (parts of 256 cost 10% on short contexts) unless there are
+    // then fewer than two blocks an SM, where parts go down to 256.
     // Tiles of 8 rows where one new token's heads (or all rows there are) fit in one,
     // else of 16, which read keys and values once for twice the rows.
     p.nt = (p.tc ? a.group : rows) <= 8 ? 1 : 2;
     p.row_tiles = p.tc ? 1 : (int)std::min<int64_t>((rows + 8 * p.nt - 1) / (8 * p.nt), 1 << 20);
     const int64_t units = std::max<int64_t>(1, (int64_t)b->n_seq * heads * p.row_tiles);
-    const int64_t want = std::max<int64_t>(1, (sms * 8 + units - 1) / units);
-    p.parts[0] = (int)std::min<int64_t>({want, std::max<int64_t>(1, len / 256), 256});
+    const int64_t want = (sms * 16 + units - 1) / units, few = (sms * 2 + units - 1) / units;
+    const int64_t most = std::max(len / 1024, std::min(few, len / 256));
+    p.parts[0] = (int)std::max<int64_t>(1, std::min<int64_t>({want, most, 256}));
     p.split[0] = (int)std::max<int64_t>(kTile * kWarps, (len + p.parts[0] - 1) / p.parts[0]);
   }
   p.tokens = p.tc ? std::max(1, kFew / a.group) : 0;
@@ -700,10 +733,8 @@ cudaError_t launch_all(int dtype, int code, int dim, AttendArgs a, const Plan& p
   if (p.parts[1] > 1) x.done = reinterpret_cast<float2*>(part_ml[1]);
   e = bf ? launch_code<__nv_bfloat16>(code, dim, p.nt, x, b, c, s)
          : launch_code<__half>(code, dim, p.nt, x, b, c, s);
-  if (!e && p.parts[0] > 1)
-    e = bf ? launch_join<__nv_bfloat16>(dim, x, b, s) : launch_join<__half>(dim, x, b, s);
-  if (!e && p.parts[1] > 1)
-    e = bf ? launch_join<__nv_bfloat16>(dim, of(1), b, s) : launch_join<__half>(dim, of(1), b, s);
+  if (!e) e = join(dtype, dim, x, b, s);
+  if (!e && p.tc) e = join(dtype, dim, of(1), b, s);
   return e;
 }
 
