@@ -3,10 +3,12 @@
 // k_heads: y = x * w / sqrt(mean x^2 + eps), then the rotation of the row's
 // position, then either a rounding to the input's type or a cache code: scale
 // amax|y| / Q (Q = 448 for e4m3, 127 for int8), code = round(y / scale). A row of
-// 64 or 128 elements is read once, 16 bytes a lane, stays in registers, and its
-// sums and maxima are shuffles among its lanes; everything is 32-bit until the one
-// rounding at the end, and the division is the exact one, so codes do not depend on
-// how a row is reached. Bound by HBM when there are many rows, by the chain
+// 64 or 128 elements is read once and stays in the registers of 8 or 16 lanes, each
+// with four elements and the four that they turn with, so only its sum and maximum go
+// between lanes; everything is 32-bit until the one rounding at the end, and the
+// division is the exact one, so codes do not depend on how a row is reached. A warp
+// takes a whole token where there are many: its place in the cache, cosines and sines
+// are fetched once for all heads. Bound by HBM when there are many rows, by the chain
 // q_start -> lengths -> page -> store when there are few.
 //
 // k_read: codes (and scales) of whole tokens back to rows of a model's type.
@@ -43,7 +45,7 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 
 template <int W> __device__ __forceinline__ float group_sum(float v) {
 #pragma unroll
-  for (int o = W / 2; o > 0; o >>= 1) v = add_rn(v, __shfl_xor_sync(0xffffffffu, v, o));
+  for (int o = W / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
 template <int W> __device__ __forceinline__ float group_max(float v) {
@@ -52,37 +54,91 @@ template <int W> __device__ __forceinline__ float group_max(float v) {
   return v;
 }
 
-// One warp takes NIT iterations of 32 / LPR rows of one token: the token's place
-// and its cosines and sines are fetched once for all of them.
-template <class T, Code CODE, int D, int NIT>
-__global__ void __launch_bounds__(kThreads)
-k_heads(HeadsArgs a, BatchArgs b, CacheArgs c, int groups, tre_diag* diag) {
-  constexpr int N = Vec<T>::N, LPR = D / N, RPW = 32 / LPR;
-  const int lane = threadIdx.x & 31, sub = lane / LPR, e0 = (lane % LPR) * N;
+// Four elements of T
+template <class T> struct Four {
+  using Raw = uint2;
+  static __device__ __forceinline__ Raw zero() { return make_uint2(0, 0); }
+  static __device__ __forceinline__ void get(const Raw& v, float* x) {
+    unpack(v.x, x[0], x[1], T());
+    unpack(v.y, x[2], x[3], T());
+  }
+  static __device__ __forceinline__ Raw put(const float* x) {
+    return make_uint2(pack<T>(x[0], x[1]), pack<T>(x[2], x[3]));
+  }
+};
+template <> struct Four<float> {
+  using Raw = uint4;
+  static __device__ __forceinline__ Raw zero() { return make_uint4(0, 0, 0, 0); }
+  static __device__ __forceinline__ void get(const Raw& v, float* x) { Vec<float>::get(v, x); }
+  static __device__ __forceinline__ Raw put(const float* x) { return Vec<float>::put(x); }
+};
+
+// x / d correctly rounded, given y = 1 / d correctly rounded: a product, its exact
+// remainder and one correction (P. Markstein, "Computation of elementary functions on
+// the IBM RISC System/6000 processor", 1990). For d in [2^-100, 2^100] and |x| <= 512 d;
+// a quotient so small that its remainder underflows rounds to a code of zero either way.
+__device__ __forceinline__ float quotient(float x, float d, float y) {
+  const float q = __fmul_rn(x, y);
+  return __fmaf_rn(__fmaf_rn(-q, d, x), y, q);
+}
+
+// Four codes of x / by
+template <Code CODE> __device__ __forceinline__ uint32_t codes_of(const float* q) {
+  if constexpr (CODE == Code::kE4m3) {
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(q[0], q[1]), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(q[2], q[3]), __NV_SATFINITE, __NV_E4M3);
+    return lo | hi << 16;
+  } else {
+    // (|x| <= 127 scales, so nothing to clamp but what is no number, which gives 0)
+    uint32_t v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = (uint32_t)__float2int_rn(q[j]);
+    return __byte_perm(__byte_perm(v[0], v[1], 0x0040), __byte_perm(v[2], v[3], 0x0040), 0x5410);
+  }
+}
+
+// A warp takes `its` steps of RPW rows of a token's q, k and v heads; `groups` warps
+// share a token.
+template <class T, Code CODE, int D>
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : 4)
+k_heads(HeadsArgs a, BatchArgs b, CacheArgs c, int groups, int its, tre_diag* diag) {
+  using F = Four<T>;
+  constexpr int LPR = D / 8, RPW = 32 / LPR, U = sizeof(T) == 4 ? 2 : 4, EL = sizeof(T);
+  const int lane = threadIdx.x & 31, sub = lane / LPR, u = lane % LPR;
   const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
   const int64_t t64 = w / groups;
   if (t64 >= a.n_rows) return;
   const int t = (int)t64, grp = (int)(w - t64 * groups);
   const int n_heads = a.heads[0] + a.heads[1] + a.heads[2];
+  // this lane's elements: ea .. ea + 3 and those they turn with, eb .. eb + 3 (a row's
+  // unturned tail is halved in the same way)
+  const int half = a.rot >> 1;
+  const bool turns = 4 * u < half;
+  const int ea = a.interleaved ? 8 * u : turns ? 4 * u : half + 4 * u;
+  const int eb = ea + (a.interleaved ? 4 : turns ? half : (D - a.rot) >> 1);
 
-  // the rows first: they depend on nothing
-  uint4 raw[NIT];
-  int kind[NIT], head[NIT];
+  typename F::Raw raw[U][2];
+  int kind[U], head[U];
+  auto load = [&](int it) {
 #pragma unroll
-  for (int it = 0; it < NIT; ++it) {
-    int h = (grp * NIT + it) * RPW + sub;
-    kind[it] = -1;
-    raw[it] = make_uint4(0, 0, 0, 0);
-    if (h < n_heads) {
-      int s = 0;
-      if (h >= a.heads[0]) { h -= a.heads[0]; s = 1; }
-      if (s == 1 && h >= a.heads[1]) { h -= a.heads[1]; s = 2; }
-      kind[it] = s;
-      head[it] = h;
-      raw[it] = *reinterpret_cast<const uint4*>(a.in[s] + t * a.row[s] + h * a.head[s] +
-                                                e0 * (int)sizeof(T));
+    for (int k = 0; k < U; ++k) {
+      int h = (it + k) * RPW + sub;
+      kind[k] = -1;
+      head[k] = 0;
+      raw[k][0] = raw[k][1] = F::zero();
+      if (it + k < (grp + 1) * its && h < n_heads) {
+        int s = 0;
+        if (h >= a.heads[0]) { h -= a.heads[0]; s = 1; }
+        if (s == 1 && h >= a.heads[1]) { h -= a.heads[1]; s = 2; }
+        kind[k] = s;
+        head[k] = h;
+        const uint8_t* p = a.in[s] + t * a.row[s] + h * a.head[s];
+        raw[k][0] = *reinterpret_cast<const typename F::Raw*>(p + ea * EL);
+        raw[k][1] = *reinterpret_cast<const typename F::Raw*>(p + eb * EL);
+      }
     }
-  }
+  };
+  load(grp * its);               // the first rows: they depend on nothing
 
   // where the token stands
   int pos, page = 0, slot = 0;
@@ -91,15 +147,12 @@ k_heads(HeadsArgs a, BatchArgs b, CacheArgs c, int groups, tre_diag* diag) {
     pos = a.positions ? a.positions[t] : 0;
   } else {
     const int i = find_seq(b, t);
-    if (i < 0) {
-      ok = counted = false;
-      pos = 0;
-    } else {
+    pos = 0;
+    ok = counted = false;
+    if (i >= 0) {
       const int end = b.q_start[i + 1];
-      if (t >= end) {
-        ok = counted = false;
-        pos = 0;
-      } else {
+      if (t < end) {
+        counted = true;
         pos = b.ctx_len[i] - (end - t);
         page = page_of(c, b, i, pos, slot);
         ok = page >= 0;
@@ -110,126 +163,109 @@ k_heads(HeadsArgs a, BatchArgs b, CacheArgs c, int groups, tre_diag* diag) {
   if (!ok && counted && diag && grp == 0 && lane == 0)
     atomicAdd((unsigned long long*)&diag->dropped_range, 1ull);
 
-  float cs[N], sn[N];
-  const int half = a.rot >> 1;
-  const bool turned = a.cos_sin && e0 < a.rot;
-  const int mate = a.interleaved || !turned ? lane : lane + (e0 < half ? half : -half) / N;
-  if (turned && ok) {
-    const float* p = a.cos_sin + pos * a.cs_row;
-    if (a.interleaved) {
-#pragma unroll
-      for (int e = 0; e < N; e += 2) {
-        cs[e] = cs[e + 1] = p[(e0 + e) >> 1];
-        sn[e + 1] = p[half + ((e0 + e) >> 1)];
-        sn[e] = -sn[e + 1];
-      }
-    } else {
-      const int i0 = e0 < half ? e0 : e0 - half;
-#pragma unroll
-      for (int e = 0; e < N; e += 4) {
-        const float4 u = *reinterpret_cast<const float4*>(p + i0 + e);
-        const float4 z = *reinterpret_cast<const float4*>(p + half + i0 + e);
-        cs[e] = u.x; cs[e + 1] = u.y; cs[e + 2] = u.z; cs[e + 3] = u.w;
-        sn[e] = z.x; sn[e + 1] = z.y; sn[e + 2] = z.z; sn[e + 3] = z.w;
-      }
-      if (e0 < half) {
-#pragma unroll
-        for (int e = 0; e < N; ++e) sn[e] = -sn[e];
-      }
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < N; ++e) { cs[e] = 1.f; sn[e] = 0.f; }
+  float cs[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
+  if (a.cos_sin && turns && ok) {
+    const float* p = a.cos_sin + pos * a.cs_row + 4 * u;
+    const float4 y = *reinterpret_cast<const float4*>(p);
+    const float4 z = *reinterpret_cast<const float4*>(p + half);
+    cs[0] = y.x; cs[1] = y.y; cs[2] = y.z; cs[3] = y.w;
+    sn[0] = z.x; sn[1] = z.y; sn[2] = z.z; sn[3] = z.w;
   }
+  const bool normed = a.weight[0] || a.weight[1];
+  auto weight = [&](const void* wt, float* g) {
+    if (a.weight_f32) {
+      Four<float>::get(*reinterpret_cast<const uint4*>(static_cast<const float*>(wt) + ea), g);
+      Four<float>::get(*reinterpret_cast<const uint4*>(static_cast<const float*>(wt) + eb), g + 4);
+    } else {
+      F::get(*reinterpret_cast<const typename F::Raw*>(static_cast<const T*>(wt) + ea), g);
+      F::get(*reinterpret_cast<const typename F::Raw*>(static_cast<const T*>(wt) + eb), g + 4);
+    }
+  };
+  const int64_t at = page * c.s_page + slot * c.s_token;
 
+  for (int it = grp * its;;) {
 #pragma unroll
-  for (int it = 0; it < NIT; ++it) {
-    const int s = kind[it];
-    float x[N];
-    Vec<T>::get(raw[it], x);
-    const void* wt = s == 0 ? a.weight[0] : s == 1 ? a.weight[1] : nullptr;
-    if (a.weight[0] || a.weight[1]) {
-      float ss = 0.f;
+    for (int k = 0; k < U; ++k) {
+      const int s = kind[k];
+      float x[8];
+      F::get(raw[k][0], x);
+      F::get(raw[k][1], x + 4);
+      if (normed) {
+        const void* wt = s == 0 ? a.weight[0] : s == 1 ? a.weight[1] : nullptr;
+        float ss = 0.f;
 #pragma unroll
-      for (int e = 0; e < N; ++e) ss = __fmaf_rn(x[e], x[e], ss);
-      ss = group_sum<LPR>(ss);
-      if (wt) {
-        const float r = div_rn(1.f, __fsqrt_rn(add_rn(div_rn(ss, (float)D), a.eps)));
-        float g[N];
-        if (a.weight_f32) {
+        for (int e = 0; e < 8; ++e) ss = __fmaf_rn(x[e], x[e], ss);
+        ss = group_sum<LPR>(ss);
+        if (wt) {
+          const float r = rsqrtf(__fmaf_rn(ss, 1.f / D, a.eps));
+          float g[8];
+          weight(wt, g);
 #pragma unroll
-          for (int e = 0; e < N; ++e) g[e] = static_cast<const float*>(wt)[e0 + e];
-        } else {
-          Vec<T>::get(*reinterpret_cast<const uint4*>(static_cast<const T*>(wt) + e0), g);
+          for (int e = 0; e < 8; ++e) x[e] = x[e] * r * g[e];
         }
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = mul_rn(mul_rn(x[e], r), g[e]);
       }
-    }
-    if (a.cos_sin) {
-      float y[N];
-      if (a.interleaved) {
+      if (a.cos_sin && s < 2 && turns) {
+        if (a.interleaved) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) y[e] = x[e ^ 1];
-      } else {
+          for (int e = 0; e < 4; ++e) {
+            const float p = x[2 * e], q = x[2 * e + 1];
+            x[2 * e] = __fmaf_rn(p, cs[e], -(q * sn[e]));
+            x[2 * e + 1] = __fmaf_rn(q, cs[e], p * sn[e]);
+          }
+        } else {
 #pragma unroll
-        for (int e = 0; e < N; ++e) y[e] = __shfl_sync(0xffffffffu, x[e], mate);
-      }
-      if (turned && s < 2) {
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = add_rn(mul_rn(x[e], cs[e]), mul_rn(y[e], sn[e]));
-      }
-    }
-    const bool stored = CODE != Code::kNone && s >= 1;
-    if (s >= 0 && !stored) {
-      if (!ok) {
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = 0.f;
-      }
-      *reinterpret_cast<uint4*>(a.out[s] + t * a.orow[s] + head[it] * a.ohead[s] +
-                                e0 * (int)sizeof(T)) = Vec<T>::put(x);
-    }
-    if (CODE == Code::kHalf && stored && ok) {
-      uint8_t* base = s == 1 ? c.k : c.v;
-      *reinterpret_cast<uint4*>(base + (page * c.s_page + slot * c.s_token + head[it] * c.s_head +
-                                        e0) * (int)sizeof(T)) = Vec<T>::put(x);
-    }
-    if (CODE == Code::kE4m3 || CODE == Code::kI8) {
-      float m = fabsf(x[0]);
-#pragma unroll
-      for (int e = 1; e < N; ++e) m = max_nan(m, fabsf(x[e]));
-      m = group_max<LPR>(m);
-      if (stored && ok) {
-        const float sc = div_rn(m, CODE == Code::kE4m3 ? 448.f : 127.f);
-        const float by = sc == 0.f ? 1.f : sc;
-        uint32_t code[N / 4 > 0 ? N / 4 : 1];
-#pragma unroll
-        for (int e = 0; e < N; e += 4) {
-          float y[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) y[j] = div_rn(x[e + j], by);
-          if (CODE == Code::kE4m3) {
-            const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(y[0], y[1]), __NV_SATFINITE,
-                                                         __NV_E4M3);
-            const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(y[2], y[3]), __NV_SATFINITE,
-                                                         __NV_E4M3);
-            code[e / 4] = lo | hi << 16;
-          } else {
-            uint32_t v = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              v |= (uint32_t)(uint8_t)(int8_t)max(-127, min(127, __float2int_rn(y[j]))) << (8 * j);
-            code[e / 4] = v;
+          for (int e = 0; e < 4; ++e) {
+            const float p = x[e], q = x[e + 4];
+            x[e] = __fmaf_rn(p, cs[e], -(q * sn[e]));
+            x[e + 4] = __fmaf_rn(q, cs[e], p * sn[e]);
           }
         }
-        uint8_t* base = (s == 1 ? c.k : c.v) + page * c.s_page + slot * c.s_token +
-                        head[it] * c.s_head + e0;
-        *reinterpret_cast<uint2*>(base) = make_uint2(code[0], code[N / 4 - 1]);
-        if (e0 == 0)
-          (s == 1 ? c.k_scale : c.v_scale)[page * c.c_page + slot * c.c_token +
-                                           head[it] * c.c_head] = sc;
+      }
+      const bool stored = CODE != Code::kNone && s >= 1;
+      if (s >= 0 && !stored) {
+        if (!ok) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = 0.f;
+        }
+        uint8_t* p = a.out[s] + t * a.orow[s] + head[k] * a.ohead[s];
+        *reinterpret_cast<typename F::Raw*>(p + ea * EL) = F::put(x);
+        *reinterpret_cast<typename F::Raw*>(p + eb * EL) = F::put(x + 4);
+      }
+      if constexpr (CODE == Code::kHalf) {
+        if (stored && ok) {
+          uint8_t* p = (s == 1 ? c.k : c.v) + (at + head[k] * c.s_head) * EL;
+          *reinterpret_cast<typename F::Raw*>(p + ea * EL) = F::put(x);
+          *reinterpret_cast<typename F::Raw*>(p + eb * EL) = F::put(x + 4);
+        }
+      }
+      if constexpr (CODE == Code::kE4m3 || CODE == Code::kI8) {
+        float m = fabsf(x[0]);
+#pragma unroll
+        for (int e = 1; e < 8; ++e) m = max_nan(m, fabsf(x[e]));
+        m = group_max<LPR>(m);
+        if (stored && ok) {
+          const float sc = div_rn(m, CODE == Code::kE4m3 ? 448.f : 127.f);
+          const float by = sc == 0.f ? 1.f : sc, r = div_rn(1.f, by);
+          float q[8];
+          if (by > 0x1p-100f && by < 0x1p100f) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) q[e] = quotient(x[e], by, r);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) q[e] = div_rn(x[e], by);
+          }
+          uint8_t* p = (s == 1 ? c.k : c.v) + at + head[k] * c.s_head;
+          *reinterpret_cast<uint32_t*>(p + ea) = codes_of<CODE>(q);
+          *reinterpret_cast<uint32_t*>(p + eb) = codes_of<CODE>(q + 4);
+          if (u == 0)
+            (s == 1 ? c.k_scale : c.v_scale)[page * c.c_page + slot * c.c_token +
+                                             head[k] * c.c_head] = sc;
+        }
       }
     }
+    it += U;
+    if (it >= (grp + 1) * its || it * RPW >= n_heads) break;
+    load(it);
   }
 }
 
@@ -364,24 +400,21 @@ bool heads_args(const tre_heads* h, bool keys_out, HeadsArgs& a) {
   return true;
 }
 
-// Four rows a lane when that still leaves every SM 32 warps (one load of the
-// token's place and of its rotation for four times the rows), one otherwise.
+// A warp takes a whole token's heads when that leaves every SM 32 warps (its place and
+// its rotation are then fetched once for all of them), else as few as still does.
 template <class T, Code CODE, int D>
 cudaError_t launch_heads(const HeadsArgs& a, const BatchArgs& b, const CacheArgs& c,
                          tre_diag* diag, cudaStream_t s) {
-  constexpr int RPW = 32 / (D / Vec<T>::N);
+  constexpr int RPW = 32 / (D / 8);
   const int n = a.heads[0] + a.heads[1] + a.heads[2];
   if (n == 0 || a.n_rows == 0) return cudaSuccess;
-  const int g4 = (n + 4 * RPW - 1) / (4 * RPW), g1 = (n + RPW - 1) / RPW;
+  const int64_t steps = (n + RPW - 1) / RPW, warps = (int64_t)device_sm_count() * 32;
+  const int64_t its = std::min(steps, std::max<int64_t>(1, a.n_rows * steps / warps));
+  const int64_t groups = (steps + its - 1) / its;
   constexpr int64_t per = kThreads / 32;
-  if ((int64_t)a.n_rows * g4 >= (int64_t)device_sm_count() * 32) {
-    const int64_t blocks = ((int64_t)a.n_rows * g4 + per - 1) / per;
-    if (blocks > 2147483647) return cudaErrorInvalidValue;
-    k_heads<T, CODE, D, 4><<<(unsigned)blocks, kThreads, 0, s>>>(a, b, c, g4, diag);
-  } else {
-    const int64_t blocks = ((int64_t)a.n_rows * g1 + per - 1) / per;
-    k_heads<T, CODE, D, 1><<<(unsigned)blocks, kThreads, 0, s>>>(a, b, c, g1, diag);
-  }
+  const int64_t blocks = ((int64_t)a.n_rows * groups + per - 1) / per;
+  if (blocks > 2147483647) return cudaErrorInvalidValue;
+  k_heads<T, CODE, D><<<(unsigned)blocks, kThreads, 0, s>>>(a, b, c, (int)groups, (int)its, diag);
   return cudaGetLastError();
 }
 
