@@ -89,10 +89,10 @@ template <Code CODE> __device__ __forceinline__ uint32_t codes_of(const float* q
     const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(q[2], q[3]), __NV_SATFINITE, __NV_E4M3);
     return lo | hi << 16;
   } else {
-    // (|x| <= 127 scales, so nothing to clamp but what is no number, which gives 0)
+    // |q| <= 127: in q + 1.5 * 2^23 the last byte is q rounded to nearest even
     uint32_t v[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = (uint32_t)__float2int_rn(q[j]);
+    for (int j = 0; j < 4; ++j) v[j] = __float_as_uint(__fadd_rn(q[j], 12582912.f));
     return __byte_perm(__byte_perm(v[0], v[1], 0x0040), __byte_perm(v[2], v[3], 0x0040), 0x5410);
   }
 }
@@ -105,11 +105,15 @@ k_heads(HeadsArgs a, BatchArgs b, CacheArgs c, int groups, int its, tre_diag* di
   using F = Four<T>;
   constexpr int LPR = D / 8, RPW = 32 / LPR, U = sizeof(T) == 4 ? 2 : 4, EL = sizeof(T);
   const int lane = threadIdx.x & 31, sub = lane / LPR, u = lane % LPR;
-  const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-  const int64_t t64 = w / groups;
-  if (t64 >= a.n_rows) return;
-  const int t = (int)t64, grp = (int)(w - t64 * groups);
-  const int n_heads = a.heads[0] + a.heads[1] + a.heads[2];
+  const uint32_t w =
+      __shfl_sync(0xffffffffu, blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), 0);
+  const int t = (int)(w / groups), grp = (int)(w - (uint32_t)t * groups);
+  if (t >= a.n_rows) return;
+  // steps of q, of k, of v: a step's rows are of one kind
+  const int first_k = (a.heads[0] + RPW - 1) / RPW;
+  const int first_v = first_k + (a.heads[1] + RPW - 1) / RPW;
+  const int n_steps = first_v + (a.heads[2] + RPW - 1) / RPW;
+  const int end_step = min((grp + 1) * its, n_steps);
   // this lane's elements: ea .. ea + 3 and those they turn with, eb .. eb + 3 (a row's
   // unturned tail is halved in the same way)
   const int half = a.rot >> 1;
@@ -118,20 +122,16 @@ k_heads(HeadsArgs a, BatchArgs b, CacheArgs c, int groups, int its, tre_diag* di
   const int eb = ea + (a.interleaved ? 4 : turns ? half : (D - a.rot) >> 1);
 
   typename F::Raw raw[U][2];
-  int kind[U], head[U];
+  auto kind_of = [&](int st) { return st < first_k ? 0 : st < first_v ? 1 : 2; };
+  auto head_of = [&](int st, int s) {
+    return (st - (s == 0 ? 0 : s == 1 ? first_k : first_v)) * RPW + sub;
+  };
   auto load = [&](int it) {
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-      int h = (it + k) * RPW + sub;
-      kind[k] = -1;
-      head[k] = 0;
+      const int s = kind_of(it + k), h = head_of(it + k, s);
       raw[k][0] = raw[k][1] = F::zero();
-      if (it + k < (grp + 1) * its && h < n_heads) {
-        int s = 0;
-        if (h >= a.heads[0]) { h -= a.heads[0]; s = 1; }
-        if (s == 1 && h >= a.heads[1]) { h -= a.heads[1]; s = 2; }
-        kind[k] = s;
-        head[k] = h;
+      if (it + k < end_step && h < a.heads[s]) {
         const uint8_t* p = a.in[s] + t * a.row[s] + h * a.head[s];
         raw[k][0] = *reinterpret_cast<const typename F::Raw*>(p + ea * EL);
         raw[k][1] = *reinterpret_cast<const typename F::Raw*>(p + eb * EL);
@@ -171,7 +171,6 @@ k_heads(HeadsArgs a, BatchArgs b, CacheArgs c, int groups, int its, tre_diag* di
     cs[0] = y.x; cs[1] = y.y; cs[2] = y.z; cs[3] = y.w;
     sn[0] = z.x; sn[1] = z.y; sn[2] = z.z; sn[3] = z.w;
   }
-  const bool normed = a.weight[0] || a.weight[1];
   auto weight = [&](const void* wt, float* g) {
     if (a.weight_f32) {
       Four<float>::get(*reinterpret_cast<const uint4*>(static_cast<const float*>(wt) + ea), g);
@@ -183,26 +182,25 @@ k_heads(HeadsArgs a, BatchArgs b, CacheArgs c, int groups, int its, tre_diag* di
   };
   const int64_t at = page * c.s_page + slot * c.s_token;
 
-  for (int it = grp * its;;) {
+  for (int it = grp * its; it < end_step; load(it += U)) {
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-      const int s = kind[k];
+      if (it + k >= end_step) break;
+      const int s = kind_of(it + k), h = head_of(it + k, s);
+      const bool there = h < a.heads[s];
       float x[8];
       F::get(raw[k][0], x);
       F::get(raw[k][1], x + 4);
-      if (normed) {
-        const void* wt = s == 0 ? a.weight[0] : s == 1 ? a.weight[1] : nullptr;
+      const void* wt = s == 0 ? a.weight[0] : s == 1 ? a.weight[1] : nullptr;
+      if (wt) {
         float ss = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) ss = __fmaf_rn(x[e], x[e], ss);
-        ss = group_sum<LPR>(ss);
-        if (wt) {
-          const float r = rsqrtf(__fmaf_rn(ss, 1.f / D, a.eps));
-          float g[8];
-          weight(wt, g);
+        const float r = rsqrtf(__fmaf_rn(group_sum<LPR>(ss), 1.f / D, a.eps));
+        float g[8];
+        weight(wt, g);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = x[e] * r * g[e];
-        }
+        for (int e = 0; e < 8; ++e) x[e] = x[e] * r * g[e];
       }
       if (a.cos_sin && s < 2 && turns) {
         if (a.interleaved) {
@@ -222,50 +220,50 @@ k_heads(HeadsArgs a, BatchArgs b, CacheArgs c, int groups, int its, tre_diag* di
         }
       }
       const bool stored = CODE != Code::kNone && s >= 1;
-      if (s >= 0 && !stored) {
+      if (there && !stored) {
         if (!ok) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] = 0.f;
         }
-        uint8_t* p = a.out[s] + t * a.orow[s] + head[k] * a.ohead[s];
+        uint8_t* p = a.out[s] + t * a.orow[s] + h * a.ohead[s];
         *reinterpret_cast<typename F::Raw*>(p + ea * EL) = F::put(x);
         *reinterpret_cast<typename F::Raw*>(p + eb * EL) = F::put(x + 4);
       }
       if constexpr (CODE == Code::kHalf) {
-        if (stored && ok) {
-          uint8_t* p = (s == 1 ? c.k : c.v) + (at + head[k] * c.s_head) * EL;
+        if (stored && ok && there) {
+          uint8_t* p = (s == 1 ? c.k : c.v) + (at + h * c.s_head) * EL;
           *reinterpret_cast<typename F::Raw*>(p + ea * EL) = F::put(x);
           *reinterpret_cast<typename F::Raw*>(p + eb * EL) = F::put(x + 4);
         }
       }
-      if constexpr (CODE == Code::kE4m3 || CODE == Code::kI8) {
+      if ((CODE == Code::kE4m3 || CODE == Code::kI8) && stored) {
         float m = fabsf(x[0]);
 #pragma unroll
         for (int e = 1; e < 8; ++e) m = max_nan(m, fabsf(x[e]));
         m = group_max<LPR>(m);
-        if (stored && ok) {
-          const float sc = div_rn(m, CODE == Code::kE4m3 ? 448.f : 127.f);
-          const float by = sc == 0.f ? 1.f : sc, r = div_rn(1.f, by);
+        if (ok && there) {
+          constexpr float Q = CODE == Code::kE4m3 ? 448.f : 127.f;
+          const bool plain = m > 0x1p-90f && m < 0x1p90f;
+          // (an infinite maximum leaves a scale that is no number)
+          const float sc = plain ? quotient(m, Q, 1.f / Q) : div_rn(m, Q) + 0.f * m;
+          const float by = sc == 0.f ? 1.f : sc, r = __frcp_rn(by);
           float q[8];
-          if (by > 0x1p-100f && by < 0x1p100f) {
+          if (plain) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) q[e] = quotient(x[e], by, r);
           } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) q[e] = div_rn(x[e], by);
           }
-          uint8_t* p = (s == 1 ? c.k : c.v) + at + head[k] * c.s_head;
+          uint8_t* p = (s == 1 ? c.k : c.v) + at + h * c.s_head;
           *reinterpret_cast<uint32_t*>(p + ea) = codes_of<CODE>(q);
           *reinterpret_cast<uint32_t*>(p + eb) = codes_of<CODE>(q + 4);
           if (u == 0)
             (s == 1 ? c.k_scale : c.v_scale)[page * c.c_page + slot * c.c_token +
-                                             head[k] * c.c_head] = sc;
+                                             h * c.c_head] = sc;
         }
       }
     }
-    it += U;
-    if (it >= (grp + 1) * its || it * RPW >= n_heads) break;
-    load(it);
   }
 }
 
@@ -406,9 +404,10 @@ template <class T, Code CODE, int D>
 cudaError_t launch_heads(const HeadsArgs& a, const BatchArgs& b, const CacheArgs& c,
                          tre_diag* diag, cudaStream_t s) {
   constexpr int RPW = 32 / (D / 8);
-  const int n = a.heads[0] + a.heads[1] + a.heads[2];
-  if (n == 0 || a.n_rows == 0) return cudaSuccess;
-  const int64_t steps = (n + RPW - 1) / RPW, warps = (int64_t)device_sm_count() * 32;
+  if (a.heads[0] + a.heads[1] + a.heads[2] == 0 || a.n_rows == 0) return cudaSuccess;
+  int64_t steps = 0;
+  for (int x = 0; x < 3; ++x) steps += (a.heads[x] + RPW - 1) / RPW;
+  const int64_t warps = (int64_t)device_sm_count() * 32;
   const int64_t its = std::min(steps, std::max<int64_t>(1, a.n_rows * steps / warps));
   const int64_t groups = (steps + its - 1) / its;
   constexpr int64_t per = kThreads / 32;
