@@ -13,6 +13,7 @@
 //
 // k_read: codes (and scales) of whole tokens back to rows of a model's type.
 #include <algorithm>
+#include <type_traits>
 
 #include "internal.h"
 #include "kvcache.cuh"
@@ -122,23 +123,18 @@ k_heads(HeadsArgs a, BatchArgs b, CacheArgs c, int groups, int its, tre_diag* di
   const int eb = ea + (a.interleaved ? 4 : turns ? half : (D - a.rot) >> 1);
 
   typename F::Raw raw[U][2];
-  auto kind_of = [&](int st) { return st < first_k ? 0 : st < first_v ? 1 : 2; };
-  auto head_of = [&](int st, int s) {
-    return (st - (s == 0 ? 0 : s == 1 ? first_k : first_v)) * RPW + sub;
-  };
-  auto load = [&](int it) {
+  // the first rows: they depend on nothing
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
-      const int s = kind_of(it + k), h = head_of(it + k, s);
-      raw[k][0] = raw[k][1] = F::zero();
-      if (it + k < end_step && h < a.heads[s]) {
-        const uint8_t* p = a.in[s] + t * a.row[s] + h * a.head[s];
-        raw[k][0] = *reinterpret_cast<const typename F::Raw*>(p + ea * EL);
-        raw[k][1] = *reinterpret_cast<const typename F::Raw*>(p + eb * EL);
-      }
+  for (int k = 0; k < U; ++k) {
+    const int st = grp * its + k, s = st < first_k ? 0 : st < first_v ? 1 : 2;
+    const int h = (st - (s == 0 ? 0 : s == 1 ? first_k : first_v)) * RPW + sub;
+    raw[k][0] = raw[k][1] = F::zero();
+    if (st < end_step && h < a.heads[s]) {
+      const uint8_t* p = a.in[s] + t * a.row[s] + h * a.head[s];
+      raw[k][0] = *reinterpret_cast<const typename F::Raw*>(p + ea * EL);
+      raw[k][1] = *reinterpret_cast<const typename F::Raw*>(p + eb * EL);
     }
-  };
-  load(grp * its);               // the first rows: they depend on nothing
+  }
 
   // where the token stands
   int pos, page = 0, slot = 0;
@@ -171,100 +167,126 @@ k_heads(HeadsArgs a, BatchArgs b, CacheArgs c, int groups, int its, tre_diag* di
     cs[0] = y.x; cs[1] = y.y; cs[2] = y.z; cs[3] = y.w;
     sn[0] = z.x; sn[1] = z.y; sn[2] = z.z; sn[3] = z.w;
   }
-  auto weight = [&](const void* wt, float* g) {
-    if (a.weight_f32) {
-      Four<float>::get(*reinterpret_cast<const uint4*>(static_cast<const float*>(wt) + ea), g);
-      Four<float>::get(*reinterpret_cast<const uint4*>(static_cast<const float*>(wt) + eb), g + 4);
-    } else {
-      F::get(*reinterpret_cast<const typename F::Raw*>(static_cast<const T*>(wt) + ea), g);
-      F::get(*reinterpret_cast<const typename F::Raw*>(static_cast<const T*>(wt) + eb), g + 4);
-    }
-  };
   const int64_t at = page * c.s_page + slot * c.s_token;
 
-  for (int it = grp * its; it < end_step; load(it += U)) {
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
-      if (it + k >= end_step) break;
-      const int s = kind_of(it + k), h = head_of(it + k, s);
-      const bool there = h < a.heads[s];
-      float x[8];
-      F::get(raw[k][0], x);
-      F::get(raw[k][1], x + 4);
-      const void* wt = s == 0 ? a.weight[0] : s == 1 ? a.weight[1] : nullptr;
-      if (wt) {
-        float ss = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ss = __fmaf_rn(x[e], x[e], ss);
-        const float r = rsqrtf(__fmaf_rn(group_sum<LPR>(ss), 1.f / D, a.eps));
-        float g[8];
-        weight(wt, g);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = x[e] * r * g[e];
+  auto part = [&](auto kind) {
+    constexpr int s = decltype(kind)::value;
+    constexpr bool stored = CODE != Code::kNone && s >= 1;
+    const int from = s == 0 ? 0 : s == 1 ? first_k : first_v;
+    const int upto = min(end_step, s == 0 ? first_k : s == 1 ? first_v : n_steps);
+    int it = max(grp * its, from);
+    if (it >= upto) return;
+    bool have = it == grp * its;
+    const uint8_t* in = a.in[s] + t * a.row[s];
+    const int64_t in_head = a.head[s];
+    uint8_t* out;
+    int64_t out_head;
+    if constexpr (stored) {
+      out = (s == 1 ? c.k : c.v) + at * (CODE == Code::kHalf ? EL : 1);
+      out_head = c.s_head * (CODE == Code::kHalf ? EL : 1);
+    } else {
+      out = a.out[s & 1] + t * a.orow[s & 1];
+      out_head = a.ohead[s & 1];
+    }
+    float g[8];
+    const void* wt = s < 2 ? a.weight[s & 1] : nullptr;
+    if (wt) {
+      if (a.weight_f32) {
+        Four<float>::get(*reinterpret_cast<const uint4*>(static_cast<const float*>(wt) + ea), g);
+        Four<float>::get(*reinterpret_cast<const uint4*>(static_cast<const float*>(wt) + eb), g + 4);
+      } else {
+        F::get(*reinterpret_cast<const typename F::Raw*>(static_cast<const T*>(wt) + ea), g);
+        F::get(*reinterpret_cast<const typename F::Raw*>(static_cast<const T*>(wt) + eb), g + 4);
       }
-      if (a.cos_sin && s < 2 && turns) {
-        if (a.interleaved) {
+    }
+    for (; it < upto; it += U) {
+      if (!have) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float p = x[2 * e], q = x[2 * e + 1];
-            x[2 * e] = __fmaf_rn(p, cs[e], -(q * sn[e]));
-            x[2 * e + 1] = __fmaf_rn(q, cs[e], p * sn[e]);
+        for (int k = 0; k < U; ++k) {
+          const int h = (it + k - from) * RPW + sub;
+          raw[k][0] = raw[k][1] = F::zero();
+          if (it + k < upto && h < a.heads[s]) {
+            const uint8_t* p = in + h * in_head;
+            raw[k][0] = *reinterpret_cast<const typename F::Raw*>(p + ea * EL);
+            raw[k][1] = *reinterpret_cast<const typename F::Raw*>(p + eb * EL);
           }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float p = x[e], q = x[e + 4];
-            x[e] = __fmaf_rn(p, cs[e], -(q * sn[e]));
-            x[e + 4] = __fmaf_rn(q, cs[e], p * sn[e]);
-          }
         }
       }
-      const bool stored = CODE != Code::kNone && s >= 1;
-      if (there && !stored) {
-        if (!ok) {
+      have = false;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = 0.f;
+      for (int k = 0; k < U; ++k) {
+        if (it + k >= upto) break;
+        const int h = (it + k - from) * RPW + sub;
+        const bool there = h < a.heads[s];
+        float x[8];
+        F::get(raw[k][0], x);
+        F::get(raw[k][1], x + 4);
+        if (wt) {
+          float ss = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) ss = __fmaf_rn(x[e], x[e], ss);
+          const float r = rsqrtf(__fmaf_rn(group_sum<LPR>(ss), 1.f / D, a.eps));
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = x[e] * r * g[e];
         }
-        uint8_t* p = a.out[s] + t * a.orow[s] + h * a.ohead[s];
-        *reinterpret_cast<typename F::Raw*>(p + ea * EL) = F::put(x);
-        *reinterpret_cast<typename F::Raw*>(p + eb * EL) = F::put(x + 4);
-      }
-      if constexpr (CODE == Code::kHalf) {
-        if (stored && ok && there) {
-          uint8_t* p = (s == 1 ? c.k : c.v) + (at + h * c.s_head) * EL;
-          *reinterpret_cast<typename F::Raw*>(p + ea * EL) = F::put(x);
-          *reinterpret_cast<typename F::Raw*>(p + eb * EL) = F::put(x + 4);
-        }
-      }
-      if ((CODE == Code::kE4m3 || CODE == Code::kI8) && stored) {
-        float m = fabsf(x[0]);
+        if (s < 2 && a.cos_sin && turns) {
+          if (a.interleaved) {
 #pragma unroll
-        for (int e = 1; e < 8; ++e) m = max_nan(m, fabsf(x[e]));
-        m = group_max<LPR>(m);
-        if (ok && there) {
-          constexpr float Q = CODE == Code::kE4m3 ? 448.f : 127.f;
-          const bool plain = m > 0x1p-90f && m < 0x1p90f;
-          // (an infinite maximum leaves a scale that is no number)
-          const float sc = plain ? quotient(m, Q, 1.f / Q) : div_rn(m, Q) + 0.f * m;
-          const float by = sc == 0.f ? 1.f : sc, r = __frcp_rn(by);
-          float q[8];
-          if (plain) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) q[e] = quotient(x[e], by, r);
+            for (int e = 0; e < 4; ++e) {
+              const float p = x[2 * e], q = x[2 * e + 1];
+              x[2 * e] = __fmaf_rn(p, cs[e], -(q * sn[e]));
+              x[2 * e + 1] = __fmaf_rn(q, cs[e], p * sn[e]);
+            }
           } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) q[e] = div_rn(x[e], by);
+            for (int e = 0; e < 4; ++e) {
+              const float p = x[e], q = x[e + 4];
+              x[e] = __fmaf_rn(p, cs[e], -(q * sn[e]));
+              x[e + 4] = __fmaf_rn(q, cs[e], p * sn[e]);
+            }
           }
-          uint8_t* p = (s == 1 ? c.k : c.v) + at + h * c.s_head;
-          *reinterpret_cast<uint32_t*>(p + ea) = codes_of<CODE>(q);
-          *reinterpret_cast<uint32_t*>(p + eb) = codes_of<CODE>(q + 4);
-          if (u == 0)
-            (s == 1 ? c.k_scale : c.v_scale)[page * c.c_page + slot * c.c_token +
-                                             h * c.c_head] = sc;
+        }
+        uint8_t* p = out + h * out_head;
+        if constexpr (!stored || CODE == Code::kHalf) {
+          if (!stored && !ok) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = 0.f;
+          }
+          if (there && (!stored || ok)) {
+            *reinterpret_cast<typename F::Raw*>(p + ea * EL) = F::put(x);
+            *reinterpret_cast<typename F::Raw*>(p + eb * EL) = F::put(x + 4);
+          }
+        } else {
+          float m = fabsf(x[0]);
+#pragma unroll
+          for (int e = 1; e < 8; ++e) m = max_nan(m, fabsf(x[e]));
+          m = group_max<LPR>(m);
+          if (ok && there) {
+            constexpr float Q = CODE == Code::kE4m3 ? 448.f : 127.f;
+            const bool plain = m > 0x1p-90f && m < 0x1p90f;
+            // (an infinite maximum leaves a scale that is no number)
+            const float sc = plain ? quotient(m, Q, 1.f / Q) : div_rn(m, Q) + 0.f * m;
+            const float by = sc == 0.f ? 1.f : sc, r = __frcp_rn(by);
+            float q[8];
+            if (plain) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) q[e] = quotient(x[e], by, r);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) q[e] = div_rn(x[e], by);
+            }
+            *reinterpret_cast<uint32_t*>(p + ea) = codes_of<CODE>(q);
+            *reinterpret_cast<uint32_t*>(p + eb) = codes_of<CODE>(q + 4);
+            if (u == 0)
+              (s == 1 ? c.k_scale : c.v_scale)[page * c.c_page + slot * c.c_token + h * c.c_head] = sc;
+          }
         }
       }
     }
-  }
+  };
+  part(std::integral_constant<int, 0>());
+  part(std::integral_constant<int, 1>());
+  if constexpr (CODE != Code::kNone) part(std::integral_constant<int, 2>());
 }
 
 struct ReadOut {
