@@ -48,22 +48,6 @@ template <> struct Mma<__half> {
   }
 };
 
-// Two 8-bit codes (the low 16 bits of w) as a pair of T. Both kinds of code are
-// exact in either type.
-template <class T, Code CODE> __device__ __forceinline__ uint32_t pair_of(uint32_t w) {
-  if constexpr (CODE == Code::kE4m3) {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)w, __NV_E4M3);
-    const __half2 v = *reinterpret_cast<const __half2*>(&h);
-    if constexpr (sizeof(T) == 2 && std::is_same<T, __half>::value)
-      return *reinterpret_cast<const uint32_t*>(&v);
-    const float2 f = __half22float2(v);
-    return pack<T>(f.x, f.y);
-  } else {
-    const float lo = (float)(int8_t)w, hi = (float)(int8_t)(w >> 8);
-    return pack<T>(lo, hi);
-  }
-}
-
 template <int N> __device__ __forceinline__ void wait_copies() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
@@ -279,8 +263,8 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
           const uint32_t wu[4] = {u.x, u.y, u.z, u.w}, wv[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            const uint32_t f[4] = {pair_of<CT, CODE>(wu[x]), pair_of<CT, CODE>(wv[x]),
-                                   pair_of<CT, CODE>(wu[x] >> 16), pair_of<CT, CODE>(wv[x] >> 16)};
+            const uint32_t f[4] = {halves<CODE>(wu[x]), halves<CODE>(wv[x]),
+                                   halves<CODE>(wu[x] >> 16), halves<CODE>(wv[x] >> 16)};
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
               Mma<CT>::run(s[nt], f, qf[nt][4 * bl + x][0], qf[nt][4 * bl + x][1]);
@@ -412,8 +396,8 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
             const uint32_t sel = hf ? 0x7362 : 0x5140;
             const uint32_t u = __byte_perm(w[0][y], w[1][y], sel);
             const uint32_t z = __byte_perm(w[2][y], w[3][y], sel);
-            const uint32_t f[4] = {pair_of<CT, CODE>(u), pair_of<CT, CODE>(u >> 16),
-                                   pair_of<CT, CODE>(z), pair_of<CT, CODE>(z >> 16)};
+            const uint32_t f[4] = {halves<CODE>(u), halves<CODE>(u >> 16),
+                                   halves<CODE>(z), halves<CODE>(z >> 16)};
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) Mma<CT>::run(o[nt][2 * y + hf], f, pf[nt][0], pf[nt][1]);
           }

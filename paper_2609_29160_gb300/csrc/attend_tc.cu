@@ -207,14 +207,14 @@ __device__ __forceinline__ void fma2(uint32_t* x, float f, float plus) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(two(x)), "l"(two(f, f)), "l"(two(plus, plus)));
   split(r, x);
 }
+__device__ __forceinline__ void fma2(uint32_t* x, float f, float plus, float plus1) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(two(x)), "l"(two(f, f)), "l"(two(plus, plus1)));
+  split(r, x);
+}
 __device__ __forceinline__ void mul2(uint32_t* x, float f, float g) {
   uint64_t r;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(two(x)), "l"(two(f, g)));
-  split(r, x);
-}
-__device__ __forceinline__ void add2(uint32_t* x, float f, float g) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(two(x)), "l"(two(f, g)));
   split(r, x);
 }
 __device__ __forceinline__ uint64_t sum2(uint64_t s, float a, float b) {
@@ -280,14 +280,17 @@ struct Ask {
 template <Code CODE, int DIM> struct Tc {
   static constexpr bool CODED = CODE != Code::kHalf;
   static constexpr int BUF = kTok * DIM * 2;            // a tile of keys or values
-  static constexpr int RING = DIM == 128 ? (CODED ? 4 : 5) : (CODED ? 8 : 8);
+  static constexpr int RING = DIM == 128 ? (CODED ? 3 : 5) : (CODED ? 6 : 8);
+  static constexpr int RAW = kTok * DIM, RAWS = CODED ? 3 : 0;   // a tile of codes, and how many
   static constexpr int META = DIM == 128 ? 4 : 8;       // tiles whose scales and masks are kept
   static constexpr int Q = 2 * kRows * DIM * 2;
   static constexpr int AT_RING = Q;
-  static constexpr int AT_MASK = AT_RING + RING * BUF;  // uint32 [META][4]
+  static constexpr int AT_RAW = AT_RING + RING * BUF;
+  static constexpr int AT_MASK = AT_RAW + RAWS * RAW;   // uint32 [META][4]
   static constexpr int AT_SCALE = AT_MASK + META * 16;  // float [META][3][kTok]
-  static constexpr int AT_BAR = AT_SCALE + (CODED ? META * 3 * kTok * 4 : 0);
-  static constexpr int BARS = 2 * RING + META + 8 + 2 * kUnits;
+  static constexpr int AT_BACK = AT_SCALE + (CODED ? META * 3 * kTok * 4 : 0);  // float [2][kRows]
+  static constexpr int AT_BAR = AT_BACK + (CODED ? 2 * kRows * 4 : 0);
+  static constexpr int BARS = 2 * RING + 2 * RAWS + META + 8 + 2 * kUnits;
   static constexpr int AT_UNIT = (AT_BAR + BARS * 8 + 16 + 63) / 64 * 64;    // Unit [kUnits]
   static constexpr int SMEM = AT_UNIT + kUnits * 64;
 };
@@ -352,20 +355,12 @@ struct alignas(64) Unit {
   }
 };
 
-// 16 bytes of codes as 16 elements of T
-template <class T, Code CODE>
-__device__ __forceinline__ void widen(const uint4& v, uint4& lo, uint4& hi) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  uint32_t r[8];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float x[4];
-    codes4(w[i], x, CODE == Code::kI8);
-    r[2 * i] = pack<T>(x[0], x[1]);
-    r[2 * i + 1] = pack<T>(x[2], x[3]);
-  }
-  lo = make_uint4(r[0], r[1], r[2], r[3]);
-  hi = make_uint4(r[4], r[5], r[6], r[7]);
+// 16 bytes of codes as 16 halves
+template <Code CODE> __device__ __forceinline__ void widen(const uint4& v, uint4& lo, uint4& hi) {
+  lo = make_uint4(halves<CODE>(v.x), halves<CODE>(v.x >> 16), halves<CODE>(v.y),
+                  halves<CODE>(v.y >> 16));
+  hi = make_uint4(halves<CODE>(v.z), halves<CODE>(v.z >> 16), halves<CODE>(v.w),
+                  halves<CODE>(v.w >> 16));
 }
 
 template <class T, Code CODE, int DIM>
@@ -373,6 +368,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps maps,
             tre_diag* diag) {
   using L = Tc<CODE, DIM>;
+  // codes are multiplied as halves, and queries and weights with them
+  using CT = typename std::conditional<L::CODED, __half, T>::type;
   extern __shared__ __align__(1024) uint8_t sm[];
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -384,11 +381,13 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
   uint64_t* bars = reinterpret_cast<uint64_t*>(sm + L::AT_BAR);
   uint64_t *full = bars, *empty = bars + L::RING, *meta = empty + L::RING, *s_full = meta + L::META,
            *p_full = s_full + 2, *o_done = p_full + 2, *q_full = o_done + 2,
-           *u_full = q_full + 2, *u_empty = u_full + kUnits;
+           *u_full = q_full + 2, *u_empty = u_full + kUnits, *raw_full = u_empty + kUnits,
+           *raw_empty = raw_full + L::RAWS;
   uint32_t* tmem_at = reinterpret_cast<uint32_t*>(bars + L::BARS);
   volatile int* dead = reinterpret_cast<volatile int*>(tmem_at + 1);
   uint32_t* mask_s = reinterpret_cast<uint32_t*>(sm + L::AT_MASK);
   float* scale_s = reinterpret_cast<float*>(sm + L::AT_SCALE);
+  float* back_s = reinterpret_cast<float*>(sm + L::AT_BACK);
   const volatile Unit* units = reinterpret_cast<const volatile Unit*>(sm + L::AT_UNIT);
 
   if (warp == kMmaWarp) {
@@ -409,6 +408,10 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
       bar_init(p_full + x, kRowWarps / 2);
       bar_init(o_done + x, 1);
       bar_init(q_full + x, kRowWarps / 2);
+    }
+    for (int k = 0; k < L::RAWS; ++k) {
+      bar_init(raw_full + k, kCopyWarps);
+      bar_init(raw_empty + k, kCopyWarps);
     }
     for (int k = 0; k < kUnits; ++k) {
       bar_init(u_full + k, 1);
@@ -455,7 +458,27 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
         }
       }
     };
-    auto q_store = [&](const uint4* v) {
+    auto q_store = [&](uint4* v) {
+      if constexpr (L::CODED && !std::is_same<T, CT>::value) {
+        // bfloat16 queries as halves, each row divided by the power of two of its largest
+        // element (nothing within 2^-24 of that is lost); its scores get it back
+#pragma unroll
+        for (int k = 0; k < QS; ++k) {
+          float y[8], top = 0.f;
+          Vec<T>::get(v[k], y);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(y[e]));
+#pragma unroll
+          for (int o = PPR / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          const int ex = min(max((int)(__float_as_uint(top) >> 23), 1), 253);
+          if (q_piece == 0)
+            back_s[x * kRows + q_row0 + k * RPW] = __uint_as_float((uint32_t)ex << 23);
+          const float by = __uint_as_float((uint32_t)(254 - ex) << 23);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] *= by;
+          v[k] = Vec<CT>::put(y);
+        }
+      }
       uint8_t* q_s = sm + x * kRows * DIM * 2 + (q_piece >> 3) * (kRows * 128);
 #pragma unroll
       for (int k = 0; k < QS; ++k) {
@@ -486,6 +509,8 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
       }
       const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
       const uint32_t s_at = tmem + lanes + x * kTok, o_at = tmem + lanes + 256 + x * 128;
+      const float back =
+          L::CODED && !std::is_same<T, CT>::value ? back_s[x * kRows + row] : 1.f;
       float m = -INFINITY, l = 0.f;
 #pragma unroll 1
       for (int k = 0; k < n_mine; ++k) {
@@ -537,8 +562,8 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
             for (int y = 0; y < 8; y += 4) {
               const float4 f = *reinterpret_cast<const float4*>(meta_s + 2 * kTok + e + y);
               uint32_t z[4] = {v[e + y], v[e + y + 1], v[e + y + 2], v[e + y + 3]};
-              add2(z, f.x, f.y);
-              add2(z + 2, f.z, f.w);
+              fma2(z, back, f.x, f.y);
+              fma2(z + 2, back, f.z, f.w);
               t0 = max3(t0, __uint_as_float(z[0]), __uint_as_float(z[1]));
               t1 = max3(t1, __uint_as_float(z[2]), __uint_as_float(z[3]));
             }
@@ -575,8 +600,8 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
 #pragma unroll
           for (int e = 32 * h; e < 32 * h + 32; e += 4) {
             if constexpr (L::CODED) {
-              add2(v + e, -use, -use);
-              add2(v + e + 2, -use, -use);
+              fma2(v + e, back, -use);
+              fma2(v + e + 2, back, -use);
             } else {
               fma2(v + e, a.scale2, -use);
               fma2(v + e + 2, a.scale2, -use);
@@ -593,8 +618,8 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
 #pragma unroll
               for (int z = 0; z < 4; ++z) y[z] = !whole && y[z] == 0.f ? 0.f : y[z] * w[z];
             }
-            p[(e - 32 * h) / 2] = pack<T>(y[0], y[1]);
-            p[(e - 32 * h) / 2 + 1] = pack<T>(y[2], y[3]);
+            p[(e - 32 * h) / 2] = pack<CT>(y[0], y[1]);
+            p[(e - 32 * h) / 2 + 1] = pack<CT>(y[2], y[3]);
           }
           tmem_st16(s_at + 16 * h, p);
         }
@@ -740,23 +765,30 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
         const int64_t y = __shfl_sync(0xffffffffu, off[1], q & 31);
         return q < 32 ? x : y;
       };
+      float sc_k[2] = {0.f, 0.f}, sc_v[2] = {0.f, 0.f};
+      bool sc_there[2] = {false, false};
+      auto scales = [&]() {                    // (asked for when their page is known)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          if (g == 1 && cw != 0) break;
+          const int pg = group[g].page(c);
+          sc_there[g] = pg >= 0;
+          const int64_t o = pg * c.c_page + group[g].slot * c.c_token + kvh * c.c_head;
+          sc_k[g] = pg >= 0 ? c.k_scale[o] : 0.f;
+          sc_v[g] = pg >= 0 ? c.v_scale[o] : 0.f;
+        }
+      };
       auto note = [&](int k) {                 // mask bits and scales, for tile k
         const int ms = (n_tile + k) % L::META;
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
           if (g == 1 && cw != 0) break;
           const int t = (g ? 96 : cw * 32) + lane;
-          const int pg = group[g].page(c);
-          const bool there = pg >= 0;
+          const bool there = L::CODED ? sc_there[g] : group[g].page(c) >= 0;
           const unsigned held = __ballot_sync(0xffffffffu, there);
           if (lane == 0) mask_s[ms * 4 + (t >> 5)] = held;
           if constexpr (L::CODED) {
-            float ks = 0.f, vs = 0.f;
-            if (there) {
-              const int64_t o = pg * c.c_page + group[g].slot * c.c_token + kvh * c.c_head;
-              ks = c.k_scale[o] * a.scale2;
-              vs = c.v_scale[o];
-            }
+            const float ks = sc_k[g] * a.scale2, vs = sc_v[g];
             scale_s[ms * 3 * kTok + t] = ks;
             scale_s[ms * 3 * kTok + kTok + t] = vs;
             scale_s[ms * 3 * kTok + 2 * kTok + t] = weight_exponent(vs);
@@ -766,91 +798,148 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
       };
       // Boxes of whole tiles, every third a warp, one a lane: its page (one that the cache
       // does not have where the table names none: its rows come as zeros).
-      const int box = L::CODED ? 0 : maps.box, boxes = box ? kTok / box : 0;
+      const int box = maps.box, boxes = box ? kTok / box : 0;
       const int my_box = cw + kCopyWarps * lane, my_boxes = (boxes + 2 - cw) / kCopyWarps;
       auto whole_box = [&](int k) { return box > 0 && lo + (k + 1) * kTok <= hi; };
       Ask boxed;
-      look(0, !whole_box(0));
-      if (my_box < boxes) boxed.at(c, b, i, lo + my_box * box, hi);
-      int pending = -1;                        // a tile copied by pieces, not yet announced
-#pragma unroll 1
-      for (int k = 0; k < n && alive; ++k) {
-        const bool by_box = !L::CODED && whole_box(k);
-        note(k);
-        if (!by_box) take();
-        int box_page = boxed.page(c);
-        const int box_slot = boxed.slot;
-        if (box_page < 0) box_page = c.n_pages;
-        look(k + 1, !whole_box(k + 1));
-        if (my_box < boxes) boxed.at(c, b, i, lo + (k + 1) * kTok + my_box * box, k + 1 < n ? hi : 0);
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-          const uint32_t seq = 2 * (n_tile + k) + kv, buf = seq % L::RING;
-          const uint8_t* src = (kv ? c.v : c.k) + piece * 16;
-          uint8_t* dst = sm + L::AT_RING + buf * L::BUF;
-          alive = alive && bar_wait(empty + buf, ((seq / L::RING) & 1) ^ 1, dead);
-          if (!alive) break;
-          if (by_box) {
-            if (lane == 0) bar_expect(full + buf, my_boxes * box * DIM * 2);
-            __syncwarp();
-            if (my_box < boxes) {
-              const uint32_t to = smem_of(dst) + my_box * box * 128;
-#pragma unroll
-              for (int h = 0; h < DIM / 64; ++h)
-                box_load(to + h * (kTok * 128), kv ? &maps.v : &maps.k, h * 64, box_slot, kvh,
-                         box_page, full + buf);
-            }
-            __syncwarp();
-          } else if constexpr (!L::CODED) {
-            const uint32_t to = smem_of(dst) + (piece >> 3) * (kTok * 128);
+      auto ask_box = [&](int k) {
+        if (my_box < boxes) boxed.at(c, b, i, lo + k * kTok + my_box * box, k < n ? hi : 0);
+      };
+      if constexpr (L::CODED) {
+        // ---- codes: raw tiles come a tile ahead, and are widened from shared memory ----
+        int box_page = 0, box_slot = 0;
+        auto fetch = [&](int k, int kv) {
+          {
+            const uint32_t seq = 2 * (n_tile + k) + kv, buf = seq % L::RAWS;
+            const uint8_t* src = (kv ? c.v : c.k) + piece * 16;
+            const uint32_t to = smem_of(sm + L::AT_RAW + buf * L::RAW);
+            alive = alive && bar_wait(raw_empty + buf, ((seq / L::RAWS) & 1) ^ 1, dead);
+            if (!alive) return;
+            if (whole_box(k)) {
+              if (lane == 0) bar_expect(raw_full + buf, my_boxes * box * DIM);
+              __syncwarp();
+              if (my_box < boxes)
+                box_load(to + my_box * box * DIM, kv ? &maps.v : &maps.k, 0, box_slot, kvh, box_page,
+                         raw_full + buf);
+              __syncwarp();
+            } else {
 #pragma unroll 4
-            for (int is = 0; is < (STEPS + 2) / kCopyWarps; ++is) {
-              const int64_t o = place(is);
-              const int st = cw + is * kCopyWarps, tk = tok0 + st * TPS;
-              if (st >= STEPS) break;
-              asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
-                               to + tk * 128 + (((piece & 7) ^ (tk & 7)) << 4)),
-                           "l"(src + (o < 0 ? 0 : o)), "r"(o < 0 ? 0 : 16)
-                           : "memory");
+              for (int is = 0; is < (STEPS + 2) / kCopyWarps; ++is) {
+                const int64_t o = place(is);
+                const int st = cw + is * kCopyWarps;
+                if (st >= STEPS) break;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                                 to + (st * 32 + lane) * 16),
+                             "l"(src + (o < 0 ? 0 : o)), "r"(o < 0 ? 0 : 16)
+                             : "memory");
+              }
+              asm volatile("cp.async.commit_group;" ::: "memory");
+              asm volatile("cp.async.wait_group 0;" ::: "memory");
+              bar_arrive_warp(raw_full + buf);
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            if (pending >= 0) {
-              asm volatile("cp.async.wait_group 1;" ::: "memory");
-              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-              bar_arrive_warp(full + pending);
-            }
-            pending = buf;
-          } else {
-            // 16 codes are two 16-byte pieces of a row
-            uint8_t* to = dst + (piece >> 2) * (kTok * 128);
-            const int pc = (piece & 3) * 2;
-            constexpr int U = 4;
+          }
+        };
+        auto convert = [&](int k, int kv) {
+          const uint32_t seq = 2 * (n_tile + k) + kv, raw = seq % L::RAWS, buf = seq % L::RING;
+          alive = alive && bar_wait(raw_full + raw, (seq / L::RAWS) & 1, dead) &&
+                  bar_wait(empty + buf, ((seq / L::RING) & 1) ^ 1, dead);
+          if (!alive) return;
+          // 16 codes are two 16-byte pieces of a row
+          const uint4* from = reinterpret_cast<const uint4*>(sm + L::AT_RAW + raw * L::RAW) + lane;
+          uint8_t* to = sm + L::AT_RING + buf * L::BUF + (piece >> 2) * (kTok * 128);
+          const int pc = (piece & 3) * 2;
+#pragma unroll 4
+          for (int st = cw; st < STEPS; st += kCopyWarps) {
+            const int tk = tok0 + st * TPS;
+            uint4 w0, w1;
+            widen<CODE>(from[st * 32], w0, w1);
+            *reinterpret_cast<uint4*>(to + tk * 128 + ((pc ^ (tk & 7)) << 4)) = w0;
+            *reinterpret_cast<uint4*>(to + tk * 128 + (((pc + 1) ^ (tk & 7)) << 4)) = w1;
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          bar_arrive_warp(full + buf);
+          bar_arrive_warp(raw_empty + raw);
+        };
+        auto resolve = [&](int k) {            // tile k's places and scales, k + 1 asked for
+          box_page = boxed.page(c);
+          box_slot = boxed.slot;
+          if (box_page < 0) box_page = c.n_pages;
+          if (!whole_box(k)) take();
+          scales();
+          look(k + 1, !whole_box(k + 1));
+          ask_box(k + 1);
+        };
+        look(0, !whole_box(0));
+        ask_box(0);
+        resolve(0);
+        if (n > 0) {
+          fetch(0, 0);
+          fetch(0, 1);
+        }
 #pragma unroll 1
-            for (int is = 0; is * kCopyWarps + cw < STEPS; is += U) {
-              const int st = cw + is * kCopyWarps;
-              uint4 v[U];
-#pragma unroll
-              for (int u = 0; u < U; ++u) {
-                const int64_t o = place(is + u);       // (-1 past the last step)
-                v[u] = make_uint4(0, 0, 0, 0);
-                if (o >= 0) v[u] = *reinterpret_cast<const uint4*>(src + o);
-              }
-#pragma unroll
-              for (int u = 0; u < U; ++u) {
-                const int s = st + u * kCopyWarps, tk = tok0 + s * TPS;
-                if (s >= STEPS) break;
-                uint4 w0, w1;
-                widen<T, CODE>(v[u], w0, w1);
-                *reinterpret_cast<uint4*>(to + tk * 128 + ((pc ^ (tk & 7)) << 4)) = w0;
-                *reinterpret_cast<uint4*>(to + tk * 128 + (((pc + 1) ^ (tk & 7)) << 4)) = w1;
-              }
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            bar_arrive_warp(full + buf);
+        for (int k = 0; k < n && alive; ++k) {
+          note(k);
+          if (k + 1 < n) resolve(k + 1);
+#pragma unroll 1
+          for (int kv = 0; kv < 2; ++kv) {
+            if (k + 1 < n) fetch(k + 1, kv);
+            convert(k, kv);
           }
         }
-      }
-      if constexpr (!L::CODED) {
+      } else {
+        look(0, !whole_box(0));
+        ask_box(0);
+        int pending = -1;                      // a tile copied by pieces, not yet announced
+#pragma unroll 1
+        for (int k = 0; k < n && alive; ++k) {
+          const bool by_box = whole_box(k);
+          note(k);
+          if (!by_box) take();
+          int box_page = boxed.page(c);
+          const int box_slot = boxed.slot;
+          if (box_page < 0) box_page = c.n_pages;
+          look(k + 1, !whole_box(k + 1));
+          ask_box(k + 1);
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv) {
+            const uint32_t seq = 2 * (n_tile + k) + kv, buf = seq % L::RING;
+            const uint8_t* src = (kv ? c.v : c.k) + piece * 16;
+            uint8_t* dst = sm + L::AT_RING + buf * L::BUF;
+            alive = alive && bar_wait(empty + buf, ((seq / L::RING) & 1) ^ 1, dead);
+            if (!alive) break;
+            if (by_box) {
+              if (lane == 0) bar_expect(full + buf, my_boxes * box * DIM * 2);
+              __syncwarp();
+              if (my_box < boxes) {
+                const uint32_t to = smem_of(dst) + my_box * box * 128;
+#pragma unroll
+                for (int h = 0; h < DIM / 64; ++h)
+                  box_load(to + h * (kTok * 128), kv ? &maps.v : &maps.k, h * 64, box_slot, kvh,
+                           box_page, full + buf);
+              }
+              __syncwarp();
+            } else {
+              const uint32_t to = smem_of(dst) + (piece >> 3) * (kTok * 128);
+#pragma unroll 4
+              for (int is = 0; is < (STEPS + 2) / kCopyWarps; ++is) {
+                const int64_t o = place(is);
+                const int st = cw + is * kCopyWarps, tk = tok0 + st * TPS;
+                if (st >= STEPS) break;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                                 to + tk * 128 + (((piece & 7) ^ (tk & 7)) << 4)),
+                             "l"(src + (o < 0 ? 0 : o)), "r"(o < 0 ? 0 : 16)
+                             : "memory");
+              }
+              asm volatile("cp.async.commit_group;" ::: "memory");
+              if (pending >= 0) {
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                bar_arrive_warp(full + pending);
+              }
+              pending = buf;
+            }
+          }
+        }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
         if (alive && pending >= 0) {
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -873,7 +962,7 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
       const int n = max(n_x[0], n_x[1]);
       bar_arrive_warp(u_empty + nu % kUnits);
       {
-        constexpr uint32_t id_s = idesc_of<T>(kTok, false), id_o = idesc_of<T>(DIM, true);
+        constexpr uint32_t id_s = idesc_of<CT>(kTok, false), id_o = idesc_of<CT>(DIM, true);
         const uint32_t q_op = operand(smem_of(sm), 16);
         const uint32_t k_op = operand(smem_of(sm + L::AT_RING), 16);
         const uint32_t v_op = operand(smem_of(sm + L::AT_RING), kTok * 128);
@@ -969,15 +1058,17 @@ Encode encoder() {
   return fn;
 }
 
-// Maps of a cache of 16-bit elements. Tiles start at multiples of 128, so a box of the
-// greatest common divisor of 128 and the page lies in one page; below 8 slots (or where
-// the encoder refuses the strides) tiles are copied by pieces.
-void make_maps(Maps& m, const CacheArgs& c, int dtype, int dim) {
+// Maps of a cache. Tiles start at multiples of 128, so a box of the greatest common
+// divisor of 128 and the page lies in one page; below 8 slots (or where the encoder
+// refuses the strides) tiles are copied by pieces. Elements of 16 bits come in columns of
+// 64 with the products' order of pieces, codes in whole rows as they are.
+void make_maps(Maps& m, const CacheArgs& c, CUtensorMapDataType type, int dim) {
   m.box = 0;
-  const int box = std::gcd(c.page, kTok);
+  const bool coded = type == CU_TENSOR_MAP_DATA_TYPE_UINT8;
+  const int box = std::gcd(c.page, kTok), el = coded ? 1 : 2;
   const Encode enc = box >= 8 && c.n_pages > 0 ? encoder() : nullptr;
   if (!enc) return;
-  const int64_t st[3] = {c.s_token * 2, c.s_head * 2, c.s_page * 2};
+  const int64_t st[3] = {c.s_token * el, c.s_head * el, c.s_page * el};
   cuuint64_t strides[3];
   for (int x = 0; x < 3; ++x) {
     if (st[x] <= 0 || st[x] >= (1ll << 40)) return;
@@ -985,12 +1076,12 @@ void make_maps(Maps& m, const CacheArgs& c, int dtype, int dim) {
   }
   const cuuint64_t dims[4] = {(cuuint64_t)dim, (cuuint64_t)c.page, (cuuint64_t)c.heads,
                               (cuuint64_t)c.n_pages};
-  const cuuint32_t size[4] = {64, (cuuint32_t)box, 1, 1}, one[4] = {1, 1, 1, 1};
-  const CUtensorMapDataType type =
-      dtype == TRE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  const cuuint32_t size[4] = {(cuuint32_t)(coded ? dim : 64), (cuuint32_t)box, 1, 1};
+  const cuuint32_t one[4] = {1, 1, 1, 1};
   for (int x = 0; x < 2; ++x)
     if (enc(x ? &m.v : &m.k, type, 4, x ? c.v : c.k, dims, strides, size, one,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_INTERLEAVE_NONE,
+            coded ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
       return;
   m.box = box;
@@ -1007,8 +1098,11 @@ cudaError_t launch_typed(const AttendArgs& a, const BatchArgs& b, const CacheArg
   const int64_t blocks = std::min<int64_t>(units, device_sm_count());
   Maps maps;
   memset(&maps, 0, sizeof(maps));
-  if (CODE == Code::kHalf)
-    make_maps(maps, c, std::is_same<T, __nv_bfloat16>::value ? TRE_BF16 : TRE_F16, DIM);
+  make_maps(maps, c,
+            CODE != Code::kHalf                       ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+            : std::is_same<T, __nv_bfloat16>::value   ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                      : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+            DIM);
   k_attend_tc<T, CODE, DIM><<<(unsigned)blocks, kThreads, L::SMEM, s>>>(a, b, c, maps, diag);
   return cudaGetLastError();
 }

@@ -76,6 +76,19 @@ __device__ __forceinline__ void codes4(uint32_t v, float* x, bool i8) {
   }
 }
 
+// Two 8-bit codes (the low 16 bits of w) as a pair of halves, which hold both kinds exactly.
+template <Code CODE> __device__ __forceinline__ uint32_t halves(uint32_t w) {
+  if constexpr (CODE == Code::kE4m3) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)w, __NV_E4M3);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  } else {
+    // 0x6400 + u is the half 1024 + u; u = code + 128
+    const uint32_t u = __byte_perm(w ^ 0x8080u, 0x6464u, 0x4140);
+    const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&u), __half2half2(__ushort_as_half(0x6480)));
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+}
+
 // A paged cache as the kernels see it (strides in elements).
 struct CacheArgs {
   uint8_t *k, *v;
