@@ -673,9 +673,12 @@ Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page) {
     // Whole rounds of one block an SM: the number of parts with the least rounds' worth
     // of context. A part costs what a row's partial sum costs to write and read, about
     // 400 positions' products, spread over all SMs; none is shorter than 512.
+    const int64_t all = (int64_t)b->n_rows * a.group;
+    const int64_t most_tiles = std::min<int64_t>(
+        (int64_t)b->n_seq * ((rows + kTcRows - 1) / kTcRows), all / kTcRows + b->n_seq);
+    // (as many as rows of the longest length make, for the choice of parts)
     const int64_t tiles = std::min<int64_t>(
-        (int64_t)b->n_seq * ((rows + kTcRows - 1) / kTcRows),
-        (int64_t)b->n_rows * a.group / kTcRows + b->n_seq);
+        most_tiles, (all + rows - 1) / rows * ((std::min(rows, all) + kTcRows - 1) / kTcRows));
     const int64_t units = std::max<int64_t>(1, tiles * heads);
     double least = 0;
     for (int n = 1; n <= 64 && (n == 1 || len / n >= 512); ++n) {
@@ -687,7 +690,7 @@ Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page) {
       }
     }
     p.split[1] = (int)std::max<int64_t>(kTcTokens, (len + p.parts[1] - 1) / p.parts[1]);
-    p.units = units * p.parts[1];
+    p.units = std::max<int64_t>(1, most_tiles * heads) * p.parts[1];
   }
   return p;
 }

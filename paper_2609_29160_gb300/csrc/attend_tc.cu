@@ -306,6 +306,9 @@ struct alignas(64) Unit {
   __device__ __forceinline__ bool find(const AttendArgs& a, const BatchArgs& b,
                                        const CacheArgs& c, uint32_t u) {
     const int lane = threadIdx.x & 31;
+    // every other round of blocks backwards, so that none has the longer end of each
+    const uint32_t round = u / gridDim.x;
+    if (round & 1) u = round * gridDim.x + (gridDim.x - 1 - (u - round * gridDim.x));
     kvh = (int)(u % c.heads);
     u /= c.heads;
     sp = (int)(u % a.parts);
@@ -731,6 +734,15 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
       if (!some) break;
       const int i = w.i, kvh = w.kvh, lo = w.lo, hi = w.hi, n = max(w.n_x[0], w.n_x[1]);
       const int cw = warp - kCopyWarp;
+      // its queries into L2, before the row warps get there
+      for (int r = w.r0 + cw * 32 + lane; r < min(w.r0 + 2 * kRows, w.rows); r += kCopyWarps * 32) {
+        const int t = a.by_group.div(r);
+        const T* p = reinterpret_cast<const T*>(a.q) + (int64_t)(w.start + t) * a.q_row +
+                     (int64_t)(kvh * a.group + (r - t * a.group)) * a.q_head;
+#pragma unroll
+        for (int e = 0; e < DIM; e += 64)
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(p + e));
+      }
       constexpr int CB = L::CODED ? 1 : 2, PPT = DIM * CB / 16;    // 16-byte pieces of a token
       constexpr int STEPS = kTok * PPT / 32, TPS = 32 / PPT;       // 32 pieces a step of a warp
       const int piece = lane % PPT, tok0 = lane / PPT;
