@@ -472,7 +472,7 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
       const int64_t row = (int64_t)(sq.start + t);
       if (__any_sync(0xffffffffu, odd) && top > -INFINITY)
         row_again<T, CODE, DIM>(a, b, c, i, kvh,
-                                reinterpret_cast<const T*>(a.q) + row * a.q_row + h * a.q_head,
+                                reinterpret_cast<const T*>(a.q) + row * a.q_row + (int64_t)h * a.q_head,
                                 base + t, lo, hi, top, x);
       const int64_t part_row = a.tokens > 0 ? (int64_t)i * a.tokens + t : row;
       if (lane == 0) row_state(a, sp, row, part_row, h, top, sum);
@@ -485,7 +485,7 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
         }
       } else {
         const float by = saw_nothing(top, sum) ? 0.f : div_rn(1.f, sum);
-        T* p = reinterpret_cast<T*>(a.out) + row * a.o_row + h * a.o_head + lane * EL;
+        T* p = reinterpret_cast<T*>(a.out) + row * a.o_row + (int64_t)h * a.o_head + lane * EL;
 #pragma unroll
         for (int e = 0; e < EL; e += 2)
           *reinterpret_cast<uint32_t*>(p + e) = pack<T>(x[e] * by, x[e + 1] * by);
@@ -564,7 +564,7 @@ k_join(AttendArgs a, BatchArgs b) {
   }
   if (!go) return;
   const float by = saw_nothing(top, sum) ? 0.f : div_rn(1.f, sum);
-  T* p = reinterpret_cast<T*>(a.out) + t * a.o_row + h * a.o_head + lane * EL;
+  T* p = reinterpret_cast<T*>(a.out) + t * a.o_row + (int64_t)h * a.o_head + lane * EL;
 #pragma unroll
   for (int e = 0; e < EL; e += 2)
     *reinterpret_cast<uint32_t*>(p + e) = pack<T>(x[e] * by, x[e + 1] * by);
@@ -745,7 +745,7 @@ extern "C" tre_status tre_chunk_attention(const tre_kv_cache* cache, const tre_k
   if (!(at->scale > 0.f) || !(at->scale < 3e38f)) return TRE_EINVAL;
   const int64_t strides[4] = {at->q_row, at->q_head, at->out_row, at->out_head};
   for (int64_t x : strides)
-    if (x % 8) return TRE_EINVAL;
+    if (x % 8 || x < 0 || x > 2147483647) return TRE_EINVAL;
   if (((uintptr_t)at->q & 15) || ((uintptr_t)at->out & 15)) return TRE_EINVAL;
   a.heads = at->heads;
   a.group = at->heads / cache->heads;
@@ -772,10 +772,10 @@ extern "C" tre_status tre_chunk_attention(const tre_kv_cache* cache, const tre_k
   a.q = static_cast<const uint8_t*>(at->q);
   a.out = static_cast<uint8_t*>(at->out);
   a.lse = at->lse;
-  a.q_row = at->q_row;
-  a.q_head = at->q_head;
-  a.o_row = at->out_row;
-  a.o_head = at->out_head;
+  a.q_row = (int32_t)at->q_row;
+  a.q_head = (int32_t)at->q_head;
+  a.o_row = (int32_t)at->out_row;
+  a.o_head = (int32_t)at->out_head;
   a.scale2 = (float)((double)at->scale * 1.4426950408889634);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const cudaError_t e =

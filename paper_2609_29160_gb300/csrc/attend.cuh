@@ -12,7 +12,7 @@ struct AttendArgs {
   const uint8_t* q;
   uint8_t* out;
   float* lse;                     // [n_rows][heads], may be null
-  int64_t q_row, q_head, o_row, o_head;   // elements
+  int32_t q_row, q_head, o_row, o_head;   // elements
   int32_t heads, group;           // query heads, query heads of one cache head
   FastDiv31 by_group;
   float scale2;                   // scale * log2(e): scores are kept in powers of two
@@ -165,7 +165,7 @@ __device__ void loose_rows(const AttendArgs& a, const BatchArgs& b) {
   for (int64_t r = threadIdx.x; r < (int64_t)loose * a.heads; r += blockDim.x) {
     const int k = (int)(r / a.heads), h = (int)(r - (int64_t)k * a.heads);
     const int64_t t = k < first ? k : last + (k - first);
-    T* o = reinterpret_cast<T*>(a.out) + t * a.o_row + h * a.o_head;
+    T* o = reinterpret_cast<T*>(a.out) + t * a.o_row + (int64_t)h * a.o_head;
     for (int e = 0; e < DIM; ++e) o[e] = T(0.f);
     if (a.lse) a.lse[t * a.heads + h] = -INFINITY;
     if (a.done) a.done[t * a.heads + h] = make_float2(0.f, -1.f);

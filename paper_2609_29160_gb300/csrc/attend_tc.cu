@@ -448,17 +448,16 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
     constexpr int PPR = DIM / 8, RPW = 32 / PPR, QS = 32 / RPW;
     const int q_row0 = (warp & 3) * 32 + lane / PPR, q_piece = lane % PPR;
     auto q_load = [&](const volatile Unit* w, uint4* v) {
-      const int rows = w->rows, r0 = w->r0 + x * kRows, kvh = w->kvh, start = w->start;
+      const int left = w->rows - w->r0 - x * kRows;      // rows of this tile
+      const uint32_t r = w->r0 + x * kRows + q_row0;
+      const T* from = reinterpret_cast<const T*>(a.q) + (int64_t)w->start * a.q_row +
+                      (int64_t)(w->kvh * a.group) * a.q_head + q_piece * 8;
 #pragma unroll
       for (int k = 0; k < QS; ++k) {
-        const int rg = r0 + q_row0 + k * RPW;
+        const int t = a.by_group.div(r + k * RPW), g = r + k * RPW - t * a.group;
+        const T* p = from + ((int64_t)t * a.q_row + (int64_t)g * a.q_head);
         v[k] = make_uint4(0, 0, 0, 0);
-        if (rg < rows) {
-          const int t = a.by_group.div(rg);
-          const T* p = reinterpret_cast<const T*>(a.q) + (int64_t)(start + t) * a.q_row +
-                       (int64_t)(kvh * a.group + (rg - t * a.group)) * a.q_head;
-          v[k] = reinterpret_cast<const uint4*>(p)[q_piece];
-        }
+        if (q_row0 + k * RPW < left) v[k] = *reinterpret_cast<const uint4*>(p);
       }
     };
     auto q_store = [&](uint4* v) {
@@ -680,7 +679,7 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
               q[e] = make_float4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
           } else {
             uint4* q = reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.out) + t_row * a.o_row +
-                                                h_q * a.o_head + 32 * h);
+                                                (int64_t)h_q * a.o_head + 32 * h);
 #pragma unroll
             for (int e = 0; e < 4; ++e) q[e] = Vec<T>::put(y + 8 * e);
           }
@@ -698,14 +697,14 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
         constexpr int EL = DIM / 32;
         float acc[EL];
         row_again<T, CODE, DIM>(a, b, c, i, kvh,
-                                reinterpret_cast<const T*>(a.q) + tr * a.q_row + hq * a.q_head, ps,
+                                reinterpret_cast<const T*>(a.q) + tr * a.q_row + (int64_t)hq * a.q_head, ps,
                                 lo, hi, mm, acc);
 #pragma unroll
         for (int e = 0; e < EL; ++e) {
           if (a.parts > 1)
             a.part_o[(((int64_t)sp * a.part_rows + tr) * a.heads + hq) * DIM + lane * EL + e] = acc[e];
           else
-            (reinterpret_cast<T*>(a.out) + tr * a.o_row + hq * a.o_head)[lane * EL + e] =
+            (reinterpret_cast<T*>(a.out) + tr * a.o_row + (int64_t)hq * a.o_head)[lane * EL + e] =
                 T(acc[e] * bb);
         }
       }
