@@ -497,79 +497,104 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
 
 // Joins the parts of each row, W warps a (row, head), the parts dealt out among them.
 constexpr int kJoinWarps = 8;
+struct JoinSets {
+  AttendArgs of[2];
+};
 template <class T, int DIM, int W>
-__global__ void __launch_bounds__(kJoinWarps * 32)
-k_join(AttendArgs a, BatchArgs b) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int h = blockIdx.y * (kJoinWarps / W) + warp / W, mine = warp % W;
-  int64_t t = blockIdx.x;
-  bool go = h < a.heads;
-  if (a.tokens > 0) {
-    const int i = blockIdx.x / a.tokens, r = blockIdx.x - i * a.tokens;
-    const Seq s = seq_of(b, i);
-    if (r >= s.n || s.n * a.group > a.few) return;
-    t = s.start + r;
-  }
-  const int64_t w = (int64_t)blockIdx.x * a.heads + h, rows_heads = a.part_rows * a.heads;
-  constexpr int EL = DIM / 32;
-  const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
-  float top = -INFINITY, first = 0.f;
-  if (go) {
-    for (int sp = lane; sp < a.parts; sp += 32) {
-      const float2 v = ml[sp * rows_heads + w];
-      if (sp == 0) first = v.y;
-      top = fmaxf(top, v.x);
-    }
-  }
-  go = go && !(__shfl_sync(0xffffffffu, first, 0) < 0.f);       // not this join's
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  float sum = 0.f, x[EL];
-#pragma unroll
-  for (int e = 0; e < EL; ++e) x[e] = 0.f;
-  if (go) {
-#pragma unroll 4
-    for (int sp = mine; sp < a.parts; sp += W) {
-      const int64_t at = sp * rows_heads + w;
-      const float2 v = ml[at];
-      const float f = v.x == -INFINITY ? 0.f : exp2_fast(v.x - top);
-      sum = __fmaf_rn(v.y, f, sum);
-      if (f == 0.f) continue;              // (nothing was left there)
-      const float* p = a.part_o + at * DIM + lane * EL;
-      float y[EL];
-      if constexpr (EL == 4) {
-        const float4 u = *reinterpret_cast<const float4*>(p);
-        y[0] = u.x; y[1] = u.y; y[2] = u.z; y[3] = u.w;
-      } else {
-        const float2 u = *reinterpret_cast<const float2*>(p);
-        y[0] = u.x; y[1] = u.y;
+__device__ __forceinline__ void join_rows(const AttendArgs& a, const BatchArgs& b, int parts) {
+  constexpr int EL = DIM / 32, HEADS = kJoinWarps / W;       // heads of a block's turn
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, mine = warp % W;
+  {
+    const int per_row = (a.heads + HEADS - 1) / HEADS;
+    for (int64_t turn = blockIdx.x; turn < a.part_rows * per_row; turn += gridDim.x) {
+      const int64_t row = turn / per_row;
+      const int h = (int)(turn - row * per_row) * HEADS + warp / W;
+      int64_t t = row;
+      if (a.tokens > 0) {
+        const int i = (int)(row / a.tokens), r = (int)(row - (int64_t)i * a.tokens);
+        const Seq s = seq_of(b, i);
+        if (r >= s.n || s.n * a.group > a.few) continue;
+        t = s.start + r;
       }
+      const int64_t w = row * a.heads + h, all = a.part_rows * a.heads;
+      const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
+      float top = -INFINITY, first = 0.f;
+      bool go = h < a.heads;
+      if (go) {
+        for (int sp = lane; sp < parts; sp += 32) {
+          const float2 v = ml[sp * all + w];
+          if (sp == 0) first = v.y;
+          top = fmaxf(top, v.x);
+        }
+      }
+      go = go && !(__shfl_sync(0xffffffffu, first, 0) < 0.f);         // not this join's
 #pragma unroll
-      for (int e = 0; e < EL; ++e) x[e] = __fmaf_rn(y[e], f, x[e]);
+      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      float sum = 0.f, x[EL];
+#pragma unroll
+      for (int e = 0; e < EL; ++e) x[e] = 0.f;
+      if (go) {
+#pragma unroll 4
+        for (int sp = mine; sp < parts; sp += W) {
+          const int64_t at = sp * all + w;
+          const float2 v = ml[at];
+          const float f = v.x == -INFINITY ? 0.f : exp2_fast(v.x - top);
+          sum = __fmaf_rn(v.y, f, sum);
+          if (f == 0.f) continue;            // (nothing was left there)
+          const float* p = a.part_o + at * DIM + lane * EL;
+          float y[EL];
+          if constexpr (EL == 4) {
+            const float4 u = *reinterpret_cast<const float4*>(p);
+            y[0] = u.x; y[1] = u.y; y[2] = u.z; y[3] = u.w;
+          } else {
+            const float2 u = *reinterpret_cast<const float2*>(p);
+            y[0] = u.x; y[1] = u.y;
+          }
+#pragma unroll
+          for (int e = 0; e < EL; ++e) x[e] = __fmaf_rn(y[e], f, x[e]);
+        }
+      }
+      if constexpr (W > 1) {
+        __shared__ float part[kJoinWarps][DIM + 1];
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < EL; ++e) part[warp][lane * EL + e] = x[e];
+        if (lane == 0) part[warp][DIM] = sum;
+        __syncthreads();
+        go = go && mine == 0;
+        if (go) {
+#pragma unroll
+          for (int y = 1; y < W; ++y) {
+            sum += part[warp + y][DIM];
+#pragma unroll
+            for (int e = 0; e < EL; ++e) x[e] += part[warp + y][lane * EL + e];
+          }
+        }
+      }
+      if (!go) continue;
+      const float by = saw_nothing(top, sum) ? 0.f : div_rn(1.f, sum);
+      T* p = reinterpret_cast<T*>(a.out) + t * a.o_row + (int64_t)h * a.o_head + lane * EL;
+#pragma unroll
+      for (int e = 0; e < EL; e += 2)
+        *reinterpret_cast<uint32_t*>(p + e) = pack<T>(x[e] * by, x[e + 1] * by);
+      if (a.lse && lane == 0)
+        a.lse[t * a.heads + h] = saw_nothing(top, sum) ? -INFINITY : (top + log2f(sum)) * kLn2;
     }
   }
-  if constexpr (W > 1) {
-    __shared__ float part[kJoinWarps][DIM + 1];
-#pragma unroll
-    for (int e = 0; e < EL; ++e) part[warp][lane * EL + e] = x[e];
-    if (lane == 0) part[warp][DIM] = sum;
-    __syncthreads();
-    if (mine != 0) return;
-#pragma unroll
-    for (int k = 1; k < W; ++k) {
-      sum += part[warp + k][DIM];
-#pragma unroll
-      for (int e = 0; e < EL; ++e) x[e] += part[warp + k][lane * EL + e];
-    }
+}
+
+// Both kernels' parts in one launch. From 16 parts on a block's eight warps share a row:
+// a warp alone reads them one after another.
+template <class T, int DIM>
+__global__ void __launch_bounds__(kJoinWarps * 32, 4)
+k_join(const __grid_constant__ JoinSets sets, BatchArgs b) {
+#pragma unroll 1
+  for (int k = 0; k < 2; ++k) {
+    const AttendArgs& a = sets.of[k];
+    const int parts = a.parts_taken ? *a.parts_taken : a.parts;
+    if (parts >= 16) join_rows<T, DIM, kJoinWarps>(a, b, parts);
+    else if (parts > 1) join_rows<T, DIM, 1>(a, b, parts);   // (else rows are written already)
   }
-  if (!go) return;
-  const float by = saw_nothing(top, sum) ? 0.f : div_rn(1.f, sum);
-  T* p = reinterpret_cast<T*>(a.out) + t * a.o_row + (int64_t)h * a.o_head + lane * EL;
-#pragma unroll
-  for (int e = 0; e < EL; e += 2)
-    *reinterpret_cast<uint32_t*>(p + e) = pack<T>(x[e] * by, x[e + 1] * by);
-  if (a.lse && lane == 0)
-    a.lse[t * a.heads + h] = saw_nothing(top, sum) ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
 template <class T, Code CODE, int DIM, int NT>
@@ -604,26 +629,24 @@ cudaError_t launch_code(int code, int dim, int nt, const AttendArgs& a, const Ba
                    : launch_rows<T, Code::kHalf, 128>(nt, a, b, c, s);
 }
 
-// From 16 parts on a block's eight warps share a row: a warp alone reads them one after
-// another.
 template <class T, int DIM>
-cudaError_t launch_join(const AttendArgs& a, const BatchArgs& b, cudaStream_t s) {
-  if (a.part_rows > 2147483647) return cudaErrorInvalidValue;
-  if (a.parts >= 16) {
-    const dim3 grid((unsigned)a.part_rows, a.heads);
-    k_join<T, DIM, kJoinWarps><<<grid, kJoinWarps * 32, 0, s>>>(a, b);
-  } else {
-    const dim3 grid((unsigned)a.part_rows, (a.heads + kJoinWarps - 1) / kJoinWarps);
-    k_join<T, DIM, 1><<<grid, kJoinWarps * 32, 0, s>>>(a, b);
+cudaError_t launch_join(const JoinSets& sets, const BatchArgs& b, cudaStream_t s) {
+  int64_t turns = 0;
+  for (const AttendArgs& a : sets.of) {
+    const int64_t heads = a.parts >= 16 ? 1 : kJoinWarps;
+    if (a.parts > 1) turns = std::max(turns, a.part_rows * ((a.heads + heads - 1) / heads));
   }
+  const unsigned blocks = (unsigned)std::min<int64_t>(turns, (int64_t)device_sm_count() * 64);
+  k_join<T, DIM><<<blocks, kJoinWarps * 32, 0, s>>>(sets, b);
   return cudaGetLastError();
 }
 
-cudaError_t join(int dtype, int dim, const AttendArgs& a, const BatchArgs& b, cudaStream_t s) {
-  if (a.parts < 2) return cudaSuccess;
+cudaError_t join(int dtype, int dim, const JoinSets& sets, const BatchArgs& b, cudaStream_t s) {
+  if (sets.of[0].parts < 2 && sets.of[1].parts < 2) return cudaSuccess;
   if (dtype == TRE_BF16)
-    return dim == 64 ? launch_join<__nv_bfloat16, 64>(a, b, s) : launch_join<__nv_bfloat16, 128>(a, b, s);
-  return dim == 64 ? launch_join<__half, 64>(a, b, s) : launch_join<__half, 128>(a, b, s);
+    return dim == 64 ? launch_join<__nv_bfloat16, 64>(sets, b, s)
+                     : launch_join<__nv_bfloat16, 128>(sets, b, s);
+  return dim == 64 ? launch_join<__half, 64>(sets, b, s) : launch_join<__half, 128>(sets, b, s);
 }
 
 // How a call is split, from what the host knows of it.
@@ -640,7 +663,7 @@ struct Plan {
 // up to four times (from L2) where k_attend_tc would multiply mostly empty rows.
 constexpr int kFew = 64;
 
-Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page) {
+Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page, int dim) {
   Plan p{};
   const int64_t max_new = std::max(1, b->max_new > 0 ? b->max_new : b->n_rows);
   const int64_t rows = max_new * a.group;
@@ -670,34 +693,26 @@ Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page) {
   p.part_rows[1] = b->n_rows;
   p.parts[1] = 1;
   if (p.tc) {
-    // Whole rounds of one block an SM: the number of parts with the least rounds' worth
-    // of context. A part costs what a row's partial sum costs to write and read, about
-    // 400 positions' products, spread over all SMs; none is shorter than 512.
+    // Parts are worth their join where there are fewer units than half the SMs, or two to
+    // six rounds of long ones (then a part evens out the last round). As many as 256 MB of
+    // partial sums allow, none shorter than 512 tokens; how many are taken is seen on the
+    // device, where the lengths are known.
     const int64_t all = (int64_t)b->n_rows * a.group;
-    const int64_t most_tiles = std::min<int64_t>(
-        (int64_t)b->n_seq * ((rows + kTcRows - 1) / kTcRows), all / kTcRows + b->n_seq);
-    // (as many as rows of the longest length make, for the choice of parts)
     const int64_t tiles = std::min<int64_t>(
-        most_tiles, (all + rows - 1) / rows * ((std::min(rows, all) + kTcRows - 1) / kTcRows));
-    const int64_t units = std::max<int64_t>(1, tiles * heads);
-    double least = 0;
-    for (int n = 1; n <= 64 && (n == 1 || len / n >= 512); ++n) {
-      const double rounds = (double)((units * n + sms - 1) / sms);
-      const double cost = rounds / n * len + (n > 1 ? 400.0 * n * units / sms + 2000 : 0);
-      if (n == 1 || cost < least) {
-        least = cost;
-        p.parts[1] = n;
-      }
-    }
+        (int64_t)b->n_seq * ((rows + kTcRows - 1) / kTcRows), all / kTcRows + b->n_seq);
+    const int64_t row = ((int64_t)dim * 4 + 8) * a.heads * std::max(b->n_rows, 1);
+    const int64_t least = std::max<int64_t>(all - (int64_t)b->n_seq * kFew, 1) / kTcRows * heads;
+    if (2 * least <= sms || (least >= 2 * sms && least <= 6 * sms && len >= 8192))
+      p.parts[1] = (int)std::max<int64_t>(1, std::min<int64_t>({64, len / 512, (256ll << 20) / row}));
     p.split[1] = (int)std::max<int64_t>(kTcTokens, (len + p.parts[1] - 1) / p.parts[1]);
-    p.units = std::max<int64_t>(1, most_tiles * heads) * p.parts[1];
+    p.units = std::max<int64_t>(1, tiles * heads) * p.parts[1];
   }
   return p;
 }
 
 cudaError_t launch_all(int dtype, int code, int dim, AttendArgs a, const Plan& p,
-                       float* const* part_o, float* const* part_ml, const BatchArgs& b,
-                       const CacheArgs& c, tre_diag* diag, cudaStream_t s) {
+                       float* const* part_o, float* const* part_ml, int32_t* parts_taken,
+                       const BatchArgs& b, const CacheArgs& c, tre_diag* diag, cudaStream_t s) {
   const bool bf = dtype == TRE_BF16;
   a.few = p.few;
   auto of = [&](int k) {
@@ -710,8 +725,11 @@ cudaError_t launch_all(int dtype, int code, int dim, AttendArgs a, const Plan& p
     return x;
   };
   cudaError_t e = cudaSuccess;
+  AttendArgs y = of(1);
+  y.parts_taken = parts_taken;
+  y.sms = device_sm_count();
   if (p.tc) {
-    e = launch_attend_tc(dtype, code, dim, of(1), b, c, p.units, diag, s);
+    e = launch_attend_tc(dtype, code, dim, y, b, c, p.units, diag, s);
     if (e) return e;
   }
   AttendArgs x = of(0);
@@ -720,8 +738,7 @@ cudaError_t launch_all(int dtype, int code, int dim, AttendArgs a, const Plan& p
   if (p.parts[1] > 1) x.done = reinterpret_cast<float2*>(part_ml[1]);
   e = bf ? launch_code<__nv_bfloat16>(code, dim, p.nt, x, b, c, s)
          : launch_code<__half>(code, dim, p.nt, x, b, c, s);
-  if (!e) e = join(dtype, dim, x, b, s);
-  if (!e && p.tc) e = join(dtype, dim, of(1), b, s);
+  if (!e) e = join(dtype, dim, JoinSets{{x, y}}, b, s);
   return e;
 }
 
@@ -753,9 +770,10 @@ extern "C" tre_status tre_chunk_attention(const tre_kv_cache* cache, const tre_k
   a.by_group = FastDiv31((uint32_t)a.group);
   a.window = at->window;
   Plan plan{};
-  if (b.n_seq > 0) plan = plan_of(batch, a, c.heads, c.page);
+  if (b.n_seq > 0) plan = plan_of(batch, a, c.heads, c.page, cache->dim);
   Arena arena(ws);
   float *part_o[2] = {}, *part_ml[2] = {};
+  int32_t* parts_taken = plan.parts[1] > 1 ? arena.take<int32_t>(1) : nullptr;
   for (int k = 0; k < 2; ++k) {
     if (plan.parts[k] < 2) continue;
     const size_t rh = (size_t)plan.part_rows[k] * a.heads * plan.parts[k];
@@ -779,6 +797,7 @@ extern "C" tre_status tre_chunk_attention(const tre_kv_cache* cache, const tre_k
   a.scale2 = (float)((double)at->scale * 1.4426950408889634);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const cudaError_t e =
-      launch_all(at->dtype, cache->dtype, cache->dim, a, plan, part_o, part_ml, b, c, diag, s);
+      launch_all(at->dtype, cache->dtype, cache->dim, a, plan, part_o, part_ml, parts_taken, b, c,
+                 diag, s);
   return e == cudaSuccess ? TRE_OK : TRE_ECUDA;
 }

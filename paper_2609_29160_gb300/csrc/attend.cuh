@@ -27,6 +27,10 @@ struct AttendArgs {
   int64_t part_rows;
   int32_t tokens;
   float2* done;                   // the other kernel's part_ml: rows that are not its
+  // k_attend_tc: `parts` is the most there is room for; how many it takes is seen on the
+  // device, where the rows of each sequence are known, and left here for the join
+  int32_t* parts_taken;
+  int32_t sms;
 };
 
 __device__ __forceinline__ float exp2_fast(float x) {

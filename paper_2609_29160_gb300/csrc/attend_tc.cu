@@ -295,6 +295,51 @@ template <Code CODE, int DIM> struct Tc {
   static constexpr int SMEM = AT_UNIT + kUnits * 64;
 };
 
+// Row tiles of sequence i, none where it is k_attend's.
+__device__ __forceinline__ int tiles_of(const AttendArgs& a, const BatchArgs& b, int i) {
+  if (i >= b.n_seq) return 0;
+  const int r = seq_of(b, i).n * a.group;
+  return r > a.few ? (r + 2 * kRows - 1) / (2 * kRows) : 0;
+}
+
+// Parts of a context: whole rounds of one unit an SM, so the number of parts with the
+// least time, in positions: a round takes its part of the longest context and about 900
+// more (a unit's start and end); a split costs what a row's partial sums cost to write
+// and read, about 400 a part, spread over all SMs, and some 1,500 for the join. The whole
+// warp looks.
+__device__ __forceinline__ int choose_parts(AttendArgs& a, const BatchArgs& b, int heads) {
+  const int lane = threadIdx.x & 31;
+  int units = 0, len = 1;
+  for (int from = 0; from < b.n_seq; from += 32) {
+    const int tiles = tiles_of(a, b, from + lane);
+    units += tiles;
+    if (tiles > 0) {
+      const Seq s = seq_of(b, from + lane);
+      const int64_t seen = a.window > 0 ? (int64_t)a.window + s.n + kTok : s.ctx;
+      len = max(len, (int)min64(s.ctx, seen));
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    units += __shfl_xor_sync(0xffffffffu, units, o);
+    len = max(len, __shfl_xor_sync(0xffffffffu, len, o));
+  }
+  units *= heads;
+  float least = 0.f;
+  int parts = 1;
+  for (int n = 1; n <= a.parts && (n == 1 || len / n >= 512); ++n) {
+    const float rounds = (float)((units * n + a.sms - 1) / a.sms);
+    const float cost = rounds * ((float)len / n + 900.f) +
+                       (n > 1 ? 400.f * n * units / a.sms + 1500.f : 0.f);
+    if (n == 1 || cost < least) {
+      least = cost;
+      parts = n;
+    }
+  }
+  a.split = max(kTok, (len + parts - 1) / parts);
+  return parts;
+}
+
 // A block's piece of work: up to 256 rows of a sequence against one part of its context
 // for one cache head. Units go through the sequences' row tiles (of those that are not
 // k_attend's), each sequence's longest ranges first, heads fastest: heads of a tile read
@@ -316,11 +361,7 @@ struct alignas(64) Unit {
     i = -1;
     int tiles = 0, rt = 0;
     for (int from = 0; from < b.n_seq; from += 32) {
-      int mine = 0;
-      if (from + lane < b.n_seq) {
-        const int r = seq_of(b, from + lane).n * a.group;
-        mine = r > a.few ? (r + 2 * kRows - 1) / (2 * kRows) : 0;
-      }
+      const int mine = tiles_of(a, b, from + lane);
       int upto = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -376,6 +417,10 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
   extern __shared__ __align__(1024) uint8_t sm[];
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+  if (a.parts > 1) {
+    a.parts = choose_parts(a, b, c.heads);
+    if (blockIdx.x == 0 && tid == 0) *a.parts_taken = a.parts;
+  }
   {
     Unit w;
     if (!w.find(a, b, c, blockIdx.x)) return;
@@ -675,8 +720,11 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
           if (a.parts > 1) {
             float4* q = reinterpret_cast<float4*>(a.part_o + at * DIM + 32 * h);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              q[e] = make_float4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
+            for (int e = 0; e < 8; e += 2)     // 32 bytes at a time: whole sectors
+              asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(q + e),
+                           "f"(y[4 * e]), "f"(y[4 * e + 1]), "f"(y[4 * e + 2]), "f"(y[4 * e + 3]),
+                           "f"(y[4 * e + 4]), "f"(y[4 * e + 5]), "f"(y[4 * e + 6]), "f"(y[4 * e + 7])
+                           : "memory");
           } else {
             uint4* q = reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.out) + t_row * a.o_row +
                                                 (int64_t)h_q * a.o_head + 32 * h);
