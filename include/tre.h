@@ -595,7 +595,7 @@ tre_status tre_kv_read(const tre_kv_cache* cache, const tre_kv_batch* batch, tre
 /* Queries of tre_chunk_attention: [n_rows][heads][dim] of dtype (TRE_BF16 or
  * TRE_F16; the cache is of the same type or of codes), heads a multiple of the
  * cache's: query head h reads cache head h / (heads / cache heads). Strides in
- * elements, multiples of 8; addresses multiples of 16 bytes. scale > 0. window:
+ * elements, multiples of 8 from 0 to 2^31 - 1; addresses multiples of 16 bytes. scale > 0. window:
  * a row sees its last `window` positions only (0: all). lse: NULL, or float
  * [n_rows][heads], the logarithm of each row's sum of exp(scale * q.k). */
 typedef struct {

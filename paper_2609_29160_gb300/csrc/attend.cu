@@ -788,6 +788,10 @@ extern "C" tre_status tre_chunk_attention(const tre_kv_cache* cache, const tre_k
   if (b.n_rows == 0) return TRE_OK;
   if (b.n_seq == 0 || !at->q || !at->out) return TRE_EINVAL;
   a.q = static_cast<const uint8_t*>(at->q);
+  if (c.n_pages == 0) {                  // nothing will be read, but copies name an address
+    c.k = c.v = const_cast<uint8_t*>(a.q);
+    c.k_scale = c.v_scale = reinterpret_cast<float*>(c.k);
+  }
   a.out = static_cast<uint8_t*>(at->out);
   a.lse = at->lse;
   a.q_row = (int32_t)at->q_row;

@@ -242,3 +242,61 @@ def test_no_rows():
     bt = ref.Batch([(30, 0)], 16, 2, 64, torch.bfloat16)
     q = torch.zeros(0, 4, 64, dtype=torch.bfloat16, device="cuda")
     assert tre.tre_chunk_attention(q, bt.cache(tre), bt.batch(tre)).shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("pool", ["bf16", "i8"])
+@pytest.mark.parametrize("new", [1, 100])
+def test_a_cache_of_no_pages(pool, new):
+    dt = ref.T[pool]
+    k = torch.zeros(0, 16, 2, 64, dtype=dt, device="cuda")
+    sc = torch.zeros(0, 16, 2, device="cuda") if dt in ref.TOP else None
+    c = tre.KvCache(k, k, sc, sc)
+    b = tre.KvBatch(torch.zeros(1, 7, dtype=torch.int32, device="cuda"),
+                    torch.tensor([new], dtype=torch.int32, device="cuda"),
+                    torch.tensor([0, new], dtype=torch.int32, device="cuda"), new)
+    out, lse = tre.tre_chunk_attention(torch.ones(new, 4, 64, device="cuda").bfloat16(), c, b, lse=True)
+    assert (out == 0).all() and (lse == -math.inf).all()
+
+
+@pytest.mark.parametrize("pool", ["bf16", "e4m3"])
+@pytest.mark.parametrize("lens", [[(2500, 1), (40, 1)], [(300, 200), (20, 1)]])
+def test_in_a_graph(pool, lens):
+    """Captured once, replayed over other contents of the same tensors."""
+    bt = ref.Batch(lens, 16, 2, 64, ref.T[pool], seed=21)
+    q = torch.randn(bt.rows, 8, 64, device="cuda").bfloat16()
+    k = torch.randn(bt.rows, 2, 64, device="cuda").bfloat16()
+    c, b = bt.cache(tre), bt.batch(tre)
+
+    def step():
+        tre.tre_kv_append(c, b, k, k)
+        return tre.tre_chunk_attention(q, c, b)
+
+    step()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = step()
+    q.copy_(torch.randn_like(q))
+    k.copy_(torch.randn_like(k))
+    bt.ctx.copy_(bt.ctx - 7)
+    g.replay()
+    torch.cuda.synchronize()
+    got = out.clone()
+    assert torch.equal(got, step())
+
+
+@pytest.mark.parametrize("groups,lens", [(1, [(5, 600), (0, 65), (0, 64), (3000, 70)]),
+                                         (8, [(0, 9), (0, 8), (100, 7), (4000, 33)]),
+                                         (5, [(0, 13), (77, 12), (2000, 400)])])
+@pytest.mark.parametrize("pool", ["f16", "e4m3", "i8"])
+def test_few_and_many_rows_side_by_side(groups, lens, pool):
+    """Sequences on both sides of the line between the two kernels, parts on either."""
+    bt = ref.Batch(lens, 32, 2, 128, ref.T[pool], seed=22, drop=0.05)
+    check(bt, 2 * groups, "f16")
+    check(bt, 2 * groups, "f16", window=90)
+
+
+def test_many_sequences():
+    """More sequences than a warp looks at in a step, most of them of no rows."""
+    lens = [((7 * i) % 300, (i * i) % 5 if i % 9 else 40 + i % 100) for i in range(150)]
+    bt = ref.Batch(lens, 16, 1, 64, torch.bfloat16, seed=23)
+    check(bt, 4)
