@@ -83,8 +83,8 @@ __device__ __forceinline__ uint32_t turned(uint32_t x) {
 }
 
 template <class T, Code CODE, int DIM, int NT>
-__global__ void __launch_bounds__(kWarps * 32, Shape<CODE, DIM, NT>::BLOCKS_AN_SM)
-k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
+__device__ __forceinline__ void attend_block(const AttendArgs& a, const BatchArgs& b,
+                                             const CacheArgs& c) {
   using S = Shape<CODE, DIM, NT>;
   using CT = typename std::conditional<CODE == Code::kHalf, T, __half>::type;
   constexpr int EPT = 16 / S::CB, SPB = EPT / 4, BLOCKS = DIM / (4 * EPT);
@@ -495,6 +495,18 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
   }
 }
 
+// Beside k_attend_tc: this launch does not wait for that one, so that its blocks run on
+// SMs that are left over. Neither reads what the other writes (rows of different
+// sequences, and the marks of those in the other's part_ml); the last block stays until
+// the other launch is done, so that what comes next in the stream waits for both.
+template <class T, Code CODE, int DIM, int NT>
+__global__ void __launch_bounds__(kWarps * 32, Shape<CODE, DIM, NT>::BLOCKS_AN_SM)
+k_attend(const __grid_constant__ AttendArgs a, const __grid_constant__ BatchArgs b,
+         const __grid_constant__ CacheArgs c) {
+  attend_block<T, CODE, DIM, NT>(a, b, c);
+  if (a.beside && blockIdx.x == gridDim.x - 1) asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // Joins the parts of each row, W warps a (row, head), the parts dealt out among them.
 constexpr int kJoinWarps = 8;
 struct JoinSets {
@@ -606,8 +618,17 @@ cudaError_t launch_typed(const AttendArgs& a, const BatchArgs& b, const CacheArg
   if (e) return e;
   const int64_t blocks = (int64_t)c.heads * a.parts * a.row_tiles * b.n_seq;
   if (blocks > 2147483647) return cudaErrorInvalidValue;
-  k_attend<T, CODE, DIM, NT><<<(unsigned)blocks, kWarps * 32, S::SMEM, s>>>(a, b, c);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3(kWarps * 32);
+  cfg.dynamicSmemBytes = S::SMEM;
+  cfg.stream = s;
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = a.beside ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, k_attend<T, CODE, DIM, NT>, a, b, c);
 }
 
 template <class T, Code CODE, int DIM>
@@ -735,6 +756,7 @@ cudaError_t launch_all(int dtype, int code, int dim, AttendArgs a, const Plan& p
   AttendArgs x = of(0);
   x.row_tiles = p.row_tiles;
   x.tokens = p.tokens;
+  x.beside = p.tc;
   if (p.parts[1] > 1) x.done = reinterpret_cast<float2*>(part_ml[1]);
   e = bf ? launch_code<__nv_bfloat16>(code, dim, p.nt, x, b, c, s)
          : launch_code<__half>(code, dim, p.nt, x, b, c, s);

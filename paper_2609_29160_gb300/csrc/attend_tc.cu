@@ -416,6 +416,7 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
   using CT = typename std::conditional<L::CODED, __half, T>::type;
   extern __shared__ __align__(1024) uint8_t sm[];
   const int tid = threadIdx.x, lane = tid & 31;
+  asm volatile("griddepcontrol.launch_dependents;");      // k_attend may run beside
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   if (a.parts > 1) {
     a.parts = choose_parts(a, b, c.heads);
