@@ -501,8 +501,7 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const BatchArg
 // the other launch is done, so that what comes next in the stream waits for both.
 template <class T, Code CODE, int DIM, int NT>
 __global__ void __launch_bounds__(kWarps * 32, Shape<CODE, DIM, NT>::BLOCKS_AN_SM)
-k_attend(const __grid_constant__ AttendArgs a, const __grid_constant__ BatchArgs b,
-         const __grid_constant__ CacheArgs c) {
+k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
   attend_block<T, CODE, DIM, NT>(a, b, c);
   if (a.beside && blockIdx.x == gridDim.x - 1) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
