@@ -290,7 +290,7 @@ template <Code CODE, int DIM> struct Tc {
   static constexpr int AT_SCALE = AT_MASK + META * 16;  // float [META][3][kTok]
   static constexpr int AT_BACK = AT_SCALE + (CODED ? META * 3 * kTok * 4 : 0);  // float [2][kRows]
   static constexpr int AT_BAR = AT_BACK + (CODED ? 2 * kRows * 4 : 0);
-  static constexpr int BARS = 2 * RING + 2 * RAWS + META + 8 + 2 * kUnits;
+  static constexpr int BARS = 2 * RING + 2 * RAWS + META + 10 + 2 * kUnits;
   static constexpr int AT_UNIT = (AT_BAR + BARS * 8 + 16 + 63) / 64 * 64;    // Unit [kUnits]
   static constexpr int SMEM = AT_UNIT + kUnits * 64;
 };
@@ -429,7 +429,7 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
 
   uint64_t* bars = reinterpret_cast<uint64_t*>(sm + L::AT_BAR);
   uint64_t *full = bars, *empty = bars + L::RING, *meta = empty + L::RING, *s_full = meta + L::META,
-           *p_full = s_full + 2, *o_done = p_full + 2, *q_full = o_done + 2,
+           *p_full = s_full + 2, *o_done = p_full + 4, *q_full = o_done + 2,
            *u_full = q_full + 2, *u_empty = u_full + kUnits, *raw_full = u_empty + kUnits,
            *raw_empty = raw_full + L::RAWS;
   uint32_t* tmem_at = reinterpret_cast<uint32_t*>(bars + L::BARS);
@@ -454,7 +454,8 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
     for (int k = 0; k < L::META; ++k) bar_init(meta + k, 4);
     for (int x = 0; x < 2; ++x) {
       bar_init(s_full + x, 1);
-      bar_init(p_full + x, kRowWarps / 2);
+      bar_init(p_full + 2 * x, kRowWarps / 2);
+      bar_init(p_full + 2 * x + 1, kRowWarps / 2);
       bar_init(o_done + x, 1);
       bar_init(q_full + x, kRowWarps / 2);
     }
@@ -570,56 +571,65 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
         }
         tmem_after();
         uint32_t v[kTok];
-#pragma unroll
-        for (int h = 0; h < 4; ++h) tmem_ld32(s_at + 32 * h, v + 32 * h);
+        tmem_ld32(s_at, v);
+        tmem_ld32(s_at + 32, v + 32);
         const int j0 = lo + k * kTok;
         const uint4 held = *reinterpret_cast<const uint4*>(mask_s + ms * 4);
         const bool whole = (held.x & held.y & held.z & held.w) == 0xffffffffu &&
                            j0 + kTok - 1 <= first && (a.window == 0 || j0 > last - a.window);
         const float* meta_s = scale_s + ms * 3 * kTok;
-#pragma unroll
-        for (int h = 0; h < 4; ++h) tmem_wait_ld(v + 32 * h);
-        if constexpr (L::CODED) {
-#pragma unroll
-          for (int e = 0; e < kTok; e += 4) {
-            const float4 f = *reinterpret_cast<const float4*>(meta_s + e);
-            mul2(v + e, f.x, f.y);
-            mul2(v + e + 2, f.z, f.w);
-          }
-        }
-        if (!whole) {
-          const uint32_t hw[4] = {held.x, held.y, held.z, held.w};
-#pragma unroll
-          for (int h = 0; h < 4; ++h) {
-            const int to = min(max(pos - j0 - 32 * h + 1, 0), 32);
-            const int from = a.window ? min(max(pos - a.window + 1 - j0 - 32 * h, 0), 32) : 0;
-            const uint32_t see = hw[h] & (to == 32 ? 0xffffffffu : (1u << to) - 1) &
-                                 (from == 32 ? 0u : 0xffffffffu << from);
-#pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (!(see >> e & 1)) v[32 * h + e] = 0xff800000u;
-          }
-        }
         float t0 = -INFINITY, t1 = -INFINITY, t2 = -INFINITY, t3 = -INFINITY;
+        // half of the scores at a time, the other on its way
 #pragma unroll
-        for (int e = 0; e < kTok; e += 8) {
+        for (int hf = 0; hf < 2; ++hf) {
+          tmem_wait_ld(v + 64 * hf);
+          tmem_wait_ld(v + 64 * hf + 32);
+          if (hf == 0) {
+            tmem_ld32(s_at + 64, v + 64);
+            tmem_ld32(s_at + 96, v + 96);
+          }
           if constexpr (L::CODED) {
-            // a value's scale counts in its weight: the largest weight is below one by
-            // the scale's power of two
 #pragma unroll
-            for (int y = 0; y < 8; y += 4) {
-              const float4 f = *reinterpret_cast<const float4*>(meta_s + 2 * kTok + e + y);
-              uint32_t z[4] = {v[e + y], v[e + y + 1], v[e + y + 2], v[e + y + 3]};
-              fma2(z, back, f.x, f.y);
-              fma2(z + 2, back, f.z, f.w);
-              t0 = max3(t0, __uint_as_float(z[0]), __uint_as_float(z[1]));
-              t1 = max3(t1, __uint_as_float(z[2]), __uint_as_float(z[3]));
+            for (int e = 64 * hf; e < 64 * hf + 64; e += 4) {
+              const float4 f = *reinterpret_cast<const float4*>(meta_s + e);
+              mul2(v + e, f.x, f.y);
+              mul2(v + e + 2, f.z, f.w);
             }
-          } else {
-            t0 = max3(t0, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
-            t1 = max3(t1, __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3]));
-            t2 = max3(t2, __uint_as_float(v[e + 4]), __uint_as_float(v[e + 5]));
-            t3 = max3(t3, __uint_as_float(v[e + 6]), __uint_as_float(v[e + 7]));
+          }
+          if (!whole) {
+            const uint32_t hw[2] = {hf ? held.z : held.x, hf ? held.w : held.y};
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              const int c0 = 64 * hf + 32 * y;
+              const int to = min(max(pos - j0 - c0 + 1, 0), 32);
+              const int from = a.window ? min(max(pos - a.window + 1 - j0 - c0, 0), 32) : 0;
+              const uint32_t see = hw[y] & (to == 32 ? 0xffffffffu : (1u << to) - 1) &
+                                   (from == 32 ? 0u : 0xffffffffu << from);
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (!(see >> e & 1)) v[c0 + e] = 0xff800000u;
+            }
+          }
+#pragma unroll
+          for (int e = 64 * hf; e < 64 * hf + 64; e += 8) {
+            if constexpr (L::CODED) {
+              // a value's scale counts in its weight: the largest weight is below one by
+              // the scale's power of two
+#pragma unroll
+              for (int y = 0; y < 8; y += 4) {
+                const float4 f = *reinterpret_cast<const float4*>(meta_s + 2 * kTok + e + y);
+                uint32_t z[4] = {v[e + y], v[e + y + 1], v[e + y + 2], v[e + y + 3]};
+                fma2(z, back, f.x, f.y);
+                fma2(z + 2, back, f.z, f.w);
+                t0 = max3(t0, __uint_as_float(z[0]), __uint_as_float(z[1]));
+                t1 = max3(t1, __uint_as_float(z[2]), __uint_as_float(z[3]));
+              }
+            } else {
+              t0 = max3(t0, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
+              t1 = max3(t1, __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3]));
+              t2 = max3(t2, __uint_as_float(v[e + 4]), __uint_as_float(v[e + 5]));
+              t3 = max3(t3, __uint_as_float(v[e + 6]), __uint_as_float(v[e + 7]));
+            }
           }
         }
         float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3));
@@ -670,11 +680,13 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
             p[(e - 32 * h) / 2 + 1] = pack<CT>(y[2], y[3]);
           }
           tmem_st16(s_at + 16 * h, p);
+          if (h & 1) {                           // half of the products may begin
+            tmem_wait_st();
+            tmem_before();
+            bar_arrive_warp(p_full + 2 * x + (h >> 1));
+          }
         }
         l += halves_sum(l0, l1);
-        tmem_wait_st();
-        tmem_before();
-        bar_arrive_warp(p_full + x);
       }
       // the next unit's queries are on their way while the last products run, and its
       // first products run while this one's rows are written
@@ -1057,15 +1069,18 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             if (k < n_x[x]) {
-              alive = alive && bar_wait(p_full + x, (n_own[x] + k) & 1, dead);
-              tmem_after();
-              if (alive && one_lane()) {
-                const uint32_t va = v_op + vb * (L::BUF >> 4), d = tmem + 256 + x * 128;
-                const uint32_t pa = tmem + x * kTok;
+              const uint32_t va = v_op + vb * (L::BUF >> 4), d = tmem + 256 + x * 128;
+              const uint32_t pa = tmem + x * kTok;
 #pragma unroll
-                for (int s = 0; s < kTok / 16; ++s)
-                  mma_ts(d, pa + s * 8, va + s * (2048 >> 4), id_o, k > 0 || s > 0);
-                if (k == n_x[x] - 1) commit(o_done + x);
+              for (int hf = 0; hf < 2; ++hf) {
+                alive = alive && bar_wait(p_full + 2 * x + hf, (n_own[x] + k) & 1, dead);
+                tmem_after();
+                if (alive && one_lane()) {
+#pragma unroll
+                  for (int s = 4 * hf; s < 4 * hf + 4; ++s)
+                    mma_ts(d, pa + s * 8, va + s * (2048 >> 4), id_o, k > 0 || s > 0);
+                  if (hf && k == n_x[x] - 1) commit(o_done + x);
+                }
               }
             }
             if (k + 1 < n_x[x]) {
