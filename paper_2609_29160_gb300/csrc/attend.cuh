@@ -115,7 +115,7 @@ __device__ __forceinline__ void cached(const uint8_t* base, int64_t off, int lan
       unpack(reinterpret_cast<const uint16_t*>(base)[at], x[e], hi, T());
     } else {
       float y[4];
-      codes4(base[at], y, CODE == Code::kI8);
+      codes4<CODE>(base[at], y);
       x[e] = y[0];
     }
   }

@@ -292,6 +292,7 @@ k_heads(HeadsArgs a, BatchArgs b, CacheArgs c, int groups, int its, tre_diag* di
 struct ReadOut {
   uint8_t *k, *v;
   int64_t row, head;             // elements
+  bool wide;                     // on 32-byte boundaries
 };
 
 // One warp takes one token's keys and values, 16 bytes of the cache a lane, the
@@ -344,15 +345,26 @@ k_read(BatchArgs b, CacheArgs c, ReadOut o, tre_diag* diag) {
       } else {
         const uint32_t q[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) codes4(q[j], x + 4 * j, CODE == Code::kI8);
+        for (int j = 0; j < 4; ++j) codes4<CODE>(q[j], x + 4 * j);
         if (page >= 0) {
 #pragma unroll
           for (int e = 0; e < N; ++e) x[e] = mul_rn(x[e], sc[u]);
         }
       }
       OUT* dst = reinterpret_cast<OUT*>(val ? o.v : o.k) + t * o.row + h * o.head + e0;
+      if (o.wide && N > OV) {
+        // 32 bytes a store: whole sectors
 #pragma unroll
-      for (int e = 0; e < N; e += OV) *reinterpret_cast<uint4*>(dst + e) = Vec<OUT>::put(x + e);
+        for (int e = 0; e + OV < N; e += 2 * OV) {
+          const uint4 y = Vec<OUT>::put(x + e), z = Vec<OUT>::put(x + e + OV);
+          asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + e),
+                       "r"(y.x), "r"(y.y), "r"(y.z), "r"(y.w), "r"(z.x), "r"(z.y), "r"(z.z), "r"(z.w)
+                       : "memory");
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; e += OV) *reinterpret_cast<uint4*>(dst + e) = Vec<OUT>::put(x + e);
+      }
     }
   }
 }
@@ -586,7 +598,9 @@ tre_status tre_kv_read(const tre_kv_cache* cache, const tre_kv_batch* batch, tre
   if (!k_out || !v_out || !at16(k_out) || !at16(v_out) || !mult16(out_row, el) ||
       !mult16(out_head, el))
     return TRE_EINVAL;
-  ReadOut o{static_cast<uint8_t*>(k_out), static_cast<uint8_t*>(v_out), out_row, out_head};
+  const bool wide = !((reinterpret_cast<uintptr_t>(k_out) | reinterpret_cast<uintptr_t>(v_out)) & 31) &&
+                    out_row * el % 32 == 0 && out_head * el % 32 == 0;
+  ReadOut o{static_cast<uint8_t*>(k_out), static_cast<uint8_t*>(v_out), out_row, out_head, wide};
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e;
   if (out_dtype == TRE_F32) e = read_by_code<float>(cache->dtype, cache->dim, b, c, o, diag, s);

@@ -59,23 +59,6 @@ template <> struct Vec<float> {
   }
 };
 
-// four 8-bit codes as floats
-__device__ __forceinline__ void codes4(uint32_t v, float* x, bool i8) {
-  if (i8) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = (float)(int8_t)(v >> (8 * e));
-  } else {
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const __half2_raw h =
-          __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(v >> (16 * e)), __NV_E4M3);
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-      x[2 * e] = f.x;
-      x[2 * e + 1] = f.y;
-    }
-  }
-}
-
 // Two 8-bit codes (the low 16 bits of w) as a pair of halves, which hold both kinds exactly.
 template <Code CODE> __device__ __forceinline__ uint32_t halves(uint32_t w) {
   if constexpr (CODE == Code::kE4m3) {
@@ -87,6 +70,12 @@ template <Code CODE> __device__ __forceinline__ uint32_t halves(uint32_t w) {
     const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&u), __half2half2(__ushort_as_half(0x6480)));
     return *reinterpret_cast<const uint32_t*>(&v);
   }
+}
+
+// four 8-bit codes as floats
+template <Code CODE> __device__ __forceinline__ void codes4(uint32_t v, float* x) {
+  unpack(halves<CODE>(v), x[0], x[1], __half());
+  unpack(halves<CODE>(v >> 16), x[2], x[3], __half());
 }
 
 // A paged cache as the kernels see it (strides in elements).
