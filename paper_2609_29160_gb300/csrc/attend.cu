@@ -819,6 +819,7 @@ extern "C" tre_status tre_chunk_attention(const tre_kv_cache* cache, const tre_k
   a.q_head = (int32_t)at->q_head;
   a.o_row = (int32_t)at->out_row;
   a.o_head = (int32_t)at->out_head;
+  a.wide = ((uintptr_t)at->out & 31) == 0 && at->out_row % 16 == 0 && at->out_head % 16 == 0;
   a.scale2 = (float)((double)at->scale * 1.4426950408889634);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const cudaError_t e =

@@ -31,6 +31,7 @@ struct AttendArgs {
   // device, where the rows of each sequence are known, and left here for the join
   int32_t* parts_taken;
   int32_t sms;
+  bool wide;                      // outputs on 32-byte boundaries
   bool beside;                    // k_attend: launched beside k_attend_tc
 };
 

@@ -741,8 +741,19 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
           } else {
             uint4* q = reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.out) + t_row * a.o_row +
                                                 (int64_t)h_q * a.o_head + 32 * h);
+            if (a.wide) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) q[e] = Vec<T>::put(y + 8 * e);
+              for (int e = 0; e < 4; e += 2) {
+                const uint4 f = Vec<T>::put(y + 8 * e), g = Vec<T>::put(y + 8 * e + 8);
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(q + e),
+                             "r"(f.x), "r"(f.y), "r"(f.z), "r"(f.w), "r"(g.x), "r"(g.y), "r"(g.z),
+                             "r"(g.w)
+                             : "memory");
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) q[e] = Vec<T>::put(y + 8 * e);
+            }
           }
         }
       }
