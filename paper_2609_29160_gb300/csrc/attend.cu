@@ -679,9 +679,15 @@ struct Plan {
   int64_t units;                  // of k_attend_tc, at most
 };
 
-// Up to 64 rows of a sequence go to k_attend, whose 16-row tiles then read each key
-// up to four times (from L2) where k_attend_tc would multiply mostly empty rows.
-constexpr int kFew = 64;
+// Which kernel takes a sequence, by its rows. k_attend reads keys and values once for 8 or
+// 16 rows (again from L2 for the next), k_attend_tc takes 128 rows in the time of one:
+// 32 sequences of 1,500 to 4,000 tokens, dim 128, took 72, 82 and 124 us with up to 16, 32
+// and 64 rows each in k_attend and 102 to 105 in k_attend_tc; 4 of 25,000 over e4m3 68, 72
+// and 112 against 185. So batches of up to 64 rows a sequence are k_attend's alone. Where
+// k_attend_tc runs in any case, sequences of more than 16 rows are its (at up to 64 in
+// k_attend chunks of up to 128 rows took 250 us, all of them in k_attend_tc 107), except
+// one new token's heads.
+constexpr int kFew = 64, kFewBeside = 16;
 
 Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page, int dim) {
   Plan p{};
@@ -692,7 +698,7 @@ Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page, in
   len = std::max<int64_t>(len, 1);
   const int64_t sms = device_sm_count();
   p.tc = rows > kFew;
-  p.few = p.tc ? kFew : 2147483647;
+  p.few = !p.tc ? 2147483647 : a.group <= kFew ? std::max(kFewBeside, a.group) : kFewBeside;
   {
     // Parts of a context: about 16 blocks an SM, so that sequences of unequal length
     // even out (8 blocks an SM took 3 to 14% longer on ragged batches, 48 up to 9%), of
@@ -708,7 +714,7 @@ Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page, in
     p.parts[0] = (int)std::max<int64_t>(1, std::min<int64_t>({want, most, 256}));
     p.split[0] = (int)std::max<int64_t>(kTile * kWarps, (len + p.parts[0] - 1) / p.parts[0]);
   }
-  p.tokens = p.tc ? std::max(1, kFew / a.group) : 0;
+  p.tokens = p.tc ? std::max(1, p.few / a.group) : 0;
   p.part_rows[0] = p.tc ? (int64_t)b->n_seq * p.tokens : b->n_rows;
   p.part_rows[1] = b->n_rows;
   p.parts[1] = 1;
@@ -721,7 +727,7 @@ Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page, in
     const int64_t tiles = std::min<int64_t>(
         (int64_t)b->n_seq * ((rows + kTcRows - 1) / kTcRows), all / kTcRows + b->n_seq);
     const int64_t row = ((int64_t)dim * 4 + 8) * a.heads * std::max(b->n_rows, 1);
-    const int64_t least = std::max<int64_t>(all - (int64_t)b->n_seq * kFew, 1) / kTcRows * heads;
+    const int64_t least = std::max<int64_t>(all - (int64_t)b->n_seq * p.few, 1) / kTcRows * heads;
     if (2 * least <= sms || (least >= 2 * sms && least <= 6 * sms && len >= 8192))
       p.parts[1] = (int)std::max<int64_t>(1, std::min<int64_t>({64, len / 512, (256ll << 20) / row}));
     p.split[1] = (int)std::max<int64_t>(kTcTokens, (len + p.parts[1] - 1) / p.parts[1]);
