@@ -15,6 +15,10 @@
 // eight rows, the query heads of one token, fill a tile that way, and a lane holds two
 // rows' weights of two positions. Elements of a key and columns of values are taken in
 // the order in which a lane's 16-byte reads deliver them, which a sum does not see.
+//
+// Bound by HBM on 16-bit caches: one token of 96 requests of up to 16,000, 32 query heads
+// on 8 of 128, 297 us, 6.4 TB/s. On codes the widening takes half of the issue slots as
+// well: 8 requests of up to 120,000, 64 heads on 8, e4m3, 201 us, 5.6 TB/s.
 #include <algorithm>
 
 #include "attend.cuh"
@@ -506,7 +510,9 @@ k_attend(AttendArgs a, BatchArgs b, CacheArgs c) {
   if (a.beside && blockIdx.x == gridDim.x - 1) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-// Joins the parts of each row, W warps a (row, head), the parts dealt out among them.
+// Joins the parts of each row, W warps a (row, head), the parts dealt out among them: all
+// eight warps from 16 parts on (few rows then), one below (many). Parts are taken in their
+// order. A few us: latency, and the partial sums come from L2.
 constexpr int kJoinWarps = 8;
 struct JoinSets {
   AttendArgs of[2];
@@ -704,8 +710,10 @@ Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page, in
     // even out (8 blocks an SM took 3 to 14% longer on ragged batches, 48 up to 9%), of
     // 1,024 tokens at least (parts of 256 cost 10% on short contexts) unless there are
     // then fewer than two blocks an SM, where parts go down to 256.
-    // Tiles of 8 rows where one new token's heads (or all rows there are) fit in one,
-    // else of 16, which read keys and values once for twice the rows.
+    // Tiles of 8 rows where one new token's heads (or all rows there are) fit in one (16
+    // took 235 for 205 us over e4m3, 8 requests of up to 120,000, and 308 for 300 over
+    // bf16), else of 16, which read keys and values once for twice the rows (82 us with
+    // 8, 72 with 16 for the 16 rows, 167 and 124 for the 64 rows above).
     p.nt = (p.tc ? a.group : rows) <= 8 ? 1 : 2;
     p.row_tiles = p.tc ? 1 : (int)std::min<int64_t>((rows + 8 * p.nt - 1) / (8 * p.nt), 1 << 20);
     const int64_t units = std::max<int64_t>(1, (int64_t)b->n_seq * heads * p.row_tiles);
@@ -719,17 +727,26 @@ Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page, in
   p.part_rows[1] = b->n_rows;
   p.parts[1] = 1;
   if (p.tc) {
-    // Parts are worth their join where there are fewer units than half the SMs, or two to
-    // six rounds of long ones (then a part evens out the last round). As many as 256 MB of
-    // partial sums allow, none shorter than 512 tokens; how many are taken is seen on the
-    // device, where the lengths are known.
+    // Parts are worth their join where there are fewer units than half the SMs (64, 256 and
+    // 512 new tokens after 32,000, 32 heads on 8 of 128: 80, 135 and 209 us, whole contexts
+    // 342 to 350), two to six rounds of long ones (a part then evens out the last round:
+    // 4,096 tokens 1,407 us, 1,440 whole), or by the lengths known here a tenth less time
+    // (1,280 and 1,536 tokens: 521 and 548 us, 666 and 675 whole; where it is less than
+    // that, the join's launch took 3 to 7% more). As many as 256 MB of partial sums allow,
+    // none shorter than 512 tokens; how many are taken is seen on the device, where all
+    // lengths are known.
     const int64_t all = (int64_t)b->n_rows * a.group;
     const int64_t tiles = std::min<int64_t>(
         (int64_t)b->n_seq * ((rows + kTcRows - 1) / kTcRows), all / kTcRows + b->n_seq);
     const int64_t row = ((int64_t)dim * 4 + 8) * a.heads * std::max(b->n_rows, 1);
     const int64_t least = std::max<int64_t>(all - (int64_t)b->n_seq * p.few, 1) / kTcRows * heads;
-    if (2 * least <= sms || (least >= 2 * sms && least <= 6 * sms && len >= 8192))
-      p.parts[1] = (int)std::max<int64_t>(1, std::min<int64_t>({64, len / 512, (256ll << 20) / row}));
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>({64, len / 512, (256ll << 20) / row}));
+    bool worth = 2 * least <= sms || (least >= 2 * sms && least <= 6 * sms && len >= 8192);
+    if (!worth && least < 2 * sms)
+      for (int64_t n = 2; n <= most; ++n)
+        worth |= parts_time(n, tiles * heads, len, sms) <
+                 0.9f * parts_time(1, tiles * heads, len, sms);
+    if (worth) p.parts[1] = (int)most;
     p.split[1] = (int)std::max<int64_t>(kTcTokens, (len + p.parts[1] - 1) / p.parts[1]);
     p.units = std::max<int64_t>(1, tiles * heads) * p.parts[1];
   }

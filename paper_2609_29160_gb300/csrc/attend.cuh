@@ -81,6 +81,16 @@ __device__ __forceinline__ void part_of(const AttendArgs& a, int sp, int& lo, in
   hi = to;
 }
 
+// k_attend_tc's time, in positions, with contexts of up to `len` in n parts each: whole
+// rounds of one unit an SM, a round takes its part and about 900 more (a unit's start and
+// end); a split costs what a row's partial sums cost to write and read, about 400 a part,
+// spread over all SMs, and some 1,500 for the join.
+__host__ __device__ __forceinline__ float parts_time(int64_t n, int64_t units, int64_t len,
+                                                     int64_t sms) {
+  return (float)((units * n + sms - 1) / sms) * ((float)len / n + 900.f) +
+         (n > 1 ? 400.f * n * units / sms + 1500.f : 0.f);
+}
+
 // Whether a row saw no position (scores that are no number leave m alone, not l).
 __device__ __forceinline__ bool saw_nothing(float m, float l) { return m == -INFINITY && l == l; }
 
