@@ -295,6 +295,23 @@ def test_few_and_many_rows_side_by_side(groups, lens, pool):
     check(bt, 2 * groups, "f16", window=90)
 
 
+@pytest.mark.parametrize("groups,lens", [
+    (1, [(300, 16), (400, 17), (100, 300), (2000, 1)]),
+    (4, [(300, 4), (300, 5), (2500, 1), (100, 100)]),
+    (20, [(700, 1), (3000, 1), (50, 2), (10, 30)]),
+    (70, [(700, 1), (3000, 1), (50, 2)])])
+@pytest.mark.parametrize("pool", ["bf16", "i8"])
+def test_a_few_rows_beside_chunks(groups, lens, pool):
+    """Sequences of one token, of 16 and of 17 rows, next to longer ones."""
+    check(ref.Batch(lens, 16, 2, 128, ref.T[pool], seed=26), 2 * groups)
+
+
+@pytest.mark.parametrize("lens", [[(16000, 1280)], [(15000, 700), (9000, 600), (200, 1)]])
+@pytest.mark.parametrize("pool", ["bf16", "e4m3"])
+def test_chunks_of_one_to_two_rounds_in_parts(lens, pool):
+    check(ref.Batch(lens, 64, 8, 64, ref.T[pool], seed=27), 32)
+
+
 def test_many_sequences():
     """More sequences than a warp looks at in a step, most of them of no rows."""
     lens = [((7 * i) % 300, (i * i) % 5 if i % 9 else 40 + i % 100) for i in range(150)]
