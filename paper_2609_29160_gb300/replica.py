@@ -102,11 +102,18 @@ def _index(t, what, n):
     return t.data_ptr()
 
 
-def _kept(stream, *tensors):
-    """Memory that torch may hand out again is not before `stream` is done with it."""
-    for t in tensors:
-        if t is not None:
-            t.record_stream(stream)
+def _on(stream, fn, *args):
+    """fn(*args) on `stream`: the memory that it makes is that stream's own (a block of the
+    current stream's may still be in use there), and what it returns is kept for the
+    current stream's work as well."""
+    cuda = tre._torch().cuda
+    here = cuda.current_stream(stream.device)
+    with cuda.stream(stream):
+        made = fn(*args)
+    for t in made if isinstance(made, tuple) else (made,):
+        if t is not None and t.is_cuda:
+            t.record_stream(here)
+    return made
 
 
 class KvCache:
@@ -248,6 +255,9 @@ def tre_qk_norm_rope(q, k, positions=None, q_weight=None, k_weight=None, eps=1e-
     """Per-head norms and position rotation of q [rows][q heads][dim] and
     k [rows][k heads][dim] (either may be None) in one pass. Weights None: not
     normed; cos_sin None: not turned. Returns (q_out, k_out)."""
+    if stream is not None:
+        return _on(stream, tre_qk_norm_rope, q, k, positions, q_weight, k_weight, eps, cos_sin,
+                   interleaved, q_out, k_out, diag)
     lib = tre._lib or tre.load()
     packed, q_out, k_out = _heads(q, k, q_weight, k_weight, eps, cos_sin, interleaved, q_out,
                                   k_out, True)
@@ -255,11 +265,9 @@ def tre_qk_norm_rope(q, k, positions=None, q_weight=None, k_weight=None, eps=1e-
     if positions is not None:
         at = _index(positions, "positions", (q if q is not None else k).shape[0])
     code = lib.tre_qk_norm_rope(packed, at, None if diag is None else diag.data_ptr(),
-                                tre._stream(stream))
+                                tre._stream(None))
     if code:
         tre._check("tre_qk_norm_rope", code)
-    if stream is not None:
-        _kept(stream, q_out, k_out)
     return q_out, k_out
 
 
@@ -268,6 +276,9 @@ def tre_kv_append(cache, batch, k, v, q=None, q_weight=None, k_weight=None, eps=
     """Writes the batch's new keys and values [rows][heads][dim] into the cache, keys
     normed and turned on the way; with q also returns the queries normed and
     turned (else None)."""
+    if stream is not None:
+        return _on(stream, tre_kv_append, cache, batch, k, v, q, q_weight, k_weight, eps, cos_sin,
+                   interleaved, q_out, diag)
     lib = tre._lib or tre.load()
     if k is None:
         raise ValueError("k: expected keys")
@@ -281,16 +292,16 @@ def tre_kv_append(cache, batch, k, v, q=None, q_weight=None, k_weight=None, eps=
     if cache.dtype is not dtype and cache.code not in _CODES:
         raise ValueError(f"k: a cache of {cache.dtype} takes no type {dtype}")
     code = lib.tre_kv_append(cache.packed, batch.packed, packed, v.data_ptr(), vr, vh,
-                             None if diag is None else diag.data_ptr(), tre._stream(stream))
+                             None if diag is None else diag.data_ptr(), tre._stream(None))
     if code:
         tre._check("tre_kv_append", code)
-    if stream is not None:
-        _kept(stream, q_out)
     return q_out
 
 
 def tre_kv_read(cache, batch, dtype="bf16", k_out=None, v_out=None, diag=None, stream=None):
     """The batch's rows out of the cache: (k, v) [rows][heads][dim] of dtype."""
+    if stream is not None:
+        return _on(stream, tre_kv_read, cache, batch, dtype, k_out, v_out, diag)
     lib = tre._lib or tre.load()
     code = _code(dtype, _FLOATS, "dtype")
     shape = (batch.n_rows, cache.heads, cache.dim)
@@ -308,11 +319,9 @@ def tre_kv_read(cache, batch, dtype="bf16", k_out=None, v_out=None, diag=None, s
             raise ValueError("k_out, v_out: expected the same strides")
     code = lib.tre_kv_read(cache.packed, batch.packed, code, k_out.data_ptr(), v_out.data_ptr(),
                            row, head, None if diag is None else diag.data_ptr(),
-                           tre._stream(stream))
+                           tre._stream(None))
     if code:
         tre._check("tre_kv_read", code)
-    if stream is not None:
-        _kept(stream, k_out, v_out)
     return k_out, v_out
 
 
@@ -321,6 +330,8 @@ def tre_chunk_attention(q, cache, batch, scale=None, window=0, lse=False, out=No
     """Attention of the batch's rows q [rows][heads][dim] over the cache, each row up
     to its own position (its last `window` positions only, with a window). Returns
     out [rows][heads][dim]; with lse also float32 [rows][heads]."""
+    if stream is not None:
+        return _on(stream, tre_chunk_attention, q, cache, batch, scale, window, lse, out, diag)
     lib = tre._lib or tre.load()
     dtype = q.dtype
     code = _code(dtype, _HALVES, "q")
@@ -339,7 +350,7 @@ def tre_chunk_attention(q, cache, batch, scale=None, window=0, lse=False, out=No
     at = ATTEND.pack(code, heads, window, 1.0 / math.sqrt(cache.dim) if scale is None else scale,
                      q.data_ptr(), qr, qh, out.data_ptr(), o_row, oh,
                      0 if ls is None else ls.data_ptr())
-    size, s = C.c_size_t(0), tre._stream(stream)
+    size, s = C.c_size_t(0), tre._stream(None)
     dg = None if diag is None else diag.data_ptr()
     code = lib.tre_chunk_attention(cache.packed, batch.packed, at, None, size, dg, s)
     if code:
@@ -349,6 +360,4 @@ def tre_chunk_attention(q, cache, batch, scale=None, window=0, lse=False, out=No
     code = lib.tre_chunk_attention(cache.packed, batch.packed, at, ws.data_ptr() or 256, size, dg, s)
     if code:
         tre._check("tre_chunk_attention", code)
-    if stream is not None:
-        _kept(stream, out, ls, ws)
     return (out, ls) if lse else out

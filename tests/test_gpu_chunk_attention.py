@@ -210,6 +210,30 @@ def test_another_stream():
     assert all(torch.equal(g, want) for g in got)
 
 
+def test_memory_still_in_use_on_the_current_stream():
+    """What a call makes for another stream is no block that the current stream's work,
+    queued before and already let go by its owner, has still to write."""
+    bt = ref.Batch([(3000, 1), (20, 160)], 16, 2, 64, torch.bfloat16, seed=28)
+    q = torch.randn(bt.rows, 4, 64, device="cuda").bfloat16()
+    cache, batch = bt.cache(tre), bt.batch(tre)
+    s = torch.cuda.Stream()
+    want = tre.tre_chunk_attention(q, cache, batch, stream=s)
+    s.synchronize()
+    torch.cuda.synchronize()
+    big = torch.zeros(1 << 28, device="cuda")
+    for _ in range(20):
+        big += 1
+    gone = [torch.empty_like(q) for _ in range(4)] + [
+        torch.empty(1 << 20, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    for t in gone:
+        t.fill_(3)
+    del gone, t
+    got = tre.tre_chunk_attention(q, cache, batch, stream=s)
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+
+
 def test_refusals():
     bt = ref.Batch([(30, 1)], 16, 2, 64, torch.bfloat16)
     c, b = bt.cache(tre), bt.batch(tre)
