@@ -30,6 +30,7 @@ struct AttendArgs {
   // k_attend_tc: `parts` is the most there is room for; how many it takes is seen on the
   // device, where the rows of each sequence are known, and left here for the join
   int32_t* parts_taken;
+  uint32_t* next;                 // k_attend_tc: units taken past the first of each block, or null
   int32_t sms;
   bool wide;                      // outputs on 32-byte boundaries
   bool beside;                    // k_attend: launched beside k_attend_tc

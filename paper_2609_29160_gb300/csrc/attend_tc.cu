@@ -29,7 +29,7 @@
 // reads from shared memory and the start of each unit. Dim 64 has half the products for
 // the same exponentials: there the chain of a row binds (scores out of TMEM, maximum,
 // 128 exponentials, weights back: some 2,600 cycles a tile, and 6,000 to start and end a
-// unit): 24 prompts of up to 2,000, 16 heads, f16, 127 us. Two threads a row spill at the
+// unit): 24 prompts of up to 2,000, 16 heads, f16, 123 us. Two threads a row spill at the
 // registers that are then left and took twice the time.
 #include <cuda.h>
 
@@ -343,9 +343,10 @@ struct alignas(64) Unit {
   __device__ __forceinline__ bool find(const AttendArgs& a, const BatchArgs& b,
                                        const CacheArgs& c, uint32_t u) {
     const int lane = threadIdx.x & 31;
-    // every other round of blocks backwards, so that none has the longer end of each
+    // (blocks that take units in turn) every other round backwards, so that none has the
+    // longer end of each
     const uint32_t round = u / gridDim.x;
-    if (round & 1) u = round * gridDim.x + (gridDim.x - 1 - (u - round * gridDim.x));
+    if (!a.next && (round & 1)) u = round * gridDim.x + (gridDim.x - 1 - (u - round * gridDim.x));
     kvh = (int)(u % c.heads);
     u /= c.heads;
     sp = (int)(u % a.parts);
@@ -457,7 +458,7 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
     }
     for (int k = 0; k < kUnits; ++k) {
       bar_init(u_full + k, 1);
-      bar_init(u_empty + k, kRowWarps + 1);
+      bar_init(u_empty + k, kRowWarps + kCopyWarps);     // (one copy warp writes it)
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -783,18 +784,24 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
     // ---- copies --------------------------------------------------------------
     uint32_t n_tile = 0, nu = 0;
     bool alive = true;
-    for (uint32_t u = blockIdx.x; alive; u += gridDim.x, ++nu) {
+    uint32_t u = blockIdx.x;
+    for (; alive; ++nu) {
       // units are found here, ahead of those who need them
       Unit w;
-      const bool some = w.find(a, b, c, u);
-      if (!some) w.i = -1;
+      Unit* shared = reinterpret_cast<Unit*>(sm + L::AT_UNIT + nu % kUnits * 64);
       if (warp == kCopyWarp) {
+        if (!w.find(a, b, c, u)) w.i = -1;
         alive = bar_wait(u_empty + nu % kUnits, ((nu / kUnits) & 1) ^ 1, dead);
         if (!alive) break;
-        if (lane == 0) *reinterpret_cast<Unit*>(sm + L::AT_UNIT + nu % kUnits * 64) = w;
+        if (lane == 0) *shared = w;
         bar_arrive_warp(u_full + nu % kUnits);
+      } else {
+        alive = bar_wait(u_full + nu % kUnits, (nu / kUnits) & 1, dead);
+        if (!alive) break;
+        w = *shared;
+        bar_arrive_warp(u_empty + nu % kUnits);
       }
-      if (!some) break;
+      if (w.i < 0) break;
       const int i = w.i, kvh = w.kvh, lo = w.lo, hi = w.hi, n = max(w.n_x[0], w.n_x[1]);
       const int cw = warp - kCopyWarp;
       // its queries into L2, before the row warps get there
@@ -1022,6 +1029,11 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
         }
       }
       n_tile += n;
+      u += gridDim.x;
+      if (a.next && warp == kCopyWarp) {         // whoever is first takes the next unit
+        if (lane == 0) u = gridDim.x + atomicAdd(a.next, 1u);
+        u = __shfl_sync(0xffffffffu, u, 0);
+      }
     }
   } else {
     // ---- products --------------------------------------------------------------

@@ -336,6 +336,26 @@ def test_chunks_of_one_to_two_rounds_in_parts(lens, pool):
     check(ref.Batch(lens, 64, 8, 64, ref.T[pool], seed=27), 32)
 
 
+@pytest.mark.parametrize("pool,heads,group,dim", [("bf16", 8, 1, 64), ("f16", 4, 4, 128),
+                                                  ("i8", 4, 4, 64), ("e4m3", 4, 2, 128)])
+def test_more_ragged_units_than_sms(pool, heads, group, dim):
+    """Which block takes which sequence's rows changes nothing, call after call."""
+    lens = [((37 * i) % 400, 40 + (389 * i) % 900) for i in range(24)] + [(70, 1), (0, 3)]
+    bt = ref.Batch(lens, 32, heads, dim, ref.T[pool], seed=29)
+    dt = "f16" if pool == "f16" else "bf16"
+    out, _ = check(bt, heads * group, dt)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q = torch.randn(bt.rows, heads * group, dim, generator=g, device="cuda").to(ref.T[dt])
+    cache, batch = bt.cache(tre), bt.batch(tre)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = tre.tre_chunk_attention(q, cache, batch)
+    for _ in range(3):
+        got.zero_()
+        graph.replay()
+        assert torch.equal(got, out)
+
+
 def test_many_sequences():
     """More sequences than a warp looks at in a step, most of them of no rows."""
     lens = [((7 * i) % 300, (i * i) % 5 if i % 9 else 40 + i % 100) for i in range(150)]
