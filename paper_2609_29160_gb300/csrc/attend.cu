@@ -92,6 +92,10 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const BatchArg
   using S = Shape<CODE, DIM, NT>;
   using CT = typename std::conditional<CODE == Code::kHalf, T, __half>::type;
   constexpr int EPT = 16 / S::CB, SPB = EPT / 4, BLOCKS = DIM / (4 * EPT);
+  // Weights are rounded to 16 bits for their product with values. In bfloat16 that is 8
+  // significant bits, as coarse as the output's own rounding: what it leaves over is
+  // multiplied as well.
+  constexpr bool SPLIT = CODE == Code::kHalf && std::is_same<T, __nv_bfloat16>::value;
   extern __shared__ __align__(128) uint8_t sm[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, cc = lane & 3;
@@ -337,7 +341,9 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const BatchArg
             }
           }
       }
-      uint32_t pf[NT][2];            // rows g by positions 2 cc, 2 cc + 1 (+ 8)
+      // rows g by positions 2 cc, 2 cc + 1 (+ 8); with SPLIT also what a weight's rounding
+      // left over
+      uint32_t pf[NT][2], rest[SPLIT ? NT : 1][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float p[4];
@@ -349,8 +355,22 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const BatchArg
           // (a masked position's scale may be anything: its weight stays zero)
           if (S::SCALES) p[e] = p[e] == 0.f ? 0.f : p[e] * vs[e >> 1];
         }
-        pf[nt][0] = turned(pack<CT>(p[0], p[1]));
-        pf[nt][1] = turned(pack<CT>(p[2], p[3]));
+        if constexpr (SPLIT) {
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            // the largest bfloat16 below a weight, so that what is left over is above zero
+            // and a value that is infinite stays so in both products
+            uint32_t b0 = __float_as_uint(p[2 * y]), b1 = __float_as_uint(p[2 * y + 1]);
+            b0 -= min(b0, 1u);
+            b1 -= min(b1, 1u);
+            pf[nt][y] = turned(__byte_perm(b0, b1, 0x7632));
+            rest[nt][y] = turned(pack<CT>(p[2 * y] - __uint_as_float(b0 & 0xffff0000u),
+                                          p[2 * y + 1] - __uint_as_float(b1 & 0xffff0000u)));
+          }
+        } else {
+          pf[nt][0] = turned(pack<CT>(p[0], p[1]));
+          pf[nt][1] = turned(pack<CT>(p[2], p[3]));
+        }
       }
       // values: an m-tile's rows g and g + 8 are neighbouring elements, as a lane's
       // read delivers them
@@ -372,7 +392,10 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const BatchArg
                                    __byte_perm(w[2][y], w[3][y], 0x5410),
                                    __byte_perm(w[2][y], w[3][y], 0x7632)};
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) Mma<CT>::run(o[nt][set * 4 + y], f, pf[nt][0], pf[nt][1]);
+            for (int nt = 0; nt < NT; ++nt) {
+              Mma<CT>::run(o[nt][set * 4 + y], f, pf[nt][0], pf[nt][1]);
+              if constexpr (SPLIT) Mma<CT>::run(o[nt][set * 4 + y], f, rest[nt][0], rest[nt][1]);
+            }
           }
         }
       } else {
