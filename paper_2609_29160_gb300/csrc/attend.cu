@@ -97,6 +97,7 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const BatchArg
   // multiplied as well.
   constexpr bool SPLIT = CODE == Code::kHalf && std::is_same<T, __nv_bfloat16>::value;
   extern __shared__ __align__(128) uint8_t sm[];
+  __shared__ float w_m[kWarps][S::ROWS], w_l[kWarps][S::ROWS];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, cc = lane & 3;
   const int kvh = blockIdx.x % c.heads;
@@ -108,7 +109,6 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const BatchArg
   const Seq sq = seq_of(b, i);
   const int rows = sq.n * a.group, base = sq.ctx - sq.n;
   if (rows > a.few) return;
-
   for (int rt = rt0; rt * S::ROWS < rows; rt += a.row_tiles) {
     const int r_first = rt * S::ROWS, r_last = min(r_first + S::ROWS, rows) - 1;
     const int t_first = a.by_group.div(r_first), t_last = a.by_group.div(r_last);
@@ -118,6 +118,8 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const BatchArg
     const int n_tiles = hi > lo ? (hi - lo + kTile - 1) / kTile : 0;
     const int mine = n_tiles > warp ? (n_tiles - warp + kWarps - 1) / kWarps : 0;
 
+    const Edges edge = edges_of<kTile>(a.window, base + t_first, base + t_last, lo, hi);
+    bool left_out = false;           // values of theirs (see finite)
     uint8_t* ring = sm + warp * (S::STAGES * S::STAGE);
     const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
     // the page of token (lane & 15) of the next tile to copy
@@ -245,13 +247,23 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const BatchArg
     for (int k = 0; k < mine; ++k) {
       wait_copies<S::STAGES - 2>();
       __syncwarp();
-      const uint8_t* st = ring + (k % S::STAGES) * S::STAGE;
+      uint8_t* st = ring + (k % S::STAGES) * S::STAGE;
       const uint4* kt = reinterpret_cast<const uint4*>(st);
-      const uint4* vt = reinterpret_cast<const uint4*>(st + kTile * S::ROW);
+      uint4* vt = reinterpret_cast<uint4*>(st + kTile * S::ROW);
+      const int j0 = lo + (warp + k * kWarps) * kTile;
+      if (CODE != Code::kI8 && (j0 < edge.behind || j0 >= edge.ahead)) {
+        for (int u = lane; u < kTile * S::CPR; u += 32) {
+          const uint4 x = vt[u], y = finite<T, CODE>(x);
+          if (differ(x, y)) {
+            vt[u] = y;
+            left_out = true;
+          }
+        }
+        __syncwarp();
+      }
       const float* sc = reinterpret_cast<const float*>(st + 2 * kTile * S::ROW);
       const uint32_t held =
           *reinterpret_cast<const uint32_t*>(st + 2 * kTile * S::ROW + S::SCALES) & 0xffffu;
-
       float s[NT][4];                // positions g, g + 8 by rows 2 cc, 2 cc + 1
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -280,7 +292,6 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const BatchArg
         }
       }
 
-      const int j0 = lo + (warp + k * kWarps) * kTile;
       float vs[2] = {1.f, 1.f}, ex[2] = {0.f, 0.f}, ks[2] = {1.f, 1.f};
       if constexpr (S::SCALES > 0) {
 #pragma unroll
@@ -435,7 +446,6 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const BatchArg
     wait_copies<0>();
 
     // join the four warps
-    __shared__ float w_m[kWarps][S::ROWS], w_l[kWarps][S::ROWS];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -449,7 +459,7 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const BatchArg
           w_l[warp][8 * nt + 2 * cc + x] = sum;
         }
       }
-    __syncthreads();
+    left_out = __syncthreads_or(left_out);
     constexpr int PITCH = DIM + 4;
     float* os = reinterpret_cast<float*>(sm);
 #pragma unroll
@@ -492,15 +502,10 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const BatchArg
 #pragma unroll
         for (int e = 0; e < EL; ++e) x[e] += os[(w * S::ROWS + r) * PITCH + lane * EL + e];
       }
-      bool odd = false;
-#pragma unroll
-      for (int e = 0; e < EL; ++e) odd |= !(fabsf(x[e]) < INFINITY);
       const int t = a.by_group.div(rr), h = kvh * a.group + (rr - t * a.group);
       const int64_t row = (int64_t)(sq.start + t);
-      if (__any_sync(0xffffffffu, odd) && top > -INFINITY)
-        row_again<T, CODE, DIM>(a, b, c, i, kvh,
-                                reinterpret_cast<const T*>(a.q) + row * a.q_row + (int64_t)h * a.q_head,
-                                base + t, lo, hi, top, x);
+      if (CODE != Code::kI8 && left_out && top > -INFINITY)
+        add_seen<T, CODE, DIM>(b, c, a.window, i, kvh, base + t, lo, edge, hi, x);
       const int64_t part_row = a.tokens > 0 ? (int64_t)i * a.tokens + t : row;
       if (lane == 0) row_state(a, sp, row, part_row, h, top, sum);
       if (a.parts > 1) {

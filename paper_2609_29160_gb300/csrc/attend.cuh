@@ -1,6 +1,8 @@
 // What the attention kernels share: the call's arguments, the range of positions
-// that a tile of rows sees, and the output of rows whose masked values are no number.
+// that a tile of rows sees, and what masked values that are no numbers are kept from.
 #pragma once
+
+#include <type_traits>
 
 #include "kvcache.cuh"
 
@@ -133,42 +135,63 @@ __device__ __forceinline__ void cached(const uint8_t* base, int64_t off, int lan
   }
 }
 
-// One row's sum of exp2(s_j - m) v_j over the positions of [lo, hi) that it sees,
-// by one warp, DIM/32 elements a lane. The tiled kernels multiply masked values by
-// zero, which leaves NaN where a masked value is infinite or no number: a row that
-// comes out that way is done again here, where masked values are not touched.
-template <class T, Code CODE, int DIM>
-__device__ void row_again(const AttendArgs& a, const BatchArgs& b, const CacheArgs& c, int i,
-                          int kvh, const T* q, int pos, int lo, int hi, float m, float* acc) {
-  constexpr int N = DIM / 32;
-  const int lane = threadIdx.x & 31;
-  float x[N];
-#pragma unroll
-  for (int e = 0; e < N; ++e) {
-    x[e] = (float)q[lane * N + e];
-    acc[e] = 0.f;
+// Words of a tile with elements that are no finite numbers as zeros. Products multiply
+// masked values by weights of zero, which such a value would turn into NaN: in tiles that
+// some row sees and another does not they are left out, and rows that see them get them
+// back from add_seen.
+template <class T, Code CODE> __device__ __forceinline__ uint32_t finite(uint32_t x) {
+  if constexpr (CODE == Code::kHalf) {
+    constexpr uint32_t top = std::is_same<T, __nv_bfloat16>::value ? 0x7f807f80u : 0x7c007c00u;
+    return x & ~__vcmpeq2(x & top, top);
+  } else if constexpr (CODE == Code::kE4m3) {
+    return x & ~__vcmpeq4(x & 0x7f7f7f7fu, 0x7f7f7f7fu);
   }
-  if (a.window > 0) lo = max(lo, pos - a.window + 1);
-  hi = min(hi, pos + 1);
+  return x;
+}
+template <class T, Code CODE> __device__ __forceinline__ uint4 finite(const uint4& v) {
+  return make_uint4(finite<T, CODE>(v.x), finite<T, CODE>(v.y), finite<T, CODE>(v.z),
+                    finite<T, CODE>(v.w));
+}
+__device__ __forceinline__ bool differ(const uint4& a, const uint4& b) {
+  return ((a.x ^ b.x) | (a.y ^ b.y) | (a.z ^ b.z) | (a.w ^ b.w)) != 0;
+}
+
+// The tiles of STEP positions of [lo, hi) (lo a multiple of STEP) that not every row sees,
+// with rows between positions p0 and p1: those below `behind` and from `ahead` on.
+struct Edges {
+  int behind, ahead;
+};
+template <int STEP>
+__device__ __forceinline__ Edges edges_of(int window, int p0, int p1, int lo, int hi) {
+  const int64_t w = window > 0 ? (int64_t)p1 - window + 1 : 0;      // the last row sees from here on
+  Edges e;
+  e.behind = w > lo ? (int)min64(hi, (w + STEP - 1) / STEP * STEP) : lo;
+  e.ahead = p0 + 1 < hi ? max(e.behind, max(lo, p0 + 1) / STEP * STEP) : hi;
+  return e;
+}
+
+// Adds to one row's sum, by one warp and DIM/32 elements a lane, the elements that are no
+// finite numbers of the edges' positions that it sees. Weights do not matter to them: any
+// that is above zero leaves an infinity or NaN as it is.
+template <class T, Code CODE, int DIM>
+__device__ __forceinline__ void add_seen(const BatchArgs& b, const CacheArgs& c, int window, int i,
+                                         int kvh, int pos, int lo, const Edges& edge, int hi,
+                                         float* acc) {
+  constexpr int N = DIM / 32;
+  if (window > 0) lo = max(lo, pos - window + 1);
+#pragma unroll 1
   for (int j = lo; j < hi; ++j) {
+    if (j >= edge.behind && j < edge.ahead) j = edge.ahead;
+    if (j > pos || j >= hi) break;
     int slot = 0;
     const int page = page_of(c, b, i, j, slot);
     if (page < 0) continue;
-    const int64_t off = page * c.s_page + slot * c.s_token + kvh * c.s_head;
-    const int64_t soff = page * c.c_page + slot * c.c_token + kvh * c.c_head;
-    float y[N], s = 0.f;
-    cached<T, CODE, DIM>(c.k, off, lane, y);
+    float y[N];
+    cached<T, CODE, DIM>(c.v, page * c.s_page + slot * c.s_token + kvh * c.s_head,
+                         threadIdx.x & 31, y);
 #pragma unroll
-    for (int e = 0; e < N; ++e) s = __fmaf_rn(x[e], y[e], s);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    s *= a.scale2;
-    if (CODE != Code::kHalf) s *= c.k_scale[soff];
-    float p = exp2_fast(s - m);
-    if (CODE != Code::kHalf) p = mul_rn(p, c.v_scale[soff]);
-    cached<T, CODE, DIM>(c.v, off, lane, y);
-#pragma unroll
-    for (int e = 0; e < N; ++e) acc[e] = __fmaf_rn(p, y[e], acc[e]);
+    for (int e = 0; e < N; ++e)
+      if (!(fabsf(y[e]) < INFINITY)) acc[e] += y[e];
   }
 }
 
