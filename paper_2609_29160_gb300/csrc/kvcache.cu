@@ -96,7 +96,7 @@ template <Code CODE> __device__ __forceinline__ uint32_t codes_of(const float* q
     const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(q[2], q[3]), __NV_SATFINITE, __NV_E4M3);
     return lo | hi << 16;
   } else {
-    // |q| <= 127: in q + 1.5 * 2^23 the last byte is q rounded to nearest even
+    // |q| <= 127 (see where it is taken): in q + 1.5 * 2^23 the last byte is q rounded to nearest even
     uint32_t v[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = __float_as_uint(__fadd_rn(q[j], 12582912.f));
@@ -279,7 +279,11 @@ k_heads(HeadsArgs a, BatchArgs b, CacheArgs c, int groups, int its, tre_diag* di
               for (int e = 0; e < 8; ++e) q[e] = quotient(x[e], by, r);
             } else {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) q[e] = div_rn(x[e], by);
+              for (int e = 0; e < 8; ++e) {
+                // (a scale that is a subnormal of few bits may be well below max|x| / Q)
+                q[e] = div_rn(x[e], by);
+                if constexpr (CODE == Code::kI8) q[e] = fminf(fmaxf(q[e], -Q), Q);
+              }
             }
             *reinterpret_cast<uint32_t*>(p + ea) = codes_of<CODE>(q);
             *reinterpret_cast<uint32_t*>(p + eb) = codes_of<CODE>(q + 4);

@@ -116,6 +116,30 @@ def test_scales_of_very_different_size(dtype, pool, lens):
     check(bt, 8, dtype)
 
 
+def test_codes_of_the_smallest_rows():
+    """Rows whose largest element is a subnormal of few bits: its scale is off by far more
+    than a rounding of a normal number, and the quotient passes the last code."""
+    for pool in (torch.int8, torch.float8_e4m3fn):
+        n = 400
+        bt = ref.Batch([(0, n)], 16, 2, 64, pool)
+        g = torch.Generator(device="cuda").manual_seed(3)
+        x = torch.randn(n, 2, 64, generator=g, device="cuda").bfloat16()
+        # cosines from 2^-149 to about 2^-80, no sines: rows of x times that, rounded once
+        c = torch.exp2(torch.linspace(-149, -80, n, device="cuda").double()).float()
+        table = torch.zeros(n, 64, device="cuda")
+        table[:, :32] = c[:, None]
+        tre.tre_kv_append(bt.cache(tre), bt.batch(tre), x, x, cos_sin=table)
+        j = torch.arange(n, device="cuda")
+        pg, slot, _ = bt.held(0, j)
+        want, sc = ref.codes(x.float() * c[:, None, None], pool)
+        assert (sc < 2.0 ** -126).any() and (sc > 0).any()
+        assert torch.equal(bt.ks[pg, slot], sc)
+        got = bt.k.view(torch.uint8)[pg, slot]
+        # (a zero keeps its sign in neither definition)
+        same = (got == want.view(torch.uint8)) | ((got & 0x7f) == 0) & ((want.view(torch.uint8) & 0x7f) == 0)
+        assert same.all(), (~same).sum()
+
+
 @pytest.mark.parametrize("pool", ["bf16", "e4m3", "i8"])
 @pytest.mark.parametrize("lens", [[(90, 1), (20, 160)], [(20000, 1)], [(0, 300), (40, 20)]])
 def test_outputs_on_16_byte_boundaries(pool, lens):
