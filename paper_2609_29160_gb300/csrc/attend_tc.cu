@@ -50,7 +50,7 @@ constexpr int kMmaWarp = kCopyWarp + kCopyWarps;
 constexpr int kThreads = (kMmaWarp + 1) * 32;
 constexpr int kUnits = 4;          // units that the copies may be ahead
 constexpr int kMarked = 64;        // units that a pass may mark (see Passes)
-constexpr long long kWaitClocks = 4000000000ll;
+constexpr long long kWaitClocks = 4000000000ll, kDrainClocks = 40000000ll;
 
 __device__ __forceinline__ uint32_t smem_of(const void* p) {
   return (uint32_t)__cvta_generic_to_shared(p);
@@ -562,6 +562,16 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
     return true;
   };
   auto finish = [&]() {
+    // A block that has given up does not know which of its copies and products are still on
+    // their way into its shared and tensor memory: it stays some 20 ms, far longer than any
+    // takes, before it lets go of them.
+    if (*dead) {
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      const long long from = clock64();
+      while (clock64() - from < kDrainClocks) {
+      }
+      __syncthreads();
+    }
     if (warp == kMmaWarp) {
       tmem_after();
       asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(*tmem_at));
