@@ -832,5 +832,5 @@ def tre_replay(latent, M, window_ms, K, profile, budget, r0, r_min, footprint, *
 
 
 from . import replica  # noqa: E402  (it uses the helpers above)
-from .replica import (KvBatch, KvCache, tre_chunk_attention, tre_kv_append,  # noqa: E402,F401
-                      tre_kv_read, tre_qk_norm_rope)
+from .replica import (KvBatch, KvCache, check_replica, replica_diag,  # noqa: E402,F401
+                      tre_chunk_attention, tre_kv_append, tre_kv_read, tre_qk_norm_rope)

@@ -116,6 +116,52 @@ def _on(stream, fn, *args):
     return made
 
 
+def host_diag():
+    """A zeroed tre_diag in pinned host memory: kernels write to it there, and the host reads
+    it (tre.read_diag) once the calls are done, without a copy."""
+    return tre._torch().zeros(tre.DIAG_BYTES, dtype=tre._torch().uint8).pin_memory()
+
+
+_own = None         # the tre_diag of calls that are given none, and its struct
+
+
+def replica_diag():
+    """The tre_diag (pinned host memory, accumulated) of the calls here that were given none.
+    An error in it (a wait on the device that gave up, whose outputs are undefined) is raised
+    by the next such call, or by check_replica."""
+    global _own
+    if _own is None:
+        t = host_diag()
+        _own = (t, tre.Diag.from_address(t.data_ptr()))
+    return _own[0]
+
+
+def _raise_error(fn):
+    d = _own[1]
+    code, d.err = d.err, 0
+    raise tre.TreError(fn, code)
+
+
+def check_replica():
+    """Waits for the device and raises what a call that was given no diag left behind."""
+    tre._torch().cuda.synchronize()
+    if _own is not None and _own[1].err:
+        _raise_error("an earlier call of a replica's step")
+
+
+def _diag(diag):
+    """Address of the caller's tre_diag, or of the calls' own."""
+    if diag is not None:
+        return diag.data_ptr()
+    if _own is None:
+        if tre._torch().cuda.is_current_stream_capturing():     # (no memory is made there)
+            return None
+        replica_diag()
+    if _own[1].err:
+        _raise_error("an earlier call of a replica's step")
+    return _own[0].data_ptr()
+
+
 class KvCache:
     """A paged cache over the caller's tensors: k, v [pages][page][heads][dim] (any
     strides with a dense last axis, the same for both) of bfloat16 or float16, or of
@@ -264,8 +310,7 @@ def tre_qk_norm_rope(q, k, positions=None, q_weight=None, k_weight=None, eps=1e-
     at = None
     if positions is not None:
         at = _index(positions, "positions", (q if q is not None else k).shape[0])
-    code = lib.tre_qk_norm_rope(packed, at, None if diag is None else diag.data_ptr(),
-                                tre._stream(None))
+    code = lib.tre_qk_norm_rope(packed, at, _diag(diag), tre._stream(None))
     if code:
         tre._check("tre_qk_norm_rope", code)
     return q_out, k_out
@@ -291,8 +336,8 @@ def tre_kv_append(cache, batch, k, v, q=None, q_weight=None, k_weight=None, eps=
     _, vr, vh = _rows(v, "v", dtype, *want)
     if cache.dtype is not dtype and cache.code not in _CODES:
         raise ValueError(f"k: a cache of {cache.dtype} takes no type {dtype}")
-    code = lib.tre_kv_append(cache.packed, batch.packed, packed, v.data_ptr(), vr, vh,
-                             None if diag is None else diag.data_ptr(), tre._stream(None))
+    code = lib.tre_kv_append(cache.packed, batch.packed, packed, v.data_ptr(), vr, vh, _diag(diag),
+                             tre._stream(None))
     if code:
         tre._check("tre_kv_append", code)
     return q_out
@@ -318,8 +363,7 @@ def tre_kv_read(cache, batch, dtype="bf16", k_out=None, v_out=None, diag=None, s
         if _rows(v_out, "v_out", tt, *shape)[1:] != (row, head):
             raise ValueError("k_out, v_out: expected the same strides")
     code = lib.tre_kv_read(cache.packed, batch.packed, code, k_out.data_ptr(), v_out.data_ptr(),
-                           row, head, None if diag is None else diag.data_ptr(),
-                           tre._stream(None))
+                           row, head, _diag(diag), tre._stream(None))
     if code:
         tre._check("tre_kv_read", code)
     return k_out, v_out
@@ -351,7 +395,7 @@ def tre_chunk_attention(q, cache, batch, scale=None, window=0, lse=False, out=No
                      q.data_ptr(), qr, qh, out.data_ptr(), o_row, oh,
                      0 if ls is None else ls.data_ptr())
     size, s = C.c_size_t(0), tre._stream(None)
-    dg = None if diag is None else diag.data_ptr()
+    dg = _diag(diag)
     code = lib.tre_chunk_attention(cache.packed, batch.packed, at, None, size, dg, s)
     if code:
         tre._check("tre_chunk_attention", code)

@@ -13,6 +13,7 @@ tss_window_reduce and PipelinePlan, and latent service times for tre_replay.
 from __future__ import annotations
 
 import paper_2609_29160_gb300 as tre
+from paper_2609_29160_gb300 import replica
 
 
 class Replica:
@@ -45,6 +46,7 @@ class Replica:
         self.time_scale, self.max_positions = time_scale, max_positions
         self.max_pages = -(-max_positions // page)
         self.steps = []                       # (prompt tokens, decode tokens, ms) of each
+        self.diag = replica.host_diag()
 
     def forward(self, tokens, batch):
         """Last-layer rows of the batch's new tokens."""
@@ -54,8 +56,8 @@ class Replica:
             qkv = (x @ w["qkv"]).view(-1, hq + 2 * hk, dim)
             q, k, v = qkv.split([hq, hk, hk], 1)
             q = tre.tre_kv_append(w["cache"], batch, k, v, q=q, q_weight=w["q_weight"],
-                                  k_weight=w["k_weight"], cos_sin=self.cos_sin)
-            y = tre.tre_chunk_attention(q, w["cache"], batch)
+                                  k_weight=w["k_weight"], cos_sin=self.cos_sin, diag=self.diag)
+            y = tre.tre_chunk_attention(q, w["cache"], batch, diag=self.diag)
             x = x + y.flatten(1) @ w["out"]
         return x
 
@@ -75,6 +77,14 @@ class Replica:
                            torch.tensor(starts, dtype=torch.int32).cuda(), starts[-1],
                            max_new=max(n for _, _, n in work), max_ctx=max(total))
 
+    def _check(self):
+        """What the kernels left in diag (the device has been waited for)."""
+        d = tre.read_diag(self.diag)
+        if d["err"]:
+            raise tre.TreError("served step", d["err"])
+        if d["dropped_range"]:
+            raise RuntimeError(f"served step: {d['dropped_range']} rows had no place")
+
     def _step(self, work):
         """Runs one step; the next token of each sequence."""
         torch = self.torch
@@ -87,6 +97,7 @@ class Replica:
         best = (x[ends] @ self.embed.T).float().argmax(1)
         b.record()
         b.synchronize()
+        self._check()
         ms = a.elapsed_time(b)
         prompt = sum(n for r, held, n in work if held < r["L_in"])
         self.steps.append((prompt, sum(n for _, _, n in work) - prompt, ms))
@@ -167,6 +178,7 @@ class Replica:
                 self.forward(tokens, batch)
             b.record()
             b.synchronize()
+            self._check()
             for r, _, _ in work:
                 self.free += r["pages"]
             ms.append(a.elapsed_time(b) / times / len(tokens))

@@ -182,3 +182,47 @@ def test_a_value_without_end_stays_so(dtype, lens):
     assert (out[..., 3] == math.inf).all() and (out[..., 9] == -math.inf).all()
     out[..., [3, 9]] = 0
     assert torch.isfinite(out).all()
+
+
+def test_calls_without_a_diag_have_their_own():
+    """Dropped rows are counted in pinned host memory, and an error there is raised by the
+    next call (once), or by check_replica. The error is written here by the host."""
+    bt = ref.Batch([(30, 3)], 16, 2, 64, torch.bfloat16)
+    c, b = bt.cache(tre), bt.batch(tre)
+    k = torch.randn(3, 2, 64, device="cuda").bfloat16()
+    tre.tre_kv_append(c, b, k, k)
+    torch.cuda.synchronize()
+    before = tre.read_diag(tre.replica_diag())["dropped_range"]
+    bt.table[0, 2] = -1                     # of position 32
+    tre.tre_kv_append(c, b, k, k)
+    torch.cuda.synchronize()
+    assert tre.read_diag(tre.replica_diag())["dropped_range"] == before + 1
+    own = tre.Diag.from_address(tre.replica_diag().data_ptr())
+    calls = [lambda: tre.tre_kv_append(c, b, k, k), lambda: tre.tre_kv_read(c, b),
+             lambda: tre.tre_chunk_attention(k, c, b), lambda: tre.tre_qk_norm_rope(k, None),
+             tre.check_replica]
+    for call in calls:
+        own.err = 5
+        with pytest.raises(tre.TreError, match="timed out") as e:
+            call()
+        assert e.value.code == 5
+        call()
+    # a call with a diag of its own does not look
+    own.err = 5
+    tre.tre_kv_append(c, b, k, k, diag=tre.new_diag())
+    own.err = 0
+    d = tre.replica.host_diag()
+    tre.tre_kv_append(c, b, k, k, diag=d)
+    torch.cuda.synchronize()
+    assert tre.read_diag(d)["dropped_range"] == 1
+
+
+def test_a_replica_looks_at_its_diag():
+    from paper_2609_29160_gb300 import served
+    rep = served.Replica()
+    d = tre.Diag.from_address(rep.diag.data_ptr())
+    for field, error in (("err", tre.TreError), ("dropped_range", RuntimeError)):
+        setattr(d, field, 5)
+        with pytest.raises(error, match="step"):
+            rep.serve([(0, 10, 2)])
+        setattr(d, field, 0)
