@@ -115,12 +115,18 @@ class Replica:
                 raise ValueError("arrivals: a request needs a token in and out, and its place")
             waiting.append({"t_arr": t, "L_in": n_in, "L_out": n_out, "pages": [], "held": 0,
                             "tokens": torch.randint(0, vocab, (n_in,), generator=g, device="cuda")})
-        # (the first launches are not the clock's)
-        first = {"pages": [], "L_in": 1, "tokens": torch.zeros(1, dtype=torch.int64, device="cuda")}
-        self._step([(first, 0, 1)])
-        self.prompt_weight(requests=1, times=1)
-        self.steps.pop()
-        self.free += first["pages"]
+        # (the first launches are not the clock's: a token's, and those of a prompt's chunk as
+        # long as there is room for)
+        for n in (1, self.chunk):
+            n = min(n, self.max_positions, len(self.free) * self.page)
+            if n == 0:
+                break
+            first = {"pages": [], "L_in": n, "tokens": torch.zeros(n, dtype=torch.int64, device="cuda")}
+            try:
+                self._step([(first, 0, n)])
+                self.steps.pop()
+            finally:
+                self.free += first["pages"]
         done, running, clock = [], [], 0.0
         need = lambda r: -(-(r["L_in"] + r["L_out"]) // self.page)      # noqa: E731
         room = len(self.free)
@@ -164,23 +170,29 @@ class Replica:
     def prompt_weight(self, requests=16, context=256, times=10):
         """What a prompt token costs against a decode token (Eq. 1's w_p): a step of a
         prompt's chunk and one of a token each of `requests` requests, timed, all with
-        `context` tokens in the cache."""
+        `context` tokens in the cache (for all of which there has to be room)."""
         torch = self.torch
         ms = []
         for n, new in ((1, self.chunk), (requests, 1)):
+            if context + new > self.max_positions:
+                raise ValueError(f"prompt_weight: {context} + {new} tokens, the replica takes {self.max_positions}")
+            if n * -(-(context + new) // self.page) > len(self.free):
+                raise ValueError(f"prompt_weight: too few free pages for {n} x {context + new} tokens")
             tokens = torch.zeros(n * new, dtype=torch.int64, device="cuda")
             work = [({"pages": []}, context, new) for _ in range(n)]
-            batch = self._batch(work)
-            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-            for k in range(times + 3):
-                if k == 3:
-                    a.record()
-                self.forward(tokens, batch)
-            b.record()
-            b.synchronize()
-            self._check()
-            for r, _, _ in work:
-                self.free += r["pages"]
+            try:
+                batch = self._batch(work)
+                a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+                for k in range(times + 3):
+                    if k == 3:
+                        a.record()
+                    self.forward(tokens, batch)
+                b.record()
+                b.synchronize()
+                self._check()
+            finally:
+                for r, _, _ in work:
+                    self.free += r["pages"]
             ms.append(a.elapsed_time(b) / times / len(tokens))
         return ms[0] / ms[1]
 
