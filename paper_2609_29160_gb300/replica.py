@@ -104,11 +104,18 @@ def _index(t, what, n):
 
 def _on(stream, fn, *args):
     """fn(*args) on `stream`: the memory that it makes is that stream's own (a block of the
-    current stream's may still be in use there), and what it returns is kept for the
-    current stream's work as well."""
-    cuda = tre._torch().cuda
-    here = cuda.current_stream(stream.device)
-    with cuda.stream(stream):
+    current stream's may still be in use there), what it returns is kept for the current
+    stream's work as well, and what it is given for that of `stream`, whose owner may let go
+    of it right after the call. (Waiting for what the current stream has still to write to
+    the inputs is the caller's, as everywhere in torch.)"""
+    torch = tre._torch()
+    here = torch.cuda.current_stream(stream.device)
+    for x in args:
+        for t in (x.k, x.v, x.k_scale, x.v_scale) if isinstance(x, KvCache) else (
+                x.pages, x.ctx_len, x.q_start) if isinstance(x, KvBatch) else (x,):
+            if isinstance(t, torch.Tensor) and t.is_cuda:
+                t.record_stream(stream)
+    with torch.cuda.stream(stream):
         made = fn(*args)
     for t in made if isinstance(made, tuple) else (made,):
         if t is not None and t.is_cuda:

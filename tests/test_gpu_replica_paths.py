@@ -226,3 +226,38 @@ def test_a_replica_looks_at_its_diag():
         with pytest.raises(error, match="step"):
             rep.serve([(0, 10, 2)])
         setattr(d, field, 0)
+
+
+def test_inputs_let_go_while_another_stream_reads_them():
+    """A query tensor that is dropped right after the call is not handed out again while the
+    other stream has still to read it."""
+    bt = ref.Batch([(3000, 1), (20, 160)], 16, 2, 64, torch.bfloat16, seed=37)
+    keep = torch.randn(bt.rows, 4, 64, device="cuda").bfloat16()
+    cache, batch = bt.cache(tre), bt.batch(tre)
+    want = tre.tre_chunk_attention(keep, cache, batch)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    big = torch.zeros(1 << 28, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        for _ in range(20):                 # `s` is busy for some milliseconds
+            big += 1
+    q = keep.clone()
+    torch.cuda.current_stream().synchronize()
+    got = tre.tre_chunk_attention(q, cache, batch, stream=s)
+    del q
+    others = [torch.full_like(keep, 3.0) for _ in range(8)]
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and len(others) == 8
+
+
+def test_first_call_on_a_stream_of_its_own():
+    """A process whose first call names a stream."""
+    import subprocess
+    import sys
+    code = ("import torch, paper_2609_29160_gb300 as tre; s = torch.cuda.Stream(); "
+            "q = torch.ones(3, 2, 64, device='cuda'); torch.cuda.synchronize(); "
+            "y, _ = tre.tre_qk_norm_rope(q, None, stream=s); s.synchronize(); "
+            "assert torch.equal(y, q)")
+    subprocess.run([sys.executable, "-c", code], check=True, timeout=300)
