@@ -724,7 +724,7 @@ struct Plan {
 // one new token's heads.
 constexpr int kFew = 64, kFewBeside = 16;
 
-Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page, int dim) {
+Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page, int dim, bool coded) {
   Plan p{};
   const int64_t max_new = std::max(1, b->max_new > 0 ? b->max_new : b->n_rows);
   const int64_t rows = max_new * a.group;
@@ -758,10 +758,14 @@ Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page, in
   if (p.tc) {
     // Parts are worth their join where there are fewer units than half the SMs (64, 256 and
     // 512 new tokens after 32,000, 32 heads on 8 of 128: 80, 135 and 209 us, whole contexts
-    // 342 to 350), two to six rounds of long ones (a part then evens out the last round:
-    // 4,096 tokens 1,407 us, 1,440 whole), or by the lengths known here a tenth less time
+    // 342 to 350), two to six rounds of long ones (a part then evens out the last round), or
+    // by the lengths known here a tenth less time
     // (1,280 and 1,536 tokens: 521 and 548 us, 666 and 675 whole; where it is less than
-    // that, the join's launch took 3 to 7% more). As many as 256 MB of partial sums allow,
+    // that, the join's launch took 3 to 7% more). Long: 2,500 to 7,200 tokens after 32,000 in
+    // bf16 took 9% less to 2% more in parts (4,096: 1,422 us, 1,458 whole), after 24,000 6% less
+    // to 4% more, after 16,000 1% less to 5% more, after 8,000 1 to 14% more; over codes, whose
+    // tiles take longer, 3,000 and 5,000 after 16,000 2 to 8% less, after 8,000 1% less to 2%
+    // more, after 4,000 1 to 4% more. As many as 256 MB of partial sums allow,
     // none shorter than 512 tokens; how many are taken is seen on the device, where all
     // lengths are known.
     const int64_t all = (int64_t)b->n_rows * a.group;
@@ -770,7 +774,7 @@ Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page, in
     const int64_t row = ((int64_t)dim * 4 + 8) * a.heads * std::max(b->n_rows, 1);
     const int64_t least = std::max<int64_t>(all - (int64_t)b->n_seq * p.few, 1) / kTcRows * heads;
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>({64, len / 512, (256ll << 20) / row}));
-    bool worth = 2 * least <= sms || (least >= 2 * sms && least <= 6 * sms && len >= 8192);
+    bool worth = 2 * least <= sms || (least >= 2 * sms && least <= 6 * sms && len >= (coded ? 12288 : 30000));
     if (!worth && least < 2 * sms)
       for (int64_t n = 2; n <= most; ++n)
         worth |= parts_time(n, tiles * heads, len, sms) <
@@ -853,7 +857,7 @@ extern "C" tre_status tre_chunk_attention(const tre_kv_cache* cache, const tre_k
   a.by_group = FastDiv31((uint32_t)a.group);
   a.window = at->window;
   Plan plan{};
-  if (b.n_seq > 0) plan = plan_of(batch, a, c.heads, c.page, cache->dim);
+  if (b.n_seq > 0) plan = plan_of(batch, a, c.heads, c.page, cache->dim, cache->dtype != at->dtype);
   Arena arena(ws);
   float *part_o[2] = {}, *part_ml[2] = {};
   int32_t* parts_taken = plan.parts[1] > 1 ? arena.take<int32_t>(1) : nullptr;
