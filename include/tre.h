@@ -35,10 +35,11 @@
  *     the device-resident `tre_diag` (added to, never reset by the library:
  *     zero it before the first call), valid after the stream is synchronised.
  *   - Layout of every per-window array is row-major [n_windows][n_models].
- *   - Floating-point results are computed in the profile's dtype with one
- *     correctly rounded IEEE operation per step and no fused multiply-add, in
- *     the same order as the sequential definitions; results are reproducible
- *     bit for bit.
+ *   - Floating-point results of scoring, calibration and replay are computed in
+ *     the profile's dtype with one correctly rounded IEEE operation per step and
+ *     no fused multiply-add, in the same order as the sequential definitions. The
+ *     calls of a replica's step are not: their roundings stand beside them.
+ *     All results are reproducible bit for bit.
  * Limits: 1 <= n_models <= 1024; window_ms >= 1; n_windows * window_ms < 2^31.
  */
 #ifndef TRE_H
@@ -505,9 +506,11 @@ tre_status tre_replay(const tre_grid* grid, const tre_latent* lat, const tre_pro
  *     tre_kv_append (or tre_qk_norm_rope without a cache), tre_chunk_attention;
  * tre_kv_read takes tokens out of a cache (to move a request to another replica).
  * No counterpart in the paper, whose replicas run an unmodified serving engine
- * (Sec. V). Sums, softmax statistics and norms are held in 32 bits; every result
- * is the same bit for bit when the same call is made again.
- * diag may be NULL in these calls.
+ * (Sec. V). Sums, softmax statistics and norms are held in 32 bits, with fused
+ * multiply-adds and the device's approximate exp2 and reciprocal square root; what
+ * has fewer bits is said at each call. Every result is the same bit for bit when
+ * the same call is made again. diag may be NULL in these calls; the errors and
+ * counts that they leave there are then lost.
  * ------------------------------------------------------------------------- */
 
 /* A paged cache: n_pages pages of `page` tokens of `heads` keys and values of
@@ -535,8 +538,8 @@ typedef struct {
  * goes for positions below zero or past max_pages pages. Rows of no sequence
  * (before q_start[0], from q_start[n_seq] on) give zeros and are not counted.
  * max_new, max_ctx: the longest sequence's new tokens and length, as far as the
- * host knows them, 0 where it does not; they set how work is split, not what is
- * computed. */
+ * host knows them, 0 where it does not; they set how work is split (and with it the
+ * order of sums), not what is computed. */
 typedef struct {
   int32_t n_seq, n_rows, max_new, max_ctx, max_pages;
   const int32_t* pages;
@@ -577,10 +580,11 @@ tre_status tre_qk_norm_rope(const tre_heads* heads, const int32_t* positions, tr
 
 /* tre_kv_append -- the new tokens' keys and values into the cache, keys (and the
  * queries, to q_out) normed and rotated at their own positions on the way; k_out
- * is not used. v: [n_rows][cache heads][dim], strides in elements. A cache of
+ * is not used. A row that is not written (no page, or a position that cos_sin does
+ * not hold) gets zeros for its queries. v: [n_rows][cache heads][dim], strides in elements. A cache of
  * codes gets scale = max|x| / 448 (e4m3) or / 127 (int8) of the 32-bit values of
- * each token and head, and x / scale rounded to nearest even; a row with a value
- * that is infinite or no number reads back as NaN. */
+ * each token and head, and x / scale rounded to nearest even, never past the last
+ * code; a row with a value that is infinite or no number reads back as NaN. */
 tre_status tre_kv_append(const tre_kv_cache* cache, const tre_kv_batch* batch,
                          const tre_heads* heads, const void* v, int64_t v_row, int64_t v_head,
                          tre_diag* diag, tre_stream stream);
@@ -612,8 +616,15 @@ typedef struct {
 /* tre_chunk_attention -- each new token's attention over its sequence up to and
  * including itself; the batch's rows are in the cache already. A row that sees no
  * position gives zeros and lse = -inf. Values at positions that a row does not
- * see do not reach it, whatever they hold. A wait on the device that does not end
- * in about two seconds gives up (diag.err = TRE_ETIMEOUT, outputs undefined). */
+ * see do not reach it, whatever they hold; infinities and NaN that it sees reach it
+ * in their own columns. Products have operands of 16 bits and sums of 32: weights
+ * are rounded for their product with values to halves over a cache of codes and to
+ * the queries' type over one of 16 bits (where a sequence has few rows over a
+ * bfloat16 cache, 16 significant bits of a weight are kept); their sum is taken
+ * before that. Over codes bfloat16 queries are multiplied as halves of their row's
+ * largest power of two, which cuts what is below 2^-24 of it. A wait on the device
+ * that does not end in about two seconds gives up (diag.err = TRE_ETIMEOUT, outputs
+ * undefined). */
 tre_status tre_chunk_attention(const tre_kv_cache* cache, const tre_kv_batch* batch,
                                const tre_attend* at, void* ws, size_t* ws_bytes,
                                tre_diag* diag, tre_stream stream);

@@ -17,8 +17,8 @@
 // the order in which a lane's 16-byte reads deliver them, which a sum does not see.
 //
 // Bound by HBM on 16-bit caches: one token of 96 requests of up to 16,000, 32 query heads
-// on 8 of 128, 297 us, 6.4 TB/s. On codes the widening takes half of the issue slots as
-// well: 8 requests of up to 120,000, 64 heads on 8, e4m3, 201 us, 5.6 TB/s.
+// on 8 of 128, 303 us, 6.3 TB/s. On codes the widening takes half of the issue slots as
+// well: 8 requests of up to 120,000, 64 heads on 8, e4m3, 202 us, 5.6 TB/s.
 #include <algorithm>
 
 #include "attend.cuh"
@@ -92,9 +92,11 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const BatchArg
   using S = Shape<CODE, DIM, NT>;
   using CT = typename std::conditional<CODE == Code::kHalf, T, __half>::type;
   constexpr int EPT = 16 / S::CB, SPB = EPT / 4, BLOCKS = DIM / (4 * EPT);
-  // Weights are rounded to 16 bits for their product with values. In bfloat16 that is 8
-  // significant bits, as coarse as the output's own rounding: what it leaves over is
-  // multiplied as well.
+  // Weights are rounded to 16 bits for their product with values, over codes and float16 to
+  // halves of 11 significant bits. In bfloat16 that is 8, as coarse as the output's own
+  // rounding (2.5e-3 off for 2 requests of up to 700, 1.7e-3 rounded once): what it leaves
+  // over is multiplied as well. That took 1% on long contexts, 5 to 17% where sequences
+  // have 16 to 64 rows.
   constexpr bool SPLIT = CODE == Code::kHalf && std::is_same<T, __nv_bfloat16>::value;
   extern __shared__ __align__(128) uint8_t sm[];
   __shared__ float w_m[kWarps][S::ROWS], w_l[kWarps][S::ROWS];
@@ -187,8 +189,8 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const BatchArg
     // The rows whose weights this lane holds: 2 cc and 2 cc + 1 of each eight.
     // Codes are multiplied as halves, which both kinds turn into in a step or two;
     // bfloat16 queries then go as halves too, each row divided by a power of two
-    // (its largest element's) that its scores get back: nothing within 2^-24 of the
-    // row's largest element is lost.
+    // (its largest element's) that its scores get back: what is below 2^-24 of that is
+    // cut.
     int pos[NT][2];
     float back[NT][2];
 #pragma unroll
@@ -716,12 +718,14 @@ struct Plan {
 
 // Which kernel takes a sequence, by its rows. k_attend reads keys and values once for 8 or
 // 16 rows (again from L2 for the next), k_attend_tc takes 128 rows in the time of one:
-// 32 sequences of 1,500 to 4,000 tokens, dim 128, took 72, 82 and 124 us with up to 16, 32
-// and 64 rows each in k_attend and 102 to 105 in k_attend_tc; 4 of 25,000 over e4m3 68, 72
-// and 112 against 185. So batches of up to 64 rows a sequence are k_attend's alone. Where
-// k_attend_tc runs in any case, sequences of more than 16 rows are its (at up to 64 in
-// k_attend chunks of up to 128 rows took 250 us, all of them in k_attend_tc 107), except
-// one new token's heads.
+// Batches of up to 64 rows a sequence are k_attend's alone: with 32, 48 and 64 rows each
+// (bf16, k_attend against k_attend_tc) 4 sequences of 6,000 to 12,000 tokens, dim 128, took 38,
+// 58 and 60 us against 70 to 74; 64 of 500 to 2,000, dim 64, 50, 60 and 72 against 81 to 99; 100
+// of up to 1,000, dim 128, 42, 47 and 52 against 54 to 58; 4 of 25,000 over e4m3 72, - and 112
+// against 175. Only 32 of 1,500 to 4,000, dim 128, were the other way from 48 rows on (90, 115
+// and 139 against 112 to 100). Where k_attend_tc runs in any case, sequences of more than 16
+// rows are its (at up to 64 in k_attend chunks of up to 128 rows took 250 us, all of them in
+// k_attend_tc 107), except one new token's heads.
 constexpr int kFew = 64, kFewBeside = 16;
 
 Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page, int dim, bool coded) {
@@ -742,7 +746,8 @@ Plan plan_of(const tre_kv_batch* b, const AttendArgs& a, int heads, int page, in
     // Tiles of 8 rows where one new token's heads (or all rows there are) fit in one (16
     // took 235 for 205 us over e4m3, 8 requests of up to 120,000, and 308 for 300 over
     // bf16), else of 16, which read keys and values once for twice the rows (82 us with
-    // 8, 72 with 16 for the 16 rows, 167 and 124 for the 64 rows above).
+    // 8, 72 with 16 for 16 rows of 32 sequences of 1,500 to 4,000, 167 and 124 for 64 rows;
+    // both before bfloat16 weights were multiplied in two halves, now 75 and 139).
     p.nt = (p.tc ? a.group : rows) <= 8 ? 1 : 2;
     p.row_tiles = p.tc ? 1 : (int)std::min<int64_t>((rows + 8 * p.nt - 1) / (8 * p.nt), 1 << 20);
     const int64_t units = std::max<int64_t>(1, (int64_t)b->n_seq * heads * p.row_tiles);

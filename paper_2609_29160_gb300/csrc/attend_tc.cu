@@ -7,7 +7,8 @@
 // tiles of 128 rows against a part of the context, 128 positions at a time:
 //
 //   S = Q K^T       both operands in shared memory, S (128 x 128, float) in TMEM
-//   P = exp2(S - m) S out of TMEM, P back over it in 16 bits
+//   P = exp2(S - m) S out of TMEM, P back over it in 16 bits (a product's operand has no
+//                   more; a second one for the rest would be half of the products again)
 //   O += P V        P from TMEM, V from shared memory, O (128 x dim, float) in TMEM
 //
 // While one tile's warps take exponentials the tensor cores multiply for the other.
@@ -24,13 +25,15 @@
 // come into a ring of their own and are widened to halves there, in which both kinds are
 // exact; the scales go into the scores and weights instead). Warp 11 issues the products.
 //
-// 4,096 new tokens after 32,000, 32 heads on 8 of 128, bf16: 1.40 ms in a loop, 1.6
+// 4,096 new tokens after 32,000, 32 heads on 8 of 128, bf16: 1.39 ms in a loop, 1.6
 // PFLOP/s; the tensor pipe is busy three quarters of the time, the rest are its operands'
 // reads from shared memory and the start of each unit. Dim 64 has half the products for
 // the same exponentials: there the chain of a row binds (scores out of TMEM, maximum,
 // 128 exponentials, weights back: some 2,600 cycles a tile, and 6,000 to start and end a
 // unit): 24 prompts of up to 2,000, 16 heads, f16, 123 us. Two threads a row spill at the
-// registers that are then left and took twice the time.
+// registers that are then left and took twice the time. Over codes the copy warps' lookups
+// and widening bind: 2,048 tokens after 8,000, 32 heads on 8 of 128, 209 us over bf16, 460
+// over e4m3, 525 over int8.
 #include <cuda.h>
 
 #include <algorithm>
@@ -607,7 +610,7 @@ k_attend_tc(AttendArgs a, BatchArgs b, CacheArgs c, const __grid_constant__ Maps
     auto q_store = [&](uint4* v) {
       if constexpr (L::CODED && !std::is_same<T, CT>::value) {
         // bfloat16 queries as halves, each row divided by the power of two of its largest
-        // element (nothing within 2^-24 of that is lost); its scores get it back
+        // element (what is below 2^-24 of that is cut); its scores get it back
 #pragma unroll
         for (int k = 0; k < QS; ++k) {
           float y[8], top = 0.f;

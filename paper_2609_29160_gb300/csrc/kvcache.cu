@@ -9,15 +9,17 @@
 // division is the exact one, so codes do not depend on how a row is reached. A warp
 // takes a whole token where there are many: its place in the cache, cosines and sines
 // are fetched once for all heads. Bound by HBM when rows are many and wide: 40,013 tokens
-// of 32 heads of 64 floats 106 us, 6.2 TB/s. With 16-bit rows and codes the instructions
-// bind: 12 chunks of up to 4,001 tokens, 48 heads of 64, f16 into int8, 93 us, 4.1 TB/s,
-// three of four issue slots taken (exact divisions, packing). By the chain q_start ->
+// of 32 heads of 64 floats 106 us, 6.2 TB/s; of bfloat16, half the bytes, 63 us, 5.3 TB/s;
+// 12 chunks of up to 4,001 tokens, 48 heads of 64, f16 into an f16 cache 51 us, 5.5 TB/s.
+// Into codes the instructions bind: the same chunks into int8 68 us, 3.5 TB/s, three of
+// four issue slots taken (exact divisions, packing). By the chain q_start ->
 // lengths -> page -> store when there are few: one token of 64 requests is a few us on
 // the device, less than what its call costs the host.
 //
 // k_read: codes (and scales) of whole tokens back to rows of a model's type, bound by
 // HBM: 16 contexts of up to 50,000 tokens, e4m3 to bf16, 138 us, 6.6 TB/s (159 us with
-// 16-byte stores; 32-byte ones where the outputs' boundaries allow).
+// 16-byte stores; 32-byte ones where the outputs' boundaries allow). The 12 chunks above
+// out of codes 27 us, 5.3 TB/s, out of f16 34 us, 5.6.
 #include <algorithm>
 #include <type_traits>
 
@@ -444,9 +446,9 @@ bool heads_args(const tre_heads* h, bool keys_out, HeadsArgs& a) {
 
 // A warp takes a whole token's heads when that leaves every SM 32 warps (its place and
 // its rotation are then fetched once for all of them), else as few as still does. One step
-// a warp took 184 us for 40,013 tokens of 32 heads (106 so) and 178 for the f16 -> int8
-// chunks above (93); whole tokens always are the same there and 39.0 against 36.4 us a
-// call for one token of 64 requests.
+// a warp took 184 us for 40,013 tokens of 32 heads (106 so) and 178 for appending the
+// f16 -> int8 chunks above and reading them back (93); whole tokens always are the same
+// there and 39.0 against 36.4 us for both calls of one token of 64 requests.
 template <class T, Code CODE, int D>
 cudaError_t launch_heads(const HeadsArgs& a, const BatchArgs& b, const CacheArgs& c,
                          tre_diag* diag, cudaStream_t s) {
