@@ -18,7 +18,8 @@
  *     and a scoring entry point that needs no workspace,
  *   - and what a replica of a served model runs on this GPU for each batch of new
  *     tokens: norms and rotation of heads, a paged cache (quantised or not) and
- *     attention over it.
+ *     attention over it; norms around blocks, products with 4-bit weights, routing
+ *     to experts and the experts' products.
  *
  * Conventions (every entry point):
  *   - Array arguments are DEVICE pointers owned by the caller, unless a field
@@ -628,6 +629,141 @@ typedef struct {
 tre_status tre_chunk_attention(const tre_kv_cache* cache, const tre_kv_batch* batch,
                                const tre_attend* at, void* ws, size_t* ws_bytes,
                                tre_diag* diag, tre_stream stream);
+
+/* ---------------------------------------------------------------------------
+ * The rest of a replica's layer: what stands between the attention of one layer
+ * and that of the next. A dense layer is
+ *     tre_block_norm, tre_linear4 (gated), tre_linear4, tre_block_norm,
+ * one of experts
+ *     tre_block_norm, tre_route, tre_experts, tre_block_norm,
+ * and the attention's own projections are tre_linear4 too. What was said of a
+ * replica's step holds here: 32-bit sums and norms, roundings beside each call,
+ * the same bits when the same call is made again, diag may be NULL.
+ * ------------------------------------------------------------------------- */
+
+/* The rows between two blocks. dtype (TRE_BF16, TRE_F16, TRE_F32): y, gate, out;
+ * stream_dtype (TRE_F32 or dtype): residual, residual_out; weight_dtype (TRE_F32 or
+ * dtype): post_weight, weight. Rows of dim elements (1 to 16384), strides in
+ * elements, last axis dense; any address and stride that an element of the type
+ * may have (rows on 16-byte boundaries, with a dim that 8 divides, are read wider).
+ *   y'           = y / sqrt(mean y^2 + eps) * post_weight   (post_weight NULL: y)
+ *   r            = residual + scale * gate * y'              (y NULL: residual)
+ *   residual_out = r                                         (NULL: not written)
+ *   out          = r / sqrt(mean r^2 + eps) * weight         (out NULL: not written)
+ * gate (NULL: 1) of row t, element i: gate[t * gate_row + i * gate_col]; gate_col
+ * is 0 or 1. out is computed from the 32-bit r, not from its rounding. residual_out
+ * may be residual and out may be y, with the same strides; no other overlap. */
+typedef struct {
+  tre_dtype dtype, stream_dtype, weight_dtype;
+  int32_t n_rows, dim;
+  const void* residual;
+  int64_t residual_row;
+  const void* y;
+  int64_t y_row;
+  const void* post_weight;
+  const void* gate;
+  int64_t gate_row, gate_col;
+  float scale, eps;
+  const void* weight;
+  void* residual_out;
+  int64_t residual_out_row;
+  void* out;
+  int64_t out_row;
+} tre_block_rows;
+
+/* tre_block_norm -- a block's output into the residual stream, and the stream
+ * normed for the next block, in one pass. */
+tre_status tre_block_norm(const tre_block_rows* rows, tre_stream stream);
+
+/* Routing of n_rows tokens to `top` (1 to 32) of `experts` (at most 1024).
+ * logits: [n_rows][experts] of dtype (TRE_F32, TRE_BF16, TRE_F16), row stride in
+ * elements. An expert whose logit is -inf or NaN is not there for that token; a
+ * logit of +inf counts as the largest float.
+ *   s = exp(l) / sum over the experts there of exp(l)   (TRE_SOFTMAX)
+ *   s = 1 / (1 + exp(-l))                               (TRE_SIGMOID)
+ *   c = s + bias[expert]                                (bias NULL: c = s)
+ * The experts stand in `groups` groups of neighbours (a divisor of experts, at most
+ * 32); a group counts as the sum of its group_best (1 or 2) largest c, and the
+ * top_groups best groups stay. ids [n_rows][top]: the experts with the largest c
+ * in them, largest first, -1 where fewer are there (an expert whose c is -inf or
+ * NaN is not); weights [n_rows][top] float: their s (of c only the choice depends
+ * on the bias), divided by their sum if renorm, times scale; 0 beside an id of -1.
+ * Ties go to the lower index. Choices are those of the formulas in 64 bits or more,
+ * weights are computed in 32. */
+typedef enum { TRE_SOFTMAX = 0, TRE_SIGMOID = 1 } tre_scores;
+typedef struct {
+  tre_dtype dtype;
+  int32_t n_rows, experts, top;
+  const void* logits;
+  int64_t logits_row;
+  tre_scores scores;
+  const float* bias;
+  int32_t groups, top_groups, group_best, renorm;
+  float scale;
+  int32_t* ids;
+  float* weights;
+} tre_router;
+
+tre_status tre_route(const tre_router* router, tre_stream stream);
+
+/* Matrices in 4 bits as they come: for each of `experts` matrices (1 for a plain
+ * one) codes [n][k/2], two a byte, the lower half first; scales [n][k/group] of
+ * dtype (TRE_BF16, TRE_F16: the type of the rows that it will be multiplied with);
+ * zeros [n][k/group] bytes of 0 to 15, NULL: 8. An element is (code - zero) * scale.
+ * group is 32, 64 or 128 and divides k. gated (n even): rows 0 to n/2-1 are a
+ * gate's, the others what it multiplies. All dense; codes on a 4-byte boundary. */
+typedef struct {
+  tre_dtype dtype;
+  int32_t experts, n, k, group, gated;
+  const uint8_t* codes;
+  const void* scales;
+  const uint8_t* zeros;
+} tre_w4_source;
+
+/* The same laid out for the products, once, by tre_w4_pack. */
+typedef struct {
+  tre_dtype dtype;
+  int32_t experts, n, k, group, gated, zeros;   /* zeros: whether it has any */
+  const void* packed;
+} tre_w4;
+
+/* tre_w4_pack -- lays matrices out at `packed` (a 256-byte boundary). packed ==
+ * NULL: the size needed is written to *bytes, nothing is done. */
+tre_status tre_w4_pack(const tre_w4_source* from, void* packed, size_t* bytes, tre_stream stream);
+
+/* tre_linear4 -- y = x W^T for rows x [n_rows][k] of w's dtype; of a gated w
+ * y = g / (1 + exp(-g)) * u with g and u the two halves of x W^T, n/2 wide. w has one
+ * matrix. x on 16-byte boundaries (strides in elements, a multiple of 8 for x).
+ * Codes less their zeros are whole numbers that 16 bits hold: products are exact,
+ * sums of a group are 32-bit, and so are scales; y is rounded once. How sums are
+ * split depends on n_rows. A wait on the device that does not end in about two
+ * seconds gives up (diag.err = TRE_ETIMEOUT, outputs undefined). */
+tre_status tre_linear4(const tre_w4* w, int32_t n_rows, const void* x, int64_t x_row, void* y,
+                       int64_t y_row, tre_diag* diag, tre_stream stream);
+
+/* Tokens of tre_experts: x [n_rows][k] of dtype and y [n_rows][n of the second
+ * matrices]; strides in elements, x's address and stride multiples of 16 bytes. ids,
+ * weights: [n_rows][top] (dense). */
+typedef struct {
+  tre_dtype dtype;
+  int32_t n_rows, top;
+  const void* x;
+  int64_t x_row;
+  const int32_t* ids;
+  const float* weights;
+  void* y;
+  int64_t y_row;
+} tre_tokens;
+
+/* tre_experts -- each token through its own experts' gated feed-forward layers:
+ *   y[t] = sum over j of weights[t][j] * W2[e] act(W1[e] x[t]),  e = ids[t][j],
+ * with w1 gated and act as in tre_linear4. An id below zero adds nothing; one past
+ * the last expert adds nothing and is counted in diag.dropped_range; a token
+ * without experts gives zeros. The same expert may come twice. act's output is
+ * rounded to dtype (an operand of the second product has no more bits), each
+ * expert's output to dtype where there are many tokens, y once. */
+tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* tokens, void* ws,
+                       size_t* ws_bytes, tre_diag* diag, tre_stream stream);
 
 /* Kernel-phase tracing (host side, not thread safe). While enabled, every
  * kernel phase an entry point enqueues is bracketed by a pair of CUDA events

@@ -154,6 +154,7 @@ def load(build_if_missing: bool = True):
                                C.POINTER(ReplayOut), P, C.POINTER(C.c_size_t), P, P]
     lib.tre_replay.restype = C.c_int
     replica.declare(lib)
+    layer.declare(lib)
     lib.tre_status_str.argtypes = [C.c_int]
     lib.tre_status_str.restype = C.c_char_p
     _lib = lib
@@ -834,3 +835,5 @@ def tre_replay(latent, M, window_ms, K, profile, budget, r0, r_min, footprint, *
 from . import replica  # noqa: E402  (it uses the helpers above)
 from .replica import (KvBatch, KvCache, check_replica, replica_diag,  # noqa: E402,F401
                       tre_chunk_attention, tre_kv_append, tre_kv_read, tre_qk_norm_rope)
+from . import layer  # noqa: E402
+from .layer import Weights4, tre_block_norm, tre_experts, tre_linear4, tre_route  # noqa: E402,F401

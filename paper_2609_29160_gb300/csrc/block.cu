@@ -1,0 +1,490 @@
+// The rows between two blocks of a layer: residual, gate, norms; and the choice of
+// experts.
+#include <algorithm>
+
+#include "internal.h"
+#include "kvcache.cuh"
+
+namespace tre {
+namespace {
+
+// ---------------------------------------------------------------------------
+// Norms around a block.
+//
+// One pass: a row's elements of y and of the residual stay in registers between the two
+// sums (mean of squares of y, where there is a post norm, and of r), so that each input is
+// read once and each output written once. Bound by HBM where there are rows enough.
+// ---------------------------------------------------------------------------
+struct BlockArgs {
+  const uint8_t *residual, *y, *post_weight, *gate, *weight;
+  uint8_t *residual_out, *out;
+  int64_t residual_row, y_row, gate_row, gate_col, residual_out_row, out_row;
+  int32_t n_rows, dim, per_row;        // per_row: threads of a row
+  float scale, eps;
+  bool weight_f32;
+};
+
+template <class T> __device__ __forceinline__ void get8(const T* p, float* x) {
+  if constexpr (sizeof(T) == 4) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
+    x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  } else {
+    Vec<T>::get(*reinterpret_cast<const uint4*>(p), x);
+  }
+}
+template <class T> __device__ __forceinline__ void put8(T* p, const float* x) {
+  if constexpr (sizeof(T) == 4) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+  } else {
+    *reinterpret_cast<uint4*>(p) = Vec<T>::put(x);
+  }
+}
+
+// A thread's elements of a row: V times eight, next to each other with WIDE, else a row's
+// threads apart.
+template <int V, bool WIDE> struct Mine {
+  int t, step, dim;
+  __device__ __forceinline__ int at(int v, int e) const {
+    return WIDE ? (v * step + t) * 8 + e : (v * 8 + e) * step + t;
+  }
+  template <class T> __device__ __forceinline__ void get(const T* p, float* x) const {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if constexpr (WIDE) {
+        if (at(v, 0) < dim) get8(p + at(v, 0), x + 8 * v);
+        else
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[8 * v + e] = 0.f;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[8 * v + e] = at(v, e) < dim ? (float)p[at(v, e)] : 0.f;
+      }
+    }
+  }
+  template <class T> __device__ __forceinline__ void put(T* p, const float* x) const {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if constexpr (WIDE) {
+        if (at(v, 0) < dim) put8(p + at(v, 0), x + 8 * v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (at(v, e) < dim) p[at(v, e)] = T(x[8 * v + e]);
+      }
+    }
+  }
+};
+
+// Sum over a row's threads (a warp, or the whole block). `part`: a warp's place each.
+__device__ __forceinline__ float row_sum(float x, bool block, float* part) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  if (!block) return x;
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = x;
+  __syncthreads();
+  const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+  x = lane < warps ? part[lane] : 0.f;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+
+template <class T, int N, class M>
+__device__ __forceinline__ void times_weight(const BlockArgs& a, const uint8_t* w, const M& mine,
+                                             float by, float* x) {
+  float f[N];
+  if (a.weight_f32) mine.get(reinterpret_cast<const float*>(w), f);
+  else mine.get(reinterpret_cast<const T*>(w), f);
+#pragma unroll
+  for (int e = 0; e < N; ++e) x[e] = x[e] * by * f[e];
+}
+
+template <class T, class S, int V, bool WIDE>
+__global__ void __launch_bounds__(512) k_block_norm(const __grid_constant__ BlockArgs a) {
+  constexpr int N = 8 * V;
+  __shared__ float part[2][32];
+  const bool block = a.per_row > 32;
+  const int64_t row = block ? blockIdx.x : (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  if (row >= a.n_rows) return;                       // (whole warps, of rows of their own)
+  const Mine<V, WIDE> mine{block ? (int)threadIdx.x : (int)(threadIdx.x & 31), a.per_row, a.dim};
+  float r[N];
+  mine.get(reinterpret_cast<const S*>(a.residual) + row * a.residual_row, r);
+  if (a.y) {
+    float y[N];
+    mine.get(reinterpret_cast<const T*>(a.y) + row * a.y_row, y);
+    if (a.post_weight) {
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < N; ++e) sum = fmaf(y[e], y[e], sum);
+      sum = row_sum(sum, block, part[0]);
+      times_weight<T, N>(a, a.post_weight, mine, rsqrtf(sum / a.dim + a.eps), y);
+    }
+    if (a.gate) {
+      const T* g = reinterpret_cast<const T*>(a.gate) + row * a.gate_row;
+      if (a.gate_col) {
+        float f[N];
+        mine.get(g, f);
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] *= f[e];
+      } else {
+        const float f = (float)*g;
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] *= f;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) r[e] = fmaf(a.scale, y[e], r[e]);
+  }
+  if (a.residual_out) mine.put(reinterpret_cast<S*>(a.residual_out) + row * a.residual_out_row, r);
+  if (!a.out) return;
+  float sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < N; ++e) sum = fmaf(r[e], r[e], sum);
+  sum = row_sum(sum, block, part[1]);
+  times_weight<T, N>(a, a.weight, mine, rsqrtf(sum / a.dim + a.eps), r);
+  mine.put(reinterpret_cast<T*>(a.out) + row * a.out_row, r);
+}
+
+constexpr int kMaxDim = 16384;
+
+template <class T, class S, bool WIDE>
+cudaError_t launch_norm(BlockArgs a, cudaStream_t s) {
+  const int eights = (a.dim + 7) / 8;
+  const int v = eights <= 32 ? 1 : eights <= 64 ? 2 : eights <= 128 ? 4 : eights <= 512 ? 1 : eights <= 1024 ? 2 : 4;
+  a.per_row = ((eights + v - 1) / v + 31) / 32 * 32;
+  const bool block = a.per_row > 32;
+  const int threads = block ? a.per_row : 128;
+  const int64_t blocks = block ? a.n_rows : ((int64_t)a.n_rows + 3) / 4;
+  const unsigned grid = (unsigned)blocks;
+  if (v == 1) k_block_norm<T, S, 1, WIDE><<<grid, threads, 0, s>>>(a);
+  else if (v == 2) k_block_norm<T, S, 2, WIDE><<<grid, threads, 0, s>>>(a);
+  else k_block_norm<T, S, 4, WIDE><<<grid, threads, 0, s>>>(a);
+  return cudaGetLastError();
+}
+
+template <class T, class S>
+cudaError_t launch_norm(const BlockArgs& a, bool wide, cudaStream_t s) {
+  return wide ? launch_norm<T, S, true>(a, s) : launch_norm<T, S, false>(a, s);
+}
+
+int float_size(int d) { return d == TRE_F32 ? 4 : d == TRE_BF16 || d == TRE_F16 ? 2 : 0; }
+bool on(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+// ---------------------------------------------------------------------------
+// Routing.
+//
+// A warp a token, a lane every 32nd expert. Choices have to be those of the formulas, not of
+// their rounding, because one other expert is another answer. Where c grows with the logit
+// (no bias, no sums) the logits themselves are compared. Else c is computed in 32 bits, and
+// a row whose choice is closer than that can tell (a chosen one against the next, a kept
+// group against one that is not) is done once more in 64 bits, whose pipe is some sixty
+// times slower; about one row in three hundred of 256 sigmoid scores.
+// ---------------------------------------------------------------------------
+struct RouteArgs {
+  const uint8_t* logits;
+  const float* bias;
+  int32_t* ids;
+  float* weights;
+  int64_t row;
+  int32_t dtype, n_rows, experts, top, groups, per, top_groups, group_best;
+  FastDiv31 by_per;
+  float scale;
+  bool softmax, renorm, raw;          // raw: choices by the logits
+};
+
+constexpr int kRouteWarps = 4;
+
+__device__ __forceinline__ float logit(const RouteArgs& a, int64_t row, int e) {
+  const int64_t at = row * a.row + e;
+  float x;
+  if (a.dtype == TRE_F32) x = reinterpret_cast<const float*>(a.logits)[at];
+  else if (a.dtype == TRE_BF16) x = (float)reinterpret_cast<const __nv_bfloat16*>(a.logits)[at];
+  else x = (float)reinterpret_cast<const __half*>(a.logits)[at];
+  return x != x ? -INFINITY : fminf(x, 3.402823466e38f);
+}
+
+// Larger floats have larger keys; -inf is the least of those used.
+__device__ __forceinline__ uint32_t order(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t key) {
+  return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
+}
+// Largest value of the lanes, and the least index that has it.
+__device__ __forceinline__ float warp_best(float x, int& at) {
+  const uint32_t key = order(x + 0.f);                // (-0 counts as 0)
+  const uint32_t top = __reduce_max_sync(0xffffffffu, key);
+  at = (int)__reduce_min_sync(0xffffffffu, key == top ? (uint32_t)at : 0x7fffffffu);
+  return value_of(top);
+}
+__device__ __forceinline__ double warp_best(double x, int& at) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const double y = __shfl_xor_sync(0xffffffffu, x, o);
+    const int b = __shfl_xor_sync(0xffffffffu, at, o);
+    if (y > x || (y == x && b < at)) {
+      x = y;
+      at = b;
+    }
+  }
+  return x;
+}
+template <class F> __device__ __forceinline__ F warp_sum(F x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+__device__ __forceinline__ float exp_of(float x) { return expf(x); }
+__device__ __forceinline__ double exp_of(double x) { return exp(x); }
+
+// Chooses: lane i's return is the i-th expert (-1: none). `close`: whether 32 bits may have
+// decided what they cannot tell. c of a sigmoid is off by at most two units of 2^-24 for the
+// exponential, the sum and the quotient each, and the bias adds half a unit of c; a softmax's
+// sum of up to 1,024 terms adds a unit for each of its 10 levels. Both sides of a comparison.
+template <class F, int NV>
+__device__ __forceinline__ int choose(const RouteArgs& a, const float* l, float most, F* room,
+                                      bool& close) {
+  const int lane = threadIdx.x & 31;
+  const F none = -(F)INFINITY;
+  F c[NV];
+  F total = 1;
+  if (a.softmax && !a.raw) {
+    F sum = 0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) sum += l[j] > -INFINITY ? exp_of((F)l[j] - (F)most) : (F)0;
+    total = warp_sum(sum);
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    c[j] = none;
+    if (!(l[j] > -INFINITY)) continue;
+    if (a.raw) {
+      c[j] = (F)l[j];
+    } else {
+      c[j] = a.softmax ? exp_of((F)l[j] - (F)most) / total : (F)1 / ((F)1 + exp_of(-(F)l[j]));
+      if (a.bias) c[j] += (F)a.bias[j * 32 + lane];
+      if (!(c[j] > none)) c[j] = none;
+    }
+  }
+  const F off = a.raw || sizeof(F) == 8 ? (F)0 : a.softmax ? (F)2.5e-6 : (F)6e-7;
+  const F rel = off > 0 ? (F)2.5e-7 : (F)0;
+  close = false;
+  if (a.groups > 1) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (j * 32 + lane < a.experts) room[j * 32 + lane] = c[j];
+    __syncwarp();
+    F first = none, second = none;
+    if (lane < a.groups) {
+      int i = lane % a.per;                          // (lanes start apart: their banks)
+      for (int n = 0; n < a.per; ++n) {
+        const F x = room[lane * a.per + i];
+        if (x > first) {
+          second = first;
+          first = x;
+        } else if (x > second) {
+          second = x;
+        }
+        if (++i == a.per) i = 0;
+      }
+      if (a.group_best == 2 && second > none) first += second;
+    }
+    __syncwarp();
+    int better = 0;
+    F under = none;                                  // the best group below this one
+    for (int g = 0; g < a.groups; ++g) {
+      const F x = __shfl_sync(0xffffffffu, first, g);
+      if (x > first || (x == first && g < lane)) ++better;
+      else if (g != lane && x > under) under = x;
+    }
+    const unsigned kept = __ballot_sync(0xffffffffu, lane < a.groups && better < a.top_groups);
+    if (off > 0)
+      close = __any_sync(0xffffffffu, lane < a.groups && better == a.top_groups - 1 && under > none &&
+                                          !(first - under > 2 * off + rel * (fabsf((float)first) + 1)));
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (j * 32 + lane < a.experts && !(kept >> a.by_per.div(j * 32 + lane) & 1)) c[j] = none;
+  }
+  int mine = -1;
+  F before = 0;
+  const int look = a.top + (off > 0 ? 1 : 0);
+  for (int k = 0; k < look; ++k) {
+    F best = none;
+    int at = 0x7fffffff;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (c[j] > best) {
+        best = c[j];
+        at = j * 32 + lane;
+      }
+    best = warp_best(best, at);
+    if (!(best > none)) break;
+    if (off > 0 && k > 0 && !(before - best > off + rel * fabsf((float)best))) close = true;
+    before = best;
+    if (lane == k && k < a.top) mine = at;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (j * 32 + lane == at) c[j] = none;
+  }
+  return mine;
+}
+
+template <int NV>
+__global__ void __launch_bounds__(kRouteWarps * 32) k_route(const __grid_constant__ RouteArgs a) {
+  extern __shared__ double room_all[];               // [warps][experts], with groups
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t row = (int64_t)blockIdx.x * kRouteWarps + warp;
+  if (row >= a.n_rows) return;
+  double* room = room_all + warp * a.experts;
+  float l[NV], most = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    l[j] = j * 32 + lane < a.experts ? logit(a, row, j * 32 + lane) : -INFINITY;
+    most = fmaxf(most, l[j]);
+  }
+  most = value_of(__reduce_max_sync(0xffffffffu, order(most)));
+  bool close;
+  int id = choose<float, NV>(a, l, most, reinterpret_cast<float*>(room), close);
+  if (close) id = choose<double, NV>(a, l, most, room, close);
+  const float x = id >= 0 ? logit(a, row, id) : -INFINITY;
+  // Weights; with their sum divided out a sigmoid's are kept from running out of exponent
+  // by the largest of them.
+  float w = 0.f;
+  if (a.renorm) {
+    const float top = value_of(__reduce_max_sync(0xffffffffu, order(x)));
+    if (id >= 0) {
+      if (a.softmax) w = expf(x - top);
+      else w = x >= 0.f ? 1.f / (1.f + expf(-x)) : expf(x - fminf(top, 0.f)) / (1.f + expf(x));
+    }
+    const float sum = warp_sum(w);
+    if (id >= 0) w = w / sum * a.scale;
+  } else if (a.softmax) {
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) sum += l[j] > -INFINITY ? expf(l[j] - most) : 0.f;
+    sum = warp_sum(sum);
+    if (id >= 0) w = expf(x - most) / sum * a.scale;
+  } else if (id >= 0) {
+    w = 1.f / (1.f + expf(-x)) * a.scale;
+  }
+  if (lane < a.top) {
+    a.ids[row * a.top + lane] = id;
+    a.weights[row * a.top + lane] = w;
+  }
+}
+
+template <int NV> cudaError_t launch_route(const RouteArgs& a, cudaStream_t s) {
+  const int64_t blocks = ((int64_t)a.n_rows + kRouteWarps - 1) / kRouteWarps;
+  const size_t room = a.groups > 1 ? sizeof(double) * kRouteWarps * a.experts : 0;
+  k_route<NV><<<(unsigned)blocks, kRouteWarps * 32, room, s>>>(a);
+  return cudaGetLastError();
+}
+
+}  // namespace
+}  // namespace tre
+
+using namespace tre;
+
+extern "C" {
+
+tre_status tre_block_norm(const tre_block_rows* b, tre_stream stream) {
+  if (!b || b->n_rows < 0 || b->dim < 1 || b->dim > kMaxDim) return TRE_EINVAL;
+  const int el = float_size(b->dtype), st = float_size(b->stream_dtype);
+  if (!el || (b->stream_dtype != TRE_F32 && b->stream_dtype != b->dtype)) return TRE_EINVAL;
+  if (b->weight_dtype != TRE_F32 && b->weight_dtype != b->dtype) return TRE_EINVAL;
+  const int wt = float_size(b->weight_dtype);
+  if (!(b->eps >= 0.f) || b->eps > 3e38f || !(b->scale >= -3e38f && b->scale <= 3e38f))
+    return TRE_EINVAL;
+  if (b->gate_col != 0 && b->gate_col != 1) return TRE_EINVAL;
+  if (!b->y && (b->post_weight || b->gate)) return TRE_EINVAL;
+  if ((b->out && !b->weight) || (!b->out && !b->residual_out)) return TRE_EINVAL;
+  if (!on(b->residual, st) || !on(b->residual_out, st) || !on(b->y, el) || !on(b->gate, el) ||
+      !on(b->out, el) || !on(b->post_weight, wt) || !on(b->weight, wt))
+    return TRE_EINVAL;
+  if (b->n_rows == 0) return TRE_OK;
+  if (!b->residual) return TRE_EINVAL;
+  BlockArgs a;
+  a.residual = static_cast<const uint8_t*>(b->residual);
+  a.y = static_cast<const uint8_t*>(b->y);
+  a.post_weight = static_cast<const uint8_t*>(b->post_weight);
+  a.gate = static_cast<const uint8_t*>(b->gate);
+  a.weight = static_cast<const uint8_t*>(b->weight);
+  a.residual_out = static_cast<uint8_t*>(b->residual_out);
+  a.out = static_cast<uint8_t*>(b->out);
+  a.residual_row = b->residual_row;
+  a.y_row = b->y_row;
+  a.gate_row = b->gate_row;
+  a.gate_col = b->gate_col;
+  a.residual_out_row = b->residual_out_row;
+  a.out_row = b->out_row;
+  a.n_rows = b->n_rows;
+  a.dim = b->dim;
+  a.scale = b->scale;
+  a.eps = b->eps;
+  a.weight_f32 = b->weight_dtype == TRE_F32;
+  const bool wide =
+      b->dim % 8 == 0 && on(b->residual, 16) && on(b->y, 16) && on(b->residual_out, 16) &&
+      on(b->out, 16) && on(b->post_weight, 16) && on(b->weight, 16) &&
+      b->residual_row * st % 16 == 0 && (!b->y || b->y_row * el % 16 == 0) &&
+      (!b->residual_out || b->residual_out_row * st % 16 == 0) &&
+      (!b->out || b->out_row * el % 16 == 0) &&
+      (!b->gate || !b->gate_col || (on(b->gate, 16) && b->gate_row * el % 16 == 0));
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  if (b->dtype == TRE_F32) e = launch_norm<float, float>(a, wide, s);
+  else if (b->dtype == TRE_BF16)
+    e = b->stream_dtype == TRE_F32 ? launch_norm<__nv_bfloat16, float>(a, wide, s)
+                                   : launch_norm<__nv_bfloat16, __nv_bfloat16>(a, wide, s);
+  else
+    e = b->stream_dtype == TRE_F32 ? launch_norm<__half, float>(a, wide, s)
+                                   : launch_norm<__half, __half>(a, wide, s);
+  return e == cudaSuccess ? TRE_OK : TRE_ECUDA;
+}
+
+tre_status tre_route(const tre_router* r, tre_stream stream) {
+  if (!r || r->n_rows < 0 || r->experts < 1 || r->experts > 1024) return TRE_EINVAL;
+  const int el = float_size(r->dtype);
+  if (!el || !on(r->logits, el)) return TRE_EINVAL;
+  if (r->top < 1 || r->top > 32 || r->top > r->experts) return TRE_EINVAL;
+  if (r->scores != TRE_SOFTMAX && r->scores != TRE_SIGMOID) return TRE_EINVAL;
+  if (r->groups < 1 || r->groups > 32 || r->experts % r->groups || r->top_groups < 1 ||
+      r->top_groups > r->groups || r->group_best < 1 || r->group_best > 2)
+    return TRE_EINVAL;
+  if (!(r->scale >= -3e38f && r->scale <= 3e38f)) return TRE_EINVAL;
+  if (r->n_rows == 0) return TRE_OK;
+  if (!r->logits || !r->ids || !r->weights) return TRE_EINVAL;
+  if (!on(r->ids, 4) || !on(r->weights, 4) || !on(r->bias, 4)) return TRE_EINVAL;
+  RouteArgs a;
+  a.logits = static_cast<const uint8_t*>(r->logits);
+  a.bias = r->bias;
+  a.ids = r->ids;
+  a.weights = r->weights;
+  a.row = r->logits_row;
+  a.dtype = r->dtype;
+  a.n_rows = r->n_rows;
+  a.experts = r->experts;
+  a.top = r->top;
+  a.groups = r->top_groups == r->groups ? 1 : r->groups;      // (all stay)
+  a.per = r->experts / r->groups;
+  a.top_groups = r->top_groups;
+  a.group_best = r->group_best;
+  a.by_per = FastDiv31((uint32_t)a.per);
+  a.scale = r->scale;
+  a.softmax = r->scores == TRE_SOFTMAX;
+  a.renorm = r->renorm != 0;
+  a.raw = !r->bias && (a.groups == 1 || r->group_best == 1);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const int nv = (r->experts + 31) / 32;
+  const cudaError_t e = nv <= 1   ? launch_route<1>(a, s)
+                        : nv <= 2 ? launch_route<2>(a, s)
+                        : nv <= 4 ? launch_route<4>(a, s)
+                        : nv <= 8 ? launch_route<8>(a, s)
+                        : nv <= 16 ? launch_route<16>(a, s)
+                                   : launch_route<32>(a, s);
+  return e == cudaSuccess ? TRE_OK : TRE_ECUDA;
+}
+
+}  // extern "C"

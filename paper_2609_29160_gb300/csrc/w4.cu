@@ -1,0 +1,535 @@
+// Products with matrices in 4 bits: their layout, the products of few rows, and the plan of
+// experts' tokens. Many rows are w4_tc.cu's.
+#include <algorithm>
+
+#include "internal.h"
+#include "w4.cuh"
+
+namespace tre {
+namespace {
+
+// ---------------------------------------------------------------------------
+// Layout
+// ---------------------------------------------------------------------------
+struct Layout {
+  int64_t tiles, chunks, groups;
+  size_t codes, scales, zeros, bytes;      // where each begins, and the whole
+};
+Layout layout_of(int experts, int n, int k, int group, bool gated, bool zeros) {
+  Layout l;
+  l.tiles = gated ? (n / 2 + 15) / 16 * 2 : ((int64_t)n + 31) / 32 * 2;
+  l.chunks = ((int64_t)k + 63) / 64;
+  l.groups = l.chunks * 64 / group > 0 ? l.chunks * 64 / group : 1;
+  Arena a(nullptr);
+  a.take<uint4>((size_t)experts * l.tiles * l.chunks * 32);
+  l.codes = 0;
+  l.scales = (a.off + 255) & ~size_t(255);
+  a.take<uint32_t>((size_t)experts * l.tiles * l.groups * 8);
+  l.zeros = (a.off + 255) & ~size_t(255);
+  if (zeros) a.take<uint32_t>((size_t)experts * l.tiles * l.groups * 8);
+  l.bytes = a.off;
+  return l;
+}
+
+struct PackArgs {
+  const uint8_t *codes, *zeros;
+  const uint16_t* scales;
+  uint32_t *to_codes, *to_scales, *to_zeros;
+  int64_t tiles, chunks, groups;
+  int32_t n, k, group;
+  bool gated, bf16;
+};
+// Row r of tile `tile`, -1: none.
+__device__ __forceinline__ int row_of(const PackArgs& a, int64_t tile, int r) {
+  if (a.gated) {
+    const int64_t i = (tile >> 1) * 16 + r;
+    return i < a.n / 2 ? (int)((tile & 1) * (a.n / 2) + i) : -1;
+  }
+  const int64_t i = tile * 16 + r;
+  return i < a.n ? (int)i : -1;
+}
+// A thread a word of codes (once in a program's life).
+__global__ void k_w4_codes(PackArgs a, int64_t words) {
+  const int64_t at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (at >= words) return;
+  const int s = at & 3, lane = (at >> 2) & 31, g = lane >> 2, t = lane & 3;
+  const int64_t chunk = (at >> 7) % a.chunks, tile = (at >> 7) / a.chunks;
+  const int64_t e = tile / a.tiles;
+  uint32_t w = 0;
+  for (int i = 0; i < 4; ++i) {
+    const int row = row_of(a, tile % a.tiles, turn(g) + 8 * (i & 1));
+    const int64_t k = chunk * 64 + 32 * (s >> 1) + 8 * t + 4 * (s & 1) + 2 * (i >> 1);
+    if (row < 0 || k >= a.k) continue;
+    const uint32_t b = a.codes[((e * a.n + row) * a.k + k) / 2];
+    w |= (b & 15) << (4 * i) | (b >> 4) << (4 * i + 16);
+  }
+  a.to_codes[at] = w;
+}
+// A thread a pair of scales and zeros. Those of no row or no element are 0, which takes what
+// the codes there give out of the sums.
+__global__ void k_w4_scales(PackArgs a, int64_t words) {
+  const int64_t at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (at >= words) return;
+  const int g = at & 7;
+  const int64_t group = (at >> 3) % a.groups, tile = (at >> 3) / a.groups, e = tile / a.tiles;
+  uint32_t sc = 0, ze = 0;
+  for (int h = 0; h < 2; ++h) {
+    const int row = row_of(a, tile % a.tiles, turn(g) + 8 * h);
+    uint32_t s = 0, z = 8;
+    if (row >= 0 && group * a.group < a.k) {
+      const int64_t from = (e * a.n + row) * (a.k / a.group) + group;
+      s = a.scales[from];
+      if (a.zeros) z = a.zeros[from] & 15;
+    }
+    sc |= s << (16 * h);
+    ze |= (z | (a.bf16 ? 0x4300u : 0x6400u)) << (16 * h);
+  }
+  a.to_scales[at] = sc;
+  if (a.to_zeros) a.to_zeros[at] = ze;
+}
+
+// ---------------------------------------------------------------------------
+// Products of few rows.
+//
+// Bound by reading the codes: every warp reads two tiles of 16 rows side by side along its
+// part of k, 16 bytes a lane and tile, a block of 128 elements ahead, and multiplies them by
+// up to 8 NB rows of x with warp products whose accumulators are a group's sums (codes less
+// zeros are whole numbers, exact in 16 bits; the scale is applied once a group, in 32 bits).
+// The warps of a block share the same rows and are joined in order through shared memory.
+// ---------------------------------------------------------------------------
+constexpr int kFewWarps = 8;
+
+template <class T>
+__device__ __forceinline__ void mma_few(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  if constexpr (std::is_same<T, __nv_bfloat16>::value)
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+        "{%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+        "{%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint4 load_once(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p));
+  return v;
+}
+
+template <class T, int NB, int GROUP>
+__global__ void __launch_bounds__(kFewWarps * 32) k_w4_few(const __grid_constant__ ProductArgs p) {
+  constexpr int PER = 128 / GROUP;                     // groups of a block of 128 elements
+  __shared__ float sums[kFewWarps][8 * NB][33];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const W4Args& w = p.w;
+  const int pair = blockIdx.x;
+  Slot slot{0, 0, p.n_rows, 0};
+  if (p.plan.order) {
+    if ((int)blockIdx.y >= p.plan.n[0]) return;
+    slot = p.plan.slots[blockIdx.y];
+  }
+  const int64_t tile = (int64_t)slot.expert * w.tiles + 2 * pair;
+  const uint4* codes = w.codes + tile * w.chunks * 32 + lane;
+  const uint32_t* scales = w.scales + tile * w.groups * 8 + g;
+  const uint32_t* zeros = w.zeros + tile * w.groups * 8 + g;
+  const int64_t next_codes = (int64_t)w.chunks * 32, next_groups = (int64_t)w.groups * 8;
+  for (int from = 0; from < slot.count; from += 8 * NB) {
+    // rows of x of this lane's columns; null: none
+    const T* x[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int c = from + b * 8 + g;
+      x[b] = nullptr;
+      if (c < slot.count) {
+        const int place = slot.start + c;
+        const int64_t row = p.gather ? p.plan.order[place] / p.top : place;
+        x[b] = reinterpret_cast<const T*>(p.x) + row * p.x_row + 8 * t;
+      }
+    }
+    float acc[2][NB][4];
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[r][b][e] = 0.f;
+    uint4 c[2][2];                                     // [tile][chunk of the block]
+    auto fetch = [&](int kb) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          c[r][h] = 2 * kb + h < w.chunks ? load_once(codes + r * next_codes + (2 * kb + h) * 32)
+                                          : make_uint4(0, 0, 0, 0);
+    };
+    const int blocks = (w.chunks + 1) / 2;
+    if (warp < blocks) fetch(warp);
+    for (int kb = warp; kb < blocks; kb += kFewWarps) {
+      uint4 now[2][2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) now[r][h] = c[r][h];
+      uint32_t sc[2][PER], ze[2][PER];
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int q = 0; q < PER; ++q) {
+          const int at = kb * PER + q;
+          const bool there = at < w.groups;
+          sc[r][q] = there ? scales[r * next_groups + at * 8] : 0u;
+          ze[r][q] = there && w.zeros ? zeros[r * next_groups + at * 8] : Whole<T>::bits + 0x00080008u;
+        }
+      if (kb + kFewWarps < blocks) fetch(kb + kFewWarps);
+      float part[2][NB][4];
+#pragma unroll
+      for (int half = 0; half < 4; ++half) {           // 32 elements at a time
+        const int q = half * 32 / GROUP;
+        const int k0 = kb * 128 + half * 32;
+        uint4 v[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+          v[b] = x[b] && k0 < w.k ? *reinterpret_cast<const uint4*>(x[b] + k0) : make_uint4(0, 0, 0, 0);
+        if (half * 32 % GROUP == 0) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) part[r][b][e] = 0.f;
+        }
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const uint4& u = now[r][half >> 1];
+            const uint32_t word = (half & 1) ? (sub ? u.w : u.z) : (sub ? u.y : u.x);
+            uint32_t a[4];
+            whole<T>(word, both_lo(ze[r][q]), both_hi(ze[r][q]), a);
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+              mma_few<T>(part[r][b], a, sub ? v[b].z : v[b].x, sub ? v[b].w : v[b].y);
+          }
+        }
+        if ((half + 1) * 32 % GROUP == 0) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            float s0, s8;
+            unpack(sc[r][q], s0, s8, T());
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+              acc[r][b][0] = fmaf(s0, part[r][b][0], acc[r][b][0]);
+              acc[r][b][1] = fmaf(s0, part[r][b][1], acc[r][b][1]);
+              acc[r][b][2] = fmaf(s8, part[r][b][2], acc[r][b][2]);
+              acc[r][b][3] = fmaf(s8, part[r][b][3], acc[r][b][3]);
+            }
+          }
+        }
+      }
+    }
+    if (from > 0) __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          sums[warp][b * 8 + 2 * t + (e & 1)][r * 16 + turn(g) + 8 * (e >> 1)] = acc[r][b][e];
+    __syncthreads();
+    const int columns = min(8 * NB, slot.count - from);
+    const int wide = w.gated ? 16 : 32;
+    for (int i = threadIdx.x; i < columns * wide; i += kFewWarps * 32) {
+      const int col = i / wide, r = i % wide;
+      const int64_t n = (int64_t)pair * wide + r;
+      if (n >= (w.gated ? w.n / 2 : w.n)) continue;
+      float a = 0.f, u = 0.f;
+#pragma unroll
+      for (int k = 0; k < kFewWarps; ++k) {
+        a += sums[k][col][r];
+        if (w.gated) u += sums[k][col][16 + r];
+      }
+      if (w.gated) a = gated(a, u);
+      const int place = slot.start + from + col;
+      const int64_t row = p.scatter ? p.plan.order[place] : place;
+      if (p.y_f32) reinterpret_cast<float*>(p.y)[row * p.y_row + n] = a;
+      else reinterpret_cast<T*>(p.y)[row * p.y_row + n] = T(a);
+    }
+  }
+}
+
+template <class T, int NB>
+cudaError_t few_by_group(int group, const ProductArgs& p, dim3 grid, cudaStream_t s) {
+  if (group == 32) k_w4_few<T, NB, 32><<<grid, kFewWarps * 32, 0, s>>>(p);
+  else if (group == 64) k_w4_few<T, NB, 64><<<grid, kFewWarps * 32, 0, s>>>(p);
+  else k_w4_few<T, NB, 128><<<grid, kFewWarps * 32, 0, s>>>(p);
+  return cudaGetLastError();
+}
+template <class T>
+cudaError_t launch_few(int group, const ProductArgs& p, int columns, int slots, cudaStream_t s) {
+  const dim3 grid((unsigned)(p.w.tiles / 2), (unsigned)slots);
+  if (columns <= 8) return few_by_group<T, 1>(group, p, grid, s);
+  if (columns <= 16) return few_by_group<T, 2>(group, p, grid, s);
+  return few_by_group<T, 4>(group, p, grid, s);
+}
+// columns: rows of x that a product has, or most have; slots: experts that may have any.
+cudaError_t launch_few(int dtype, int group, const ProductArgs& p, int columns, int slots,
+                       cudaStream_t s) {
+  return dtype == TRE_BF16 ? launch_few<__nv_bfloat16>(group, p, columns, slots, s)
+                           : launch_few<__half>(group, p, columns, slots, s);
+}
+
+// ---------------------------------------------------------------------------
+// Experts: the plan of their tokens, and the sum of a token's experts.
+// ---------------------------------------------------------------------------
+constexpr int kPlanThreads = 1024, kMaxExperts = 1024;
+
+// Pairs (token, j) counted and sorted by expert. Which place of its expert a pair gets
+// depends on the order of atomics; the products do not depend on places.
+__global__ void __launch_bounds__(kPlanThreads) k_plan(const int32_t* ids, int64_t pairs, int experts,
+                                                       PlanArgs plan, tre_diag* diag) {
+  __shared__ int32_t count[kMaxExperts];
+  __shared__ int32_t warp_sums[3][32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  count[tid] = 0;
+  __syncthreads();
+  unsigned long long past = 0;
+  for (int64_t i = tid; i < pairs; i += kPlanThreads) {
+    const int e = ids[i];
+    if (e >= experts) ++past;
+    else if (e >= 0) atomicAdd(&count[e], 1);
+  }
+  if (diag) warp_add_counter(reinterpret_cast<unsigned long long*>(&diag->dropped_range), past);
+  __syncthreads();
+  const int mine = count[tid];
+  const int tiles = (mine + kTileTokens - 1) / kTileTokens;
+  int v[3] = {mine, mine > 0, tiles};                // places, slots, tiles before this expert
+#pragma unroll
+  for (int x = 0; x < 3; ++x) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, v[x], o);
+      if (lane >= o) v[x] += y;
+    }
+    if (lane == 31) warp_sums[x][warp] = v[x];
+  }
+  __syncthreads();
+  if (warp < 3) {
+    int y = warp_sums[warp][lane];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int z = __shfl_up_sync(0xffffffffu, y, o);
+      if (lane >= o) y += z;
+    }
+    warp_sums[warp][lane] = y;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < 3; ++x) v[x] += warp > 0 ? warp_sums[x][warp - 1] : 0;
+  const int start = v[0] - mine;
+  if (mine > 0) {
+    plan.slots[v[1] - 1] = Slot{tid, start, mine, 0};
+    // pieces of one size, whole sixteens
+    const int size = ((mine + tiles - 1) / tiles + 15) / 16 * 16;
+    for (int k = 0; k < tiles; ++k)
+      plan.tiles[v[2] - tiles + k] = Slot{tid, start + k * size, max(0, min(size, mine - k * size)), 0};
+  }
+  if (tid == kPlanThreads - 1) {
+    plan.n[0] = v[1];
+    plan.n[1] = v[2];
+  }
+  __syncthreads();
+  count[tid] = start;
+  __syncthreads();
+  for (int64_t i = tid; i < pairs; i += kPlanThreads) {
+    const int e = ids[i];
+    if (e >= 0 && e < experts) plan.order[atomicAdd(&count[e], 1)] = (int)i;
+  }
+}
+
+// y[t] = sum over j, in order, of weights[t][j] * each[t * top + j]; a block a token.
+template <class T, class E>
+__global__ void k_combine(const E* each, const int32_t* ids, const float* weights, int experts,
+                          int top, int dim, T* y, int64_t y_row) {
+  const int64_t t = blockIdx.x;
+  const int i = blockIdx.y * blockDim.x + threadIdx.x;
+  if (i >= dim) return;
+  float sum = 0.f;
+  for (int j = 0; j < top; ++j) {
+    const int e = ids[t * top + j];
+    if (e >= 0 && e < experts) sum = fmaf(weights[t * top + j], (float)each[(t * top + j) * dim + i], sum);
+  }
+  y[t * y_row + i] = T(sum);
+}
+
+template <class T>
+cudaError_t launch_combine(const void* each, bool f32, const tre_tokens* t, int experts, int dim,
+                           cudaStream_t s) {
+  const int threads = 256;
+  const dim3 grid((unsigned)t->n_rows, (unsigned)((dim + threads - 1) / threads));
+  if (f32)
+    k_combine<T, float><<<grid, threads, 0, s>>>(static_cast<const float*>(each), t->ids, t->weights,
+                                                 experts, t->top, dim, static_cast<T*>(t->y), t->y_row);
+  else
+    k_combine<T, T><<<grid, threads, 0, s>>>(static_cast<const T*>(each), t->ids, t->weights, experts,
+                                             t->top, dim, static_cast<T*>(t->y), t->y_row);
+  return cudaGetLastError();
+}
+
+bool half_type(int d) { return d == TRE_BF16 || d == TRE_F16; }
+bool at16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool shape_ok(int experts, int n, int k, int group, int gated) {
+  return experts >= 1 && experts <= kMaxExperts && n >= 1 && n <= (1 << 20) && k >= 1 &&
+         k <= (1 << 20) && (group == 32 || group == 64 || group == 128) && k % group == 0 &&
+         (!gated || n % 2 == 0);
+}
+
+// Rows up to which a plain product is k_w4_few's.
+constexpr int kFewRows = 32;
+
+}  // namespace
+
+bool w4_args(const tre_w4* w, W4Args& a) {
+  if (!w || !half_type(w->dtype) || !shape_ok(w->experts, w->n, w->k, w->group, w->gated)) return false;
+  if (!w->packed || (reinterpret_cast<uintptr_t>(w->packed) & 255)) return false;
+  const Layout l = layout_of(w->experts, w->n, w->k, w->group, w->gated != 0, w->zeros != 0);
+  const uint8_t* p = static_cast<const uint8_t*>(w->packed);
+  a.codes = reinterpret_cast<const uint4*>(p + l.codes);
+  a.scales = reinterpret_cast<const uint32_t*>(p + l.scales);
+  a.zeros = w->zeros ? reinterpret_cast<const uint32_t*>(p + l.zeros) : nullptr;
+  a.experts = w->experts;
+  a.n = w->n;
+  a.k = w->k;
+  a.tiles = (int32_t)l.tiles;
+  a.chunks = (int32_t)l.chunks;
+  a.groups = (int32_t)l.groups;
+  a.gated = w->gated != 0;
+  return true;
+}
+
+}  // namespace tre
+
+using namespace tre;
+
+extern "C" {
+
+tre_status tre_w4_pack(const tre_w4_source* f, void* packed, size_t* bytes, tre_stream stream) {
+  if (!f || !bytes || !half_type(f->dtype) || !shape_ok(f->experts, f->n, f->k, f->group, f->gated))
+    return TRE_EINVAL;
+  const Layout l = layout_of(f->experts, f->n, f->k, f->group, f->gated != 0, f->zeros != nullptr);
+  if (!packed) {
+    *bytes = l.bytes;
+    return TRE_OK;
+  }
+  if (*bytes < l.bytes) return TRE_ENOMEM;
+  if (!f->codes || !f->scales || (reinterpret_cast<uintptr_t>(f->scales) & 1) ||
+      (reinterpret_cast<uintptr_t>(packed) & 255))
+    return TRE_EINVAL;
+  uint8_t* p = static_cast<uint8_t*>(packed);
+  PackArgs a;
+  a.codes = f->codes;
+  a.zeros = f->zeros;
+  a.scales = static_cast<const uint16_t*>(f->scales);
+  a.to_codes = reinterpret_cast<uint32_t*>(p + l.codes);
+  a.to_scales = reinterpret_cast<uint32_t*>(p + l.scales);
+  a.to_zeros = f->zeros ? reinterpret_cast<uint32_t*>(p + l.zeros) : nullptr;
+  a.tiles = l.tiles;
+  a.chunks = l.chunks;
+  a.groups = l.groups;
+  a.n = f->n;
+  a.k = f->k;
+  a.group = f->group;
+  a.gated = f->gated != 0;
+  a.bf16 = f->dtype == TRE_BF16;
+  const int64_t words = f->experts * l.tiles * l.chunks * 128, pairs = f->experts * l.tiles * l.groups * 8;
+  if ((words + 255) / 256 > 2147483647) return TRE_EINVAL;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  k_w4_codes<<<(unsigned)((words + 255) / 256), 256, 0, s>>>(a, words);
+  k_w4_scales<<<(unsigned)((pairs + 255) / 256), 256, 0, s>>>(a, pairs);
+  return cudaGetLastError() == cudaSuccess ? TRE_OK : TRE_ECUDA;
+}
+
+tre_status tre_linear4(const tre_w4* w, int32_t n_rows, const void* x, int64_t x_row, void* y,
+                       int64_t y_row, tre_diag* diag, tre_stream stream) {
+  ProductArgs p{};
+  if (!w4_args(w, p.w) || w->experts != 1 || n_rows < 0) return TRE_EINVAL;
+  if (x_row % 8 || x_row < 0 || y_row < 0 || !at16(x) || (reinterpret_cast<uintptr_t>(y) & 1))
+    return TRE_EINVAL;
+  if (n_rows == 0) return TRE_OK;
+  if (!x || !y) return TRE_EINVAL;
+  p.x = static_cast<const uint8_t*>(x);
+  p.x_row = x_row;
+  p.y = static_cast<uint8_t*>(y);
+  p.y_row = y_row;
+  p.n_rows = n_rows;
+  p.top = 1;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const cudaError_t e = launch_few(w->dtype, w->group, p, n_rows, 1, s);
+  return e == cudaSuccess ? TRE_OK : TRE_ECUDA;
+}
+
+tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* t, void* ws,
+                       size_t* ws_bytes, tre_diag* diag, tre_stream stream) {
+  ProductArgs a{}, b{};
+  if (!t || !ws_bytes || !w4_args(w1, a.w) || !w4_args(w2, b.w)) return TRE_EINVAL;
+  if (w1->dtype != t->dtype || w2->dtype != t->dtype || !a.w.gated || b.w.gated ||
+      w1->experts != w2->experts || w2->k != w1->n / 2)
+    return TRE_EINVAL;
+  if (t->n_rows < 0 || t->top < 1 || t->top > 32 || (int64_t)t->n_rows * t->top > 2147483647 / 2)
+    return TRE_EINVAL;
+  if (t->x_row % 8 || t->x_row < 0 || t->y_row < 0 || !at16(t->x) ||
+      (reinterpret_cast<uintptr_t>(t->y) & 1) || (reinterpret_cast<uintptr_t>(t->ids) & 3) ||
+      (reinterpret_cast<uintptr_t>(t->weights) & 3))
+    return TRE_EINVAL;
+  const int64_t pairs = (int64_t)t->n_rows * t->top;
+  const int inner = w2->k, inner_row = (inner + 7) / 8 * 8, dim = w2->n;
+  const int64_t slots = std::min<int64_t>(w1->experts, pairs);
+  const bool few = true;
+  Arena arena(ws);
+  PlanArgs plan;
+  plan.order = arena.take<int32_t>(pairs);
+  plan.slots = arena.take<Slot>(slots);
+  plan.tiles = arena.take<Slot>(slots + pairs / kTileTokens);
+  plan.n = arena.take<int32_t>(2);
+  uint8_t* h = arena.take<uint8_t>((size_t)pairs * inner_row * 2);
+  uint8_t* each = arena.take<uint8_t>((size_t)pairs * dim * (few ? 4 : 2));
+  if (!ws) {
+    *ws_bytes = arena.off;
+    return TRE_OK;
+  }
+  if (*ws_bytes < arena.off) return TRE_ENOMEM;
+  if (t->n_rows == 0) return TRE_OK;
+  if (!t->x || !t->y || !t->ids || !t->weights) return TRE_EINVAL;
+  a.x = static_cast<const uint8_t*>(t->x);
+  a.x_row = t->x_row;
+  a.y = h;
+  a.y_row = inner_row;
+  a.gather = true;
+  b.x = h;
+  b.x_row = inner_row;
+  b.y = each;
+  b.y_row = dim;
+  b.scatter = true;
+  b.y_f32 = few;
+  a.plan = b.plan = plan;
+  a.n_rows = b.n_rows = t->n_rows;
+  a.top = b.top = t->top;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  k_plan<<<1, kPlanThreads, 0, s>>>(t->ids, pairs, w1->experts, plan, diag);
+  cudaError_t e = cudaGetLastError();
+  const int columns = (int)std::min<int64_t>(32, (pairs + slots - 1) / slots * 2);
+  if (!e) e = launch_few(t->dtype, w1->group, a, columns, (int)slots, s);
+  if (!e) e = launch_few(t->dtype, w2->group, b, columns, (int)slots, s);
+  if (!e)
+    e = t->dtype == TRE_BF16 ? launch_combine<__nv_bfloat16>(each, few, t, w1->experts, dim, s)
+                             : launch_combine<__half>(each, few, t, w1->experts, dim, s);
+  return e == cudaSuccess ? TRE_OK : TRE_ECUDA;
+}
+
+}  // extern "C"

@@ -1,0 +1,99 @@
+// Matrices in 4 bits as the products read them, and what both kernels of the products
+// share.
+//
+// A tile is 16 rows by 64 elements of k, 512 bytes, the tiles of 16 rows one after the other
+// along k. Lane (g, t) = (lane / 4, lane % 4) of a warp has 16 bytes of it: word s holds, of
+// rows r = turn(g) and r + 8, the elements k = 32 (s / 2) + 8 t + 4 (s % 2) + 0..3, as
+//   half-byte i      : row r + 8 (i % 2), element 2 (i / 2)
+//   half-byte i + 4  : the same row, the element after it        (i = 0..3)
+// so that one mask gives two neighbours of a row as the two halves of a register. Four
+// registers are a warp product's A operand (with the matching order of k in B: any order
+// will do for a sum over k), and two words of a row are 16 bytes of a tile in shared memory
+// as tcgen05 reads it. turn() puts rows r and r + 4 on neighbouring lanes, whose 16-byte
+// pieces then lie in different banks.
+// Scales [tile of 16 rows][group][g] are pairs (rows r, r + 8), 4 bytes; zeros the same, as
+// the number that is taken from a code that has been read as the last bits of kWhole.
+//
+// Of a gated matrix every even tile holds 16 rows of the gate and the next tile those that
+// they multiply.
+#pragma once
+
+#include "kvcache.cuh"
+
+namespace tre {
+
+struct W4Args {
+  const uint4* codes;
+  const uint32_t *scales, *zeros;      // zeros may be null: 8
+  int32_t experts, n, k, tiles, chunks, groups;   // groups: those of a row, to whole chunks
+  bool gated;
+};
+
+__host__ __device__ constexpr int turn(int g) { return g >> 1 | (g & 1) << 2; }
+
+// A whole number below 16 in the last bits of this one is itself plus `kWhole`.
+template <class T> struct Whole;
+template <> struct Whole<__nv_bfloat16> {
+  static constexpr uint32_t bits = 0x43004300u;      // 128
+};
+template <> struct Whole<__half> {
+  static constexpr uint32_t bits = 0x64006400u;      // 1024
+};
+template <class T> __device__ __forceinline__ uint32_t minus2(uint32_t a, uint32_t b);
+template <> __device__ __forceinline__ uint32_t minus2<__nv_bfloat16>(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a),
+                                   *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <> __device__ __forceinline__ uint32_t minus2<__half>(uint32_t a, uint32_t b) {
+  const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+// Both halves the lower / upper half of x
+__device__ __forceinline__ uint32_t both_lo(uint32_t x) { return __byte_perm(x, 0, 0x1010); }
+__device__ __forceinline__ uint32_t both_hi(uint32_t x) { return __byte_perm(x, 0, 0x3232); }
+
+// A word of codes as whole numbers: a[i] = (half-byte i, half-byte i + 4) less the zero of
+// its row (z0: of row r, z8: of row r + 8, with kWhole, in both halves).
+template <class T>
+__device__ __forceinline__ void whole(uint32_t w, uint32_t z0, uint32_t z8, uint32_t* a) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    a[i] = minus2<T>(((w >> (4 * i)) & 0x000f000fu) | Whole<T>::bits, i & 1 ? z8 : z0);
+}
+
+// What a gate does
+__device__ __forceinline__ float gated(float g, float u) { return g / (1.f + __expf(-g)) * u; }
+
+// Tokens of experts, sorted by expert (k_plan): places of one expert lie together; place p is
+// pair order[p] = token * top + j.
+struct Slot {
+  int32_t expert, start, count, pad;
+};
+struct PlanArgs {
+  int32_t* order;                      // [pairs]
+  Slot* slots;                         // experts that have any
+  Slot* tiles;                         // their places in pieces of up to kTileTokens
+  int32_t* n;                          // [2]: how many slots, tiles
+};
+constexpr int kTileTokens = 256;       // columns of a product on the tensor cores
+
+// One product of a call.
+struct ProductArgs {
+  W4Args w;
+  const uint8_t* x;
+  int64_t x_row;                       // elements
+  uint8_t* y;
+  int64_t y_row;
+  PlanArgs plan;                       // order null: rows as they are, one matrix
+  int32_t n_rows, top;
+  bool gather, scatter;                // x's / y's rows by pair: token of it / itself
+  bool y_f32;
+};
+
+bool w4_args(const tre_w4* w, W4Args& a);
+// w4_tc.cu. rows: most rows that x has.
+cudaError_t launch_w4_tc(int dtype, int group, const ProductArgs& p, int64_t rows, tre_diag* diag,
+                         cudaStream_t s);
+
+}  // namespace tre

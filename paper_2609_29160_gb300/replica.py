@@ -112,7 +112,7 @@ def _on(stream, fn, *args):
     here = torch.cuda.current_stream(stream.device)
     for x in args:
         for t in (x.k, x.v, x.k_scale, x.v_scale) if isinstance(x, KvCache) else (
-                x.pages, x.ctx_len, x.q_start) if isinstance(x, KvBatch) else (x,):
+                x.pages, x.ctx_len, x.q_start) if isinstance(x, KvBatch) else getattr(x, "tensors", (x,)):
             if isinstance(t, torch.Tensor) and t.is_cuda:
                 t.record_stream(stream)
     with torch.cuda.stream(stream):
