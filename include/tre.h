@@ -641,20 +641,21 @@ tre_status tre_chunk_attention(const tre_kv_cache* cache, const tre_kv_batch* ba
  * the same bits when the same call is made again, diag may be NULL.
  * ------------------------------------------------------------------------- */
 
-/* The rows between two blocks. dtype (TRE_BF16, TRE_F16, TRE_F32): y, gate, out;
- * stream_dtype (TRE_F32 or dtype): residual, residual_out; weight_dtype (TRE_F32 or
- * dtype): post_weight, weight. Rows of dim elements (1 to 16384), strides in
- * elements, last axis dense; any address and stride that an element of the type
- * may have (rows on 16-byte boundaries, with a dim that 8 divides, are read wider).
- *   y'           = y / sqrt(mean y^2 + eps) * post_weight   (post_weight NULL: y)
+/* The rows between two blocks. dtype (TRE_BF16, TRE_F16, TRE_F32): the model's, which
+ * the gate is of; y, residual (and residual_out), out, and the weights are each of it
+ * or TRE_F32. Rows of dim elements (1 to 16384), strides in elements, last axis dense;
+ * any address and stride that an element of the type may have (rows on 16-byte
+ * boundaries, with a dim that 8 divides, are read wider).
+   y'           = y / sqrt(mean y^2 + eps) * post_weight   (post_weight NULL: y)
  *   r            = residual + scale * gate * y'              (y NULL: residual)
  *   residual_out = r                                         (NULL: not written)
  *   out          = r / sqrt(mean r^2 + eps) * weight         (out NULL: not written)
  * gate (NULL: 1) of row t, element i: gate[t * gate_row + i * gate_col]; gate_col
  * is 0 or 1. out is computed from the 32-bit r, not from its rounding. residual_out
- * may be residual and out may be y, with the same strides; no other overlap. */
+ * may be residual and out may be y (of its type), with the same strides; no other
+ * overlap. */
 typedef struct {
-  tre_dtype dtype, stream_dtype, weight_dtype;
+  tre_dtype dtype, y_dtype, stream_dtype, weight_dtype, out_dtype;
   int32_t n_rows, dim;
   const void* residual;
   int64_t residual_row;
@@ -731,15 +732,27 @@ typedef struct {
  * NULL: the size needed is written to *bytes, nothing is done. */
 tre_status tre_w4_pack(const tre_w4_source* from, void* packed, size_t* bytes, tre_stream stream);
 
-/* tre_linear4 -- y = x W^T for rows x [n_rows][k] of w's dtype; of a gated w
- * y = g / (1 + exp(-g)) * u with g and u the two halves of x W^T, n/2 wide. w has one
- * matrix. x on 16-byte boundaries (strides in elements, a multiple of 8 for x).
- * Codes less their zeros are whole numbers that 16 bits hold: products are exact,
- * sums of a group are 32-bit, and so are scales; y is rounded once. How sums are
- * split depends on n_rows. A wait on the device that does not end in about two
- * seconds gives up (diag.err = TRE_ETIMEOUT, outputs undefined). */
-tre_status tre_linear4(const tre_w4* w, int32_t n_rows, const void* x, int64_t x_row, void* y,
-                       int64_t y_row, tre_diag* diag, tre_stream stream);
+/* Rows of tre_linear4: x [n_rows][k] and y [n_rows][n, or n/2 of a gated matrix] of
+ * dtype: the matrix's (x's address and stride multiples of 16 bytes), or TRE_F32.
+ * Strides in elements. */
+typedef struct {
+  tre_dtype dtype;
+  int32_t n_rows;
+  const void* x;
+  int64_t x_row;
+  void* y;
+  int64_t y_row;
+} tre_linear;
+
+/* tre_linear4 -- y = x W^T; of a gated w y = g / (1 + exp(-g)) * u with g and u the
+ * two halves of x W^T. w has one matrix. Codes less their zeros are whole numbers
+ * that 16 bits hold: products are exact, sums of a group are 32-bit, and so are
+ * scales; y is rounded once. Of a row in 32 bits 22 bits are taken of each element
+ * down to 2^-28 of the row's largest, and fewer of smaller ones. How sums are split
+ * depends on n_rows. A wait on the device that does not end in about two seconds
+ * gives up (diag.err = TRE_ETIMEOUT, outputs undefined). */
+tre_status tre_linear4(const tre_w4* w, const tre_linear* rows, void* ws, size_t* ws_bytes,
+                       tre_diag* diag, tre_stream stream);
 
 /* Tokens of tre_experts: x [n_rows][k] of dtype and y [n_rows][n of the second
  * matrices]; strides in elements, x's address and stride multiples of 16 bytes. ids,

@@ -14,7 +14,7 @@ LIB = os.path.join(OUT_DIR, "libtre.so")
 SOURCES = ["api.cu", "reduce.cu", "score.cu", "calibrate.cu", "select.cu", "noalloc.cu",
            "classes.cu", "device.cu", "stage.cu",
            "replay.cu", "kvcache.cu", "attend.cu", "attend_tc.cu", "block.cu",
-           "w4.cu"]
+           "w4.cu", "w4_tc.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-fmad=false", "-Xcompiler", "-fPIC",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]

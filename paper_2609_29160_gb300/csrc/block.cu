@@ -21,7 +21,7 @@ struct BlockArgs {
   int64_t residual_row, y_row, gate_row, gate_col, residual_out_row, out_row;
   int32_t n_rows, dim, per_row;        // per_row: threads of a row
   float scale, eps;
-  bool weight_f32;
+  bool weight_f32, y_f32, out_f32;
 };
 
 template <class T> __device__ __forceinline__ void get8(const T* p, float* x) {
@@ -113,7 +113,8 @@ __global__ void __launch_bounds__(512) k_block_norm(const __grid_constant__ Bloc
   mine.get(reinterpret_cast<const S*>(a.residual) + row * a.residual_row, r);
   if (a.y) {
     float y[N];
-    mine.get(reinterpret_cast<const T*>(a.y) + row * a.y_row, y);
+    if (a.y_f32) mine.get(reinterpret_cast<const float*>(a.y) + row * a.y_row, y);
+    else mine.get(reinterpret_cast<const T*>(a.y) + row * a.y_row, y);
     if (a.post_weight) {
       float sum = 0.f;
 #pragma unroll
@@ -144,7 +145,8 @@ __global__ void __launch_bounds__(512) k_block_norm(const __grid_constant__ Bloc
   for (int e = 0; e < N; ++e) sum = fmaf(r[e], r[e], sum);
   sum = row_sum(sum, block, part[1]);
   times_weight<T, N>(a, a.weight, mine, rsqrtf(sum / a.dim + a.eps), r);
-  mine.put(reinterpret_cast<T*>(a.out) + row * a.out_row, r);
+  if (a.out_f32) mine.put(reinterpret_cast<float*>(a.out) + row * a.out_row, r);
+  else mine.put(reinterpret_cast<T*>(a.out) + row * a.out_row, r);
 }
 
 constexpr int kMaxDim = 16384;
@@ -393,16 +395,17 @@ extern "C" {
 tre_status tre_block_norm(const tre_block_rows* b, tre_stream stream) {
   if (!b || b->n_rows < 0 || b->dim < 1 || b->dim > kMaxDim) return TRE_EINVAL;
   const int el = float_size(b->dtype), st = float_size(b->stream_dtype);
-  if (!el || (b->stream_dtype != TRE_F32 && b->stream_dtype != b->dtype)) return TRE_EINVAL;
-  if (b->weight_dtype != TRE_F32 && b->weight_dtype != b->dtype) return TRE_EINVAL;
-  const int wt = float_size(b->weight_dtype);
+  const int yt = float_size(b->y_dtype), ot = float_size(b->out_dtype), wt = float_size(b->weight_dtype);
+  if (!el) return TRE_EINVAL;
+  for (tre_dtype d : {b->stream_dtype, b->y_dtype, b->out_dtype, b->weight_dtype})
+    if (d != TRE_F32 && d != b->dtype) return TRE_EINVAL;
   if (!(b->eps >= 0.f) || b->eps > 3e38f || !(b->scale >= -3e38f && b->scale <= 3e38f))
     return TRE_EINVAL;
   if (b->gate_col != 0 && b->gate_col != 1) return TRE_EINVAL;
   if (!b->y && (b->post_weight || b->gate)) return TRE_EINVAL;
   if ((b->out && !b->weight) || (!b->out && !b->residual_out)) return TRE_EINVAL;
-  if (!on(b->residual, st) || !on(b->residual_out, st) || !on(b->y, el) || !on(b->gate, el) ||
-      !on(b->out, el) || !on(b->post_weight, wt) || !on(b->weight, wt))
+  if (!on(b->residual, st) || !on(b->residual_out, st) || !on(b->y, yt) || !on(b->gate, el) ||
+      !on(b->out, ot) || !on(b->post_weight, wt) || !on(b->weight, wt))
     return TRE_EINVAL;
   if (b->n_rows == 0) return TRE_OK;
   if (!b->residual) return TRE_EINVAL;
@@ -425,12 +428,14 @@ tre_status tre_block_norm(const tre_block_rows* b, tre_stream stream) {
   a.scale = b->scale;
   a.eps = b->eps;
   a.weight_f32 = b->weight_dtype == TRE_F32;
+  a.y_f32 = b->y_dtype == TRE_F32;
+  a.out_f32 = b->out_dtype == TRE_F32;
   const bool wide =
       b->dim % 8 == 0 && on(b->residual, 16) && on(b->y, 16) && on(b->residual_out, 16) &&
       on(b->out, 16) && on(b->post_weight, 16) && on(b->weight, 16) &&
-      b->residual_row * st % 16 == 0 && (!b->y || b->y_row * el % 16 == 0) &&
+      b->residual_row * st % 16 == 0 && (!b->y || b->y_row * yt % 16 == 0) &&
       (!b->residual_out || b->residual_out_row * st % 16 == 0) &&
-      (!b->out || b->out_row * el % 16 == 0) &&
+      (!b->out || b->out_row * ot % 16 == 0) &&
       (!b->gate || !b->gate_col || (on(b->gate, 16) && b->gate_row * el % 16 == 0));
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e;

@@ -123,7 +123,7 @@ __device__ __forceinline__ uint4 load_once(const uint4* p) {
   return v;
 }
 
-template <class T, int NB, int GROUP>
+template <class T, class S, int NB, int GROUP>
 __global__ void __launch_bounds__(kFewWarps * 32) k_w4_few(const __grid_constant__ ProductArgs p) {
   constexpr int PER = 128 / GROUP;                     // groups of a block of 128 elements
   __shared__ float sums[kFewWarps][8 * NB][33];
@@ -185,7 +185,8 @@ __global__ void __launch_bounds__(kFewWarps * 32) k_w4_few(const __grid_constant
           const int at = kb * PER + q;
           const bool there = at < w.groups;
           sc[r][q] = there ? scales[r * next_groups + at * 8] : 0u;
-          ze[r][q] = there && w.zeros ? zeros[r * next_groups + at * 8] : Whole<T>::bits + 0x00080008u;
+          ze[r][q] = zero_as<T, S>(there && w.zeros ? zeros[r * next_groups + at * 8]
+                                                    : Whole<S>::bits + 0x00080008u);
         }
       if (kb + kFewWarps < blocks) fetch(kb + kFewWarps);
       float part[2][NB][4];
@@ -222,7 +223,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) k_w4_few(const __grid_constant
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
             float s0, s8;
-            unpack(sc[r][q], s0, s8, T());
+            unpack(sc[r][q], s0, s8, S());
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
               acc[r][b][0] = fmaf(s0, part[r][b][0], acc[r][b][0]);
@@ -244,18 +245,20 @@ __global__ void __launch_bounds__(kFewWarps * 32) k_w4_few(const __grid_constant
           sums[warp][b * 8 + 2 * t + (e & 1)][r * 16 + turn(g) + 8 * (e >> 1)] = acc[r][b][e];
     __syncthreads();
     const int columns = min(8 * NB, slot.count - from);
-    const int wide = w.gated ? 16 : 32;
+    const bool joined = w.gated && !p.apart;
+    const int wide = joined ? 16 : 32;
     for (int i = threadIdx.x; i < columns * wide; i += kFewWarps * 32) {
       const int col = i / wide, r = i % wide;
-      const int64_t n = (int64_t)pair * wide + r;
+      int64_t n = (int64_t)pair * (w.gated ? 16 : 32) + (w.gated ? r & 15 : r);
       if (n >= (w.gated ? w.n / 2 : w.n)) continue;
+      if (w.gated) n += (r >> 4) * (w.n / 2);
       float a = 0.f, u = 0.f;
 #pragma unroll
       for (int k = 0; k < kFewWarps; ++k) {
         a += sums[k][col][r];
-        if (w.gated) u += sums[k][col][16 + r];
+        if (joined) u += sums[k][col][16 + r];
       }
-      if (w.gated) a = gated(a, u);
+      if (joined) a = gated(a, u);
       const int place = slot.start + from + col;
       const int64_t row = p.scatter ? p.plan.order[place] : place;
       if (p.y_f32) reinterpret_cast<float*>(p.y)[row * p.y_row + n] = a;
@@ -264,31 +267,94 @@ __global__ void __launch_bounds__(kFewWarps * 32) k_w4_few(const __grid_constant
   }
 }
 
-template <class T, int NB>
+template <class T, class S, int NB>
 cudaError_t few_by_group(int group, const ProductArgs& p, dim3 grid, cudaStream_t s) {
-  if (group == 32) k_w4_few<T, NB, 32><<<grid, kFewWarps * 32, 0, s>>>(p);
-  else if (group == 64) k_w4_few<T, NB, 64><<<grid, kFewWarps * 32, 0, s>>>(p);
-  else k_w4_few<T, NB, 128><<<grid, kFewWarps * 32, 0, s>>>(p);
+  if (group == 32) k_w4_few<T, S, NB, 32><<<grid, kFewWarps * 32, 0, s>>>(p);
+  else if (group == 64) k_w4_few<T, S, NB, 64><<<grid, kFewWarps * 32, 0, s>>>(p);
+  else k_w4_few<T, S, NB, 128><<<grid, kFewWarps * 32, 0, s>>>(p);
   return cudaGetLastError();
 }
-template <class T>
-cudaError_t launch_few(int group, const ProductArgs& p, int columns, int slots, cudaStream_t s) {
+template <class T, class S>
+cudaError_t few_by_columns(int group, const ProductArgs& p, int columns, int slots, cudaStream_t s) {
   const dim3 grid((unsigned)(p.w.tiles / 2), (unsigned)slots);
-  if (columns <= 8) return few_by_group<T, 1>(group, p, grid, s);
-  if (columns <= 16) return few_by_group<T, 2>(group, p, grid, s);
-  return few_by_group<T, 4>(group, p, grid, s);
+  if (columns <= 8) return few_by_group<T, S, 1>(group, p, grid, s);
+  if (columns <= 16) return few_by_group<T, S, 2>(group, p, grid, s);
+  return few_by_group<T, S, 4>(group, p, grid, s);
 }
 // columns: rows of x that a product has, or most have; slots: experts that may have any.
-cudaError_t launch_few(int dtype, int group, const ProductArgs& p, int columns, int slots,
-                       cudaStream_t s) {
-  return dtype == TRE_BF16 ? launch_few<__nv_bfloat16>(group, p, columns, slots, s)
-                           : launch_few<__half>(group, p, columns, slots, s);
+cudaError_t launch_few(int dtype, int scale_dtype, int group, const ProductArgs& p, int64_t columns,
+                       int slots, cudaStream_t s) {
+  const int c = (int)std::min<int64_t>(columns, 32);
+  if (dtype == TRE_BF16) return few_by_columns<__nv_bfloat16, __nv_bfloat16>(group, p, c, slots, s);
+  return scale_dtype == TRE_BF16 ? few_by_columns<__half, __nv_bfloat16>(group, p, c, slots, s)
+                                 : few_by_columns<__half, __half>(group, p, c, slots, s);
+}
+
+// Rows up to which a plain product is k_w4_few's.
+constexpr int kFewRows = 32;
+
+cudaError_t launch_rows(int dtype, int scale_dtype, int group, const ProductArgs& p, tre_diag* diag,
+                        cudaStream_t s) {
+  if (p.n_rows > kFewRows) {
+    const cudaError_t e = launch_w4_tc(dtype, scale_dtype, group, p, p.n_rows, 0, diag, s);
+    if (e != cudaErrorNotSupported) return e;
+  }
+  return launch_few(dtype, scale_dtype, group, p, p.n_rows, 1, s);
+}
+
+// ---------------------------------------------------------------------------
+// Rows in 32 bits: each is two rows of halves, which times codes (whole numbers, exact as
+// halves too) give exact products. The first half has the row's elements over a power of two
+// that puts the largest at 2^14 to 2^15, the second what that leaves of them: 22 bits
+// together of elements down to 2^-28 of the largest.
+// ---------------------------------------------------------------------------
+constexpr int kRowThreads = 256;
+
+__global__ void __launch_bounds__(kRowThreads) k_split(const float* x, int64_t x_row, int k, int n_rows,
+                                                       __half* to, float* back) {
+  __shared__ float part[kRowThreads / 32];
+  const int64_t t = blockIdx.x;
+  const float* from = x + t * x_row;
+  float top = 0.f;
+  for (int i = threadIdx.x; i < k; i += kRowThreads) {
+    const float v = fabsf(from[i]);
+    if (v < INFINITY) top = fmaxf(top, v);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kRowThreads / 32; ++i) top = fmaxf(top, part[i]);
+  // (bounded, so that both powers are numbers)
+  const int ex = min(max((int)(__float_as_uint(top) >> 23), 30), 250);       // 127 + exponent
+  const float by = __uint_as_float((uint32_t)(254 + 14 - ex) << 23);
+  if (threadIdx.x == 0) back[t] = __uint_as_float((uint32_t)(ex - 14) << 23);
+  for (int i = threadIdx.x; i < k; i += kRowThreads) {
+    const float v = from[i] * by;
+    const __half hi = __float2half_rn(v);
+    to[t * k + i] = hi;
+    to[(n_rows + t) * k + i] = __float2half_rn(fabsf(v) < INFINITY ? v - __half2float(hi) : 0.f);
+  }
+}
+// both [2 n_rows][n] to y [n_rows][n], or [n_rows][n / 2] of a gated matrix
+__global__ void __launch_bounds__(kRowThreads) k_whole_rows(const float* both, const float* back, int n,
+                                                            int n_rows, bool join, float* y, int64_t y_row) {
+  const int64_t t = blockIdx.x;
+  const int wide = join ? n / 2 : n, i = blockIdx.y * kRowThreads + threadIdx.x;
+  if (i >= wide) return;
+  const float *hi = both + t * n, *lo = both + (n_rows + t) * n;
+  const float f = back[t];
+  float a = (hi[i] + lo[i]) * f;
+  if (join) a = gated(a, (hi[wide + i] + lo[wide + i]) * f);
+  y[t * y_row + i] = a;
 }
 
 // ---------------------------------------------------------------------------
 // Experts: the plan of their tokens, and the sum of a token's experts.
 // ---------------------------------------------------------------------------
 constexpr int kPlanThreads = 1024, kMaxExperts = 1024;
+constexpr int kFewTokens = 12;       // tokens an expert up to which k_w4_few is taken
 
 // Pairs (token, j) counted and sorted by expert. Which place of its expert a pair gets
 // depends on the order of atomics; the products do not depend on places.
@@ -390,9 +456,6 @@ bool shape_ok(int experts, int n, int k, int group, int gated) {
          (!gated || n % 2 == 0);
 }
 
-// Rows up to which a plain product is k_w4_few's.
-constexpr int kFewRows = 32;
-
 }  // namespace
 
 bool w4_args(const tre_w4* w, W4Args& a) {
@@ -455,22 +518,57 @@ tre_status tre_w4_pack(const tre_w4_source* f, void* packed, size_t* bytes, tre_
   return cudaGetLastError() == cudaSuccess ? TRE_OK : TRE_ECUDA;
 }
 
-tre_status tre_linear4(const tre_w4* w, int32_t n_rows, const void* x, int64_t x_row, void* y,
-                       int64_t y_row, tre_diag* diag, tre_stream stream) {
+tre_status tre_linear4(const tre_w4* w, const tre_linear* l, void* ws, size_t* ws_bytes, tre_diag* diag,
+                       tre_stream stream) {
   ProductArgs p{};
-  if (!w4_args(w, p.w) || w->experts != 1 || n_rows < 0) return TRE_EINVAL;
-  if (x_row % 8 || x_row < 0 || y_row < 0 || !at16(x) || (reinterpret_cast<uintptr_t>(y) & 1))
+  if (!l || !ws_bytes || !w4_args(w, p.w) || w->experts != 1 || l->n_rows < 0) return TRE_EINVAL;
+  const bool f32 = l->dtype == TRE_F32;
+  if (!f32 && l->dtype != w->dtype) return TRE_EINVAL;
+  if (l->x_row < 0 || l->y_row < 0 || reinterpret_cast<uintptr_t>(l->y) % (f32 ? 4 : 2) ||
+      reinterpret_cast<uintptr_t>(l->x) % (f32 ? 4 : 16) || (!f32 && l->x_row % 8))
     return TRE_EINVAL;
-  if (n_rows == 0) return TRE_OK;
-  if (!x || !y) return TRE_EINVAL;
-  p.x = static_cast<const uint8_t*>(x);
-  p.x_row = x_row;
-  p.y = static_cast<uint8_t*>(y);
-  p.y_row = y_row;
-  p.n_rows = n_rows;
+  if (f32 && l->n_rows > 2147483647 / 2) return TRE_EINVAL;
+  Arena arena(ws);
+  const size_t twice = f32 ? 2 * (size_t)l->n_rows : 0;
+  __half* halves = arena.take<__half>(twice * w->k);
+  float* both = arena.take<float>(twice * w->n);
+  float* back = arena.take<float>(twice / 2);
+  if (!ws) {
+    *ws_bytes = f32 ? arena.off : 0;
+    return TRE_OK;
+  }
+  if (f32 && *ws_bytes < arena.off) return TRE_ENOMEM;
+  if (l->n_rows == 0) return TRE_OK;
+  if (!l->x || !l->y) return TRE_EINVAL;
+  p.x = static_cast<const uint8_t*>(l->x);
+  p.x_row = l->x_row;
+  p.y = static_cast<uint8_t*>(l->y);
+  p.y_row = l->y_row;
+  p.n_rows = l->n_rows;
   p.top = 1;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const cudaError_t e = launch_few(w->dtype, w->group, p, n_rows, 1, s);
+  cudaError_t e;
+  if (!f32) {
+    e = launch_rows(w->dtype, w->dtype, w->group, p, diag, s);
+  } else {
+    k_split<<<l->n_rows, kRowThreads, 0, s>>>(static_cast<const float*>(l->x), l->x_row, w->k, l->n_rows,
+                                              halves, back);
+    e = cudaGetLastError();
+    p.x = reinterpret_cast<const uint8_t*>(halves);
+    p.x_row = w->k;
+    p.y = reinterpret_cast<uint8_t*>(both);
+    p.y_row = w->n;
+    p.n_rows = 2 * l->n_rows;
+    p.y_f32 = p.apart = true;
+    if (!e) e = launch_rows(TRE_F16, w->dtype, w->group, p, diag, s);
+    if (!e) {
+      const int wide = p.w.gated ? w->n / 2 : w->n;
+      k_whole_rows<<<dim3((unsigned)l->n_rows, (unsigned)((wide + kRowThreads - 1) / kRowThreads)),
+                     kRowThreads, 0, s>>>(both, back, w->n, l->n_rows, p.w.gated,
+                                          static_cast<float*>(l->y), l->y_row);
+      e = cudaGetLastError();
+    }
+  }
   return e == cudaSuccess ? TRE_OK : TRE_ECUDA;
 }
 
@@ -490,7 +588,8 @@ tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* t, 
   const int64_t pairs = (int64_t)t->n_rows * t->top;
   const int inner = w2->k, inner_row = (inner + 7) / 8 * 8, dim = w2->n;
   const int64_t slots = std::min<int64_t>(w1->experts, pairs);
-  const bool few = true;
+  // Few tokens an expert: k_w4_few, whose outputs are small enough to be kept in 32 bits.
+  const bool few = pairs <= kFewTokens * slots;
   Arena arena(ws);
   PlanArgs plan;
   plan.order = arena.take<int32_t>(pairs);
@@ -523,9 +622,16 @@ tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* t, 
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   k_plan<<<1, kPlanThreads, 0, s>>>(t->ids, pairs, w1->experts, plan, diag);
   cudaError_t e = cudaGetLastError();
-  const int columns = (int)std::min<int64_t>(32, (pairs + slots - 1) / slots * 2);
-  if (!e) e = launch_few(t->dtype, w1->group, a, columns, (int)slots, s);
-  if (!e) e = launch_few(t->dtype, w2->group, b, columns, (int)slots, s);
+  const int64_t columns = (pairs + slots - 1) / slots * 2, tiles = slots + pairs / kTileTokens;
+  auto product = [&](const ProductArgs& p, const tre_w4* w, int64_t rows) {
+    if (!few) {
+      const cudaError_t x = launch_w4_tc(t->dtype, t->dtype, w->group, p, rows, tiles, diag, s);
+      if (x != cudaErrorNotSupported) return x;
+    }
+    return launch_few(t->dtype, t->dtype, w->group, p, columns, (int)slots, s);
+  };
+  if (!e) e = product(a, w1, t->n_rows);
+  if (!e) e = product(b, w2, pairs);
   if (!e)
     e = t->dtype == TRE_BF16 ? launch_combine<__nv_bfloat16>(each, few, t, w1->experts, dim, s)
                              : launch_combine<__half>(each, few, t, w1->experts, dim, s);

@@ -18,6 +18,8 @@
 // they multiply.
 #pragma once
 
+#include <type_traits>
+
 #include "kvcache.cuh"
 
 namespace tre {
@@ -48,6 +50,10 @@ template <> __device__ __forceinline__ uint32_t minus2<__nv_bfloat16>(uint32_t a
 template <> __device__ __forceinline__ uint32_t minus2<__half>(uint32_t a, uint32_t b) {
   const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
   return *reinterpret_cast<const uint32_t*>(&v);
+}
+// A pair of zeros, kept for scales of type S, for rows of type T.
+template <class T, class S> __device__ __forceinline__ uint32_t zero_as(uint32_t z) {
+  return std::is_same<T, S>::value ? z : (z & 0x000f000fu) | Whole<T>::bits;
 }
 // Both halves the lower / upper half of x
 __device__ __forceinline__ uint32_t both_lo(uint32_t x) { return __byte_perm(x, 0, 0x1010); }
@@ -89,11 +95,14 @@ struct ProductArgs {
   int32_t n_rows, top;
   bool gather, scatter;                // x's / y's rows by pair: token of it / itself
   bool y_f32;
+  bool apart;                          // a gated matrix's two halves as they are
 };
 
 bool w4_args(const tre_w4* w, W4Args& a);
-// w4_tc.cu. rows: most rows that x has.
-cudaError_t launch_w4_tc(int dtype, int group, const ProductArgs& p, int64_t rows, tre_diag* diag,
-                         cudaStream_t s);
+// w4_tc.cu. dtype: of the rows (TRE_BF16 only over scales of that type); rows: how many x has;
+// tiles: most that a plan has. cudaErrorNotSupported (nothing was launched): no tensor copy
+// takes these rows.
+cudaError_t launch_w4_tc(int dtype, int scale_dtype, int group, const ProductArgs& p, int64_t rows,
+                         int64_t tiles, tre_diag* diag, cudaStream_t s);
 
 }  // namespace tre

@@ -1,0 +1,516 @@
+// Products with matrices in 4 bits of many rows, on the tensor cores with their
+// accumulators in tensor memory.
+//
+//   y[t][n] = sum over groups q of scale[n][q] * sum over k in q of (code[n][k] - zero[n][q]) x[t][k]
+//
+// The matrix is the product's A operand: a unit is 256 rows of it against up to 256 rows of
+// x, for two blocks on neighbouring SMs (cta_group::2), each of which holds 128 rows of the
+// matrix and half of the rows of x in shared memory, and in tensor memory its 128 rows of
+// the sums. Codes less their zeros are whole numbers that 16 bits hold, so the products
+// inside a group are exact and its sum is one accumulator in tensor memory; the scale comes
+// when that accumulator is added, in 32 bits, to the sums that the scaling warps keep in
+// registers. Scaling the codes instead would round every element of the matrix to 16 bits
+// and need no adding; the adding is 256 multiply-adds a thread pair for 128 x 256 x group
+// products, a quarter of the issue slots at groups of 128 and, with them, of no time.
+//
+// A block's warps: 0-7 add groups (a thread a row of the matrix and half of the columns) and
+// write rows of y; 8-11 turn codes into the operand, through which 128 x 64 elements go at a
+// time; 12 copies rows of x (tensor copies, by four gathered rows where they are tokens of an
+// expert), 13 codes; 14 of the pair's first block issues the products. Of a gated matrix a
+// warp holds 16 rows of the gate and the 16 that they multiply.
+#include <algorithm>
+#include <cstring>
+
+#include "internal.h"
+#include "tensor.cuh"
+#include "w4.cuh"
+
+namespace tre {
+namespace {
+
+constexpr int kStages = 6, kRaws = 8;
+constexpr int kBytesA = 128 * 128, kBytesB = 128 * 128, kBytesRaw = 4096;
+constexpr int kAtB = kStages * kBytesA, kAtRaw = kAtB + kStages * kBytesB;
+constexpr int kAtBar = kAtRaw + kRaws * kBytesRaw;
+constexpr int kBars = 2 * kRaws + 3 * kStages + 4;
+constexpr int kSmem = kAtBar + kBars * 8 + 16;
+static_assert(kSmem <= 227 * 1024, "shared memory of a block");
+constexpr int kScaleWarps = 8, kCodeWarp = 8, kCodeWarps = 4, kRowWarp = 12, kRawWarp = 13, kMmaWarp = 14;
+constexpr int kThreads = 512;
+
+// A tile of rows of x, the same for both blocks of a pair.
+struct Unit {
+  int expert, block;                   // block: of 256 rows of the matrix
+  int start, count, columns;           // rows of x; to whole 32
+};
+
+struct TcArgs {
+  ProductArgs p;
+  int32_t row_blocks, tile;            // tile: rows of x of a unit, where there is no plan
+  int32_t box;                         // rows of x of one copy; 0: gathered by four
+};
+
+__device__ __forceinline__ bool unit_at(const TcArgs& a, int u, Unit& w) {
+  const int t = u / a.row_blocks;
+  w.block = u - t * a.row_blocks;
+  if (a.p.plan.order) {
+    if (t >= a.p.plan.n[1]) return false;
+    const Slot s = a.p.plan.tiles[t];
+    w.expert = s.expert;
+    w.start = s.start;
+    w.count = s.count;
+  } else {
+    w.expert = 0;
+    w.start = t * a.tile;
+    w.count = min(a.tile, a.p.n_rows - w.start);
+    if (w.count <= 0) return false;
+    w.columns = a.tile;                // (whole copies; rows past the last come as zeros)
+    return true;
+  }
+  w.columns = (w.count + 31) & ~31;
+  return true;
+}
+
+// Waits of a warp for arrivals that may come from the other block of the pair.
+__device__ __forceinline__ bool pair_poll(uint64_t* b, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2; "
+      "selp.b32 %0, 1, 0, p; }"
+      : "=r"(ok)
+      : "r"(smem_of(b)), "r"(parity)
+      : "memory");
+  return ok;
+}
+__device__ __forceinline__ bool pair_wait(uint64_t* b, uint32_t parity, volatile int* dead) {
+  bool ok = pair_poll(b, parity);
+  if (!ok) {
+    const long long from = clock64();
+    while (!(ok = pair_poll(b, parity))) {
+      if (*dead) break;
+      if (clock64() - from > kWaitClocks) {
+        *dead = 1;
+        break;
+      }
+    }
+  }
+  return __all_sync(0xffffffffu, ok);
+}
+// A warp's arrival at a barrier of the pair's first block.
+__device__ __forceinline__ void arrive_first(uint64_t* b) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0)
+    asm volatile(
+        "{ .reg .b32 a; mapa.shared::cluster.u32 a, %0, 0;\n"
+        "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [a]; }" ::"r"(smem_of(b))
+        : "memory");
+}
+__device__ __forceinline__ void commit_pair(uint64_t* b) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 "
+      "[%0], %1;" ::"r"(smem_of(b)),
+      "h"((uint16_t)3)
+      : "memory");
+}
+__device__ __forceinline__ void mma_pair(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{ .reg .pred p; .reg .b64 x, y; setp.ne.b32 p, %4, 0; mov.b64 x, {%1, %5}; "
+      "mov.b64 y, {%2, %5};\n"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], x, y, %3, p; }" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "n"(kOperandHigh)
+      : "memory");
+}
+__device__ __forceinline__ void pair_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// acc += s * v, two at a time
+__device__ __forceinline__ void add_scaled(float* acc, const uint32_t* v, float s) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(two(v)), "l"(two(s, s)), "l"(two(acc[0], acc[1])));
+  uint32_t x[2];
+  split(r, x);
+  acc[0] = __uint_as_float(x[0]);
+  acc[1] = __uint_as_float(x[1]);
+}
+
+template <class T, class S, int GROUP>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap rows, tre_diag* diag) {
+  extern __shared__ __align__(1024) uint8_t sm[];
+  constexpr int PER = GROUP >= 64 ? 1 : 2;             // groups of a stage
+  constexpr int STAGES_OF = GROUP == 128 ? 2 : 1;      // stages of a group
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+  const int side = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const W4Args& w = a.p.w;
+
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sm + kAtBar);
+  uint64_t *raw_full = bars, *raw_empty = raw_full + kRaws, *x_full = raw_empty + kRaws,
+           *full = x_full + kStages, *empty = full + kStages, *sum_full = empty + kStages,
+           *sum_empty = sum_full + 2;
+  uint32_t* tmem_at = reinterpret_cast<uint32_t*>(bars + kBars);
+  volatile int* dead = reinterpret_cast<volatile int*>(tmem_at + 1);
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(
+                     smem_of(tmem_at))
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+  }
+  if (tid == 0) {
+    *dead = 0;
+    for (int k = 0; k < kRaws; ++k) {
+      bar_init(raw_full + k, 1);
+      bar_init(raw_empty + k, kCodeWarps);
+    }
+    for (int k = 0; k < kStages; ++k) {
+      bar_init(x_full + k, 1);
+      bar_init(full + k, 2 * kCodeWarps);
+      bar_init(empty + k, 1);
+    }
+    for (int k = 0; k < 2; ++k) {
+      bar_init(sum_full + k, 1);
+      bar_init(sum_empty + k, 2 * kScaleWarps);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  tmem_before();
+  __syncthreads();
+  pair_sync();
+  tmem_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_at, 0);
+  Unit u;
+
+  // Registers move once, from the launch's 4 x 128 (in groups of four warps).
+  if (warp < kScaleWarps) {
+    // ---- sums of groups ----------------------------------------------------------
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    const int quarter = warp & 3, half = warp >> 2, r16 = lane & 15;
+    const int g = (r16 & 3) << 1 | (r16 >> 2 & 1);       // turn(g) == r16 & 7
+    uint32_t n = 0;                                      // groups so far
+    bool alive = true;
+    for (int i = pair; alive && unit_at(a, i, u); i += pairs) {
+      const int mine = u.columns / 2;                    // columns of this warp, from half * mine on
+      const int tile = (2 * u.block + side) * 8 + 2 * quarter + (lane >> 4);
+      const bool there = tile < w.tiles;
+      const uint16_t* scale =
+          reinterpret_cast<const uint16_t*>(
+              w.scales + (((int64_t)u.expert * w.tiles + min(tile, w.tiles - 1)) * w.groups) * 8 + g) +
+          (r16 >> 3);
+      float acc[128];
+#pragma unroll
+      for (int c = 0; c < 128; ++c) acc[c] = 0.f;
+      uint16_t ahead = scale[0];
+#pragma unroll 1
+      for (int q = 0; q < w.groups; ++q, ++n) {
+        const uint16_t bits = ahead;
+        if (q + 1 < w.groups) ahead = scale[(q + 1) * 16];
+        const uint32_t buf = n & 1;
+        if (!(alive = bar_wait(sum_full + buf, (n >> 1) & 1, dead))) break;
+        tmem_after();
+        float s, unused;
+        unpack((uint32_t)bits, s, unused, S());
+        const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + buf * 256 + half * mine;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          if (b * 32 >= mine) break;
+          uint32_t v[32];
+          tmem_ld32(at + b * 32, v);
+          tmem_wait_ld(v);
+          if ((b + 1) * 32 >= mine) {                    // all read
+            tmem_before();
+            arrive_first(sum_empty + buf);
+          }
+#pragma unroll
+          for (int c = 0; c < 32; c += 2) add_scaled(acc + b * 32 + c, v + c, s);
+        }
+      }
+      if (!alive) break;
+      // rows of y: a thread's row of the matrix is a column of them
+      const int first = half * mine;
+      const int in_pair = (2 * u.block + side) * 4 + quarter;    // of tiles
+      const int halves = w.n / 2;
+      int feature;
+      bool mine_too;
+      if (w.gated) {
+        feature = in_pair * 16 + r16;
+        mine_too = there && feature < halves;
+        if (a.p.apart && lane >= 16) feature += halves;
+      } else {
+        feature = tile * 16 + r16;
+        mine_too = there && feature < w.n;
+      }
+      int place[4];
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const int c = first + b * 32 + lane;
+        place[b] = u.start + c;
+        if (a.p.scatter) place[b] = c < u.count ? a.p.plan.order[u.start + c] : 0;
+      }
+      auto put = [&](int row, float v) {
+        const int64_t to = (int64_t)row * a.p.y_row + feature;
+        if (a.p.y_f32) reinterpret_cast<float*>(a.p.y)[to] = v;
+        else reinterpret_cast<T*>(a.p.y)[to] = T(v);
+      };
+      const bool joined = w.gated && !a.p.apart;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        if (b * 32 >= mine) break;
+#pragma unroll
+        for (int c = 0; c < 32; c += 2) {
+          const int col = first + b * 32 + c;
+          if (b * 32 + c < mine && col < u.count) {      // (the same for the whole warp)
+            const int row0 = __shfl_sync(0xffffffffu, place[b], c);
+            const int row1 = __shfl_sync(0xffffffffu, place[b], c + 1);
+            const float x0 = acc[b * 32 + c], x1 = acc[b * 32 + c + 1];
+            if (joined) {
+              const float other = __shfl_xor_sync(0xffffffffu, lane < 16 ? x1 : x0, 16);
+              const float v = lane < 16 ? gated(x0, other) : gated(other, x1);
+              if (mine_too && col + (lane >> 4) < u.count) put(lane < 16 ? row0 : row1, v);
+            } else if (mine_too) {
+              put(row0, x0);
+              if (col + 1 < u.count) put(row1, x1);
+            }
+          }
+        }
+      }
+    }
+  } else if (warp < kCodeWarp + kCodeWarps) {
+    // ---- codes to an operand -------------------------------------------------------
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    const int cw = warp - kCodeWarp, g = lane >> 2, t = lane & 3;
+    uint32_t n = 0;                                      // stages so far
+    bool alive = true;
+    for (int i = pair; alive && unit_at(a, i, u); i += pairs) {
+      const int tile0 = (2 * u.block + side) * 8 + 2 * cw;
+      const uint32_t* zero[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        zero[x] = w.zeros + (((int64_t)u.expert * w.tiles + min(tile0 + x, w.tiles - 1)) * w.groups) * 8 + g;
+      uint32_t ahead[2][PER];
+      auto look = [&](int c) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int y = 0; y < PER; ++y)
+            ahead[x][y] = w.zeros ? zero[x][(c * 64 / GROUP + y) * 8] : Whole<S>::bits + 0x00080008u;
+      };
+      look(0);
+#pragma unroll 1
+      for (int c = 0; c < w.chunks; ++c, ++n) {
+        const uint32_t s = n % kStages, r = n % kRaws;
+        if (!(alive = bar_wait(raw_full + r, (n / kRaws) & 1, dead))) break;
+        uint4 code[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          code[x] = reinterpret_cast<const uint4*>(sm + kAtRaw + r * kBytesRaw)[(2 * cw + x) * 32 + lane];
+        bar_arrive_warp(raw_empty + r);
+        uint32_t z[2][PER];
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int y = 0; y < PER; ++y) z[x][y] = zero_as<T, S>(ahead[x][y]);
+        if (c + 1 < w.chunks) look(c + 1);
+        if (!(alive = bar_wait(empty + s, ((n / kStages) & 1) ^ 1, dead))) break;
+        uint8_t* to = sm + s * kBytesA;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int row = (2 * cw + x) * 16 + turn(g);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {                  // 32 elements each
+            const uint32_t zz = z[x][h * (PER - 1)];
+            uint32_t p[4], q[4];
+            whole<T>(h ? code[x].z : code[x].x, both_lo(zz), both_hi(zz), p);
+            whole<T>(h ? code[x].w : code[x].y, both_lo(zz), both_hi(zz), q);
+            const int at = ((4 * h + t) ^ (row & 7)) << 4;
+            *reinterpret_cast<uint4*>(to + row * 128 + at) = make_uint4(p[0], p[2], q[0], q[2]);
+            *reinterpret_cast<uint4*>(to + (row + 8) * 128 + at) = make_uint4(p[1], p[3], q[1], q[3]);
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        if (!(alive = bar_wait(x_full + s, (n / kStages) & 1, dead))) break;
+        arrive_first(full + s);
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (warp == kRowWarp) {
+      // ---- rows of x ---------------------------------------------------------------
+      uint32_t n = 0;
+      bool alive = true;
+      for (int i = pair; alive && unit_at(a, i, u); i += pairs) {
+        const int mine = u.columns / 2, first = u.start + side * mine;
+        int r[4] = {0, 0, 0, 0};
+        if (a.box == 0) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            // (columns past the last are not written: any row will do)
+            const int p = min(first + lane * 4 + x, u.start + u.count - 1);
+            r[x] = a.p.plan.order[p] / a.p.top;
+          }
+        }
+#pragma unroll 1
+        for (int c = 0; c < w.chunks; ++c, ++n) {
+          const uint32_t s = n % kStages;
+          if (!(alive = bar_wait(empty + s, ((n / kStages) & 1) ^ 1, dead))) break;
+          if (lane == 0) bar_expect(x_full + s, mine * 128);
+          __syncwarp();
+          const uint32_t to = smem_of(sm + kAtB + s * kBytesB);
+          if (a.box == 0) {
+            if (lane * 4 < mine)
+              asm volatile(
+                  "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes "
+                  "[%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(to + lane * 512),
+                  "l"(&rows), "r"(c * 64), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(smem_of(x_full + s))
+                  : "memory");
+          } else if (lane * a.box < mine) {
+            asm volatile(
+                "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                "[%0], [%1, {%2, %3}], [%4];" ::"r"(to + lane * a.box * 128),
+                "l"(&rows), "r"(c * 64), "r"(first + lane * a.box), "r"(smem_of(x_full + s))
+                : "memory");
+          }
+          __syncwarp();
+        }
+      }
+      // the products' arrivals that no copy waits for any more
+      for (uint32_t k = n > kStages ? n - kStages : 0; alive && k < n; ++k)
+        alive = bar_wait(empty + k % kStages, (k / kStages) & 1, dead);
+    } else if (warp == kRawWarp) {
+      // ---- codes -------------------------------------------------------------------
+      uint32_t n = 0;
+      bool alive = true;
+      for (int i = pair; alive && unit_at(a, i, u); i += pairs) {
+        const int tile = min((2 * u.block + side) * 8 + (lane & 7), w.tiles - 1);
+        const uint4* from = w.codes + ((int64_t)u.expert * w.tiles + tile) * w.chunks * 32;
+#pragma unroll 1
+        for (int c = 0; c < w.chunks; ++c, ++n) {
+          const uint32_t r = n % kRaws;
+          if (!(alive = bar_wait(raw_empty + r, ((n / kRaws) & 1) ^ 1, dead))) break;
+          if (lane == 0) bar_expect(raw_full + r, kBytesRaw);
+          __syncwarp();
+          if (lane < 8)
+            asm volatile(
+                "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], 512, [%2];" ::"r"(
+                    smem_of(sm + kAtRaw + r * kBytesRaw) + lane * 512),
+                "l"(from + c * 32), "r"(smem_of(raw_full + r))
+                : "memory");
+          __syncwarp();
+        }
+      }
+    } else if (warp == kMmaWarp && side == 0) {
+      // ---- products ------------------------------------------------------------------
+      uint32_t n = 0, groups = 0;
+      bool alive = true;
+      for (int i = pair; alive && unit_at(a, i, u); i += pairs) {
+        // 256 rows of the matrix over the two blocks
+        const uint32_t id = (idesc_of<T>(u.columns, false) & 0x00ffffffu) | (256u >> 4) << 24;
+#pragma unroll 1
+        for (int c = 0; c < w.chunks; ++c, ++n) {
+          const uint32_t s = n % kStages;
+          if (!(alive = pair_wait(full + s, (n / kStages) & 1, dead))) break;
+          const uint32_t x = operand(smem_of(sm + s * kBytesA), 16), y = operand(smem_of(sm + kAtB + s * kBytesB), 16);
+#pragma unroll
+          for (int h = 0; h < PER; ++h) {
+            const uint32_t buf = groups & 1;
+            const bool fresh = STAGES_OF == 1 || (c & 1) == 0;
+            if (fresh && !(alive = pair_wait(sum_empty + buf, ((groups >> 1) & 1) ^ 1, dead))) break;
+            tmem_after();
+            const bool whole_group = STAGES_OF == 1 || (c & 1) == 1;
+            if (one_lane()) {
+#pragma unroll
+              for (int k = h * 4 / PER; k < (h + 1) * 4 / PER; ++k)
+                mma_pair(tmem + buf * 256, x + k * 2, y + k * 2, id, !(fresh && k == h * 4 / PER));
+              if (whole_group) commit_pair(sum_full + buf);
+              if (h == PER - 1) commit_pair(empty + s);
+            }
+            __syncwarp();
+            if (whole_group) ++groups;
+          }
+          if (!alive) break;
+        }
+      }
+    }
+  }
+  // A block that has given up does not know which of its copies and products are still on
+  // their way: it stays some 20 ms, far longer than any takes.
+  __syncthreads();
+  if (*dead) {
+    const long long from = clock64();
+    while (clock64() - from < kDrainClocks) {
+    }
+  }
+  tmem_before();
+  pair_sync();
+  tmem_after();
+  if (warp == kMmaWarp)
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+  if (tid == 0 && *dead && diag) diag->err = TRE_ETIMEOUT;
+}
+
+// Rows of x in boxes of `box` rows and 64 elements, or one row for a gather by four.
+bool make_map(CUtensorMap& m, bool bf16, const ProductArgs& p, int64_t rows, int box) {
+  const Encode enc = encoder();
+  const int64_t stride = p.x_row * 2;
+  if (!enc || stride <= 0 || stride >= (1ll << 40)) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)p.w.k, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)stride};
+  const cuuint32_t size[2] = {64, (cuuint32_t)(box ? box : 1)}, one[2] = {1, 1};
+  return enc(&m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+             const_cast<uint8_t*>(p.x), dims, strides, size, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <class T, class S, int GROUP>
+cudaError_t launch_typed(const TcArgs& a, const CUtensorMap& rows, int64_t units, tre_diag* diag,
+                         cudaStream_t s) {
+  const void* fn = (const void*)k_w4_tc<T, S, GROUP>;
+  cudaError_t e = func_smem_once(fn, kSmem, true);
+  if (e) return e;
+  const int64_t pairs = std::min<int64_t>(units, std::max(1, device_sm_count() / 2));
+  k_w4_tc<T, S, GROUP><<<(unsigned)(2 * pairs), kThreads, kSmem, s>>>(a, rows, diag);
+  return cudaGetLastError();
+}
+template <class T, class S>
+cudaError_t launch_group(int group, const TcArgs& a, const CUtensorMap& rows, int64_t units, tre_diag* diag,
+                         cudaStream_t s) {
+  if (group == 32) return launch_typed<T, S, 32>(a, rows, units, diag, s);
+  if (group == 64) return launch_typed<T, S, 64>(a, rows, units, diag, s);
+  return launch_typed<T, S, 128>(a, rows, units, diag, s);
+}
+
+}  // namespace
+
+cudaError_t launch_w4_tc(int dtype, int scale_dtype, int group, const ProductArgs& p, int64_t rows,
+                         int64_t tiles, tre_diag* diag, cudaStream_t s) {
+  TcArgs a;
+  a.p = p;
+  a.row_blocks = (p.w.tiles + 15) / 16;
+  a.tile = kTileTokens;
+  if (!p.plan.order) {
+    // Rows of a unit: those with which the rounds of units take least, each its columns and
+    // what a unit costs besides.
+    const int64_t pairs = std::max(1, device_sm_count() / 2);
+    int64_t least = -1;
+    for (int n = 32; n <= kTileTokens; n += 32) {
+      const int64_t units = (rows + n - 1) / n * a.row_blocks;
+      const int64_t cost = (units + pairs - 1) / pairs * (n + 32);
+      if (least < 0 || cost <= least) {
+        least = cost;
+        a.tile = n;
+      }
+    }
+    tiles = (rows + a.tile - 1) / a.tile;
+  }
+  a.box = p.gather ? 0 : p.plan.order ? 16 : a.tile / 2;
+  if (tiles * a.row_blocks > 2000000000) return cudaErrorNotSupported;
+  CUtensorMap map;
+  memset(&map, 0, sizeof(map));
+  if (!make_map(map, dtype == TRE_BF16, p, rows, a.box)) return cudaErrorNotSupported;
+  const int64_t units = tiles * a.row_blocks;
+  if (dtype == TRE_BF16) return launch_group<__nv_bfloat16, __nv_bfloat16>(group, a, map, units, diag, s);
+  return scale_dtype == TRE_BF16 ? launch_group<__half, __nv_bfloat16>(group, a, map, units, diag, s)
+                                 : launch_group<__half, __half>(group, a, map, units, diag, s);
+}
+
+}  // namespace tre

@@ -15,10 +15,11 @@ from . import replica
 from .replica import BF16, F16, F32, _codes, _diag
 
 # The structs of include/tre.h by their fields (see replica).
-BLOCK = struct.Struct("@5iPqPqPPqqffPPqPq0q")      # tre_block_rows
+BLOCK = struct.Struct("@7iPqPqPPqqffPPqPq0q")      # tre_block_rows
 ROUTER = struct.Struct("@4iPqiP4ifPP0q")           # tre_router
 SOURCE = struct.Struct("@6iPPP0q")                 # tre_w4_source
 W4 = struct.Struct("@7iP0q")                       # tre_w4
+LINEAR = struct.Struct("@2iPqPq0q")                  # tre_linear
 TOKENS = struct.Struct("@3iPqPPPq0q")              # tre_tokens
 
 SCORES = {"softmax": 0, "sigmoid": 1}
@@ -27,12 +28,12 @@ _torch = None
 
 def declare(lib):
     """Argument types of the entry points (called when the library is loaded)."""
-    P, L, I = C.c_void_p, C.c_int64, C.c_int32
+    P = C.c_void_p
     size = C.POINTER(C.c_size_t)
     lib.tre_block_norm.argtypes = [P, P]
     lib.tre_route.argtypes = [P, P]
     lib.tre_w4_pack.argtypes = [P, P, size, P]
-    lib.tre_linear4.argtypes = [P, I, P, L, P, L, P, P]
+    lib.tre_linear4.argtypes = [P, P, P, size, P, P]
     lib.tre_experts.argtypes = [P, P, P, P, size, P, P]
     for f in ("tre_block_norm", "tre_route", "tre_w4_pack", "tre_linear4", "tre_experts"):
         getattr(lib, f).restype = C.c_int
@@ -72,15 +73,13 @@ def _rows(t, what, dtype, dev, shape=None):
     return row
 
 
-def _weight(t, what, dim, dev, dtype):
-    """Code of the type of `dim` dense weights."""
+def _weight(t, what, dim, dev):
+    """Type of `dim` dense weights."""
     if t.dim() != 1 or t.shape[0] != dim or (dim > 1 and t.stride(0) != 1):
         raise ValueError(f"{what}: expected {dim} dense elements")
-    if t.dtype is not dtype and t.dtype is not _torch.float32:
-        raise ValueError(f"{what}: expected float32 or {dtype}, got {t.dtype}")
     if t.get_device() != dev:
         raise ValueError(f"{what}: must be on the device of the other tensors")
-    return _codes[t.dtype]
+    return t.dtype
 
 
 def tre_block_norm(residual, y=None, post_weight=None, gate=None, scale=1.0, weight=None, eps=1e-6,
@@ -89,76 +88,91 @@ def tre_block_norm(residual, y=None, post_weight=None, gate=None, scale=1.0, wei
     norm(y) (post_weight None: y as it is; gate: [dim], [rows][1] or [rows][dim], None: 1; y
     None: residual as it is), and the stream normed for the next block (weight None: not).
     Returns (r, normed): r is `residual` itself where there is no y and no residual_out, normed
-    is None without a weight. dtype: of the normed rows where there is no y (None: the
-    residual's). residual_out may be residual, out may be y."""
+    is None without a weight. Types: one of 16 bits or float32 throughout, or both (a gate
+    is of the former); dtype: that of the normed rows (None: y's, without one the residual's).
+    residual_out may be residual, out may be y."""
     if stream is not None:
         return replica._on(stream, tre_block_norm, residual, y, post_weight, gate, scale, weight, eps,
                            residual_out, out, dtype)
     lib = _ready()
     dev = _here(residual, "residual")
-    stream_dtype = residual.dtype
-    if y is not None:
-        kind = y.dtype
-    elif out is not None:
-        kind = out.dtype
-    else:
-        kind = stream_dtype if dtype is None else replica._torch_type(replica._code(dtype, replica._FLOATS, "dtype"))
-    code = replica._code(kind, replica._FLOATS, "y")
-    if stream_dtype is not kind and stream_dtype is not _torch.float32:
-        raise ValueError(f"residual: expected float32 or {kind}, got {stream_dtype}")
-    r_row = _rows(residual, "residual", stream_dtype, dev)
+    f32 = _torch.float32
+    r_kind = residual.dtype
+    r_row = _rows(residual, "residual", r_kind, dev)
     shape = residual.shape
     rows, dim = shape
     if not 1 <= dim <= 16384:
         raise ValueError(f"residual: expected rows of 1 to 16384 elements, got {dim}")
-    yp = y_row = gp = g_row = g_col = pp = wp = 0
-    wt = None
+    kinds = [r_kind]
+    yp = y_row = gp = g_row = g_col = pp = wp = ro_row = rp = o_row = op = 0
+    y_kind = w_kind = f32
     if y is not None:
-        y_row = _rows(y, "y", kind, dev, shape)
+        y_kind = y.dtype
+        kinds.append(y_kind)
+        y_row = _rows(y, "y", y_kind, dev, shape)
         yp = y.data_ptr()
     elif post_weight is not None or gate is not None:
         raise ValueError("post_weight, gate: only with a block's output y")
     if post_weight is not None:
-        wt = _weight(post_weight, "post_weight", dim, dev, kind)
+        w_kind = _weight(post_weight, "post_weight", dim, dev)
+        kinds.append(w_kind)
         pp = post_weight.data_ptr()
     if gate is not None:
         if gate.dim() == 1:
             gate = gate[None]
         if gate.dim() != 2 or gate.shape[0] not in (1, rows) or gate.shape[1] not in (1, dim):
             raise ValueError(f"gate: expected [{dim}], [{rows}][1] or [{rows}][{dim}], got {tuple(gate.shape)}")
-        g_row = _rows(gate, "gate", kind, dev)
+        g_row = _rows(gate, "gate", gate.dtype, dev)
         if gate.shape[0] == 1:
             g_row = 0
         g_col = 1 if gate.shape[1] == dim and dim > 1 else 0
+        kinds.append(gate.dtype)
         gp = gate.data_ptr()
+    o_kind = f32
     if weight is not None:
-        w2 = _weight(weight, "weight", dim, dev, kind)
-        if wt is not None and wt != w2:
+        kind = _weight(weight, "weight", dim, dev)
+        if post_weight is not None and w_kind is not kind:
             raise ValueError("post_weight, weight: expected one type")
-        wt = w2
+        w_kind = kind
         wp = weight.data_ptr()
-        if out is None:
-            out = _torch.empty(shape, dtype=kind, device=residual.device)
-            o_row, op = dim, out.data_ptr()
+        if out is not None:
+            o_kind = out.dtype
+        elif dtype is not None:
+            o_kind = replica._torch_type(replica._code(dtype, replica._FLOATS, "dtype"))
         else:
-            o_row, op = _rows(out, "out", kind, dev, shape), out.data_ptr()
+            o_kind = r_kind if y is None else y_kind
+        kinds += [w_kind, o_kind]
     elif out is not None:
         raise ValueError("out: expected a weight")
-    else:
-        o_row = op = 0
-    if residual_out is None and y is not None:
-        residual_out = _torch.empty(shape, dtype=stream_dtype, device=residual.device)
-        ro_row, rp = dim, residual_out.data_ptr()
-    elif residual_out is not None:
-        ro_row, rp = _rows(residual_out, "residual_out", stream_dtype, dev, shape), residual_out.data_ptr()
-    else:
-        ro_row = rp = 0
+    kind = f32
+    for k in kinds:
+        if k is not f32:
+            if replica._code(k, replica._FLOATS, "y") and kind is not f32 and k is not kind:
+                raise ValueError(f"types: expected float32 and one of 16 bits, got {kind} and {k}")
+            kind = k
+    if gate is not None and gate.dtype is not kind:
+        raise ValueError(f"gate: expected {kind}, got {gate.dtype}")
+    if residual_out is not None:
+        ro_row = _rows(residual_out, "residual_out", r_kind, dev, shape)
+    elif y is not None:
+        residual_out = _torch.empty(shape, dtype=r_kind, device=residual.device)
+        ro_row = dim
+    elif weight is None:
+        raise ValueError("y, weight: expected at least one of them")
+    if residual_out is not None:
+        rp = residual_out.data_ptr()
+    if weight is not None:
         if out is None:
-            raise ValueError("y, weight: expected at least one of them")
+            out = _torch.empty(shape, dtype=o_kind, device=residual.device)
+            o_row = dim
+        else:
+            o_row = _rows(out, "out", o_kind, dev, shape)
+        op = out.data_ptr()
     if rows:
         err = lib.tre_block_norm(
-            BLOCK.pack(code, _codes[stream_dtype], F32 if wt is None else wt, rows, dim, residual.data_ptr(),
-                       r_row, yp, y_row, pp, gp, g_row, g_col, scale, eps, wp, rp, ro_row, op, o_row),
+            BLOCK.pack(_codes[kind], _codes[y_kind], _codes[r_kind], _codes[w_kind], _codes[o_kind], rows, dim,
+                       residual.data_ptr(), r_row, yp, y_row, pp, gp, g_row, g_col, scale, eps, wp, rp,
+                       ro_row, op, o_row),
             tre._stream(None))
         if err:
             tre._check("tre_block_norm", err)
@@ -184,7 +198,7 @@ def tre_route(logits, top, scores="softmax", bias=None, groups=1, top_groups=1, 
     rows, experts = logits.shape
     bp = 0
     if bias is not None:
-        if _weight(bias, "bias", experts, dev, _torch.float32) != F32:
+        if _weight(bias, "bias", experts, dev) is not _torch.float32:
             raise ValueError("bias: expected float32")
         bp = bias.data_ptr()
     if group_best is None:
@@ -259,36 +273,45 @@ class Weights4:
         self.tensors = (self.packed,)
 
 
-def _operand(x, what, w, dev):
-    """Row stride of rows that w is multiplied with."""
-    row = _rows(x, what, w.dtype, dev)
+def _operand(x, what, w, dev, dtype):
+    """Row stride of rows of dtype that w is multiplied with."""
+    row = _rows(x, what, dtype, dev)
     if x.shape[1] != w.k:
         raise ValueError(f"{what}: expected rows of {w.k} elements, got {x.shape[1]}")
     if w.packed.get_device() != dev:
         raise ValueError(f"{what}: must be on the device of the weights")
-    if x.shape[0] < 2 and row % 8:                        # (no other row is looked at)
-        row = w.k
-    return row
+    return w.k if x.shape[0] < 2 else row                 # (no other row is looked at)
 
 
 def tre_linear4(x, w, out=None, diag=None, stream=None):
     """x [rows][k] times the transpose of w (Weights4 of one matrix): [rows][n]; of a gated w
-    silu(its first half) * its second half, [rows][n/2]."""
+    silu(its first half) * its second half, [rows][n/2]. x of w's type, or float32, which out
+    is then too."""
     if stream is not None:
         return replica._on(stream, tre_linear4, x, w, out, diag)
     lib = _ready()
     dev = _here(x, "x")
-    row = _operand(x, "x", w, dev)
+    f32 = x.dtype is _torch.float32
+    kind = _torch.float32 if f32 else w.dtype
+    row = _operand(x, "x", w, dev, kind)
     if w.experts != 1:
         raise ValueError(f"w: expected one matrix, got {w.experts}")
     rows = x.shape[0]
     shape = (rows, w.out)
     if out is None:
-        out = _torch.empty(shape, dtype=w.dtype, device=x.device)
+        out = _torch.empty(shape, dtype=kind, device=x.device)
         o_row = w.out
     else:
-        o_row = _rows(out, "out", w.dtype, dev, shape)
-    err = lib.tre_linear4(w.handle, rows, x.data_ptr(), row, out.data_ptr(), o_row, _diag(diag), tre._stream(None))
+        o_row = _rows(out, "out", kind, dev, shape)
+    at = LINEAR.pack(F32 if f32 else w.code, rows, x.data_ptr(), row, out.data_ptr(), o_row)
+    size, s, dg = C.c_size_t(0), tre._stream(None), _diag(diag)
+    ws = out                       # (a call that needs none still wants an address)
+    if f32:
+        err = lib.tre_linear4(w.handle, at, None, size, dg, s)
+        if err:
+            tre._check("tre_linear4", err)
+        ws = _torch.empty(size.value, dtype=_torch.uint8, device=x.device)
+    err = lib.tre_linear4(w.handle, at, ws.data_ptr() or 256, size, dg, s)
     if err:
         tre._check("tre_linear4", err)
     return out
@@ -302,7 +325,7 @@ def tre_experts(x, ids, weights, w1, w2, out=None, diag=None, stream=None):
         return replica._on(stream, tre_experts, x, ids, weights, w1, w2, out, diag)
     lib = _ready()
     dev = _here(x, "x")
-    row = _operand(x, "x", w1, dev)
+    row = _operand(x, "x", w1, dev, w1.dtype)
     if not w1.gated or w2.gated:
         raise ValueError("w1, w2: expected a gated and a plain set of matrices")
     if w1.dtype is not w2.dtype or w1.experts != w2.experts or w2.k != w1.out or w2.packed.get_device() != dev:
