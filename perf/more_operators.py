@@ -273,10 +273,14 @@ def run_own(s):
     if op in ("norm", "block"):
         how = dict(post_weight=s.get("post_weight"), gate=s.get("gate"), scale=c["scale"],
                    weight=s["weight"], eps=EPS)
-        r, n = tre.tre_block_norm(s["residual"], s["y"], **how)
-        if op == "block":
-            h = tre.tre_linear4(n, s["w1_own"])
-            r, n = tre.tre_block_norm(r, tre.tre_linear4(h, s["w2_own"]), **how)
+        if op == "norm":
+            r, n = tre.tre_block_norm(s["residual"], s["y"], **how)
+            return {"residual": r, "out": n}
+        # (a residual stream in 32 bits has its block's rows in 32 bits too)
+        r, n = tre.tre_block_norm(s["residual"], s["y"], dtype=c["stream"], **how)
+        h = tre.tre_linear4(n, s["w1_own"])
+        y = tre.tre_linear4(h, s["w2_own"])
+        r, n = tre.tre_block_norm(r, y, dtype=c["dtype"], **how)
         return {"residual": r, "out": n}
     if op == "linear":
         return {"out": tre.tre_linear4(s["x"], s["w_own"])}
