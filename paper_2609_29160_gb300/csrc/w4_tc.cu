@@ -71,38 +71,16 @@ __device__ __forceinline__ bool unit_at(const TcArgs& a, int u, Unit& w) {
   return true;
 }
 
-// Waits of a warp for arrivals that may come from the other block of the pair.
-__device__ __forceinline__ bool pair_poll(uint64_t* b, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2; "
-      "selp.b32 %0, 1, 0, p; }"
-      : "=r"(ok)
-      : "r"(smem_of(b)), "r"(parity)
-      : "memory");
-  return ok;
-}
-__device__ __forceinline__ bool pair_wait(uint64_t* b, uint32_t parity, volatile int* dead) {
-  bool ok = pair_poll(b, parity);
-  if (!ok) {
-    const long long from = clock64();
-    while (!(ok = pair_poll(b, parity))) {
-      if (*dead) break;
-      if (clock64() - from > kWaitClocks) {
-        *dead = 1;
-        break;
-      }
-    }
-  }
-  return __all_sync(0xffffffffu, ok);
-}
-// A warp's arrival at a barrier of the pair's first block.
+// A warp's arrival at a barrier of the pair's first block. What it announces has been ordered
+// already, for the unit that will read it: rows written to shared memory by a proxy fence,
+// tensor memory read by a wait. (A release for the cluster takes a microsecond here, which a
+// warp would spend at every stage.)
 __device__ __forceinline__ void arrive_first(uint64_t* b) {
   __syncwarp();
   if ((threadIdx.x & 31) == 0)
     asm volatile(
         "{ .reg .b32 a; mapa.shared::cluster.u32 a, %0, 0;\n"
-        "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [a]; }" ::"r"(smem_of(b))
+        "mbarrier.arrive.shared::cluster.b64 _, [a]; }" ::"r"(smem_of(b))
         : "memory");
 }
 __device__ __forceinline__ void commit_pair(uint64_t* b) {
@@ -407,13 +385,13 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
 #pragma unroll 1
         for (int c = 0; c < w.chunks; ++c, ++n) {
           const uint32_t s = n % kStages;
-          if (!(alive = pair_wait(full + s, (n / kStages) & 1, dead))) break;
+          if (!(alive = bar_wait(full + s, (n / kStages) & 1, dead))) break;
           const uint32_t x = operand(smem_of(sm + s * kBytesA), 16), y = operand(smem_of(sm + kAtB + s * kBytesB), 16);
 #pragma unroll
           for (int h = 0; h < PER; ++h) {
             const uint32_t buf = groups & 1;
             const bool fresh = STAGES_OF == 1 || (c & 1) == 0;
-            if (fresh && !(alive = pair_wait(sum_empty + buf, ((groups >> 1) & 1) ^ 1, dead))) break;
+            if (fresh && !(alive = bar_wait(sum_empty + buf, ((groups >> 1) & 1) ^ 1, dead))) break;
             tmem_after();
             const bool whole_group = STAGES_OF == 1 || (c & 1) == 1;
             if (one_lane()) {
