@@ -138,11 +138,11 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
     *dead = 0;
     for (int k = 0; k < kRaws; ++k) {
       bar_init(raw_full + k, 1);
-      bar_init(raw_empty + k, kCodeWarps);
+      bar_init(raw_empty + k, 1);
     }
     for (int k = 0; k < kStages; ++k) {
       bar_init(x_full + k, 1);
-      bar_init(full + k, 2 * kCodeWarps);
+      bar_init(full + k, 2);
       bar_init(empty + k, 1);
     }
     for (int k = 0; k < 2; ++k) {
@@ -161,7 +161,7 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
   // Registers move once, from the launch's 4 x 128 (in groups of four warps).
   if (warp < kScaleWarps) {
     // ---- sums of groups ----------------------------------------------------------
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
     const int quarter = warp & 3, half = warp >> 2, r16 = lane & 15;
     const int g = (r16 & 3) << 1 | (r16 >> 2 & 1);       // turn(g) == r16 & 7
     uint32_t n = 0;                                      // groups so far
@@ -254,63 +254,54 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
     }
   } else if (warp < kCodeWarp + kCodeWarps) {
     // ---- codes to an operand -------------------------------------------------------
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    // A warp takes every fourth stage: what a stage waits for (its codes, its place, its rows
+    // of x) is some 900 cycles one after the other, twice what its products take.
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     const int cw = warp - kCodeWarp, g = lane >> 2, t = lane & 3;
     uint32_t n = 0;                                      // stages so far
     bool alive = true;
     for (int i = pair; alive && unit_at(a, i, u); i += pairs) {
-      const int tile0 = (2 * u.block + side) * 8 + 2 * cw;
-      const uint32_t* zero[2];
+      const int tile0 = (2 * u.block + side) * 8;
+      const uint32_t* zeros = w.zeros + ((int64_t)u.expert * w.tiles * w.groups) * 8 + g;
+#pragma unroll 1
+      for (int c = (cw - n) & 3; c < w.chunks; c += kCodeWarps) {
+        const uint32_t k = n + c, s = k % kStages, r = k % kRaws;
+        uint32_t z[8][PER];
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
-        zero[x] = w.zeros + (((int64_t)u.expert * w.tiles + min(tile0 + x, w.tiles - 1)) * w.groups) * 8 + g;
-      uint32_t ahead[2][PER];
-      auto look = [&](int c) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int x = 0; x < 8; ++x)
 #pragma unroll
           for (int y = 0; y < PER; ++y)
-            ahead[x][y] = w.zeros ? zero[x][(c * 64 / GROUP + y) * 8] : Whole<S>::bits + 0x00080008u;
-      };
-      look(0);
-#pragma unroll 1
-      for (int c = 0; c < w.chunks; ++c, ++n) {
-        const uint32_t s = n % kStages, r = n % kRaws;
-        if (!(alive = bar_wait(raw_full + r, (n / kRaws) & 1, dead))) break;
-        uint4 code[2];
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-          code[x] = reinterpret_cast<const uint4*>(sm + kAtRaw + r * kBytesRaw)[(2 * cw + x) * 32 + lane];
-        bar_arrive_warp(raw_empty + r);
-        uint32_t z[2][PER];
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int y = 0; y < PER; ++y) z[x][y] = zero_as<T, S>(ahead[x][y]);
-        if (c + 1 < w.chunks) look(c + 1);
-        if (!(alive = bar_wait(empty + s, ((n / kStages) & 1) ^ 1, dead))) break;
+            z[x][y] = zero_as<T, S>(
+                w.zeros ? zeros[((int64_t)min(tile0 + x, w.tiles - 1) * w.groups + (c * 64 / GROUP + y)) * 8]
+                        : Whole<S>::bits + 0x00080008u);
+        if (!(alive = bar_wait(raw_full + r, (k / kRaws) & 1, dead))) break;
+        if (!(alive = bar_wait(empty + s, ((k / kStages) & 1) ^ 1, dead))) break;
+        const uint4* codes = reinterpret_cast<const uint4*>(sm + kAtRaw + r * kBytesRaw) + lane;
         uint8_t* to = sm + s * kBytesA;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int row = (2 * cw + x) * 16 + turn(g);
+        for (int x = 0; x < 8; ++x) {
+          const uint4 code = codes[x * 32];
+          const int row = x * 16 + turn(g);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {                  // 32 elements each
             const uint32_t zz = z[x][h * (PER - 1)];
             uint32_t p[4], q[4];
-            whole<T>(h ? code[x].z : code[x].x, both_lo(zz), both_hi(zz), p);
-            whole<T>(h ? code[x].w : code[x].y, both_lo(zz), both_hi(zz), q);
+            whole<T>(h ? code.z : code.x, both_lo(zz), both_hi(zz), p);
+            whole<T>(h ? code.w : code.y, both_lo(zz), both_hi(zz), q);
             const int at = ((4 * h + t) ^ (row & 7)) << 4;
             *reinterpret_cast<uint4*>(to + row * 128 + at) = make_uint4(p[0], p[2], q[0], q[2]);
             *reinterpret_cast<uint4*>(to + (row + 8) * 128 + at) = make_uint4(p[1], p[3], q[1], q[3]);
           }
         }
+        bar_arrive_warp(raw_empty + r);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        if (!(alive = bar_wait(x_full + s, (n / kStages) & 1, dead))) break;
+        if (!(alive = bar_wait(x_full + s, (k / kStages) & 1, dead))) break;
         arrive_first(full + s);
       }
+      n += w.chunks;
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp == kRowWarp) {
       // ---- rows of x ---------------------------------------------------------------
       uint32_t n = 0;
