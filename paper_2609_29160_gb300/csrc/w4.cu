@@ -12,16 +12,17 @@ namespace {
 // Layout
 // ---------------------------------------------------------------------------
 struct Layout {
-  int64_t tiles, chunks, groups;
+  int64_t tiles, blocks, chunks, groups;
   size_t codes, scales, zeros, bytes;      // where each begins, and the whole
 };
 Layout layout_of(int experts, int n, int k, int group, bool gated, bool zeros) {
   Layout l;
   l.tiles = gated ? (n / 2 + 15) / 16 * 2 : ((int64_t)n + 31) / 32 * 2;
+  l.blocks = (l.tiles + 7) / 8;
   l.chunks = ((int64_t)k + 63) / 64;
   l.groups = l.chunks * 64 / group > 0 ? l.chunks * 64 / group : 1;
   Arena a(nullptr);
-  a.take<uint4>((size_t)experts * l.tiles * l.chunks * 32);
+  a.take<uint4>((size_t)experts * l.blocks * l.chunks * 256);
   l.codes = 0;
   l.scales = (a.off + 255) & ~size_t(255);
   a.take<uint32_t>((size_t)experts * l.tiles * l.groups * 8);
@@ -35,7 +36,7 @@ struct PackArgs {
   const uint8_t *codes, *zeros;
   const uint16_t* scales;
   uint32_t *to_codes, *to_scales, *to_zeros;
-  int64_t tiles, chunks, groups;
+  int64_t tiles, blocks, chunks, groups;
   int32_t n, k, group;
   bool gated, bf16;
 };
@@ -53,11 +54,11 @@ __global__ void k_w4_codes(PackArgs a, int64_t words) {
   const int64_t at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (at >= words) return;
   const int s = at & 3, lane = (at >> 2) & 31, g = lane >> 2, t = lane & 3;
-  const int64_t chunk = (at >> 7) % a.chunks, tile = (at >> 7) / a.chunks;
-  const int64_t e = tile / a.tiles;
+  const int64_t block = (at >> 10) / a.chunks, chunk = (at >> 10) - block * a.chunks;
+  const int64_t e = block / a.blocks, tile = block % a.blocks * 8 + (at >> 7 & 7);
   uint32_t w = 0;
   for (int i = 0; i < 4; ++i) {
-    const int row = row_of(a, tile % a.tiles, turn(g) + 8 * (i & 1));
+    const int row = row_of(a, tile, turn(g) + 8 * (i & 1));
     const int64_t k = chunk * 64 + 32 * (s >> 1) + 8 * t + 4 * (s & 1) + 2 * (i >> 1);
     if (row < 0 || k >= a.k) continue;
     const uint32_t b = a.codes[((e * a.n + row) * a.k + k) / 2];
@@ -136,10 +137,10 @@ __global__ void __launch_bounds__(kFewWarps * 32) k_w4_few(const __grid_constant
     slot = p.plan.slots[blockIdx.y];
   }
   const int64_t tile = (int64_t)slot.expert * w.tiles + 2 * pair;
-  const uint4* codes = w.codes + tile * w.chunks * 32 + lane;
+  const uint4* codes[2] = {w.codes_of(slot.expert, 2 * pair) + lane, w.codes_of(slot.expert, 2 * pair + 1) + lane};
   const uint32_t* scales = w.scales + tile * w.groups * 8 + g;
   const uint32_t* zeros = w.zeros + tile * w.groups * 8 + g;
-  const int64_t next_codes = (int64_t)w.chunks * 32, next_groups = (int64_t)w.groups * 8;
+  const int64_t next_groups = (int64_t)w.groups * 8;
   for (int from = 0; from < slot.count; from += 8 * NB) {
     // rows of x of this lane's columns; null: none
     const T* x[NB];
@@ -166,7 +167,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) k_w4_few(const __grid_constant
       for (int r = 0; r < 2; ++r)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-          c[r][h] = 2 * kb + h < w.chunks ? load_once(codes + r * next_codes + (2 * kb + h) * 32)
+          c[r][h] = 2 * kb + h < w.chunks ? load_once(codes[r] + (int64_t)(2 * kb + h) * kNextChunk)
                                           : make_uint4(0, 0, 0, 0);
     };
     const int blocks = (w.chunks + 1) / 2;
@@ -470,6 +471,7 @@ bool w4_args(const tre_w4* w, W4Args& a) {
   a.n = w->n;
   a.k = w->k;
   a.tiles = (int32_t)l.tiles;
+  a.blocks = (int32_t)l.blocks;
   a.chunks = (int32_t)l.chunks;
   a.groups = (int32_t)l.groups;
   a.gated = w->gated != 0;
@@ -503,6 +505,7 @@ tre_status tre_w4_pack(const tre_w4_source* f, void* packed, size_t* bytes, tre_
   a.to_scales = reinterpret_cast<uint32_t*>(p + l.scales);
   a.to_zeros = f->zeros ? reinterpret_cast<uint32_t*>(p + l.zeros) : nullptr;
   a.tiles = l.tiles;
+  a.blocks = l.blocks;
   a.chunks = l.chunks;
   a.groups = l.groups;
   a.n = f->n;
@@ -510,7 +513,7 @@ tre_status tre_w4_pack(const tre_w4_source* f, void* packed, size_t* bytes, tre_
   a.group = f->group;
   a.gated = f->gated != 0;
   a.bf16 = f->dtype == TRE_BF16;
-  const int64_t words = f->experts * l.tiles * l.chunks * 128, pairs = f->experts * l.tiles * l.groups * 8;
+  const int64_t words = f->experts * l.blocks * l.chunks * 1024, pairs = f->experts * l.tiles * l.groups * 8;
   if ((words + 255) / 256 > 2147483647) return TRE_EINVAL;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   k_w4_codes<<<(unsigned)((words + 255) / 256), 256, 0, s>>>(a, words);

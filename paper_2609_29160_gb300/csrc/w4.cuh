@@ -1,8 +1,8 @@
 // Matrices in 4 bits as the products read them, and what both kernels of the products
 // share.
 //
-// A tile is 16 rows by 64 elements of k, 512 bytes, the tiles of 16 rows one after the other
-// along k. Lane (g, t) = (lane / 4, lane % 4) of a warp has 16 bytes of it: word s holds, of
+// A tile is 16 rows by 64 elements of k, 512 bytes; eight tiles of 128 rows lie together (one
+// copy), those blocks one after the other along k. Lane (g, t) = (lane / 4, lane % 4) of a warp has 16 bytes of it: word s holds, of
 // rows r = turn(g) and r + 8, the elements k = 32 (s / 2) + 8 t + 4 (s % 2) + 0..3, as
 //   half-byte i      : row r + 8 (i % 2), element 2 (i / 2)
 //   half-byte i + 4  : the same row, the element after it        (i = 0..3)
@@ -27,9 +27,14 @@ namespace tre {
 struct W4Args {
   const uint4* codes;
   const uint32_t *scales, *zeros;      // zeros may be null: 8
-  int32_t experts, n, k, tiles, chunks, groups;   // groups: those of a row, to whole chunks
-  bool gated;
+  int32_t experts, n, k, tiles, blocks, chunks, groups;   // blocks of eight tiles, of an expert;
+  bool gated;                                              // groups of a row, to whole chunks
+  // tile `tile` of expert e along k: from here on, kNextChunk further for the next 64 elements
+  __device__ __forceinline__ const uint4* codes_of(int e, int tile) const {
+    return codes + (((int64_t)e * blocks + (tile >> 3)) * chunks * 8 + (tile & 7)) * 32;
+  }
 };
+constexpr int kNextChunk = 8 * 32;     // in pieces of 16 bytes
 
 __host__ __device__ constexpr int turn(int g) { return g >> 1 | (g & 1) << 2; }
 

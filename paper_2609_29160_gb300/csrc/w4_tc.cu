@@ -321,7 +321,7 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
         for (int c = 0; c < w.chunks; ++c, ++n) {
           const uint32_t s = n % kStages;
           if (!(alive = bar_wait(empty + s, ((n / kStages) & 1) ^ 1, dead))) break;
-          if (lane == 0) bar_expect(x_full + s, mine * 128);
+          if (lane == 0) bar_expect(x_full + s, (a.box ? (mine + a.box - 1) / a.box * a.box : mine) * 128);
           __syncwarp();
           const uint32_t to = smem_of(sm + kAtB + s * kBytesB);
           if (a.box == 0) {
@@ -349,20 +349,20 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
       uint32_t n = 0;
       bool alive = true;
       for (int i = pair; alive && unit_at(a, i, u); i += pairs) {
-        const int tile = min((2 * u.block + side) * 8 + (lane & 7), w.tiles - 1);
-        const uint4* from = w.codes + ((int64_t)u.expert * w.tiles + tile) * w.chunks * 32;
+        // (past the last block of 128 rows: the last again, whose sums are not written)
+        const uint4* from = w.codes_of(u.expert, min(2 * u.block + side, w.blocks - 1) * 8);
 #pragma unroll 1
         for (int c = 0; c < w.chunks; ++c, ++n) {
           const uint32_t r = n % kRaws;
           if (!(alive = bar_wait(raw_empty + r, ((n / kRaws) & 1) ^ 1, dead))) break;
-          if (lane == 0) bar_expect(raw_full + r, kBytesRaw);
-          __syncwarp();
-          if (lane < 8)
+          if (one_lane()) {
+            bar_expect(raw_full + r, kBytesRaw);
             asm volatile(
-                "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], 512, [%2];" ::"r"(
-                    smem_of(sm + kAtRaw + r * kBytesRaw) + lane * 512),
-                "l"(from + c * 32), "r"(smem_of(raw_full + r))
+                "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                    smem_of(sm + kAtRaw + r * kBytesRaw)),
+                "l"(from + (int64_t)c * kNextChunk), "n"(kBytesRaw), "r"(smem_of(raw_full + r))
                 : "memory");
+          }
           __syncwarp();
         }
       }
@@ -471,7 +471,14 @@ cudaError_t launch_w4_tc(int dtype, int scale_dtype, int group, const ProductArg
     }
     tiles = (rows + a.tile - 1) / a.tile;
   }
-  a.box = p.gather ? 0 : p.plan.order ? 16 : a.tile / 2;
+  // (a copy is issued in some hundred cycles, whatever its size: few of them, of a power of
+  // two so that they fit)
+  a.box = a.tile / 2;
+  if (p.plan.order) {
+    a.box = 16;
+    while (a.box < 128 && a.box * 2 * tiles < rows) a.box *= 2;
+  }
+  if (p.gather) a.box = 0;
   if (tiles * a.row_blocks > 2000000000) return cudaErrorNotSupported;
   CUtensorMap map;
   memset(&map, 0, sizeof(map));
