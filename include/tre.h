@@ -773,8 +773,7 @@ typedef struct {
  * with w1 gated and act as in tre_linear4. An id below zero adds nothing; one past
  * the last expert adds nothing and is counted in diag.dropped_range; a token
  * without experts gives zeros. The same expert may come twice. act's output is
- * rounded to dtype (an operand of the second product has no more bits), each
- * expert's output to dtype where there are many tokens, y once. */
+ * rounded to dtype (an operand of the second product has no more bits), and y once. */
 tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* tokens, void* ws,
                        size_t* ws_bytes, tre_diag* diag, tre_stream stream);
 

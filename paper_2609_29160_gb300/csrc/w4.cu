@@ -375,7 +375,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const int32_t* ids, int64
   if (diag) warp_add_counter(reinterpret_cast<unsigned long long*>(&diag->dropped_range), past);
   __syncthreads();
   const int mine = count[tid];
-  const int tiles = (mine + kTileTokens - 1) / kTileTokens;
+  const int tiles = (mine + plan.piece - 1) / plan.piece;
   int v[3] = {mine, mine > 0, tiles};                // places, slots, tiles before this expert
 #pragma unroll
   for (int x = 0; x < 3; ++x) {
@@ -420,32 +420,27 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const int32_t* ids, int64
   }
 }
 
-// y[t] = sum over j, in order, of weights[t][j] * each[t * top + j]; a block a token.
-template <class T, class E>
-__global__ void k_combine(const E* each, const int32_t* ids, const float* weights, int experts,
-                          int top, int dim, T* y, int64_t y_row) {
+// y[t] = sum over j, in order, of weights[t][j] * each[t * top + j].
+template <class T>
+__global__ void __launch_bounds__(kRowThreads) k_combine(const float* each, const int32_t* ids,
+                                                         const float* weights, int experts, int top,
+                                                         int dim, T* y, int64_t y_row) {
   const int64_t t = blockIdx.x;
-  const int i = blockIdx.y * blockDim.x + threadIdx.x;
+  const int i = blockIdx.y * kRowThreads + threadIdx.x;
   if (i >= dim) return;
   float sum = 0.f;
   for (int j = 0; j < top; ++j) {
     const int e = ids[t * top + j];
-    if (e >= 0 && e < experts) sum = fmaf(weights[t * top + j], (float)each[(t * top + j) * dim + i], sum);
+    if (e >= 0 && e < experts) sum = fmaf(weights[t * top + j], each[(t * top + j) * dim + i], sum);
   }
   y[t * y_row + i] = T(sum);
 }
 
 template <class T>
-cudaError_t launch_combine(const void* each, bool f32, const tre_tokens* t, int experts, int dim,
-                           cudaStream_t s) {
-  const int threads = 256;
-  const dim3 grid((unsigned)t->n_rows, (unsigned)((dim + threads - 1) / threads));
-  if (f32)
-    k_combine<T, float><<<grid, threads, 0, s>>>(static_cast<const float*>(each), t->ids, t->weights,
-                                                 experts, t->top, dim, static_cast<T*>(t->y), t->y_row);
-  else
-    k_combine<T, T><<<grid, threads, 0, s>>>(static_cast<const T*>(each), t->ids, t->weights, experts,
-                                             t->top, dim, static_cast<T*>(t->y), t->y_row);
+cudaError_t launch_combine(const float* each, const tre_tokens* t, int experts, int dim, cudaStream_t s) {
+  const dim3 grid((unsigned)t->n_rows, (unsigned)((dim + kRowThreads - 1) / kRowThreads));
+  k_combine<T><<<grid, kRowThreads, 0, s>>>(each, t->ids, t->weights, experts, t->top, dim,
+                                            static_cast<T*>(t->y), t->y_row);
   return cudaGetLastError();
 }
 
@@ -591,16 +586,16 @@ tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* t, 
   const int64_t pairs = (int64_t)t->n_rows * t->top;
   const int inner = w2->k, inner_row = (inner + 7) / 8 * 8, dim = w2->n;
   const int64_t slots = std::min<int64_t>(w1->experts, pairs);
-  // Few tokens an expert: k_w4_few, whose outputs are small enough to be kept in 32 bits.
   const bool few = pairs <= kFewTokens * slots;
   Arena arena(ws);
   PlanArgs plan;
   plan.order = arena.take<int32_t>(pairs);
   plan.slots = arena.take<Slot>(slots);
-  plan.tiles = arena.take<Slot>(slots + pairs / kTileTokens);
+  plan.piece = pairs <= 128 * slots ? 128 : kTileTokens;
+  plan.tiles = arena.take<Slot>(slots + pairs / plan.piece);
   plan.n = arena.take<int32_t>(2);
   uint8_t* h = arena.take<uint8_t>((size_t)pairs * inner_row * 2);
-  uint8_t* each = arena.take<uint8_t>((size_t)pairs * dim * (few ? 4 : 2));
+  float* each = arena.take<float>((size_t)pairs * dim);
   if (!ws) {
     *ws_bytes = arena.off;
     return TRE_OK;
@@ -615,17 +610,17 @@ tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* t, 
   a.gather = true;
   b.x = h;
   b.x_row = inner_row;
-  b.y = each;
+  b.y = reinterpret_cast<uint8_t*>(each);
   b.y_row = dim;
   b.scatter = true;
-  b.y_f32 = few;
+  b.y_f32 = true;
   a.plan = b.plan = plan;
   a.n_rows = b.n_rows = t->n_rows;
   a.top = b.top = t->top;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   k_plan<<<1, kPlanThreads, 0, s>>>(t->ids, pairs, w1->experts, plan, diag);
   cudaError_t e = cudaGetLastError();
-  const int64_t columns = (pairs + slots - 1) / slots * 2, tiles = slots + pairs / kTileTokens;
+  const int64_t columns = (pairs + slots - 1) / slots * 2, tiles = slots + pairs / plan.piece;
   auto product = [&](const ProductArgs& p, const tre_w4* w, int64_t rows) {
     if (!few) {
       const cudaError_t x = launch_w4_tc(t->dtype, t->dtype, w->group, p, rows, tiles, diag, s);
@@ -636,8 +631,8 @@ tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* t, 
   if (!e) e = product(a, w1, t->n_rows);
   if (!e) e = product(b, w2, pairs);
   if (!e)
-    e = t->dtype == TRE_BF16 ? launch_combine<__nv_bfloat16>(each, few, t, w1->experts, dim, s)
-                             : launch_combine<__half>(each, few, t, w1->experts, dim, s);
+    e = t->dtype == TRE_BF16 ? launch_combine<__nv_bfloat16>(each, t, w1->experts, dim, s)
+                             : launch_combine<__half>(each, t, w1->experts, dim, s);
   return e == cudaSuccess ? TRE_OK : TRE_ECUDA;
 }
 

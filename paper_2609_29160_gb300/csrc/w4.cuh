@@ -84,8 +84,9 @@ struct Slot {
 struct PlanArgs {
   int32_t* order;                      // [pairs]
   Slot* slots;                         // experts that have any
-  Slot* tiles;                         // their places in pieces of up to kTileTokens
+  Slot* tiles;                         // their places in pieces of up to `piece`
   int32_t* n;                          // [2]: how many slots, tiles
+  int32_t piece;
 };
 constexpr int kTileTokens = 256;       // columns of a product on the tensor cores
 

@@ -28,13 +28,19 @@
 namespace tre {
 namespace {
 
-constexpr int kStages = 6, kRaws = 8;
-constexpr int kBytesA = 128 * 128, kBytesB = 128 * 128, kBytesRaw = 4096;
-constexpr int kAtB = kStages * kBytesA, kAtRaw = kAtB + kStages * kBytesB;
-constexpr int kAtBar = kAtRaw + kRaws * kBytesRaw;
-constexpr int kBars = 2 * kRaws + 3 * kStages + 4;
-constexpr int kSmem = kAtBar + kBars * 8 + 16;
-static_assert(kSmem <= 227 * 1024, "shared memory of a block");
+// Shared memory of a block for units of up to WIDTH rows of x. A stage of the operand lasts
+// from its last product to its next, through the turning of codes, an arrival at the other
+// block and the products themselves, about 0.9 us; one of x's rows also waits for its copy,
+// about 2 us: hence more of them.
+template <int WIDTH> struct Ring {
+  static constexpr int A = WIDTH == 256 ? 4 : 6, B = WIDTH == 256 ? 8 : 12, RAW = 8;
+  static constexpr int BYTES_A = 128 * 128, BYTES_B = WIDTH / 2 * 128, BYTES_RAW = 4096;
+  static constexpr int SUMS = 512 / WIDTH;             // accumulators
+  static constexpr int AT_B = A * BYTES_A, AT_RAW = AT_B + B * BYTES_B, AT_BAR = AT_RAW + RAW * BYTES_RAW;
+  static constexpr int BARS = 2 * (RAW + A + B + SUMS);
+  static constexpr int SMEM = AT_BAR + BARS * 8 + 16;
+  static_assert(SMEM <= 227 * 1024, "shared memory of a block");
+};
 constexpr int kScaleWarps = 8, kCodeWarp = 8, kCodeWarps = 4, kRowWarp = 12, kRawWarp = 13, kMmaWarp = 14;
 constexpr int kThreads = 512;
 
@@ -46,7 +52,7 @@ struct Unit {
 
 struct TcArgs {
   ProductArgs p;
-  int32_t row_blocks, tile;            // tile: rows of x of a unit, where there is no plan
+  int32_t row_blocks, tile;            // tile: most rows of x of a unit
   int32_t box;                         // rows of x of one copy; 0: gathered by four
 };
 
@@ -71,6 +77,12 @@ __device__ __forceinline__ bool unit_at(const TcArgs& a, int u, Unit& w) {
   return true;
 }
 
+// The same barrier of the pair's first block
+__device__ __forceinline__ uint32_t first_of(uint64_t* b) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_of(b)));
+  return r;
+}
 // A warp's arrival at a barrier of the pair's first block. What it announces has been ordered
 // already, for the unit that will read it: rows written to shared memory by a proxy fence,
 // tensor memory read by a wait. (A release for the cluster takes a microsecond here, which a
@@ -78,10 +90,7 @@ __device__ __forceinline__ bool unit_at(const TcArgs& a, int u, Unit& w) {
 __device__ __forceinline__ void arrive_first(uint64_t* b) {
   __syncwarp();
   if ((threadIdx.x & 31) == 0)
-    asm volatile(
-        "{ .reg .b32 a; mapa.shared::cluster.u32 a, %0, 0;\n"
-        "mbarrier.arrive.shared::cluster.b64 _, [a]; }" ::"r"(smem_of(b))
-        : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(first_of(b)) : "memory");
 }
 __device__ __forceinline__ void commit_pair(uint64_t* b) {
   asm volatile(
@@ -111,7 +120,7 @@ __device__ __forceinline__ void add_scaled(float* acc, const uint32_t* v, float 
   acc[1] = __uint_as_float(x[1]);
 }
 
-template <class T, class S, int GROUP>
+template <class T, class S, int GROUP, int WIDTH>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap rows, tre_diag* diag) {
   extern __shared__ __align__(1024) uint8_t sm[];
@@ -122,11 +131,14 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
   const int side = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   const W4Args& w = a.p.w;
 
-  uint64_t* bars = reinterpret_cast<uint64_t*>(sm + kAtBar);
-  uint64_t *raw_full = bars, *raw_empty = raw_full + kRaws, *x_full = raw_empty + kRaws,
-           *full = x_full + kStages, *empty = full + kStages, *sum_full = empty + kStages,
-           *sum_empty = sum_full + 2;
-  uint32_t* tmem_at = reinterpret_cast<uint32_t*>(bars + kBars);
+  using R = Ring<WIDTH>;
+  // What products need (a_full, b_full) and free accumulators (sum_empty) are barriers of the
+  // pair's first block, the others each block's own.
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sm + R::AT_BAR);
+  uint64_t *raw_full = bars, *raw_empty = raw_full + R::RAW, *a_full = raw_empty + R::RAW,
+           *a_empty = a_full + R::A, *b_full = a_empty + R::A, *b_empty = b_full + R::B,
+           *sum_full = b_empty + R::B, *sum_empty = sum_full + R::SUMS;
+  uint32_t* tmem_at = reinterpret_cast<uint32_t*>(bars + R::BARS);
   volatile int* dead = reinterpret_cast<volatile int*>(tmem_at + 1);
   if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(
@@ -136,16 +148,19 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
   }
   if (tid == 0) {
     *dead = 0;
-    for (int k = 0; k < kRaws; ++k) {
+    for (int k = 0; k < R::RAW; ++k) {
       bar_init(raw_full + k, 1);
       bar_init(raw_empty + k, 1);
     }
-    for (int k = 0; k < kStages; ++k) {
-      bar_init(x_full + k, 1);
-      bar_init(full + k, 2);
-      bar_init(empty + k, 1);
+    for (int k = 0; k < R::A; ++k) {
+      bar_init(a_full + k, 2);
+      bar_init(a_empty + k, 1);
     }
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < R::B; ++k) {
+      bar_init(b_full + k, 1);
+      bar_init(b_empty + k, 1);
+    }
+    for (int k = 0; k < R::SUMS; ++k) {
       bar_init(sum_full + k, 1);
       bar_init(sum_empty + k, 2 * kScaleWarps);
     }
@@ -182,12 +197,12 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
       for (int q = 0; q < w.groups; ++q, ++n) {
         const uint16_t bits = ahead;
         if (q + 1 < w.groups) ahead = scale[(q + 1) * 16];
-        const uint32_t buf = n & 1;
-        if (!(alive = bar_wait(sum_full + buf, (n >> 1) & 1, dead))) break;
+        const uint32_t buf = n % R::SUMS;
+        if (!(alive = bar_wait(sum_full + buf, (n / R::SUMS) & 1, dead))) break;
         tmem_after();
         float s, unused;
         unpack((uint32_t)bits, s, unused, S());
-        const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + buf * 256 + half * mine;
+        const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + buf * WIDTH + half * mine;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
           if (b * 32 >= mine) break;
@@ -254,8 +269,8 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
     }
   } else if (warp < kCodeWarp + kCodeWarps) {
     // ---- codes to an operand -------------------------------------------------------
-    // A warp takes every fourth stage: what a stage waits for (its codes, its place, its rows
-    // of x) is some 900 cycles one after the other, twice what its products take.
+    // A warp takes every fourth stage: what happens to one, step after step, takes longer than
+    // its products.
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     const int cw = warp - kCodeWarp, g = lane >> 2, t = lane & 3;
     uint32_t n = 0;                                      // stages so far
@@ -265,7 +280,7 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
       const uint32_t* zeros = w.zeros + ((int64_t)u.expert * w.tiles * w.groups) * 8 + g;
 #pragma unroll 1
       for (int c = (cw - n) & 3; c < w.chunks; c += kCodeWarps) {
-        const uint32_t k = n + c, s = k % kStages, r = k % kRaws;
+        const uint32_t k = n + c, s = k % R::A, r = k % R::RAW;
         uint32_t z[8][PER];
 #pragma unroll
         for (int x = 0; x < 8; ++x)
@@ -274,10 +289,10 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
             z[x][y] = zero_as<T, S>(
                 w.zeros ? zeros[((int64_t)min(tile0 + x, w.tiles - 1) * w.groups + (c * 64 / GROUP + y)) * 8]
                         : Whole<S>::bits + 0x00080008u);
-        if (!(alive = bar_wait(raw_full + r, (k / kRaws) & 1, dead))) break;
-        if (!(alive = bar_wait(empty + s, ((k / kStages) & 1) ^ 1, dead))) break;
-        const uint4* codes = reinterpret_cast<const uint4*>(sm + kAtRaw + r * kBytesRaw) + lane;
-        uint8_t* to = sm + s * kBytesA;
+        if (!(alive = bar_wait(raw_full + r, (k / R::RAW) & 1, dead))) break;
+        if (!(alive = bar_wait(a_empty + s, ((k / R::A) & 1) ^ 1, dead))) break;
+        const uint4* codes = reinterpret_cast<const uint4*>(sm + R::AT_RAW + r * R::BYTES_RAW) + lane;
+        uint8_t* to = sm + s * R::BYTES_A;
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
           const uint4 code = codes[x * 32];
@@ -295,8 +310,7 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
         }
         bar_arrive_warp(raw_empty + r);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        if (!(alive = bar_wait(x_full + s, (k / kStages) & 1, dead))) break;
-        arrive_first(full + s);
+        arrive_first(a_full + s);
       }
       n += w.chunks;
     }
@@ -308,6 +322,7 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
       bool alive = true;
       for (int i = pair; alive && unit_at(a, i, u); i += pairs) {
         const int mine = u.columns / 2, first = u.start + side * mine;
+        const uint32_t bytes = (a.box ? (mine + a.box - 1) / a.box * a.box : mine) * 128;
         int r[4] = {0, 0, 0, 0};
         if (a.box == 0) {
 #pragma unroll
@@ -319,31 +334,33 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
         }
 #pragma unroll 1
         for (int c = 0; c < w.chunks; ++c, ++n) {
-          const uint32_t s = n % kStages;
-          if (!(alive = bar_wait(empty + s, ((n / kStages) & 1) ^ 1, dead))) break;
-          if (lane == 0) bar_expect(x_full + s, (a.box ? (mine + a.box - 1) / a.box * a.box : mine) * 128);
+          const uint32_t s = n % R::B;
+          if (!(alive = bar_wait(b_empty + s, ((n / R::B) & 1) ^ 1, dead))) break;
+          if (side == 0 && lane == 0) bar_expect(b_full + s, 2 * bytes);
           __syncwarp();
-          const uint32_t to = smem_of(sm + kAtB + s * kBytesB);
+          const uint32_t to = smem_of(sm + R::AT_B + s * R::BYTES_B), bar = first_of(b_full + s);
           if (a.box == 0) {
             if (lane * 4 < mine)
               asm volatile(
-                  "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes "
-                  "[%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(to + lane * 512),
-                  "l"(&rows), "r"(c * 64), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(smem_of(x_full + s))
+                  "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes"
+                  ".cta_group::2 [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(to + lane * 512),
+                  "l"(&rows), "r"(c * 64), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(bar)
                   : "memory");
           } else if (lane * a.box < mine) {
             asm volatile(
-                "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
                 "[%0], [%1, {%2, %3}], [%4];" ::"r"(to + lane * a.box * 128),
-                "l"(&rows), "r"(c * 64), "r"(first + lane * a.box), "r"(smem_of(x_full + s))
+                "l"(&rows), "r"(c * 64), "r"(first + lane * a.box), "r"(bar)
                 : "memory");
           }
           __syncwarp();
         }
       }
-      // the products' arrivals that no copy waits for any more
-      for (uint32_t k = n > kStages ? n - kStages : 0; alive && k < n; ++k)
-        alive = bar_wait(empty + k % kStages, (k / kStages) & 1, dead);
+      // the products' arrivals that nothing waits for any more
+      for (uint32_t k = n > R::B ? n - R::B : 0; alive && k < n; ++k)
+        alive = bar_wait(b_empty + k % R::B, (k / R::B) & 1, dead);
+      for (uint32_t k = n > R::A ? n - R::A : 0; alive && k < n; ++k)
+        alive = bar_wait(a_empty + k % R::A, (k / R::A) & 1, dead);
     } else if (warp == kRawWarp) {
       // ---- codes -------------------------------------------------------------------
       uint32_t n = 0;
@@ -353,14 +370,14 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
         const uint4* from = w.codes_of(u.expert, min(2 * u.block + side, w.blocks - 1) * 8);
 #pragma unroll 1
         for (int c = 0; c < w.chunks; ++c, ++n) {
-          const uint32_t r = n % kRaws;
-          if (!(alive = bar_wait(raw_empty + r, ((n / kRaws) & 1) ^ 1, dead))) break;
+          const uint32_t r = n % R::RAW;
+          if (!(alive = bar_wait(raw_empty + r, ((n / R::RAW) & 1) ^ 1, dead))) break;
           if (one_lane()) {
-            bar_expect(raw_full + r, kBytesRaw);
+            bar_expect(raw_full + r, R::BYTES_RAW);
             asm volatile(
                 "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-                    smem_of(sm + kAtRaw + r * kBytesRaw)),
-                "l"(from + (int64_t)c * kNextChunk), "n"(kBytesRaw), "r"(smem_of(raw_full + r))
+                    smem_of(sm + R::AT_RAW + r * R::BYTES_RAW)),
+                "l"(from + (int64_t)c * kNextChunk), "n"(R::BYTES_RAW), "r"(smem_of(raw_full + r))
                 : "memory");
           }
           __syncwarp();
@@ -375,22 +392,27 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
         const uint32_t id = (idesc_of<T>(u.columns, false) & 0x00ffffffu) | (256u >> 4) << 24;
 #pragma unroll 1
         for (int c = 0; c < w.chunks; ++c, ++n) {
-          const uint32_t s = n % kStages;
-          if (!(alive = bar_wait(full + s, (n / kStages) & 1, dead))) break;
-          const uint32_t x = operand(smem_of(sm + s * kBytesA), 16), y = operand(smem_of(sm + kAtB + s * kBytesB), 16);
+          const uint32_t sa = n % R::A, sb = n % R::B;
+          if (!(alive = bar_wait(b_full + sb, (n / R::B) & 1, dead) && bar_wait(a_full + sa, (n / R::A) & 1, dead)))
+            break;
+          const uint32_t x = operand(smem_of(sm + sa * R::BYTES_A), 16);
+          const uint32_t y = operand(smem_of(sm + R::AT_B + sb * R::BYTES_B), 16);
 #pragma unroll
           for (int h = 0; h < PER; ++h) {
-            const uint32_t buf = groups & 1;
+            const uint32_t buf = groups % R::SUMS;
             const bool fresh = STAGES_OF == 1 || (c & 1) == 0;
-            if (fresh && !(alive = bar_wait(sum_empty + buf, ((groups >> 1) & 1) ^ 1, dead))) break;
+            if (fresh && !(alive = bar_wait(sum_empty + buf, ((groups / R::SUMS) & 1) ^ 1, dead))) break;
             tmem_after();
             const bool whole_group = STAGES_OF == 1 || (c & 1) == 1;
             if (one_lane()) {
 #pragma unroll
               for (int k = h * 4 / PER; k < (h + 1) * 4 / PER; ++k)
-                mma_pair(tmem + buf * 256, x + k * 2, y + k * 2, id, !(fresh && k == h * 4 / PER));
+                mma_pair(tmem + buf * WIDTH, x + k * 2, y + k * 2, id, !(fresh && k == h * 4 / PER));
               if (whole_group) commit_pair(sum_full + buf);
-              if (h == PER - 1) commit_pair(empty + s);
+              if (h == PER - 1) {
+                commit_pair(a_empty + sa);
+                commit_pair(b_empty + sb);
+              }
             }
             __syncwarp();
             if (whole_group) ++groups;
@@ -430,15 +452,21 @@ bool make_map(CUtensorMap& m, bool bf16, const ProductArgs& p, int64_t rows, int
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+template <class T, class S, int GROUP, int WIDTH>
+cudaError_t launch_wide(const TcArgs& a, const CUtensorMap& rows, int64_t units, tre_diag* diag,
+                        cudaStream_t s) {
+  const void* fn = (const void*)k_w4_tc<T, S, GROUP, WIDTH>;
+  cudaError_t e = func_smem_once(fn, Ring<WIDTH>::SMEM, true);
+  if (e) return e;
+  const int64_t pairs = std::min<int64_t>(units, std::max(1, device_sm_count() / 2));
+  k_w4_tc<T, S, GROUP, WIDTH><<<(unsigned)(2 * pairs), kThreads, Ring<WIDTH>::SMEM, s>>>(a, rows, diag);
+  return cudaGetLastError();
+}
 template <class T, class S, int GROUP>
 cudaError_t launch_typed(const TcArgs& a, const CUtensorMap& rows, int64_t units, tre_diag* diag,
                          cudaStream_t s) {
-  const void* fn = (const void*)k_w4_tc<T, S, GROUP>;
-  cudaError_t e = func_smem_once(fn, kSmem, true);
-  if (e) return e;
-  const int64_t pairs = std::min<int64_t>(units, std::max(1, device_sm_count() / 2));
-  k_w4_tc<T, S, GROUP><<<(unsigned)(2 * pairs), kThreads, kSmem, s>>>(a, rows, diag);
-  return cudaGetLastError();
+  return a.tile <= 128 ? launch_wide<T, S, GROUP, 128>(a, rows, units, diag, s)
+                       : launch_wide<T, S, GROUP, 256>(a, rows, units, diag, s);
 }
 template <class T, class S>
 cudaError_t launch_group(int group, const TcArgs& a, const CUtensorMap& rows, int64_t units, tre_diag* diag,
@@ -455,7 +483,7 @@ cudaError_t launch_w4_tc(int dtype, int scale_dtype, int group, const ProductArg
   TcArgs a;
   a.p = p;
   a.row_blocks = (p.w.tiles + 15) / 16;
-  a.tile = kTileTokens;
+  a.tile = p.plan.piece;
   if (!p.plan.order) {
     // Rows of a unit: those with which the rounds of units take least, each its columns and
     // what a unit costs besides.
@@ -476,7 +504,7 @@ cudaError_t launch_w4_tc(int dtype, int scale_dtype, int group, const ProductArg
   a.box = a.tile / 2;
   if (p.plan.order) {
     a.box = 16;
-    while (a.box < 128 && a.box * 2 * tiles < rows) a.box *= 2;
+    while (a.box < a.tile / 2 && a.box * 2 * tiles < rows) a.box *= 2;
   }
   if (p.gather) a.box = 0;
   if (tiles * a.row_blocks > 2000000000) return cudaErrorNotSupported;

@@ -121,7 +121,7 @@ def act(y, off):
     return s * u, 1.1 * og * u.abs() + s.abs() * ou + 1.1 * og * ou + 2.0 ** -19 * (s * u).abs()
 
 
-def experts(x, ids, weights, m1, m2, dtype, rounded=True):
+def experts(x, ids, weights, m1, m2, dtype, rounded=False):
     """(y, error) with m1, m2 [experts][..]; the error counts the rounding of the inner rows
     and of each expert's output (where there are many tokens)."""
     y = torch.zeros(x.shape[0], m2.shape[1], dtype=torch.float64, device=x.device)
