@@ -36,9 +36,9 @@ __device__ __forceinline__ bool bar_poll(uint64_t* b, uint32_t parity) {
       : "memory");
   return ok;
 }
-// A whole warp waits. False when the barrier did not come in about two seconds, here
-// or in another warp: the warp then does no more work, and every warp meets at the end.
-__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* dead) {
+// Waits. False when the barrier did not come in about two seconds, here or in another warp:
+// then there is no more work, and every warp meets at the end. (A thread for itself; a warp.)
+__device__ __forceinline__ bool bar_wait_one(uint64_t* b, uint32_t parity, volatile int* dead) {
   bool ok = bar_poll(b, parity);
   if (!ok) {
     const long long from = clock64();
@@ -50,7 +50,10 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile 
       }
     }
   }
-  return __all_sync(0xffffffffu, ok);
+  return ok;
+}
+__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* dead) {
+  return __all_sync(0xffffffffu, bar_wait_one(b, parity, dead));
 }
 
 __device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t* r) {

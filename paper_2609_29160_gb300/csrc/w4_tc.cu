@@ -31,13 +31,13 @@ namespace {
 // Shared memory of a block for units of up to WIDTH rows of x. A stage of the operand lasts
 // from its last product to its next, through the turning of codes, an arrival at the other
 // block and the products themselves, about 0.9 us; one of x's rows also waits for its copy,
-// about 2 us: hence more of them.
+// more than 2 us: hence more of them.
 template <int WIDTH> struct Ring {
   static constexpr int A = WIDTH == 256 ? 4 : 6, B = WIDTH == 256 ? 8 : 12, RAW = 8;
   static constexpr int BYTES_A = 128 * 128, BYTES_B = WIDTH / 2 * 128, BYTES_RAW = 4096;
   static constexpr int SUMS = 512 / WIDTH;             // accumulators
   static constexpr int AT_B = A * BYTES_A, AT_RAW = AT_B + B * BYTES_B, AT_BAR = AT_RAW + RAW * BYTES_RAW;
-  static constexpr int BARS = 2 * (RAW + A + B + SUMS);
+  static constexpr int BARS = 2 * (RAW + B + SUMS);
   static constexpr int SMEM = AT_BAR + BARS * 8 + 16;
   static_assert(SMEM <= 227 * 1024, "shared memory of a block");
 };
@@ -132,12 +132,12 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
   const W4Args& w = a.p.w;
 
   using R = Ring<WIDTH>;
-  // What products need (a_full, b_full) and free accumulators (sum_empty) are barriers of the
-  // pair's first block, the others each block's own.
+  // What products need (full) and free accumulators (sum_empty) are barriers of the pair's
+  // first block, the others each block's own. `done` says that a stage's products are over: its
+  // rows' place is free for the stage R::B later, its operand's for the one R::A later.
   uint64_t* bars = reinterpret_cast<uint64_t*>(sm + R::AT_BAR);
-  uint64_t *raw_full = bars, *raw_empty = raw_full + R::RAW, *a_full = raw_empty + R::RAW,
-           *a_empty = a_full + R::A, *b_full = a_empty + R::A, *b_empty = b_full + R::B,
-           *sum_full = b_empty + R::B, *sum_empty = sum_full + R::SUMS;
+  uint64_t *raw_full = bars, *raw_empty = raw_full + R::RAW, *full = raw_empty + R::RAW,
+           *done = full + R::B, *sum_full = done + R::B, *sum_empty = sum_full + R::SUMS;
   uint32_t* tmem_at = reinterpret_cast<uint32_t*>(bars + R::BARS);
   volatile int* dead = reinterpret_cast<volatile int*>(tmem_at + 1);
   if (warp == kMmaWarp) {
@@ -152,13 +152,9 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
       bar_init(raw_full + k, 1);
       bar_init(raw_empty + k, 1);
     }
-    for (int k = 0; k < R::A; ++k) {
-      bar_init(a_full + k, 2);
-      bar_init(a_empty + k, 1);
-    }
     for (int k = 0; k < R::B; ++k) {
-      bar_init(b_full + k, 1);
-      bar_init(b_empty + k, 1);
+      bar_init(full + k, 3);             // both blocks' operands, and the rows
+      bar_init(done + k, 1);
     }
     for (int k = 0; k < R::SUMS; ++k) {
       bar_init(sum_full + k, 1);
@@ -290,7 +286,8 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
                 w.zeros ? zeros[((int64_t)min(tile0 + x, w.tiles - 1) * w.groups + (c * 64 / GROUP + y)) * 8]
                         : Whole<S>::bits + 0x00080008u);
         if (!(alive = bar_wait(raw_full + r, (k / R::RAW) & 1, dead))) break;
-        if (!(alive = bar_wait(a_empty + s, ((k / R::A) & 1) ^ 1, dead))) break;
+        const uint32_t last = k - R::A;                  // the stage before in its place
+        if (k >= R::A && !(alive = bar_wait(done + last % R::B, (last / R::B) & 1, dead))) break;
         const uint4* codes = reinterpret_cast<const uint4*>(sm + R::AT_RAW + r * R::BYTES_RAW) + lane;
         uint8_t* to = sm + s * R::BYTES_A;
 #pragma unroll
@@ -310,7 +307,7 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
         }
         bar_arrive_warp(raw_empty + r);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        arrive_first(a_full + s);
+        arrive_first(full + k % R::B);
       }
       n += w.chunks;
     }
@@ -335,10 +332,10 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
 #pragma unroll 1
         for (int c = 0; c < w.chunks; ++c, ++n) {
           const uint32_t s = n % R::B;
-          if (!(alive = bar_wait(b_empty + s, ((n / R::B) & 1) ^ 1, dead))) break;
-          if (side == 0 && lane == 0) bar_expect(b_full + s, 2 * bytes);
+          if (!(alive = bar_wait(done + s, ((n / R::B) & 1) ^ 1, dead))) break;
+          if (side == 0 && lane == 0) bar_expect(full + s, 2 * bytes);
           __syncwarp();
-          const uint32_t to = smem_of(sm + R::AT_B + s * R::BYTES_B), bar = first_of(b_full + s);
+          const uint32_t to = smem_of(sm + R::AT_B + s * R::BYTES_B), bar = first_of(full + s);
           if (a.box == 0) {
             if (lane * 4 < mine)
               asm volatile(
@@ -358,9 +355,7 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
       }
       // the products' arrivals that nothing waits for any more
       for (uint32_t k = n > R::B ? n - R::B : 0; alive && k < n; ++k)
-        alive = bar_wait(b_empty + k % R::B, (k / R::B) & 1, dead);
-      for (uint32_t k = n > R::A ? n - R::A : 0; alive && k < n; ++k)
-        alive = bar_wait(a_empty + k % R::A, (k / R::A) & 1, dead);
+        alive = bar_wait(done + k % R::B, (k / R::B) & 1, dead);
     } else if (warp == kRawWarp) {
       // ---- codes -------------------------------------------------------------------
       uint32_t n = 0;
@@ -383,8 +378,10 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
           __syncwarp();
         }
       }
-    } else if (warp == kMmaWarp && side == 0) {
+    } else if (warp == kMmaWarp && side == 0 && one_lane()) {
       // ---- products ------------------------------------------------------------------
+      // One thread, which does as little as it can: with waits of a whole warp and an arrival
+      // for each ring a stage took it 700 cycles, more than the stage's products.
       uint32_t n = 0, groups = 0;
       bool alive = true;
       for (int i = pair; alive && unit_at(a, i, u); i += pairs) {
@@ -393,34 +390,29 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
 #pragma unroll 1
         for (int c = 0; c < w.chunks; ++c, ++n) {
           const uint32_t sa = n % R::A, sb = n % R::B;
-          if (!(alive = bar_wait(b_full + sb, (n / R::B) & 1, dead) && bar_wait(a_full + sa, (n / R::A) & 1, dead)))
-            break;
           const uint32_t x = operand(smem_of(sm + sa * R::BYTES_A), 16);
           const uint32_t y = operand(smem_of(sm + R::AT_B + sb * R::BYTES_B), 16);
+          if (!(alive = bar_wait_one(full + sb, (n / R::B) & 1, dead))) break;
 #pragma unroll
           for (int h = 0; h < PER; ++h) {
             const uint32_t buf = groups % R::SUMS;
             const bool fresh = STAGES_OF == 1 || (c & 1) == 0;
-            if (fresh && !(alive = bar_wait(sum_empty + buf, ((groups / R::SUMS) & 1) ^ 1, dead))) break;
+            if (fresh && !(alive = bar_wait_one(sum_empty + buf, ((groups / R::SUMS) & 1) ^ 1, dead))) break;
             tmem_after();
-            const bool whole_group = STAGES_OF == 1 || (c & 1) == 1;
-            if (one_lane()) {
 #pragma unroll
-              for (int k = h * 4 / PER; k < (h + 1) * 4 / PER; ++k)
-                mma_pair(tmem + buf * WIDTH, x + k * 2, y + k * 2, id, !(fresh && k == h * 4 / PER));
-              if (whole_group) commit_pair(sum_full + buf);
-              if (h == PER - 1) {
-                commit_pair(a_empty + sa);
-                commit_pair(b_empty + sb);
-              }
+            for (int k = h * 4 / PER; k < (h + 1) * 4 / PER; ++k)
+              mma_pair(tmem + buf * WIDTH, x + k * 2, y + k * 2, id, !(fresh && k == h * 4 / PER));
+            if (STAGES_OF == 1 || (c & 1) == 1) {        // the group is whole
+              commit_pair(sum_full + buf);
+              ++groups;
             }
-            __syncwarp();
-            if (whole_group) ++groups;
           }
           if (!alive) break;
+          commit_pair(done + sb);
         }
       }
     }
+    __syncwarp();
   }
   // A block that has given up does not know which of its copies and products are still on
   // their way: it stays some 20 ms, far longer than any takes.
