@@ -14,10 +14,10 @@
 // products, a quarter of the issue slots at groups of 128 and, with them, of no time.
 //
 // A block's warps: 0-7 add groups (a thread a row of the matrix and half of the columns) and
-// write rows of y; 8-11 turn codes into the operand, through which 128 x 64 elements go at a
-// time; 12 copies rows of x (tensor copies, by four gathered rows where they are tokens of an
-// expert), 13 codes; 14 of the pair's first block issues the products. Of a gated matrix a
-// warp holds 16 rows of the gate and the 16 that they multiply.
+// write rows of y; 8-12 turn codes into the operand, a stage of 128 x 64 elements a warp; 13
+// copies rows of x (tensor copies, by four gathered rows where they are tokens of an expert),
+// 14 codes; 15 of the pair's first block issues the products. Of a gated matrix a warp of the
+// first eight holds 16 rows of the gate and the 16 that they multiply.
 #include <algorithm>
 #include <cstring>
 
@@ -33,7 +33,7 @@ namespace {
 // block and the products themselves, about 0.9 us; one of x's rows also waits for its copy,
 // more than 2 us: hence more of them.
 template <int WIDTH> struct Ring {
-  static constexpr int A = WIDTH == 256 ? 4 : 6, B = WIDTH == 256 ? 8 : 12, RAW = 8;
+  static constexpr int A = WIDTH == 256 ? 6 : 8, B = A, RAW = 8;
   static constexpr int BYTES_A = 128 * 128, BYTES_B = WIDTH / 2 * 128, BYTES_RAW = 4096;
   static constexpr int SUMS = 512 / WIDTH;             // accumulators
   static constexpr int AT_B = A * BYTES_A, AT_RAW = AT_B + B * BYTES_B, AT_BAR = AT_RAW + RAW * BYTES_RAW;
@@ -41,7 +41,7 @@ template <int WIDTH> struct Ring {
   static constexpr int SMEM = AT_BAR + BARS * 8 + 16;
   static_assert(SMEM <= 227 * 1024, "shared memory of a block");
 };
-constexpr int kScaleWarps = 8, kCodeWarp = 8, kCodeWarps = 4, kRowWarp = 12, kRawWarp = 13, kMmaWarp = 14;
+constexpr int kScaleWarps = 8, kCodeWarp = 8, kCodeWarps = 5, kRowWarp = 13, kRawWarp = 14, kMmaWarp = 15;
 constexpr int kThreads = 512;
 
 // A tile of rows of x, the same for both blocks of a pair.
@@ -170,9 +170,10 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
   Unit u;
 
   // Registers move once, from the launch's 4 x 128 (in groups of four warps).
+  if (warp < kScaleWarps) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+  else asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
   if (warp < kScaleWarps) {
     // ---- sums of groups ----------------------------------------------------------
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
     const int quarter = warp & 3, half = warp >> 2, r16 = lane & 15;
     const int g = (r16 & 3) << 1 | (r16 >> 2 & 1);       // turn(g) == r16 & 7
     uint32_t n = 0;                                      // groups so far
@@ -265,18 +266,18 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
     }
   } else if (warp < kCodeWarp + kCodeWarps) {
     // ---- codes to an operand -------------------------------------------------------
-    // A warp takes every fourth stage: what happens to one, step after step, takes longer than
-    // its products.
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    // A warp takes every fifth stage: what happens to one, step after step, takes three times
+    // as long as its products.
     const int cw = warp - kCodeWarp, g = lane >> 2, t = lane & 3;
-    uint32_t n = 0;                                      // stages so far
+    uint32_t n = 0, own = cw;                            // stages so far, and this warp's next
     bool alive = true;
     for (int i = pair; alive && unit_at(a, i, u); i += pairs) {
       const int tile0 = (2 * u.block + side) * 8;
       const uint32_t* zeros = w.zeros + ((int64_t)u.expert * w.tiles * w.groups) * 8 + g;
 #pragma unroll 1
-      for (int c = (cw - n) & 3; c < w.chunks; c += kCodeWarps) {
-        const uint32_t k = n + c, s = k % R::A, r = k % R::RAW;
+      for (; own < n + w.chunks; own += kCodeWarps) {
+        const uint32_t k = own, s = k % R::A, r = k % R::RAW;
+        const int c = (int)(k - n);
         uint32_t z[8][PER];
 #pragma unroll
         for (int x = 0; x < 8; ++x)
@@ -285,9 +286,13 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
             z[x][y] = zero_as<T, S>(
                 w.zeros ? zeros[((int64_t)min(tile0 + x, w.tiles - 1) * w.groups + (c * 64 / GROUP + y)) * 8]
                         : Whole<S>::bits + 0x00080008u);
-        if (!(alive = bar_wait(raw_full + r, (k / R::RAW) & 1, dead))) break;
-        const uint32_t last = k - R::A;                  // the stage before in its place
+        // A wait for a parity also passes a phase early, and this warp does not see all phases.
+        // With the products of stage k - A over those before it are: the code copied to this
+        // stage's place before has been used, and `done` itself has come so far.
+        static_assert(R::A <= R::RAW && R::B >= kCodeWarps && R::A <= R::B, "phases that are known to be over");
+        const uint32_t last = k - R::A;
         if (k >= R::A && !(alive = bar_wait(done + last % R::B, (last / R::B) & 1, dead))) break;
+        if (!(alive = bar_wait(raw_full + r, (k / R::RAW) & 1, dead))) break;
         const uint4* codes = reinterpret_cast<const uint4*>(sm + R::AT_RAW + r * R::BYTES_RAW) + lane;
         uint8_t* to = sm + s * R::BYTES_A;
 #pragma unroll
@@ -312,7 +317,6 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
       n += w.chunks;
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp == kRowWarp) {
       // ---- rows of x ---------------------------------------------------------------
       uint32_t n = 0;
