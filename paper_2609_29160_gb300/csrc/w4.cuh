@@ -73,8 +73,10 @@ __device__ __forceinline__ void whole(uint32_t w, uint32_t z0, uint32_t z8, uint
     a[i] = minus2<T>(((w >> (4 * i)) & 0x000f000fu) | Whole<T>::bits, i & 1 ? z8 : z0);
 }
 
-// What a gate does
-__device__ __forceinline__ float gated(float g, float u) { return g / (1.f + __expf(-g)) * u; }
+// What a gate does (the quick exponential and quotient: each within a few units of 2^-24)
+__device__ __forceinline__ float gated(float g, float u) {
+  return __fdividef(g, 1.f + __expf(-g)) * u;
+}
 
 // Tokens of experts, sorted by expert (k_plan): places of one expert lie together; place p is
 // pair order[p] = token * top + j.
@@ -83,9 +85,10 @@ struct Slot {
 };
 struct PlanArgs {
   int32_t* order;                      // [pairs]
+  int32_t* where;                      // [pairs]: the place of a pair
   Slot* slots;                         // experts that have any
   Slot* tiles;                         // their places in pieces of up to `piece`
-  int32_t* n;                          // [2]: how many slots, tiles
+  int32_t* n;                          // [3]: how many slots, tiles, places
   int32_t piece;
 };
 constexpr int kTileTokens = 256;       // columns of a product on the tensor cores
@@ -99,9 +102,10 @@ struct ProductArgs {
   int64_t y_row;
   PlanArgs plan;                       // order null: rows as they are, one matrix
   int32_t n_rows, top;
-  bool gather, scatter;                // x's / y's rows by pair: token of it / itself
-  bool y_f32;
+  bool gather;                         // x's rows are tokens', by place
+  bool y_f32;                          // and with it
   bool apart;                          // a gated matrix's two halves as they are
+  bool y_wide;                         // eight neighbours of a row of y can be written at once
 };
 
 bool w4_args(const tre_w4* w, W4Args& a);

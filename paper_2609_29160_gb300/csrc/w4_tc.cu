@@ -15,8 +15,7 @@
 //
 // A block's warps: 0-7 add groups (a thread a row of the matrix and half of the columns) and
 // write rows of y; 8-12 turn codes into the operand, a stage of 128 x 64 elements a warp; 13
-// copies rows of x (tensor copies, by four gathered rows where they are tokens of an expert),
-// 14 codes; 15 of the pair's first block issues the products. Of a gated matrix a warp of the
+// copies rows of x, 14 codes; 15 of the pair's first block issues the products. Of a gated matrix a warp of the
 // first eight holds 16 rows of the gate and the 16 that they multiply.
 #include <algorithm>
 #include <cstring>
@@ -28,21 +27,23 @@
 namespace tre {
 namespace {
 
+constexpr int kScaleWarps = 8, kCodeWarp = 8, kCodeWarps = 5, kRowWarp = 13, kRawWarp = 14, kMmaWarp = 15;
+constexpr int kThreads = 512;
+
 // Shared memory of a block for units of up to WIDTH rows of x. A stage of the operand lasts
 // from its last product to its next, through the turning of codes, an arrival at the other
 // block and the products themselves, about 0.9 us; one of x's rows also waits for its copy,
 // more than 2 us: hence more of them.
 template <int WIDTH> struct Ring {
-  static constexpr int A = WIDTH == 256 ? 6 : 8, B = A, RAW = 8;
+  static constexpr int A = WIDTH == 256 ? 6 : 7, B = WIDTH == 256 ? 6 : 8, RAW = WIDTH == 256 ? 6 : 8;
   static constexpr int BYTES_A = 128 * 128, BYTES_B = WIDTH / 2 * 128, BYTES_RAW = 4096;
   static constexpr int SUMS = 512 / WIDTH;             // accumulators
-  static constexpr int AT_B = A * BYTES_A, AT_RAW = AT_B + B * BYTES_B, AT_BAR = AT_RAW + RAW * BYTES_RAW;
+  static constexpr int AT_B = A * BYTES_A, AT_RAW = AT_B + B * BYTES_B;
+  static constexpr int AT_OUT = AT_RAW + RAW * BYTES_RAW, AT_BAR = AT_OUT + kScaleWarps * 1024;
   static constexpr int BARS = 2 * (RAW + B + SUMS);
   static constexpr int SMEM = AT_BAR + BARS * 8 + 16;
   static_assert(SMEM <= 227 * 1024, "shared memory of a block");
 };
-constexpr int kScaleWarps = 8, kCodeWarp = 8, kCodeWarps = 5, kRowWarp = 13, kRawWarp = 14, kMmaWarp = 15;
-constexpr int kThreads = 512;
 
 // A tile of rows of x, the same for both blocks of a pair.
 struct Unit {
@@ -53,7 +54,7 @@ struct Unit {
 struct TcArgs {
   ProductArgs p;
   int32_t row_blocks, tile;            // tile: most rows of x of a unit
-  int32_t box;                         // rows of x of one copy; 0: gathered by four
+  int32_t box;                         // rows of x of one copy
 };
 
 __device__ __forceinline__ bool unit_at(const TcArgs& a, int u, Unit& w) {
@@ -110,6 +111,14 @@ __device__ __forceinline__ void mma_pair(uint32_t d, uint32_t a, uint32_t b, uin
 __device__ __forceinline__ void pair_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// Four matrices of eight rows of 16 bytes (lane l names row l % 8 of the (l / 8)th), turned: a
+// lane gets column l / 4, elements 2 (l % 4) and the next, of each.
+__device__ __forceinline__ void turned(uint32_t at, uint32_t* v) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+               : "r"(at)
+               : "memory");
+}
 // acc += s * v, two at a time
 __device__ __forceinline__ void add_scaled(float* acc, const uint32_t* v, float s) {
   uint64_t r;
@@ -118,6 +127,96 @@ __device__ __forceinline__ void add_scaled(float* acc, const uint32_t* v, float 
   split(r, x);
   acc[0] = __uint_as_float(x[0]);
   acc[1] = __uint_as_float(x[1]);
+}
+
+// A warp's sums into rows of y: lane l holds row l of its two tiles of the matrix, acc[c] the
+// column first + c of the unit's, `columns` of them. Elements of 16 bits are turned through
+// shared memory, sixteen columns at a time (a row of the matrix, its columns along it, and
+// back by ldmatrix, which turns), so that a lane has eight neighbours of a row of y: written
+// as they lie, 64 bytes a store, they took 6.5 us a unit of 256 columns, a fifth of its time.
+template <class T>
+__device__ __forceinline__ void write_rows(const ProductArgs& p, const Unit& u, int tile, int first,
+                                           int columns, const float* acc, uint8_t* room) {
+  const W4Args& w = p.w;
+  const int lane = threadIdx.x & 31;
+  const int there = min(u.count - first, columns);      // columns that are rows of y
+  const int64_t row0 = (int64_t)u.start + first;
+  const int halves = w.n / 2;
+  if (p.y_f32) {
+    const int r = lane & 15;
+    int feature = tile * 16 + r, end = w.n;
+    if (w.gated) {                                       // (the two halves as they are)
+      feature = (tile >> 1) * 16 + r;
+      end = feature < halves ? w.n : 0;
+      if (lane >= 16) feature += halves;
+    }
+    float* y = reinterpret_cast<float*>(p.y) + row0 * p.y_row + feature;
+    const int mine = feature < end ? there : 0;
+#pragma unroll
+    for (int c = 0; c < 128; ++c) {
+      if (c < mine) *y = acc[c];
+      y += p.y_row;
+    }
+    return;
+  }
+  const bool joined = w.gated;
+  // where this lane's row stands in the turned tile, so that a matrix of eight by eight has the
+  // rows that give a lane neighbours: all 32, or of a gated matrix 16
+  const int f = joined ? lane & 15 : lane;
+  const int i = joined ? f >> 1 & 1 : f >> 1 & 3, at = 8 * i + 2 * (joined ? f >> 2 : f >> 3) + (f & 1);
+  auto place = [&](int row, int piece) { return room + row * 32 + ((piece ^ ((row >> 2 ^ row >> 3) & 1)) << 4); };
+  const int per = joined ? 4 : 8;                        // neighbours of a lane
+  const int feature = (joined ? (tile >> 1) * 16 : (tile & ~1) * 16) + (lane & 3) * per;
+  const int end = joined ? halves : w.n;
+  const bool wide = p.y_wide && feature + per <= end;
+  T* y = reinterpret_cast<T*>(p.y) + (row0 + (lane >> 2)) * p.y_row + feature;
+  auto store = [&](int col, const uint32_t* v) {         // of column col + lane / 4
+    if (col + (lane >> 2) >= there) return;
+    T* to = y + (int64_t)col * p.y_row;
+    if (wide) {
+      if (joined) *reinterpret_cast<uint2*>(to) = make_uint2(v[0], v[1]);
+      else *reinterpret_cast<uint4*>(to) = make_uint4(v[0], v[1], v[2], v[3]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < per && feature + e < end)
+          to[e] = reinterpret_cast<const T*>(v)[e];
+    }
+  };
+#pragma unroll
+  for (int c = 0; c < 128; c += 16) {
+    if (c >= columns) break;
+    __syncwarp();
+    if (joined) {
+      // lanes of gates take the first eight columns, the others the next
+      const bool gate = lane < 16;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float other = __shfl_xor_sync(0xffffffffu, gate ? acc[c + 8 + e] : acc[c + e], 16);
+        v[e] = gated(gate ? acc[c + e] : other, gate ? other : acc[c + 8 + e]);
+      }
+      *reinterpret_cast<uint4*>(place(at, gate ? 0 : 1)) = Vec<T>::put(v);
+    } else {
+      *reinterpret_cast<uint4*>(place(at, 0)) = Vec<T>::put(acc + c);
+      *reinterpret_cast<uint4*>(place(at, 1)) = Vec<T>::put(acc + c + 8);
+    }
+    __syncwarp();
+    if (joined) {
+      // matrices: rows 0-7 and 8-15 of the first eight columns, then of the next
+      uint32_t v[4];
+      turned(smem_of(place((lane >> 3 & 1) * 8 + (lane & 7), lane >> 4)), v);
+      store(c, v);
+      store(c + 8, v + 2);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t v[4];
+        turned(smem_of(place(lane, h)), v);
+        store(c + 8 * h, v);
+      }
+    }
+  }
 }
 
 template <class T, class S, int GROUP, int WIDTH>
@@ -181,7 +280,6 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
     for (int i = pair; alive && unit_at(a, i, u); i += pairs) {
       const int mine = u.columns / 2;                    // columns of this warp, from half * mine on
       const int tile = (2 * u.block + side) * 8 + 2 * quarter + (lane >> 4);
-      const bool there = tile < w.tiles;
       const uint16_t* scale =
           reinterpret_cast<const uint16_t*>(
               w.scales + (((int64_t)u.expert * w.tiles + min(tile, w.tiles - 1)) * w.groups) * 8 + g) +
@@ -215,54 +313,7 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
         }
       }
       if (!alive) break;
-      // rows of y: a thread's row of the matrix is a column of them
-      const int first = half * mine;
-      const int in_pair = (2 * u.block + side) * 4 + quarter;    // of tiles
-      const int halves = w.n / 2;
-      int feature;
-      bool mine_too;
-      if (w.gated) {
-        feature = in_pair * 16 + r16;
-        mine_too = there && feature < halves;
-        if (a.p.apart && lane >= 16) feature += halves;
-      } else {
-        feature = tile * 16 + r16;
-        mine_too = there && feature < w.n;
-      }
-      int place[4];
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const int c = first + b * 32 + lane;
-        place[b] = u.start + c;
-        if (a.p.scatter) place[b] = c < u.count ? a.p.plan.order[u.start + c] : 0;
-      }
-      auto put = [&](int row, float v) {
-        const int64_t to = (int64_t)row * a.p.y_row + feature;
-        if (a.p.y_f32) reinterpret_cast<float*>(a.p.y)[to] = v;
-        else reinterpret_cast<T*>(a.p.y)[to] = T(v);
-      };
-      const bool joined = w.gated && !a.p.apart;
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        if (b * 32 >= mine) break;
-#pragma unroll
-        for (int c = 0; c < 32; c += 2) {
-          const int col = first + b * 32 + c;
-          if (b * 32 + c < mine && col < u.count) {      // (the same for the whole warp)
-            const int row0 = __shfl_sync(0xffffffffu, place[b], c);
-            const int row1 = __shfl_sync(0xffffffffu, place[b], c + 1);
-            const float x0 = acc[b * 32 + c], x1 = acc[b * 32 + c + 1];
-            if (joined) {
-              const float other = __shfl_xor_sync(0xffffffffu, lane < 16 ? x1 : x0, 16);
-              const float v = lane < 16 ? gated(x0, other) : gated(other, x1);
-              if (mine_too && col + (lane >> 4) < u.count) put(lane < 16 ? row0 : row1, v);
-            } else if (mine_too) {
-              put(row0, x0);
-              if (col + 1 < u.count) put(row1, x1);
-            }
-          }
-        }
-      }
+      write_rows<T>(a.p, u, tile, half * mine, mine, acc, sm + R::AT_OUT + warp * 1024);
     }
   } else if (warp < kCodeWarp + kCodeWarps) {
     // ---- codes to an operand -------------------------------------------------------
@@ -323,37 +374,19 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
       bool alive = true;
       for (int i = pair; alive && unit_at(a, i, u); i += pairs) {
         const int mine = u.columns / 2, first = u.start + side * mine;
-        const uint32_t bytes = (a.box ? (mine + a.box - 1) / a.box * a.box : mine) * 128;
-        int r[4] = {0, 0, 0, 0};
-        if (a.box == 0) {
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            // (columns past the last are not written: any row will do)
-            const int p = min(first + lane * 4 + x, u.start + u.count - 1);
-            r[x] = a.p.plan.order[p] / a.p.top;
-          }
-        }
+        const uint32_t bytes = (mine + a.box - 1) / a.box * a.box * 128;
 #pragma unroll 1
         for (int c = 0; c < w.chunks; ++c, ++n) {
           const uint32_t s = n % R::B;
           if (!(alive = bar_wait(done + s, ((n / R::B) & 1) ^ 1, dead))) break;
           if (side == 0 && lane == 0) bar_expect(full + s, 2 * bytes);
           __syncwarp();
-          const uint32_t to = smem_of(sm + R::AT_B + s * R::BYTES_B), bar = first_of(full + s);
-          if (a.box == 0) {
-            if (lane * 4 < mine)
-              asm volatile(
-                  "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes"
-                  ".cta_group::2 [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(to + lane * 512),
-                  "l"(&rows), "r"(c * 64), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(bar)
-                  : "memory");
-          } else if (lane * a.box < mine) {
+          if (lane * a.box < mine)
             asm volatile(
                 "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
-                "[%0], [%1, {%2, %3}], [%4];" ::"r"(to + lane * a.box * 128),
-                "l"(&rows), "r"(c * 64), "r"(first + lane * a.box), "r"(bar)
+                "[%0], [%1, {%2, %3}], [%4];" ::"r"(smem_of(sm + R::AT_B + s * R::BYTES_B) + lane * a.box * 128),
+                "l"(&rows), "r"(c * 64), "r"(first + lane * a.box), "r"(first_of(full + s))
                 : "memory");
-          }
           __syncwarp();
         }
       }
@@ -434,14 +467,14 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
   if (tid == 0 && *dead && diag) diag->err = TRE_ETIMEOUT;
 }
 
-// Rows of x in boxes of `box` rows and 64 elements, or one row for a gather by four.
+// Rows of x in boxes of `box` rows and 64 elements.
 bool make_map(CUtensorMap& m, bool bf16, const ProductArgs& p, int64_t rows, int box) {
   const Encode enc = encoder();
   const int64_t stride = p.x_row * 2;
   if (!enc || stride <= 0 || stride >= (1ll << 40)) return false;
   const cuuint64_t dims[2] = {(cuuint64_t)p.w.k, (cuuint64_t)rows};
   const cuuint64_t strides[1] = {(cuuint64_t)stride};
-  const cuuint32_t size[2] = {64, (cuuint32_t)(box ? box : 1)}, one[2] = {1, 1};
+  const cuuint32_t size[2] = {64, (cuuint32_t)box}, one[2] = {1, 1};
   return enc(&m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
              const_cast<uint8_t*>(p.x), dims, strides, size, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -478,6 +511,7 @@ cudaError_t launch_w4_tc(int dtype, int scale_dtype, int group, const ProductArg
                          int64_t tiles, tre_diag* diag, cudaStream_t s) {
   TcArgs a;
   a.p = p;
+  a.p.y_wide = p.y_row % 8 == 0 && reinterpret_cast<uintptr_t>(p.y) % 16 == 0;
   a.row_blocks = (p.w.tiles + 15) / 16;
   a.tile = p.plan.piece;
   if (!p.plan.order) {
@@ -502,7 +536,6 @@ cudaError_t launch_w4_tc(int dtype, int scale_dtype, int group, const ProductArg
     a.box = 16;
     while (a.box < a.tile / 2 && a.box * 2 * tiles < rows) a.box *= 2;
   }
-  if (p.gather) a.box = 0;
   if (tiles * a.row_blocks > 2000000000) return cudaErrorNotSupported;
   CUtensorMap map;
   memset(&map, 0, sizeof(map));
