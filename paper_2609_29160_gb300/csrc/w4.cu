@@ -366,10 +366,17 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const int32_t* ids, int64
   count[tid] = 0;
   __syncthreads();
   unsigned long long past = 0;
-  for (int64_t i = tid; i < pairs; i += kPlanThreads) {
-    const int e = ids[i];
-    if (e >= experts) ++past;
-    else if (e >= 0) atomicAdd(&count[e], 1);
+  // (eight ids on their way at a time: one after the other the loads' latency is all there is)
+  constexpr int kIds = 8;
+  for (int64_t i = tid; i < pairs; i += kIds * kPlanThreads) {
+    int e[kIds];
+#pragma unroll
+    for (int k = 0; k < kIds; ++k) e[k] = i + k * kPlanThreads < pairs ? ids[i + k * kPlanThreads] : -1;
+#pragma unroll
+    for (int k = 0; k < kIds; ++k) {
+      if (e[k] >= experts) ++past;
+      else if (e[k] >= 0) atomicAdd(&count[e[k]], 1);
+    }
   }
   if (diag) warp_add_counter(reinterpret_cast<unsigned long long*>(&diag->dropped_range), past);
   __syncthreads();
@@ -414,13 +421,20 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const int32_t* ids, int64
   __syncthreads();
   count[tid] = start;
   __syncthreads();
-  for (int64_t i = tid; i < pairs; i += kPlanThreads) {
-    const int e = ids[i];
-    if (e >= 0 && e < experts) {
-      const int place = atomicAdd(&count[e], 1);
-      plan.order[place] = (int)i;
-      plan.where[i] = place;
-    }
+  for (int64_t i = tid; i < pairs; i += kIds * kPlanThreads) {
+    int e[kIds];
+#pragma unroll
+    for (int k = 0; k < kIds; ++k) e[k] = i + k * kPlanThreads < pairs ? ids[i + k * kPlanThreads] : -1;
+#pragma unroll
+    for (int k = 0; k < kIds; ++k)
+      if (e[k] >= 0 && e[k] < experts) e[k] = atomicAdd(&count[e[k]], 1);
+      else e[k] = -1;
+#pragma unroll
+    for (int k = 0; k < kIds; ++k)
+      if (e[k] >= 0) {
+        plan.order[e[k]] = (int)(i + k * kPlanThreads);
+        plan.where[i + k * kPlanThreads] = e[k];
+      }
   }
 }
 
@@ -435,26 +449,49 @@ __global__ void __launch_bounds__(kRowThreads) k_gather(const uint4* x, int64_t 
   for (int i = threadIdx.x; i < pieces; i += kRowThreads) to[place * pieces + i] = x[row * x_row + i];
 }
 
-// y[t] = sum over j, in order, of weights[t][j] * each[where[t * top + j]].
+// y[t] = sum over j, in order, of weights[t][j] * each[where[t * top + j]]; a row of `each` has
+// whole fours (row elements). Four elements a thread.
 template <class T>
-__global__ void __launch_bounds__(kRowThreads) k_combine(const float* each, const int32_t* where, const int32_t* ids,
-                                                         const float* weights, int experts, int top,
-                                                         int dim, T* y, int64_t y_row) {
+__global__ void __launch_bounds__(kRowThreads) k_combine(const float* each, const int32_t* where,
+                                                         const int32_t* ids, const float* weights,
+                                                         int experts, int top, int dim, int row, T* y,
+                                                         int64_t y_row) {
+  __shared__ int32_t place[32];
+  __shared__ float weight[32];
   const int64_t t = blockIdx.x;
-  const int i = blockIdx.y * kRowThreads + threadIdx.x;
-  if (i >= dim) return;
-  float sum = 0.f;
-  for (int j = 0; j < top; ++j) {
-    const int e = ids[t * top + j];
-    if (e >= 0 && e < experts) sum = fmaf(weights[t * top + j], each[(int64_t)where[t * top + j] * dim + i], sum);
+  const int i = (blockIdx.y * kRowThreads + threadIdx.x) * 4;
+  if (threadIdx.x < top) {
+    const int e = ids[t * top + threadIdx.x];
+    const bool there = e >= 0 && e < experts;
+    place[threadIdx.x] = there ? where[t * top + threadIdx.x] : -1;
+    weight[threadIdx.x] = weights[t * top + threadIdx.x];
   }
-  y[t * y_row + i] = T(sum);
+  __syncthreads();
+  if (i >= dim) return;
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int j = 0; j < top; ++j) {
+    if (place[j] < 0) continue;
+    const float4 v = *reinterpret_cast<const float4*>(each + (int64_t)place[j] * row + i);
+    const float f = weight[j];
+    sum = make_float4(fmaf(f, v.x, sum.x), fmaf(f, v.y, sum.y), fmaf(f, v.z, sum.z), fmaf(f, v.w, sum.w));
+  }
+  T* to = y + t * y_row + i;
+  const float out[4] = {sum.x, sum.y, sum.z, sum.w};
+  if (i + 4 <= dim && (reinterpret_cast<uintptr_t>(to) & 7) == 0) {
+    *reinterpret_cast<uint2*>(to) = make_uint2(pack<T>(out[0], out[1]), pack<T>(out[2], out[3]));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (i + e < dim) to[e] = T(out[e]);
+  }
 }
 
 template <class T>
-cudaError_t launch_combine(const float* each, const int32_t* where, const tre_tokens* t, int experts, int dim, cudaStream_t s) {
-  const dim3 grid((unsigned)t->n_rows, (unsigned)((dim + kRowThreads - 1) / kRowThreads));
-  k_combine<T><<<grid, kRowThreads, 0, s>>>(each, where, t->ids, t->weights, experts, t->top, dim,
+cudaError_t launch_combine(const float* each, int row, const int32_t* where, const tre_tokens* t, int experts,
+                           int dim, cudaStream_t s) {
+  const dim3 grid((unsigned)t->n_rows, (unsigned)((dim + 4 * kRowThreads - 1) / (4 * kRowThreads)));
+  k_combine<T><<<grid, kRowThreads, 0, s>>>(each, where, t->ids, t->weights, experts, t->top, dim, row,
                                             static_cast<T*>(t->y), t->y_row);
   return cudaGetLastError();
 }
@@ -611,7 +648,8 @@ tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* t, 
   plan.tiles = arena.take<Slot>(slots + pairs / plan.piece);
   plan.n = arena.take<int32_t>(3);
   uint8_t* h = arena.take<uint8_t>((size_t)pairs * inner_row * 2);
-  float* each = arena.take<float>((size_t)pairs * dim);
+  const int row = (dim + 3) / 4 * 4;                  // of `each`
+  float* each = arena.take<float>((size_t)pairs * row);
   uint4* gathered = arena.take<uint4>(few ? 0 : (size_t)pairs * (w1->k / 8));
   if (!ws) {
     *ws_bytes = arena.off;
@@ -628,7 +666,7 @@ tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* t, 
   b.x = h;
   b.x_row = inner_row;
   b.y = reinterpret_cast<uint8_t*>(each);
-  b.y_row = dim;
+  b.y_row = row;
   b.y_f32 = true;
   a.plan = b.plan = plan;
   a.n_rows = b.n_rows = t->n_rows;
@@ -655,8 +693,8 @@ tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* t, 
   if (!e) e = product(a, w1);
   if (!e) e = product(b, w2);
   if (!e)
-    e = t->dtype == TRE_BF16 ? launch_combine<__nv_bfloat16>(each, plan.where, t, w1->experts, dim, s)
-                             : launch_combine<__half>(each, plan.where, t, w1->experts, dim, s);
+    e = t->dtype == TRE_BF16 ? launch_combine<__nv_bfloat16>(each, row, plan.where, t, w1->experts, dim, s)
+                             : launch_combine<__half>(each, row, plan.where, t, w1->experts, dim, s);
   return e == cudaSuccess ? TRE_OK : TRE_ECUDA;
 }
 

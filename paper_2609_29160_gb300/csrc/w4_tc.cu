@@ -29,6 +29,7 @@ namespace {
 
 constexpr int kScaleWarps = 8, kCodeWarp = 8, kCodeWarps = 5, kRowWarp = 13, kRawWarp = 14, kMmaWarp = 15;
 constexpr int kThreads = 512;
+constexpr int kAsk = 12;               // stages of codes that are asked for ahead
 
 // Shared memory of a block for units of up to WIDTH rows of x. A stage of the operand lasts
 // from its last product to its next, through the turning of codes, an arrival at the other
@@ -399,10 +400,21 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
       bool alive = true;
       for (int i = pair; alive && unit_at(a, i, u); i += pairs) {
         // (past the last block of 128 rows: the last again, whose sums are not written)
+        // Copies ask for codes some way ahead of the ring, whose places are taken while codes are
+        // turned: memory's latency then stays out of that round.
         const uint4* from = w.codes_of(u.expert, min(2 * u.block + side, w.blocks - 1) * 8);
+        auto ask = [&](int c) {
+          if (c < w.chunks && lane == 0)
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from + (int64_t)c * kNextChunk),
+                         "n"(R::BYTES_RAW)
+                         : "memory");
+        };
+#pragma unroll 1
+        for (int c = 0; c < kAsk; ++c) ask(c);
 #pragma unroll 1
         for (int c = 0; c < w.chunks; ++c, ++n) {
           const uint32_t r = n % R::RAW;
+          ask(c + kAsk);
           if (!(alive = bar_wait(raw_empty + r, ((n / R::RAW) & 1) ^ 1, dead))) break;
           if (one_lane()) {
             bar_expect(raw_full + r, R::BYTES_RAW);
