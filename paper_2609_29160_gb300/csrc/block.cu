@@ -179,10 +179,12 @@ bool on(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % byte
 //
 // A warp a token, a lane every 32nd expert. Choices have to be those of the formulas, not of
 // their rounding, because one other expert is another answer. Where c grows with the logit
-// (no bias, no sums) the logits themselves are compared. Else c is computed in 32 bits, and
-// a row whose choice is closer than that can tell (a chosen one against the next, a kept
-// group against one that is not) is done once more in 64 bits, whose pipe is some sixty
-// times slower; about one row in three hundred of 256 sigmoid scores.
+// (no bias, no sums) the logits themselves are compared. Else c is computed in 32 bits. Where
+// two that follow each other in the choice are closer than 32 bits can tell (one row in some
+// hundred of 256 sigmoid scores), the chosen and all that come as near to the last of them get
+// theirs in 64 bits, a lane each, and are put in that order; where a kept group is that close
+// to one that is not (one row in 100,000), or more than 32 come near, the whole row is done in
+// 64 bits, whose pipe is some sixty times slower.
 // ---------------------------------------------------------------------------
 struct RouteArgs {
   const uint8_t* logits;
@@ -242,96 +244,198 @@ template <class F> __device__ __forceinline__ F warp_sum(F x) {
 __device__ __forceinline__ float exp_of(float x) { return expf(x); }
 __device__ __forceinline__ double exp_of(double x) { return exp(x); }
 
-// Chooses: lane i's return is the i-th expert (-1: none). `close`: whether 32 bits may have
-// decided what they cannot tell. c of a sigmoid is off by at most two units of 2^-24 for the
-// exponential, the sum and the quotient each, and the bias adds half a unit of c; a softmax's
-// sum of up to 1,024 terms adds a unit for each of its 10 levels. Both sides of a comparison.
+// 1 / (1 + exp(-x)), e^x
+__device__ __forceinline__ float sigmoid_of(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
+__device__ __forceinline__ double sigmoid_of(double x) { return 1.0 / (1.0 + exp(-x)); }
+
+// How far a c in 32 bits may be off, both sides of a comparison. The quick exponential is off by
+// (2 + 1.2 |x|) units of 2^-23 of itself, which reach a sigmoid by s (1 - s): less than 1e-7 in
+// all; its sum and quotient add 3 units of 2^-24 of s, the bias half a unit of c. A softmax's sum
+// of up to 1,024 terms adds a unit for each of its 10 levels.
+constexpr float kOffSigmoid = 7e-7f, kOffSoftmax = 3e-6f, kOffBias = 2.5e-7f;
+
+// c of expert j * 32 + lane
+template <class F>
+__device__ __forceinline__ F score(const RouteArgs& a, float l, float most, F total, int e) {
+  const F none = -(F)INFINITY;
+  if (!(l > -INFINITY)) return none;
+  if (a.raw) return (F)l;
+  F c = a.softmax ? exp_of((F)l - (F)most) / total : sigmoid_of((F)l);
+  if (a.bias) c += (F)a.bias[e];
+  return c > none ? c : none;
+}
+
+// The two largest of a lane's
+template <class F> __device__ __forceinline__ void keep_two(F x, F& first, F& second) {
+  if (x > first) {
+    second = first;
+    first = x;
+  } else if (x > second) {
+    second = x;
+  }
+}
+
+// Lane g's return: what group g counts as.
 template <class F, int NV>
-__device__ __forceinline__ int choose(const RouteArgs& a, const float* l, float most, F* room,
-                                      bool& close) {
+__device__ __forceinline__ F group_scores(const RouteArgs& a, const F* c, F* room) {
   const int lane = threadIdx.x & 31;
   const F none = -(F)INFINITY;
-  F c[NV];
-  F total = 1;
-  if (a.softmax && !a.raw) {
-    F sum = 0;
+  F mine = none, first = none, second = none;
+  if (a.per % 32 == 0) {                             // groups of whole registers
+    const int regs = a.per / 32;
+    int left = regs, g = 0;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) sum += l[j] > -INFINITY ? exp_of((F)l[j] - (F)most) : (F)0;
-    total = warp_sum(sum);
-  }
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    c[j] = none;
-    if (!(l[j] > -INFINITY)) continue;
-    if (a.raw) {
-      c[j] = (F)l[j];
-    } else {
-      c[j] = a.softmax ? exp_of((F)l[j] - (F)most) / total : (F)1 / ((F)1 + exp_of(-(F)l[j]));
-      if (a.bias) c[j] += (F)a.bias[j * 32 + lane];
-      if (!(c[j] > none)) c[j] = none;
-    }
-  }
-  const F off = a.raw || sizeof(F) == 8 ? (F)0 : a.softmax ? (F)2.5e-6 : (F)6e-7;
-  const F rel = off > 0 ? (F)2.5e-7 : (F)0;
-  close = false;
-  if (a.groups > 1) {
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (j * 32 + lane < a.experts) room[j * 32 + lane] = c[j];
-    __syncwarp();
-    F first = none, second = none;
-    if (lane < a.groups) {
-      int i = lane % a.per;                          // (lanes start apart: their banks)
-      for (int n = 0; n < a.per; ++n) {
-        const F x = room[lane * a.per + i];
-        if (x > first) {
-          second = first;
-          first = x;
-        } else if (x > second) {
-          second = x;
+    for (int j = 0; j < NV; ++j) {
+      keep_two(c[j], first, second);
+      if (--left == 0) {
+        int at = lane;
+        const F best = warp_best(first, at);
+        F sum = best;
+        if (a.group_best == 2) {
+          int unused = lane;
+          const F next = warp_best(lane == at ? second : first, unused);
+          if (next > none) sum += next;
         }
-        if (++i == a.per) i = 0;
+        if (lane == g) mine = sum;
+        ++g;
+        left = regs;
+        first = second = none;
       }
-      if (a.group_best == 2 && second > none) first += second;
     }
-    __syncwarp();
-    int better = 0;
-    F under = none;                                  // the best group below this one
-    for (int g = 0; g < a.groups; ++g) {
-      const F x = __shfl_sync(0xffffffffu, first, g);
-      if (x > first || (x == first && g < lane)) ++better;
-      else if (g != lane && x > under) under = x;
-    }
-    const unsigned kept = __ballot_sync(0xffffffffu, lane < a.groups && better < a.top_groups);
-    if (off > 0)
-      close = __any_sync(0xffffffffu, lane < a.groups && better == a.top_groups - 1 && under > none &&
-                                          !(first - under > 2 * off + rel * (fabsf((float)first) + 1)));
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (j * 32 + lane < a.experts && !(kept >> a.by_per.div(j * 32 + lane) & 1)) c[j] = none;
+    return mine;
   }
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+    if (j * 32 + lane < a.experts) room[j * 32 + lane] = c[j];
+  __syncwarp();
+  if (lane < a.groups) {
+    int i = lane % a.per;                            // (lanes start apart: their banks)
+    for (int n = 0; n < a.per; ++n) {
+      keep_two(room[lane * a.per + i], first, second);
+      if (++i == a.per) i = 0;
+    }
+    mine = first;
+    if (a.group_best == 2 && second > none) mine += second;
+  }
+  __syncwarp();
+  return mine;
+}
+
+// Takes those of groups that stay out of c; whether 32 bits may have kept the wrong ones.
+template <class F, int NV>
+__device__ __forceinline__ bool keep_groups(const RouteArgs& a, F* c, F* room, float off) {
+  const int lane = threadIdx.x & 31;
+  const F none = -(F)INFINITY, mine = group_scores<F, NV>(a, c, room);
+  int better = 0;
+  F under = none;                                    // the best group below this one
+  for (int g = 0; g < a.groups; ++g) {
+    const F x = __shfl_sync(0xffffffffu, mine, g);
+    if (x > mine || (x == mine && g < lane)) ++better;
+    else if (g != lane && x > under) under = x;
+  }
+  const unsigned kept = __ballot_sync(0xffffffffu, lane < a.groups && better < a.top_groups);
+  const bool close = lane < a.groups && better == a.top_groups - 1 && under > none &&
+                     !(mine - under > (F)(2.f * off + kOffBias * (fabsf((float)mine) + 1.f)));
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+    if (j * 32 + lane < a.experts && !(kept >> a.by_per.div(j * 32 + lane) & 1)) c[j] = none;
+  return off > 0.f && __any_sync(0xffffffffu, close);
+}
+
+// The largest c and its expert, which is taken out.
+template <class F, int NV> __device__ __forceinline__ F take_best(F* c, int& at) {
+  const int lane = threadIdx.x & 31;
+  F best = -(F)INFINITY;
+  at = 0x7fffffff;
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+    if (c[j] > best) {
+      best = c[j];
+      at = j * 32 + lane;
+    }
+  best = warp_best(best, at);
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+    if (j * 32 + lane == at) c[j] = -(F)INFINITY;
+  return best;
+}
+
+template <class F, int NV>
+__device__ __forceinline__ F softmax_total(const float* l, float most) {
+  F sum = 0;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) sum += l[j] > -INFINITY ? exp_of((F)l[j] - (F)most) : (F)0;
+  return warp_sum(sum);
+}
+
+// Lane i's return is the i-th expert of the whole row in 64 bits (-1: none).
+template <int NV>
+__device__ __noinline__ int choose_double(const RouteArgs& a, int64_t row, float most, double* room) {
+  const int lane = threadIdx.x & 31;
+  float l[NV];
+  double c[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) l[j] = j * 32 + lane < a.experts ? logit(a, row, j * 32 + lane) : -INFINITY;
+  const double total = a.softmax ? softmax_total<double, NV>(l, most) : 1.0;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) c[j] = score(a, l[j], most, total, j * 32 + lane);
+  if (a.groups > 1) keep_groups<double, NV>(a, c, room, 0.f);
   int mine = -1;
-  F before = 0;
-  const int look = a.top + (off > 0 ? 1 : 0);
-  for (int k = 0; k < look; ++k) {
-    F best = none;
-    int at = 0x7fffffff;
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (c[j] > best) {
-        best = c[j];
-        at = j * 32 + lane;
-      }
-    best = warp_best(best, at);
-    if (!(best > none)) break;
-    if (off > 0 && k > 0 && !(before - best > off + rel * fabsf((float)best))) close = true;
-    before = best;
-    if (lane == k && k < a.top) mine = at;
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (j * 32 + lane == at) c[j] = none;
+  for (int k = 0; k < a.top; ++k) {
+    int at;
+    if (!(take_best<double, NV>(c, at) > -(double)INFINITY)) break;
+    if (lane == k) mine = at;
   }
   return mine;
+}
+
+// The same in 32 bits where they can tell.
+template <int NV>
+__device__ __forceinline__ int choose(const RouteArgs& a, int64_t row, const float* l, float most, double* room) {
+  const int lane = threadIdx.x & 31;
+  float c[NV];
+  const float total = a.softmax && !a.raw ? softmax_total<float, NV>(l, most) : 1.f;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) c[j] = score(a, l[j], most, total, j * 32 + lane);
+  const float off = a.raw ? 0.f : a.softmax ? kOffSoftmax : kOffSigmoid;
+  if (a.groups > 1 && keep_groups<float, NV>(a, c, reinterpret_cast<float*>(room), off))
+    return choose_double<NV>(a, row, most, room);
+  int mine = -1, taken = 0;
+  bool close = false;
+  float before = INFINITY;
+  for (; taken < 32; ++taken) {
+    if (taken >= a.top && off == 0.f) break;
+    int at;
+    const float best = take_best<float, NV>(c, at);
+    if (!(best > -INFINITY)) break;
+    const bool near = off > 0.f && !(before - best > off + kOffBias * fabsf(best));
+    if (taken >= a.top && !near) break;              // (the last chosen, and one near it, and so on)
+    close |= near && taken > 0;
+    before = best;
+    if (lane == taken) mine = at;
+  }
+  if (!close) return mine;
+  if (taken == 32) return choose_double<NV>(a, row, most, room);
+  // The order of the taken in 64 bits
+  double x = -(double)INFINITY;
+  if (a.softmax) {
+    const double sum = softmax_total<double, NV>(l, most);
+    if (mine >= 0) x = score(a, logit(a, row, mine), most, sum, mine);
+  } else if (mine >= 0) {
+    x = score(a, logit(a, row, mine), most, 1.0, mine);
+  }
+  int better = 0, sorted = -1;
+  for (int k = 0; k < taken; ++k) {
+    const double y = __shfl_sync(0xffffffffu, x, k);
+    const int e = __shfl_sync(0xffffffffu, mine, k);
+    if (y > x || (y == x && e < mine)) ++better;
+  }
+  if (mine < 0) better = 32;
+  for (int k = 0; k < taken; ++k) {
+    const int place = __shfl_sync(0xffffffffu, better, k), e = __shfl_sync(0xffffffffu, mine, k);
+    if (place == lane) sorted = e;
+  }
+  return lane < a.top ? sorted : -1;
 }
 
 template <int NV>
@@ -348,9 +452,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32) k_route(const __grid_constan
     most = fmaxf(most, l[j]);
   }
   most = value_of(__reduce_max_sync(0xffffffffu, order(most)));
-  bool close;
-  int id = choose<float, NV>(a, l, most, reinterpret_cast<float*>(room), close);
-  if (close) id = choose<double, NV>(a, l, most, room, close);
+  const int id = choose<NV>(a, row, l, most, room);
   const float x = id >= 0 ? logit(a, row, id) : -INFINITY;
   // Weights; with their sum divided out a sigmoid's are kept from running out of exponent
   // by the largest of them.

@@ -121,7 +121,7 @@ def act(y, off):
     return s * u, 1.1 * og * u.abs() + s.abs() * ou + 1.1 * og * ou + 2.0 ** -19 * (s * u).abs()
 
 
-def experts(x, ids, weights, m1, m2, dtype, rounded=False):
+def experts(x, ids, weights, m1, m2, dtype):
     """(y, error) with m1, m2 [experts][..]; the error counts the rounding of the inner rows
     and of each expert's output (where there are many tokens)."""
     y = torch.zeros(x.shape[0], m2.shape[1], dtype=torch.float64, device=x.device)
@@ -134,8 +134,6 @@ def experts(x, ids, weights, m1, m2, dtype, rounded=False):
         oh = oh + rounding(h, dtype) * 1.01
         z, oz = product(h, m2[e])
         oz = oz + oh @ m2[e].abs().T
-        if rounded:
-            oz = oz + rounding(z.abs() + oz, dtype)
         w = weights[token, slot].double()[:, None]
         y.index_add_(0, token, w * z)
         off.index_add_(0, token, w.abs() * oz + 2.0 ** -22 * (w * z).abs())
