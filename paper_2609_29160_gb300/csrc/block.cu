@@ -181,10 +181,15 @@ bool on(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % byte
 // their rounding, because one other expert is another answer. Where c grows with the logit
 // (no bias, no sums) the logits themselves are compared. Else c is computed in 32 bits. Where
 // two that follow each other in the choice are closer than 32 bits can tell (one row in some
-// hundred of 256 sigmoid scores), the chosen and all that come as near to the last of them get
-// theirs in 64 bits, a lane each, and are put in that order; where a kept group is that close
-// to one that is not (one row in 100,000), or more than 32 come near, the whole row is done in
-// 64 bits, whose pipe is some sixty times slower.
+// hundred of 256 sigmoid scores), the candidates get theirs in 64 bits, a lane each, and are put in
+// that order; where a kept group is that close to one that is not (one row in 100,000), or there
+// are too many candidates, the whole row is done in 64 bits, whose pipe is some sixty times
+// slower.
+//
+// Candidates: the top-th largest of the lanes' own maxima is not above the top-th largest of all,
+// so that what is not below it (some ten to fifteen of 256 for the best eight) has the chosen in
+// it. They go to a lane each, which counts how many come before. Taking the best out one after
+// the other took 100 instructions each, 1.45 us for 16,384 rows.
 // ---------------------------------------------------------------------------
 struct RouteArgs {
   const uint8_t* logits;
@@ -198,17 +203,36 @@ struct RouteArgs {
   bool softmax, renorm, raw;          // raw: choices by the logits
 };
 
-constexpr int kRouteWarps = 4;
+constexpr int kRouteWarps = 8, kWideRouteWarps = 4;      // with more than 512 experts (their room)
 
+// NaN is not there, +inf the largest float.
+__device__ __forceinline__ float sane(float x) { return x != x ? -INFINITY : fminf(x, 3.402823466e38f); }
+template <class T> __device__ __forceinline__ const T* logits_of(const RouteArgs& a, int64_t row) {
+  return reinterpret_cast<const T*>(a.logits) + row * a.row;
+}
 __device__ __forceinline__ float logit(const RouteArgs& a, int64_t row, int e) {
-  const int64_t at = row * a.row + e;
-  float x;
-  if (a.dtype == TRE_F32) x = reinterpret_cast<const float*>(a.logits)[at];
-  else if (a.dtype == TRE_BF16) x = (float)reinterpret_cast<const __nv_bfloat16*>(a.logits)[at];
-  else x = (float)reinterpret_cast<const __half*>(a.logits)[at];
-  return x != x ? -INFINITY : fminf(x, 3.402823466e38f);
+  if (a.dtype == TRE_F32) return sane(logits_of<float>(a, row)[e]);
+  if (a.dtype == TRE_BF16) return sane((float)logits_of<__nv_bfloat16>(a, row)[e]);
+  return sane((float)logits_of<__half>(a, row)[e]);
+}
+// A lane's logits of a row, as they are (all loads before any is looked at).
+template <int NV> __device__ __forceinline__ void row_logits(const RouteArgs& a, int64_t row, float* l) {
+  const int lane = threadIdx.x & 31;
+  auto all = [&](const auto* p) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) l[j] = j * 32 + lane < a.experts ? (float)p[j * 32 + lane] : -INFINITY;
+  };
+  if (a.dtype == TRE_F32) all(logits_of<float>(a, row));
+  else if (a.dtype == TRE_BF16) all(logits_of<__nv_bfloat16>(a, row));
+  else all(logits_of<__half>(a, row));
 }
 
+// Largest of the lanes (none is NaN)
+__device__ __forceinline__ float warp_max(float x) {
+  float r;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
+}
 // Larger floats have larger keys; -inf is the least of those used.
 __device__ __forceinline__ uint32_t order(float x) {
   const uint32_t u = __float_as_uint(x);
@@ -259,10 +283,36 @@ template <class F>
 __device__ __forceinline__ F score(const RouteArgs& a, float l, float most, F total, int e) {
   const F none = -(F)INFINITY;
   if (!(l > -INFINITY)) return none;
-  if (a.raw) return (F)l;
+  if (a.raw) return (F)l + (F)0;                     // (-0 counts as 0)
   F c = a.softmax ? exp_of((F)l - (F)most) / total : sigmoid_of((F)l);
   if (a.bias) c += (F)a.bias[e];
   return c > none ? c : none;
+}
+
+// Those of a lane's experts (the cases outside the loop: a branch an expert costs more than c).
+template <class F, int NV>
+__device__ __forceinline__ void all_scores(const RouteArgs& a, const float* l, float most, F total, F* c) {
+  const int lane = threadIdx.x & 31;
+  const F none = -(F)INFINITY;
+  if (a.raw) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) c[j] = (F)l[j] + (F)0;
+    return;
+  }
+  if (a.softmax) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) c[j] = exp_of((F)l[j] - (F)most) / total;
+  } else {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) c[j] = sigmoid_of((F)l[j]);
+  }
+  if (a.bias) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (j * 32 + lane < a.experts) c[j] += (F)a.bias[j * 32 + lane];
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) c[j] = l[j] > -INFINITY && c[j] > none ? c[j] : none;
 }
 
 // The two largest of a lane's
@@ -288,13 +338,22 @@ __device__ __forceinline__ F group_scores(const RouteArgs& a, const F* c, F* roo
     for (int j = 0; j < NV; ++j) {
       keep_two(c[j], first, second);
       if (--left == 0) {
-        int at = lane;
-        const F best = warp_best(first, at);
-        F sum = best;
-        if (a.group_best == 2) {
-          int unused = lane;
-          const F next = warp_best(lane == at ? second : first, unused);
-          if (next > none) sum += next;
+        F sum;
+        if constexpr (sizeof(F) == 4) {
+          sum = warp_max(first);
+          if (a.group_best == 2) {
+            const int who = __ffs(__ballot_sync(0xffffffffu, first == sum)) - 1;
+            const float next = warp_max(lane == who ? second : first);
+            if (next > none) sum += next;
+          }
+        } else {
+          int at = lane;
+          sum = warp_best(first, at);
+          if (a.group_best == 2) {
+            int unused = lane;
+            const F next = warp_best(lane == at ? second : first, unused);
+            if (next > none) sum += next;
+          }
         }
         if (lane == g) mine = sum;
         ++g;
@@ -336,9 +395,23 @@ __device__ __forceinline__ bool keep_groups(const RouteArgs& a, F* c, F* room, f
   const unsigned kept = __ballot_sync(0xffffffffu, lane < a.groups && better < a.top_groups);
   const bool close = lane < a.groups && better == a.top_groups - 1 && under > none &&
                      !(mine - under > (F)(2.f * off + kOffBias * (fabsf((float)mine) + 1.f)));
+  if (a.per % 32 == 0) {
+    const int regs = a.per / 32;
+    int left = regs;
+    unsigned rest = kept;
 #pragma unroll
-  for (int j = 0; j < NV; ++j)
-    if (j * 32 + lane < a.experts && !(kept >> a.by_per.div(j * 32 + lane) & 1)) c[j] = none;
+    for (int j = 0; j < NV; ++j) {
+      if (!(rest & 1)) c[j] = none;
+      if (--left == 0) {
+        rest >>= 1;
+        left = regs;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (j * 32 + lane < a.experts && !(kept >> a.by_per.div(j * 32 + lane) & 1)) c[j] = none;
+  }
   return off > 0.f && __any_sync(0xffffffffu, close);
 }
 
@@ -377,8 +450,7 @@ __device__ __noinline__ int choose_double(const RouteArgs& a, int64_t row, float
 #pragma unroll
   for (int j = 0; j < NV; ++j) l[j] = j * 32 + lane < a.experts ? logit(a, row, j * 32 + lane) : -INFINITY;
   const double total = a.softmax ? softmax_total<double, NV>(l, most) : 1.0;
-#pragma unroll
-  for (int j = 0; j < NV; ++j) c[j] = score(a, l[j], most, total, j * 32 + lane);
+  all_scores<double, NV>(a, l, most, total, c);
   if (a.groups > 1) keep_groups<double, NV>(a, c, room, 0.f);
   int mine = -1;
   for (int k = 0; k < a.top; ++k) {
@@ -389,101 +461,143 @@ __device__ __noinline__ int choose_double(const RouteArgs& a, int64_t row, float
   return mine;
 }
 
-// The same in 32 bits where they can tell.
+// What a lane has of the choice: an expert and its place in the order (past `top`: not chosen).
+struct Choice {
+  int expert, place;
+};
+
+// The same in 32 bits where they can tell. near: the warp's room for candidates.
+struct Near {
+  float c[32];
+  int expert[32];
+};
 template <int NV>
-__device__ __forceinline__ int choose(const RouteArgs& a, int64_t row, const float* l, float most, double* room) {
+__device__ __forceinline__ Choice choose(const RouteArgs& a, int64_t row, const float* l, float most, double* room,
+                                         Near& near) {
   const int lane = threadIdx.x & 31;
   float c[NV];
   const float total = a.softmax && !a.raw ? softmax_total<float, NV>(l, most) : 1.f;
-#pragma unroll
-  for (int j = 0; j < NV; ++j) c[j] = score(a, l[j], most, total, j * 32 + lane);
-  const float off = a.raw ? 0.f : a.softmax ? kOffSoftmax : kOffSigmoid;
+  all_scores<float, NV>(a, l, most, total, c);
+  const float off = a.raw ? 0.f : a.softmax ? kOffSoftmax : kOffSigmoid, rel = a.raw ? 0.f : kOffBias;
   if (a.groups > 1 && keep_groups<float, NV>(a, c, reinterpret_cast<float*>(room), off))
-    return choose_double<NV>(a, row, most, room);
-  int mine = -1, taken = 0;
-  bool close = false;
-  float before = INFINITY;
-  for (; taken < 32; ++taken) {
-    if (taken >= a.top && off == 0.f) break;
-    int at;
-    const float best = take_best<float, NV>(c, at);
-    if (!(best > -INFINITY)) break;
-    const bool near = off > 0.f && !(before - best > off + kOffBias * fabsf(best));
-    if (taken >= a.top && !near) break;              // (the last chosen, and one near it, and so on)
-    close |= near && taken > 0;
-    before = best;
-    if (lane == taken) mine = at;
+    return Choice{choose_double<NV>(a, row, most, room), lane};
+  // the top-th largest of the lanes' maxima, and what 32 bits cannot tell from it
+  float own = c[0];
+#pragma unroll
+  for (int j = 1; j < NV; ++j) own = fmaxf(own, c[j]);
+  float least = -INFINITY;
+  for (int k = 0; k < a.top; ++k) {
+    least = warp_max(own);
+    if (own == least) own = -INFINITY;               // (all that are equal: the bound is then lower)
   }
-  if (!close) return mine;
-  if (taken == 32) return choose_double<NV>(a, row, most, room);
-  // The order of the taken in 64 bits
-  double x = -(double)INFINITY;
-  if (a.softmax) {
-    const double sum = softmax_total<double, NV>(l, most);
-    if (mine >= 0) x = score(a, logit(a, row, mine), most, sum, mine);
-  } else if (mine >= 0) {
-    x = score(a, logit(a, row, mine), most, 1.0, mine);
-  }
-  int better = 0, sorted = -1;
-  for (int k = 0; k < taken; ++k) {
-    const double y = __shfl_sync(0xffffffffu, x, k);
-    const int e = __shfl_sync(0xffffffffu, mine, k);
-    if (y > x || (y == x && e < mine)) ++better;
-  }
-  if (mine < 0) better = 32;
-  for (int k = 0; k < taken; ++k) {
-    const int place = __shfl_sync(0xffffffffu, better, k), e = __shfl_sync(0xffffffffu, mine, k);
-    if (place == lane) sorted = e;
-  }
-  return lane < a.top ? sorted : -1;
-}
-
-template <int NV>
-__global__ void __launch_bounds__(kRouteWarps * 32) k_route(const __grid_constant__ RouteArgs a) {
-  extern __shared__ double room_all[];               // [warps][experts], with groups
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t row = (int64_t)blockIdx.x * kRouteWarps + warp;
-  if (row >= a.n_rows) return;
-  double* room = room_all + warp * a.experts;
-  float l[NV], most = -INFINITY;
+  least -= off + rel * fabsf(least);
+  if (!(least > -INFINITY)) least = -INFINITY;       // (also what infinities make of it)
+  int count = 0;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    l[j] = j * 32 + lane < a.experts ? logit(a, row, j * 32 + lane) : -INFINITY;
+    const bool in = c[j] >= least && c[j] > -INFINITY;
+    const unsigned all = __ballot_sync(0xffffffffu, in);
+    const int at = count + __popc(all & ((1u << lane) - 1));
+    if (in && at < 32) {
+      near.c[at] = c[j];
+      near.expert[at] = j * 32 + lane;
+    }
+    count += __popc(all);
+  }
+  __syncwarp();
+  Choice mine{-1, 32};
+  if (count > 32) {                                  // many equal ones, or few lanes that have any
+    if (off > 0.f) return Choice{choose_double<NV>(a, row, most, room), lane};
+    for (int k = 0; k < a.top; ++k) {
+      int at;
+      if (!(take_best<float, NV>(c, at) > -INFINITY)) break;
+      if (lane == k) mine = Choice{at, k};
+    }
+    return mine;
+  }
+  // (candidates stand in the order of experts, which decides between equal ones)
+  const float x = lane < count ? near.c[lane] : -INFINITY;
+  if (lane < count) mine.expert = near.expert[lane];
+  __syncwarp();
+  int before = 0;
+  float under = -INFINITY;                           // the largest that comes after
+  for (int k = 0; k < count; ++k) {
+    const float y = __shfl_sync(0xffffffffu, x, k);
+    if (y > x || (y == x && k < lane)) ++before;
+    else if (k != lane) under = fmaxf(under, y);
+  }
+  if (lane < count) mine.place = before;
+  const bool unsure = off > 0.f && lane < count && before < a.top && under > -INFINITY &&
+                      !(x - under > off + rel * fabsf(x));
+  if (!__any_sync(0xffffffffu, unsure)) return mine;
+  const double sum = a.softmax ? softmax_total<double, NV>(l, most) : 1.0;
+  double z = -(double)INFINITY;
+  if (mine.expert >= 0) z = score(a, logit(a, row, mine.expert), most, sum, mine.expert);
+  before = 0;
+  for (int k = 0; k < count; ++k) {
+    const double y = __shfl_sync(0xffffffffu, z, k);
+    if (y > z || (y == z && k < lane)) ++before;
+  }
+  if (lane < count) mine.place = before;
+  return mine;
+}
+
+template <int NV> constexpr int route_warps = NV > 16 ? kWideRouteWarps : kRouteWarps;
+template <int NV>
+__global__ void __launch_bounds__(route_warps<NV> * 32) k_route(const __grid_constant__ RouteArgs a) {
+  extern __shared__ double room_all[];               // [warps][experts], with groups
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __shared__ Near near[kRouteWarps];
+  double* room = room_all + warp * a.experts;
+  const int64_t row = (int64_t)blockIdx.x * route_warps<NV> + warp;
+  if (row >= a.n_rows) return;
+  float l[NV], most = -INFINITY;
+  row_logits<NV>(a, row, l);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    l[j] = sane(l[j]);
     most = fmaxf(most, l[j]);
   }
-  most = value_of(__reduce_max_sync(0xffffffffu, order(most)));
-  const int id = choose<NV>(a, row, l, most, room);
-  const float x = id >= 0 ? logit(a, row, id) : -INFINITY;
+  most = warp_max(most);
+  const Choice mine = choose<NV>(a, row, l, most, room, near[warp]);
+  const bool chosen = mine.expert >= 0 && mine.place < a.top;
+  const float x = chosen ? logit(a, row, mine.expert) : -INFINITY;
   // Weights; with their sum divided out a sigmoid's are kept from running out of exponent
   // by the largest of them.
   float w = 0.f;
   if (a.renorm) {
-    const float top = value_of(__reduce_max_sync(0xffffffffu, order(x)));
-    if (id >= 0) {
+    const float top = warp_max(x);
+    if (chosen) {
       if (a.softmax) w = expf(x - top);
       else w = x >= 0.f ? 1.f / (1.f + expf(-x)) : expf(x - fminf(top, 0.f)) / (1.f + expf(x));
     }
     const float sum = warp_sum(w);
-    if (id >= 0) w = w / sum * a.scale;
+    if (chosen) w = w / sum * a.scale;
   } else if (a.softmax) {
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) sum += l[j] > -INFINITY ? expf(l[j] - most) : 0.f;
     sum = warp_sum(sum);
-    if (id >= 0) w = expf(x - most) / sum * a.scale;
-  } else if (id >= 0) {
+    if (chosen) w = expf(x - most) / sum * a.scale;
+  } else if (chosen) {
     w = 1.f / (1.f + expf(-x)) * a.scale;
   }
-  if (lane < a.top) {
-    a.ids[row * a.top + lane] = id;
-    a.weights[row * a.top + lane] = w;
+  if (chosen) {
+    a.ids[row * a.top + mine.place] = mine.expert;
+    a.weights[row * a.top + mine.place] = w;
+  }
+  const int found = __popc(__ballot_sync(0xffffffffu, chosen));
+  if (lane >= found && lane < a.top) {
+    a.ids[row * a.top + lane] = -1;
+    a.weights[row * a.top + lane] = 0.f;
   }
 }
 
 template <int NV> cudaError_t launch_route(const RouteArgs& a, cudaStream_t s) {
-  const int64_t blocks = ((int64_t)a.n_rows + kRouteWarps - 1) / kRouteWarps;
-  const size_t room = a.groups > 1 ? sizeof(double) * kRouteWarps * a.experts : 0;
-  k_route<NV><<<(unsigned)blocks, kRouteWarps * 32, room, s>>>(a);
+  constexpr int warps = route_warps<NV>;
+  const int64_t blocks = ((int64_t)a.n_rows + warps - 1) / warps;
+  const size_t room = a.groups > 1 ? sizeof(double) * warps * a.experts : 0;
+  k_route<NV><<<(unsigned)blocks, warps * 32, room, s>>>(a);
   return cudaGetLastError();
 }
 
