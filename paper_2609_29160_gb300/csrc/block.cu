@@ -248,17 +248,20 @@ __device__ __forceinline__ float warp_best(float x, int& at) {
   at = (int)__reduce_min_sync(0xffffffffu, key == top ? (uint32_t)at : 0x7fffffffu);
   return value_of(top);
 }
-__device__ __forceinline__ double warp_best(double x, int& at) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const double y = __shfl_xor_sync(0xffffffffu, x, o);
-    const int b = __shfl_xor_sync(0xffffffffu, at, o);
-    if (y > x || (y == x && b < at)) {
-      x = y;
-      at = b;
-    }
-  }
-  return x;
+// The same of doubles by their keys: comparisons of doubles would go through their slow pipe.
+__device__ __forceinline__ uint64_t order(double x) {
+  const uint64_t u = (uint64_t)__double_as_longlong(x + 0.0);
+  return u >> 63 ? ~u : u | 1ull << 63;
+}
+__device__ __forceinline__ double value_of(uint64_t key) {
+  return __longlong_as_double((long long)(key >> 63 ? key & ~(1ull << 63) : ~key));
+}
+__device__ __forceinline__ uint64_t warp_best(uint64_t key, int& at) {
+  const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(key >> 32));
+  const bool in = (uint32_t)(key >> 32) == hi;
+  const uint32_t lo = __reduce_max_sync(0xffffffffu, in ? (uint32_t)key : 0u);
+  at = (int)__reduce_min_sync(0xffffffffu, in && (uint32_t)key == lo ? (uint32_t)at : 0x7fffffffu);
+  return (uint64_t)hi << 32 | lo;
 }
 template <class F> __device__ __forceinline__ F warp_sum(F x) {
 #pragma unroll
@@ -326,11 +329,11 @@ template <class F> __device__ __forceinline__ void keep_two(F x, F& first, F& se
 }
 
 // Lane g's return: what group g counts as.
-template <class F, int NV>
-__device__ __forceinline__ F group_scores(const RouteArgs& a, const F* c, F* room) {
+template <int NV>
+__device__ __forceinline__ float group_scores(const RouteArgs& a, const float* c, float* room) {
   const int lane = threadIdx.x & 31;
-  const F none = -(F)INFINITY;
-  F mine = none, first = none, second = none;
+  const float none = -INFINITY;
+  float mine = none, first = none, second = none;
   if (a.per % 32 == 0) {                             // groups of whole registers
     const int regs = a.per / 32;
     int left = regs, g = 0;
@@ -338,22 +341,11 @@ __device__ __forceinline__ F group_scores(const RouteArgs& a, const F* c, F* roo
     for (int j = 0; j < NV; ++j) {
       keep_two(c[j], first, second);
       if (--left == 0) {
-        F sum;
-        if constexpr (sizeof(F) == 4) {
-          sum = warp_max(first);
-          if (a.group_best == 2) {
-            const int who = __ffs(__ballot_sync(0xffffffffu, first == sum)) - 1;
-            const float next = warp_max(lane == who ? second : first);
-            if (next > none) sum += next;
-          }
-        } else {
-          int at = lane;
-          sum = warp_best(first, at);
-          if (a.group_best == 2) {
-            int unused = lane;
-            const F next = warp_best(lane == at ? second : first, unused);
-            if (next > none) sum += next;
-          }
+        float sum = warp_max(first);
+        if (a.group_best == 2) {
+          const int who = __ffs(__ballot_sync(0xffffffffu, first == sum)) - 1;
+          const float next = warp_max(lane == who ? second : first);
+          if (next > none) sum += next;
         }
         if (lane == g) mine = sum;
         ++g;
@@ -379,31 +371,45 @@ __device__ __forceinline__ F group_scores(const RouteArgs& a, const F* c, F* roo
   __syncwarp();
   return mine;
 }
-
-// Takes those of groups that stay out of c; whether 32 bits may have kept the wrong ones.
-template <class F, int NV>
-__device__ __forceinline__ bool keep_groups(const RouteArgs& a, F* c, F* room, float off) {
+// The same in 64 bits, of keys.
+__device__ __forceinline__ uint64_t group_scores(const RouteArgs& a, const uint64_t* room) {
   const int lane = threadIdx.x & 31;
-  const F none = -(F)INFINITY, mine = group_scores<F, NV>(a, c, room);
-  int better = 0;
-  F under = none;                                    // the best group below this one
+  const uint64_t none = order(-(double)INFINITY);
+  if (lane >= a.groups) return none;
+  uint64_t first = none, second = none;
+  int i = lane % a.per;
+  for (int n = 0; n < a.per; ++n) {
+    keep_two(room[lane * a.per + i], first, second);
+    if (++i == a.per) i = 0;
+  }
+  if (a.group_best == 1 || second == none) return first;
+  return order(value_of(first) + value_of(second));
+}
+
+// The groups that stay, by lanes' scores of them; under: the best that comes after a lane's.
+template <class K>
+__device__ __forceinline__ unsigned kept_groups(const RouteArgs& a, K mine, K none, int& better, K& under) {
+  const int lane = threadIdx.x & 31;
+  better = 0;
+  under = none;
   for (int g = 0; g < a.groups; ++g) {
-    const F x = __shfl_sync(0xffffffffu, mine, g);
+    const K x = __shfl_sync(0xffffffffu, mine, g);
     if (x > mine || (x == mine && g < lane)) ++better;
     else if (g != lane && x > under) under = x;
   }
-  const unsigned kept = __ballot_sync(0xffffffffu, lane < a.groups && better < a.top_groups);
-  const bool close = lane < a.groups && better == a.top_groups - 1 && under > none &&
-                     !(mine - under > (F)(2.f * off + kOffBias * (fabsf((float)mine) + 1.f)));
+  return __ballot_sync(0xffffffffu, lane < a.groups && better < a.top_groups);
+}
+template <int NV, class K>
+__device__ __forceinline__ void only_kept(const RouteArgs& a, unsigned kept, K none, K* c) {
+  const int lane = threadIdx.x & 31;
   if (a.per % 32 == 0) {
     const int regs = a.per / 32;
     int left = regs;
-    unsigned rest = kept;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      if (!(rest & 1)) c[j] = none;
+      if (!(kept & 1)) c[j] = none;
       if (--left == 0) {
-        rest >>= 1;
+        kept >>= 1;
         left = regs;
       }
     }
@@ -412,13 +418,12 @@ __device__ __forceinline__ bool keep_groups(const RouteArgs& a, F* c, F* room, f
     for (int j = 0; j < NV; ++j)
       if (j * 32 + lane < a.experts && !(kept >> a.by_per.div(j * 32 + lane) & 1)) c[j] = none;
   }
-  return off > 0.f && __any_sync(0xffffffffu, close);
 }
 
 // The largest c and its expert, which is taken out.
-template <class F, int NV> __device__ __forceinline__ F take_best(F* c, int& at) {
+template <int NV, class K> __device__ __forceinline__ K take_best(K* c, K none, int& at) {
   const int lane = threadIdx.x & 31;
-  F best = -(F)INFINITY;
+  K best = none;
   at = 0x7fffffff;
 #pragma unroll
   for (int j = 0; j < NV; ++j)
@@ -429,7 +434,7 @@ template <class F, int NV> __device__ __forceinline__ F take_best(F* c, int& at)
   best = warp_best(best, at);
 #pragma unroll
   for (int j = 0; j < NV; ++j)
-    if (j * 32 + lane == at) c[j] = -(F)INFINITY;
+    if (j * 32 + lane == at) c[j] = none;
   return best;
 }
 
@@ -443,19 +448,34 @@ __device__ __forceinline__ F softmax_total(const float* l, float most) {
 
 // Lane i's return is the i-th expert of the whole row in 64 bits (-1: none).
 template <int NV>
-__device__ __noinline__ int choose_double(const RouteArgs& a, int64_t row, float most, double* room) {
+__device__ __noinline__ int choose_double(const RouteArgs& a, int64_t row, float most, uint64_t* room) {
   const int lane = threadIdx.x & 31;
-  float l[NV];
-  double c[NV];
+  const uint64_t none = order(-(double)INFINITY);
+  uint64_t c[NV];
+  {
+    float l[NV];
+    row_logits<NV>(a, row, l);
 #pragma unroll
-  for (int j = 0; j < NV; ++j) l[j] = j * 32 + lane < a.experts ? logit(a, row, j * 32 + lane) : -INFINITY;
-  const double total = a.softmax ? softmax_total<double, NV>(l, most) : 1.0;
-  all_scores<double, NV>(a, l, most, total, c);
-  if (a.groups > 1) keep_groups<double, NV>(a, c, room, 0.f);
+    for (int j = 0; j < NV; ++j) l[j] = sane(l[j]);
+    const double total = a.softmax ? softmax_total<double, NV>(l, most) : 1.0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      c[j] = j * 32 + lane < a.experts ? order(score(a, l[j], most, total, j * 32 + lane)) : none;
+  }
+  if (a.groups > 1) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (j * 32 + lane < a.experts) room[j * 32 + lane] = c[j];
+    __syncwarp();
+    int better;
+    uint64_t under;
+    only_kept<NV>(a, kept_groups(a, group_scores(a, room), none, better, under), none, c);
+    __syncwarp();
+  }
   int mine = -1;
   for (int k = 0; k < a.top; ++k) {
     int at;
-    if (!(take_best<double, NV>(c, at) > -(double)INFINITY)) break;
+    if (take_best<NV>(c, none, at) == none) break;
     if (lane == k) mine = at;
   }
   return mine;
@@ -472,15 +492,23 @@ struct Near {
   int expert[32];
 };
 template <int NV>
-__device__ __forceinline__ Choice choose(const RouteArgs& a, int64_t row, const float* l, float most, double* room,
+__device__ __forceinline__ Choice choose(const RouteArgs& a, int64_t row, const float* l, float most, uint64_t* room,
                                          Near& near) {
   const int lane = threadIdx.x & 31;
   float c[NV];
   const float total = a.softmax && !a.raw ? softmax_total<float, NV>(l, most) : 1.f;
   all_scores<float, NV>(a, l, most, total, c);
   const float off = a.raw ? 0.f : a.softmax ? kOffSoftmax : kOffSigmoid, rel = a.raw ? 0.f : kOffBias;
-  if (a.groups > 1 && keep_groups<float, NV>(a, c, reinterpret_cast<float*>(room), off))
-    return Choice{choose_double<NV>(a, row, most, room), lane};
+  if (a.groups > 1) {
+    const float score = group_scores<NV>(a, c, reinterpret_cast<float*>(room));
+    int better;
+    float under;
+    only_kept<NV>(a, kept_groups<float>(a, score, -INFINITY, better, under), (float)-INFINITY, c);
+    const bool unsure = lane < a.groups && better == a.top_groups - 1 && under > -INFINITY &&
+                        !(score - under > 2.f * off + rel * (fabsf(score) + 1.f));
+    if (off > 0.f && __any_sync(0xffffffffu, unsure))
+      return Choice{choose_double<NV>(a, row, most, room), lane};
+  }
   // the top-th largest of the lanes' maxima, and what 32 bits cannot tell from it
   float own = c[0];
 #pragma unroll
@@ -510,7 +538,7 @@ __device__ __forceinline__ Choice choose(const RouteArgs& a, int64_t row, const 
     if (off > 0.f) return Choice{choose_double<NV>(a, row, most, room), lane};
     for (int k = 0; k < a.top; ++k) {
       int at;
-      if (!(take_best<float, NV>(c, at) > -INFINITY)) break;
+      if (!(take_best<NV>(c, (float)-INFINITY, at) > -INFINITY)) break;
       if (lane == k) mine = Choice{at, k};
     }
     return mine;
@@ -545,10 +573,10 @@ __device__ __forceinline__ Choice choose(const RouteArgs& a, int64_t row, const 
 template <int NV> constexpr int route_warps = NV > 16 ? kWideRouteWarps : kRouteWarps;
 template <int NV>
 __global__ void __launch_bounds__(route_warps<NV> * 32) k_route(const __grid_constant__ RouteArgs a) {
-  extern __shared__ double room_all[];               // [warps][experts], with groups
+  extern __shared__ uint64_t room_all[];               // [warps][experts], with groups
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   __shared__ Near near[kRouteWarps];
-  double* room = room_all + warp * a.experts;
+  uint64_t* room = room_all + warp * a.experts;
   const int64_t row = (int64_t)blockIdx.x * route_warps<NV> + warp;
   if (row >= a.n_rows) return;
   float l[NV], most = -INFINITY;
@@ -596,7 +624,7 @@ __global__ void __launch_bounds__(route_warps<NV> * 32) k_route(const __grid_con
 template <int NV> cudaError_t launch_route(const RouteArgs& a, cudaStream_t s) {
   constexpr int warps = route_warps<NV>;
   const int64_t blocks = ((int64_t)a.n_rows + warps - 1) / warps;
-  const size_t room = a.groups > 1 ? sizeof(double) * warps * a.experts : 0;
+  const size_t room = a.groups > 1 ? sizeof(uint64_t) * warps * a.experts : 0;
   k_route<NV><<<(unsigned)blocks, warps * 32, room, s>>>(a);
   return cudaGetLastError();
 }

@@ -92,13 +92,15 @@ __global__ void k_w4_scales(PackArgs a, int64_t words) {
 // ---------------------------------------------------------------------------
 // Products of few rows.
 //
-// Bound by reading the codes: every warp reads two tiles of 16 rows side by side along its
-// part of k, 16 bytes a lane and tile, a block of 128 elements ahead, and multiplies them by
-// up to 8 NB rows of x with warp products whose accumulators are a group's sums (codes less
-// zeros are whole numbers, exact in 16 bits; the scale is applied once a group, in 32 bits).
-// The warps of a block share the same rows and are joined in order through shared memory.
+// Bound by reading the codes, and nearly by the instructions that turn them (some 250 for the
+// 2 KB that a step of a warp takes). A warp takes two tiles of 16 rows, 128 elements of k at a
+// time, out of a ring of its own that asynchronous copies fill three steps ahead, and multiplies
+// them by up to 8 NB rows of x with warp products whose accumulators are a group's sums (codes
+// less zeros are whole numbers, exact in 16 bits; the scale is applied once a group, in 32
+// bits). Where there are few tiles `split` warps share one and go through k in turn; their sums
+// are joined in order through shared memory.
 // ---------------------------------------------------------------------------
-constexpr int kFewWarps = 8;
+constexpr int kFewWarps = 8, kFewSteps = 4;
 
 template <class T>
 __device__ __forceinline__ void mma_few(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
@@ -116,32 +118,67 @@ __device__ __forceinline__ void mma_few(float* d, const uint32_t* a, uint32_t b0
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ uint4 load_once(const uint4* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "l"(p));
-  return v;
+__device__ __forceinline__ void copy16(void* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
+               "l"(from)
+               : "memory");
 }
 
+// A step's place in a warp's ring: codes [tile][chunk][lane], scales and zeros
+// [tile][group][g] (a group of 128 elements a step: half of their room is not used).
+template <int GROUP> struct Step {
+  static constexpr int PER = 128 / GROUP, SCALES = 2 * PER * 32;
+  static constexpr int BYTES = 2048 + 2 * SCALES;
+};
+template <int NB, int GROUP> struct FewRoom {
+  static constexpr int RING = kFewSteps * Step<GROUP>::BYTES, SUMS = 8 * NB * 33 * 4;
+  static constexpr int WARP = RING > SUMS ? (RING + 15) / 16 * 16 : (SUMS + 15) / 16 * 16;
+};
+
 template <class T, class S, int NB, int GROUP>
-__global__ void __launch_bounds__(kFewWarps * 32) k_w4_few(const __grid_constant__ ProductArgs p) {
-  constexpr int PER = 128 / GROUP;                     // groups of a block of 128 elements
-  __shared__ float sums[kFewWarps][8 * NB][33];
+__global__ void __launch_bounds__(kFewWarps * 32, 2)
+k_w4_few(const __grid_constant__ ProductArgs p, int split) {
+  using St = Step<GROUP>;
+  constexpr int PER = St::PER;
+  extern __shared__ __align__(16) uint8_t room[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const W4Args& w = p.w;
-  const int pair = blockIdx.x;
+  const int pair = blockIdx.x * (kFewWarps / split) + warp / split, part = warp % split;
   Slot slot{0, 0, p.n_rows, 0};
   if (p.plan.order) {
+    slot = p.plan.slots[blockIdx.y];                   // (there is room for all; what is past n is not used)
     if ((int)blockIdx.y >= p.plan.n[0]) return;
-    slot = p.plan.slots[blockIdx.y];
   }
-  const int64_t tile = (int64_t)slot.expert * w.tiles + 2 * pair;
-  const uint4* codes[2] = {w.codes_of(slot.expert, 2 * pair) + lane, w.codes_of(slot.expert, 2 * pair + 1) + lane};
-  const uint32_t* scales = w.scales + tile * w.groups * 8 + g;
-  const uint32_t* zeros = w.zeros + tile * w.groups * 8 + g;
-  const int64_t next_groups = (int64_t)w.groups * 8;
+  uint8_t* ring = room + warp * FewRoom<NB, GROUP>::WARP;
+  const bool works = 2 * pair < w.tiles;
+  const int pr = works ? pair : 0;
+  const int64_t tile = (int64_t)slot.expert * w.tiles + 2 * pr;
+  const uint4* codes = w.codes_of(slot.expert, 2 * pr) + lane;   // the other tile lies behind it
+  const int steps = works ? (w.chunks + 1) / 2 : 0;
+  // Step kb into the ring: two tiles of two chunks, their scales and zeros (16 bytes a lane)
+  auto fetch = [&](int kb, int at) {
+    uint8_t* to = ring + at * St::BYTES;
+    if (kb < steps) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (2 * kb + h < w.chunks)
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+            copy16(to + ((r * 2 + h) * 32 + lane) * 16, codes + (int64_t)(2 * kb + h) * kNextChunk + r * 32);
+      // pieces: two of each (tile, group)
+      const int r = lane / (2 * PER), q = lane / 2 % PER, half = lane & 1;
+      if (lane < 4 * PER && kb * PER + q < w.groups) {
+        const int64_t from = ((tile + r) * w.groups + kb * PER + q) * 8 + half * 4;
+        copy16(to + 2048 + ((r * PER + q) * 2 + half) * 16, w.scales + from);
+        if (w.zeros) copy16(to + 2048 + St::SCALES + ((r * PER + q) * 2 + half) * 16, w.zeros + from);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
   for (int from = 0; from < slot.count; from += 8 * NB) {
+    int at = 0;
+#pragma unroll
+    for (int k = 0; k < kFewSteps - 1; ++k) fetch(part + k * split, k);
     // rows of x of this lane's columns; null: none
     const T* x[NB];
 #pragma unroll
@@ -161,125 +198,145 @@ __global__ void __launch_bounds__(kFewWarps * 32) k_w4_few(const __grid_constant
       for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[r][b][e] = 0.f;
-    uint4 c[2][2];                                     // [tile][chunk of the block]
-    auto fetch = [&](int kb) {
+    for (int kb = part; kb < steps; kb += split) {
+      // elements of x are asked for before the step's codes are waited for, as many as there are
+      // registers for
+      constexpr int AHEAD = NB <= 2 ? 4 : 2;
+      uint4 v[AHEAD][NB];
+      auto look = [&](int half0) {
 #pragma unroll
-      for (int r = 0; r < 2; ++r)
+        for (int half = 0; half < AHEAD; ++half)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          c[r][h] = 2 * kb + h < w.chunks ? load_once(codes[r] + (int64_t)(2 * kb + h) * kNextChunk)
-                                          : make_uint4(0, 0, 0, 0);
-    };
-    const int blocks = (w.chunks + 1) / 2;
-    if (warp < blocks) fetch(warp);
-    for (int kb = warp; kb < blocks; kb += kFewWarps) {
-      uint4 now[2][2];
-#pragma unroll
-      for (int r = 0; r < 2; ++r)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) now[r][h] = c[r][h];
-      uint32_t sc[2][PER], ze[2][PER];
-#pragma unroll
-      for (int r = 0; r < 2; ++r)
-#pragma unroll
-        for (int q = 0; q < PER; ++q) {
-          const int at = kb * PER + q;
-          const bool there = at < w.groups;
-          sc[r][q] = there ? scales[r * next_groups + at * 8] : 0u;
-          ze[r][q] = zero_as<T, S>(there && w.zeros ? zeros[r * next_groups + at * 8]
-                                                    : Whole<S>::bits + 0x00080008u);
-        }
-      if (kb + kFewWarps < blocks) fetch(kb + kFewWarps);
-      float part[2][NB][4];
-#pragma unroll
-      for (int half = 0; half < 4; ++half) {           // 32 elements at a time
-        const int q = half * 32 / GROUP;
-        const int k0 = kb * 128 + half * 32;
-        uint4 v[NB];
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-          v[b] = x[b] && k0 < w.k ? *reinterpret_cast<const uint4*>(x[b] + k0) : make_uint4(0, 0, 0, 0);
-        if (half * 32 % GROUP == 0) {
-#pragma unroll
-          for (int r = 0; r < 2; ++r)
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) part[r][b][e] = 0.f;
-        }
-#pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const uint4& u = now[r][half >> 1];
-            const uint32_t word = (half & 1) ? (sub ? u.w : u.z) : (sub ? u.y : u.x);
-            uint32_t a[4];
-            whole<T>(word, both_lo(ze[r][q]), both_hi(ze[r][q]), a);
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-              mma_few<T>(part[r][b], a, sub ? v[b].z : v[b].x, sub ? v[b].w : v[b].y);
+          for (int b = 0; b < NB; ++b) {
+            const int k0 = kb * 128 + (half0 + half) * 32;
+            v[half][b] = x[b] && k0 < w.k ? *reinterpret_cast<const uint4*>(x[b] + k0) : make_uint4(0, 0, 0, 0);
           }
+      };
+      look(0);
+      fetch(kb + (kFewSteps - 1) * split, (at + kFewSteps - 1) % kFewSteps);
+      asm volatile("cp.async.wait_group %0;" ::"n"(kFewSteps - 1) : "memory");
+      __syncwarp();
+      const uint8_t* now = ring + at * St::BYTES;
+      at = (at + 1) % kFewSteps;
+#pragma unroll
+      for (int q = 0; q < PER; ++q) {
+        const bool there = kb * PER + q < w.groups;
+        uint32_t sc[2], z0[2], z8[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          sc[r] = there ? reinterpret_cast<const uint32_t*>(now + 2048)[(r * PER + q) * 8 + g] : 0u;
+          const uint32_t z = zero_as<T, S>(
+              there && w.zeros ? reinterpret_cast<const uint32_t*>(now + 2048 + St::SCALES)[(r * PER + q) * 8 + g]
+                               : Whole<S>::bits + 0x00080008u);
+          z0[r] = both_lo(z);
+          z8[r] = both_hi(z);
         }
-        if ((half + 1) * 32 % GROUP == 0) {
+        float sum[2][NB][4];
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[r][b][e] = 0.f;
+#pragma unroll
+        for (int h = 0; h < GROUP / 32; ++h) {           // 32 elements at a time
+          const int half = q * GROUP / 32 + h, vh = half % AHEAD;
+          if (half > 0 && vh == 0) look(half);
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            float s0, s8;
-            unpack(sc[r][q], s0, s8, S());
+            // (past the last chunk: old codes, by elements of x that are zeros)
+            const uint2 word =
+                *reinterpret_cast<const uint2*>(now + ((r * 2 + (half >> 1)) * 32 + lane) * 16 + (half & 1) * 8);
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-              acc[r][b][0] = fmaf(s0, part[r][b][0], acc[r][b][0]);
-              acc[r][b][1] = fmaf(s0, part[r][b][1], acc[r][b][1]);
-              acc[r][b][2] = fmaf(s8, part[r][b][2], acc[r][b][2]);
-              acc[r][b][3] = fmaf(s8, part[r][b][3], acc[r][b][3]);
+            for (int sub = 0; sub < 2; ++sub) {
+              uint32_t a[4];
+              whole<T>(sub ? word.y : word.x, z0[r], z8[r], a);
+#pragma unroll
+              for (int b = 0; b < NB; ++b)
+                mma_few<T>(sum[r][b], a, sub ? v[vh][b].z : v[vh][b].x, sub ? v[vh][b].w : v[vh][b].y);
             }
           }
         }
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          float s0, s8;
+          unpack(sc[r], s0, s8, S());
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            acc[r][b][0] = fmaf(s0, sum[r][b][0], acc[r][b][0]);
+            acc[r][b][1] = fmaf(s0, sum[r][b][1], acc[r][b][1]);
+            acc[r][b][2] = fmaf(s8, sum[r][b][2], acc[r][b][2]);
+            acc[r][b][3] = fmaf(s8, sum[r][b][3], acc[r][b][3]);
+          }
+        }
       }
+      __syncwarp();
     }
-    if (from > 0) __syncthreads();
+    // The sums take the ring's place: [column][row]
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncwarp();
+    auto sums = [&](int of) {
+      return reinterpret_cast<float(*)[33]>(room + of * FewRoom<NB, GROUP>::WARP);
+    };
 #pragma unroll
     for (int r = 0; r < 2; ++r)
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          sums[warp][b * 8 + 2 * t + (e & 1)][r * 16 + turn(g) + 8 * (e >> 1)] = acc[r][b][e];
-    __syncthreads();
-    const int columns = min(8 * NB, slot.count - from);
+          sums(warp)[b * 8 + 2 * t + (e & 1)][r * 16 + turn(g) + 8 * (e >> 1)] = acc[r][b][e];
+    if (split > 1) __syncthreads();
+    else __syncwarp();
+    const int columns = works ? min(8 * NB, slot.count - from) : 0;
     const bool joined = w.gated && !p.apart;
-    const int wide = joined ? 16 : 32;
-    for (int i = threadIdx.x; i < columns * wide; i += kFewWarps * 32) {
+    const int wide = joined ? 16 : 32, first = warp - part;
+    for (int i = part * 32 + lane; i < columns * wide; i += split * 32) {
       const int col = i / wide, r = i % wide;
       int64_t n = (int64_t)pair * (w.gated ? 16 : 32) + (w.gated ? r & 15 : r);
       if (n >= (w.gated ? w.n / 2 : w.n)) continue;
       if (w.gated) n += (r >> 4) * (w.n / 2);
       float a = 0.f, u = 0.f;
-#pragma unroll
-      for (int k = 0; k < kFewWarps; ++k) {
-        a += sums[k][col][r];
-        if (joined) u += sums[k][col][16 + r];
+      for (int k = 0; k < split; ++k) {
+        a += sums(first + k)[col][r];
+        if (joined) u += sums(first + k)[col][16 + r];
       }
       if (joined) a = gated(a, u);
       const int64_t row = slot.start + from + col;
       if (p.y_f32) reinterpret_cast<float*>(p.y)[row * p.y_row + n] = a;
       else reinterpret_cast<T*>(p.y)[row * p.y_row + n] = T(a);
     }
+    if (split > 1) __syncthreads();
+    else __syncwarp();
   }
 }
 
-template <class T, class S, int NB>
-cudaError_t few_by_group(int group, const ProductArgs& p, dim3 grid, cudaStream_t s) {
-  if (group == 32) k_w4_few<T, S, NB, 32><<<grid, kFewWarps * 32, 0, s>>>(p);
-  else if (group == 64) k_w4_few<T, S, NB, 64><<<grid, kFewWarps * 32, 0, s>>>(p);
-  else k_w4_few<T, S, NB, 128><<<grid, kFewWarps * 32, 0, s>>>(p);
+template <class T, class S, int NB, int GROUP>
+cudaError_t few_typed(const ProductArgs& p, int slots, cudaStream_t s) {
+  constexpr int room = kFewWarps * FewRoom<NB, GROUP>::WARP;
+  const void* fn = (const void*)k_w4_few<T, S, NB, GROUP>;
+  cudaError_t e = func_smem_once(fn, room, true);
+  if (e) return e;
+  // Warps a tile of 32 rows: the fewest that give each SM its sixteen.
+  const int64_t pairs = p.w.tiles / 2, warps = 16ll * device_sm_count(), steps = (p.w.chunks + 1) / 2;
+  int split = 1;
+  while (split < kFewWarps && pairs * slots * split < warps && split < steps) split *= 2;
+  const int per = kFewWarps / split;
+  const dim3 grid((unsigned)((pairs + per - 1) / per), (unsigned)slots);
+  k_w4_few<T, S, NB, GROUP><<<grid, kFewWarps * 32, room, s>>>(p, split);
   return cudaGetLastError();
+}
+template <class T, class S, int NB>
+cudaError_t few_by_group(int group, const ProductArgs& p, int slots, cudaStream_t s) {
+  if (group == 32) return few_typed<T, S, NB, 32>(p, slots, s);
+  if (group == 64) return few_typed<T, S, NB, 64>(p, slots, s);
+  return few_typed<T, S, NB, 128>(p, slots, s);
 }
 template <class T, class S>
 cudaError_t few_by_columns(int group, const ProductArgs& p, int columns, int slots, cudaStream_t s) {
-  const dim3 grid((unsigned)(p.w.tiles / 2), (unsigned)slots);
-  if (columns <= 8) return few_by_group<T, S, 1>(group, p, grid, s);
-  if (columns <= 16) return few_by_group<T, S, 2>(group, p, grid, s);
-  return few_by_group<T, S, 4>(group, p, grid, s);
+  if (columns <= 8) return few_by_group<T, S, 1>(group, p, slots, s);
+  if (columns <= 16) return few_by_group<T, S, 2>(group, p, slots, s);
+  if (columns <= 24) return few_by_group<T, S, 3>(group, p, slots, s);
+  return few_by_group<T, S, 4>(group, p, slots, s);
 }
 // columns: rows of x that a product has, or most have; slots: experts that may have any.
 cudaError_t launch_few(int dtype, int scale_dtype, int group, const ProductArgs& p, int64_t columns,
