@@ -102,26 +102,30 @@ __global__ void k_w4_scales(PackArgs a, int64_t words) {
 // ---------------------------------------------------------------------------
 constexpr int kFewWarps = 8, kFewSteps = 4;
 
-template <class T>
+// d = a b, or d += a b
+template <class T, bool FRESH>
 __device__ __forceinline__ void mma_few(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  if constexpr (std::is_same<T, __nv_bfloat16>::value)
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
-        "{%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-  else
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
-        "{%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+#define TRE_MMA(type)                                                                              \
+  if constexpr (FRESH)                                                                             \
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32." type "." type                            \
+                 ".f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"                  \
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])                                  \
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));        \
+  else                                                                                             \
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32." type "." type                            \
+                 ".f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"                      \
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])                                  \
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1))
+  if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+    TRE_MMA("bf16");
+  } else {
+    TRE_MMA("f16");
+  }
+#undef TRE_MMA
 }
 
-__device__ __forceinline__ void copy16(void* to, const void* from) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
-               "l"(from)
-               : "memory");
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 
 // A step's place in a warp's ring: codes [tile][chunk][lane], scales and zeros
@@ -155,41 +159,49 @@ k_w4_few(const __grid_constant__ ProductArgs p, int split) {
   const int64_t tile = (int64_t)slot.expert * w.tiles + 2 * pr;
   const uint4* codes = w.codes_of(slot.expert, 2 * pr) + lane;   // the other tile lies behind it
   const int steps = works ? (w.chunks + 1) / 2 : 0;
-  // Step kb into the ring: two tiles of two chunks, their scales and zeros (16 bytes a lane)
-  auto fetch = [&](int kb, int at) {
-    uint8_t* to = ring + at * St::BYTES;
-    if (kb < steps) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (2 * kb + h < w.chunks)
-#pragma unroll
-          for (int r = 0; r < 2; ++r)
-            copy16(to + ((r * 2 + h) * 32 + lane) * 16, codes + (int64_t)(2 * kb + h) * kNextChunk + r * 32);
-      // pieces: two of each (tile, group)
-      const int r = lane / (2 * PER), q = lane / 2 % PER, half = lane & 1;
-      if (lane < 4 * PER && kb * PER + q < w.groups) {
-        const int64_t from = ((tile + r) * w.groups + kb * PER + q) * 8 + half * 4;
-        copy16(to + 2048 + ((r * PER + q) * 2 + half) * 16, w.scales + from);
-        if (w.zeros) copy16(to + 2048 + St::SCALES + ((r * PER + q) * 2 + half) * 16, w.zeros + from);
-      }
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
+  // Each lane's copies of a step: 16 bytes of both chunks of both tiles, and of the scales and
+  // zeros of one (tile, group); all go on by `split` steps.
+  const bool scale_lane = lane < 4 * PER;
+  const int sr = lane / (2 * PER), sq = lane / 2 % PER;
+  const int64_t scale0 = ((tile + sr) * w.groups + sq) * 8 + (lane & 1) * 4;
+  const uint32_t to_scale = 2048 + ((sr * PER + sq) * 2 + (lane & 1)) * 16;
+  const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+  constexpr uint32_t kRing = kFewSteps * St::BYTES;
   for (int from = 0; from < slot.count; from += 8 * NB) {
-    int at = 0;
+    const uint4* next_codes = codes + (int64_t)part * 2 * kNextChunk;
+    int64_t next_scale = scale0 + part * PER * 8;
+    int next = part;
+    uint32_t put = 0, get = 0;                           // offsets in the ring
+    auto fetch = [&]() {
+      if (next < steps) {
+        const uint32_t to = ring_at + put + lane * 16;
+        copy16(to, next_codes);
+        copy16(to + 1024, next_codes + 32);
+        if (2 * next + 1 < w.chunks) {
+          copy16(to + 512, next_codes + kNextChunk);
+          copy16(to + 1536, next_codes + kNextChunk + 32);
+        }
+        if (scale_lane && next * PER + sq < w.groups) {
+          copy16(ring_at + put + to_scale, w.scales + next_scale);
+          if (w.zeros) copy16(ring_at + put + to_scale + St::SCALES, w.zeros + next_scale);
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      next += split;
+      next_codes += split * 2 * kNextChunk;
+      next_scale += split * PER * 8;
+      put = put + St::BYTES == kRing ? 0 : put + St::BYTES;
+    };
 #pragma unroll
-    for (int k = 0; k < kFewSteps - 1; ++k) fetch(part + k * split, k);
-    // rows of x of this lane's columns; null: none
+    for (int k = 0; k < kFewSteps - 1; ++k) fetch();
+    // rows of x of this lane's columns (of columns that are not there, the last one's: what
+    // comes of them is not written)
     const T* x[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      const int c = from + b * 8 + g;
-      x[b] = nullptr;
-      if (c < slot.count) {
-        const int place = slot.start + c;
-        const int64_t row = p.gather ? p.plan.order[place] / p.top : place;
-        x[b] = reinterpret_cast<const T*>(p.x) + row * p.x_row + 8 * t;
-      }
+      const int place = slot.start + min(from + b * 8 + g, slot.count - 1);
+      const int64_t row = p.gather ? p.plan.order[place] / p.top : place;
+      x[b] = reinterpret_cast<const T*>(p.x) + row * p.x_row + 8 * t + part * 128;
     }
     float acc[2][NB][4];
 #pragma unroll
@@ -203,48 +215,49 @@ k_w4_few(const __grid_constant__ ProductArgs p, int split) {
       // registers for
       constexpr int AHEAD = NB <= 2 ? 4 : 2;
       uint4 v[AHEAD][NB];
+      const int left = w.k - kb * 128;                   // elements from this step on
       auto look = [&](int half0) {
+        if (left >= 128) {
 #pragma unroll
-        for (int half = 0; half < AHEAD; ++half)
+          for (int half = 0; half < AHEAD; ++half)
 #pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            const int k0 = kb * 128 + (half0 + half) * 32;
-            v[half][b] = x[b] && k0 < w.k ? *reinterpret_cast<const uint4*>(x[b] + k0) : make_uint4(0, 0, 0, 0);
-          }
+            for (int b = 0; b < NB; ++b) v[half][b] = *reinterpret_cast<const uint4*>(x[b] + (half0 + half) * 32);
+        } else {                                         // past k: zeros
+#pragma unroll
+          for (int half = 0; half < AHEAD; ++half)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+              v[half][b] = (half0 + half) * 32 < left ? *reinterpret_cast<const uint4*>(x[b] + (half0 + half) * 32)
+                                                      : make_uint4(0, 0, 0, 0);
+        }
       };
       look(0);
-      fetch(kb + (kFewSteps - 1) * split, (at + kFewSteps - 1) % kFewSteps);
+      fetch();
       asm volatile("cp.async.wait_group %0;" ::"n"(kFewSteps - 1) : "memory");
       __syncwarp();
-      const uint8_t* now = ring + at * St::BYTES;
-      at = (at + 1) % kFewSteps;
+      const uint8_t* now = ring + get;
+      get = get + St::BYTES == kRing ? 0 : get + St::BYTES;
 #pragma unroll
       for (int q = 0; q < PER; ++q) {
-        const bool there = kb * PER + q < w.groups;
+        // (past the last group: whatever codes by elements of x that are zeros)
+        const bool there = PER == 1 || q * GROUP < left;
         uint32_t sc[2], z0[2], z8[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           sc[r] = there ? reinterpret_cast<const uint32_t*>(now + 2048)[(r * PER + q) * 8 + g] : 0u;
-          const uint32_t z = zero_as<T, S>(
-              there && w.zeros ? reinterpret_cast<const uint32_t*>(now + 2048 + St::SCALES)[(r * PER + q) * 8 + g]
-                               : Whole<S>::bits + 0x00080008u);
+          uint32_t z = Whole<S>::bits + 0x00080008u;
+          if (w.zeros && there) z = reinterpret_cast<const uint32_t*>(now + 2048 + St::SCALES)[(r * PER + q) * 8 + g];
+          z = zero_as<T, S>(z);
           z0[r] = both_lo(z);
           z8[r] = both_hi(z);
         }
         float sum[2][NB][4];
-#pragma unroll
-        for (int r = 0; r < 2; ++r)
-#pragma unroll
-          for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum[r][b][e] = 0.f;
 #pragma unroll
         for (int h = 0; h < GROUP / 32; ++h) {           // 32 elements at a time
           const int half = q * GROUP / 32 + h, vh = half % AHEAD;
           if (half > 0 && vh == 0) look(half);
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            // (past the last chunk: old codes, by elements of x that are zeros)
             const uint2 word =
                 *reinterpret_cast<const uint2*>(now + ((r * 2 + (half >> 1)) * 32 + lane) * 16 + (half & 1) * 8);
 #pragma unroll
@@ -252,8 +265,11 @@ k_w4_few(const __grid_constant__ ProductArgs p, int split) {
               uint32_t a[4];
               whole<T>(sub ? word.y : word.x, z0[r], z8[r], a);
 #pragma unroll
-              for (int b = 0; b < NB; ++b)
-                mma_few<T>(sum[r][b], a, sub ? v[vh][b].z : v[vh][b].x, sub ? v[vh][b].w : v[vh][b].y);
+              for (int b = 0; b < NB; ++b) {
+                const uint32_t b0 = sub ? v[vh][b].z : v[vh][b].x, b1 = sub ? v[vh][b].w : v[vh][b].y;
+                if (h == 0 && sub == 0) mma_few<T, true>(sum[r][b], a, b0, b1);
+                else mma_few<T, false>(sum[r][b], a, b0, b1);
+              }
             }
           }
         }
@@ -270,6 +286,8 @@ k_w4_few(const __grid_constant__ ProductArgs p, int split) {
           }
         }
       }
+#pragma unroll
+      for (int b = 0; b < NB; ++b) x[b] += split * 128;
       __syncwarp();
     }
     // The sums take the ring's place: [column][row]

@@ -65,12 +65,28 @@ __device__ __forceinline__ uint32_t both_lo(uint32_t x) { return __byte_perm(x, 
 __device__ __forceinline__ uint32_t both_hi(uint32_t x) { return __byte_perm(x, 0, 0x3232); }
 
 // A word of codes as whole numbers: a[i] = (half-byte i, half-byte i + 4) less the zero of
-// its row (z0: of row r, z8: of row r + 8, with kWhole, in both halves).
+// its row (z0: of row r, z8: of row r + 8, with kWhole, in both halves). Halves have room for
+// a half-byte four bits up, which is sixteen times itself there: two of three shifts become
+// part of the subtraction.
 template <class T>
 __device__ __forceinline__ void whole(uint32_t w, uint32_t z0, uint32_t z8, uint32_t* a) {
+  if constexpr (std::is_same<T, __half>::value) {
+    const __half2 part = __float2half2_rn(0.0625f);
+    // (1024 + 16 c) / 16 - (64 + z), of row r + 8; z8 has 1024 + z
+    const __half2 z = __hsub2(__float2half2_rn(960.f), *reinterpret_cast<const __half2*>(&z8));
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    a[i] = minus2<T>(((w >> (4 * i)) & 0x000f000fu) | Whole<T>::bits, i & 1 ? z8 : z0);
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t v = w >> (8 * i);
+      a[2 * i] = minus2<T>((v & 0x000f000fu) | Whole<T>::bits, z0);
+      const uint32_t up = (v & 0x00f000f0u) | Whole<T>::bits;
+      const __half2 x = __hfma2(*reinterpret_cast<const __half2*>(&up), part, z);
+      a[2 * i + 1] = *reinterpret_cast<const uint32_t*>(&x);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      a[i] = minus2<T>(((w >> (4 * i)) & 0x000f000fu) | Whole<T>::bits, i & 1 ? z8 : z0);
+  }
 }
 
 // What a gate does (the quick exponential and quotient: each within a few units of 2^-24)
