@@ -94,13 +94,14 @@ __global__ void k_w4_scales(PackArgs a, int64_t words) {
 //
 // Bound by reading the codes, and nearly by the instructions that turn them (some 250 for the
 // 2 KB that a step of a warp takes). A warp takes two tiles of 16 rows, 128 elements of k at a
-// time, out of a ring of its own that asynchronous copies fill three steps ahead, and multiplies
-// them by up to 8 NB rows of x with warp products whose accumulators are a group's sums (codes
+// time, out of a ring of its own that asynchronous copies fill two steps ahead with codes and
+// with x (elements of x loaded a step ahead into registers were waited for: 68 against @@ us for
+// 61 tokens' first product), and multiplies them by up to 8 NB rows of x with warp products whose accumulators are a group's sums (codes
 // less zeros are whole numbers, exact in 16 bits; the scale is applied once a group, in 32
 // bits). Where there are few tiles `split` warps share one and go through k in turn; their sums
 // are joined in order through shared memory.
 // ---------------------------------------------------------------------------
-constexpr int kFewWarps = 8, kFewSteps = 4;
+constexpr int kFewWarps = 8;
 
 // d = a b, or d += a b
 template <class T, bool FRESH>
@@ -128,21 +129,27 @@ __device__ __forceinline__ void copy16(uint32_t to, const void* from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 
+__device__ __forceinline__ void zero16(uint32_t to) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0) : "memory");
+}
+
 // A step's place in a warp's ring: codes [tile][chunk][lane], scales and zeros
-// [tile][group][g] (a group of 128 elements a step: half of their room is not used).
-template <int GROUP> struct Step {
-  static constexpr int PER = 128 / GROUP, SCALES = 2 * PER * 32;
-  static constexpr int BYTES = 2048 + 2 * SCALES;
-};
+// [tile][group][g], x [32 elements][8 rows][lane]; and how many there are. Two blocks an SM
+// with up to 16 rows, one with more.
 template <int NB, int GROUP> struct FewRoom {
-  static constexpr int RING = kFewSteps * Step<GROUP>::BYTES, SUMS = 8 * NB * 33 * 4;
-  static constexpr int WARP = RING > SUMS ? (RING + 15) / 16 * 16 : (SUMS + 15) / 16 * 16;
+  static constexpr int PER = 128 / GROUP, SCALES = 2 * PER * 32;
+  static constexpr int AT_SCALE = 2048, AT_ZERO = AT_SCALE + SCALES, AT_X = AT_ZERO + SCALES;
+  static constexpr int STEP = AT_X + 4 * NB * 512, STEPS = NB % 2 ? 3 : 2;
+  static constexpr int RING = STEPS * STEP, SUMS = 8 * NB * 33 * 4;
+  static constexpr int WARP = RING > SUMS ? RING : (SUMS + 15) / 16 * 16;
+  static constexpr int BLOCKS = NB <= 2 ? 2 : 1;
+  static_assert(kFewWarps * WARP * BLOCKS <= 227 * 1024, "shared memory of an SM");
 };
 
 template <class T, class S, int NB, int GROUP>
-__global__ void __launch_bounds__(kFewWarps * 32, 2)
+__global__ void __launch_bounds__(kFewWarps * 32, FewRoom<NB, GROUP>::BLOCKS)
 k_w4_few(const __grid_constant__ ProductArgs p, int split) {
-  using St = Step<GROUP>;
+  using St = FewRoom<NB, GROUP>;
   constexpr int PER = St::PER;
   extern __shared__ __align__(16) uint8_t room[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
@@ -153,7 +160,7 @@ k_w4_few(const __grid_constant__ ProductArgs p, int split) {
     slot = p.plan.slots[blockIdx.y];                   // (there is room for all; what is past n is not used)
     if ((int)blockIdx.y >= p.plan.n[0]) return;
   }
-  uint8_t* ring = room + warp * FewRoom<NB, GROUP>::WARP;
+  uint8_t* ring = room + warp * St::WARP;
   const bool works = 2 * pair < w.tiles;
   const int pr = works ? pair : 0;
   const int64_t tile = (int64_t)slot.expert * w.tiles + 2 * pr;
@@ -164,10 +171,18 @@ k_w4_few(const __grid_constant__ ProductArgs p, int split) {
   const bool scale_lane = lane < 4 * PER;
   const int sr = lane / (2 * PER), sq = lane / 2 % PER;
   const int64_t scale0 = ((tile + sr) * w.groups + sq) * 8 + (lane & 1) * 4;
-  const uint32_t to_scale = 2048 + ((sr * PER + sq) * 2 + (lane & 1)) * 16;
+  const uint32_t to_scale = St::AT_SCALE + ((sr * PER + sq) * 2 + (lane & 1)) * 16;
   const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
-  constexpr uint32_t kRing = kFewSteps * St::BYTES;
   for (int from = 0; from < slot.count; from += 8 * NB) {
+    // rows of x of this lane's columns (of columns that are not there, the last one's: what
+    // comes of them is not written)
+    const T* x[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int place = slot.start + min(from + b * 8 + g, slot.count - 1);
+      const int64_t row = p.gather ? p.plan.order[place] / p.top : place;
+      x[b] = reinterpret_cast<const T*>(p.x) + row * p.x_row + 8 * t + part * 128;
+    }
     const uint4* next_codes = codes + (int64_t)part * 2 * kNextChunk;
     int64_t next_scale = scale0 + part * PER * 8;
     int next = part;
@@ -185,24 +200,26 @@ k_w4_few(const __grid_constant__ ProductArgs p, int split) {
           copy16(ring_at + put + to_scale, w.scales + next_scale);
           if (w.zeros) copy16(ring_at + put + to_scale + St::SCALES, w.zeros + next_scale);
         }
+        const int left = w.k - next * 128;               // elements from this step on
+#pragma unroll
+        for (int half = 0; half < 4; ++half)
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            const uint32_t at = to + St::AT_X + (half * NB + b) * 512;
+            if (half * 32 < left) copy16(at, x[b] + half * 32);
+            else zero16(at);                             // past k
+          }
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
       next += split;
       next_codes += split * 2 * kNextChunk;
       next_scale += split * PER * 8;
-      put = put + St::BYTES == kRing ? 0 : put + St::BYTES;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) x[b] += split * 128;
+      put = put + St::STEP == St::RING ? 0 : put + St::STEP;
     };
 #pragma unroll
-    for (int k = 0; k < kFewSteps - 1; ++k) fetch();
-    // rows of x of this lane's columns (of columns that are not there, the last one's: what
-    // comes of them is not written)
-    const T* x[NB];
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int place = slot.start + min(from + b * 8 + g, slot.count - 1);
-      const int64_t row = p.gather ? p.plan.order[place] / p.top : place;
-      x[b] = reinterpret_cast<const T*>(p.x) + row * p.x_row + 8 * t + part * 128;
-    }
+    for (int k = 0; k < St::STEPS - 1; ++k) fetch();
     float acc[2][NB][4];
 #pragma unroll
     for (int r = 0; r < 2; ++r)
@@ -211,32 +228,12 @@ k_w4_few(const __grid_constant__ ProductArgs p, int split) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[r][b][e] = 0.f;
     for (int kb = part; kb < steps; kb += split) {
-      // elements of x are asked for before the step's codes are waited for, as many as there are
-      // registers for
-      constexpr int AHEAD = NB <= 2 ? 4 : 2;
-      uint4 v[AHEAD][NB];
-      const int left = w.k - kb * 128;                   // elements from this step on
-      auto look = [&](int half0) {
-        if (left >= 128) {
-#pragma unroll
-          for (int half = 0; half < AHEAD; ++half)
-#pragma unroll
-            for (int b = 0; b < NB; ++b) v[half][b] = *reinterpret_cast<const uint4*>(x[b] + (half0 + half) * 32);
-        } else {                                         // past k: zeros
-#pragma unroll
-          for (int half = 0; half < AHEAD; ++half)
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-              v[half][b] = (half0 + half) * 32 < left ? *reinterpret_cast<const uint4*>(x[b] + (half0 + half) * 32)
-                                                      : make_uint4(0, 0, 0, 0);
-        }
-      };
-      look(0);
       fetch();
-      asm volatile("cp.async.wait_group %0;" ::"n"(kFewSteps - 1) : "memory");
+      asm volatile("cp.async.wait_group %0;" ::"n"(St::STEPS - 1) : "memory");
       __syncwarp();
       const uint8_t* now = ring + get;
-      get = get + St::BYTES == kRing ? 0 : get + St::BYTES;
+      get = get + St::STEP == St::RING ? 0 : get + St::STEP;
+      const int left = w.k - kb * 128;
 #pragma unroll
       for (int q = 0; q < PER; ++q) {
         // (past the last group: whatever codes by elements of x that are zeros)
@@ -244,9 +241,9 @@ k_w4_few(const __grid_constant__ ProductArgs p, int split) {
         uint32_t sc[2], z0[2], z8[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          sc[r] = there ? reinterpret_cast<const uint32_t*>(now + 2048)[(r * PER + q) * 8 + g] : 0u;
+          sc[r] = there ? reinterpret_cast<const uint32_t*>(now + St::AT_SCALE)[(r * PER + q) * 8 + g] : 0u;
           uint32_t z = Whole<S>::bits + 0x00080008u;
-          if (w.zeros && there) z = reinterpret_cast<const uint32_t*>(now + 2048 + St::SCALES)[(r * PER + q) * 8 + g];
+          if (w.zeros && there) z = reinterpret_cast<const uint32_t*>(now + St::AT_ZERO)[(r * PER + q) * 8 + g];
           z = zero_as<T, S>(z);
           z0[r] = both_lo(z);
           z8[r] = both_hi(z);
@@ -254,8 +251,11 @@ k_w4_few(const __grid_constant__ ProductArgs p, int split) {
         float sum[2][NB][4];
 #pragma unroll
         for (int h = 0; h < GROUP / 32; ++h) {           // 32 elements at a time
-          const int half = q * GROUP / 32 + h, vh = half % AHEAD;
-          if (half > 0 && vh == 0) look(half);
+          const int half = q * GROUP / 32 + h;
+          uint4 v[NB];
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+            v[b] = *reinterpret_cast<const uint4*>(now + St::AT_X + (half * NB + b) * 512 + lane * 16);
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
             const uint2 word =
@@ -266,7 +266,7 @@ k_w4_few(const __grid_constant__ ProductArgs p, int split) {
               whole<T>(sub ? word.y : word.x, z0[r], z8[r], a);
 #pragma unroll
               for (int b = 0; b < NB; ++b) {
-                const uint32_t b0 = sub ? v[vh][b].z : v[vh][b].x, b1 = sub ? v[vh][b].w : v[vh][b].y;
+                const uint32_t b0 = sub ? v[b].z : v[b].x, b1 = sub ? v[b].w : v[b].y;
                 if (h == 0 && sub == 0) mma_few<T, true>(sum[r][b], a, b0, b1);
                 else mma_few<T, false>(sum[r][b], a, b0, b1);
               }
@@ -286,15 +286,13 @@ k_w4_few(const __grid_constant__ ProductArgs p, int split) {
           }
         }
       }
-#pragma unroll
-      for (int b = 0; b < NB; ++b) x[b] += split * 128;
       __syncwarp();
     }
     // The sums take the ring's place: [column][row]
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncwarp();
     auto sums = [&](int of) {
-      return reinterpret_cast<float(*)[33]>(room + of * FewRoom<NB, GROUP>::WARP);
+      return reinterpret_cast<float(*)[33]>(room + of * St::WARP);
     };
 #pragma unroll
     for (int r = 0; r < 2; ++r)
@@ -334,8 +332,8 @@ cudaError_t few_typed(const ProductArgs& p, int slots, cudaStream_t s) {
   const void* fn = (const void*)k_w4_few<T, S, NB, GROUP>;
   cudaError_t e = func_smem_once(fn, room, true);
   if (e) return e;
-  // Warps a tile of 32 rows: the fewest that give each SM its sixteen.
-  const int64_t pairs = p.w.tiles / 2, warps = 16ll * device_sm_count(), steps = (p.w.chunks + 1) / 2;
+  // Warps a tile of 32 rows: the fewest that give each SM all that it takes.
+  const int64_t pairs = p.w.tiles / 2, warps = (int64_t)FewRoom<NB, GROUP>::BLOCKS * kFewWarps * device_sm_count(), steps = (p.w.chunks + 1) / 2;
   int split = 1;
   while (split < kFewWarps && pairs * slots * split < warps && split < steps) split *= 2;
   const int per = kFewWarps / split;
