@@ -146,21 +146,17 @@ template <int NB, int GROUP> struct FewRoom {
   static_assert(kFewWarps * WARP * BLOCKS <= 227 * 1024, "shared memory of an SM");
 };
 
-template <class T, class S, int NB, int GROUP>
-__global__ void __launch_bounds__(kFewWarps * 32, FewRoom<NB, GROUP>::BLOCKS)
-k_w4_few(const __grid_constant__ ProductArgs p, int split) {
+// A warp's part of the product of its tiles with the rows of a slot. WARP: bytes of a warp's
+// room.
+template <class T, class S, int NB, int GROUP, int WARP>
+__device__ __forceinline__ void few_rows(const ProductArgs& p, const Slot& slot, int split, uint8_t* room) {
   using St = FewRoom<NB, GROUP>;
   constexpr int PER = St::PER;
-  extern __shared__ __align__(16) uint8_t room[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const W4Args& w = p.w;
   const int pair = blockIdx.x * (kFewWarps / split) + warp / split, part = warp % split;
-  Slot slot{0, 0, p.n_rows, 0};
-  if (p.plan.order) {
-    slot = p.plan.slots[blockIdx.y];                   // (there is room for all; what is past n is not used)
-    if ((int)blockIdx.y >= p.plan.n[0]) return;
-  }
-  uint8_t* ring = room + warp * St::WARP;
+  const uint32_t bits = hidden(Whole<T>::bits);
+  uint8_t* ring = room + warp * WARP;
   const bool works = 2 * pair < w.tiles;
   const int pr = works ? pair : 0;
   const int64_t tile = (int64_t)slot.expert * w.tiles + 2 * pr;
@@ -263,7 +259,7 @@ k_w4_few(const __grid_constant__ ProductArgs p, int split) {
 #pragma unroll
             for (int sub = 0; sub < 2; ++sub) {
               uint32_t a[4];
-              whole<T>(sub ? word.y : word.x, z0[r], z8[r], a);
+              whole<T>(sub ? word.y : word.x, z0[r], z8[r], bits, a);
 #pragma unroll
               for (int b = 0; b < NB; ++b) {
                 const uint32_t b0 = sub ? v[b].z : v[b].x, b1 = sub ? v[b].w : v[b].y;
@@ -292,7 +288,7 @@ k_w4_few(const __grid_constant__ ProductArgs p, int split) {
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncwarp();
     auto sums = [&](int of) {
-      return reinterpret_cast<float(*)[33]>(room + of * St::WARP);
+      return reinterpret_cast<float(*)[33]>(room + of * WARP);
     };
 #pragma unroll
     for (int r = 0; r < 2; ++r)
@@ -326,41 +322,78 @@ k_w4_few(const __grid_constant__ ProductArgs p, int split) {
   }
 }
 
+// NB: rows of x in eights; 0: one or two, as a slot has them (experts).
+template <int NB, int GROUP> struct FewKernel {
+  using One = FewRoom<NB ? NB : 1, GROUP>;
+  using Two = FewRoom<NB ? NB : 2, GROUP>;
+  static constexpr int WARP = One::WARP > Two::WARP ? One::WARP : Two::WARP, BLOCKS = Two::BLOCKS;
+};
 template <class T, class S, int NB, int GROUP>
-cudaError_t few_typed(const ProductArgs& p, int slots, cudaStream_t s) {
-  constexpr int room = kFewWarps * FewRoom<NB, GROUP>::WARP;
+__global__ void __launch_bounds__(kFewWarps * 32, FewKernel<NB, GROUP>::BLOCKS)
+k_w4_few(const __grid_constant__ ProductArgs p, int split) {
+  extern __shared__ __align__(16) uint8_t room[];
+  constexpr int WARP = FewKernel<NB, GROUP>::WARP;
+  Slot slot{0, 0, p.n_rows, 0};
+  if (p.plan.order) {
+    slot = p.plan.tiles[blockIdx.y];                   // (there is room for all; what is past n is not used)
+    if (p.first_slot + (int)blockIdx.y >= p.plan.n[0]) return;
+  }
+  if constexpr (NB > 0) {
+    few_rows<T, S, NB, GROUP, WARP>(p, slot, split, room);
+  } else {
+    if (slot.count <= 8) few_rows<T, S, 1, GROUP, WARP>(p, slot, split, room);
+    else few_rows<T, S, 2, GROUP, WARP>(p, slot, split, room);
+  }
+}
+
+template <class T, class S, int NB, int GROUP>
+cudaError_t few_typed(const ProductArgs& p, int64_t slots, cudaStream_t s) {
+  using K = FewKernel<NB, GROUP>;
+  constexpr int room = kFewWarps * K::WARP;
   const void* fn = (const void*)k_w4_few<T, S, NB, GROUP>;
   cudaError_t e = func_smem_once(fn, room, true);
   if (e) return e;
   // Warps a tile of 32 rows: the fewest that give each SM all that it takes.
-  const int64_t pairs = p.w.tiles / 2, warps = (int64_t)FewRoom<NB, GROUP>::BLOCKS * kFewWarps * device_sm_count(), steps = (p.w.chunks + 1) / 2;
+  const int64_t pairs = p.w.tiles / 2, warps = (int64_t)K::BLOCKS * kFewWarps * device_sm_count();
+  const int64_t steps = (p.w.chunks + 1) / 2;
   int split = 1;
   while (split < kFewWarps && pairs * slots * split < warps && split < steps) split *= 2;
   const int per = kFewWarps / split;
-  const dim3 grid((unsigned)((pairs + per - 1) / per), (unsigned)slots);
-  k_w4_few<T, S, NB, GROUP><<<grid, kFewWarps * 32, room, s>>>(p, split);
-  return cudaGetLastError();
+  for (int64_t from = 0; from < slots; from += 65535) {          // (a grid has no more rows)
+    ProductArgs q = p;
+    if (q.plan.order) {
+      q.plan.tiles += from;
+      q.first_slot = (int32_t)from;
+    }
+    const dim3 grid((unsigned)((pairs + per - 1) / per), (unsigned)std::min<int64_t>(slots - from, 65535));
+    k_w4_few<T, S, NB, GROUP><<<grid, kFewWarps * 32, room, s>>>(q, split);
+    e = cudaGetLastError();
+    if (e) return e;
+  }
+  return cudaSuccess;
 }
 template <class T, class S, int NB>
-cudaError_t few_by_group(int group, const ProductArgs& p, int slots, cudaStream_t s) {
+cudaError_t few_by_group(int group, const ProductArgs& p, int64_t slots, cudaStream_t s) {
   if (group == 32) return few_typed<T, S, NB, 32>(p, slots, s);
   if (group == 64) return few_typed<T, S, NB, 64>(p, slots, s);
   return few_typed<T, S, NB, 128>(p, slots, s);
 }
 template <class T, class S>
-cudaError_t few_by_columns(int group, const ProductArgs& p, int columns, int slots, cudaStream_t s) {
-  if (columns <= 8) return few_by_group<T, S, 1>(group, p, slots, s);
-  if (columns <= 16) return few_by_group<T, S, 2>(group, p, slots, s);
-  if (columns <= 24) return few_by_group<T, S, 3>(group, p, slots, s);
-  return few_by_group<T, S, 4>(group, p, slots, s);
+cudaError_t few_by_columns(int group, const ProductArgs& p, cudaStream_t s) {
+  if (p.n_rows <= 8) return few_by_group<T, S, 1>(group, p, 1, s);
+  if (p.n_rows <= 16) return few_by_group<T, S, 2>(group, p, 1, s);
+  if (p.n_rows <= 24) return few_by_group<T, S, 3>(group, p, 1, s);
+  return few_by_group<T, S, 4>(group, p, 1, s);
 }
-// columns: rows of x that a product has, or most have; slots: experts that may have any.
-cudaError_t launch_few(int dtype, int scale_dtype, int group, const ProductArgs& p, int64_t columns,
-                       int slots, cudaStream_t s) {
-  const int c = (int)std::min<int64_t>(columns, 32);
-  if (dtype == TRE_BF16) return few_by_columns<__nv_bfloat16, __nv_bfloat16>(group, p, c, slots, s);
-  return scale_dtype == TRE_BF16 ? few_by_columns<__half, __nv_bfloat16>(group, p, c, slots, s)
-                                 : few_by_columns<__half, __half>(group, p, c, slots, s);
+// tiles: pieces that a plan has at most.
+cudaError_t launch_few(int dtype, int scale_dtype, int group, const ProductArgs& p, int64_t tiles,
+                       cudaStream_t s) {
+  if (p.plan.order)
+    return dtype == TRE_BF16 ? few_by_group<__nv_bfloat16, __nv_bfloat16, 0>(group, p, tiles, s)
+                             : few_by_group<__half, __half, 0>(group, p, tiles, s);
+  if (dtype == TRE_BF16) return few_by_columns<__nv_bfloat16, __nv_bfloat16>(group, p, s);
+  return scale_dtype == TRE_BF16 ? few_by_columns<__half, __nv_bfloat16>(group, p, s)
+                                 : few_by_columns<__half, __half>(group, p, s);
 }
 
 // Rows up to which a plain product is k_w4_few's.
@@ -372,7 +405,7 @@ cudaError_t launch_rows(int dtype, int scale_dtype, int group, const ProductArgs
     const cudaError_t e = launch_w4_tc(dtype, scale_dtype, group, p, p.n_rows, 0, diag, s);
     if (e != cudaErrorNotSupported) return e;
   }
-  return launch_few(dtype, scale_dtype, group, p, p.n_rows, 1, s);
+  return launch_few(dtype, scale_dtype, group, p, 0, s);
 }
 
 // ---------------------------------------------------------------------------
@@ -434,7 +467,7 @@ constexpr int kFewTokens = 12;       // tokens an expert up to which k_w4_few is
 __global__ void __launch_bounds__(kPlanThreads) k_plan(const int32_t* ids, int64_t pairs, int experts,
                                                        PlanArgs plan, tre_diag* diag) {
   __shared__ int32_t count[kMaxExperts];
-  __shared__ int32_t warp_sums[3][32];
+  __shared__ int32_t warp_sums[2][32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   count[tid] = 0;
   __syncthreads();
@@ -455,9 +488,9 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const int32_t* ids, int64
   __syncthreads();
   const int mine = count[tid];
   const int tiles = (mine + plan.piece - 1) / plan.piece;
-  int v[3] = {mine, mine > 0, tiles};                // places, slots, tiles before this expert
+  int v[2] = {mine, tiles};                          // places and tiles up to this expert
 #pragma unroll
-  for (int x = 0; x < 3; ++x) {
+  for (int x = 0; x < 2; ++x) {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int y = __shfl_up_sync(0xffffffffu, v[x], o);
@@ -466,7 +499,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const int32_t* ids, int64
     if (lane == 31) warp_sums[x][warp] = v[x];
   }
   __syncthreads();
-  if (warp < 3) {
+  if (warp < 2) {
     int y = warp_sums[warp][lane];
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -477,19 +510,17 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const int32_t* ids, int64
   }
   __syncthreads();
 #pragma unroll
-  for (int x = 0; x < 3; ++x) v[x] += warp > 0 ? warp_sums[x][warp - 1] : 0;
+  for (int x = 0; x < 2; ++x) v[x] += warp > 0 ? warp_sums[x][warp - 1] : 0;
   const int start = v[0] - mine;
   if (mine > 0) {
-    plan.slots[v[1] - 1] = Slot{tid, start, mine, 0};
     // pieces of one size, whole sixteens
     const int size = ((mine + tiles - 1) / tiles + 15) / 16 * 16;
     for (int k = 0; k < tiles; ++k)
-      plan.tiles[v[2] - tiles + k] = Slot{tid, start + k * size, max(0, min(size, mine - k * size)), 0};
+      plan.tiles[v[1] - tiles + k] = Slot{tid, start + k * size, max(0, min(size, mine - k * size)), 0};
   }
   if (tid == kPlanThreads - 1) {
     plan.n[0] = v[1];
-    plan.n[1] = v[2];
-    plan.n[2] = v[0];
+    plan.n[1] = v[0];
   }
   __syncthreads();
   count[tid] = start;
@@ -517,7 +548,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const int32_t* ids, int64
 __global__ void __launch_bounds__(kRowThreads) k_gather(const uint4* x, int64_t x_row, int pieces, int top,
                                                         PlanArgs plan, int64_t pairs, uint4* to) {
   const int64_t place = blockIdx.x;
-  if (place >= plan.n[2]) return;                      // (pairs of no expert have no place)
+  if (place >= plan.n[1]) return;                      // (pairs of no expert have no place)
   const int64_t row = plan.order[place] / top;
   for (int i = threadIdx.x; i < pieces; i += kRowThreads) to[place * pieces + i] = x[row * x_row + i];
 }
@@ -716,10 +747,9 @@ tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* t, 
   PlanArgs plan;
   plan.order = arena.take<int32_t>(pairs);
   plan.where = arena.take<int32_t>(pairs);
-  plan.slots = arena.take<Slot>(slots);
-  plan.piece = pairs <= 64 * slots ? 128 : kTileTokens;
+  plan.piece = few ? 16 : pairs <= 64 * slots ? 128 : kTileTokens;
   plan.tiles = arena.take<Slot>(slots + pairs / plan.piece);
-  plan.n = arena.take<int32_t>(3);
+  plan.n = arena.take<int32_t>(2);
   uint8_t* h = arena.take<uint8_t>((size_t)pairs * inner_row * 2);
   const int row = (dim + 3) / 4 * 4;                  // of `each`
   float* each = arena.take<float>((size_t)pairs * row);
@@ -747,7 +777,7 @@ tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* t, 
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   k_plan<<<1, kPlanThreads, 0, s>>>(t->ids, pairs, w1->experts, plan, diag);
   cudaError_t e = cudaGetLastError();
-  const int64_t columns = (pairs + slots - 1) / slots * 2, tiles = slots + pairs / plan.piece;
+  const int64_t tiles = slots + pairs / plan.piece;
   if (!few && !e) {
     k_gather<<<(unsigned)pairs, kRowThreads, 0, s>>>(static_cast<const uint4*>(t->x), t->x_row / 8, w1->k / 8,
                                                      t->top, plan, pairs, gathered);
@@ -761,7 +791,7 @@ tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* t, 
       const cudaError_t x = launch_w4_tc(t->dtype, t->dtype, w->group, p, pairs, tiles, diag, s);
       if (x != cudaErrorNotSupported) return x;
     }
-    return launch_few(t->dtype, t->dtype, w->group, p, columns, (int)slots, s);
+    return launch_few(t->dtype, t->dtype, w->group, p, tiles, s);
   };
   if (!e) e = product(a, w1);
   if (!e) e = product(b, w2);

@@ -68,8 +68,21 @@ __device__ __forceinline__ uint32_t both_hi(uint32_t x) { return __byte_perm(x, 
 // its row (z0: of row r, z8: of row r + 8, with kWhole, in both halves). Halves have room for
 // a half-byte four bits up, which is sixteen times itself there: two of three shifts become
 // part of the subtraction.
+// (w & mask) | bits in one operation, which has room for one constant: `bits` is kept from the
+// compiler's sight in a register (with both constants in sight it made two of it).
+__device__ __forceinline__ uint32_t hidden(uint32_t bits) {
+  uint32_t r;
+  asm volatile("mov.b32 %0, %1;" : "=r"(r) : "r"(bits));
+  return r;
+}
+template <uint32_t MASK> __device__ __forceinline__ uint32_t masked(uint32_t w, uint32_t bits) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(w), "n"(MASK), "r"(bits));
+  return r;
+}
+// bits: hidden(Whole<T>::bits)
 template <class T>
-__device__ __forceinline__ void whole(uint32_t w, uint32_t z0, uint32_t z8, uint32_t* a) {
+__device__ __forceinline__ void whole(uint32_t w, uint32_t z0, uint32_t z8, uint32_t bits, uint32_t* a) {
   if constexpr (std::is_same<T, __half>::value) {
     const __half2 part = __float2half2_rn(0.0625f);
     // (1024 + 16 c) / 16 - (64 + z), of row r + 8; z8 has 1024 + z
@@ -77,15 +90,14 @@ __device__ __forceinline__ void whole(uint32_t w, uint32_t z0, uint32_t z8, uint
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const uint32_t v = w >> (8 * i);
-      a[2 * i] = minus2<T>((v & 0x000f000fu) | Whole<T>::bits, z0);
-      const uint32_t up = (v & 0x00f000f0u) | Whole<T>::bits;
+      a[2 * i] = minus2<T>(masked<0x000f000fu>(v, bits), z0);
+      const uint32_t up = masked<0x00f000f0u>(v, bits);
       const __half2 x = __hfma2(*reinterpret_cast<const __half2*>(&up), part, z);
       a[2 * i + 1] = *reinterpret_cast<const uint32_t*>(&x);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      a[i] = minus2<T>(((w >> (4 * i)) & 0x000f000fu) | Whole<T>::bits, i & 1 ? z8 : z0);
+    for (int i = 0; i < 4; ++i) a[i] = minus2<T>(masked<0x000f000fu>(w >> (4 * i), bits), i & 1 ? z8 : z0);
   }
 }
 
@@ -102,9 +114,8 @@ struct Slot {
 struct PlanArgs {
   int32_t* order;                      // [pairs]
   int32_t* where;                      // [pairs]: the place of a pair
-  Slot* slots;                         // experts that have any
   Slot* tiles;                         // their places in pieces of up to `piece`
-  int32_t* n;                          // [3]: how many slots, tiles, places
+  int32_t* n;                          // [2]: how many tiles, places
   int32_t piece;
 };
 constexpr int kTileTokens = 256;       // columns of a product on the tensor cores
@@ -118,6 +129,7 @@ struct ProductArgs {
   int64_t y_row;
   PlanArgs plan;                       // order null: rows as they are, one matrix
   int32_t n_rows, top;
+  int32_t first_slot;                  // of the plan's pieces that a launch of k_w4_few takes
   bool gather;                         // x's rows are tokens', by place
   bool y_f32;                          // and with it
   bool apart;                          // a gated matrix's two halves as they are

@@ -62,7 +62,7 @@ __device__ __forceinline__ bool unit_at(const TcArgs& a, int u, Unit& w) {
   const int t = u / a.row_blocks;
   w.block = u - t * a.row_blocks;
   if (a.p.plan.order) {
-    if (t >= a.p.plan.n[1]) return false;
+    if (t >= a.p.plan.n[0]) return false;
     const Slot s = a.p.plan.tiles[t];
     w.expert = s.expert;
     w.start = s.start;
@@ -321,6 +321,7 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
     // A warp takes every fifth stage: what happens to one, step after step, takes three times
     // as long as its products.
     const int cw = warp - kCodeWarp, g = lane >> 2, t = lane & 3;
+    const uint32_t bits = hidden(Whole<T>::bits);
     uint32_t n = 0, own = cw;                            // stages so far, and this warp's next
     bool alive = true;
     for (int i = pair; alive && unit_at(a, i, u); i += pairs) {
@@ -355,8 +356,8 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
           for (int h = 0; h < 2; ++h) {                  // 32 elements each
             const uint32_t zz = z[x][h * (PER - 1)];
             uint32_t p[4], q[4];
-            whole<T>(h ? code.z : code.x, both_lo(zz), both_hi(zz), p);
-            whole<T>(h ? code.w : code.y, both_lo(zz), both_hi(zz), q);
+            whole<T>(h ? code.z : code.x, both_lo(zz), both_hi(zz), bits, p);
+            whole<T>(h ? code.w : code.y, both_lo(zz), both_hi(zz), bits, q);
             const int at = ((4 * h + t) ^ (row & 7)) << 4;
             *reinterpret_cast<uint4*>(to + row * 128 + at) = make_uint4(p[0], p[2], q[0], q[2]);
             *reinterpret_cast<uint4*>(to + (row + 8) * 128 + at) = make_uint4(p[1], p[3], q[1], q[3]);
