@@ -90,6 +90,26 @@ __global__ void k_w4_scales(PackArgs a, int64_t words) {
 }
 
 // ---------------------------------------------------------------------------
+// Launches that may begin while the one before still runs (programmatic serialisation): what
+// it has written is read after after_launch alone, which every block comes to.
+__device__ __forceinline__ void after_launch() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+template <class... A, class... B>
+cudaError_t launch_behind(void (*kernel)(A...), dim3 grid, int threads, int room, cudaStream_t s, B... args) {
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t c{};
+  c.gridDim = grid;
+  c.blockDim = dim3((unsigned)threads);
+  c.dynamicSmemBytes = (size_t)room;
+  c.stream = s;
+  c.attrs = &at;
+  c.numAttrs = 1;
+  return cudaLaunchKernelEx(&c, kernel, A(args)...);
+}
+
+// ---------------------------------------------------------------------------
 // Products of few rows.
 //
 // Bound by reading the codes, and nearly by the instructions that turn them (some 250 for the
@@ -170,52 +190,55 @@ __device__ __forceinline__ void few_rows(const ProductArgs& p, const Slot& slot,
   const uint32_t to_scale = St::AT_SCALE + ((sr * PER + sq) * 2 + (lane & 1)) * 16;
   const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
   for (int from = 0; from < slot.count; from += 8 * NB) {
-    // rows of x of this lane's columns (of columns that are not there, the last one's: what
-    // comes of them is not written)
-    const T* x[NB];
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int place = slot.start + min(from + b * 8 + g, slot.count - 1);
-      const int64_t row = p.gather ? p.plan.order[place] / p.top : place;
-      x[b] = reinterpret_cast<const T*>(p.x) + row * p.x_row + 8 * t + part * 128;
-    }
     const uint4* next_codes = codes + (int64_t)part * 2 * kNextChunk;
     int64_t next_scale = scale0 + part * PER * 8;
-    int next = part;
-    uint32_t put = 0, get = 0;                           // offsets in the ring
-    auto fetch = [&]() {
-      if (next < steps) {
-        const uint32_t to = ring_at + put + lane * 16;
-        copy16(to, next_codes);
-        copy16(to + 1024, next_codes + 32);
-        if (2 * next + 1 < w.chunks) {
-          copy16(to + 512, next_codes + kNextChunk);
-          copy16(to + 1536, next_codes + kNextChunk + 32);
-        }
-        if (scale_lane && next * PER + sq < w.groups) {
-          copy16(ring_at + put + to_scale, w.scales + next_scale);
-          if (w.zeros) copy16(ring_at + put + to_scale + St::SCALES, w.zeros + next_scale);
-        }
-        const int left = w.k - next * 128;               // elements from this step on
+    const T* x[NB];
+    uint32_t get = 0, put = (St::STEPS - 1) * St::STEP;  // offsets in the ring
+    // Step `step` into the ring at `at`, `ahead` steps of this warp's after what the pointers name
+    auto fetch_codes = [&](int step, int ahead, uint32_t at) {
+      if (step >= steps) return;
+      const uint4* from = next_codes + ahead * split * 2 * kNextChunk;
+      const uint32_t to = ring_at + at + lane * 16;
+      copy16(to, from);
+      copy16(to + 1024, from + 32);
+      if (2 * step + 1 < w.chunks) {
+        copy16(to + 512, from + kNextChunk);
+        copy16(to + 1536, from + kNextChunk + 32);
+      }
+      if (scale_lane && step * PER + sq < w.groups) {
+        const int64_t scale = next_scale + ahead * split * PER * 8;
+        copy16(ring_at + at + to_scale, w.scales + scale);
+        if (w.zeros) copy16(ring_at + at + to_scale + St::SCALES, w.zeros + scale);
+      }
+    };
+    auto fetch_x = [&](int step, int ahead, uint32_t at) {
+      if (step < steps) {
+        const int left = w.k - step * 128;               // elements from this step on
+        const uint32_t to = ring_at + at + St::AT_X + lane * 16;
 #pragma unroll
         for (int half = 0; half < 4; ++half)
 #pragma unroll
           for (int b = 0; b < NB; ++b) {
-            const uint32_t at = to + St::AT_X + (half * NB + b) * 512;
-            if (half * 32 < left) copy16(at, x[b] + half * 32);
-            else zero16(at);                             // past k
+            if (half * 32 < left) copy16(to + (half * NB + b) * 512, x[b] + ahead * split * 128 + half * 32);
+            else zero16(to + (half * NB + b) * 512);     // past k
           }
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
-      next += split;
-      next_codes += split * 2 * kNextChunk;
-      next_scale += split * PER * 8;
-#pragma unroll
-      for (int b = 0; b < NB; ++b) x[b] += split * 128;
-      put = put + St::STEP == St::RING ? 0 : put + St::STEP;
     };
+    // (codes do not depend on the launch before, x may)
 #pragma unroll
-    for (int k = 0; k < St::STEPS - 1; ++k) fetch();
+    for (int k = 0; k < St::STEPS - 1; ++k) fetch_codes(part + k * split, k, k * St::STEP);
+    if (from == 0) after_launch();
+    // rows of x of this lane's columns (of columns that are not there, the last one's: what
+    // comes of them is not written)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int place = slot.start + min(from + b * 8 + g, slot.count - 1);
+      const int64_t row = !p.gather ? place : (p.plan.order ? p.plan.order[place] : place) / p.top;
+      x[b] = reinterpret_cast<const T*>(p.x) + row * p.x_row + 8 * t + part * 128;
+    }
+#pragma unroll
+    for (int k = 0; k < St::STEPS - 1; ++k) fetch_x(part + k * split, k, k * St::STEP);
     float acc[2][NB][4];
 #pragma unroll
     for (int r = 0; r < 2; ++r)
@@ -224,7 +247,14 @@ __device__ __forceinline__ void few_rows(const ProductArgs& p, const Slot& slot,
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[r][b][e] = 0.f;
     for (int kb = part; kb < steps; kb += split) {
-      fetch();
+      constexpr int AHEAD = St::STEPS - 1;
+      fetch_codes(kb + AHEAD * split, AHEAD, put);
+      fetch_x(kb + AHEAD * split, AHEAD, put);
+      put = put + St::STEP == St::RING ? 0 : put + St::STEP;
+      next_codes += split * 2 * kNextChunk;
+      next_scale += split * PER * 8;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) x[b] += split * 128;
       asm volatile("cp.async.wait_group %0;" ::"n"(St::STEPS - 1) : "memory");
       __syncwarp();
       const uint8_t* now = ring + get;
@@ -333,10 +363,20 @@ __global__ void __launch_bounds__(kFewWarps * 32, FewKernel<NB, GROUP>::BLOCKS)
 k_w4_few(const __grid_constant__ ProductArgs p, int split) {
   extern __shared__ __align__(16) uint8_t room[];
   constexpr int WARP = FewKernel<NB, GROUP>::WARP;
+  let_next();
   Slot slot{0, 0, p.n_rows, 0};
-  if (p.plan.order) {
-    slot = p.plan.tiles[blockIdx.y];                   // (there is room for all; what is past n is not used)
-    if (p.first_slot + (int)blockIdx.y >= p.plan.n[0]) return;
+  const int piece = p.first_slot + (int)blockIdx.y;
+  if (p.ids) {                                         // a pair of a token and its expert each
+    const int e = p.ids[piece];
+    slot = Slot{e, piece, e >= 0 && e < p.w.experts ? 1 : 0, 0};
+  } else if (p.plan.order) {
+    after_launch();
+    if (piece < p.plan.n[0]) slot = p.plan.tiles[piece];
+    else slot.count = 0;
+  }
+  if (slot.count == 0) {
+    after_launch();
+    return;
   }
   if constexpr (NB > 0) {
     few_rows<T, S, NB, GROUP, WARP>(p, slot, split, room);
@@ -361,13 +401,12 @@ cudaError_t few_typed(const ProductArgs& p, int64_t slots, cudaStream_t s) {
   const int per = kFewWarps / split;
   for (int64_t from = 0; from < slots; from += 65535) {          // (a grid has no more rows)
     ProductArgs q = p;
-    if (q.plan.order) {
-      q.plan.tiles += from;
-      q.first_slot = (int32_t)from;
-    }
+    q.first_slot = (int32_t)from;
     const dim3 grid((unsigned)((pairs + per - 1) / per), (unsigned)std::min<int64_t>(slots - from, 65535));
-    k_w4_few<T, S, NB, GROUP><<<grid, kFewWarps * 32, room, s>>>(q, split);
-    e = cudaGetLastError();
+    // (behind the plan, or behind the first product)
+    if (p.behind && from == 0) e = launch_behind(k_w4_few<T, S, NB, GROUP>, grid, kFewWarps * 32, room, s, q, split);
+    else k_w4_few<T, S, NB, GROUP><<<grid, kFewWarps * 32, room, s>>>(q, split);
+    if (!e) e = cudaGetLastError();
     if (e) return e;
   }
   return cudaSuccess;
@@ -385,9 +424,12 @@ cudaError_t few_by_columns(int group, const ProductArgs& p, cudaStream_t s) {
   if (p.n_rows <= 24) return few_by_group<T, S, 3>(group, p, 1, s);
   return few_by_group<T, S, 4>(group, p, 1, s);
 }
-// tiles: pieces that a plan has at most.
+// tiles: pairs, or pieces that a plan has at most.
 cudaError_t launch_few(int dtype, int scale_dtype, int group, const ProductArgs& p, int64_t tiles,
                        cudaStream_t s) {
+  if (p.ids)
+    return dtype == TRE_BF16 ? few_by_group<__nv_bfloat16, __nv_bfloat16, 1>(group, p, tiles, s)
+                             : few_by_group<__half, __half, 1>(group, p, tiles, s);
   if (p.plan.order)
     return dtype == TRE_BF16 ? few_by_group<__nv_bfloat16, __nv_bfloat16, 0>(group, p, tiles, s)
                              : few_by_group<__half, __half, 0>(group, p, tiles, s);
@@ -469,6 +511,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const int32_t* ids, int64
   __shared__ int32_t count[kMaxExperts];
   __shared__ int32_t warp_sums[2][32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  let_next();
   count[tid] = 0;
   __syncthreads();
   unsigned long long past = 0;
@@ -553,21 +596,26 @@ __global__ void __launch_bounds__(kRowThreads) k_gather(const uint4* x, int64_t 
   for (int i = threadIdx.x; i < pieces; i += kRowThreads) to[place * pieces + i] = x[row * x_row + i];
 }
 
-// y[t] = sum over j, in order, of weights[t][j] * each[where[t * top + j]]; a row of `each` has
-// whole fours (row elements). Four elements a thread.
+// y[t] = sum over j, in order, of weights[t][j] * each[where[t * top + j]] (where null: the pair's
+// own number); a row of `each` has whole fours (row elements). Four elements a thread.
 template <class T>
 __global__ void __launch_bounds__(kRowThreads) k_combine(const float* each, const int32_t* where,
                                                          const int32_t* ids, const float* weights,
                                                          int experts, int top, int dim, int row, T* y,
-                                                         int64_t y_row) {
+                                                         int64_t y_row, tre_diag* diag) {
   __shared__ int32_t place[32];
   __shared__ float weight[32];
   const int64_t t = blockIdx.x;
+  after_launch();
   const int i = (blockIdx.y * kRowThreads + threadIdx.x) * 4;
   if (threadIdx.x < top) {
     const int e = ids[t * top + threadIdx.x];
     const bool there = e >= 0 && e < experts;
-    place[threadIdx.x] = there ? where[t * top + threadIdx.x] : -1;
+    const int64_t pair = t * top + threadIdx.x;
+    place[threadIdx.x] = !there ? -1 : where ? where[pair] : (int)pair;
+    // (without a plan nobody has counted those yet)
+    if (!where && diag && e >= experts && blockIdx.y == 0)
+      atomicAdd(reinterpret_cast<unsigned long long*>(&diag->dropped_range), 1ull);
     weight[threadIdx.x] = weights[t * top + threadIdx.x];
   }
   __syncthreads();
@@ -593,11 +641,10 @@ __global__ void __launch_bounds__(kRowThreads) k_combine(const float* each, cons
 
 template <class T>
 cudaError_t launch_combine(const float* each, int row, const int32_t* where, const tre_tokens* t, int experts,
-                           int dim, cudaStream_t s) {
+                           int dim, tre_diag* diag, cudaStream_t s) {
   const dim3 grid((unsigned)t->n_rows, (unsigned)((dim + 4 * kRowThreads - 1) / (4 * kRowThreads)));
-  k_combine<T><<<grid, kRowThreads, 0, s>>>(each, where, t->ids, t->weights, experts, t->top, dim, row,
-                                            static_cast<T*>(t->y), t->y_row);
-  return cudaGetLastError();
+  return launch_behind(k_combine<T>, grid, kRowThreads, 0, s, each, where, t->ids, t->weights, experts, t->top,
+                       dim, row, static_cast<T*>(t->y), t->y_row, diag);
 }
 
 bool half_type(int d) { return d == TRE_BF16 || d == TRE_F16; }
@@ -743,6 +790,8 @@ tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* t, 
   const int inner = w2->k, inner_row = (inner + 7) / 8 * 8, dim = w2->n;
   const int64_t slots = std::min<int64_t>(w1->experts, pairs);
   const bool few = pairs <= kFewTokens * slots;
+  // Hardly any expert twice: a pair is a piece of its own, without a plan.
+  const bool direct = few && (t->n_rows == 1 || pairs * 4 <= w1->experts);
   Arena arena(ws);
   PlanArgs plan;
   plan.order = arena.take<int32_t>(pairs);
@@ -775,9 +824,19 @@ tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* t, 
   a.n_rows = b.n_rows = t->n_rows;
   a.top = b.top = t->top;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  k_plan<<<1, kPlanThreads, 0, s>>>(t->ids, pairs, w1->experts, plan, diag);
-  cudaError_t e = cudaGetLastError();
-  const int64_t tiles = slots + pairs / plan.piece;
+  cudaError_t e = cudaSuccess;
+  const int32_t* where = plan.where;
+  if (direct) {
+    a.plan.order = b.plan.order = nullptr;
+    a.ids = b.ids = t->ids;
+    where = nullptr;
+    b.behind = true;
+  } else {
+    k_plan<<<1, kPlanThreads, 0, s>>>(t->ids, pairs, w1->experts, plan, diag);
+    e = cudaGetLastError();
+    a.behind = b.behind = few;
+  }
+  const int64_t tiles = direct ? pairs : slots + pairs / plan.piece;
   if (!few && !e) {
     k_gather<<<(unsigned)pairs, kRowThreads, 0, s>>>(static_cast<const uint4*>(t->x), t->x_row / 8, w1->k / 8,
                                                      t->top, plan, pairs, gathered);
@@ -796,8 +855,8 @@ tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* t, 
   if (!e) e = product(a, w1);
   if (!e) e = product(b, w2);
   if (!e)
-    e = t->dtype == TRE_BF16 ? launch_combine<__nv_bfloat16>(each, row, plan.where, t, w1->experts, dim, s)
-                             : launch_combine<__half>(each, row, plan.where, t, w1->experts, dim, s);
+    e = t->dtype == TRE_BF16 ? launch_combine<__nv_bfloat16>(each, row, where, t, w1->experts, dim, diag, s)
+                             : launch_combine<__half>(each, row, where, t, w1->experts, dim, diag, s);
   return e == cudaSuccess ? TRE_OK : TRE_ECUDA;
 }
 

@@ -127,7 +127,9 @@ struct ProductArgs {
   int64_t x_row;                       // elements
   uint8_t* y;
   int64_t y_row;
-  PlanArgs plan;                       // order null: rows as they are, one matrix
+  PlanArgs plan;                       // order null: rows as they are, one matrix, or
+  const int32_t* ids;                  // a pair each with an expert of these
+  bool behind;                         // launched behind what it reads
   int32_t n_rows, top;
   int32_t first_slot;                  // of the plan's pieces that a launch of k_w4_few takes
   bool gather;                         // x's rows are tokens', by place

@@ -12,7 +12,7 @@ import struct
 
 import paper_2609_29160_gb300 as tre
 from . import replica
-from .replica import BF16, F16, F32, _codes, _diag
+from .replica import F32, _codes, _diag
 
 # The structs of include/tre.h by their fields (see replica).
 BLOCK = struct.Struct("@7iPqPqPPqqffPPqPq0q")      # tre_block_rows
@@ -39,13 +39,24 @@ def declare(lib):
         getattr(lib, f).restype = C.c_int
 
 
+_device = _stream = None      # torch's quickest ways to the current device, and to its stream
+
+
 def _ready():
-    """The library, with the tables of types filled."""
-    global _torch
+    """The library, with what calls look up filled in."""
+    global _torch, _device, _stream
     if _torch is None:
         replica._types()
         _torch = tre._torch()
+        _device = getattr(_torch._C, "_cuda_getDevice", _torch.cuda.current_device)
+        _stream = getattr(_torch._C, "_cuda_getCurrentRawStream",
+                          lambda dev: _torch.cuda.current_stream(dev).cuda_stream)
     return tre._lib or tre.load()
+
+
+def _like(t):
+    """A dense tensor of t's shape (torch's quickest way to one)."""
+    return _torch.empty_like(t, memory_format=_torch.contiguous_format)
 
 
 def _here(t, what):
@@ -53,7 +64,7 @@ def _here(t, what):
     dev = t.get_device()
     if dev < 0:
         raise ValueError(f"{what}: must be a CUDA tensor")
-    if dev != _torch.cuda.current_device():
+    if dev != _device():
         raise ValueError(f"{what}: must be on the current device")
     return dev
 
@@ -62,24 +73,36 @@ def _rows(t, what, dtype, dev, shape=None):
     """Row stride of a [rows][elements] tensor with a dense last axis."""
     if t.dtype is not dtype:
         raise ValueError(f"{what}: expected type {dtype}, got {t.dtype}")
-    if t.dim() != 2 or (shape is not None and t.shape != shape):
+    size, st = t.shape, t.stride()
+    if len(size) != 2 or (shape is not None and size != shape):
         want = "[rows][elements]" if shape is None else list(shape)
-        raise ValueError(f"{what}: expected {want}, got {tuple(t.shape)}")
-    row, one = t.stride()
-    if one != 1 and t.shape[1] > 1:
+        raise ValueError(f"{what}: expected {want}, got {tuple(size)}")
+    if st[1] != 1 and size[1] > 1:
         raise ValueError(f"{what}: the last axis must be dense")
     if t.get_device() != dev:
         raise ValueError(f"{what}: must be on the device of the other tensors")
-    return row
+    return st[0]
 
 
 def _weight(t, what, dim, dev):
     """Type of `dim` dense weights."""
-    if t.dim() != 1 or t.shape[0] != dim or (dim > 1 and t.stride(0) != 1):
+    if t.shape != (dim,) or (t.stride(0) != 1 and dim > 1):
         raise ValueError(f"{what}: expected {dim} dense elements")
     if t.get_device() != dev:
         raise ValueError(f"{what}: must be on the device of the other tensors")
     return t.dtype
+
+
+def _model_type(kinds):
+    """The one type of 16 bits among them (float32 where there is none)."""
+    kind = _torch.float32
+    for k in kinds:
+        if k is not _torch.float32 and k is not kind:
+            if kind is not _torch.float32:
+                raise ValueError(f"types: expected float32 and one of 16 bits, got {kind} and {k}")
+            replica._code(k, replica._FLOATS, "types")
+            kind = k
+    return kind
 
 
 def tre_block_norm(residual, y=None, post_weight=None, gate=None, scale=1.0, weight=None, eps=1e-6,
@@ -96,84 +119,76 @@ def tre_block_norm(residual, y=None, post_weight=None, gate=None, scale=1.0, wei
                            residual_out, out, dtype)
     lib = _ready()
     dev = _here(residual, "residual")
-    f32 = _torch.float32
-    r_kind = residual.dtype
+    kind = r_kind = residual.dtype
     r_row = _rows(residual, "residual", r_kind, dev)
     shape = residual.shape
     rows, dim = shape
     if not 1 <= dim <= 16384:
         raise ValueError(f"residual: expected rows of 1 to 16384 elements, got {dim}")
-    kinds = [r_kind]
     yp = y_row = gp = g_row = g_col = pp = wp = ro_row = rp = o_row = op = 0
-    y_kind = w_kind = f32
+    y_kind = w_kind = o_kind = r_kind          # (of what is not there: any of them)
+    g_kind = None
     if y is not None:
         y_kind = y.dtype
-        kinds.append(y_kind)
         y_row = _rows(y, "y", y_kind, dev, shape)
         yp = y.data_ptr()
+        if residual_out is None:
+            residual_out = _like(residual)
+            ro_row = dim
+        if gate is not None:
+            g_kind = gate.dtype
+            if gate.dim() == 1:
+                gate = gate[None]
+            if gate.dim() != 2 or gate.shape[0] not in (1, rows) or gate.shape[1] not in (1, dim):
+                raise ValueError(
+                    f"gate: expected [{dim}], [{rows}][1] or [{rows}][{dim}], got {tuple(gate.shape)}")
+            g_row = _rows(gate, "gate", g_kind, dev)
+            if gate.shape[0] == 1:
+                g_row = 0
+            g_col = 1 if gate.shape[1] == dim and dim > 1 else 0
+            gp = gate.data_ptr()
+        if post_weight is not None:
+            w_kind = _weight(post_weight, "post_weight", dim, dev)
+            pp = post_weight.data_ptr()
     elif post_weight is not None or gate is not None:
         raise ValueError("post_weight, gate: only with a block's output y")
-    if post_weight is not None:
-        w_kind = _weight(post_weight, "post_weight", dim, dev)
-        kinds.append(w_kind)
-        pp = post_weight.data_ptr()
-    if gate is not None:
-        if gate.dim() == 1:
-            gate = gate[None]
-        if gate.dim() != 2 or gate.shape[0] not in (1, rows) or gate.shape[1] not in (1, dim):
-            raise ValueError(f"gate: expected [{dim}], [{rows}][1] or [{rows}][{dim}], got {tuple(gate.shape)}")
-        g_row = _rows(gate, "gate", gate.dtype, dev)
-        if gate.shape[0] == 1:
-            g_row = 0
-        g_col = 1 if gate.shape[1] == dim and dim > 1 else 0
-        kinds.append(gate.dtype)
-        gp = gate.data_ptr()
-    o_kind = f32
+    elif weight is None and residual_out is None:
+        raise ValueError("y, weight: expected at least one of them")
     if weight is not None:
-        kind = _weight(weight, "weight", dim, dev)
-        if post_weight is not None and w_kind is not kind:
+        o_kind = _weight(weight, "weight", dim, dev)
+        if post_weight is not None and w_kind is not o_kind:
             raise ValueError("post_weight, weight: expected one type")
-        w_kind = kind
+        w_kind = o_kind
         wp = weight.data_ptr()
         if out is not None:
             o_kind = out.dtype
-        elif dtype is not None:
-            o_kind = replica._torch_type(replica._code(dtype, replica._FLOATS, "dtype"))
+            o_row = _rows(out, "out", o_kind, dev, shape)
         else:
-            o_kind = r_kind if y is None else y_kind
-        kinds += [w_kind, o_kind]
+            o_kind = y_kind if dtype is None else replica._torch_type(
+                replica._code(dtype, replica._FLOATS, "dtype"))
+            out = _like(residual) if o_kind is r_kind else _torch.empty(shape, dtype=o_kind, device=residual.device)
+            o_row = dim
+        op = out.data_ptr()
     elif out is not None:
         raise ValueError("out: expected a weight")
-    kind = f32
-    for k in kinds:
-        if k is not f32:
-            if replica._code(k, replica._FLOATS, "y") and kind is not f32 and k is not kind:
-                raise ValueError(f"types: expected float32 and one of 16 bits, got {kind} and {k}")
-            kind = k
-    if gate is not None and gate.dtype is not kind:
-        raise ValueError(f"gate: expected {kind}, got {gate.dtype}")
     if residual_out is not None:
-        ro_row = _rows(residual_out, "residual_out", r_kind, dev, shape)
-    elif y is not None:
-        residual_out = _torch.empty(shape, dtype=r_kind, device=residual.device)
-        ro_row = dim
-    elif weight is None:
-        raise ValueError("y, weight: expected at least one of them")
-    if residual_out is not None:
+        if ro_row == 0:
+            ro_row = _rows(residual_out, "residual_out", r_kind, dev, shape)
         rp = residual_out.data_ptr()
-    if weight is not None:
-        if out is None:
-            out = _torch.empty(shape, dtype=o_kind, device=residual.device)
-            o_row = dim
-        else:
-            o_row = _rows(out, "out", o_kind, dev, shape)
-        op = out.data_ptr()
+    if not (y_kind is kind and w_kind is kind and o_kind is kind and g_kind in (None, kind)):
+        kind = _model_type((r_kind, y_kind, w_kind, o_kind) if g_kind is None else
+                           (r_kind, y_kind, w_kind, o_kind, g_kind))
+        if g_kind not in (None, kind):
+            raise ValueError(f"gate: expected {kind}, got {g_kind}")
+    codes = _codes
+    if codes.get(kind) not in replica._FLOATS:
+        raise ValueError(f"residual: type {kind} is not one of those it takes")
     if rows:
         err = lib.tre_block_norm(
-            BLOCK.pack(_codes[kind], _codes[y_kind], _codes[r_kind], _codes[w_kind], _codes[o_kind], rows, dim,
+            BLOCK.pack(codes[kind], codes[y_kind], codes[r_kind], codes[w_kind], codes[o_kind], rows, dim,
                        residual.data_ptr(), r_row, yp, y_row, pp, gp, g_row, g_col, scale, eps, wp, rp,
                        ro_row, op, o_row),
-            tre._stream(None))
+            _stream(dev))
         if err:
             tre._check("tre_block_norm", err)
     return residual if residual_out is None else residual_out, out
@@ -220,7 +235,7 @@ def tre_route(logits, top, scores="softmax", bias=None, groups=1, top_groups=1, 
         err = lib.tre_route(
             ROUTER.pack(code, rows, experts, top, logits.data_ptr(), row, SCORES[scores], bp, groups, top_groups,
                         group_best, 1 if renorm else 0, scale, ids.data_ptr(), weights.data_ptr()),
-            tre._stream(None))
+            _stream(dev))
         if err:
             tre._check("tre_route", err)
     return ids, weights
@@ -267,7 +282,7 @@ class Weights4:
         size = C.c_size_t(0)
         tre._check("tre_w4_pack", lib.tre_w4_pack(source, None, size, None))
         self.packed = _torch.empty(size.value, dtype=_torch.uint8, device=codes.device)
-        tre._check("tre_w4_pack", lib.tre_w4_pack(source, self.packed.data_ptr(), size, tre._stream(None)))
+        tre._check("tre_w4_pack", lib.tre_w4_pack(source, self.packed.data_ptr(), size, _stream(dev)))
         self.handle = W4.pack(code, experts, n, k, self.group, self.gated, zeros is not None,
                               self.packed.data_ptr())
         self.tensors = (self.packed,)
@@ -304,7 +319,7 @@ def tre_linear4(x, w, out=None, diag=None, stream=None):
     else:
         o_row = _rows(out, "out", kind, dev, shape)
     at = LINEAR.pack(F32 if f32 else w.code, rows, x.data_ptr(), row, out.data_ptr(), o_row)
-    size, s, dg = C.c_size_t(0), tre._stream(None), _diag(diag)
+    size, s, dg = C.c_size_t(0), _stream(dev), _diag(diag)
     ws = out                       # (a call that needs none still wants an address)
     if f32:
         err = lib.tre_linear4(w.handle, at, None, size, dg, s)
@@ -345,7 +360,7 @@ def tre_experts(x, ids, weights, w1, w2, out=None, diag=None, stream=None):
         o_row = _rows(out, "out", w1.dtype, dev, (rows, w2.n))
     tokens = TOKENS.pack(w1.code, rows, shape[1], x.data_ptr(), row, ids.data_ptr(), weights.data_ptr(),
                          out.data_ptr(), o_row)
-    size, s, dg = C.c_size_t(0), tre._stream(None), _diag(diag)
+    size, s, dg = C.c_size_t(0), _stream(dev), _diag(diag)
     err = lib.tre_experts(w1.handle, w2.handle, tokens, None, size, dg, s)
     if err:
         tre._check("tre_experts", err)
