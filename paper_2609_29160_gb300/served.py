@@ -3,7 +3,8 @@
 A small decoder with random weights serves requests on this GPU by continuous
 batching: every step takes one token of each running request and a chunk of one
 prompt, through tre_kv_append and tre_chunk_attention over a paged cache, layer by
-layer. The clock is the measured time of the steps, so that what a prompt token and a
+layer; with experts also through tre_block_norm, tre_linear4, tre_route and tre_experts, its
+matrices in 4 bits. The clock is the measured time of the steps, so that what a prompt token and a
 decode token cost here, against each other (Eq. 1's w_p) and in milliseconds, is what
 this machine takes. The outcome is the library's own inputs: request records for
 tss_window_reduce and PipelinePlan, and latent service times for tre_replay.
@@ -16,15 +17,28 @@ import paper_2609_29160_gb300 as tre
 from paper_2609_29160_gb300 import replica
 
 
+def in_four_bits(w, group=32, gated=False):
+    """Weights4 of w [n][k] or [experts][n][k]: the nearest of sixteen steps, zero among them,
+    to each group's element farthest from zero."""
+    torch = tre._torch()
+    g = w.float().unflatten(-1, (-1, group))
+    scales = (g.abs().amax(-1) / 7).to(w.dtype)
+    step = torch.where(scales > 0, scales, torch.ones_like(scales)).float()[..., None]
+    codes = (torch.round(g / step).clamp(-8, 7) + 8).to(torch.uint8).flatten(-2)
+    return tre.Weights4(codes[..., 0::2] | codes[..., 1::2] << 4, scales, gated=gated)
+
+
 class Replica:
     """A decoder of `layers` layers with its paged caches, and the requests it runs.
 
     cache: type of the caches ("bf16", "e4m3", "i8"). chunk: most prompt tokens a step.
     time_scale: milliseconds of the clock for each millisecond measured (a model with so
-    many more layers)."""
+    many more layers). experts: with some, layers have norms around their blocks, matrices in
+    4 bits and a feed-forward block of so many experts, `top` of them for a token."""
 
     def __init__(self, layers=2, q_heads=8, kv_heads=2, dim=64, vocab=256, pages=512, page=16,
-                 chunk=128, cache="bf16", max_positions=4096, time_scale=1.0, seed=0):
+                 chunk=128, cache="bf16", max_positions=4096, time_scale=1.0, seed=0,
+                 experts=0, top=2):
         torch = self.torch = tre._torch()
         g = torch.Generator(device="cuda").manual_seed(seed)
         width = q_heads * dim
@@ -39,6 +53,15 @@ class Replica:
             "out": weight(width, width, scale=width ** -0.5),
             "q_weight": (1 + weight(dim, scale=0.1)), "k_weight": (1 + weight(dim, scale=0.1)),
             "cache": tre.KvCache.empty(pages, page, kv_heads, dim, cache)} for _ in range(layers)]
+        self.experts, self.top = experts, top
+        if experts:
+            for w in self.layers:
+                w["qkv"], w["out"] = in_four_bits(w["qkv"].T.contiguous()), in_four_bits(w["out"].T.contiguous())
+                w["norm"], w["ff_norm"] = 1 + weight(width, scale=0.1), 1 + weight(width, scale=0.1)
+                w["router"] = weight(width, experts, scale=width ** -0.5)
+                w["up"] = in_four_bits(weight(experts, 2 * width, width, scale=width ** -0.5), gated=True)
+                w["down"] = in_four_bits(weight(experts, width, width, scale=width ** -0.5))
+            self.norm = 1 + weight(width, scale=0.1)
         f = 10000.0 ** (-torch.arange(0, dim, 2, dtype=torch.float64, device="cuda") / dim)
         angle = torch.arange(max_positions, dtype=torch.float64, device="cuda")[:, None] * f
         self.cos_sin = torch.cat([angle.cos(), angle.sin()], 1).float()
@@ -48,18 +71,29 @@ class Replica:
         self.steps = []                       # (prompt tokens, decode tokens, ms) of each
         self.diag = replica.host_diag()
 
+    def attention(self, w, qkv, batch):
+        """A layer's attention of the batch's new tokens."""
+        hq, hk, dim = self.heads
+        q, k, v = qkv.view(-1, hq + 2 * hk, dim).split([hq, hk, hk], 1)
+        q = tre.tre_kv_append(w["cache"], batch, k, v, q=q, q_weight=w["q_weight"],
+                              k_weight=w["k_weight"], cos_sin=self.cos_sin, diag=self.diag)
+        return tre.tre_chunk_attention(q, w["cache"], batch, diag=self.diag).flatten(1)
+
     def forward(self, tokens, batch):
         """Last-layer rows of the batch's new tokens."""
-        hq, hk, dim = self.heads
         x = self.embed[tokens]
+        if not self.experts:
+            for w in self.layers:
+                x = x + self.attention(w, x @ w["qkv"], batch) @ w["out"]
+            return x
+        y = None
         for w in self.layers:
-            qkv = (x @ w["qkv"]).view(-1, hq + 2 * hk, dim)
-            q, k, v = qkv.split([hq, hk, hk], 1)
-            q = tre.tre_kv_append(w["cache"], batch, k, v, q=q, q_weight=w["q_weight"],
-                                  k_weight=w["k_weight"], cos_sin=self.cos_sin, diag=self.diag)
-            y = tre.tre_chunk_attention(q, w["cache"], batch, diag=self.diag)
-            x = x + y.flatten(1) @ w["out"]
-        return x
+            x, n = tre.tre_block_norm(x, y, weight=w["norm"])
+            y = self.attention(w, tre.tre_linear4(n, w["qkv"], diag=self.diag), batch)
+            x, n = tre.tre_block_norm(x, tre.tre_linear4(y, w["out"], diag=self.diag), weight=w["ff_norm"])
+            ids, weights = tre.tre_route((n @ w["router"]).float(), self.top)
+            y = tre.tre_experts(n, ids, weights, w["up"], w["down"], diag=self.diag)
+        return tre.tre_block_norm(x, y, weight=self.norm)[1]
 
     def _batch(self, work):
         """KvBatch of [(request, tokens in the cache, new tokens)]."""
