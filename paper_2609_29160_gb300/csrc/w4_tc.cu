@@ -432,33 +432,41 @@ k_w4_tc(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap ro
       // ---- products ------------------------------------------------------------------
       // One thread, which does as little as it can: with waits of a whole warp and an arrival
       // for each ring a stage took it 700 cycles, more than the stage's products.
-      uint32_t n = 0, groups = 0;
-      bool alive = true;
+      const uint32_t x0 = operand(smem_of(sm), 16), y0 = operand(smem_of(sm + R::AT_B), 16);
+      uint32_t sa = 0, sb = 0, full_phase = 0, buf = 0, sum_phase = 1;
+      bool alive = true, fresh = true;                   // fresh: a group begins
       for (int i = pair; alive && unit_at(a, i, u); i += pairs) {
         // 256 rows of the matrix over the two blocks
         const uint32_t id = (idesc_of<T>(u.columns, false) & 0x00ffffffu) | (256u >> 4) << 24;
 #pragma unroll 1
-        for (int c = 0; c < w.chunks; ++c, ++n) {
-          const uint32_t sa = n % R::A, sb = n % R::B;
-          const uint32_t x = operand(smem_of(sm + sa * R::BYTES_A), 16);
-          const uint32_t y = operand(smem_of(sm + R::AT_B + sb * R::BYTES_B), 16);
-          if (!(alive = bar_wait_one(full + sb, (n / R::B) & 1, dead))) break;
+        for (int c = 0; c < w.chunks; ++c) {
+          if (!(alive = bar_wait_one(full + sb, full_phase, dead))) break;
+          const uint32_t x = x0 + sa * (R::BYTES_A >> 4), y = y0 + sb * (R::BYTES_B >> 4);
 #pragma unroll
           for (int h = 0; h < PER; ++h) {
-            const uint32_t buf = groups % R::SUMS;
-            const bool fresh = STAGES_OF == 1 || (c & 1) == 0;
-            if (fresh && !(alive = bar_wait_one(sum_empty + buf, ((groups / R::SUMS) & 1) ^ 1, dead))) break;
+            if (fresh && !(alive = bar_wait_one(sum_empty + buf, sum_phase, dead))) break;
             tmem_after();
 #pragma unroll
             for (int k = h * 4 / PER; k < (h + 1) * 4 / PER; ++k)
               mma_pair(tmem + buf * WIDTH, x + k * 2, y + k * 2, id, !(fresh && k == h * 4 / PER));
-            if (STAGES_OF == 1 || (c & 1) == 1) {        // the group is whole
+            if (STAGES_OF == 1 || !fresh) {              // the group is whole
               commit_pair(sum_full + buf);
-              ++groups;
+              fresh = true;
+              if (++buf == R::SUMS) {
+                buf = 0;
+                sum_phase ^= 1;
+              }
+            } else {
+              fresh = false;
             }
           }
           if (!alive) break;
           commit_pair(done + sb);
+          if (++sa == R::A) sa = 0;
+          if (++sb == R::B) {
+            sb = 0;
+            full_phase ^= 1;
+          }
         }
       }
     }
