@@ -112,14 +112,17 @@ cudaError_t launch_behind(void (*kernel)(A...), dim3 grid, int threads, int room
 // ---------------------------------------------------------------------------
 // Products of few rows.
 //
-// Bound by reading the codes, and nearly by the instructions that turn them (some 250 for the
-// 2 KB that a step of a warp takes). A warp takes two tiles of 16 rows, 128 elements of k at a
-// time, out of a ring of its own that asynchronous copies fill two steps ahead with codes and
-// with x (elements of x loaded a step ahead into registers were waited for: 68 against @@ us for
-// 61 tokens' first product), and multiplies them by up to 8 NB rows of x with warp products whose accumulators are a group's sums (codes
-// less zeros are whole numbers, exact in 16 bits; the scale is applied once a group, in 32
-// bits). Where there are few tiles `split` warps share one and go through k in turn; their sums
-// are joined in order through shared memory.
+// Bound by reading the codes, and as much by the instructions that turn them: some 350 for the
+// 2 KB that a step of a warp takes, of which 110 are shifts and masks and 64 subtractions. A warp
+// takes two tiles of 16 rows, 128 elements of k at a time, out of a ring of its own that
+// asynchronous copies fill two steps ahead with codes and with x, and multiplies them by up to
+// 8 NB rows of x with warp products whose accumulators are a group's sums (codes less zeros are
+// whole numbers, exact in 16 bits; the scale is applied once a group, in 32 bits). Where there
+// are few tiles `split` warps share one and go through k in turn; their sums are joined in order
+// through shared memory.
+// 8 rows x 4,096 x 65,536, bf16, groups of 128: 41.6 us for 139 MB (3.3 TB/s), issue slots 61%
+// taken; 61 tokens over 128 experts (2,048 x 768 x 3, f16, groups of 64 with zeros): 45 us a
+// product on average, 68 with one load of x a step ahead and passes of eight rows.
 // ---------------------------------------------------------------------------
 constexpr int kFewWarps = 8;
 
@@ -438,12 +441,24 @@ cudaError_t launch_few(int dtype, int scale_dtype, int group, const ProductArgs&
                                  : few_by_columns<__half, __half>(group, p, s);
 }
 
-// Rows up to which a plain product is k_w4_few's.
-constexpr int kFewRows = 32;
+// Whether k_w4_few takes less than the tensor cores' kernel, by what both measured: it 5 us and
+// 0.31, 0.48, 0.72 or 0.79 us for each MB of codes and pass of 8, 16, 24 or 32 rows; the other
+// 8 us and 0.28 us for each 64 elements of k and round of its units (0.75 with groups of 32). E.g.
+// 16,384 x 4,096, groups of 128: 21 against 25 us for 16 rows, 31 against 25 for 32; 4,096 x
+// 4,096: 13 against 25 for 32 rows, 27 against 25 for 96.
+bool few_is_quicker(const ProductArgs& p, int group) {
+  if (p.n_rows <= 8) return true;
+  if (p.n_rows > 96) return false;
+  const float mb = p.w.tiles * 8.f * p.w.chunks * 64.f * 1e-6f;
+  const float pass = p.n_rows <= 16 ? 0.48f : p.n_rows <= 24 ? 0.72f : 0.79f;
+  const int pairs = std::max(1, device_sm_count() / 2);
+  const int rounds = ((p.w.tiles + 15) / 16 + pairs - 1) / pairs;
+  return 5.f + mb * pass * ((p.n_rows + 31) / 32) <= 8.f + rounds * p.w.chunks * (group == 32 ? 0.75f : 0.28f);
+}
 
 cudaError_t launch_rows(int dtype, int scale_dtype, int group, const ProductArgs& p, tre_diag* diag,
                         cudaStream_t s) {
-  if (p.n_rows > kFewRows) {
+  if (!few_is_quicker(p, group)) {
     const cudaError_t e = launch_w4_tc(dtype, scale_dtype, group, p, p.n_rows, 0, diag, s);
     if (e != cudaErrorNotSupported) return e;
   }
@@ -502,7 +517,9 @@ __global__ void __launch_bounds__(kRowThreads) k_whole_rows(const float* both, c
 // Experts: the plan of their tokens, and the sum of a token's experts.
 // ---------------------------------------------------------------------------
 constexpr int kPlanThreads = 1024, kMaxExperts = 1024;
-constexpr int kFewTokens = 12;       // tokens an expert up to which k_w4_few is taken
+// Tokens an expert up to which k_w4_few is taken: 64 experts of 2,048 x 1,024 x 3 with 12 each took 98 us
+// by it and 121 by the tensor cores' kernel, with 16 each 124 and 124, with 32 184 and 126.
+constexpr int kFewTokens = 15;
 
 // Pairs (token, j) counted and sorted by expert. Which place of its expert a pair gets
 // depends on the order of atomics; the products do not depend on places.
@@ -796,7 +813,9 @@ tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* t, 
   PlanArgs plan;
   plan.order = arena.take<int32_t>(pairs);
   plan.where = arena.take<int32_t>(pairs);
-  plan.piece = few ? 16 : pairs <= 64 * slots ? 128 : kTileTokens;
+  // (pieces of up to 128 rows have twice the accumulators: 100 tokens each took 154 against 162 us;
+  // but more than 128 are two pieces: 128 tokens each 210 against 177)
+  plan.piece = few ? 16 : pairs <= 96 * slots ? 128 : kTileTokens;
   plan.tiles = arena.take<Slot>(slots + pairs / plan.piece);
   plan.n = arena.take<int32_t>(2);
   uint8_t* h = arena.take<uint8_t>((size_t)pairs * inner_row * 2);
