@@ -732,11 +732,12 @@ typedef struct {
  * NULL: the size needed is written to *bytes, nothing is done. */
 tre_status tre_w4_pack(const tre_w4_source* from, void* packed, size_t* bytes, tre_stream stream);
 
-/* Rows of tre_linear4: x [n_rows][k] and y [n_rows][n, or n/2 of a gated matrix] of
- * dtype: the matrix's (x's address and stride multiples of 16 bytes), or TRE_F32.
- * Strides in elements. */
+/* Rows of tre_linear4: x [n_rows][k] of dtype, the matrix's (x's address and stride
+ * multiples of 16 bytes) or TRE_F32; y [n_rows][n, or n/2 of a gated matrix] of
+ * y_dtype, which is dtype, or TRE_F32 where the matrix is not gated. Strides in
+ * elements. */
 typedef struct {
-  tre_dtype dtype;
+  tre_dtype dtype, y_dtype;
   int32_t n_rows;
   const void* x;
   int64_t x_row;

@@ -443,7 +443,8 @@ cudaError_t launch_few(int dtype, int scale_dtype, int group, const ProductArgs&
 
 // Whether k_w4_few takes less than the tensor cores' kernel, by what both measured: it 5 us and
 // 0.31, 0.48, 0.72 or 0.79 us for each MB of codes and pass of 8, 16, 24 or 32 rows; the other
-// 8 us and 0.28 us for each 64 elements of k and round of its units (0.75 with groups of 32). E.g.
+// 8 us and 0.28 us for each 64 elements of k and round of its units (0.38 with groups of 64, 0.75
+// with 32). E.g.
 // 16,384 x 4,096, groups of 128: 21 against 25 us for 16 rows, 31 against 25 for 32; 4,096 x
 // 4,096: 13 against 25 for 32 rows, 27 against 25 for 96.
 bool few_is_quicker(const ProductArgs& p, int group) {
@@ -453,7 +454,7 @@ bool few_is_quicker(const ProductArgs& p, int group) {
   const float pass = p.n_rows <= 16 ? 0.48f : p.n_rows <= 24 ? 0.72f : 0.79f;
   const int pairs = std::max(1, device_sm_count() / 2);
   const int rounds = ((p.w.tiles + 15) / 16 + pairs - 1) / pairs;
-  return 5.f + mb * pass * ((p.n_rows + 31) / 32) <= 8.f + rounds * p.w.chunks * (group == 32 ? 0.75f : 0.28f);
+  return 5.f + mb * pass * ((p.n_rows + 31) / 32) <= 8.f + rounds * p.w.chunks * (group == 32 ? 0.75f : group == 64 ? 0.38f : 0.28f);
 }
 
 cudaError_t launch_rows(int dtype, int scale_dtype, int group, const ProductArgs& p, tre_diag* diag,
@@ -517,9 +518,10 @@ __global__ void __launch_bounds__(kRowThreads) k_whole_rows(const float* both, c
 // Experts: the plan of their tokens, and the sum of a token's experts.
 // ---------------------------------------------------------------------------
 constexpr int kPlanThreads = 1024, kMaxExperts = 1024;
-// Tokens an expert up to which k_w4_few is taken: 64 experts of 2,048 x 1,024 x 3 with 12 each took 98 us
-// by it and 121 by the tensor cores' kernel, with 16 each 124 and 124, with 32 184 and 126.
-constexpr int kFewTokens = 15;
+// Tokens an expert up to which k_w4_few is taken. 64 experts of 2,048 x 1,024 x 3, groups of 128,
+// 12 tokens each: 98 us by it, 121 by the tensor cores' kernel, 16 each 124 and 124, 32 each 184 and
+// 126; groups of 64, 24 each: 170 and 176; groups of 32, 32 each: 208 and 290, 48 each 286 and 292.
+constexpr int few_tokens(int group) { return group == 32 ? 48 : group == 64 ? 24 : 15; }
 
 // Pairs (token, j) counted and sorted by expert. Which place of its expert a pair gets
 // depends on the order of atomics; the products do not depend on places.
@@ -741,8 +743,10 @@ tre_status tre_linear4(const tre_w4* w, const tre_linear* l, void* ws, size_t* w
   ProductArgs p{};
   if (!l || !ws_bytes || !w4_args(w, p.w) || w->experts != 1 || l->n_rows < 0) return TRE_EINVAL;
   const bool f32 = l->dtype == TRE_F32;
+  const bool y_f32 = l->y_dtype == TRE_F32;
   if (!f32 && l->dtype != w->dtype) return TRE_EINVAL;
-  if (l->x_row < 0 || l->y_row < 0 || reinterpret_cast<uintptr_t>(l->y) % (f32 ? 4 : 2) ||
+  if (l->y_dtype != l->dtype && (!y_f32 || p.w.gated)) return TRE_EINVAL;
+  if (l->x_row < 0 || l->y_row < 0 || reinterpret_cast<uintptr_t>(l->y) % (y_f32 ? 4 : 2) ||
       reinterpret_cast<uintptr_t>(l->x) % (f32 ? 4 : 16) || (!f32 && l->x_row % 8))
     return TRE_EINVAL;
   if (f32 && l->n_rows > 2147483647 / 2) return TRE_EINVAL;
@@ -767,6 +771,7 @@ tre_status tre_linear4(const tre_w4* w, const tre_linear* l, void* ws, size_t* w
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e;
   if (!f32) {
+    p.y_f32 = y_f32;
     e = launch_rows(w->dtype, w->dtype, w->group, p, diag, s);
   } else {
     k_split<<<l->n_rows, kRowThreads, 0, s>>>(static_cast<const float*>(l->x), l->x_row, w->k, l->n_rows,
@@ -806,7 +811,7 @@ tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* t, 
   const int64_t pairs = (int64_t)t->n_rows * t->top;
   const int inner = w2->k, inner_row = (inner + 7) / 8 * 8, dim = w2->n;
   const int64_t slots = std::min<int64_t>(w1->experts, pairs);
-  const bool few = pairs <= kFewTokens * slots;
+  const bool few = pairs <= few_tokens(std::max(w1->group, w2->group)) * slots;
   // Hardly any expert twice: a pair is a piece of its own, without a plan.
   const bool direct = few && (t->n_rows == 1 || pairs * 4 <= w1->experts);
   Arena arena(ws);

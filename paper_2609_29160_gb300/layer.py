@@ -19,7 +19,7 @@ BLOCK = struct.Struct("@7iPqPqPPqqffPPqPq0q")      # tre_block_rows
 ROUTER = struct.Struct("@4iPqiP4ifPP0q")           # tre_router
 SOURCE = struct.Struct("@6iPPP0q")                 # tre_w4_source
 W4 = struct.Struct("@7iP0q")                       # tre_w4
-LINEAR = struct.Struct("@2iPqPq0q")                  # tre_linear
+LINEAR = struct.Struct("@3iPqPq0q")                  # tre_linear
 TOKENS = struct.Struct("@3iPqPPPq0q")              # tre_tokens
 
 SCORES = {"softmax": 0, "sigmoid": 1}
@@ -298,12 +298,12 @@ def _operand(x, what, w, dev, dtype):
     return w.k if x.shape[0] < 2 else row                 # (no other row is looked at)
 
 
-def tre_linear4(x, w, out=None, diag=None, stream=None):
+def tre_linear4(x, w, out=None, dtype=None, diag=None, stream=None):
     """x [rows][k] times the transpose of w (Weights4 of one matrix): [rows][n]; of a gated w
     silu(its first half) * its second half, [rows][n/2]. x of w's type, or float32, which out
-    is then too."""
+    is then too; dtype "f32": out is in any case (not of a gated w)."""
     if stream is not None:
-        return replica._on(stream, tre_linear4, x, w, out, diag)
+        return replica._on(stream, tre_linear4, x, w, out, dtype, diag)
     lib = _ready()
     dev = _here(x, "x")
     f32 = x.dtype is _torch.float32
@@ -311,6 +311,15 @@ def tre_linear4(x, w, out=None, diag=None, stream=None):
     row = _operand(x, "x", w, dev, kind)
     if w.experts != 1:
         raise ValueError(f"w: expected one matrix, got {w.experts}")
+    code = y_code = F32 if f32 else w.code
+    if dtype is not None:
+        y_code = replica._code(dtype, replica._FLOATS, "dtype")
+    elif out is not None and out.dtype is _torch.float32:
+        y_code = F32
+    if y_code != code:
+        if y_code != F32 or w.gated:
+            raise ValueError(f"dtype: expected {kind}, or float32 of a matrix that is not gated")
+        kind = _torch.float32
     rows = x.shape[0]
     shape = (rows, w.out)
     if out is None:
@@ -318,7 +327,7 @@ def tre_linear4(x, w, out=None, diag=None, stream=None):
         o_row = w.out
     else:
         o_row = _rows(out, "out", kind, dev, shape)
-    at = LINEAR.pack(F32 if f32 else w.code, rows, x.data_ptr(), row, out.data_ptr(), o_row)
+    at = LINEAR.pack(code, y_code, rows, x.data_ptr(), row, out.data_ptr(), o_row)
     size, s, dg = C.c_size_t(0), _stream(dev), _diag(diag)
     ws = out                       # (a call that needs none still wants an address)
     if f32:

@@ -146,6 +146,8 @@ def bad_calls(tre):
         lambda: tre.Weights4(z(63, 64, dtype=u8), z(63, 2), gated=True), lambda: tre.Weights4(codes, sc.cpu()),
         lambda: tre.tre_linear4(x.half(), m), lambda: tre.tre_linear4(x[:, :64], m), lambda: tre.tre_linear4(x, up),
         lambda: tre.tre_linear4(x.cpu(), m), lambda: tre.tre_linear4(x, m, out=z(3, 63)), lambda: tre.tre_linear4(x, m, out=z(3, 64).half()),
+        lambda: tre.tre_linear4(x, m, dtype="f16"), lambda: tre.tre_linear4(x, tre.Weights4(codes, sc, gated=True), dtype="f32"),
+        lambda: tre.tre_linear4(x.float(), m, dtype="bf16"),
         lambda: tre.tre_experts(x, ids.long(), ws, up, down), lambda: tre.tre_experts(x, ids, ws.half(), up, down),
         lambda: tre.tre_experts(x, ids[:2], ws, up, down), lambda: tre.tre_experts(x, ids, ws, down, up),
         lambda: tre.tre_experts(x, ids, ws, up, up), lambda: tre.tre_experts(x, ids, ws, up, m),

@@ -168,3 +168,43 @@ def test_streams_and_graphs(tre, t, kind):
     torch.cuda.synchronize()
     assert all(torch.equal(o, want) for o in outs)
     tre.check_replica()
+
+
+@pytest.mark.parametrize("t,n,k,group", [(20, 20000, 512, 128), (40, 18000, 256, 64), (97, 300, 320, 64), (130, 520, 96, 32),
+                                         (200, 6000, 256, 128), (333, 20000, 128, 128), (500, 9000, 192, 64)])
+def test_units_of_every_width(tre, t, n, k, group):
+    """Few and many rows on the tensor cores, by themselves and as a gated matrix in 32 bits."""
+    check(tre, t, n, k, group, "bf16", group == 64)
+    check(tre, t, n, k, group, "f16", gated=True)
+    check(tre, t, n // 4 * 2, k, group, "f16", True, gated=True, kind="f32")
+
+
+def test_outputs_on_any_element(tre):
+    """Rows of y that 16 bytes do not divide, of both kernels' widest stores."""
+    codes, scales, z, m = R.matrix4(None, 264, 128, 64, torch.bfloat16, False, 6)
+    for gated in (False, True):
+        w = tre.Weights4(codes, scales, gated=gated)
+        for t in (5, 300):
+            x = rows(t, 128, torch.bfloat16)
+            want = tre.tre_linear4(x, w)
+            for shift, wide in ((1, 270), (2, 270), (8, 272), (4, 269)):
+                out = torch.full((t, wide), 7.0, dtype=torch.bfloat16, device="cuda")
+                got = tre.tre_linear4(x, w, out=out[:, shift:shift + want.shape[1]])
+                assert torch.equal(got, want)
+                assert (out[:, :shift] == 7).all() and (out[:, shift + want.shape[1]:] == 7).all()
+
+
+@pytest.mark.parametrize("t", [1, 20, 40, 300])
+@pytest.mark.parametrize("n", [31, 264])
+def test_rows_out_in_32_bits(tre, t, n):
+    """Rows of 16 bits into rows of 32, which are then rounded no more."""
+    codes, scales, z, m = R.matrix4(None, n, 192, 64, torch.bfloat16, True, 6)
+    w = tre.Weights4(codes, scales, z)
+    x = rows(t, 192, torch.bfloat16)
+    got = tre.tre_linear4(x, w, dtype="f32")
+    assert got.dtype == torch.float32
+    R.near(got, *R.product(x, m))
+    assert torch.equal(got.bfloat16(), tre.tre_linear4(x, w))
+    out = torch.full((t, n + 3), 7.0, device="cuda")
+    assert torch.equal(tre.tre_linear4(x, w, out=out[:, 2:n + 2]), got)
+    assert (out[:, :2] == 7).all() and (out[:, n + 2:] == 7).all()

@@ -34,8 +34,8 @@ def w4(dtype=R.BF16, experts=1, n=64, k=128, group=64, gated=0, zeros=0, packed=
     return L.W4.pack(dtype, experts, n, k, group, gated, zeros, packed)
 
 
-def linear(dtype=R.BF16, rows=3, x=A, x_row=128, y=A, y_row=64):
-    return L.LINEAR.pack(dtype, rows, x, x_row, y, y_row)
+def linear(dtype=R.BF16, rows=3, x=A, x_row=128, y=A, y_row=64, y_dtype=None):
+    return L.LINEAR.pack(dtype, dtype if y_dtype is None else y_dtype, rows, x, x_row, y, y_row)
 
 
 def tokens(dtype=R.BF16, rows=3, top=2, x=A, x_row=128, ids=A, weights=A, y=A, y_row=128):
@@ -46,7 +46,7 @@ def test_struct_sizes(tmp_path):
     """The sizes that the header's fields have for a C compiler."""
     names = ("tre_block_rows", "tre_router", "tre_w4_source", "tre_w4", "tre_linear", "tre_tokens")
     sizes = (L.BLOCK.size, L.ROUTER.size, L.SOURCE.size, L.W4.size, L.LINEAR.size, L.TOKENS.size)
-    assert sizes == (144, 88, 48, 40, 40, 64)
+    assert sizes == (144, 88, 48, 40, 48, 64)
     text = '#include "tre.h"\n' + "".join(f"_Static_assert(sizeof({n}) == {s}, \"{n}\");\n" for n, s in zip(names, sizes))
     src = tmp_path / "sizes.c"
     src.write_text(text)
@@ -114,9 +114,11 @@ def test_pack():
 
 @pytest.mark.parametrize("bad", [
     dict(dtype=R.F16), dict(dtype=1), dict(rows=-1), dict(x=0), dict(y=0), dict(x=A + 8), dict(y=A + 1),
-    dict(x_row=127), dict(x_row=-8), dict(y_row=-1), dict(dtype=R.F32, x=A + 2), dict(dtype=R.F32, y=A + 2)])
+    dict(x_row=127), dict(x_row=-8), dict(y_row=-1), dict(dtype=R.F32, x=A + 2), dict(dtype=R.F32, y=A + 2),
+    dict(y_dtype=R.F16), dict(y_dtype=1), dict(y_dtype=R.F32, y=A + 2), dict(dtype=R.F32, y_dtype=R.BF16)])
 def test_linear_is_checked(bad):
     n = C.c_size_t(1 << 40)
+    assert tre.load().tre_linear4(w4(gated=1), linear(y_dtype=R.F32), A, n, None, None) == 1
     assert tre.load().tre_linear4(w4(), linear(**bad), A, n, None, None) == 1
 
 
