@@ -276,10 +276,11 @@ def run_own(s):
         if op == "norm":
             r, n = tre.tre_block_norm(s["residual"], s["y"], **how)
             return {"residual": r, "out": n}
-        # (a residual stream in 32 bits has its block's rows in 32 bits too)
+        # (a residual stream in 32 bits has its block's rows in 32 bits too; what goes into it
+        # is rounded there alone)
         r, n = tre.tre_block_norm(s["residual"], s["y"], dtype=c["stream"], **how)
         h = tre.tre_linear4(n, s["w1_own"])
-        y = tre.tre_linear4(h, s["w2_own"])
+        y = tre.tre_linear4(h, s["w2_own"], dtype="f32")
         r, n = tre.tre_block_norm(r, y, dtype=c["dtype"], **how)
         return {"residual": r, "out": n}
     if op == "linear":
