@@ -711,8 +711,9 @@ tre_status tre_route(const tre_router* router, tre_stream stream);
  * one) codes [n][k/2], two a byte, the lower half first; scales [n][k/group] of
  * dtype (TRE_BF16, TRE_F16: the type of the rows that it will be multiplied with);
  * zeros [n][k/group] bytes of 0 to 15, NULL: 8. An element is (code - zero) * scale.
- * group is 32, 64 or 128 and divides k. gated (n even): rows 0 to n/2-1 are a
- * gate's, the others what it multiplies. All dense; codes on a 4-byte boundary. */
+ * group is 32, 64 or 128 and divides k; n and k up to 2^20, experts up to 1024.
+ * gated (n even): rows 0 to n/2-1 are a gate's, the others what it multiplies. All
+ * dense. */
 typedef struct {
   tre_dtype dtype;
   int32_t experts, n, k, group, gated;
@@ -735,7 +736,7 @@ tre_status tre_w4_pack(const tre_w4_source* from, void* packed, size_t* bytes, t
 /* Rows of tre_linear4: x [n_rows][k] of dtype, the matrix's (x's address and stride
  * multiples of 16 bytes) or TRE_F32; y [n_rows][n, or n/2 of a gated matrix] of
  * y_dtype, which is dtype, or TRE_F32 where the matrix is not gated. Strides in
- * elements. */
+ * elements; at most 2^30 rows (2^29 in 32 bits); y does not overlap x. */
 typedef struct {
   tre_dtype dtype, y_dtype;
   int32_t n_rows;
@@ -757,7 +758,8 @@ tre_status tre_linear4(const tre_w4* w, const tre_linear* rows, void* ws, size_t
 
 /* Tokens of tre_experts: x [n_rows][k] of dtype and y [n_rows][n of the second
  * matrices]; strides in elements, x's address and stride multiples of 16 bytes. ids,
- * weights: [n_rows][top] (dense). */
+ * weights: [n_rows][top] (dense), top from 1 to 32, at most 2^30 pairs. y overlaps
+ * none of them. */
 typedef struct {
   tre_dtype dtype;
   int32_t n_rows, top;

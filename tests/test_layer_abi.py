@@ -115,7 +115,7 @@ def test_pack():
 @pytest.mark.parametrize("bad", [
     dict(dtype=R.F16), dict(dtype=1), dict(rows=-1), dict(x=0), dict(y=0), dict(x=A + 8), dict(y=A + 1),
     dict(x_row=127), dict(x_row=-8), dict(y_row=-1), dict(dtype=R.F32, x=A + 2), dict(dtype=R.F32, y=A + 2),
-    dict(y_dtype=R.F16), dict(y_dtype=1), dict(y_dtype=R.F32, y=A + 2), dict(dtype=R.F32, y_dtype=R.BF16)])
+    dict(rows=2 ** 30 + 1), dict(dtype=R.F32, rows=2 ** 29 + 1), dict(y_dtype=R.F16), dict(y_dtype=1), dict(y_dtype=R.F32, y=A + 2), dict(dtype=R.F32, y_dtype=R.BF16)])
 def test_linear_is_checked(bad):
     n = C.c_size_t(1 << 40)
     assert tre.load().tre_linear4(w4(gated=1), linear(y_dtype=R.F32), A, n, None, None) == 1
