@@ -91,7 +91,8 @@ __global__ void k_w4_scales(PackArgs a, int64_t words) {
 
 // ---------------------------------------------------------------------------
 // Launches that may begin while the one before still runs (programmatic serialisation): what
-// it has written is read after after_launch alone, which every block comes to.
+// it has written is read after after_launch alone, which every block comes to. Only launches that
+// are followed by one of these let it begin: what a caller launches next is ordered as ever.
 __device__ __forceinline__ void after_launch() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 template <class... A, class... B>
@@ -131,12 +132,12 @@ template <class T, bool FRESH>
 __device__ __forceinline__ void mma_few(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
 #define TRE_MMA(type)                                                                              \
   if constexpr (FRESH)                                                                             \
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32." type "." type                            \
+    asm("mma.sync.aligned.m16n8k16.row.col.f32." type "." type                                     \
                  ".f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"                  \
                  : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])                                  \
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));        \
   else                                                                                             \
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32." type "." type                            \
+    asm("mma.sync.aligned.m16n8k16.row.col.f32." type "." type                                     \
                  ".f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"                      \
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])                                  \
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1))
@@ -193,44 +194,67 @@ __device__ __forceinline__ void few_rows(const ProductArgs& p, const Slot& slot,
   const uint32_t to_scale = St::AT_SCALE + ((sr * PER + sq) * 2 + (lane & 1)) * 16;
   const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
   for (int from = 0; from < slot.count; from += 8 * NB) {
+    // What is fetched next: step `next`, its codes, scales and x, into the ring at `put`
     const uint4* next_codes = codes + (int64_t)part * 2 * kNextChunk;
-    int64_t next_scale = scale0 + part * PER * 8;
+    const uint32_t* next_scale = w.scales + scale0 + part * PER * 8;
+    const uint32_t* next_zero = w.zeros + scale0 + part * PER * 8;
     const T* x[NB];
-    uint32_t get = 0, put = (St::STEPS - 1) * St::STEP;  // offsets in the ring
-    // Step `step` into the ring at `at`, `ahead` steps of this warp's after what the pointers name
-    auto fetch_codes = [&](int step, int ahead, uint32_t at) {
-      if (step >= steps) return;
-      const uint4* from = next_codes + ahead * split * 2 * kNextChunk;
-      const uint32_t to = ring_at + at + lane * 16;
-      copy16(to, from);
-      copy16(to + 1024, from + 32);
-      if (2 * step + 1 < w.chunks) {
-        copy16(to + 512, from + kNextChunk);
-        copy16(to + 1536, from + kNextChunk + 32);
+    uint32_t get = 0, put = ring_at;                     // places in the ring
+    auto fetch_codes = [&](int step) {
+      const uint32_t to = put + lane * 16;
+      if ((step + 1) * 128 <= w.k) {                     // (nearly always: no more to ask)
+        copy16(to, next_codes);
+        copy16(to + 1024, next_codes + 32);
+        copy16(to + 512, next_codes + kNextChunk);
+        copy16(to + 1536, next_codes + kNextChunk + 32);
+        if (scale_lane) {
+          copy16(put + to_scale, next_scale);
+          if (w.zeros) copy16(put + to_scale + St::SCALES, next_zero);
+        }
+      } else if (step < steps) {
+        copy16(to, next_codes);
+        copy16(to + 1024, next_codes + 32);
+        if (2 * step + 1 < w.chunks) {
+          copy16(to + 512, next_codes + kNextChunk);
+          copy16(to + 1536, next_codes + kNextChunk + 32);
+        }
+        if (scale_lane && step * PER + sq < w.groups) {
+          copy16(put + to_scale, next_scale);
+          if (w.zeros) copy16(put + to_scale + St::SCALES, next_zero);
+        }
       }
-      if (scale_lane && step * PER + sq < w.groups) {
-        const int64_t scale = next_scale + ahead * split * PER * 8;
-        copy16(ring_at + at + to_scale, w.scales + scale);
-        if (w.zeros) copy16(ring_at + at + to_scale + St::SCALES, w.zeros + scale);
-      }
+      next_codes += split * 2 * kNextChunk;
+      next_scale += split * PER * 8;
+      next_zero += split * PER * 8;
     };
-    auto fetch_x = [&](int step, int ahead, uint32_t at) {
-      if (step < steps) {
-        const int left = w.k - step * 128;               // elements from this step on
-        const uint32_t to = ring_at + at + St::AT_X + lane * 16;
+    auto fetch_x = [&](int step) {
+      const uint32_t to = put + St::AT_X + lane * 16;
+      const int left = w.k - step * 128;                 // elements from this step on
+      if (left >= 128) {
+#pragma unroll
+        for (int half = 0; half < 4; ++half)
+#pragma unroll
+          for (int b = 0; b < NB; ++b) copy16(to + (half * NB + b) * 512, x[b] + half * 32);
+      } else if (step < steps) {
 #pragma unroll
         for (int half = 0; half < 4; ++half)
 #pragma unroll
           for (int b = 0; b < NB; ++b) {
-            if (half * 32 < left) copy16(to + (half * NB + b) * 512, x[b] + ahead * split * 128 + half * 32);
+            if (half * 32 < left) copy16(to + (half * NB + b) * 512, x[b] + half * 32);
             else zero16(to + (half * NB + b) * 512);     // past k
           }
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
+#pragma unroll
+      for (int b = 0; b < NB; ++b) x[b] += split * 128;
     };
+    auto go_on = [&]() { put = put + St::STEP == ring_at + St::RING ? ring_at : put + St::STEP; };
     // (codes do not depend on the launch before, x may)
 #pragma unroll
-    for (int k = 0; k < St::STEPS - 1; ++k) fetch_codes(part + k * split, k, k * St::STEP);
+    for (int k = 0; k < St::STEPS - 1; ++k) {
+      fetch_codes(part + k * split);
+      go_on();
+    }
     if (from == 0) after_launch();
     // rows of x of this lane's columns (of columns that are not there, the last one's: what
     // comes of them is not written)
@@ -240,8 +264,12 @@ __device__ __forceinline__ void few_rows(const ProductArgs& p, const Slot& slot,
       const int64_t row = !p.gather ? place : (p.plan.order ? p.plan.order[place] : place) / p.top;
       x[b] = reinterpret_cast<const T*>(p.x) + row * p.x_row + 8 * t + part * 128;
     }
+    put = ring_at;
 #pragma unroll
-    for (int k = 0; k < St::STEPS - 1; ++k) fetch_x(part + k * split, k, k * St::STEP);
+    for (int k = 0; k < St::STEPS - 1; ++k) {
+      fetch_x(part + k * split);
+      go_on();
+    }
     float acc[2][NB][4];
 #pragma unroll
     for (int r = 0; r < 2; ++r)
@@ -250,19 +278,16 @@ __device__ __forceinline__ void few_rows(const ProductArgs& p, const Slot& slot,
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[r][b][e] = 0.f;
     for (int kb = part; kb < steps; kb += split) {
-      constexpr int AHEAD = St::STEPS - 1;
-      fetch_codes(kb + AHEAD * split, AHEAD, put);
-      fetch_x(kb + AHEAD * split, AHEAD, put);
-      put = put + St::STEP == St::RING ? 0 : put + St::STEP;
-      next_codes += split * 2 * kNextChunk;
-      next_scale += split * PER * 8;
-#pragma unroll
-      for (int b = 0; b < NB; ++b) x[b] += split * 128;
+      const int next = kb + (St::STEPS - 1) * split;
+      fetch_codes(next);
+      fetch_x(next);
+      go_on();
       asm volatile("cp.async.wait_group %0;" ::"n"(St::STEPS - 1) : "memory");
       __syncwarp();
       const uint8_t* now = ring + get;
       get = get + St::STEP == St::RING ? 0 : get + St::STEP;
       const int left = w.k - kb * 128;
+      uint4 words[2];                                    // of a chunk, of both tiles
 #pragma unroll
       for (int q = 0; q < PER; ++q) {
         // (past the last group: whatever codes by elements of x that are zeros)
@@ -285,10 +310,15 @@ __device__ __forceinline__ void few_rows(const ProductArgs& p, const Slot& slot,
 #pragma unroll
           for (int b = 0; b < NB; ++b)
             v[b] = *reinterpret_cast<const uint4*>(now + St::AT_X + (half * NB + b) * 512 + lane * 16);
+          // (past the last chunk: old codes, by elements of x that are zeros)
+          if ((half & 1) == 0) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+              words[r] = *reinterpret_cast<const uint4*>(now + ((r * 2 + (half >> 1)) * 32 + lane) * 16);
+          }
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            const uint2 word =
-                *reinterpret_cast<const uint2*>(now + ((r * 2 + (half >> 1)) * 32 + lane) * 16 + (half & 1) * 8);
+            const uint2 word = half & 1 ? make_uint2(words[r].z, words[r].w) : make_uint2(words[r].x, words[r].y);
 #pragma unroll
             for (int sub = 0; sub < 2; ++sub) {
               uint32_t a[4];
@@ -366,7 +396,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, FewKernel<NB, GROUP>::BLOCKS)
 k_w4_few(const __grid_constant__ ProductArgs p, int split) {
   extern __shared__ __align__(16) uint8_t room[];
   constexpr int WARP = FewKernel<NB, GROUP>::WARP;
-  let_next();
+  if (p.leads) let_next();
   Slot slot{0, 0, p.n_rows, 0};
   const int piece = p.first_slot + (int)blockIdx.y;
   if (p.ids) {                                         // a pair of a token and its expert each
@@ -921,6 +951,7 @@ tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* t, 
     e = launch_plan(t->ids, pairs, w1->experts, plan, diag, s);
     a.behind = b.behind = few;
   }
+  a.leads = b.leads = few;
   const int64_t tiles = direct ? pairs : slots + pairs / plan.piece;
   if (!few && !e) {
     constexpr int rows = kRowThreads / 32;

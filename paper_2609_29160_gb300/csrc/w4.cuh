@@ -129,7 +129,7 @@ struct ProductArgs {
   int64_t y_row;
   PlanArgs plan;                       // order null: rows as they are, one matrix, or
   const int32_t* ids;                  // a pair each with an expert of these
-  bool behind;                         // launched behind what it reads
+  bool behind, leads;                  // launched behind what it reads; the next launch is behind it
   int32_t n_rows, top;
   int32_t first_slot;                  // of the plan's pieces that a launch of k_w4_few takes
   bool gather;                         // x's rows are tokens', by place
