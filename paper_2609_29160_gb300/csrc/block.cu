@@ -334,6 +334,19 @@ __device__ __forceinline__ float group_scores(const RouteArgs& a, const float* c
   const int lane = threadIdx.x & 31;
   const float none = -INFINITY;
   float mine = none, first = none, second = none;
+  if (a.per == 32) {                                 // a group a register
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      float sum = warp_max(c[j]);
+      if (a.group_best == 2) {
+        const int who = __ffs(__ballot_sync(0xffffffffu, c[j] == sum)) - 1;
+        const float next = warp_max(lane == who ? none : c[j]);
+        if (next > none) sum += next;
+      }
+      if (lane == j) mine = sum;
+    }
+    return lane < a.groups ? mine : none;
+  }
   if (a.per % 32 == 0) {                             // groups of whole registers
     const int regs = a.per / 32;
     int left = regs, g = 0;
@@ -386,23 +399,35 @@ __device__ __forceinline__ uint64_t group_scores(const RouteArgs& a, const uint6
   return order(value_of(first) + value_of(second));
 }
 
-// The groups that stay, by lanes' scores of them; under: the best that comes after a lane's.
-template <class K>
-__device__ __forceinline__ unsigned kept_groups(const RouteArgs& a, K mine, K none, int& better, K& under) {
+// The groups that stay, by lanes' scores of them, and how far the last of them is from the next.
+__device__ __forceinline__ unsigned kept_groups(const RouteArgs& a, float mine, float& last, float& next) {
+  unsigned kept = 0;
+  for (int k = 0; k < a.top_groups; ++k) {
+    last = warp_max(mine);
+    const int who = __ffs(__ballot_sync(0xffffffffu, mine == last)) - 1;
+    kept |= 1u << who;                               // (of what is left, none of them -inf: any)
+    if ((threadIdx.x & 31) == who) mine = -INFINITY;
+  }
+  next = warp_max(mine);
+  return kept;
+}
+__device__ __forceinline__ unsigned kept_groups(const RouteArgs& a, uint64_t mine) {
   const int lane = threadIdx.x & 31;
-  better = 0;
-  under = none;
+  int better = 0;
   for (int g = 0; g < a.groups; ++g) {
-    const K x = __shfl_sync(0xffffffffu, mine, g);
+    const uint64_t x = __shfl_sync(0xffffffffu, mine, g);
     if (x > mine || (x == mine && g < lane)) ++better;
-    else if (g != lane && x > under) under = x;
   }
   return __ballot_sync(0xffffffffu, lane < a.groups && better < a.top_groups);
 }
 template <int NV, class K>
 __device__ __forceinline__ void only_kept(const RouteArgs& a, unsigned kept, K none, K* c) {
   const int lane = threadIdx.x & 31;
-  if (a.per % 32 == 0) {
+  if (a.per == 32) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (!(kept >> j & 1)) c[j] = none;
+  } else if (a.per % 32 == 0) {
     const int regs = a.per / 32;
     int left = regs;
 #pragma unroll
@@ -467,9 +492,7 @@ __device__ __noinline__ int choose_double(const RouteArgs& a, int64_t row, float
     for (int j = 0; j < NV; ++j)
       if (j * 32 + lane < a.experts) room[j * 32 + lane] = c[j];
     __syncwarp();
-    int better;
-    uint64_t under;
-    only_kept<NV>(a, kept_groups(a, group_scores(a, room), none, better, under), none, c);
+    only_kept<NV>(a, kept_groups(a, group_scores(a, room)), none, c);
     __syncwarp();
   }
   int mine = -1;
@@ -500,13 +523,12 @@ __device__ __forceinline__ Choice choose(const RouteArgs& a, int64_t row, const 
   all_scores<float, NV>(a, l, most, total, c);
   const float off = a.raw ? 0.f : a.softmax ? kOffSoftmax : kOffSigmoid, rel = a.raw ? 0.f : kOffBias;
   if (a.groups > 1) {
-    const float score = group_scores<NV>(a, c, reinterpret_cast<float*>(room));
-    int better;
-    float under;
-    only_kept<NV>(a, kept_groups<float>(a, score, -INFINITY, better, under), (float)-INFINITY, c);
-    const bool unsure = lane < a.groups && better == a.top_groups - 1 && under > -INFINITY &&
-                        !(score - under > 2.f * off + rel * (fabsf(score) + 1.f));
-    if (off > 0.f && __any_sync(0xffffffffu, unsure))
+    float last = 0.f, next = 0.f;
+    const unsigned kept =
+        kept_groups(a, group_scores<NV>(a, c, reinterpret_cast<float*>(room)), last, next);
+    only_kept<NV>(a, kept, (float)-INFINITY, c);
+    const bool unsure = next > -INFINITY && !(last - next > 2.f * off + rel * (fabsf(last) + 1.f));
+    if (off > 0.f && unsure)
       return Choice{choose_double<NV>(a, row, most, room), lane};
   }
   // the top-th largest of the lanes' maxima, and what 32 bits cannot tell from it
@@ -519,11 +541,11 @@ __device__ __forceinline__ Choice choose(const RouteArgs& a, int64_t row, const 
     if (own == least) own = -INFINITY;               // (all that are equal: the bound is then lower)
   }
   least -= off + rel * fabsf(least);
-  if (!(least > -INFINITY)) least = -INFINITY;       // (also what infinities make of it)
+  if (!(least > -3.402823466e38f)) least = -3.402823466e38f;     // (also what infinities make of it)
   int count = 0;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const bool in = c[j] >= least && c[j] > -INFINITY;
+    const bool in = c[j] >= least;                   // (not -inf)
     const unsigned all = __ballot_sync(0xffffffffu, in);
     const int at = count + __popc(all & ((1u << lane) - 1));
     if (in && at < 32) {

@@ -141,3 +141,9 @@ def test_strides_streams_graphs(tre, t):
 def test_no_rows(tre):
     c = Case(tre, 0, 2, 4, 256, 128, 64, "bf16")
     assert tre.tre_experts(c.x, c.ids, c.weights, c.w1, c.w2).shape == (0, 256)
+
+
+@pytest.mark.parametrize("t,top,experts", [(500, 6, 200), (2000, 1, 1024), (300, 8, 512), (2100, 1, 3)])
+def test_many_experts(tre, t, top, experts):
+    """Plans of more pairs than a block sorts alone, for few and for many tokens an expert."""
+    Case(tre, t, top, experts, 64, 32, 32, "bf16", liked=0.2).check(tre)
