@@ -13,7 +13,9 @@ namespace {
 //
 // One pass: a row's elements of y and of the residual stay in registers between the two
 // sums (mean of squares of y, where there is a post norm, and of r), so that each input is
-// read once and each output written once. Bound by HBM where there are rows enough.
+// read once and each output written once; 16 elements a thread and as many threads as a row then
+// has. Bound by HBM where there are rows enough: 20,011 rows of 5,120, bfloat16 beside a 32-bit
+// stream, both norms and a gate: 193 us for 1.18 GB, 6.1 TB/s.
 // ---------------------------------------------------------------------------
 struct BlockArgs {
   const uint8_t *residual, *y, *post_weight, *gate, *weight;
@@ -189,7 +191,9 @@ bool on(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % byte
 // Candidates: the top-th largest of the lanes' own maxima is not above the top-th largest of all,
 // so that what is not below it (some ten to fifteen of 256 for the best eight) has the chosen in
 // it. They go to a lane each, which counts how many come before. Taking the best out one after
-// the other took 100 instructions each, 1.45 us for 16,384 rows.
+// the other took 100 instructions each, 1.45 us for 16,384 rows. Bound by instructions, some 900
+// for a row of 256 sigmoid scores with a bias in groups: 16,384 rows 22 us, 12 without bias and
+// groups.
 // ---------------------------------------------------------------------------
 struct RouteArgs {
   const uint8_t* logits;

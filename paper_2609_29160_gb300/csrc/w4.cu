@@ -121,7 +121,7 @@ cudaError_t launch_behind(void (*kernel)(A...), dim3 grid, int threads, int room
 // whole numbers, exact in 16 bits; the scale is applied once a group, in 32 bits). Where there
 // are few tiles `split` warps share one and go through k in turn; their sums are joined in order
 // through shared memory.
-// 8 rows x 4,096 x 65,536, bf16, groups of 128: 41.6 us for 139 MB (3.3 TB/s), issue slots 61%
+// 8 rows x 4,096 x 65,536, bf16, groups of 128: 36 us for 139 MB (3.9 TB/s), issue slots 60%
 // taken; 61 tokens over 128 experts (2,048 x 768 x 3, f16, groups of 64 with zeros): 45 us a
 // product on average, 68 with one load of x a step ahead and passes of eight rows.
 // ---------------------------------------------------------------------------
