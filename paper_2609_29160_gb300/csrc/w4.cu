@@ -522,8 +522,9 @@ __global__ void __launch_bounds__(kRowThreads) k_split(const float* x, int64_t x
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kRowThreads / 32; ++i) top = fmaxf(top, part[i]);
-  // (bounded, so that both powers are numbers)
-  const int ex = min(max((int)(__float_as_uint(top) >> 23), 30), 250);       // 127 + exponent
+  // (from the least with which both powers are normal numbers: smaller rows end lower, with a step
+  // that is below the smallest float; the largest float's needs no bound)
+  const int ex = max((int)(__float_as_uint(top) >> 23), 15);                 // 127 + exponent
   const float by = __uint_as_float((uint32_t)(254 + 14 - ex) << 23);
   if (threadIdx.x == 0) back[t] = __uint_as_float((uint32_t)(ex - 14) << 23);
   for (int i = threadIdx.x; i < k; i += kRowThreads) {
