@@ -501,10 +501,13 @@ cudaError_t launch_rows(int dtype, int scale_dtype, int group, const ProductArgs
 // ---------------------------------------------------------------------------
 // Rows in 32 bits: each is two rows of halves, which times codes (whole numbers, exact as
 // halves too) give exact products. The first half has the row's elements over a power of two
-// that puts the largest at 2^14 to 2^15, the second what that leaves of them: 22 bits
-// together of elements down to 2^-28 of the largest.
+// that puts the largest at 2^14 to 2^15, the second what that leaves of them, 2^kSecond times
+// (at most 2^3 in the first's steps, so it has room for 2^11 of them): 22 bits together of elements down
+// to 2^-28 of the largest, as the second's least step is then 2^-35. With both at one power it
+// was 2^-24, and bits went from 2^-17 of the largest on.
 // ---------------------------------------------------------------------------
 constexpr int kRowThreads = 256;
+constexpr int kSecond = 11;
 
 __global__ void __launch_bounds__(kRowThreads) k_split(const float* x, int64_t x_row, int k, int n_rows,
                                                        __half* to, float* back) {
@@ -531,7 +534,8 @@ __global__ void __launch_bounds__(kRowThreads) k_split(const float* x, int64_t x
     const float v = from[i] * by;
     const __half hi = __float2half_rn(v);
     to[t * k + i] = hi;
-    to[(n_rows + t) * k + i] = __float2half_rn(fabsf(v) < INFINITY ? v - __half2float(hi) : 0.f);
+    to[(n_rows + t) * k + i] =
+        __float2half_rn(fabsf(v) < INFINITY ? (v - __half2float(hi)) * (float)(1 << kSecond) : 0.f);
   }
 }
 // both [2 n_rows][n] to y [n_rows][n], or [n_rows][n / 2] of a gated matrix
@@ -542,8 +546,9 @@ __global__ void __launch_bounds__(kRowThreads) k_whole_rows(const float* both, c
   if (i >= wide) return;
   const float *hi = both + t * n, *lo = both + (n_rows + t) * n;
   const float f = back[t];
-  float a = (hi[i] + lo[i]) * f;
-  if (join) a = gated(a, (hi[wide + i] + lo[wide + i]) * f);
+  constexpr float second = 1.f / (1 << kSecond);
+  float a = fmaf(lo[i], second, hi[i]) * f;
+  if (join) a = gated(a, fmaf(lo[wide + i], second, hi[wide + i]) * f);
   y[t * y_row + i] = a;
 }
 

@@ -52,3 +52,30 @@ def test_rows_of_the_smallest_numbers(tre, t, dtype):
     x = x * torch.tensor([1e-30, 1e-34, 1e-36, 1e-37, 1e-38, 1e-39, 1e-40, 1e-42], device="cuda").repeat(t // 8)[:, None]
     got = tre.tre_linear4(x, w)
     R.near(got, *R.product(x, m))
+
+
+@pytest.mark.parametrize("t", [6, 102])
+@pytest.mark.parametrize("below", [12, 17, 20, 24, 27])
+def test_small_elements_beside_a_large_one(tre, t, below):
+    """Elements of 2^-below of a row's largest, whose code is its zero, keep 22 bits: the bound
+    is of their own size, as the large one has no part in the result."""
+    codes, scales, z, m = R.matrix4(None, 96, 256, 64, torch.bfloat16, False, 9)
+    at = 37                                            # (the odd elements are the upper half bytes)
+    codes[:, at // 2] = (codes[:, at // 2] & 15) | 8 << 4
+    m[:, at] = 0
+    w = tre.Weights4(codes, scales)
+    g = torch.Generator(device="cuda").manual_seed(below)
+    x = (torch.rand(t, 256, generator=g, device="cuda") + 1) * 2.0 ** -below
+    x = x * (torch.randint(0, 2, x.shape, generator=g, device="cuda") * 2 - 1)
+    x[:, at] = torch.rand(t, generator=g, device="cuda") * 0.99 + 1
+    size = x.double().abs() @ m.abs().T
+    # 2^-22 of each element; R.product's bound is of the same sizes
+    y, off = R.product(x, m)
+    R.near(tre.tre_linear4(x, w), y, off + 2.0 ** -22 * size)
+    # one element alone: no sum hides its bits
+    one = torch.zeros_like(x)
+    one[:, at] = x[:, at]
+    one[:, 5] = x[:, 5]
+    want = one.double() @ m.T
+    off = want.abs() * (2.0 ** -22 + 4 * 2.0 ** -24)      # its bits; product, scale, both halves' sum, the power
+    R.near(tre.tre_linear4(one, w), want, off)
