@@ -375,7 +375,7 @@ __device__ __forceinline__ void few_rows(const ProductArgs& p, const Slot& slot,
         a += sums(first + k)[col][r];
         if (joined) u += sums(first + k)[col][16 + r];
       }
-      if (joined) a = gated(a, u);
+      if (joined) a = gated<true>(a, u);
       const int64_t row = slot.start + from + col;
       if (p.y_f32) reinterpret_cast<float*>(p.y)[row * p.y_row + n] = a;
       else reinterpret_cast<T*>(p.y)[row * p.y_row + n] = T(a);
@@ -548,7 +548,7 @@ __global__ void __launch_bounds__(kRowThreads) k_whole_rows(const float* both, c
   const float f = back[t];
   constexpr float second = 1.f / (1 << kSecond);
   float a = fmaf(lo[i], second, hi[i]) * f;
-  if (join) a = gated(a, fmaf(lo[wide + i], second, hi[wide + i]) * f);
+  if (join) a = gated<false>(a, fmaf(lo[wide + i], second, hi[wide + i]) * f);
   y[t * y_row + i] = a;
 }
 

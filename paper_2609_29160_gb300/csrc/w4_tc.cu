@@ -197,7 +197,7 @@ __device__ __forceinline__ void write_rows(const ProductArgs& p, const Unit& u, 
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float other = __shfl_xor_sync(0xffffffffu, gate ? acc[c + 8 + e] : acc[c + e], 16);
-        v[e] = gated(gate ? acc[c + e] : other, gate ? other : acc[c + 8 + e]);
+        v[e] = gated<true>(gate ? acc[c + e] : other, gate ? other : acc[c + 8 + e]);
       }
       *reinterpret_cast<uint4*>(place(at, gate ? 0 : 1)) = Vec<T>::put(v);
     } else {
