@@ -282,7 +282,8 @@ __device__ __forceinline__ double sigmoid_of(double x) { return 1.0 / (1.0 + exp
 // How far a c in 32 bits may be off, both sides of a comparison. The quick exponential is off by
 // (2 + 1.2 |x|) units of 2^-23 of itself, which reach a sigmoid by s (1 - s): less than 1e-7 in
 // all; its sum and quotient add 3 units of 2^-24 of s, the bias half a unit of c. A softmax's sum
-// of up to 1,024 terms adds a unit for each of its 10 levels.
+// of up to 1,024 terms adds a unit for each of its 10 levels. A group's sum of two is off by twice
+// that and, as each c and the sum are rounded, by a unit of 2^-23 of what both c are in size.
 constexpr float kOffSigmoid = 7e-7f, kOffSoftmax = 3e-6f, kOffBias = 2.5e-7f;
 
 // c of expert j * 32 + lane
@@ -332,61 +333,70 @@ template <class F> __device__ __forceinline__ void keep_two(F x, F& first, F& se
   }
 }
 
-// Lane g's return: what group g counts as.
+// Lane g's return: what group g counts as. size: of what that is the sum of (its error is theirs,
+// which may be far larger than the sum).
 template <int NV>
-__device__ __forceinline__ float group_scores(const RouteArgs& a, const float* c, float* room) {
+__device__ __forceinline__ float group_scores(const RouteArgs& a, const float* c, float* room, float& size) {
   const int lane = threadIdx.x & 31;
   const float none = -INFINITY;
-  float mine = none, first = none, second = none;
+  float first = none, second = none, best = none, next = none;   // best, next: of this lane's group
+  auto take = [&](int g, float x, float y) {
+    if (lane == g) {
+      best = x;
+      next = y;
+    }
+  };
   if (a.per == 32) {                                 // a group a register
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      float sum = warp_max(c[j]);
+      const float x = warp_max(c[j]);
+      float y = none;
       if (a.group_best == 2) {
-        const int who = __ffs(__ballot_sync(0xffffffffu, c[j] == sum)) - 1;
-        const float next = warp_max(lane == who ? none : c[j]);
-        if (next > none) sum += next;
+        const int who = __ffs(__ballot_sync(0xffffffffu, c[j] == x)) - 1;
+        y = warp_max(lane == who ? none : c[j]);
       }
-      if (lane == j) mine = sum;
+      take(j, x, y);                                 // (registers past the last group have -inf)
     }
-    return lane < a.groups ? mine : none;
-  }
-  if (a.per % 32 == 0) {                             // groups of whole registers
+  } else if (a.per % 32 == 0) {                      // groups of whole registers
     const int regs = a.per / 32;
     int left = regs, g = 0;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       keep_two(c[j], first, second);
       if (--left == 0) {
-        float sum = warp_max(first);
+        const float x = warp_max(first);
+        float y = none;
         if (a.group_best == 2) {
-          const int who = __ffs(__ballot_sync(0xffffffffu, first == sum)) - 1;
-          const float next = warp_max(lane == who ? second : first);
-          if (next > none) sum += next;
+          const int who = __ffs(__ballot_sync(0xffffffffu, first == x)) - 1;
+          y = warp_max(lane == who ? second : first);
         }
-        if (lane == g) mine = sum;
+        take(g, x, y);
         ++g;
         left = regs;
         first = second = none;
       }
     }
-    return mine;
-  }
+  } else {
 #pragma unroll
-  for (int j = 0; j < NV; ++j)
-    if (j * 32 + lane < a.experts) room[j * 32 + lane] = c[j];
-  __syncwarp();
-  if (lane < a.groups) {
-    int i = lane % a.per;                            // (lanes start apart: their banks)
-    for (int n = 0; n < a.per; ++n) {
-      keep_two(room[lane * a.per + i], first, second);
-      if (++i == a.per) i = 0;
+    for (int j = 0; j < NV; ++j)
+      if (j * 32 + lane < a.experts) room[j * 32 + lane] = c[j];
+    __syncwarp();
+    if (lane < a.groups) {
+      int i = lane % a.per;                          // (lanes start apart: their banks)
+      for (int n = 0; n < a.per; ++n) {
+        keep_two(room[lane * a.per + i], best, next);
+        if (++i == a.per) i = 0;
+      }
+      if (a.group_best == 1) next = none;
     }
-    mine = first;
-    if (a.group_best == 2 && second > none) mine += second;
+    __syncwarp();
   }
-  __syncwarp();
-  return mine;
+  size = best > none ? fabsf(best) : 0.f;
+  if (next > none) {
+    best += next;
+    size += fabsf(next);
+  }
+  return best;
 }
 // The same in 64 bits, of keys.
 __device__ __forceinline__ uint64_t group_scores(const RouteArgs& a, const uint64_t* room) {
@@ -527,11 +537,12 @@ __device__ __forceinline__ Choice choose(const RouteArgs& a, int64_t row, const 
   all_scores<float, NV>(a, l, most, total, c);
   const float off = a.raw ? 0.f : a.softmax ? kOffSoftmax : kOffSigmoid, rel = a.raw ? 0.f : kOffBias;
   if (a.groups > 1) {
-    float last = 0.f, next = 0.f;
-    const unsigned kept =
-        kept_groups(a, group_scores<NV>(a, c, reinterpret_cast<float*>(room)), last, next);
+    float last = 0.f, next = 0.f, size;
+    const float value = group_scores<NV>(a, c, reinterpret_cast<float*>(room), size);
+    const unsigned kept = kept_groups(a, value, last, next);
     only_kept<NV>(a, kept, (float)-INFINITY, c);
-    const bool unsure = next > -INFINITY && !(last - next > 2.f * off + rel * (fabsf(last) + 1.f));
+    // (of the largest group: others than these two may be further off than they are apart)
+    const bool unsure = next > -INFINITY && !(last - next > 2.f * off + rel * warp_max(size));
     if (off > 0.f && unsure)
       return Choice{choose_double<NV>(a, row, most, room), lane};
   }
