@@ -689,8 +689,9 @@ tre_status tre_block_norm(const tre_block_rows* rows, tre_stream stream);
  * in them, largest first, -1 where fewer are there (an expert whose c is -inf or
  * NaN is not); weights [n_rows][top] float: their s (of c only the choice depends
  * on the bias), divided by their sum if renorm, times scale; 0 beside an id of -1.
- * Ties go to the lower index. Choices are those of the formulas in 64 bits or more,
- * weights are computed in 32. */
+ * Ties go to the lower index. Choices are those of the formulas in 64 bits (of experts
+ * without a bias by their logits, which tell scores apart however close), weights are
+ * computed in 32. */
 typedef enum { TRE_SOFTMAX = 0, TRE_SIGMOID = 1 } tre_scores;
 typedef struct {
   tre_dtype dtype;

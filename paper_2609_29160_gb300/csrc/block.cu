@@ -181,12 +181,13 @@ bool on(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % byte
 //
 // A warp a token, a lane every 32nd expert. Choices have to be those of the formulas, not of
 // their rounding, because one other expert is another answer. Where c grows with the logit
-// (no bias, no sums) the logits themselves are compared. Else c is computed in 32 bits. Where
+// (no bias) the logits themselves are compared: scores that 64 bits round to the same number
+// are not equal. Else, and for sums of groups, c is computed in 32 bits. Where
 // two that follow each other in the choice are closer than 32 bits can tell (one row in some
 // hundred of 256 sigmoid scores), the candidates get theirs in 64 bits, a lane each, and are put in
 // that order; where a kept group is that close to one that is not (one row in 100,000), or there
-// are too many candidates, the whole row is done in 64 bits, whose pipe is some sixty times
-// slower.
+// are too many candidates, the whole row's groups or choice are done in 64 bits, whose pipe is some
+// sixty times slower.
 //
 // Candidates: the top-th largest of the lanes' own maxima is not above the top-th largest of all,
 // so that what is not below it (some ten to fifteen of 256 for the best eight) has the chosen in
@@ -485,30 +486,42 @@ __device__ __forceinline__ F softmax_total(const float* l, float most) {
   return warp_sum(sum);
 }
 
-// Lane i's return is the i-th expert of the whole row in 64 bits (-1: none).
+// A lane's c of the whole row in 64 bits, by their keys.
 template <int NV>
-__device__ __noinline__ int choose_double(const RouteArgs& a, int64_t row, float most, uint64_t* room) {
+__device__ __forceinline__ void double_scores(const RouteArgs& a, int64_t row, float most, uint64_t* c) {
+  const int lane = threadIdx.x & 31;
+  const uint64_t none = order(-(double)INFINITY);
+  float l[NV];
+  row_logits<NV>(a, row, l);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) l[j] = sane(l[j]);
+  const double total = a.softmax ? softmax_total<double, NV>(l, most) : 1.0;
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+    c[j] = j * 32 + lane < a.experts ? order(score(a, l[j], most, total, j * 32 + lane)) : none;
+}
+// The groups that stay, by them.
+template <int NV>
+__device__ __noinline__ unsigned kept_double(const RouteArgs& a, int64_t row, float most, uint64_t* room) {
+  const int lane = threadIdx.x & 31;
+  uint64_t c[NV];
+  double_scores<NV>(a, row, most, c);
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+    if (j * 32 + lane < a.experts) room[j * 32 + lane] = c[j];
+  __syncwarp();
+  const unsigned kept = kept_groups(a, group_scores(a, room));
+  __syncwarp();
+  return kept;
+}
+// Lane i's return is the i-th expert of the groups that stay (-1: none).
+template <int NV>
+__device__ __noinline__ int choose_double(const RouteArgs& a, int64_t row, float most, unsigned kept) {
   const int lane = threadIdx.x & 31;
   const uint64_t none = order(-(double)INFINITY);
   uint64_t c[NV];
-  {
-    float l[NV];
-    row_logits<NV>(a, row, l);
-#pragma unroll
-    for (int j = 0; j < NV; ++j) l[j] = sane(l[j]);
-    const double total = a.softmax ? softmax_total<double, NV>(l, most) : 1.0;
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-      c[j] = j * 32 + lane < a.experts ? order(score(a, l[j], most, total, j * 32 + lane)) : none;
-  }
-  if (a.groups > 1) {
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (j * 32 + lane < a.experts) room[j * 32 + lane] = c[j];
-    __syncwarp();
-    only_kept<NV>(a, kept_groups(a, group_scores(a, room)), none, c);
-    __syncwarp();
-  }
+  double_scores<NV>(a, row, most, c);
+  if (a.groups > 1) only_kept<NV>(a, kept, none, c);
   int mine = -1;
   for (int k = 0; k < a.top; ++k) {
     int at;
@@ -535,16 +548,21 @@ __device__ __forceinline__ Choice choose(const RouteArgs& a, int64_t row, const 
   float c[NV];
   const float total = a.softmax && !a.raw ? softmax_total<float, NV>(l, most) : 1.f;
   all_scores<float, NV>(a, l, most, total, c);
-  const float off = a.raw ? 0.f : a.softmax ? kOffSoftmax : kOffSigmoid, rel = a.raw ? 0.f : kOffBias;
+  float off = a.raw ? 0.f : a.softmax ? kOffSoftmax : kOffSigmoid, rel = a.raw ? 0.f : kOffBias;
+  unsigned kept = 0;
   if (a.groups > 1) {
     float last = 0.f, next = 0.f, size;
     const float value = group_scores<NV>(a, c, reinterpret_cast<float*>(room), size);
-    const unsigned kept = kept_groups(a, value, last, next);
-    only_kept<NV>(a, kept, (float)-INFINITY, c);
+    kept = kept_groups(a, value, last, next);
     // (of the largest group: others than these two may be further off than they are apart)
     const bool unsure = next > -INFINITY && !(last - next > 2.f * off + rel * warp_max(size));
-    if (off > 0.f && unsure)
-      return Choice{choose_double<NV>(a, row, most, room), lane};
+    if (off > 0.f && unsure) kept = kept_double<NV>(a, row, most, room);
+    if (!a.bias && !a.raw) {                         // in the groups that stay it is the logits
+#pragma unroll
+      for (int j = 0; j < NV; ++j) c[j] = l[j] + 0.f;
+      off = rel = 0.f;
+    }
+    only_kept<NV>(a, kept, (float)-INFINITY, c);
   }
   // the top-th largest of the lanes' maxima, and what 32 bits cannot tell from it
   float own = c[0];
@@ -572,7 +590,7 @@ __device__ __forceinline__ Choice choose(const RouteArgs& a, int64_t row, const 
   __syncwarp();
   Choice mine{-1, 32};
   if (count > 32) {                                  // many equal ones, or few lanes that have any
-    if (off > 0.f) return Choice{choose_double<NV>(a, row, most, room), lane};
+    if (off > 0.f) return Choice{choose_double<NV>(a, row, most, kept), lane};
     for (int k = 0; k < a.top; ++k) {
       int at;
       if (!(take_best<NV>(c, (float)-INFINITY, at) > -INFINITY)) break;

@@ -61,3 +61,17 @@ def test_one_group_of_large_biases(tre):
     bias[0:8] = torch.tensor([5e4] + [-5e4] * 7, device="cuda")
     near = closest(x, "sigmoid", bias, 4, 2, 1500)
     check(tre, near, 3, scores="sigmoid", bias=bias, groups=4, top_groups=2, group_best=2)
+
+
+@pytest.mark.parametrize("scores", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("experts,groups", [(64, 8), (256, 8), (96, 4), (1024, 16)])
+def test_choices_go_by_logits_without_a_bias(tre, scores, experts, groups):
+    """Scores that 64 bits round to the same number are as different as their logits."""
+    x = logits(60, experts, 6)
+    x[:20] = x[:20].abs() * 9 + 38                        # sigmoids of 1, less than 2^-54
+    x[20:40, ::3] += 60
+    x[40:50] *= 700                                       # softmax scores of 0
+    x[50:] = x[50:] * 40 - 200
+    for top, best in ((4, 2), (8, 2), (8, 1), (24, 2)):
+        check(tre, x, top, scores=scores, groups=groups, top_groups=groups // 2, group_best=best, renorm=False)
+    check(tre, x[:40], 6, scores=scores, groups=groups, top_groups=groups // 2, group_best=2)
