@@ -192,9 +192,10 @@ bool on(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % byte
 // Candidates: the top-th largest of the lanes' own maxima is not above the top-th largest of all,
 // so that what is not below it (some ten to fifteen of 256 for the best eight) has the chosen in
 // it. They go to a lane each, which counts how many come before. Taking the best out one after
-// the other took 100 instructions each, 1.45 us for 16,384 rows. Bound by instructions, some 900
-// for a row of 256 sigmoid scores with a bias in groups: 16,384 rows 22 us, 12 without bias and
-// groups.
+// the other took 100 instructions each, 1.45 us for 16,384 rows. Where they are more than the lanes
+// (one row in some hundred at the best 16, one in five at 20, nearly all from 24 on) a higher bound is
+// looked for by halves. Bound by instructions, some 900 for a row of 256 sigmoid scores with a bias in
+// groups: 16,384 rows 19 us, 11 without bias and groups, 32 for the best 32 with a bias.
 // ---------------------------------------------------------------------------
 struct RouteArgs {
   const uint8_t* logits;
@@ -565,31 +566,63 @@ __device__ __forceinline__ Choice choose(const RouteArgs& a, int64_t row, const 
     only_kept<NV>(a, kept, (float)-INFINITY, c);
   }
   // the top-th largest of the lanes' maxima, and what 32 bits cannot tell from it
+  constexpr float kLeast = -3.402823466e38f;
   float own = c[0];
 #pragma unroll
   for (int j = 1; j < NV; ++j) own = fmaxf(own, c[j]);
-  float least = -INFINITY;
+  float bound = -INFINITY, best = own;
   for (int k = 0; k < a.top; ++k) {
-    least = warp_max(own);
-    if (own == least) own = -INFINITY;               // (all that are equal: the bound is then lower)
+    bound = warp_max(own);
+    if (own == bound) own = -INFINITY;               // (all that are equal: the bound is then lower)
   }
-  least -= off + rel * fabsf(least);
-  if (!(least > -3.402823466e38f)) least = -3.402823466e38f;     // (also what infinities make of it)
-  int count = 0;
+  bound = fmaxf(bound, kLeast);
+  auto below = [&](float x) {
+    const float least = x - (off + rel * fabsf(x));
+    return least > kLeast ? least : kLeast;          // (also what infinities make of it)
+  };
+  // Those not below it (not -inf), a place each of the first 32; how many
+  auto list = [&](float least) {
+    int count = 0;
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const bool in = c[j] >= least;                   // (not -inf)
-    const unsigned all = __ballot_sync(0xffffffffu, in);
-    const int at = count + __popc(all & ((1u << lane) - 1));
-    if (in && at < 32) {
-      near.c[at] = c[j];
-      near.expert[at] = j * 32 + lane;
+    for (int j = 0; j < NV; ++j) {
+      const bool in = c[j] >= least;
+      const unsigned all = __ballot_sync(0xffffffffu, in);
+      const int at = count + __popc(all & ((1u << lane) - 1));
+      if (in && at < 32) {
+        near.c[at] = c[j];
+        near.expert[at] = j * 32 + lane;
+      }
+      count += __popc(all);
     }
-    count += __popc(all);
-  }
-  __syncwarp();
+    __syncwarp();
+    return count;
+  };
+  int count = list(below(bound));
   Choice mine{-1, 32};
-  if (count > 32) {                                  // many equal ones, or few lanes that have any
+  if (count > 32) {
+    // more than lanes (`top` near their number, or many equal ones): a higher bound that has `top` of
+    // them not below it, by halves between this one and the largest
+    auto many = [&](float least) {
+      int n = 0;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) n += c[j] >= least;
+      return (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
+    };
+    best = warp_max(best);
+    uint32_t low = order(bound), high = order(best) + 1;
+    while (high - low > 1) {
+      const uint32_t mid = low + (high - low) / 2;
+      const float x = value_of(mid);
+      if (many(x) < a.top) {
+        high = mid;
+        continue;
+      }
+      low = mid;
+      if (many(below(x)) <= 32) break;
+    }
+    count = list(below(value_of(low)));
+  }
+  if (count > 32) {                                  // many equal ones, or closer than 32 bits tell
     if (off > 0.f) return Choice{choose_double<NV>(a, row, most, kept), lane};
     for (int k = 0; k < a.top; ++k) {
       int at;

@@ -75,3 +75,39 @@ def test_choices_go_by_logits_without_a_bias(tre, scores, experts, groups):
     for top, best in ((4, 2), (8, 2), (8, 1), (24, 2)):
         check(tre, x, top, scores=scores, groups=groups, top_groups=groups // 2, group_best=best, renorm=False)
     check(tre, x[:40], 6, scores=scores, groups=groups, top_groups=groups // 2, group_best=2)
+
+
+@pytest.mark.parametrize("top", [11, 16, 20, 24, 31, 32])
+@pytest.mark.parametrize("experts", [33, 64, 200, 256, 512, 1024])
+def test_many_of_them(tre, experts, top):
+    """More candidates than lanes: every kind of choice, with logits that repeat and that do not."""
+    bias = 0.1 * torch.randn(experts, generator=torch.Generator(device="cuda").manual_seed(7), device="cuda")
+    x = logits(50, experts, top)
+    x[20:30] = x[20:30].bfloat16().float()
+    x[30:35] = (2 * x[30:35]).round() / 2
+    x[35] = 0
+    x[36, 5:] = -float("inf")
+    x[37:40, ::2] = -float("inf")
+    x[40:45] *= 30
+    for scores in ("softmax", "sigmoid"):
+        check(tre, x, top, scores=scores)
+        check(tre, x, top, scores=scores, bias=bias)
+        check(tre, x, top, scores=scores, bias=bias + 100)
+        if experts % 8 == 0:
+            for best in (1, 2):
+                check(tre, x, top, scores=scores, bias=bias, groups=8, top_groups=4, group_best=best)
+                check(tre, x, top, scores=scores, groups=8, top_groups=4, group_best=best)
+
+
+@pytest.mark.parametrize("gap", [0.0, 1e-9, 3e-8, 1e-6])
+def test_many_of_them_close_to_each_other(tre, gap):
+    """As many equal or nearly equal c as there are lanes and more, around the last that is chosen."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    for experts in (64, 256, 1024):
+        x = logits(12, experts, 9)
+        s = torch.sigmoid(x.double())
+        bias = (0.7 - s[0] + gap * torch.randn(experts, generator=g, device="cuda").double()).float()
+        bias[::7] += 0.2
+        for top in (12, 24, 32):
+            check(tre, x[:1], top, scores="sigmoid", bias=bias)
+            check(tre, x, top, scores="sigmoid", bias=bias)
