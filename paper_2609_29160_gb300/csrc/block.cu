@@ -13,8 +13,8 @@ namespace {
 //
 // One pass: a row's elements of y and of the residual stay in registers between the two
 // sums (mean of squares of y, where there is a post norm, and of r), so that each input is
-// read once and each output written once; 16 elements a thread and as many threads as a row then
-// has. Bound by HBM where there are rows enough: 20,011 rows of 5,120, bfloat16 beside a 32-bit
+// read once and each output written once; 8, 16 or 32 elements a thread: a warp has rows of up to 1,024,
+// a block of up to 512 threads the others. Bound by HBM where there are rows enough: 20,011 rows of 5,120, bfloat16 beside a 32-bit
 // stream, both norms and a gate: 193 us for 1.18 GB, 6.1 TB/s.
 // ---------------------------------------------------------------------------
 struct BlockArgs {
@@ -45,10 +45,13 @@ template <class T> __device__ __forceinline__ void put8(T* p, const float* x) {
 }
 
 // A thread's elements of a row: V times eight, next to each other with WIDE, else a row's
-// threads apart.
-template <int V, bool WIDE> struct Mine {
-  int t, step, dim;
+// threads apart: `per_row`, or STEP of them where that is known, so that 32 elements' addresses are one
+// and constants. (Kept in registers they went past 128 and to memory: 20,000 rows of 1,001 bfloat16
+// 109 us, 51 so; 4,000 of 16,383 444, 230 so.)
+template <int V, bool WIDE, int STEP> struct Mine {
+  int t, per_row, dim;
   __device__ __forceinline__ int at(int v, int e) const {
+    const int step = STEP ? STEP : per_row;
     return WIDE ? (v * step + t) * 8 + e : (v * 8 + e) * step + t;
   }
   template <class T> __device__ __forceinline__ void get(const T* p, float* x) const {
@@ -97,25 +100,25 @@ template <class T, int N, class M>
 __device__ __forceinline__ void times_weight(const BlockArgs& a, const uint8_t* w, const M& mine,
                                              float by, float* x) {
   float f[N];
-  if (a.weight_f32) mine.get(reinterpret_cast<const float*>(w), f);
+  if (std::is_same<T, float>::value || a.weight_f32) mine.get(reinterpret_cast<const float*>(w), f);
   else mine.get(reinterpret_cast<const T*>(w), f);
 #pragma unroll
   for (int e = 0; e < N; ++e) x[e] = x[e] * by * f[e];
 }
 
-template <class T, class S, int V, bool WIDE>
+template <class T, class S, int V, bool WIDE, int STEP>
 __global__ void __launch_bounds__(512) k_block_norm(const __grid_constant__ BlockArgs a) {
   constexpr int N = 8 * V;
   __shared__ float part[2][32];
   const bool block = a.per_row > 32;
   const int64_t row = block ? blockIdx.x : (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
   if (row >= a.n_rows) return;                       // (whole warps, of rows of their own)
-  const Mine<V, WIDE> mine{block ? (int)threadIdx.x : (int)(threadIdx.x & 31), a.per_row, a.dim};
+  const Mine<V, WIDE, STEP> mine{block ? (int)threadIdx.x : (int)(threadIdx.x & 31), a.per_row, a.dim};
   float r[N];
   mine.get(reinterpret_cast<const S*>(a.residual) + row * a.residual_row, r);
   if (a.y) {
     float y[N];
-    if (a.y_f32) mine.get(reinterpret_cast<const float*>(a.y) + row * a.y_row, y);
+    if (std::is_same<T, float>::value || a.y_f32) mine.get(reinterpret_cast<const float*>(a.y) + row * a.y_row, y);
     else mine.get(reinterpret_cast<const T*>(a.y) + row * a.y_row, y);
     if (a.post_weight) {
       float sum = 0.f;
@@ -147,7 +150,7 @@ __global__ void __launch_bounds__(512) k_block_norm(const __grid_constant__ Bloc
   for (int e = 0; e < N; ++e) sum = fmaf(r[e], r[e], sum);
   sum = row_sum(sum, block, part[1]);
   times_weight<T, N>(a, a.weight, mine, rsqrtf(sum / a.dim + a.eps), r);
-  if (a.out_f32) mine.put(reinterpret_cast<float*>(a.out) + row * a.out_row, r);
+  if (std::is_same<T, float>::value || a.out_f32) mine.put(reinterpret_cast<float*>(a.out) + row * a.out_row, r);
   else mine.put(reinterpret_cast<T*>(a.out) + row * a.out_row, r);
 }
 
@@ -158,13 +161,15 @@ cudaError_t launch_norm(BlockArgs a, cudaStream_t s) {
   const int eights = (a.dim + 7) / 8;
   const int v = eights <= 32 ? 1 : eights <= 64 ? 2 : eights <= 128 ? 4 : eights <= 512 ? 1 : eights <= 1024 ? 2 : 4;
   a.per_row = ((eights + v - 1) / v + 31) / 32 * 32;
+  if (!WIDE && v == 4 && a.per_row > 32) a.per_row = 512;
   const bool block = a.per_row > 32;
   const int threads = block ? a.per_row : 128;
   const int64_t blocks = block ? a.n_rows : ((int64_t)a.n_rows + 3) / 4;
   const unsigned grid = (unsigned)blocks;
-  if (v == 1) k_block_norm<T, S, 1, WIDE><<<grid, threads, 0, s>>>(a);
-  else if (v == 2) k_block_norm<T, S, 2, WIDE><<<grid, threads, 0, s>>>(a);
-  else k_block_norm<T, S, 4, WIDE><<<grid, threads, 0, s>>>(a);
+  if (v == 1) k_block_norm<T, S, 1, WIDE, 0><<<grid, threads, 0, s>>>(a);
+  else if (v == 2) k_block_norm<T, S, 2, WIDE, 0><<<grid, threads, 0, s>>>(a);
+  else if (block) k_block_norm<T, S, 4, WIDE, WIDE ? 0 : 512><<<grid, threads, 0, s>>>(a);
+  else k_block_norm<T, S, 4, WIDE, WIDE ? 0 : 32><<<grid, threads, 0, s>>>(a);
   return cudaGetLastError();
 }
 
