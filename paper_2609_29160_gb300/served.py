@@ -58,7 +58,7 @@ class Replica:
             for w in self.layers:
                 w["qkv"], w["out"] = in_four_bits(w["qkv"].T.contiguous()), in_four_bits(w["out"].T.contiguous())
                 w["norm"], w["ff_norm"] = 1 + weight(width, scale=0.1), 1 + weight(width, scale=0.1)
-                w["router"] = weight(width, experts, scale=width ** -0.5)
+                w["router"] = weight(width, experts, scale=width ** -0.5).float()
                 w["up"] = in_four_bits(weight(experts, 2 * width, width, scale=width ** -0.5), gated=True)
                 w["down"] = in_four_bits(weight(experts, width, width, scale=width ** -0.5))
             self.norm = 1 + weight(width, scale=0.1)
@@ -91,7 +91,8 @@ class Replica:
             x, n = tre.tre_block_norm(x, y, weight=w["norm"])
             y = self.attention(w, tre.tre_linear4(n, w["qkv"], diag=self.diag), batch)
             x, n = tre.tre_block_norm(x, tre.tre_linear4(y, w["out"], diag=self.diag), weight=w["ff_norm"])
-            ids, weights = tre.tre_route((n @ w["router"]).float(), self.top)
+            # (in 32 bits: with logits of 16, experts that differ would tie and go by their number)
+            ids, weights = tre.tre_route(n.float() @ w["router"], self.top)
             y = tre.tre_experts(n, ids, weights, w["up"], w["down"], diag=self.diag)
         return tre.tre_block_norm(x, y, weight=self.norm)[1]
 
