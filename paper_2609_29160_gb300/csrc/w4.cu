@@ -4,6 +4,7 @@
 
 #include "internal.h"
 #include "w4.cuh"
+#include "w4_rule.h"
 
 namespace tre {
 namespace {
@@ -473,25 +474,9 @@ cudaError_t launch_few(int dtype, int scale_dtype, int group, const ProductArgs&
                                  : few_by_columns<__half, __half>(group, p, s);
 }
 
-// Whether k_w4_few takes less than the tensor cores' kernel, by what both measured: it 5 us and
-// 0.31, 0.48, 0.72 or 0.79 us for each MB of codes and pass of 8, 16, 24 or 32 rows; the other
-// 8 us and 0.28 us for each 64 elements of k and round of its units (0.38 with groups of 64, 0.75
-// with 32). E.g.
-// 16,384 x 4,096, groups of 128: 21 against 25 us for 16 rows, 31 against 25 for 32; 4,096 x
-// 4,096: 13 against 25 for 32 rows, 27 against 25 for 96.
-bool few_is_quicker(const ProductArgs& p, int group) {
-  if (p.n_rows <= 8) return true;
-  if (p.n_rows > 96) return false;
-  const float mb = p.w.tiles * 8.f * p.w.chunks * 64.f * 1e-6f;
-  const float pass = p.n_rows <= 16 ? 0.48f : p.n_rows <= 24 ? 0.72f : 0.79f;
-  const int pairs = std::max(1, device_sm_count() / 2);
-  const int rounds = ((p.w.tiles + 15) / 16 + pairs - 1) / pairs;
-  return 5.f + mb * pass * ((p.n_rows + 31) / 32) <= 8.f + rounds * p.w.chunks * (group == 32 ? 0.75f : group == 64 ? 0.38f : 0.28f);
-}
-
 cudaError_t launch_rows(int dtype, int scale_dtype, int group, const ProductArgs& p, tre_diag* diag,
                         cudaStream_t s) {
-  if (!few_is_quicker(p, group)) {
+  if (!few_is_quicker(p.n_rows, p.w.tiles, p.w.chunks, group, device_sm_count())) {
     const cudaError_t e = launch_w4_tc(dtype, scale_dtype, group, p, p.n_rows, 0, diag, s);
     if (e != cudaErrorNotSupported) return e;
   }
@@ -559,6 +544,10 @@ constexpr int kPlanThreads = 1024, kMaxExperts = 1024;
 // Tokens an expert up to which k_w4_few is taken. 64 experts of 2,048 x 1,024 x 3, groups of 128,
 // 12 tokens each: 98 us by it, 121 by the tensor cores' kernel, 16 each 124 and 124, 32 each 184 and
 // 126; groups of 64, 24 each: 170 and 176; groups of 32, 32 each: 208 and 290, 48 each 286 and 292.
+// It is the mean that counts: an expert that gets most of them is done in pieces of 16 that read its codes
+// again, out of L2, and others' are not read at all. 900 tokens to 64 such experts take 99 us evenly
+// spread and 74 all to one, 15,000 to 1,024 of 512 x 256 x 3 187 and 160, 56 with two of 8 of
+// 4,096 x 14,336 x 3 each 278, and 324 with one for all of them.
 constexpr int few_tokens(int group) { return group == 32 ? 48 : group == 64 ? 24 : 15; }
 
 // Pairs (token, j) counted and sorted by expert, by one block or a cluster of eight that have a
@@ -687,7 +676,7 @@ cudaError_t launch_plan(const int32_t* ids, int64_t pairs, int experts, const Pl
 
 // Rows of tokens in the order of their places, for the tensor cores' kernel: copies that gather
 // rows there took 1,350 cycles a stage of 256 rows (by tensor copies of four rows or by pieces
-// of 16 bytes), 2.5 times its products; this pass 17 us for 24,576 rows of 2,048.
+// of 16 bytes), 2.5 times its products; this pass 20 us for 24,576 rows of 2,048.
 // A warp a row, four pieces a lane on their way.
 __global__ void __launch_bounds__(kRowThreads) k_gather(const uint4* x, int64_t x_row, int pieces, int top,
                                                         PlanArgs plan, uint4* to) {
