@@ -651,7 +651,8 @@ tre_status tre_chunk_attention(const tre_kv_cache* cache, const tre_kv_batch* ba
  *   residual_out = r                                         (NULL: not written)
  *   out          = r / sqrt(mean r^2 + eps) * weight         (out NULL: not written)
  * gate (NULL: 1) of row t, element i: gate[t * gate_row + i * gate_col]; gate_col
- * is 0 or 1. out is computed from the 32-bit r, not from its rounding. residual_out
+ * is 0 or 1. out is computed from the 32-bit r, not from its rounding; squares are
+ * summed in 32 bits (rows of elements past some 1e17 have no norm there). residual_out
  * may be residual and out may be y (of its type), with the same strides; no other
  * overlap. */
 typedef struct {
@@ -777,7 +778,8 @@ typedef struct {
  * with w1 gated and act as in tre_linear4. An id below zero adds nothing; one past
  * the last expert adds nothing and is counted in diag.dropped_range; a token
  * without experts gives zeros. The same expert may come twice. act's output is
- * rounded to dtype (an operand of the second product has no more bits), and y once. */
+ * rounded to dtype (an operand of the second product has no more bits; past float16's
+ * range it is an infinity), and y once. */
 tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* tokens, void* ws,
                        size_t* ws_bytes, tre_diag* diag, tre_stream stream);
 

@@ -910,6 +910,9 @@ tre_status tre_experts(const tre_w4* w1, const tre_w4* w2, const tre_tokens* t, 
   plan.piece = few ? 16 : pairs <= 96 * slots ? 128 : kTileTokens;
   plan.tiles = arena.take<Slot>(slots + pairs / plan.piece);
   plan.n = arena.take<int32_t>(2);
+  // act's output in 16 bits: the second product's operand has no more. Beside the output's own rounding
+  // it takes the error against 64 bits from 1.7e-3 to 2.4e-3 in bfloat16, 2.1e-4 to 3.0e-4 in half, where past
+  // 65,504 it is an infinity. As two rows, like rows in 32 bits, the second product would be done twice.
   uint8_t* h = arena.take<uint8_t>((size_t)pairs * inner_row * 2);
   const int row = (dim + 3) / 4 * 4;                  // of `each`
   float* each = arena.take<float>((size_t)pairs * row);
